@@ -275,6 +275,130 @@ malt_status_t malt_profile_read(malt_plan_t* plan, malt_profile_t* out, int32_t 
 /* Release the plan (host memory and profiling events only). */
 void malt_destroy_state(malt_plan_t* plan);
 
+/* ===========================================================================
+ * Operators of a training step around the optimizer: the token table, the
+ * distillation loss and linear layers in 8-bit floating point.  They need no
+ * plan.  Matrices are row-major with a row pitch (`ld`, in elements, >= the
+ * row's length); pointers are aligned to their element type, and rows of
+ * 16-byte-aligned start and pitch take a vectorised path.  Work is enqueued on
+ * `stream`, which must belong to the current device; nothing waits on the host
+ * and nothing is allocated.  A buffer that is written may overlap no other
+ * unless stated (MALT_ERR_ALIAS).  An empty product of sizes enqueues nothing
+ * but what the definition asks for (a gradient over no tokens is zero).
+ * ======================================================================== */
+
+typedef enum { MALT_FLOAT32 = 0, MALT_BFLOAT16 = 1 } malt_dtype_t;
+typedef enum { MALT_INT32 = 0, MALT_INT64 = 1 } malt_index_t;
+
+/* Rows of a token table:
+ *   out[t, :] = scale * table[ids[t], :]     t < tokens, `width` columns
+ * computed in float32, rounded once to out_type.  An id outside [0, vocab)
+ * stands for no token: its row is zero.
+ * Limits: tokens <= 2^25, 1 <= vocab <= 2^25, 1 <= width <= 2^20. */
+malt_status_t malt_embed_lookup(const void* ids, malt_index_t id_type, int64_t tokens, const void* table,
+                                malt_dtype_t table_type, int64_t vocab, int64_t width, int64_t table_ld, float scale,
+                                void* out, malt_dtype_t out_type, int64_t out_ld, void* stream);
+
+/* Its gradient, dense:
+ *   dtable[v, :] = (accumulate ? dtable[v, :] : 0) + scale * sum_{t: ids[t] = v} grad[t, :]
+ * Sums are float32 in an order fixed by the ids alone (tokens sorted by id,
+ * stably), so equal inputs give equal bits; rounded once to dtable_type.  With
+ * accumulate, rows without tokens are neither read nor written.
+ * workspace: device memory of malt_embed_grad_size's bytes, 256-byte aligned,
+ * of no meaning before or after the call. */
+malt_status_t malt_embed_grad_size(int64_t tokens, int64_t vocab, int64_t width, size_t* workspace_bytes);
+malt_status_t malt_embed_grad(const void* ids, malt_index_t id_type, int64_t tokens, const void* grad,
+                              malt_dtype_t grad_type, int64_t grad_ld, float scale, int32_t accumulate, void* dtable,
+                              malt_dtype_t dtable_type, int64_t vocab, int64_t width, int64_t dtable_ld,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Distillation from a teacher's top logits, labels mixed in.  For row r, with
+ * student logits z over the vocabulary, the teacher's logits a_j at ids i_j
+ * (j < n_top), label y, temperature tau:
+ *   p  = softmax(a / tau) over the row's valid entries
+ *   q  = softmax(z / tau),  q1 = softmax(z)
+ *   losses[r]  = (1 - alpha) tau^2 sum_j p_j (log p_j - log q_{i_j}) - alpha log q1_y
+ *   dlogits[r] = weight_r [ (1 - alpha) tau (q - p) + alpha (q1 - 1_y) ]
+ * (p scattered to its ids; an id named twice counts twice.)  dlogits is the
+ * gradient of sum_r weight_r losses[r].
+ *  - An id outside [0, vocab) is no entry, a teacher's logit of -inf an entry
+ *    without mass, a label outside [0, vocab) no label.  The part of a row
+ *    without teacher (label) is zero in loss and gradient, whatever its logits
+ *    hold; a row of weight 0 has a zero gradient.
+ *  - Logits of -inf have probability zero; a row that has a teacher or a label
+ *    but no finite logit is NaN, as are rows with a NaN or +inf.
+ *  - losses may be NULL, and dlogits may (then weights are not used).  dlogits
+ *    may be the logits themselves (same pointer and pitch).
+ *  - Everything is computed in float32; dlogits is rounded once.
+ * top, top_ids: NULL when n_top = 0 (labels alone); labels: NULL for none.
+ * weights: float32, one every weight_stride elements (0: one for all rows), or
+ * NULL for the scalar `weight`.
+ * Limits: rows <= 2^21, 1 <= vocab <= 2^30, n_top <= 1024, tau finite and > 0,
+ * 0 <= alpha <= 1. */
+typedef struct {
+  const void* logits;        /* rows x vocab, type dtype */
+  malt_dtype_t dtype;        /* of logits and dlogits */
+  int64_t rows, vocab, ld;
+  const void* top;           /* rows x n_top, pitch top_ld */
+  malt_dtype_t top_type;
+  const void* top_ids;       /* rows x n_top, pitch id_ld */
+  malt_index_t id_type;
+  int64_t n_top, top_ld, id_ld;
+  const void* labels;        /* rows */
+  malt_index_t label_type;
+  float tau, alpha;
+  const float* weights;
+  int64_t weight_stride;
+  float weight;
+  float* losses;             /* rows */
+  void* dlogits;             /* rows x vocab, pitch dld */
+  int64_t dld;
+} malt_distill_t;
+malt_status_t malt_distill(const malt_distill_t* args, void* stream);
+
+/* 8-bit operands with a power-of-two scale for each block of 128 values.  A
+ * block x becomes a scale s = 2^e, the least e >= -127 with max|x| <= 448 s
+ * (s = 1 for a block of zeros), and q = x / s rounded to the nearest 8-bit float
+ * (4 exponent, 3 mantissa bits, ties to even).  A block holding an infinity or a
+ * NaN makes every sum it enters NaN.
+ *
+ * An operand of `rows` rows over a contraction of `cols` values is
+ *   values: rows x pad128(cols) bytes, zeros past cols;
+ *   scales: bytes e + 127, one for each row and 128 values, in the order the
+ *     matrix instructions take them: [block of cols][row, padded to 256], row r
+ *     at 128 (r / 128) + 8 (r % 16) + (r / 16) % 8.
+ * malt_block_size gives the bytes of both. */
+malt_status_t malt_block_size(int64_t rows, int64_t cols, size_t* value_bytes, size_t* scale_bytes);
+
+/* x (rows x cols) as an operand contracted along its columns (values, scales)
+ * and, transposed, as one contracted along its rows (t_values, t_scales: an
+ * operand of `cols` rows over `rows` values).  Either pair may be NULL.  Values
+ * and scales must be 16-byte aligned.
+ * Limits: 1 <= rows, cols <= 2^22. */
+malt_status_t malt_block_quantize(const void* x, malt_dtype_t type, int64_t rows, int64_t cols, int64_t ld,
+                                  void* values, void* scales, void* t_values, void* t_scales, void* stream);
+
+/* A weight w (rows x cols) with one scale for each 128 x 128 block,
+ * block_scales [ceil(rows / 128)][ceil(cols / 128)], which serves values and the
+ * transpose's t_values alike (either may be NULL). */
+malt_status_t malt_block_quantize_weight(const void* w, malt_dtype_t type, int64_t rows, int64_t cols, int64_t ld,
+                                         void* values, void* block_scales, void* t_values, void* stream);
+
+/* out (m x n) = (accumulate ? out : 0) + A B^T over k values, A m x k, B n x k,
+ * sums in float32, rounded once to out_type.
+ *  b_blocks = 0: b_scales are an operand's.
+ *  b_blocks = 1: B is a weight's values, or its transpose's; the scale of rows
+ *    128 i .. and values 128 j .. is b_scales[i * b_row_stride + j * b_col_stride].
+ * Operands 16-byte aligned.  Limits: 1 <= m, n, k <= 2^22, m n <= 2^37, an
+ * operand's scales below 4 GiB.
+ * workspace: device memory of malt_block_matmul_size's bytes (may be 0; then
+ * NULL), 256-byte aligned. */
+malt_status_t malt_block_matmul_size(int64_t m, int64_t n, int64_t k, size_t* workspace_bytes);
+malt_status_t malt_block_matmul(int64_t m, int64_t n, int64_t k, const void* a_values, const void* a_scales,
+                                const void* b_values, const void* b_scales, int32_t b_blocks, int64_t b_row_stride,
+                                int64_t b_col_stride, void* out, malt_dtype_t out_type, int64_t ldo,
+                                int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
 const char* malt_status_string(malt_status_t status);
 const char* malt_last_error(void);
 const char* malt_version(void);

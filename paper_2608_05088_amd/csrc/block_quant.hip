@@ -1,0 +1,206 @@
+// Bringing a matrix to 8 bits with a power-of-two scale for each block of 128:
+// s = 2^e with the least e >= -127 for which max|x| <= 448 s, q = x / s rounded
+// to the nearest 8-bit float.  A power of two makes the division exact and lets
+// the matrix instruction apply the scale by itself.
+//
+// Bound by memory: one workgroup reads a 128 x 128 tile once, into registers,
+// and writes what is wanted of it: the rows' form (blocks along a row), the
+// transpose's (blocks along a column), or both under one scale (a weight).
+#include "block_fp8.h"
+#include "ops_common.h"
+
+namespace malt {
+
+namespace {
+
+// Largest magnitude as a bit pattern: an infinity or a NaN is larger than any number.
+__device__ __forceinline__ uint32_t mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// Exponent byte of the scale for a largest magnitude: 448 = 1.75 * 2^8; 255 (not
+// a number) where the block holds an infinity or a NaN.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t b) {
+  if (b >= 0x7f800000u) return 255u;
+  if (b == 0) return 127u;
+  const int e = (int)(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return e < 0 ? 0u : (uint32_t)e;
+}
+// 1 / s, exact; NaN for a block that holds an infinity or a NaN.
+__device__ __forceinline__ float scale_inverse(uint32_t byte) {
+  return __uint_as_float(byte < 254u ? (254u - byte) << 23 : 0x7fc00000u);
+}
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+  return (uint32_t)r;
+}
+
+// Maximum over the 16 lanes of a row of lanes, in every one of them.
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+  v = umax(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true));   // rotate by 8, 4, 2, 1
+  v = umax(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, true));
+  v = umax(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, true));
+  v = umax(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, true));
+  return v;
+}
+
+template <bool VEC>
+__device__ __forceinline__ void load8(const float* row, int c, int cols, float (&v)[8]) {
+  if (VEC && c + 8 <= cols) {
+    const op_f32x4 a = load4(row + c), b = load4(row + c + 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[j] = a[j];
+      v[4 + j] = b[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? gptr(row)[c + j] : 0.f;
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void load8(const bf16_t* row, int c, int cols, float (&v)[8]) {
+  if (VEC && c + 8 <= cols) {
+    const op_u32x4 r = *reinterpret_cast<const MALT_GLOBAL op_u32x4*>(gptr(row) + c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] = bf16_lo(r[j]);
+      v[2 * j + 1] = bf16_hi(r[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? to_f32(gptr(row)[c + j]) : 0.f;
+  }
+}
+
+// Thread (rg, cg) holds rows 8 rg .. + 7, columns 8 cg .. + 7 of the tile.
+// WEIGHT: one scale for the whole tile.
+template <class T, bool VEC, bool WEIGHT>
+__global__ __launch_bounds__(256) void block_quant_kernel(QuantArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t tile[QB * QB];   // the transpose's bytes
+  __shared__ uint32_t col_max[4][QB];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int cg = tid & 15, rg = tid >> 4;
+  const int64_t r0 = (int64_t)blockIdx.y * QB, c0 = (int64_t)blockIdx.x * QB;
+  const int rows = (int)(a.rows - r0 < QB ? a.rows - r0 : QB), cols = (int)(a.cols - c0 < QB ? a.cols - c0 : QB);
+  const T* x = static_cast<const T*>(a.x) + r0 * a.ld + c0;
+  const int64_t pitch = q_pad(a.cols), t_pitch = q_pad(a.rows);
+
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = 8 * rg + i;
+    if (r < rows) load8<VEC>(x + (int64_t)r * a.ld, 8 * cg, cols, v[i]);
+    else
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+  }
+
+  uint32_t one = 127;   // the tile's scale
+  if constexpr (WEIGHT) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) b = umax(b, mag(v[i][j]));
+    b = max16(b);
+    b = umax(b, (uint32_t)__shfl_xor((int)b, 16, 64));
+    b = umax(b, (uint32_t)__shfl_xor((int)b, 32, 64));
+    if (lane == 0) col_max[wave][0] = b;
+    __syncthreads();
+    one = scale_byte(umax(umax(col_max[0][0], col_max[1][0]), umax(col_max[2][0], col_max[3][0])));
+    if (tid == 0) gptr(a.block_scales)[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = (uint8_t)one;
+  }
+
+  if (a.values) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 8 * rg + i;
+      uint32_t byte = one;
+      if constexpr (!WEIGHT) {
+        uint32_t b = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b = umax(b, mag(v[i][j]));
+        byte = scale_byte(max16(b));
+      }
+      if (r < rows) {
+        const float s = scale_inverse(byte);
+        const op_u32x2 q = {pack4(v[i][0] * s, v[i][1] * s, v[i][2] * s, v[i][3] * s),
+                            pack4(v[i][4] * s, v[i][5] * s, v[i][6] * s, v[i][7] * s)};
+        *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(a.values) + (r0 + r) * pitch + c0 + 8 * cg) = q;
+        if (!WEIGHT && cg == 0)
+          gptr(a.scales)[blockIdx.x * q_scale_rows(a.rows) + r0 + q_scale_pos(r)] = (uint8_t)byte;
+      }
+    }
+  }
+
+  if (a.t_values) {
+    uint32_t byte[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) byte[j] = one;
+    if constexpr (!WEIGHT) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint32_t b = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b = umax(b, mag(v[i][j]));
+        b = umax(b, (uint32_t)__shfl_xor((int)b, 16, 64));
+        b = umax(b, (uint32_t)__shfl_xor((int)b, 32, 64));
+        if (lane < 16) col_max[wave][8 * cg + j] = b;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int c = 8 * cg + j;
+        byte[j] = scale_byte(umax(umax(col_max[0][c], col_max[1][c]), umax(col_max[2][c], col_max[3][c])));
+      }
+      if (rg == 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (8 * cg + j < cols)
+            gptr(a.t_scales)[blockIdx.y * q_scale_rows(a.cols) + c0 + q_scale_pos(8 * cg + j)] = (uint8_t)byte[j];
+      }
+    }
+    // Column c's 128 bytes lie in 8-byte pieces, piece rg at rg ^ (c / 8): the
+    // 16 lanes that write one rg fill 128 consecutive bytes' worth of banks.
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float s = scale_inverse(byte[j]);
+      const op_u32x2 q = {pack4(v[0][j] * s, v[1][j] * s, v[2][j] * s, v[3][j] * s),
+                          pack4(v[4][j] * s, v[5][j] * s, v[6][j] * s, v[7][j] * s)};
+      *reinterpret_cast<op_u32x2*>(tile + (8 * cg + j) * QB + ((rg ^ cg) << 3)) = q;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = (tid >> 3) + 32 * i, p = tid & 7;   // column, 16-byte piece of its 128 bytes
+      const int g = c >> 3;
+      op_u32x4 q = *reinterpret_cast<const op_u32x4*>(tile + c * QB + ((p ^ (g >> 1)) << 4));
+      if (g & 1) q = op_u32x4{q.z, q.w, q.x, q.y};
+      if (c < cols) *reinterpret_cast<MALT_GLOBAL op_u32x4*>(gptr(a.t_values) + (c0 + c) * t_pitch + r0 + 16 * p) = q;
+    }
+  }
+}
+
+template <class T>
+void quant_typed(const QuantArgs& a, bool vec, hipStream_t s) {
+  const dim3 grid((unsigned)((a.cols + QB - 1) / QB), (unsigned)((a.rows + QB - 1) / QB));
+  if (a.block_scales) {
+    if (vec) hipLaunchKernelGGL((block_quant_kernel<T, true, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((block_quant_kernel<T, false, true>), grid, dim3(256), 0, s, a);
+  } else {
+    if (vec) hipLaunchKernelGGL((block_quant_kernel<T, true, false>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((block_quant_kernel<T, false, false>), grid, dim3(256), 0, s, a);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_block_quant(const QuantArgs& a, bool f32, hipStream_t s) {
+  const bool vec = op_aligned(a.x, 16) && a.ld % (f32 ? 4 : 8) == 0;
+  if (f32) quant_typed<float>(a, vec, s);
+  else quant_typed<bf16_t>(a, vec, s);
+  return hipGetLastError();
+}
+
+}  // namespace malt

@@ -1,0 +1,314 @@
+// Distillation loss of one row of student logits z over the vocabulary against
+// a teacher's top logits a_j at ids i_j, labels y mixed in, and its gradient:
+//
+//   p = softmax(a / tau) over the row's valid entries, q = softmax(z / tau), q1 = softmax(z)
+//   loss = (1 - alpha) tau^2 sum_j p_j (log p_j - log q_{i_j}) - alpha log q1_y
+//   dz   = w [ (1 - alpha) tau (q - p) + alpha (q1 - 1_y) ]
+//
+// A workgroup takes a row and holds it in registers: it is read once, for the
+// maximum, the sums and the gradient, which is all the memory traffic there has
+// to be.  Wave 0 also deals with the teacher's entries.  What does not fit the
+// registers is read again for each pass.  q and q1 are written to every column
+// first; then the columns of the teacher's entries and of the label, whose
+// logits were fetched at the start, are written again with p and 1_y taken off.
+#include "distill.h"
+#include "ops_common.h"
+
+namespace malt {
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
+template <class T>
+struct Vec;
+template <>
+struct Vec<float> {
+  static constexpr int N = 4;
+  static constexpr uint32_t NEG_INF = 0xff800000u;
+  __device__ static void open(op_u32x4 r, float (&f)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(r[e]);
+  }
+  __device__ static op_u32x4 close(const float (&f)[4]) {
+    op_u32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = __float_as_uint(f[e]);
+    return r;
+  }
+};
+template <>
+struct Vec<bf16_t> {
+  static constexpr int N = 8;
+  static constexpr uint32_t NEG_INF = 0xff80ff80u;
+  __device__ static void open(op_u32x4 r, float (&f)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      f[2 * e] = bf16_lo(r[e]);
+      f[2 * e + 1] = bf16_hi(r[e]);
+    }
+  }
+  __device__ static op_u32x4 close(const float (&f)[8]) {
+    op_u32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = pack_bf16x2(f[2 * e], f[2 * e + 1]);
+    return r;
+  }
+};
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+
+// NT threads hold H vectors of 16 bytes each.  TWO: both temperatures count
+// (0 < alpha < 1, tau != 1); otherwise one normaliser serves.  STEP: the
+// gradient is written.
+template <class T, int NT, int H, bool TWO, bool STEP>
+__global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
+  using V = Vec<T>;
+  constexpr int N = V::N, NW = NT / 64;
+  __shared__ float red_max[NW], red_tau[NW], red_one[NW];
+  __shared__ float ent_off[DISTILL_MAX_TOP + 1], ent_z[DISTILL_MAX_TOP + 1];   // what a column is lowered by; its logit
+  __shared__ int32_t ent_id[DISTILL_MAX_TOP + 1];                              // -1: no entry
+  __shared__ float flags[2];                                                   // the row has a teacher, a label
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t row = blockIdx.x;
+  const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+  const int vocab = (int)a.vocab;
+  // Columns before the first 16-byte boundary and after the last: one a thread.
+  const int ahead = (int)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (int)sizeof(T);
+  const int head = ahead < vocab ? ahead : vocab;
+  const int nvec = (vocab - head) / N;
+  const int tail0 = head + nvec * N;
+  const bool edge = tid < head + (vocab - tail0);
+  const int edge_col = tid < head ? tid : tail0 + (tid - head);
+  const MALT_GLOBAL op_u32x4* body = reinterpret_cast<const MALT_GLOBAL op_u32x4*>(gptr(z) + head);
+
+  op_u32x4 held[H];
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    held[i] = op_u32x4{V::NEG_INF, V::NEG_INF, V::NEG_INF, V::NEG_INF};
+    if (tid + i * NT < nvec) held[i] = body[tid + i * NT];
+  }
+  const float edge_z = edge ? to_f32(gptr(z)[edge_col]) : -INFINITY;
+
+  // ------------------------------------------------ teacher and label (wave 0)
+  const float inv_tau = 1.f / a.tau;
+  float top = -INFINITY, top_sum = 0.f;   // the entries' maximum and sum of exp((a - top) / tau)
+  if (wave == 0) {
+    bool some = false;
+    for (int j = lane; j < a.n_top; j += 64) {
+      const int64_t id = load_id(static_cast<const char*>(a.top_ids) + row * a.id_ld * (a.wide_ids ? 8 : 4), a.wide_ids, j);
+      float v = -INFINITY;
+      const bool there = id >= 0 && id < vocab;
+      if (there) {
+        v = (a.top_f32 ? gptr(static_cast<const float*>(a.top) + row * a.top_ld)[j]
+                       : to_f32(gptr(static_cast<const bf16_t*>(a.top) + row * a.top_ld)[j])) * inv_tau;
+        ent_z[j] = to_f32(gptr(z)[id]);
+      }
+      ent_id[j] = there ? (int32_t)id : -1;
+      ent_off[j] = v;
+      some |= there && v != -INFINITY;
+      top = fmaxf(top, v);
+    }
+    top = wave_max(top);
+    const bool teacher = __any(some);
+    for (int j = lane; j < a.n_top; j += 64) {
+      // An entry without mass (no id, or a logit of -inf) has p = 0.
+      const float v = ent_off[j];
+      if (v != -INFINITY) top_sum += exp2f((v - top) * LOG2E);
+    }
+    top_sum = wave_sum(top_sum);
+    if (lane == 0) {
+      flags[0] = teacher ? 1.f : 0.f;
+      int64_t y = -1;
+      if (a.labels) y = load_id(a.labels, a.wide_labels, row);
+      const bool there = y >= 0 && y < vocab;
+      ent_id[a.n_top] = there ? (int32_t)y : -1;
+      ent_z[a.n_top] = there ? to_f32(gptr(z)[y]) : 0.f;
+      flags[1] = there ? 1.f : 0.f;
+    }
+  }
+
+  // ------------------------------------------------------------------ maximum
+  float m = edge_z;
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    float f[N];
+    V::open(held[i], f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) m = fmaxf(m, f[e]);
+  }
+  for (int q = H * NT + tid; q < nvec; q += NT) {
+    float f[N];
+    V::open(body[q], f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) m = fmaxf(m, f[e]);
+  }
+  m = wave_max(m);
+  if (lane == 0) red_max[wave] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) m = fmaxf(m, red_max[w]);
+
+  // --------------------------------------------------------------------- sums
+  // exp((z - m) / t) = 2^(z c - m c), c = log2(e) / t; the same rounded m c goes
+  // into the sums, the loss and the gradient, so it cancels.
+  const float c_tau = LOG2E * (TWO ? inv_tau : a.alpha < 1.f ? inv_tau : 1.f), c_one = LOG2E;
+  const float mc_tau = m * c_tau, mc_one = m * c_one;
+  float s_tau = 0.f, s_one = 0.f;
+  auto add = [&](float f) {
+    s_tau += __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_tau, -mc_tau));
+    if constexpr (TWO) s_one += __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_one, -mc_one));
+  };
+  add(edge_z);
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    float f[N];
+    V::open(held[i], f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) add(f[e]);
+  }
+  for (int q = H * NT + tid; q < nvec; q += NT) {
+    float f[N];
+    V::open(body[q], f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) add(f[e]);
+  }
+  s_tau = wave_sum(s_tau);
+  if constexpr (TWO) s_one = wave_sum(s_one);
+  if (lane == 0) {
+    red_tau[wave] = s_tau;
+    if constexpr (TWO) red_one[wave] = s_one;
+  }
+  __syncthreads();
+  s_tau = s_one = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    s_tau += red_tau[w];
+    if constexpr (TWO) s_one += red_one[w];
+  }
+  if constexpr (!TWO) s_one = s_tau;
+  const bool use_teacher = flags[0] != 0.f && a.alpha < 1.f, use_label = flags[1] != 0.f && a.alpha > 0.f;
+  const float log_tau = log2f(s_tau), log_one = log2f(s_one);
+  const float mc_label = TWO ? mc_one : mc_tau, c_label = TWO ? c_one : c_tau;
+
+  // --------------------------------------------------------------------- loss
+  if (wave == 0) {
+    float kl = 0.f;
+    const float log_sum = log2f(top_sum);
+    for (int j = lane; j < a.n_top; j += 64) {
+      const float v = ent_off[j];
+      float p = 0.f;
+      if (v != -INFINITY) {
+        const float lp = (v - top) * LOG2E - log_sum;   // log2 p
+        p = exp2f(lp);
+        const float lq = __builtin_fmaf(ent_z[j], c_tau, -mc_tau) - log_tau;
+        if (p != 0.f) kl += p * (lp - lq);
+      }
+      ent_off[j] = (1.f - a.alpha) * a.tau * p;
+    }
+    kl = wave_sum(kl);
+    if (lane == 0) {
+      ent_off[a.n_top] = a.alpha;
+      float loss = 0.f;
+      if (use_teacher) loss += (1.f - a.alpha) * a.tau * a.tau * LN2 * kl;
+      if (use_label)
+        loss += a.alpha * LN2 * (log_one - __builtin_fmaf(ent_z[a.n_top], c_label, -mc_label));
+      if (a.losses) gptr(a.losses)[row] = loss;
+    }
+  }
+
+  // ----------------------------------------------------------------- gradient
+  if constexpr (STEP) {
+    const float w = a.weight ? gptr(a.weight)[row * a.weight_stride] : a.weight_value;
+    T* d = static_cast<T*>(a.dlogits) + row * a.dld;
+    // A row without weight, teacher and label has no gradient, whatever its logits hold.
+    const bool any = w != 0.f && (use_teacher || use_label);
+    const float k_tau = use_teacher ? w * (1.f - a.alpha) * a.tau : 0.f, k_one = use_label ? w * a.alpha : 0.f;
+    const float k_all = k_tau + k_one;   // one normaliser
+    const float g_tau = mc_tau + log_tau, g_one = mc_one + log_one;
+    auto grad = [&](float f) {
+      const float q = __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_tau, -g_tau));
+      if constexpr (TWO) {
+        const float q1 = __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_one, -g_one));
+        return any ? __builtin_fmaf(k_tau, q, k_one * q1) : 0.f;
+      }
+      return any ? k_all * q : 0.f;
+    };
+    // Vector stores where the gradient's row has the logits' alignment.
+    const bool together = ((reinterpret_cast<uintptr_t>(d) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0;
+    MALT_GLOBAL T* const dg = gptr(d);
+    auto put = [&](int q, op_u32x4 r) {
+      float f[N];
+      V::open(r, f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) f[e] = grad(f[e]);
+      if (together) {
+        *reinterpret_cast<MALT_GLOBAL op_u32x4*>(dg + head + (int64_t)q * N) = V::close(f);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) dg[head + (int64_t)q * N + e] = from_f32<T>(f[e]);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+      if (tid + i * NT < nvec) put(tid + i * NT, held[i]);
+    for (int q = H * NT + tid; q < nvec; q += NT) put(q, body[q]);
+    if (edge) dg[edge_col] = from_f32<T>(grad(edge_z));
+    if (!any) return;
+    // Every store above has reached memory before a column is written again.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const int n_ent = a.n_top + 1;
+    for (int j = tid; j < n_ent; j += NT) {
+      const int id = ent_id[j];
+      if (id < 0) continue;
+      float off = 0.f;   // an id named twice is lowered by both, and both write the same value
+      for (int i = 0; i < n_ent; ++i)
+        if (ent_id[i] == id && (i < a.n_top ? use_teacher : use_label)) off += ent_off[i];
+      dg[id] = from_f32<T>(grad(ent_z[j]) - w * off);
+    }
+  }
+}
+
+template <class T, int NT, int H>
+void launch_held(const DistillArgs& a, hipStream_t s) {
+  const bool two = a.alpha > 0.f && a.alpha < 1.f && a.tau != 1.f;
+  const dim3 grid((unsigned)a.rows), threads(NT);
+  if (a.dlogits) {
+    if (two) hipLaunchKernelGGL((distill_kernel<T, NT, H, true, true>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((distill_kernel<T, NT, H, false, true>), grid, threads, 0, s, a);
+  } else {
+    if (two) hipLaunchKernelGGL((distill_kernel<T, NT, H, true, false>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((distill_kernel<T, NT, H, false, false>), grid, threads, 0, s, a);
+  }
+}
+
+template <class T>
+void launch_typed(const DistillArgs& a, hipStream_t s) {
+  const int64_t nvec = a.vocab / Vec<T>::N;
+  if (nvec <= 256) launch_held<T, 256, 1>(a, s);
+  else if (nvec <= 256 * 4) launch_held<T, 256, 4>(a, s);
+  else if (nvec <= 1024 * 4) launch_held<T, 1024, 4>(a, s);
+  else if (nvec <= 1024 * 8) launch_held<T, 1024, 8>(a, s);
+  else launch_held<T, 1024, 16>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_distill(const DistillArgs& a, bool f32, hipStream_t s) {
+  if (f32) launch_typed<float>(a, s);
+  else launch_typed<bf16_t>(a, s);
+  return hipGetLastError();
+}
+
+}  // namespace malt

@@ -1,0 +1,52 @@
+// Arguments and launchers of the token table's kernels (embed.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace malt {
+
+constexpr int SORT_THREADS = 256, SORT_TILE = 4096;   // keys a block of the sort takes
+
+struct EmbedLookupArgs {
+  const void* ids;
+  const void* table;
+  void* out;
+  int64_t tokens, vocab, table_ld, out_ld;
+  int32_t width;
+  bool wide_ids;
+  float scale;
+  int32_t lanes_log2;   // set by the launcher
+};
+
+struct EmbedGradArgs {
+  const void* ids;
+  const void* grad;
+  void* dtable;
+  int64_t tokens, vocab, grad_ld, dtable_ld;
+  int32_t width;
+  bool wide_ids, accumulate;
+  float scale;
+  // set by the launcher
+  const uint32_t* keys;    // sorted keys and the tokens they belong to
+  const uint32_t* order;
+  uint32_t* table;         // [digit][block] counts of the sort
+  uint32_t* seg;           // [vocab][2]: first and one past the last sorted token
+  float* part;             // [chunk][2][part_ld]
+  int64_t part_ld;
+  int32_t chunk;
+};
+
+struct EmbedGradLayout {
+  size_t keys[2], index[2], table, seg, part, bytes;
+  int64_t blocks, part_ld;
+  int32_t chunk;
+};
+
+EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width);
+// vec: rows of every matrix can be read four columns at a time.
+hipError_t launch_embed_lookup(EmbedLookupArgs a, bool table_f32, bool out_f32, bool vec, hipStream_t s);
+hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32, bool vec,
+                             hipStream_t s);
+
+}  // namespace malt

@@ -1,0 +1,408 @@
+// Token table: rows looked up by id and scaled, and the table's gradient by
+// sorted tokens.
+//
+//   out[t, :] = s table[id_t, :]            (zeros for an id outside the table)
+//   dtable[v, :] (+)= s sum_{t : id_t = v} grad[t, :]
+//
+// Both are bound by memory.  The gradient sorts the tokens by id, stably, so
+// every row's sum is taken in the order of its tokens: the result does not
+// depend on how the work was scheduled.  A row with few tokens is summed by the
+// wave that writes it; the sorted tokens of longer rows (one id in sixteen may
+// be the same word) are first summed in chunks by waves of their own.
+#include "embed.h"
+#include "ops_common.h"
+
+namespace malt {
+
+namespace {
+
+constexpr int DIGIT = 8, BINS = 1 << DIGIT;
+
+// ------------------------------------------------------------------- lookup
+template <class TI, class TO, bool VEC>
+__global__ __launch_bounds__(256) void embed_lookup_kernel(EmbedLookupArgs a) {
+  // 2^lanes_log2 lanes take a token (a wave at most), four columns a lane at a time.
+  const int lanes = 1 << a.lanes_log2;
+  const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2;
+  if (t >= a.tokens) return;
+  const int c = threadIdx.x & (lanes - 1);
+  const int64_t id = load_id(a.ids, a.wide_ids, t);
+  const bool there = id >= 0 && id < a.vocab;
+  const TI* row = static_cast<const TI*>(a.table) + (there ? id : 0) * a.table_ld;
+  TO* out = static_cast<TO*>(a.out) + t * a.out_ld;
+  if constexpr (VEC) {
+    const int n = a.width >> 2;
+    for (int q = c; q < n; q += 4 * lanes) {
+      op_f32x4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        v[u] = op_f32x4{0.f, 0.f, 0.f, 0.f};
+        if (there && q + u * lanes < n) v[u] = load4(row + 4 * (q + u * lanes));
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (q + u * lanes < n) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[u][e] = there ? v[u][e] * a.scale : 0.f;
+          store4(out + 4 * (q + u * lanes), v[u]);
+        }
+    }
+  } else {
+    for (int q = c; q < a.width; q += 4 * lanes) {
+      float v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        v[u] = 0.f;
+        if (there && q + u * lanes < a.width) v[u] = to_f32(gptr(row)[q + u * lanes]);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (q + u * lanes < a.width) gptr(out)[q + u * lanes] = from_f32<TO>(there ? v[u] * a.scale : 0.f);
+    }
+  }
+}
+
+// --------------------------------------------------------------------- sort
+// Keys: the id, or `vocab` for an id outside the table (sorted past the rest).
+__device__ __forceinline__ uint32_t token_key(const EmbedGradArgs& a, int64_t t) {
+  const int64_t id = load_id(a.ids, a.wide_ids, t);
+  return id >= 0 && id < a.vocab ? (uint32_t)id : (uint32_t)a.vocab;
+}
+
+// Lanes of the wave whose digit equals this lane's.
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, bool valid) {
+  uint64_t m = __ballot(valid);
+#pragma unroll
+  for (int b = 0; b < DIGIT; ++b) {
+    const uint64_t s = __ballot((d >> b) & 1);
+    m &= ((d >> b) & 1) ? s : ~s;
+  }
+  return m;
+}
+
+__device__ __forceinline__ int lanes_below(uint64_t m) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+
+// Ranks of one wave's R rounds of 64 keys among the wave's keys of the same
+// digit, in (round, lane) order; hist (this wave's BINS counters, zeroed)
+// receives the digits' counts.
+template <int R>
+__device__ __forceinline__ void wave_ranks(const uint32_t (&key)[R], int shift, int rounds, int n, int lane,
+                                           uint32_t* hist, uint32_t (&rank)[R]) {
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (r >= rounds) break;
+    const bool valid = r * 64 + lane < n;
+    const uint32_t d = (key[r] >> shift) & (BINS - 1);
+    const uint64_t m = same_digit(d, valid);
+    const int below = lanes_below(m);
+    uint32_t before = 0;
+    if (valid) before = hist[d];
+    asm volatile("" ::: "memory");   // a wave's LDS accesses are in order
+    if (valid && below == 0) hist[d] = before + (uint32_t)__popcll(m);
+    asm volatile("" ::: "memory");
+    rank[r] = before + (uint32_t)below;
+  }
+}
+
+// Exclusive sum over the first BINS threads of a workgroup (whole waves; the
+// others pass 0 and get no meaning); `part` holds BINS / 64 values.
+__device__ __forceinline__ uint32_t bins_exclusive(uint32_t v, int tid, uint32_t* part) {
+  uint32_t x = v;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t y = (uint32_t)__shfl_up((int)x, off, 64);
+    if ((tid & 63) >= off) x += y;
+  }
+  if (tid < BINS && (tid & 63) == 63) part[tid >> 6] = x;
+  __syncthreads();
+  uint32_t base = 0;
+  for (int w = 0; w < BINS / 64; ++w)
+    if (w < (tid >> 6)) base += part[w];
+  __syncthreads();
+  return base + x - v;
+}
+
+// Rows without tokens have an empty segment.
+__global__ __launch_bounds__(256) void embed_segments_kernel(EmbedGradArgs a) {
+  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (j >= a.tokens) return;
+  const uint32_t k = gptr(a.keys)[j];
+  if (k >= (uint32_t)a.vocab) return;
+  if (j == 0 || gptr(a.keys)[j - 1] != k) gptr(a.seg)[2 * (int64_t)k] = (uint32_t)j;
+  if (j + 1 == a.tokens || gptr(a.keys)[j + 1] != k) gptr(a.seg)[2 * (int64_t)k + 1] = (uint32_t)(j + 1);
+}
+
+// One pass of the sort over one digit in three kernels: each block's counts of
+// the digits, their sums in digit order, and the keys' places.
+template <bool FIRST>
+__global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(EmbedGradArgs a, int shift, const uint32_t* keys) {
+  __shared__ uint32_t hist[BINS];
+  hist[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t base = (int64_t)blockIdx.x * SORT_TILE;
+  for (int i = threadIdx.x; i < SORT_TILE; i += SORT_THREADS) {
+    if (base + i >= a.tokens) break;
+    const uint32_t k = FIRST ? token_key(a, base + i) : gptr(keys)[base + i];
+    atomicAdd(&hist[(k >> shift) & (BINS - 1)], 1u);
+  }
+  __syncthreads();
+  gptr(a.table)[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = hist[threadIdx.x];
+}
+
+__global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t* table, int n) {
+  __shared__ uint32_t part[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t carry = 0;
+  for (int i0 = 0; i0 < n; i0 += 4096) {
+    const int i = i0 + 4 * tid;
+    uint32_t v[4], own = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = i + e < n ? gptr(table)[i + e] : 0;
+      own += v[e];
+    }
+    uint32_t x = own;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const uint32_t y = (uint32_t)__shfl_up((int)x, off, 64);
+      if (lane >= off) x += y;
+    }
+    if (lane == 63) part[wave] = x;
+    __syncthreads();
+    uint32_t base = carry, all = 0;
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) base += part[w];
+      all += part[w];
+    }
+    base += x - own;
+    carry += all;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (i + e < n) gptr(table)[i + e] = base;
+      base += v[e];
+    }
+    __syncthreads();
+  }
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(EmbedGradArgs a, int shift, const uint32_t* keys,
+                                                                  const uint32_t* index, uint32_t* keys_out,
+                                                                  uint32_t* index_out) {
+  constexpr int NW = SORT_THREADS / 64, R = SORT_TILE / SORT_THREADS;
+  __shared__ uint32_t hist[NW][BINS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int i = tid; i < NW * BINS; i += SORT_THREADS) (&hist[0][0])[i] = 0;
+  const int64_t base = (int64_t)blockIdx.x * SORT_TILE + (int64_t)wave * (R * 64);
+  const int64_t left = a.tokens - base;
+  const int n = left < 0 ? 0 : left > R * 64 ? R * 64 : (int)left;
+  uint32_t key[R], idx[R], rank[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    key[r] = idx[r] = 0;
+    const int i = r * 64 + lane;
+    if (i < n) {
+      key[r] = FIRST ? token_key(a, base + i) : gptr(keys)[base + i];
+      idx[r] = FIRST ? (uint32_t)(base + i) : gptr(index)[base + i];
+    }
+  }
+  __syncthreads();
+  wave_ranks(key, shift, R, n, lane, hist[wave], rank);
+  __syncthreads();
+  {   // thread d: places of digit d's keys, wave after wave
+    uint32_t at = gptr(a.table)[(int64_t)tid * gridDim.x + blockIdx.x];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const uint32_t c = hist[w][tid];
+      hist[w][tid] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (r * 64 + lane < n) {
+      const uint32_t p = hist[wave][(key[r] >> shift) & (BINS - 1)] + rank[r];
+      gptr(keys_out)[p] = key[r];
+      gptr(index_out)[p] = idx[r];
+    }
+}
+
+// --------------------------------------------------------------------- sums
+// Rows order[j .. end) of grad, columns of one strip, added in that order.
+template <bool VEC, class TG>
+__device__ __forceinline__ op_f32x4 sum_rows(const TG* grad, int64_t ld, const uint32_t* order, int64_t j, int64_t end,
+                                             int c0, int lane, int width) {
+  op_f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 8;
+  for (; j + U <= end; j += U) {
+    op_f32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = strip_load<VEC>(grad + (int64_t)order[j + u] * ld, c0, lane, width);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += v[u][e];
+  }
+  for (; j < end; ++j) {
+    const op_f32x4 v = strip_load<VEC>(grad + (int64_t)order[j] * ld, c0, lane, width);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += v[e];
+  }
+  return s;
+}
+
+// Chunk c of the sorted tokens, one strip: partial sums of the segments longer
+// than a chunk.  Such a segment holds the chunk's first or last token, so a
+// chunk has two slots: 0 for the segment its first token belongs to, 1 for one
+// that starts after it.
+template <bool VEC, class TG>
+__global__ __launch_bounds__(256) void embed_chunks_kernel(EmbedGradArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int strip = __builtin_amdgcn_readfirstlane(blockIdx.y * 4 + (threadIdx.x >> 6));
+  const int c0 = strip * STRIP;
+  if (c0 >= a.width) return;
+  const int64_t j0 = (int64_t)blockIdx.x * a.chunk, j1 = j0 + a.chunk < a.tokens ? j0 + a.chunk : a.tokens;
+  const uint32_t first = a.keys[j0], last = a.keys[j1 - 1];
+  float* part = a.part + (int64_t)blockIdx.x * 2 * a.part_ld + c0 + 4 * lane;
+  const TG* grad = static_cast<const TG*>(a.grad);
+  if (first < (uint32_t)a.vocab) {
+    const int64_t s = a.seg[2 * (int64_t)first], e = a.seg[2 * (int64_t)first + 1];
+    if (e - s > a.chunk) store4(part, sum_rows<VEC>(grad, a.grad_ld, a.order, j0, e < j1 ? e : j1, c0, lane, a.width));
+  }
+  if (last != first && last < (uint32_t)a.vocab) {
+    const int64_t s = a.seg[2 * (int64_t)last], e = a.seg[2 * (int64_t)last + 1];
+    if (e - s > a.chunk) store4(part + a.part_ld, sum_rows<VEC>(grad, a.grad_ld, a.order, s, j1, c0, lane, a.width));
+  }
+}
+
+// One row of the table, one strip a wave.
+template <bool VEC, class TG, class TO>
+__global__ __launch_bounds__(256) void embed_rows_kernel(EmbedGradArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t v = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (v >= a.vocab) return;
+  const int c0 = blockIdx.y * STRIP;
+  const int64_t s = a.seg[2 * v], e = a.seg[2 * v + 1];
+  TO* out = static_cast<TO*>(a.dtable) + v * a.dtable_ld;
+  op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  if (s == e) {
+    if (!a.accumulate) strip_store<VEC>(out, c0, lane, a.width, x);
+    return;
+  }
+  if (e - s <= a.chunk) {
+    x = sum_rows<VEC>(static_cast<const TG*>(a.grad), a.grad_ld, a.order, s, e, c0, lane, a.width);
+  } else {
+    const int64_t k0 = s / a.chunk, k1 = (e - 1) / a.chunk;
+    const float* part = a.part + c0 + 4 * lane;
+    x = load4(part + (2 * k0 + (s > k0 * a.chunk ? 1 : 0)) * a.part_ld);
+#pragma unroll 8
+    for (int64_t k = k0 + 1; k <= k1; ++k) {
+      const op_f32x4 p = load4(part + 2 * k * a.part_ld);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] += p[i];
+    }
+  }
+  if (a.accumulate) {
+    const op_f32x4 old = strip_load<VEC>(out, c0, lane, a.width);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = old[i] + a.scale * x[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] *= a.scale;
+  }
+  strip_store<VEC>(out, c0, lane, a.width, x);
+}
+
+}  // namespace
+
+// -------------------------------------------------------------------- launch
+template <class TI, class TO>
+static void lookup_typed(const EmbedLookupArgs& a, bool vec, dim3 grid, hipStream_t s) {
+  if (vec) hipLaunchKernelGGL((embed_lookup_kernel<TI, TO, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((embed_lookup_kernel<TI, TO, false>), grid, dim3(256), 0, s, a);
+}
+
+hipError_t launch_embed_lookup(EmbedLookupArgs a, bool table_f32, bool out_f32, bool vec, hipStream_t s) {
+  const int64_t per = vec ? a.width / 4 : a.width;
+  a.lanes_log2 = 0;
+  while (a.lanes_log2 < 6 && (int64_t(1) << a.lanes_log2) < per) ++a.lanes_log2;
+  const int64_t blocks = (a.tokens + (256 >> a.lanes_log2) - 1) / (256 >> a.lanes_log2);
+  const dim3 grid((unsigned)blocks);
+  if (table_f32 && out_f32) lookup_typed<float, float>(a, vec, grid, s);
+  else if (table_f32) lookup_typed<float, bf16_t>(a, vec, grid, s);
+  else if (out_f32) lookup_typed<bf16_t, float>(a, vec, grid, s);
+  else lookup_typed<bf16_t, bf16_t>(a, vec, grid, s);
+  return hipGetLastError();
+}
+
+EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width) {
+  EmbedGradLayout L = {};
+  auto take = [&](size_t bytes) {
+    const size_t at = L.bytes;
+    L.bytes += (bytes + 255) & ~size_t(255);
+    return at;
+  };
+  L.chunk = 32;
+  while (tokens / L.chunk >= 1024) L.chunk *= 2;
+  L.blocks = (tokens + SORT_TILE - 1) / SORT_TILE;
+  L.part_ld = (width + STRIP - 1) / STRIP * STRIP;
+  for (size_t& k : L.keys) k = take(4 * size_t(tokens));
+  for (size_t& k : L.index) k = take(4 * size_t(tokens));
+  L.table = take(4 * size_t(BINS) * L.blocks);
+  L.seg = take(8 * size_t(vocab));
+  L.part = take(8 * size_t((tokens + L.chunk - 1) / L.chunk) * L.part_ld);
+  return L;
+}
+
+template <bool VEC, class TG>
+static void grad_typed(const EmbedGradArgs& a, bool out_f32, hipStream_t s) {
+  const unsigned strips = (unsigned)((a.width + STRIP - 1) / STRIP);
+  const unsigned chunks = (unsigned)((a.tokens + a.chunk - 1) / a.chunk);
+  if (chunks > 0) hipLaunchKernelGGL((embed_chunks_kernel<VEC, TG>), dim3(chunks, (strips + 3) / 4), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)((a.vocab + 3) / 4), strips);
+  if (out_f32) hipLaunchKernelGGL((embed_rows_kernel<VEC, TG, float>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((embed_rows_kernel<VEC, TG, bf16_t>), grid, dim3(256), 0, s, a);
+}
+
+hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32, bool vec,
+                             hipStream_t s) {
+  uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + L.keys[0]), reinterpret_cast<uint32_t*>(ws + L.keys[1])};
+  uint32_t* index[2] = {reinterpret_cast<uint32_t*>(ws + L.index[0]), reinterpret_cast<uint32_t*>(ws + L.index[1])};
+  a.table = reinterpret_cast<uint32_t*>(ws + L.table);
+  a.seg = reinterpret_cast<uint32_t*>(ws + L.seg);
+  a.part = reinterpret_cast<float*>(ws + L.part);
+  a.part_ld = L.part_ld;
+  a.chunk = L.chunk;
+  hipError_t e = launch_zero_fill(a.seg, 8 * size_t(a.vocab), s);
+  if (e != hipSuccess) return e;
+  int to = 0;
+  if (a.tokens > 0) {
+    const dim3 grid((unsigned)L.blocks), threads(SORT_THREADS);
+    int bits = 1;   // keys run up to vocab
+    while ((int64_t(1) << bits) <= a.vocab) ++bits;
+    for (int shift = 0; shift < bits; shift += DIGIT, to ^= 1) {
+      const uint32_t *k = keys[to ^ 1], *i = index[to ^ 1];
+      if (shift == 0) hipLaunchKernelGGL(sort_count_kernel<true>, grid, threads, 0, s, a, shift, k);
+      else hipLaunchKernelGGL(sort_count_kernel<false>, grid, threads, 0, s, a, shift, k);
+      hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(1024), 0, s, a.table, int(BINS * L.blocks));
+      if (shift == 0) hipLaunchKernelGGL(sort_place_kernel<true>, grid, threads, 0, s, a, shift, k, i, keys[to], index[to]);
+      else hipLaunchKernelGGL(sort_place_kernel<false>, grid, threads, 0, s, a, shift, k, i, keys[to], index[to]);
+    }
+    a.keys = keys[to ^ 1];
+    a.order = index[to ^ 1];
+    hipLaunchKernelGGL(embed_segments_kernel, dim3((unsigned)((a.tokens + 255) / 256)), dim3(256), 0, s, a);
+  }
+  if (vec) {
+    if (grad_f32) grad_typed<true, float>(a, out_f32, s);
+    else grad_typed<true, bf16_t>(a, out_f32, s);
+  } else {
+    if (grad_f32) grad_typed<false, float>(a, out_f32, s);
+    else grad_typed<false, bf16_t>(a, out_f32, s);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace malt

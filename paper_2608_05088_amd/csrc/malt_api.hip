@@ -14,29 +14,32 @@
 #include <vector>
 
 #include "../../include/libmalt.h"
+#include "errors.h"
 #include "malt_internal.h"
 #include "ns_common.h"
 
 using namespace malt;
 
-namespace {
+namespace malt {
 
-thread_local std::string g_last_error;
+// A fixed buffer: recording a failure neither allocates nor throws.
+static thread_local char g_last_error[512];
 
-malt_status_t fail(malt_status_t st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 malt_status_t fail(malt_status_t st, const char* fmt, ...) {
-  char buf[512];
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
+  vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
   va_end(ap);
-  g_last_error = buf;
   return st;
 }
 
 malt_status_t hip_fail(hipError_t e, const char* what) {
   return fail(MALT_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace malt
+
+namespace {
 
 constexpr int64_t kMaxDim = int64_t(1) << 20;        // rows or cols
 constexpr int64_t kMaxShort = 32768;                   // min(rows, cols): NS Gram side
@@ -1656,7 +1659,7 @@ const char* malt_status_string(malt_status_t s) {
   return "MALT_ERR_UNKNOWN";
 }
 
-const char* malt_last_error(void) { return g_last_error.c_str(); }
+const char* malt_last_error(void) { return g_last_error; }
 
 const char* malt_version(void) { return "libmalt 0.1 (gfx950)"; }
 

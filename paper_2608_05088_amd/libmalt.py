@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import operator
 import os
-from ctypes import POINTER, c_char_p, c_double, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 from typing import List, Optional, Sequence, Tuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -29,6 +29,11 @@ MALT_SCRATCH_BYTES = 64 << 20
 
 MALT_VARIANT_MALT = 0
 MALT_VARIANT_MALTER = 1
+MALT_FLOAT32 = 0
+MALT_BFLOAT16 = 1
+MALT_INT32 = 0
+MALT_INT64 = 1
+DISTILL_MAX_TOP = 1024
 VARIANTS = {"malt": MALT_VARIANT_MALT, "malter": MALT_VARIANT_MALTER}
 
 NUM_PHASES = 9
@@ -70,6 +75,15 @@ class malt_profile_t(ctypes.Structure):
                 ("bytes", c_double * NUM_PHASES), ("flops", c_double * NUM_PHASES)]
 
 
+class malt_distill_t(ctypes.Structure):
+    _fields_ = [("logits", c_void_p), ("dtype", c_int32), ("rows", c_int64), ("vocab", c_int64), ("ld", c_int64),
+                ("top", c_void_p), ("top_type", c_int32), ("top_ids", c_void_p), ("id_type", c_int32),
+                ("n_top", c_int64), ("top_ld", c_int64), ("id_ld", c_int64), ("labels", c_void_p),
+                ("label_type", c_int32), ("tau", c_float), ("alpha", c_float), ("weights", c_void_p),
+                ("weight_stride", c_int64), ("weight", c_float), ("losses", c_void_p), ("dlogits", c_void_p),
+                ("dld", c_int64)]
+
+
 class MaltError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{status_string(status)}: {message}")
@@ -99,6 +113,20 @@ _SIGNATURES = [
     ("malt_plan_routes", c_int32, [POINTER(malt_shape_t), c_int32, c_int32, POINTER(malt_route_t)]),
     ("malt_profile_enable", c_int32, [c_void_p, c_int32]),
     ("malt_profile_read", c_int32, [c_void_p, POINTER(malt_profile_t), c_int32]),
+    ("malt_embed_lookup", c_int32, [c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_int64, c_int64, c_float,
+                                    c_void_p, c_int32, c_int64, c_void_p]),
+    ("malt_embed_grad_size", c_int32, [c_int64, c_int64, c_int64, POINTER(c_size_t)]),
+    ("malt_embed_grad", c_int32, [c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_float, c_int32, c_void_p,
+                                  c_int32, c_int64, c_int64, c_int64, c_void_p, c_size_t, c_void_p]),
+    ("malt_distill", c_int32, [POINTER(malt_distill_t), c_void_p]),
+    ("malt_block_size", c_int32, [c_int64, c_int64, POINTER(c_size_t), POINTER(c_size_t)]),
+    ("malt_block_quantize", c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p,
+                                      c_void_p, c_void_p]),
+    ("malt_block_quantize_weight", c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p, c_void_p,
+                                             c_void_p, c_void_p]),
+    ("malt_block_matmul_size", c_int32, [c_int64, c_int64, c_int64, POINTER(c_size_t)]),
+    ("malt_block_matmul", c_int32, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int64,
+                                    c_int64, c_void_p, c_int32, c_int64, c_int32, c_void_p, c_size_t, c_void_p]),
     ("malt_destroy_state", None, [c_void_p]),
     ("malt_status_string", c_char_p, [c_int32]),
     ("malt_last_error", c_char_p, []),

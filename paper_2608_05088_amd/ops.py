@@ -1,0 +1,490 @@
+"""Operators of a training step around the optimizer, on libmalt's HIP kernels:
+
+  embedding, embedding_grad            rows of a token table, scaled, and the table's gradient
+  distill_loss, distill_step           loss against a teacher's top logits (and labels), and its gradient
+  fp8_linear                           a linear layer in 8-bit floating point, with its backward pass
+  fp8_quantize_weight, fp8_forward     the same layer on kept 8-bit weights
+
+The definitions stand in include/libmalt.h.  This module checks arguments,
+allocates outputs and workspaces with torch, and calls the library; there is
+no CPU fallback.  Wrong arguments raise ValueError (TypeError for what is no
+tensor) before anything is enqueued.
+
+Work runs on the current stream of the tensors' device, or on `stream`; the
+caller orders that stream after whatever produces the inputs.  Outputs and
+workspaces belong to the stream the work runs on.  Tensors whose rows are not
+contiguous are copied first; row pitches larger than a row are taken as they are.
+"""
+from __future__ import annotations
+
+import contextlib
+import math
+from ctypes import byref, c_size_t
+from typing import Optional, Tuple, Union
+
+import torch
+
+from . import libmalt as lm
+
+_DTYPES = {torch.float32: lm.MALT_FLOAT32, torch.bfloat16: lm.MALT_BFLOAT16}
+_INDEX = {torch.int32: lm.MALT_INT32, torch.int64: lm.MALT_INT64}
+BLOCK = 128   # values that share a scale
+_NOTHING = contextlib.nullcontext()
+
+
+# ------------------------------------------------------------------ arguments
+def _tensor(name: str, x, types, device=None) -> None:
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor (got {type(x).__name__})")
+    if x.dtype not in types:
+        raise ValueError(f"{name} must be {' or '.join(str(t).replace('torch.', '') for t in types)} (got {x.dtype})")
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be on a GPU (got {x.device})")
+    if device is not None and x.device != device:
+        raise ValueError(f"{name} is on {x.device}, the other tensors on {device}")
+
+
+def _type(name: str, dtype) -> int:
+    if dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float32 or bfloat16 (got {dtype})")
+    return _DTYPES[dtype]
+
+
+def _rows(x: torch.Tensor) -> Tuple[torch.Tensor, int]:
+    """A 2-D tensor whose rows are contiguous and do not overlap, and its row pitch."""
+    r, c = x.shape
+    if (c > 1 and x.stride(1) != 1) or (r > 1 and x.stride(0) < c):
+        x = x.contiguous()
+    return x, (x.stride(0) if r > 1 else c)
+
+
+def _no_stream(stream) -> None:
+    """A differentiable call follows the current stream, as its backward pass will."""
+    if stream is not None:
+        raise ValueError("a differentiable call takes no stream: make it within torch.cuda.stream(...)")
+
+
+def _flat(x: torch.Tensor) -> torch.Tensor:
+    """All but the last dimension as one."""
+    return x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
+
+
+class _Call:
+    """The device and stream of one call: entered, they are current, so that what is allocated belongs to them."""
+
+    def __init__(self, device: torch.device, stream, *inputs):
+        if stream is None:
+            self.ctx = _NOTHING if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+            self.handle = torch.cuda.current_stream(device).cuda_stream
+        else:
+            if isinstance(stream, int):
+                stream = torch.cuda.ExternalStream(stream, device=device)
+            if stream.device != device:
+                raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
+            self.ctx = torch.cuda.stream(stream)
+            self.handle = stream.cuda_stream
+            for x in inputs:   # their memory is not handed out again before this work is done
+                if x is not None:
+                    x.record_stream(stream)
+
+    def __enter__(self):
+        self.ctx.__enter__()
+        return self.handle
+
+    def __exit__(self, *exc):
+        return self.ctx.__exit__(*exc)
+
+
+# ------------------------------------------------------------------ embedding
+def _ids(ids, device) -> torch.Tensor:
+    _tensor("ids", ids, _INDEX, device)
+    return ids.reshape(-1)
+
+
+def _lookup(ids, weight, scale, out_dtype, stream):
+    flat = _ids(ids, weight.device).contiguous()
+    table, ld = _rows(weight)
+    v, w = weight.shape
+    with _Call(weight.device, stream, flat, table) as s:
+        out = torch.empty((flat.numel(), w), dtype=out_dtype, device=weight.device)
+        lm._check(lm.lib().malt_embed_lookup(flat.data_ptr(), _INDEX[flat.dtype], flat.numel(), table.data_ptr(),
+                                             _DTYPES[weight.dtype], v, w, ld, scale, out.data_ptr(),
+                                             _DTYPES[out_dtype], w, s))
+    return out.reshape(*ids.shape, w)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ids, weight, scale, out_dtype):
+        ctx.save_for_backward(ids)
+        ctx.args = (weight.shape[0], scale, weight.dtype)
+        return _lookup(ids, weight, scale, out_dtype, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        (ids,) = ctx.saved_tensors
+        rows, scale, dtype = ctx.args
+        if grad.dtype not in _DTYPES:
+            grad = grad.float()
+        return None, embedding_grad(ids, grad, rows, scale=scale, dtype=dtype), None, None
+
+
+def embedding(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None,
+              stream=None) -> torch.Tensor:
+    """scale * weight[ids], shape ids.shape + (width,); zeros for ids outside
+    the table.  weight: (vocab, width) float32 or bfloat16; ids: int32 or int64
+    of any shape; out_dtype: weight's unless given.  Differentiable in weight
+    (the gradient is dense, of weight's type, see embedding_grad)."""
+    _tensor("weight", weight, _DTYPES)
+    if weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
+        raise ValueError(f"weight must be (vocab, width) (got {tuple(weight.shape)})")
+    _tensor("ids", ids, _INDEX, weight.device)
+    out_dtype = weight.dtype if out_dtype is None else out_dtype
+    _type("out_dtype", out_dtype)
+    scale = float(scale)
+    if weight.requires_grad and torch.is_grad_enabled():
+        _no_stream(stream)
+        return _Embedding.apply(ids, weight, scale, out_dtype)
+    return _lookup(ids, weight, scale, out_dtype, stream)
+
+
+def embedding_grad(ids: torch.Tensor, grad: torch.Tensor, num_rows: int, scale: float = 1.0,
+                   dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, accumulate: bool = False,
+                   stream=None) -> torch.Tensor:
+    """Gradient of a (num_rows, width) table: row v is scale times the sum of
+    grad over the tokens with id v, in float32 and in the tokens' order (equal
+    inputs give equal bits).  grad: ids.shape + (width,).  Written to `out`
+    (contiguous rows) when given, with accumulate added to it; otherwise to a
+    new tensor of `dtype` (default: grad's)."""
+    _tensor("grad", grad, _DTYPES)
+    dev = grad.device
+    flat = _ids(ids, dev).contiguous()
+    if grad.dim() < 1 or tuple(grad.shape[:-1]) != tuple(ids.shape):
+        raise ValueError(f"grad must be ids.shape + (width,) (got {tuple(grad.shape)} for ids {tuple(ids.shape)})")
+    w = grad.shape[-1]
+    if num_rows < 1 or w < 1:
+        raise ValueError(f"the table must have rows and columns (got {num_rows} x {w})")
+    g, ld = _rows(grad.reshape(-1, w))
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        dtype = grad.dtype if dtype is None else dtype
+        _type("dtype", dtype)
+    else:
+        _tensor("out", out, _DTYPES, dev)
+        if tuple(out.shape) != (num_rows, w) or (w > 1 and out.stride(1) != 1) or (num_rows > 1 and out.stride(0) < w):
+            raise ValueError(f"out must be ({num_rows}, {w}) with contiguous rows (got {tuple(out.shape)}, "
+                             f"strides {out.stride()})")
+        if dtype is not None and dtype != out.dtype:
+            raise ValueError(f"dtype {dtype} differs from out's {out.dtype}")
+    size = c_size_t(0)
+    lm._check(lm.lib().malt_embed_grad_size(flat.numel(), num_rows, w, byref(size)))
+    with _Call(dev, stream, flat, g, out) as s:
+        if out is None:
+            out = torch.empty((num_rows, w), dtype=dtype, device=dev)
+        ws = torch.empty(size.value, dtype=torch.uint8, device=dev)
+        lm._check(lm.lib().malt_embed_grad(flat.data_ptr(), _INDEX[flat.dtype], flat.numel(), g.data_ptr(),
+                                           _DTYPES[g.dtype], ld, float(scale), int(bool(accumulate)), out.data_ptr(),
+                                           _DTYPES[out.dtype], num_rows, w, out.stride(0) if num_rows > 1 else w,
+                                           ws.data_ptr(), size.value, s))
+    return out
+
+
+# --------------------------------------------------------------- distillation
+def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss, want_grad, out, stream):
+    _tensor("logits", logits, _DTYPES)
+    dev = logits.device
+    if logits.dim() < 1 or logits.shape[-1] < 1:
+        raise ValueError(f"logits must be (..., vocab) (got {tuple(logits.shape)})")
+    lead, v = tuple(logits.shape[:-1]), logits.shape[-1]
+    tau, alpha = float(tau), float(alpha)
+    if not (math.isfinite(tau) and tau > 0):
+        raise ValueError(f"tau must be finite and > 0 (got {tau})")
+    if not 0 <= alpha <= 1:
+        raise ValueError(f"alpha must be in [0, 1] (got {alpha})")
+    z, ld = _rows(_flat(logits) if logits.dim() > 1 else logits.reshape(1, v))
+    n = z.shape[0]
+    a = lm.malt_distill_t()
+    a.logits, a.dtype, a.rows, a.vocab, a.ld = z.data_ptr(), _DTYPES[z.dtype], n, v, ld
+    keep = [z]
+    if (top_logits is None) != (top_ids is None):
+        raise ValueError("top_logits and top_ids come together")
+    if top_logits is not None:
+        _tensor("top_logits", top_logits, _DTYPES, dev)
+        _tensor("top_ids", top_ids, _INDEX, dev)
+        if tuple(top_logits.shape[:-1]) != lead or top_logits.shape != top_ids.shape:
+            raise ValueError(f"top_logits and top_ids must be {lead} + (k,) (got {tuple(top_logits.shape)}, "
+                             f"{tuple(top_ids.shape)})")
+        k = top_logits.shape[-1]
+        if k > lm.DISTILL_MAX_TOP:
+            raise ValueError(f"at most {lm.DISTILL_MAX_TOP} teacher entries a row (got {k})")
+        if k > 0:
+            t, tld = _rows(top_logits.reshape(n, k))
+            i, ild = _rows(top_ids.reshape(n, k))
+            a.top, a.top_type, a.top_ids, a.id_type = t.data_ptr(), _DTYPES[t.dtype], i.data_ptr(), _INDEX[i.dtype]
+            a.n_top, a.top_ld, a.id_ld = k, tld, ild
+            keep += [t, i]
+    if labels is not None:
+        _tensor("labels", labels, _INDEX, dev)
+        if tuple(labels.shape) != lead:
+            raise ValueError(f"labels must be {lead} (got {tuple(labels.shape)})")
+        y = labels.reshape(-1).contiguous()
+        a.labels, a.label_type = y.data_ptr(), _INDEX[y.dtype]
+        keep.append(y)
+    a.tau, a.alpha = tau, alpha
+    if isinstance(weight, torch.Tensor):
+        _tensor("grad", weight, (torch.float32,), dev)
+        if weight.dim() == 0:
+            w, a.weight_stride = weight, 0
+        elif tuple(weight.shape) == lead:
+            w = weight.reshape(-1)
+            a.weight_stride = w.stride(0) if n > 1 else 0
+        else:
+            raise ValueError(f"grad must be a number, a scalar tensor or {lead} (got {tuple(weight.shape)})")
+        a.weights = w.data_ptr()
+        keep.append(w)
+    else:
+        a.weight = float(weight)
+    if out is not None:
+        _tensor("out", out, (logits.dtype,), dev)
+        if out.shape != logits.shape:
+            raise ValueError(f"out must be {tuple(logits.shape)} (got {tuple(out.shape)})")
+        d = out if out.dim() == 2 else out.view(-1, v)   # a view, or an error: the result is written through it
+        if (v > 1 and d.stride(1) != 1) or (n > 1 and d.stride(0) < v):
+            raise ValueError(f"out must have contiguous rows (got strides {out.stride()})")
+        keep.append(out)
+    with _Call(dev, stream, *keep) as s:
+        losses = grad = None
+        if want_loss:
+            losses = torch.empty(lead, dtype=torch.float32, device=dev)
+            a.losses = losses.data_ptr()
+        if want_grad:
+            if out is None:
+                grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+                d = grad
+                a.dld = v
+            else:
+                grad = out
+                a.dld = d.stride(0) if n > 1 else v
+            a.dlogits = d.data_ptr()
+        lm._check(lm.lib().malt_distill(byref(a), s))
+    return losses, grad
+
+
+class _DistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, top_logits, top_ids, labels, tau, alpha):
+        ctx.save_for_backward(logits, top_logits, top_ids, labels)
+        ctx.args = (tau, alpha)
+        return _distill(logits, top_logits, top_ids, labels, tau, alpha, 1.0, True, False, None, None)[0]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        logits, top_logits, top_ids, labels = ctx.saved_tensors
+        # The row is read once for its sums and gradient together: nothing but the inputs was kept.
+        d = _distill(logits, top_logits, top_ids, labels, *ctx.args, grad.float(), False, True, None, None)[1]
+        return d, None, None, None, None, None
+
+
+def distill_loss(logits: torch.Tensor, top_logits: Optional[torch.Tensor], top_ids: Optional[torch.Tensor],
+                 labels: Optional[torch.Tensor] = None, tau: float = 1.0, alpha: float = 0.0,
+                 stream=None) -> torch.Tensor:
+    """Loss of each row of student logits (..., vocab) against a teacher's top
+    logits (..., k) at top_ids, float32 of shape (...):
+    (1 - alpha) tau^2 KL(p || q) + alpha * cross entropy of `labels`, where
+    p = softmax(top_logits / tau) over the valid entries and
+    q = softmax(logits / tau) over the vocabulary.  Ids and labels outside the
+    vocabulary (-1, -100) are no entries and no labels; a part that a row lacks
+    is zero.  Differentiable in logits."""
+    if isinstance(logits, torch.Tensor) and logits.requires_grad and torch.is_grad_enabled():
+        _no_stream(stream)
+        return _DistillLoss.apply(logits, top_logits, top_ids, labels, tau, alpha)
+    return _distill(logits, top_logits, top_ids, labels, tau, alpha, 1.0, True, False, None, stream)[0]
+
+
+def distill_step(logits: torch.Tensor, top_logits: Optional[torch.Tensor], top_ids: Optional[torch.Tensor],
+                 labels: Optional[torch.Tensor] = None, tau: float = 1.0, alpha: float = 0.0,
+                 grad: Union[float, torch.Tensor] = 1.0, out: Optional[torch.Tensor] = None,
+                 stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The losses of distill_loss and the gradient of sum(grad * losses) to the
+    logits, in one pass over the logits.  grad: a number, a float32 scalar
+    tensor or one weight for each row (0: no gradient).  The gradient goes to
+    `out` when given, which may be `logits` itself."""
+    if isinstance(logits, torch.Tensor):
+        logits = logits.detach()
+    return _distill(logits, top_logits, top_ids, labels, tau, alpha, grad, True, True, out, stream)
+
+
+# --------------------------------------------------------------- 8-bit linear
+def _pad(n: int, to: int) -> int:
+    return -(-n // to) * to
+
+
+def _operand(rows: int, cols: int, device) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Uninitialised values and scales of an 8-bit operand (malt_block_size)."""
+    k = _pad(cols, BLOCK)
+    buf = torch.empty(rows * k + k // BLOCK * _pad(rows, 256), dtype=torch.uint8, device=device)
+    return buf[:rows * k], buf[rows * k:]
+
+
+def _quantize(x, s, rows_form: bool, cols_form: bool):
+    """x (2-D) as an operand along its columns and, transposed, along its rows."""
+    x, ld = _rows(x)
+    r, c = x.shape
+    q = _operand(r, c, x.device) if rows_form else (None, None)
+    t = _operand(c, r, x.device) if cols_form else (None, None)
+    ptr = [None if b is None else b.data_ptr() for b in (*q, *t)]
+    lm._check(lm.lib().malt_block_quantize(x.data_ptr(), _DTYPES[x.dtype], r, c, ld, *ptr, s))
+    return q, t
+
+
+def _quantize_weight(w, s, plain: bool, transposed: bool):
+    w, ld = _rows(w)
+    r, c = w.shape
+    values = torch.empty((r, _pad(c, BLOCK)), dtype=torch.uint8, device=w.device) if plain else None
+    t_values = torch.empty((c, _pad(r, BLOCK)), dtype=torch.uint8, device=w.device) if transposed else None
+    scales = torch.empty((-(-r // BLOCK), -(-c // BLOCK)), dtype=torch.uint8, device=w.device)
+    lm._check(lm.lib().malt_block_quantize_weight(w.data_ptr(), _DTYPES[w.dtype], r, c, ld,
+                                                  None if values is None else values.data_ptr(), scales.data_ptr(),
+                                                  None if t_values is None else t_values.data_ptr(), s))
+    return values, scales, t_values
+
+
+def _matmul(m, n, k, a, b, b_strides, dtype, device, s):
+    """a b^T over k; b_strides: those of a weight's block scales, or None for an operand's."""
+    out = torch.empty((m, n), dtype=dtype, device=device)
+    size = c_size_t(0)
+    lm._check(lm.lib().malt_block_matmul_size(m, n, k, byref(size)))
+    ws = torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None
+    blocks, (i, j) = (0, (0, 0)) if b_strides is None else (1, b_strides)
+    lm._check(lm.lib().malt_block_matmul(m, n, k, a[0].data_ptr(), a[1].data_ptr(), b[0].data_ptr(), b[1].data_ptr(),
+                                         blocks, i, j, out.data_ptr(), _DTYPES[dtype], n, 0,
+                                         None if ws is None else ws.data_ptr(), size.value, s))
+    return out
+
+
+class _Fp8Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, out_dtype):
+        y, xt, wt = _linear(x, weight, out_dtype, None, ctx.needs_input_grad[1], ctx.needs_input_grad[0])
+        ctx.save_for_backward(*xt, *wt)
+        ctx.args = (x.shape, x.dtype, weight.shape, weight.dtype)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        xt_values, xt_scales, wt_values, w_scales = ctx.saved_tensors
+        x_shape, x_dtype, (n, k), w_dtype = ctx.args
+        dev = dy.device
+        if dy.dtype not in _DTYPES:
+            dy = dy.float()
+        g = dy.reshape(-1, n)
+        m = g.shape[0]
+        need_x, need_w = ctx.needs_input_grad[:2]
+        dx = dw = None
+        if m == 0:
+            return (torch.zeros(x_shape, dtype=x_dtype, device=dev) if need_x else None,
+                    torch.zeros((n, k), dtype=w_dtype, device=dev) if need_w else None, None)
+        with _Call(dev, None) as s:
+            q, t = _quantize(g, s, need_x, need_w)
+            if need_x:
+                dx = _matmul(m, k, n, q, (wt_values, w_scales), (1, w_scales.shape[1]), x_dtype, dev, s).reshape(x_shape)
+            if need_w:
+                dw = _matmul(n, k, m, t, (xt_values, xt_scales), None, w_dtype, dev, s)
+        return dx, dw, None
+
+
+def _linear(x, weight, out_dtype, stream, keep_x, keep_w):
+    """The layer's output, and what its backward pass needs: x^T and W^T in 8 bits."""
+    dev = x.device
+    n, k = weight.shape
+    flat = _flat(x) if x.dim() > 1 else x.reshape(1, -1)
+    m = flat.shape[0]
+    xt, wt = (None, None), (None, None)
+    with _Call(dev, stream, x, weight) as s:
+        if m == 0:
+            y = torch.empty((0, n), dtype=out_dtype, device=dev)
+        else:
+            q, xt = _quantize(flat, s, True, keep_x)
+            w_values, w_scales, wt_values = _quantize_weight(weight, s, True, keep_w)
+            if keep_w:
+                wt = (wt_values, w_scales)
+            y = _matmul(m, n, k, q, (w_values, w_scales), (w_scales.shape[1], 1), out_dtype, dev, s)
+    return y.reshape(*x.shape[:-1], n), xt, wt
+
+
+def _linear_args(x, k: int, out_dtype):
+    _tensor("x", x, _DTYPES)
+    if x.dim() < 1 or x.shape[-1] != k:
+        raise ValueError(f"x must be (..., {k}) (got {tuple(x.shape)})")
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    _type("out_dtype", out_dtype)
+    return out_dtype
+
+
+def fp8_linear(x: torch.Tensor, weight: torch.Tensor, out_dtype: Optional[torch.dtype] = None,
+               stream=None) -> torch.Tensor:
+    """x weight^T with both brought to 8 bits: x with a scale for each row and
+    128 values, weight (outer, inner) with one for each 128 x 128 block.  Sums
+    are float32; out_dtype: x's unless given.
+
+    The backward pass runs in 8 bits too: the output's gradient by rows times
+    the same 8-bit weight, and the transposes of gradient and x, with a scale for each column and
+    128 tokens, for the weight's gradient (of weight's type).  Rounding to 8
+    bits passes gradients through unchanged."""
+    _tensor("weight", weight, _DTYPES)
+    if weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
+        raise ValueError(f"weight must be (outer, inner) (got {tuple(weight.shape)})")
+    out_dtype = _linear_args(x, weight.shape[1], out_dtype)
+    _tensor("weight", weight, _DTYPES, x.device)
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad):
+        _no_stream(stream)
+        return _Fp8Linear.apply(x, weight, out_dtype)
+    return _linear(x, weight, out_dtype, stream, False, False)[0]
+
+
+def fp8_quantize_weight(weight: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """A weight (outer, inner) in 8 bits, to be kept for fp8_forward: values
+    float8_e4m3fn (outer, inner padded with zeros to whole blocks), and the
+    exponent (plus 127) of each 128 x 128 block's power-of-two scale, uint8
+    (outer blocks, inner blocks).  value * 2^(scale - 127) is what it stands for."""
+    _tensor("weight", weight, _DTYPES)
+    if weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
+        raise ValueError(f"weight must be (outer, inner) (got {tuple(weight.shape)})")
+    weight = weight.detach()
+    with _Call(weight.device, stream, weight) as s:
+        values, scales, _ = _quantize_weight(weight, s, True, False)
+    return values.view(torch.float8_e4m3fn), scales
+
+
+def fp8_forward(x: torch.Tensor, values: torch.Tensor, scales: torch.Tensor,
+                out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
+    """fp8_linear on kept weights (fp8_quantize_weight), without gradients:
+    x (..., inner), values (outer, inner padded to whole blocks)."""
+    _tensor("values", values, (torch.float8_e4m3fn,))
+    dev = values.device
+    _tensor("x", x, _DTYPES, dev)
+    _tensor("scales", scales, (torch.uint8,), dev)
+    k = x.shape[-1] if x.dim() else 0
+    if k < 1:
+        raise ValueError(f"x must be (..., inner) (got {tuple(x.shape)})")
+    out_dtype = _linear_args(x, k, out_dtype)
+    if values.dim() != 2 or values.shape[0] < 1 or values.shape[1] != _pad(k, BLOCK) or not values.is_contiguous():
+        raise ValueError(f"values must be contiguous, (outer, {_pad(k, BLOCK)}) (got {tuple(values.shape)}, "
+                         f"strides {values.stride()})")
+    n = values.shape[0]
+    if tuple(scales.shape) != (-(-n // BLOCK), _pad(k, BLOCK) // BLOCK) or not scales.is_contiguous():
+        raise ValueError(f"scales must be contiguous, ({-(-n // BLOCK)}, {_pad(k, BLOCK) // BLOCK}) "
+                         f"(got {tuple(scales.shape)}, strides {scales.stride()})")
+    x = x.detach()
+    flat = _flat(x) if x.dim() > 1 else x.reshape(1, -1)
+    m = flat.shape[0]
+    with _Call(dev, stream, x, values, scales) as s:
+        if m == 0:
+            return torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
+        q, _ = _quantize(flat, s, True, False)
+        y = _matmul(m, n, k, q, (values, scales), (scales.shape[1], 1), out_dtype, dev, s)
+    return y.reshape(*x.shape[:-1], n)

@@ -41,9 +41,10 @@ struct BlockMatmulArgs {
   void* out;
   int64_t ldo;
   bool accumulate;
+  bool by_four;   // set by the launcher: four columns of out at a time
 };
 
 hipError_t launch_block_quant(const QuantArgs& a, bool f32, hipStream_t s);
-hipError_t launch_block_matmul(const BlockMatmulArgs& a, bool b_blocks, bool out_f32, hipStream_t s);
+hipError_t launch_block_matmul(BlockMatmulArgs a, bool b_blocks, bool out_f32, hipStream_t s);
 
 }  // namespace malt

@@ -73,7 +73,7 @@ struct MmGeom {
   static constexpr int A_LOADS = TM / 8, LOADS = (TM + TN) / 8 / NW;
   static_assert(LOADS * NW * 8 == TM + TN && A_LOADS % NW == 0, "loads split evenly over the waves");
   static_assert(SN <= 64 && 64 % SN == 0 && SM <= 128 && 128 % SM == 0, "a wave's scales lie in one group");
-  static_assert(MB % 2 == 0, "row blocks are taken in pairs");
+  static_assert(MB % 4 == 0, "row blocks are taken in pairs, an even number of times");
   static_assert(SLOT % 16 == 0, "slots are aligned");
 };
 
@@ -127,6 +127,8 @@ void block_matmul_kernel(BlockMatmulArgs g) {
     voff[q] = (uint32_t)(src * kp) + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
     dst[q] = l * 1024;
   }
+  // Loads a wave has in flight for one stage: its share and, of two waves, the scales.
+  const int in_flight = G::LOADS + (wave == 0 || (!BLOCKS && wave == 1) ? 1 : 0);
   const uint32_t lds0 = lds_u32(lds);
   auto issue = [&](int kt) {
     const uint32_t at = lds0 + (kt & 1) * G::SLOT, soff = (uint32_t)kt * QB;
@@ -157,21 +159,99 @@ void block_matmul_kernel(BlockMatmulArgs g) {
 #pragma unroll
     for (int a = 0; a < MB; ++a) acc[b][a] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  // Fragments of one row block: the two chunks of a lane.
+  auto frag = [&](const char* st, const int (&off)[2], int block) {
+    const i32x4 lo = *reinterpret_cast<const i32x4*>(st + off[0] + block * 16 * QB);
+    const i32x4 hi = *reinterpret_cast<const i32x4*>(st + off[1] + block * 16 * QB);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  constexpr int SAW = MB > 4 ? 2 : 1;   // registers of A's scales
   int wheld = 0;
-  issue(0);
-  for (int kt = 0; kt < KT; ++kt) {
-    if constexpr (BLOCKS)
-      if ((kt & 63) == 0) wheld = n0 + wn * G::SN < g.n && kt + lane < KT ? gptr(wscale)[(kt + lane) * g.b_col_stride] : 0;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (kt + 1 < KT) issue(kt + 1);
-    const char* st = lds + (kt & 1) * G::SLOT;
-    int sa[MB > 4 ? 2 : 1], sb;
+  auto weight_scales = [&](int kt) {   // the next 64 blocks of the contraction
+    if (n0 + wn * G::SN < g.n && kt + lane < KT) wheld = gptr(wscale)[(kt + lane) * g.b_col_stride];
+  };
+  auto read_scales = [&](const char* st, int kt, int (&sa)[SAW], int& sb) {
 #pragma unroll
-    for (int i = 0; i < (MB > 4 ? 2 : 1); ++i) sa[i] = *reinterpret_cast<const int*>(st + off_sa + 4 * i);
+    for (int i = 0; i < SAW; ++i) sa[i] = *reinterpret_cast<const int*>(st + off_sa + 4 * i);
     if constexpr (BLOCKS) sb = __builtin_amdgcn_readlane(wheld, kt & 63);
-    else sb = NB == 2 ? *reinterpret_cast<const uint16_t*>(st + off_sb) : *reinterpret_cast<const int*>(st + off_sb);
-    if constexpr (WIDE) {
+    else sb = *reinterpret_cast<const int*>(st + off_sb);
+  };
+
+  // Two slots: at the barrier that closes stage kt, stage kt + 1 has landed and
+  // every wave holds the rest of stage kt in registers, so its slot takes stage
+  // kt + 2.
+  if constexpr (BLOCKS) weight_scales(0);
+  issue(0);
+  if (KT > 1) issue(1);
+  ns::wait_vm(KT > 1 ? in_flight : 0);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  int sa[SAW], sb;
+  read_scales(lds, 0, sa, sb);
+  auto next_stage = [&](int kt) {   // false: kt is the last one
+    if (kt + 1 == KT) return false;
+    if constexpr (BLOCKS)
+      if (((kt + 1) & 63) == 0) weight_scales(kt + 1);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's reads of stage kt are done
+    ns::wait_vm_c<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (kt + 2 < KT) issue(kt + 2);
+    return true;
+  };
+
+  if constexpr (!WIDE) {
+    constexpr int H = MB / 2;   // sub-steps of two row blocks of A against all of B
+    i32x8 fa[2][2], fb[NB];
+    fa[0][0] = frag(lds, off_a, 0);
+    fa[0][1] = frag(lds, off_a, 1);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) fb[b] = frag(lds, off_b, b);
+    for (int kt = 0; kt < KT; ++kt) {
+      const char* st = lds + (kt & 1) * G::SLOT;
+      const char* nx = lds + (~kt & 1) * G::SLOT;
+      int sa_next[SAW], sb_next = sb;
+#pragma unroll
+      for (int i = 0; i < SAW; ++i) sa_next[i] = sa[i];
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        bool more = true;
+        if (h + 1 < H) {
+          fa[(h + 1) & 1][0] = frag(st, off_a, 2 * h + 2);
+          fa[(h + 1) & 1][1] = frag(st, off_a, 2 * h + 3);
+        } else {
+          more = next_stage(kt);
+          if (more) {
+            fa[0][0] = frag(nx, off_a, 0);
+            fa[0][1] = frag(nx, off_a, 1);
+            read_scales(nx, kt + 1, sa_next, sb_next);
+          }
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int a = 2 * h + i;
+            acc[b][a] = mma_sel(fb[b], fa[h & 1][i], acc[b][a], sb, BLOCKS ? 0 : b, sa[a / 4], a % 4);
+          }
+          if (h + 1 == H && more) fb[b] = frag(nx, off_b, b);   // its products of this stage are done
+        }
+        if (h + 1 < H) {
+#pragma unroll
+          for (int j = 0; j < 2 * NB; ++j) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      sb = sb_next;
+#pragma unroll
+      for (int i = 0; i < SAW; ++i) sa[i] = sa_next[i];
+    }
+  } else {
+    for (int kt = 0; kt < KT; ++kt) {
+      const char* st = lds + (kt & 1) * G::SLOT;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {   // the 16-byte chunks of a lane, 8 values a matrix instruction
         bf16x8 fb[NB][2];
@@ -194,27 +274,12 @@ void block_matmul_kernel(BlockMatmulArgs g) {
               acc[b][a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[b][i], fa[i], acc[b][a], 0, 0, 0);
         }
       }
-    } else {
-      i32x8 fb[NB];
-      auto frag = [&](const int (&off)[2], int block) {
-        const i32x4 lo = *reinterpret_cast<const i32x4*>(st + off[0] + block * 16 * QB);
-        const i32x4 hi = *reinterpret_cast<const i32x4*>(st + off[1] + block * 16 * QB);
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      };
-#pragma unroll
-      for (int b = 0; b < NB; ++b) fb[b] = frag(off_b, b);
-#pragma unroll
-      for (int a = 0; a < MB; ++a) {
-        const i32x8 fa = frag(off_a, a);
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-          acc[b][a] = mma_sel(fb[b], fa, acc[b][a], sb, BLOCKS ? 0 : b, sa[a / 4], a % 4);
-      }
+      if (next_stage(kt)) read_scales(lds + (~kt & 1) * G::SLOT, kt + 1, sa, sb);
     }
-    __syncthreads();
   }
 
   // acc[b][a][e] = out(m, n + e): m = block a, row lane % 16; n = block b, column 4 (lane / 16).
+  const bool four = g.by_four;
 #pragma unroll
   for (int a = 0; a < MB; ++a) {
     const int64_t m = m0 + wm * G::SM + 16 * a + (lane & 15);
@@ -223,13 +288,25 @@ void block_matmul_kernel(BlockMatmulArgs g) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int64_t n = n0 + wn * G::SN + 16 * b + 4 * (lane >> 4);
+      if (four) {
+        if (n < g.n) {
+          op_f32x4 v = {acc[b][a][0], acc[b][a][1], acc[b][a][2], acc[b][a][3]};
+          if (g.accumulate) {
+            const op_f32x4 old = load4(row + n);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (n + e < g.n) {
-          float v = acc[b][a][e];
-          if (g.accumulate) v += to_f32(gptr(row)[n + e]);
-          gptr(row)[n + e] = from_f32<TO>(v);
+            for (int e = 0; e < 4; ++e) v[e] += old[e];
+          }
+          store4(row + n, v);
         }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n + e < g.n) {
+            float v = acc[b][a][e];
+            if (g.accumulate) v += to_f32(gptr(row)[n + e]);
+            gptr(row)[n + e] = from_f32<TO>(v);
+          }
+      }
     }
   }
 }
@@ -259,7 +336,8 @@ hipError_t launch_typed(const BlockMatmulArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_block_matmul(const BlockMatmulArgs& a, bool b_blocks, bool out_f32, hipStream_t s) {
+hipError_t launch_block_matmul(BlockMatmulArgs a, bool b_blocks, bool out_f32, hipStream_t s) {
+  a.by_four = op_rows_by_four(a.out, out_f32 ? MALT_FLOAT32 : MALT_BFLOAT16, a.ldo, a.n);
   if (b_blocks) return out_f32 ? launch_typed<true, float>(a, s) : launch_typed<true, bf16_t>(a, s);
   return out_f32 ? launch_typed<false, float>(a, s) : launch_typed<false, bf16_t>(a, s);
 }

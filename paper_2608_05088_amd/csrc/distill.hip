@@ -67,11 +67,17 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// NT threads hold H vectors of 16 bytes each.  TWO: both temperatures count
-// (0 < alpha < 1, tau != 1); otherwise one normaliser serves.  STEP: the
-// gradient is written.
-template <class T, int NT, int H, bool TWO, bool STEP>
-__global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
+// Which normalisers a call needs.
+enum Mode {
+  ONE,      // alpha = 0, alpha = 1 or tau = 1: a single one
+  TWO,      // those of tau and of 1
+  SQUARE    // tau = 2: exp(z) is the square of exp(z / 2), one exponential serves both
+};
+
+// NT threads hold H vectors of 16 bytes each.  STEP: the gradient is written.
+template <class T, int NT, int H, int MODE, bool STEP, int WPE>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE)))
+void distill_kernel(DistillArgs a) {
   using V = Vec<T>;
   constexpr int N = V::N, NW = NT / 64;
   __shared__ float red_max[NW], red_tau[NW], red_one[NW];
@@ -79,7 +85,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   __shared__ int32_t ent_id[DISTILL_MAX_TOP + 1];                              // -1: no entry
   __shared__ float flags[2];                                                   // the row has a teacher, a label
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = blockIdx.x;
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
   const int vocab = (int)a.vocab;
@@ -92,6 +98,26 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   const int edge_col = tid < head ? tid : tail0 + (tid - head);
   const MALT_GLOBAL op_u32x4* body = reinterpret_cast<const MALT_GLOBAL op_u32x4*>(gptr(z) + head);
 
+  // Teacher and label are wave 0's.  Their first loads go out before the row's,
+  // and the logits at their columns right behind it, so that nobody waits for
+  // a chain of loads; the arithmetic comes after the row's sums.
+  const char* const ids = static_cast<const char*>(a.top_ids) + row * a.id_ld * (a.wide_ids ? 8 : 4);
+  auto entry = [&](int j, int32_t& id, float& v) {
+    const int64_t i = load_id(ids, a.wide_ids, j);
+    v = a.top_f32 ? gptr(static_cast<const float*>(a.top) + row * a.top_ld)[j]
+                  : to_f32(gptr(static_cast<const bf16_t*>(a.top) + row * a.top_ld)[j]);
+    id = i >= 0 && i < vocab ? (int32_t)i : -1;
+  };
+  int32_t id0 = -1, label = -1;
+  float top0 = -INFINITY, z0 = 0.f, z_label = 0.f;
+  if (wave == 0) {
+    if (lane < a.n_top) entry(lane, id0, top0);
+    if (a.labels) {
+      const int64_t y = load_id(a.labels, a.wide_labels, row);
+      label = y >= 0 && y < vocab ? (int32_t)y : -1;
+    }
+  }
+
   op_u32x4 held[H];
 #pragma unroll
   for (int i = 0; i < H; ++i) {
@@ -99,42 +125,35 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
     if (tid + i * NT < nvec) held[i] = body[tid + i * NT];
   }
   const float edge_z = edge ? to_f32(gptr(z)[edge_col]) : -INFINITY;
+  // The held bits are opened anew in each pass: kept open they would take twice the registers.
+  auto close_held = [&]() {
+#pragma unroll
+    for (int i = 0; i < H; ++i) asm volatile("" : "+v"(held[i]));
+  };
 
-  // ------------------------------------------------ teacher and label (wave 0)
-  const float inv_tau = 1.f / a.tau;
-  float top = -INFINITY, top_sum = 0.f;   // the entries' maximum and sum of exp((a - top) / tau)
   if (wave == 0) {
-    bool some = false;
-    for (int j = lane; j < a.n_top; j += 64) {
-      const int64_t id = load_id(static_cast<const char*>(a.top_ids) + row * a.id_ld * (a.wide_ids ? 8 : 4), a.wide_ids, j);
-      float v = -INFINITY;
-      const bool there = id >= 0 && id < vocab;
-      if (there) {
-        v = (a.top_f32 ? gptr(static_cast<const float*>(a.top) + row * a.top_ld)[j]
-                       : to_f32(gptr(static_cast<const bf16_t*>(a.top) + row * a.top_ld)[j])) * inv_tau;
-        ent_z[j] = to_f32(gptr(z)[id]);
-      }
-      ent_id[j] = there ? (int32_t)id : -1;
-      ent_off[j] = v;
-      some |= there && v != -INFINITY;
-      top = fmaxf(top, v);
+    if (id0 >= 0) z0 = to_f32(gptr(z)[id0]);
+    if (label >= 0) z_label = to_f32(gptr(z)[label]);
+    // An entry without an id or with a logit of -inf has no mass.
+    bool some = id0 >= 0 && top0 != -INFINITY;
+    if (lane < a.n_top) {
+      ent_id[lane] = id0;
+      ent_off[lane] = id0 >= 0 ? top0 : -INFINITY;
     }
-    top = wave_max(top);
+    for (int j = lane + 64; j < a.n_top; j += 64) {
+      int32_t id;
+      float v;
+      entry(j, id, v);
+      ent_id[j] = id;
+      ent_off[j] = id >= 0 ? v : -INFINITY;
+      ent_z[j] = id >= 0 ? to_f32(gptr(z)[id]) : 0.f;
+      some |= id >= 0 && v != -INFINITY;
+    }
     const bool teacher = __any(some);
-    for (int j = lane; j < a.n_top; j += 64) {
-      // An entry without mass (no id, or a logit of -inf) has p = 0.
-      const float v = ent_off[j];
-      if (v != -INFINITY) top_sum += exp2f((v - top) * LOG2E);
-    }
-    top_sum = wave_sum(top_sum);
     if (lane == 0) {
       flags[0] = teacher ? 1.f : 0.f;
-      int64_t y = -1;
-      if (a.labels) y = load_id(a.labels, a.wide_labels, row);
-      const bool there = y >= 0 && y < vocab;
-      ent_id[a.n_top] = there ? (int32_t)y : -1;
-      ent_z[a.n_top] = there ? to_f32(gptr(z)[y]) : 0.f;
-      flags[1] = there ? 1.f : 0.f;
+      flags[1] = label >= 0 ? 1.f : 0.f;
+      ent_id[a.n_top] = label;
     }
   }
 
@@ -158,16 +177,21 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < NW; ++w) m = fmaxf(m, red_max[w]);
+  close_held();
 
   // --------------------------------------------------------------------- sums
   // exp((z - m) / t) = 2^(z c - m c), c = log2(e) / t; the same rounded m c goes
   // into the sums, the loss and the gradient, so it cancels.
-  const float c_tau = LOG2E * (TWO ? inv_tau : a.alpha < 1.f ? inv_tau : 1.f), c_one = LOG2E;
-  const float mc_tau = m * c_tau, mc_one = m * c_one;
+  const float inv_tau = 1.f / a.tau;
+  const float c_tau = MODE != ONE || a.alpha < 1.f ? LOG2E * inv_tau : LOG2E;
+  const float c_one = MODE == ONE ? c_tau : LOG2E;
+  const float mc_tau = m * c_tau, mc_one = MODE == SQUARE ? 2.f * mc_tau : m * c_one;
   float s_tau = 0.f, s_one = 0.f;
   auto add = [&](float f) {
-    s_tau += __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_tau, -mc_tau));
-    if constexpr (TWO) s_one += __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_one, -mc_one));
+    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_tau, -mc_tau));
+    s_tau += x;
+    if constexpr (MODE == TWO) s_one += __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_one, -mc_one));
+    if constexpr (MODE == SQUARE) s_one = __builtin_fmaf(x, x, s_one);
   };
   add(edge_z);
 #pragma unroll
@@ -184,32 +208,37 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
     for (int e = 0; e < N; ++e) add(f[e]);
   }
   s_tau = wave_sum(s_tau);
-  if constexpr (TWO) s_one = wave_sum(s_one);
+  if constexpr (MODE != ONE) s_one = wave_sum(s_one);
   if (lane == 0) {
     red_tau[wave] = s_tau;
-    if constexpr (TWO) red_one[wave] = s_one;
+    if constexpr (MODE != ONE) red_one[wave] = s_one;
   }
   __syncthreads();
   s_tau = s_one = 0.f;
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
     s_tau += red_tau[w];
-    if constexpr (TWO) s_one += red_one[w];
+    if constexpr (MODE != ONE) s_one += red_one[w];
   }
-  if constexpr (!TWO) s_one = s_tau;
+  if constexpr (MODE == ONE) s_one = s_tau;
+  close_held();
   const bool use_teacher = flags[0] != 0.f && a.alpha < 1.f, use_label = flags[1] != 0.f && a.alpha > 0.f;
-  const float log_tau = log2f(s_tau), log_one = log2f(s_one);
-  const float mc_label = TWO ? mc_one : mc_tau, c_label = TWO ? c_one : c_tau;
 
-  // --------------------------------------------------------------------- loss
+  // ----------------------------------------------------------- loss (wave 0)
   if (wave == 0) {
-    float kl = 0.f;
-    const float log_sum = log2f(top_sum);
+    const float log_tau = log2f(s_tau), log_one = log2f(s_one);
+    float top = -INFINITY, sum = 0.f, kl = 0.f;
+    for (int j = lane; j < a.n_top; j += 64) top = fmaxf(top, ent_off[j]);
+    top = wave_max(top);
+    const float c_top = LOG2E * inv_tau;
+    for (int j = lane; j < a.n_top; j += 64)
+      if (ent_off[j] != -INFINITY) sum += exp2f((ent_off[j] - top) * c_top);
+    const float log_sum = log2f(wave_sum(sum));
+    if (lane < a.n_top) ent_z[lane] = z0;
     for (int j = lane; j < a.n_top; j += 64) {
-      const float v = ent_off[j];
       float p = 0.f;
-      if (v != -INFINITY) {
-        const float lp = (v - top) * LOG2E - log_sum;   // log2 p
+      if (ent_off[j] != -INFINITY) {
+        const float lp = (ent_off[j] - top) * c_top - log_sum;   // log2 p
         p = exp2f(lp);
         const float lq = __builtin_fmaf(ent_z[j], c_tau, -mc_tau) - log_tau;
         if (p != 0.f) kl += p * (lp - lq);
@@ -219,10 +248,10 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
     kl = wave_sum(kl);
     if (lane == 0) {
       ent_off[a.n_top] = a.alpha;
+      ent_z[a.n_top] = z_label;
       float loss = 0.f;
       if (use_teacher) loss += (1.f - a.alpha) * a.tau * a.tau * LN2 * kl;
-      if (use_label)
-        loss += a.alpha * LN2 * (log_one - __builtin_fmaf(ent_z[a.n_top], c_label, -mc_label));
+      if (use_label) loss += a.alpha * LN2 * (log_one - __builtin_fmaf(z_label, c_one, -mc_one));
       if (a.losses) gptr(a.losses)[row] = loss;
     }
   }
@@ -231,27 +260,10 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   if constexpr (STEP) {
     const float w = a.weight ? gptr(a.weight)[row * a.weight_stride] : a.weight_value;
     T* d = static_cast<T*>(a.dlogits) + row * a.dld;
-    // A row without weight, teacher and label has no gradient, whatever its logits hold.
-    const bool any = w != 0.f && (use_teacher || use_label);
-    const float k_tau = use_teacher ? w * (1.f - a.alpha) * a.tau : 0.f, k_one = use_label ? w * a.alpha : 0.f;
-    const float k_all = k_tau + k_one;   // one normaliser
-    const float g_tau = mc_tau + log_tau, g_one = mc_one + log_one;
-    auto grad = [&](float f) {
-      const float q = __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_tau, -g_tau));
-      if constexpr (TWO) {
-        const float q1 = __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_one, -g_one));
-        return any ? __builtin_fmaf(k_tau, q, k_one * q1) : 0.f;
-      }
-      return any ? k_all * q : 0.f;
-    };
+    MALT_GLOBAL T* const dg = gptr(d);
     // Vector stores where the gradient's row has the logits' alignment.
     const bool together = ((reinterpret_cast<uintptr_t>(d) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0;
-    MALT_GLOBAL T* const dg = gptr(d);
-    auto put = [&](int q, op_u32x4 r) {
-      float f[N];
-      V::open(r, f);
-#pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = grad(f[e]);
+    auto put = [&](int q, const float (&f)[N]) {
       if (together) {
         *reinterpret_cast<MALT_GLOBAL op_u32x4*>(dg + head + (int64_t)q * N) = V::close(f);
       } else {
@@ -259,12 +271,40 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
         for (int e = 0; e < N; ++e) dg[head + (int64_t)q * N + e] = from_f32<T>(f[e]);
       }
     };
+    // A row without weight, or without teacher and label, has no gradient, whatever its logits hold.
+    if (w == 0.f || !(use_teacher || use_label)) {
+      const float none[N] = {};
+      for (int q = tid; q < nvec; q += NT) put(q, none);
+      if (edge) dg[edge_col] = from_f32<T>(0.f);
+      return;
+    }
+    // q = exp(..) / sum: the coefficient of each exponential.
+    const float w_tau = use_teacher ? w * (1.f - a.alpha) * a.tau : 0.f, w_one = use_label ? w * a.alpha : 0.f;
+    const float k_tau = MODE == ONE ? (w_tau + w_one) / s_tau : w_tau / s_tau, k_one = w_one / s_one;
+    auto grad = [&](float f) {
+      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_tau, -mc_tau));
+      if constexpr (MODE == TWO)
+        return __builtin_fmaf(k_tau, x, k_one * __builtin_amdgcn_exp2f(__builtin_fmaf(f, c_one, -mc_one)));
+      if constexpr (MODE == SQUARE) return x * __builtin_fmaf(k_one, x, k_tau);
+      return k_tau * x;
+    };
 #pragma unroll
     for (int i = 0; i < H; ++i)
-      if (tid + i * NT < nvec) put(tid + i * NT, held[i]);
-    for (int q = H * NT + tid; q < nvec; q += NT) put(q, body[q]);
+      if (tid + i * NT < nvec) {
+        float f[N];
+        V::open(held[i], f);
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = grad(f[e]);
+        put(tid + i * NT, f);
+      }
+    for (int q = H * NT + tid; q < nvec; q += NT) {
+      float f[N];
+      V::open(body[q], f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) f[e] = grad(f[e]);
+      put(q, f);
+    }
     if (edge) dg[edge_col] = from_f32<T>(grad(edge_z));
-    if (!any) return;
     // Every store above has reached memory before a column is written again.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -280,27 +320,29 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   }
 }
 
-template <class T, int NT, int H>
-void launch_held(const DistillArgs& a, hipStream_t s) {
-  const bool two = a.alpha > 0.f && a.alpha < 1.f && a.tau != 1.f;
+template <class T, int NT, int H, int WPE, int MODE>
+void launch_mode(const DistillArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.rows), threads(NT);
-  if (a.dlogits) {
-    if (two) hipLaunchKernelGGL((distill_kernel<T, NT, H, true, true>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((distill_kernel<T, NT, H, false, true>), grid, threads, 0, s, a);
-  } else {
-    if (two) hipLaunchKernelGGL((distill_kernel<T, NT, H, true, false>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((distill_kernel<T, NT, H, false, false>), grid, threads, 0, s, a);
-  }
+  if (a.dlogits) hipLaunchKernelGGL((distill_kernel<T, NT, H, MODE, true, WPE>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((distill_kernel<T, NT, H, MODE, false, WPE>), grid, threads, 0, s, a);
+}
+
+template <class T, int NT, int H, int WPE>
+void launch_held(const DistillArgs& a, hipStream_t s) {
+  if (a.alpha == 0.f || a.alpha == 1.f || a.tau == 1.f) launch_mode<T, NT, H, WPE, ONE>(a, s);
+  else if (a.tau == 2.f) launch_mode<T, NT, H, WPE, SQUARE>(a, s);
+  else launch_mode<T, NT, H, WPE, TWO>(a, s);
 }
 
 template <class T>
 void launch_typed(const DistillArgs& a, hipStream_t s) {
   const int64_t nvec = a.vocab / Vec<T>::N;
-  if (nvec <= 256) launch_held<T, 256, 1>(a, s);
-  else if (nvec <= 256 * 4) launch_held<T, 256, 4>(a, s);
-  else if (nvec <= 1024 * 4) launch_held<T, 1024, 4>(a, s);
-  else if (nvec <= 1024 * 8) launch_held<T, 1024, 8>(a, s);
-  else launch_held<T, 1024, 16>(a, s);
+  if (nvec <= 256) launch_held<T, 256, 1, 8>(a, s);
+  else if (nvec <= 256 * 4) launch_held<T, 256, 4, 6>(a, s);
+  else if (nvec <= 512 * 7) launch_held<T, 512, 7, 6>(a, s);
+  else if (nvec <= 512 * 13) launch_held<T, 512, 13, 6>(a, s);
+  else if (nvec <= 512 * 25) launch_held<T, 512, 25, 4>(a, s);
+  else launch_held<T, 1024, 25, 4>(a, s);
 }
 
 }  // namespace

@@ -304,8 +304,8 @@ malt_status_t malt_embed_lookup(const void* ids, malt_index_t id_type, int64_t t
  * Sums are float32 in an order fixed by the ids alone (tokens sorted by id,
  * stably), so equal inputs give equal bits; rounded once to dtable_type.  With
  * accumulate, rows without tokens are neither read nor written.
- * workspace: device memory of malt_embed_grad_size's bytes, 256-byte aligned,
- * of no meaning before or after the call. */
+ * workspace: device memory of malt_embed_grad_size's bytes (may be 0; then
+ * NULL), 256-byte aligned, of no meaning before or after the call. */
 malt_status_t malt_embed_grad_size(int64_t tokens, int64_t vocab, int64_t width, size_t* workspace_bytes);
 malt_status_t malt_embed_grad(const void* ids, malt_index_t id_type, int64_t tokens, const void* grad,
                               malt_dtype_t grad_type, int64_t grad_ld, float scale, int32_t accumulate, void* dtable,

@@ -91,23 +91,24 @@ template <int R>
 __device__ __forceinline__ void wave_ranks(const uint32_t (&key)[R], int shift, int rounds, int n, int lane,
                                            uint32_t* hist, uint32_t (&rank)[R]) {
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    if (r >= rounds) break;
-    const bool valid = r * 64 + lane < n;
-    const uint32_t d = (key[r] >> shift) & (BINS - 1);
-    const uint64_t m = same_digit(d, valid);
-    const int below = lanes_below(m);
-    uint32_t before = 0;
-    if (valid) before = hist[d];
-    asm volatile("" ::: "memory");   // a wave's LDS accesses are in order
-    if (valid && below == 0) hist[d] = before + (uint32_t)__popcll(m);
-    asm volatile("" ::: "memory");
-    rank[r] = before + (uint32_t)below;
-  }
+  for (int r = 0; r < R; ++r)
+    if (r < rounds) {
+      const bool valid = r * 64 + lane < n;
+      const uint32_t d = (key[r] >> shift) & (BINS - 1);
+      const uint64_t m = same_digit(d, valid);
+      const int below = lanes_below(m);
+      uint32_t before = 0;
+      if (valid) before = hist[d];
+      asm volatile("" ::: "memory");   // a wave's LDS accesses are in order
+      if (valid && below == 0) hist[d] = before + (uint32_t)__popcll(m);
+      asm volatile("" ::: "memory");
+      rank[r] = before + (uint32_t)below;
+      __builtin_amdgcn_sched_barrier(0);   // one round's masks at a time: all of them together would not fit the registers
+    }
 }
 
-// Exclusive sum over the first BINS threads of a workgroup (whole waves; the
-// others pass 0 and get no meaning); `part` holds BINS / 64 values.
+// Exclusive sum over the threads 0 .. BINS - 1 of a workgroup (every thread calls;
+// the others pass 0); `part` holds BINS / 64 values.
 __device__ __forceinline__ uint32_t bins_exclusive(uint32_t v, int tid, uint32_t* part) {
   uint32_t x = v;
 #pragma unroll
@@ -118,28 +119,23 @@ __device__ __forceinline__ uint32_t bins_exclusive(uint32_t v, int tid, uint32_t
   if (tid < BINS && (tid & 63) == 63) part[tid >> 6] = x;
   __syncthreads();
   uint32_t base = 0;
+#pragma unroll
   for (int w = 0; w < BINS / 64; ++w)
     if (w < (tid >> 6)) base += part[w];
   __syncthreads();
   return base + x - v;
 }
 
-// Rows without tokens have an empty segment.
-__global__ __launch_bounds__(256) void embed_segments_kernel(EmbedGradArgs a) {
-  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (j >= a.tokens) return;
-  const uint32_t k = gptr(a.keys)[j];
-  if (k >= (uint32_t)a.vocab) return;
-  if (j == 0 || gptr(a.keys)[j - 1] != k) gptr(a.seg)[2 * (int64_t)k] = (uint32_t)j;
-  if (j + 1 == a.tokens || gptr(a.keys)[j + 1] != k) gptr(a.seg)[2 * (int64_t)k + 1] = (uint32_t)(j + 1);
-}
-
-// One pass of the sort over one digit in three kernels: each block's counts of
-// the digits, their sums in digit order, and the keys' places.
+// Many tokens: each pass of the sort takes one digit in three kernels: every
+// block's counts of the digits, their sums over the blocks for each digit, and
+// the keys' places.  The first also empties the table rows' segments.
 template <bool FIRST>
 __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(EmbedGradArgs a, int shift, const uint32_t* keys) {
   __shared__ uint32_t hist[BINS];
   hist[threadIdx.x] = 0;
+  if (FIRST)
+    for (int64_t v = (int64_t)blockIdx.x * SORT_THREADS + threadIdx.x; v < a.vocab; v += (int64_t)gridDim.x * SORT_THREADS)
+      gptr(reinterpret_cast<op_u32x2*>(a.seg))[v] = op_u32x2{0u, 0u};
   __syncthreads();
   const int64_t base = (int64_t)blockIdx.x * SORT_TILE;
   for (int i = threadIdx.x; i < SORT_TILE; i += SORT_THREADS) {
@@ -151,19 +147,16 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(EmbedGradArgs 
   gptr(a.table)[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = hist[threadIdx.x];
 }
 
-__global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t* table, int n) {
-  __shared__ uint32_t part[16];
+// Workgroup d: exclusive sums over the blocks of digit d's counts, in place, and
+// the digit's total behind the table.
+__global__ __launch_bounds__(256) void sort_scan_kernel(uint32_t* table, int blocks) {
+  __shared__ uint32_t part[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t* const row = table + (int64_t)blockIdx.x * blocks;
   uint32_t carry = 0;
-  for (int i0 = 0; i0 < n; i0 += 4096) {
-    const int i = i0 + 4 * tid;
-    uint32_t v[4], own = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = i + e < n ? gptr(table)[i + e] : 0;
-      own += v[e];
-    }
-    uint32_t x = own;
+  for (int i0 = 0; i0 < blocks; i0 += 256) {
+    const uint32_t v = i0 + tid < blocks ? gptr(row)[i0 + tid] : 0;
+    uint32_t x = v;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
       const uint32_t y = (uint32_t)__shfl_up((int)x, off, 64);
@@ -171,20 +164,16 @@ __global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t* table, int n)
     }
     if (lane == 63) part[wave] = x;
     __syncthreads();
-    uint32_t base = carry, all = 0;
-    for (int w = 0; w < 16; ++w) {
-      if (w < wave) base += part[w];
-      all += part[w];
-    }
-    base += x - own;
-    carry += all;
+    uint32_t base = carry;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (i + e < n) gptr(table)[i + e] = base;
-      base += v[e];
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) base += part[w];
+      carry += part[w];
     }
+    if (i0 + tid < blocks) gptr(row)[i0 + tid] = base + x - v;
     __syncthreads();
   }
+  if (tid == 0) gptr(table)[(int64_t)BINS * blocks + blockIdx.x] = carry;
 }
 
 template <bool FIRST>
@@ -192,7 +181,8 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(EmbedGradArgs 
                                                                   const uint32_t* index, uint32_t* keys_out,
                                                                   uint32_t* index_out) {
   constexpr int NW = SORT_THREADS / 64, R = SORT_TILE / SORT_THREADS;
-  __shared__ uint32_t hist[NW][BINS];
+  static_assert(SORT_THREADS == BINS, "a thread for each digit");
+  __shared__ uint32_t hist[NW][BINS], part[BINS / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int i = tid; i < NW * BINS; i += SORT_THREADS) (&hist[0][0])[i] = 0;
   const int64_t base = (int64_t)blockIdx.x * SORT_TILE + (int64_t)wave * (R * 64);
@@ -210,9 +200,9 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(EmbedGradArgs 
   }
   __syncthreads();
   wave_ranks(key, shift, R, n, lane, hist[wave], rank);
-  __syncthreads();
+  const uint32_t start = bins_exclusive(gptr(a.table)[(int64_t)BINS * gridDim.x + tid], tid, part);
   {   // thread d: places of digit d's keys, wave after wave
-    uint32_t at = gptr(a.table)[(int64_t)tid * gridDim.x + blockIdx.x];
+    uint32_t at = start + gptr(a.table)[(int64_t)tid * gridDim.x + blockIdx.x];
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       const uint32_t c = hist[w][tid];
@@ -230,28 +220,170 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(EmbedGradArgs 
     }
 }
 
+__global__ __launch_bounds__(256) void embed_segments_kernel(EmbedGradArgs a) {
+  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (j >= a.tokens) return;
+  const uint32_t k = gptr(a.keys)[j];
+  if (k >= (uint32_t)a.vocab) return;
+  if (j == 0 || gptr(a.keys)[j - 1] != k) gptr(a.seg)[2 * (int64_t)k] = (uint32_t)j;
+  if (j + 1 == a.tokens || gptr(a.keys)[j + 1] != k) gptr(a.seg)[2 * (int64_t)k + 1] = (uint32_t)(j + 1);
+}
+
+// Up to SORT_ONE tokens: all passes in the LDS of one workgroup, and the
+// segments.  Wave w's keys are a run of them, so ranks by wave are stable.
+__global__ __launch_bounds__(1024) void sort_one_kernel(EmbedGradArgs a, int bits, uint32_t* keys_out, uint32_t* order_out) {
+  constexpr int NW = 16, R = SORT_ONE / 1024;
+  __shared__ uint32_t skey[SORT_ONE];
+  __shared__ uint16_t sidx[SORT_ONE];
+  __shared__ uint32_t hist[NW][BINS], part[BINS / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tokens = (int)a.tokens;
+  const int rounds = (tokens + 1023) / 1024;
+  const int base = wave * rounds * 64;
+  const int left = tokens - base, n = left < 0 ? 0 : left < rounds * 64 ? left : rounds * 64;
+  uint32_t key[R], idx[R], rank[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    key[r] = 0;
+    idx[r] = (uint32_t)(base + r * 64 + lane);
+    if (r * 64 + lane < n) key[r] = token_key(a, base + r * 64 + lane);
+  }
+  // Rows without tokens have an empty segment.
+  for (int64_t v = tid; v < a.vocab; v += 1024) gptr(reinterpret_cast<op_u32x2*>(a.seg))[v] = op_u32x2{0u, 0u};
+  for (int shift = 0; shift < bits; shift += DIGIT) {
+    for (int i = tid; i < NW * BINS; i += 1024) (&hist[0][0])[i] = 0;
+    __syncthreads();
+    wave_ranks(key, shift, rounds, n, lane, hist[wave], rank);
+    __syncthreads();
+    uint32_t total = 0;
+    if (tid < BINS)
+#pragma unroll
+      for (int w = 0; w < NW; ++w) total += hist[w][tid];
+    uint32_t at = bins_exclusive(tid < BINS ? total : 0, tid, part);
+    if (tid < BINS)
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const uint32_t c = hist[w][tid];
+        hist[w][tid] = at;
+        at += c;
+      }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (r * 64 + lane < n) {
+        const uint32_t p = hist[wave][(key[r] >> shift) & (BINS - 1)] + rank[r];
+        skey[p] = key[r];
+        sidx[p] = (uint16_t)idx[r];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (r * 64 + lane < n) {
+        key[r] = skey[base + r * 64 + lane];
+        idx[r] = sidx[base + r * 64 + lane];
+      }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the segments are empty before any is written
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (r * 64 + lane < n) {
+      const int j = base + r * 64 + lane;
+      const uint32_t k = key[r];
+      gptr(keys_out)[j] = k;
+      gptr(order_out)[j] = idx[r];
+      if (k < (uint32_t)a.vocab) {
+        if (j == 0 || skey[j - 1] != k) gptr(a.seg)[2 * (int64_t)k] = (uint32_t)j;
+        if (j + 1 == tokens || skey[j + 1] != k) gptr(a.seg)[2 * (int64_t)k + 1] = (uint32_t)(j + 1);
+      }
+    }
+}
+
 // --------------------------------------------------------------------- sums
+// s += up to 8 rows of grad, whose loads are all in flight together; at(u) is
+// the u-th token's number (wave-uniform, u < n).
+template <bool VEC, class TG, class At>
+__device__ __forceinline__ void add_rows(op_f32x4& s, const TG* grad, int64_t ld, int n, int c0, int lane, int width,
+                                         At&& at) {
+  op_f32x4 v[8];
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    v[u] = op_f32x4{0.f, 0.f, 0.f, 0.f};
+    if (u < n) v[u] = strip_load<VEC>(grad + (int64_t)at(u) * ld, c0, lane, width);
+  }
+#pragma unroll
+  for (int u = 0; u < 8; ++u)
+    if (u < n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += v[u][e];
+}
+
 // Rows order[j .. end) of grad, columns of one strip, added in that order.
 template <bool VEC, class TG>
 __device__ __forceinline__ op_f32x4 sum_rows(const TG* grad, int64_t ld, const uint32_t* order, int64_t j, int64_t end,
                                              int c0, int lane, int width) {
   op_f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  constexpr int U = 8;
-  for (; j + U <= end; j += U) {
-    op_f32x4 v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = strip_load<VEC>(grad + (int64_t)order[j + u] * ld, c0, lane, width);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += v[u][e];
-  }
-  for (; j < end; ++j) {
-    const op_f32x4 v = strip_load<VEC>(grad + (int64_t)order[j] * ld, c0, lane, width);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] += v[e];
+  for (; j < end; j += 64) {
+    const int n = end - j < 64 ? (int)(end - j) : 64;
+    const uint32_t mine = lane < n ? gptr(order)[j + lane] : 0;   // 64 tokens' numbers in one load
+    for (int i = 0; i < n; i += 8)
+      add_rows<VEC>(s, grad, ld, n - i < 8 ? n - i : 8, c0, lane, width,
+                    [&](int u) { return (uint32_t)__builtin_amdgcn_readlane((int)mine, i + u); });
   }
   return s;
+}
+
+template <bool VEC, class TO>
+__device__ __forceinline__ void finish_row(const EmbedGradArgs& a, TO* out, int c0, int lane, op_f32x4 x) {
+  if (a.accumulate) {
+    const op_f32x4 old = strip_load<VEC>(out, c0, lane, a.width);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = old[i] + a.scale * x[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] *= a.scale;
+  }
+  strip_store<VEC>(out, c0, lane, a.width, x);
+}
+
+// Few tokens: the wave of a row and strip looks all of them over itself.
+template <bool VEC, class TG, class TO>
+__global__ __launch_bounds__(256) void embed_few_kernel(EmbedGradArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t v = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (v >= a.vocab) return;
+  const int c0 = blockIdx.y * STRIP, tokens = (int)a.tokens;
+  uint64_t met[FEW / 64];
+#pragma unroll
+  for (int b = 0; b < FEW / 64; ++b) {
+    const int t = b * 64 + lane;
+    met[b] = b * 64 < tokens ? __ballot(t < tokens && load_id(a.ids, a.wide_ids, t) == v) : 0;
+  }
+  uint64_t any = 0;
+#pragma unroll
+  for (int b = 0; b < FEW / 64; ++b) any |= met[b];
+  TO* out = static_cast<TO*>(a.dtable) + v * a.dtable_ld;
+  op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  if (!any) {
+    if (!a.accumulate) strip_store<VEC>(out, c0, lane, a.width, x);
+    return;
+  }
+#pragma unroll
+  for (int b = 0; b < FEW / 64; ++b) {
+    uint64_t m = met[b];
+    while (m) {
+      const int n = __popcll(m);
+      uint32_t t[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        t[u] = m ? (uint32_t)(b * 64 + __builtin_ctzll(m)) : 0;
+        m &= m - 1;   // 0 stays 0
+      }
+      add_rows<VEC>(x, static_cast<const TG*>(a.grad), a.grad_ld, n < 8 ? n : 8, c0, lane, a.width,
+                    [&](int u) { return t[u]; });
+    }
+  }
+  finish_row<VEC>(a, out, c0, lane, x);
 }
 
 // Chunk c of the sorted tokens, one strip: partial sums of the segments longer
@@ -305,15 +437,7 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(EmbedGradArgs a) {
       for (int i = 0; i < 4; ++i) x[i] += p[i];
     }
   }
-  if (a.accumulate) {
-    const op_f32x4 old = strip_load<VEC>(out, c0, lane, a.width);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = old[i] + a.scale * x[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] *= a.scale;
-  }
-  strip_store<VEC>(out, c0, lane, a.width, x);
+  finish_row<VEC>(a, out, c0, lane, x);
 }
 
 }  // namespace
@@ -345,63 +469,72 @@ EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width) 
     L.bytes += (bytes + 255) & ~size_t(255);
     return at;
   };
+  if (tokens <= FEW) return L;
   L.chunk = 32;
-  while (tokens / L.chunk >= 1024) L.chunk *= 2;
+  while (tokens / L.chunk >= 8192) L.chunk *= 2;
   L.blocks = (tokens + SORT_TILE - 1) / SORT_TILE;
   L.part_ld = (width + STRIP - 1) / STRIP * STRIP;
   for (size_t& k : L.keys) k = take(4 * size_t(tokens));
   for (size_t& k : L.index) k = take(4 * size_t(tokens));
-  L.table = take(4 * size_t(BINS) * L.blocks);
+  L.table = take(4 * size_t(BINS) * (L.blocks + 1));
   L.seg = take(8 * size_t(vocab));
   L.part = take(8 * size_t((tokens + L.chunk - 1) / L.chunk) * L.part_ld);
   return L;
 }
 
-template <bool VEC, class TG>
-static void grad_typed(const EmbedGradArgs& a, bool out_f32, hipStream_t s) {
+template <bool VEC, class TG, class TO>
+static void grad_typed(const EmbedGradArgs& a, hipStream_t s) {
   const unsigned strips = (unsigned)((a.width + STRIP - 1) / STRIP);
-  const unsigned chunks = (unsigned)((a.tokens + a.chunk - 1) / a.chunk);
-  if (chunks > 0) hipLaunchKernelGGL((embed_chunks_kernel<VEC, TG>), dim3(chunks, (strips + 3) / 4), dim3(256), 0, s, a);
   const dim3 grid((unsigned)((a.vocab + 3) / 4), strips);
-  if (out_f32) hipLaunchKernelGGL((embed_rows_kernel<VEC, TG, float>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((embed_rows_kernel<VEC, TG, bf16_t>), grid, dim3(256), 0, s, a);
+  if (a.tokens <= FEW) {
+    hipLaunchKernelGGL((embed_few_kernel<VEC, TG, TO>), grid, dim3(256), 0, s, a);
+    return;
+  }
+  const unsigned chunks = (unsigned)((a.tokens + a.chunk - 1) / a.chunk);
+  hipLaunchKernelGGL((embed_chunks_kernel<VEC, TG>), dim3(chunks, (strips + 3) / 4), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((embed_rows_kernel<VEC, TG, TO>), grid, dim3(256), 0, s, a);
 }
 
 hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32, bool vec,
                              hipStream_t s) {
-  uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + L.keys[0]), reinterpret_cast<uint32_t*>(ws + L.keys[1])};
-  uint32_t* index[2] = {reinterpret_cast<uint32_t*>(ws + L.index[0]), reinterpret_cast<uint32_t*>(ws + L.index[1])};
-  a.table = reinterpret_cast<uint32_t*>(ws + L.table);
-  a.seg = reinterpret_cast<uint32_t*>(ws + L.seg);
-  a.part = reinterpret_cast<float*>(ws + L.part);
-  a.part_ld = L.part_ld;
-  a.chunk = L.chunk;
-  hipError_t e = launch_zero_fill(a.seg, 8 * size_t(a.vocab), s);
-  if (e != hipSuccess) return e;
-  int to = 0;
-  if (a.tokens > 0) {
-    const dim3 grid((unsigned)L.blocks), threads(SORT_THREADS);
+  if (a.tokens > FEW) {
+    uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + L.keys[0]), reinterpret_cast<uint32_t*>(ws + L.keys[1])};
+    uint32_t* index[2] = {reinterpret_cast<uint32_t*>(ws + L.index[0]), reinterpret_cast<uint32_t*>(ws + L.index[1])};
+    a.table = reinterpret_cast<uint32_t*>(ws + L.table);
+    a.seg = reinterpret_cast<uint32_t*>(ws + L.seg);
+    a.part = reinterpret_cast<float*>(ws + L.part);
+    a.part_ld = L.part_ld;
+    a.chunk = L.chunk;
     int bits = 1;   // keys run up to vocab
     while ((int64_t(1) << bits) <= a.vocab) ++bits;
-    for (int shift = 0; shift < bits; shift += DIGIT, to ^= 1) {
-      const uint32_t *k = keys[to ^ 1], *i = index[to ^ 1];
-      if (shift == 0) hipLaunchKernelGGL(sort_count_kernel<true>, grid, threads, 0, s, a, shift, k);
-      else hipLaunchKernelGGL(sort_count_kernel<false>, grid, threads, 0, s, a, shift, k);
-      hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(1024), 0, s, a.table, int(BINS * L.blocks));
-      if (shift == 0) hipLaunchKernelGGL(sort_place_kernel<true>, grid, threads, 0, s, a, shift, k, i, keys[to], index[to]);
-      else hipLaunchKernelGGL(sort_place_kernel<false>, grid, threads, 0, s, a, shift, k, i, keys[to], index[to]);
+    int to = 0;
+    if (a.tokens <= SORT_ONE) {
+      hipLaunchKernelGGL(sort_one_kernel, dim3(1), dim3(1024), 0, s, a, bits, keys[0], index[0]);
+      to = 1;
+    } else {
+      const dim3 grid((unsigned)L.blocks), threads(SORT_THREADS);
+      for (int shift = 0; shift < bits; shift += DIGIT, to ^= 1) {
+        const uint32_t *k = keys[to ^ 1], *i = index[to ^ 1];
+        if (shift == 0) hipLaunchKernelGGL(sort_count_kernel<true>, grid, threads, 0, s, a, shift, k);
+        else hipLaunchKernelGGL(sort_count_kernel<false>, grid, threads, 0, s, a, shift, k);
+        hipLaunchKernelGGL(sort_scan_kernel, dim3(BINS), dim3(256), 0, s, a.table, int(L.blocks));
+        if (shift == 0) hipLaunchKernelGGL(sort_place_kernel<true>, grid, threads, 0, s, a, shift, k, i, keys[to], index[to]);
+        else hipLaunchKernelGGL(sort_place_kernel<false>, grid, threads, 0, s, a, shift, k, i, keys[to], index[to]);
+      }
+      a.keys = keys[to ^ 1];
+      hipLaunchKernelGGL(embed_segments_kernel, dim3((unsigned)((a.tokens + 255) / 256)), dim3(256), 0, s, a);
     }
     a.keys = keys[to ^ 1];
     a.order = index[to ^ 1];
-    hipLaunchKernelGGL(embed_segments_kernel, dim3((unsigned)((a.tokens + 255) / 256)), dim3(256), 0, s, a);
   }
-  if (vec) {
-    if (grad_f32) grad_typed<true, float>(a, out_f32, s);
-    else grad_typed<true, bf16_t>(a, out_f32, s);
-  } else {
-    if (grad_f32) grad_typed<false, float>(a, out_f32, s);
-    else grad_typed<false, bf16_t>(a, out_f32, s);
-  }
+  if (vec && grad_f32 && out_f32) grad_typed<true, float, float>(a, s);
+  else if (vec && grad_f32) grad_typed<true, float, bf16_t>(a, s);
+  else if (vec && out_f32) grad_typed<true, bf16_t, float>(a, s);
+  else if (vec) grad_typed<true, bf16_t, bf16_t>(a, s);
+  else if (grad_f32 && out_f32) grad_typed<false, float, float>(a, s);
+  else if (grad_f32) grad_typed<false, float, bf16_t>(a, s);
+  else if (out_f32) grad_typed<false, bf16_t, float>(a, s);
+  else grad_typed<false, bf16_t, bf16_t>(a, s);
   return hipGetLastError();
 }
 

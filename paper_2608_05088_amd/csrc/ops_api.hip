@@ -113,7 +113,7 @@ malt_status_t malt_embed_grad(const void* ids, malt_index_t id_type, int64_t tok
   MALT_TRY(check_mat(g));
   MALT_TRY(check_mat(d));
   const EmbedGradLayout L = embed_grad_layout(tokens, vocab, width);
-  if (!workspace) return fail(MALT_ERR_INVALID_ARG, "workspace is NULL");
+  if (L.bytes > 0 && !workspace) return fail(MALT_ERR_INVALID_ARG, "workspace is NULL");
   if (!op_aligned(workspace, 256)) return fail(MALT_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
   if (workspace_bytes < L.bytes)
     return fail(MALT_ERR_INVALID_ARG, "a workspace of %zu bytes where %zu are needed", workspace_bytes, L.bytes);

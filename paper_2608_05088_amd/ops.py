@@ -183,11 +183,11 @@ def embedding_grad(ids: torch.Tensor, grad: torch.Tensor, num_rows: int, scale: 
     with _Call(dev, stream, flat, g, out) as s:
         if out is None:
             out = torch.empty((num_rows, w), dtype=dtype, device=dev)
-        ws = torch.empty(size.value, dtype=torch.uint8, device=dev)
+        ws = torch.empty(size.value, dtype=torch.uint8, device=dev) if size.value else None
         lm._check(lm.lib().malt_embed_grad(flat.data_ptr(), _INDEX[flat.dtype], flat.numel(), g.data_ptr(),
                                            _DTYPES[g.dtype], ld, float(scale), int(bool(accumulate)), out.data_ptr(),
                                            _DTYPES[out.dtype], num_rows, w, out.stride(0) if num_rows > 1 else w,
-                                           ws.data_ptr(), size.value, s))
+                                           None if ws is None else ws.data_ptr(), size.value, s))
     return out
 
 

@@ -393,7 +393,7 @@ malt_status_t malt_block_quantize_weight(const void* w, malt_dtype_t type, int64
  * operand's scales below 4 GiB.
  * workspace: device memory of malt_block_matmul_size's bytes (may be 0; then
  * NULL), 256-byte aligned. */
-malt_status_t malt_block_matmul_size(int64_t m, int64_t n, int64_t k, size_t* workspace_bytes);
+malt_status_t malt_block_matmul_size(int64_t m, int64_t n, int64_t k, malt_dtype_t out_type, size_t* workspace_bytes);
 malt_status_t malt_block_matmul(int64_t m, int64_t n, int64_t k, const void* a_values, const void* a_scales,
                                 const void* b_values, const void* b_scales, int32_t b_blocks, int64_t b_row_stride,
                                 int64_t b_col_stride, void* out, malt_dtype_t out_type, int64_t ldo,

@@ -41,8 +41,18 @@ struct BlockMatmulArgs {
   void* out;
   int64_t ldo;
   bool accumulate;
-  bool by_four;   // set by the launcher: four columns of out at a time
+  float* partial;   // parts > 1: [part][tile][rows][columns]
+  bool by_four;     // set by the launcher: four columns of out at a time
+  int32_t parts;    // and the parts the contraction is cut into
 };
+
+// How a product is tiled, by its sizes and the type of its result.
+struct BlockMatmulPlan {
+  bool big;       // 256 x 256 tiles; otherwise 128 x 128
+  int32_t parts;  // of the contraction
+  size_t bytes;   // of the partial sums
+};
+BlockMatmulPlan block_matmul_plan(int64_t m, int64_t n, int64_t k, bool out_f32);
 
 hipError_t launch_block_quant(const QuantArgs& a, bool f32, hipStream_t s);
 hipError_t launch_block_matmul(BlockMatmulArgs a, bool b_blocks, bool out_f32, hipStream_t s);

@@ -263,12 +263,14 @@ malt_status_t malt_block_quantize_weight(const void* w, malt_dtype_t type, int64
   return quantize("w", w, type, rows, cols, ld, values, nullptr, t_values, nullptr, block_scales, stream);
 }
 
-malt_status_t malt_block_matmul_size(int64_t m, int64_t n, int64_t k, size_t* workspace_bytes) {
+malt_status_t malt_block_matmul_size(int64_t m, int64_t n, int64_t k, malt_dtype_t out_type, size_t* workspace_bytes) {
   if (!workspace_bytes) return fail(MALT_ERR_INVALID_ARG, "output pointer is NULL");
+  if (!op_dtype_ok(out_type)) return fail(MALT_ERR_INVALID_ARG, "unknown element type %d", int(out_type));
   size_t v, s;
   MALT_TRY(malt_block_size(m, k, &v, &s));
   MALT_TRY(malt_block_size(n, k, &v, &s));
-  *workspace_bytes = 0;
+  if (m > kMaxProduct / n) return fail(MALT_ERR_SHAPE, "a product of %lld x %lld", (long long)m, (long long)n);
+  *workspace_bytes = block_matmul_plan(m, n, k, out_type == MALT_FLOAT32).bytes;
   return MALT_OK;
 }
 
@@ -279,7 +281,7 @@ malt_status_t malt_block_matmul(int64_t m, int64_t n, int64_t k, const void* a_v
   size_t av, as, bv, bs, need;
   MALT_TRY(malt_block_size(m, k, &av, &as));
   MALT_TRY(malt_block_size(n, k, &bv, &bs));
-  MALT_TRY(malt_block_matmul_size(m, n, k, &need));
+  MALT_TRY(malt_block_matmul_size(m, n, k, out_type, &need));
   if (!a_values || !a_scales || !b_values || !b_scales) return fail(MALT_ERR_INVALID_ARG, "an operand is NULL");
   if (!op_aligned(a_values, 16) || !op_aligned(a_scales, 16) || !op_aligned(b_values, 16) || (!b_blocks && !op_aligned(b_scales, 16)))
     return fail(MALT_ERR_ALIGNMENT, "an operand is not 16-byte aligned");
@@ -291,7 +293,6 @@ malt_status_t malt_block_matmul(int64_t m, int64_t n, int64_t k, const void* a_v
       return fail(MALT_ERR_SHAPE, "strides %lld, %lld of a weight's scales", (long long)b_row_stride, (long long)b_col_stride);
     bs = size_t((q_pad(n) / QB - 1) * b_row_stride + (q_pad(k) / QB - 1) * b_col_stride + 1);
   }
-  if (m > kMaxProduct / n) return fail(MALT_ERR_SHAPE, "a product of %lld x %lld", (long long)m, (long long)n);
   const Mat o = {"out", out, out_type, m, n, ldo};
   MALT_TRY(check_mat(o));
   if (op_overlap(out, o.bytes(), a_values, av) || op_overlap(out, o.bytes(), a_scales, as) ||
@@ -320,6 +321,7 @@ malt_status_t malt_block_matmul(int64_t m, int64_t n, int64_t k, const void* a_v
   g.out = out;
   g.ldo = ldo;
   g.accumulate = accumulate != 0;
+  g.partial = static_cast<float*>(workspace);
   return launched(launch_block_matmul(g, b_blocks != 0, out_type == MALT_FLOAT32, static_cast<hipStream_t>(stream)),
                   "launching the 8-bit product");
 }

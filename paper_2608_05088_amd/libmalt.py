@@ -124,7 +124,7 @@ _SIGNATURES = [
                                       c_void_p, c_void_p]),
     ("malt_block_quantize_weight", c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p, c_void_p,
                                              c_void_p, c_void_p]),
-    ("malt_block_matmul_size", c_int32, [c_int64, c_int64, c_int64, POINTER(c_size_t)]),
+    ("malt_block_matmul_size", c_int32, [c_int64, c_int64, c_int64, c_int32, POINTER(c_size_t)]),
     ("malt_block_matmul", c_int32, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int64,
                                     c_int64, c_void_p, c_int32, c_int64, c_int32, c_void_p, c_size_t, c_void_p]),
     ("malt_destroy_state", None, [c_void_p]),

@@ -17,7 +17,7 @@ contiguous are copied first; row pitches larger than a row are taken as they are
 """
 from __future__ import annotations
 
-import contextlib
+import functools
 import math
 from ctypes import byref, c_size_t
 from typing import Optional, Tuple, Union
@@ -29,7 +29,6 @@ from . import libmalt as lm
 _DTYPES = {torch.float32: lm.MALT_FLOAT32, torch.bfloat16: lm.MALT_BFLOAT16}
 _INDEX = {torch.int32: lm.MALT_INT32, torch.int64: lm.MALT_INT64}
 BLOCK = 128   # values that share a scale
-_NOTHING = contextlib.nullcontext()
 
 
 # ------------------------------------------------------------------ arguments
@@ -53,6 +52,8 @@ def _type(name: str, dtype) -> int:
 def _rows(x: torch.Tensor) -> Tuple[torch.Tensor, int]:
     """A 2-D tensor whose rows are contiguous and do not overlap, and its row pitch."""
     r, c = x.shape
+    if x.is_contiguous():
+        return x, c
     if (c > 1 and x.stride(1) != 1) or (r > 1 and x.stride(0) < c):
         x = x.contiguous()
     return x, (x.stride(0) if r > 1 else c)
@@ -69,48 +70,53 @@ def _flat(x: torch.Tensor) -> torch.Tensor:
     return x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
 
 
-class _Call:
-    """The device and stream of one call: entered, they are current, so that what is allocated belongs to them."""
+# The current device and its current stream, as numbers.
+_current_device = torch.cuda.current_device
+_current_stream = torch._C._cuda_getCurrentRawStream
 
-    def __init__(self, device: torch.device, stream, *inputs):
-        if stream is None:
-            self.ctx = _NOTHING if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-            self.handle = torch.cuda.current_stream(device).cuda_stream
-        else:
-            if isinstance(stream, int):
-                stream = torch.cuda.ExternalStream(stream, device=device)
-            if stream.device != device:
-                raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
-            self.ctx = torch.cuda.stream(stream)
-            self.handle = stream.cuda_stream
-            for x in inputs:   # their memory is not handed out again before this work is done
-                if x is not None:
-                    x.record_stream(stream)
 
-    def __enter__(self):
-        self.ctx.__enter__()
-        return self.handle
-
-    def __exit__(self, *exc):
-        return self.ctx.__exit__(*exc)
+def _on(device: torch.device, stream, inputs, work):
+    """work(stream handle) with `device` and `stream` current, so that what it
+    allocates belongs to them."""
+    if stream is None:
+        if device.index == _current_device():
+            return work(_current_stream(device.index))
+        with torch.cuda.device(device):
+            return work(_current_stream(device.index))
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    if stream.device != device:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
+    for x in inputs:   # their memory is not handed out again before this work is done
+        if x is not None:
+            x.record_stream(stream)
+    with torch.cuda.stream(stream):
+        return work(stream.cuda_stream)
 
 
 # ------------------------------------------------------------------ embedding
-def _ids(ids, device) -> torch.Tensor:
-    _tensor("ids", ids, _INDEX, device)
-    return ids.reshape(-1)
-
-
 def _lookup(ids, weight, scale, out_dtype, stream):
-    flat = _ids(ids, weight.device).contiguous()
+    flat = ids if ids.dim() == 1 and ids.is_contiguous() else ids.reshape(-1).contiguous()
     table, ld = _rows(weight)
     v, w = weight.shape
-    with _Call(weight.device, stream, flat, table) as s:
-        out = torch.empty((flat.numel(), w), dtype=out_dtype, device=weight.device)
-        lm._check(lm.lib().malt_embed_lookup(flat.data_ptr(), _INDEX[flat.dtype], flat.numel(), table.data_ptr(),
+    n = flat.shape[0]
+    dev = weight.device
+
+    def work(s):
+        out = torch.empty((*ids.shape, w), dtype=out_dtype, device=dev)
+        lm._check(lm.lib().malt_embed_lookup(flat.data_ptr(), _INDEX[flat.dtype], n, table.data_ptr(),
                                              _DTYPES[weight.dtype], v, w, ld, scale, out.data_ptr(),
                                              _DTYPES[out_dtype], w, s))
-    return out.reshape(*ids.shape, w)
+        return out
+
+    return _on(dev, stream, (flat, table), work)
+
+
+@functools.lru_cache(maxsize=4096)
+def _embed_grad_size(tokens: int, vocab: int, width: int) -> int:
+    size = c_size_t(0)
+    lm._check(lm.lib().malt_embed_grad_size(tokens, vocab, width, byref(size)))
+    return size.value
 
 
 class _Embedding(torch.autograd.Function):
@@ -159,7 +165,8 @@ def embedding_grad(ids: torch.Tensor, grad: torch.Tensor, num_rows: int, scale: 
     new tensor of `dtype` (default: grad's)."""
     _tensor("grad", grad, _DTYPES)
     dev = grad.device
-    flat = _ids(ids, dev).contiguous()
+    _tensor("ids", ids, _INDEX, dev)
+    flat = ids.reshape(-1).contiguous()
     if grad.dim() < 1 or tuple(grad.shape[:-1]) != tuple(ids.shape):
         raise ValueError(f"grad must be ids.shape + (width,) (got {tuple(grad.shape)} for ids {tuple(ids.shape)})")
     w = grad.shape[-1]
@@ -178,17 +185,19 @@ def embedding_grad(ids: torch.Tensor, grad: torch.Tensor, num_rows: int, scale: 
                              f"strides {out.stride()})")
         if dtype is not None and dtype != out.dtype:
             raise ValueError(f"dtype {dtype} differs from out's {out.dtype}")
-    size = c_size_t(0)
-    lm._check(lm.lib().malt_embed_grad_size(flat.numel(), num_rows, w, byref(size)))
-    with _Call(dev, stream, flat, g, out) as s:
-        if out is None:
-            out = torch.empty((num_rows, w), dtype=dtype, device=dev)
-        ws = torch.empty(size.value, dtype=torch.uint8, device=dev) if size.value else None
-        lm._check(lm.lib().malt_embed_grad(flat.data_ptr(), _INDEX[flat.dtype], flat.numel(), g.data_ptr(),
-                                           _DTYPES[g.dtype], ld, float(scale), int(bool(accumulate)), out.data_ptr(),
-                                           _DTYPES[out.dtype], num_rows, w, out.stride(0) if num_rows > 1 else w,
-                                           None if ws is None else ws.data_ptr(), size.value, s))
-    return out
+    n = flat.shape[0]
+    size = _embed_grad_size(n, num_rows, w)
+
+    def work(s):
+        d = torch.empty((num_rows, w), dtype=dtype, device=dev) if out is None else out
+        ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+        lm._check(lm.lib().malt_embed_grad(flat.data_ptr(), _INDEX[flat.dtype], n, g.data_ptr(), _DTYPES[g.dtype], ld,
+                                           float(scale), int(bool(accumulate)), d.data_ptr(), _DTYPES[d.dtype],
+                                           num_rows, w, d.stride(0) if num_rows > 1 else w,
+                                           None if ws is None else ws.data_ptr(), size, s))
+        return d
+
+    return _on(dev, stream, (flat, g, out), work)
 
 
 # --------------------------------------------------------------- distillation
@@ -254,7 +263,7 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         if (v > 1 and d.stride(1) != 1) or (n > 1 and d.stride(0) < v):
             raise ValueError(f"out must have contiguous rows (got strides {out.stride()})")
         keep.append(out)
-    with _Call(dev, stream, *keep) as s:
+    def work(s):
         losses = grad = None
         if want_loss:
             losses = torch.empty(lead, dtype=torch.float32, device=dev)
@@ -262,14 +271,14 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         if want_grad:
             if out is None:
                 grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-                d = grad
-                a.dld = v
+                a.dlogits, a.dld = grad.data_ptr(), v
             else:
                 grad = out
-                a.dld = d.stride(0) if n > 1 else v
-            a.dlogits = d.data_ptr()
+                a.dlogits, a.dld = d.data_ptr(), (d.stride(0) if n > 1 else v)
         lm._check(lm.lib().malt_distill(byref(a), s))
-    return losses, grad
+        return losses, grad
+
+    return _on(dev, stream, keep, work)
 
 
 class _DistillLoss(torch.autograd.Function):
@@ -322,107 +331,136 @@ def _pad(n: int, to: int) -> int:
     return -(-n // to) * to
 
 
-def _operand(rows: int, cols: int, device) -> Tuple[torch.Tensor, torch.Tensor]:
-    """Uninitialised values and scales of an 8-bit operand (malt_block_size)."""
+def _operand_bytes(rows: int, cols: int) -> Tuple[int, int]:
+    """Bytes of an 8-bit operand's values, and of values and scales (malt_block_size)."""
     k = _pad(cols, BLOCK)
-    buf = torch.empty(rows * k + k // BLOCK * _pad(rows, 256), dtype=torch.uint8, device=device)
-    return buf[:rows * k], buf[rows * k:]
+    return rows * k, rows * k + k // BLOCK * _pad(rows, 256)
+
+
+class _Operand:
+    """An 8-bit operand in a buffer of its own: values, then scales."""
+    __slots__ = ("buf", "values", "scales")
+
+    def __init__(self, buf: torch.Tensor, rows: int, cols: int):
+        self.buf = buf
+        self.values = buf.data_ptr()
+        self.scales = self.values + _operand_bytes(rows, cols)[0]
+
+    @staticmethod
+    def empty(rows: int, cols: int, device) -> "_Operand":
+        return _Operand(torch.empty(_operand_bytes(rows, cols)[1], dtype=torch.uint8, device=device), rows, cols)
 
 
 def _quantize(x, s, rows_form: bool, cols_form: bool):
     """x (2-D) as an operand along its columns and, transposed, along its rows."""
     x, ld = _rows(x)
     r, c = x.shape
-    q = _operand(r, c, x.device) if rows_form else (None, None)
-    t = _operand(c, r, x.device) if cols_form else (None, None)
-    ptr = [None if b is None else b.data_ptr() for b in (*q, *t)]
-    lm._check(lm.lib().malt_block_quantize(x.data_ptr(), _DTYPES[x.dtype], r, c, ld, *ptr, s))
+    q = _Operand.empty(r, c, x.device) if rows_form else None
+    t = _Operand.empty(c, r, x.device) if cols_form else None
+    lm._check(lm.lib().malt_block_quantize(x.data_ptr(), _DTYPES[x.dtype], r, c, ld, q.values if q else None,
+                                           q.scales if q else None, t.values if t else None, t.scales if t else None, s))
     return q, t
 
 
 def _quantize_weight(w, s, plain: bool, transposed: bool):
+    """A weight's values, its block scales and its transpose's values."""
     w, ld = _rows(w)
     r, c = w.shape
     values = torch.empty((r, _pad(c, BLOCK)), dtype=torch.uint8, device=w.device) if plain else None
     t_values = torch.empty((c, _pad(r, BLOCK)), dtype=torch.uint8, device=w.device) if transposed else None
     scales = torch.empty((-(-r // BLOCK), -(-c // BLOCK)), dtype=torch.uint8, device=w.device)
     lm._check(lm.lib().malt_block_quantize_weight(w.data_ptr(), _DTYPES[w.dtype], r, c, ld,
-                                                  None if values is None else values.data_ptr(), scales.data_ptr(),
-                                                  None if t_values is None else t_values.data_ptr(), s))
+                                                  values.data_ptr() if plain else None, scales.data_ptr(),
+                                                  t_values.data_ptr() if transposed else None, s))
     return values, scales, t_values
 
 
-def _matmul(m, n, k, a, b, b_strides, dtype, device, s):
+@functools.lru_cache(maxsize=4096)
+def _matmul_size(m: int, n: int, k: int, out_type: int) -> int:
+    size = c_size_t(0)
+    lm._check(lm.lib().malt_block_matmul_size(m, n, k, out_type, byref(size)))
+    return size.value
+
+
+def _matmul(m, n, k, a: _Operand, b_values: int, b_scales: int, b_strides, dtype, device, s):
     """a b^T over k; b_strides: those of a weight's block scales, or None for an operand's."""
     out = torch.empty((m, n), dtype=dtype, device=device)
-    size = c_size_t(0)
-    lm._check(lm.lib().malt_block_matmul_size(m, n, k, byref(size)))
-    ws = torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None
+    size = _matmul_size(m, n, k, _DTYPES[dtype])
+    ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
     blocks, (i, j) = (0, (0, 0)) if b_strides is None else (1, b_strides)
-    lm._check(lm.lib().malt_block_matmul(m, n, k, a[0].data_ptr(), a[1].data_ptr(), b[0].data_ptr(), b[1].data_ptr(),
-                                         blocks, i, j, out.data_ptr(), _DTYPES[dtype], n, 0,
-                                         None if ws is None else ws.data_ptr(), size.value, s))
+    lm._check(lm.lib().malt_block_matmul(m, n, k, a.values, a.scales, b_values, b_scales, blocks, i, j, out.data_ptr(),
+                                         _DTYPES[dtype], n, 0, ws.data_ptr() if size else None, size, s))
     return out
 
 
 class _Fp8Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, out_dtype):
-        y, xt, wt = _linear(x, weight, out_dtype, None, ctx.needs_input_grad[1], ctx.needs_input_grad[0])
-        ctx.save_for_backward(*xt, *wt)
+        need_x, need_w = ctx.needs_input_grad[:2]
+        y, xt, wt, w_scales = _linear(x, weight, out_dtype, None, need_w, need_x)
+        ctx.save_for_backward(xt.buf if xt else None, wt, w_scales)
         ctx.args = (x.shape, x.dtype, weight.shape, weight.dtype)
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        xt_values, xt_scales, wt_values, w_scales = ctx.saved_tensors
+        xt, wt, w_scales = ctx.saved_tensors
         x_shape, x_dtype, (n, k), w_dtype = ctx.args
+        need_x, need_w = ctx.needs_input_grad[:2]
         dev = dy.device
         if dy.dtype not in _DTYPES:
             dy = dy.float()
         g = dy.reshape(-1, n)
         m = g.shape[0]
-        need_x, need_w = ctx.needs_input_grad[:2]
-        dx = dw = None
         if m == 0:
             return (torch.zeros(x_shape, dtype=x_dtype, device=dev) if need_x else None,
                     torch.zeros((n, k), dtype=w_dtype, device=dev) if need_w else None, None)
-        with _Call(dev, None) as s:
+
+        def work(s):
             q, t = _quantize(g, s, need_x, need_w)
+            dx = dw = None
             if need_x:
-                dx = _matmul(m, k, n, q, (wt_values, w_scales), (1, w_scales.shape[1]), x_dtype, dev, s).reshape(x_shape)
+                dx = _matmul(m, k, n, q, wt.data_ptr(), w_scales.data_ptr(), (1, w_scales.shape[1]), x_dtype, dev, s)
+                dx = dx.reshape(x_shape)
             if need_w:
-                dw = _matmul(n, k, m, t, (xt_values, xt_scales), None, w_dtype, dev, s)
-        return dx, dw, None
+                o = _Operand(xt, k, m)
+                dw = _matmul(n, k, m, t, o.values, o.scales, None, w_dtype, dev, s)
+            return dx, dw, None
+
+        return _on(dev, None, (), work)
 
 
 def _linear(x, weight, out_dtype, stream, keep_x, keep_w):
-    """The layer's output, and what its backward pass needs: x^T and W^T in 8 bits."""
+    """The layer's output, and what its backward pass needs: x^T and W^T in 8 bits, W's scales."""
     dev = x.device
     n, k = weight.shape
     flat = _flat(x) if x.dim() > 1 else x.reshape(1, -1)
     m = flat.shape[0]
-    xt, wt = (None, None), (None, None)
-    with _Call(dev, stream, x, weight) as s:
+
+    def work(s):
         if m == 0:
-            y = torch.empty((0, n), dtype=out_dtype, device=dev)
-        else:
-            q, xt = _quantize(flat, s, True, keep_x)
-            w_values, w_scales, wt_values = _quantize_weight(weight, s, True, keep_w)
-            if keep_w:
-                wt = (wt_values, w_scales)
-            y = _matmul(m, n, k, q, (w_values, w_scales), (w_scales.shape[1], 1), out_dtype, dev, s)
-    return y.reshape(*x.shape[:-1], n), xt, wt
+            return torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev), None, None, None
+        q, xt = _quantize(flat, s, True, keep_x)
+        values, scales, wt = _quantize_weight(weight, s, True, keep_w)
+        y = _matmul(m, n, k, q, values.data_ptr(), scales.data_ptr(), (scales.shape[1], 1), out_dtype, dev, s)
+        return y if x.dim() == 2 else y.reshape(*x.shape[:-1], n), xt, wt, scales
+
+    return _on(dev, stream, (x, weight), work)
 
 
 def _linear_args(x, k: int, out_dtype):
-    _tensor("x", x, _DTYPES)
     if x.dim() < 1 or x.shape[-1] != k:
         raise ValueError(f"x must be (..., {k}) (got {tuple(x.shape)})")
     out_dtype = x.dtype if out_dtype is None else out_dtype
     _type("out_dtype", out_dtype)
     return out_dtype
+
+
+def _weight(weight, device=None) -> None:
+    _tensor("weight", weight, _DTYPES, device)
+    if weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
+        raise ValueError(f"weight must be (outer, inner) (got {tuple(weight.shape)})")
 
 
 def fp8_linear(x: torch.Tensor, weight: torch.Tensor, out_dtype: Optional[torch.dtype] = None,
@@ -432,14 +470,12 @@ def fp8_linear(x: torch.Tensor, weight: torch.Tensor, out_dtype: Optional[torch.
     are float32; out_dtype: x's unless given.
 
     The backward pass runs in 8 bits too: the output's gradient by rows times
-    the same 8-bit weight, and the transposes of gradient and x, with a scale for each column and
-    128 tokens, for the weight's gradient (of weight's type).  Rounding to 8
-    bits passes gradients through unchanged."""
-    _tensor("weight", weight, _DTYPES)
-    if weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
-        raise ValueError(f"weight must be (outer, inner) (got {tuple(weight.shape)})")
+    the same 8-bit weight, and the transposes of gradient and x, with a scale for
+    each column and 128 tokens, for the weight's gradient (of weight's type).
+    Rounding to 8 bits passes gradients through unchanged."""
+    _tensor("x", x, _DTYPES)
+    _weight(weight, x.device)
     out_dtype = _linear_args(x, weight.shape[1], out_dtype)
-    _tensor("weight", weight, _DTYPES, x.device)
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad):
         _no_stream(stream)
         return _Fp8Linear.apply(x, weight, out_dtype)
@@ -451,12 +487,9 @@ def fp8_quantize_weight(weight: torch.Tensor, stream=None) -> Tuple[torch.Tensor
     float8_e4m3fn (outer, inner padded with zeros to whole blocks), and the
     exponent (plus 127) of each 128 x 128 block's power-of-two scale, uint8
     (outer blocks, inner blocks).  value * 2^(scale - 127) is what it stands for."""
-    _tensor("weight", weight, _DTYPES)
-    if weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
-        raise ValueError(f"weight must be (outer, inner) (got {tuple(weight.shape)})")
+    _weight(weight)
     weight = weight.detach()
-    with _Call(weight.device, stream, weight) as s:
-        values, scales, _ = _quantize_weight(weight, s, True, False)
+    values, scales, _ = _on(weight.device, stream, (weight,), lambda s: _quantize_weight(weight, s, True, False))
     return values.view(torch.float8_e4m3fn), scales
 
 
@@ -472,19 +505,23 @@ def fp8_forward(x: torch.Tensor, values: torch.Tensor, scales: torch.Tensor,
     if k < 1:
         raise ValueError(f"x must be (..., inner) (got {tuple(x.shape)})")
     out_dtype = _linear_args(x, k, out_dtype)
-    if values.dim() != 2 or values.shape[0] < 1 or values.shape[1] != _pad(k, BLOCK) or not values.is_contiguous():
-        raise ValueError(f"values must be contiguous, (outer, {_pad(k, BLOCK)}) (got {tuple(values.shape)}, "
+    kb = -(-k // BLOCK)
+    if values.dim() != 2 or values.shape[0] < 1 or values.shape[1] != kb * BLOCK or not values.is_contiguous():
+        raise ValueError(f"values must be contiguous, (outer, {kb * BLOCK}) (got {tuple(values.shape)}, "
                          f"strides {values.stride()})")
     n = values.shape[0]
-    if tuple(scales.shape) != (-(-n // BLOCK), _pad(k, BLOCK) // BLOCK) or not scales.is_contiguous():
-        raise ValueError(f"scales must be contiguous, ({-(-n // BLOCK)}, {_pad(k, BLOCK) // BLOCK}) "
+    if tuple(scales.shape) != (-(-n // BLOCK), kb) or not scales.is_contiguous():
+        raise ValueError(f"scales must be contiguous, ({-(-n // BLOCK)}, {kb}) "
                          f"(got {tuple(scales.shape)}, strides {scales.stride()})")
     x = x.detach()
     flat = _flat(x) if x.dim() > 1 else x.reshape(1, -1)
     m = flat.shape[0]
-    with _Call(dev, stream, x, values, scales) as s:
+
+    def work(s):
         if m == 0:
             return torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
         q, _ = _quantize(flat, s, True, False)
-        y = _matmul(m, n, k, q, (values, scales), (scales.shape[1], 1), out_dtype, dev, s)
-    return y.reshape(*x.shape[:-1], n)
+        y = _matmul(m, n, k, q, values.data_ptr(), scales.data_ptr(), (kb, 1), out_dtype, dev, s)
+        return y if x.dim() == 2 else y.reshape(*x.shape[:-1], n)
+
+    return _on(dev, stream, (x, values, scales), work)

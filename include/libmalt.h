@@ -399,6 +399,17 @@ malt_status_t malt_block_matmul(int64_t m, int64_t n, int64_t k, const void* a_v
                                 int64_t b_col_stride, void* out, malt_dtype_t out_type, int64_t ldo,
                                 int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
+/* A linear layer on a kept weight (malt_block_quantize_weight's values and
+ * block_scales, n x k): x (m x k) is brought to 8 bits and multiplied,
+ * out (m x n) = x w^T; up to 32 rows in one launch.  Types and limits as above.
+ * workspace: device memory of malt_block_linear_size's bytes (may be 0; then
+ * NULL), 256-byte aligned. */
+malt_status_t malt_block_linear_size(int64_t m, int64_t n, int64_t k, malt_dtype_t out_type, size_t* workspace_bytes);
+malt_status_t malt_block_linear(const void* x, malt_dtype_t x_type, int64_t m, int64_t k, int64_t ldx,
+                                const void* w_values, const void* w_scales, int64_t n, void* out,
+                                malt_dtype_t out_type, int64_t ldo, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
 const char* malt_status_string(malt_status_t status);
 const char* malt_last_error(void);
 const char* malt_version(void);

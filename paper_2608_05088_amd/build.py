@@ -17,7 +17,8 @@ LIB = os.path.join(PKG, "lib", "libmalt.so")
 CALIB = os.path.join(PKG, "calib")
 CALIB_LIB = os.path.join(PKG, "lib", "libmalt_calib.so")
 SOURCES = ["malt_api.hip", "elementwise.hip", "ns_sym.hip", "ns_update.hip", "ns_mid.hip", "small_ns.hip",
-           "embed.hip", "distill.hip", "block_quant.hip", "block_matmul.hip", "ops_api.hip"]
+           "embed.hip", "distill.hip", "block_quant.hip", "block_matmul.hip", "block_linear.hip",
+           "ops_api.hip"]
 ARCH = "gfx950"
 
 

@@ -1,5 +1,5 @@
 // 8-bit operands with a power-of-two scale for each block of 128 values: layout,
-// arguments and launchers (block_quant.hip, block_matmul.hip).
+// arguments and launchers (block_quant.hip, block_matmul.hip, block_linear.hip).
 //
 // An operand of `rows` rows over a contraction of `cols` values is
 //   values  [rows][pad128(cols)] bytes (4 exponent, 3 mantissa bits), zeros past cols;
@@ -45,6 +45,19 @@ struct BlockMatmulArgs {
   bool by_four;     // set by the launcher: four columns of out at a time
   int32_t parts;    // and the parts the contraction is cut into
 };
+
+// A linear layer on kept weights, x (m x k) W^T, for m <= BLOCK_FEW rows.
+constexpr int BLOCK_FEW = 32;
+struct BlockLinearArgs {
+  const void* x;
+  int64_t m, n, k, ldx;
+  const uint8_t* w;         // n x pad128(k)
+  const uint8_t* w_scales;  // [n / 128][k / 128]
+  void* out;
+  int64_t ldo;
+  bool by_four;             // set by the launcher
+};
+hipError_t launch_block_linear(BlockLinearArgs g, bool x_f32, bool out_f32, hipStream_t s);
 
 // How a product is tiled, by its sizes and the type of its result.
 struct BlockMatmulPlan {

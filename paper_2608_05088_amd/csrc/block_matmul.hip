@@ -20,7 +20,7 @@
 // first operand is B, so that a lane ends up with four consecutive columns.
 #include <type_traits>
 
-#include "block_fp8.h"
+#include "block_mma.h"
 #include "ns_common.h"
 #include "ops_common.h"
 
@@ -34,7 +34,6 @@ using ns::dma16;
 using ns::f32x4;
 using ns::i32x4;
 using ns::lds_u32;
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // 4 bytes a lane into LDS, as dma16.
 __device__ __forceinline__ void dma4(const i32x4& rsrc, uint32_t voff, uint32_t soff, uint32_t lds_addr) {
@@ -44,28 +43,10 @@ __device__ __forceinline__ void dma4(const i32x4& rsrc, uint32_t voff, uint32_t 
                : "memory");
 }
 
-// c += (2^sb B) (2^sa A)^T of one block; byte OB / OA of the scale registers counts.
-template <int OB, int OA>
-__device__ __forceinline__ f32x4 mma(i32x8 b, i32x8 a, f32x4 c, int sb, int sa) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, OB, sb, OA, sa);
-}
-__device__ __forceinline__ f32x4 mma_sel(i32x8 b, i32x8 a, f32x4 c, int sb, int ob, int sa, int oa) {
-  // ob, oa are constants after unrolling
-  switch (ob * 4 + oa) {
-#define MALT_SEL(x, y) case x * 4 + y: return mma<x, y>(b, a, c, sb, sa);
-    MALT_SEL(0, 0) MALT_SEL(0, 1) MALT_SEL(0, 2) MALT_SEL(0, 3)
-    MALT_SEL(1, 0) MALT_SEL(1, 1) MALT_SEL(1, 2) MALT_SEL(1, 3)
-    MALT_SEL(2, 0) MALT_SEL(2, 1) MALT_SEL(2, 2) MALT_SEL(2, 3)
-    MALT_SEL(3, 0) MALT_SEL(3, 1) MALT_SEL(3, 2) default: return mma<3, 3>(b, a, c, sb, sa);
-#undef MALT_SEL
-  }
-}
-
 // TM x TN tile, WM x WN waves of SM x SN each.
-template <int TM_, int TN_, int WM_, int WN_, int STAGES_, int WPE_>
+template <int TM_, int TN_, int WM_, int WN_, int WPE_>
 struct MmGeom {
   static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, WPE = WPE_;
-  static constexpr int STAGES = STAGES_;                     // slots of the LDS ring
   static constexpr int NW = WM * WN, NT = 64 * NW;
   static constexpr int SM = TM / WM, SN = TN / WN;
   static constexpr int MB = SM / 16, NB = SN / 16;           // 16-row blocks of a wave
@@ -75,24 +56,10 @@ struct MmGeom {
   static_assert(LOADS * NW * 8 == TM + TN && A_LOADS % NW == 0, "loads split evenly over the waves");
   static_assert(SN <= 64 && 64 % SN == 0 && SM <= 128 && 128 % SM == 0, "a wave's scales lie in one group");
   static_assert(MB % 4 == 0, "row blocks are taken in pairs, an even number of times");
-  static_assert(SLOT % 16 == 0 && STAGES * SLOT <= 160 * 1024, "slots are aligned, the ring fits");
+  static_assert(SLOT % 16 == 0 && 2 * SLOT <= 160 * 1024, "slots are aligned, the ring fits");
 };
 
 __device__ __forceinline__ int swz(int row, int chunk) { return row * QB + ((chunk ^ ((row >> 1) & 7)) << 4); }
-
-// Eight 8-bit values (two dwords) times 2^e as bf16, exactly; `scale` is 2^e.
-__device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)lo, scale, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)lo, scale, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)hi, scale, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)hi, scale, true);
-  return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
-}
-// The power of two of exponent byte i of a scale register.
-__device__ __forceinline__ float scale_of(int bytes, int i) {
-  return __uint_as_float((((uint32_t)bytes >> (8 * i)) & 0xffu) << 23);
-}
 
 template <class G, bool BLOCKS, bool WIDE, bool SPLIT, class TO>
 __global__ __launch_bounds__(G::NT) __attribute__((amdgpu_waves_per_eu(G::WPE, G::WPE)))
@@ -140,9 +107,8 @@ void block_matmul_kernel(BlockMatmulArgs g) {
   const int64_t s_pitch = b_wave ? sb_pitch : sa_pitch;
   const int s_lanes = (b_wave ? G::TN : G::TM) / 4, s_dst = G::A_BYTES + G::B_BYTES + (b_wave ? G::TM : 0);
   const uint32_t lds0 = lds_u32(lds);
-  auto slot_of = [](int kt) { return (G::STAGES & (G::STAGES - 1)) ? kt % G::STAGES : kt & (G::STAGES - 1); };
   auto issue = [&](int kt) {
-    const uint32_t at = lds0 + slot_of(kt) * G::SLOT, soff = (uint32_t)kt * QB;
+    const uint32_t at = lds0 + (kt & 1) * G::SLOT, soff = (uint32_t)kt * QB;
 #pragma unroll
     for (int q = 0; q < G::LOADS; ++q) dma16(q < G::A_LOADS / G::NW ? rs_a : rs_b, voff[q], soff, at + dst[q]);
     if (lane < s_lanes) dma4(rs_s, 4 * lane, (uint32_t)(kt * s_pitch), at + s_dst);
@@ -185,14 +151,17 @@ void block_matmul_kernel(BlockMatmulArgs g) {
     else sb = *reinterpret_cast<const int*>(st + off_sb);
   };
 
-  // At the barrier that closes stage kt, stage kt + 1 has landed and every wave
-  // holds the rest of stage kt in registers, so its slot takes stage kt + STAGES.
-  constexpr int STAGES = G::STAGES;
+  // Two slots: at the barrier that closes stage kt, stage kt + 1 has landed and
+  // every wave holds the rest of stage kt in registers, so its slot takes stage
+  // kt + 2.
   if constexpr (BLOCKS) weight_scales(0);
-#pragma unroll
-  for (int i = 0; i < STAGES; ++i)
-    if (i < KT) issue(i);
-  ns::wait_vm(min(STAGES - 1, KT - 1) * IN_FLIGHT);
+  issue(0);
+  if (KT > 1) {
+    issue(1);
+    ns::wait_vm_c<IN_FLIGHT>();
+  } else {
+    ns::wait_vm_c<0>();
+  }
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   int sa[SAW], sb;
@@ -202,13 +171,10 @@ void block_matmul_kernel(BlockMatmulArgs g) {
     if constexpr (BLOCKS)
       if (((kt + 1) & 63) == 0) weight_scales(kt + 1);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's reads of stage kt are done
-    // In flight: stages kt + 2 .. kt + STAGES - 1, where they exist.
-    if constexpr (STAGES == 2) ns::wait_vm_c<0>();
-    else if (kt + STAGES <= KT) ns::wait_vm_c<(STAGES - 2) * IN_FLIGHT>();
-    else ns::wait_vm_c<0>();
+    ns::wait_vm_c<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (kt + STAGES < KT) issue(kt + STAGES);
+    if (kt + 2 < KT) issue(kt + 2);
     return true;
   };
 
@@ -220,8 +186,8 @@ void block_matmul_kernel(BlockMatmulArgs g) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) fb[b] = frag(lds, off_b, b);
     for (int kt = 0; kt < KT; ++kt) {
-      const char* st = lds + slot_of(kt) * G::SLOT;
-      const char* nx = lds + slot_of(kt + 1) * G::SLOT;
+      const char* st = lds + (kt & 1) * G::SLOT;
+      const char* nx = lds + (~kt & 1) * G::SLOT;
       int sa_next[SAW], sb_next = sb;
 #pragma unroll
       for (int i = 0; i < SAW; ++i) sa_next[i] = sa[i];
@@ -282,8 +248,8 @@ void block_matmul_kernel(BlockMatmulArgs g) {
     for (int b = 0; b < NB; ++b) open(fb[b], chunk(lds, off_b[0], b), scale_of(sb, BLOCKS ? 0 : b));
     ra[1] = chunk(lds, off_a[0], 1);
     for (int kt = 0; kt < KT; ++kt) {
-      const char* st = lds + slot_of(kt) * G::SLOT;
-      const char* nx = lds + slot_of(kt + 1) * G::SLOT;
+      const char* st = lds + (kt & 1) * G::SLOT;
+      const char* nx = lds + (~kt & 1) * G::SLOT;
       int sa_next[SAW], sb_next = sb;
 #pragma unroll
       for (int i = 0; i < SAW; ++i) sa_next[i] = sa[i];
@@ -395,13 +361,13 @@ __global__ __launch_bounds__(256) void block_sum_kernel(BlockMatmulArgs g) {
 
 // Rings of two slots; with three or four, and one workgroup a CU, the 128-tile ran
 // 5 to 10% slower: what a stage of few workgroups waits for is LDS, not memory.
-using Mm256 = MmGeom<256, 256, 2, 4, 2, 2>;
-using Mm128 = MmGeom<128, 128, 2, 2, 2, 2>;   // two workgroups a CU
+using Mm256 = MmGeom<256, 256, 2, 4, 2>;
+using Mm128 = MmGeom<128, 128, 2, 2, 2>;   // two workgroups a CU
 
 template <class G, bool BLOCKS, bool SPLIT, class TO>
 hipError_t launch_tiled(const BlockMatmulArgs& a, hipStream_t s) {
   const auto kernel = &block_matmul_kernel<G, BLOCKS, std::is_same<TO, float>::value, SPLIT, TO>;
-  constexpr int bytes = G::STAGES * G::SLOT;
+  constexpr int bytes = 2 * G::SLOT;
   // More LDS than the default limit: raised each time, for whichever device is current.
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, bytes);

@@ -6,34 +6,12 @@
 // Bound by memory: one workgroup reads a 128 x 128 tile once, into registers,
 // and writes what is wanted of it: the rows' form (blocks along a row), the
 // transpose's (blocks along a column), or both under one scale (a weight).
-#include "block_fp8.h"
+#include "block_mma.h"
 #include "ops_common.h"
 
 namespace malt {
 
 namespace {
-
-// Largest magnitude as a bit pattern: an infinity or a NaN is larger than any number.
-__device__ __forceinline__ uint32_t mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
-
-// Exponent byte of the scale for a largest magnitude: 448 = 1.75 * 2^8; 255 (not
-// a number) where the block holds an infinity or a NaN.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t b) {
-  if (b >= 0x7f800000u) return 255u;
-  if (b == 0) return 127u;
-  const int e = (int)(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return e < 0 ? 0u : (uint32_t)e;
-}
-// 1 / s, exact; NaN for a block that holds an infinity or a NaN.
-__device__ __forceinline__ float scale_inverse(uint32_t byte) {
-  return __uint_as_float(byte < 254u ? (254u - byte) << 23 : 0x7fc00000u);
-}
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
-  return (uint32_t)r;
-}
 
 // Maximum over the 16 lanes of a row of lanes, in every one of them.
 __device__ __forceinline__ uint32_t max16(uint32_t v) {
@@ -42,35 +20,6 @@ __device__ __forceinline__ uint32_t max16(uint32_t v) {
   v = umax(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, true));
   v = umax(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, true));
   return v;
-}
-
-template <bool VEC>
-__device__ __forceinline__ void load8(const float* row, int c, int cols, float (&v)[8]) {
-  if (VEC && c + 8 <= cols) {
-    const op_f32x4 a = load4(row + c), b = load4(row + c + 4);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[j] = a[j];
-      v[4 + j] = b[j];
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? gptr(row)[c + j] : 0.f;
-  }
-}
-template <bool VEC>
-__device__ __forceinline__ void load8(const bf16_t* row, int c, int cols, float (&v)[8]) {
-  if (VEC && c + 8 <= cols) {
-    const op_u32x4 r = *reinterpret_cast<const MALT_GLOBAL op_u32x4*>(gptr(row) + c);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[2 * j] = bf16_lo(r[j]);
-      v[2 * j + 1] = bf16_hi(r[j]);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? to_f32(gptr(row)[c + j]) : 0.f;
-  }
 }
 
 // Thread (rg, cg) holds rows 8 rg .. + 7, columns 8 cg .. + 7 of the tile.

@@ -55,6 +55,15 @@ malt_status_t check_table(int64_t tokens, int64_t vocab, int64_t width) {
 
 malt_status_t launched(hipError_t e, const char* what) { return e == hipSuccess ? MALT_OK : hip_fail(e, what); }
 
+malt_status_t check_workspace(const void* p, size_t bytes, size_t need) {
+  if (need > 0 && !p) return fail(MALT_ERR_INVALID_ARG, "workspace is NULL");
+  if (!op_aligned(p, 256)) return fail(MALT_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+  if (bytes < need) return fail(MALT_ERR_INVALID_ARG, "a workspace of %zu bytes where %zu are needed", bytes, need);
+  return MALT_OK;
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
 #define MALT_TRY(expr)                          \
   do {                                          \
     const malt_status_t st_ = (expr);           \
@@ -113,10 +122,7 @@ malt_status_t malt_embed_grad(const void* ids, malt_index_t id_type, int64_t tok
   MALT_TRY(check_mat(g));
   MALT_TRY(check_mat(d));
   const EmbedGradLayout L = embed_grad_layout(tokens, vocab, width);
-  if (L.bytes > 0 && !workspace) return fail(MALT_ERR_INVALID_ARG, "workspace is NULL");
-  if (!op_aligned(workspace, 256)) return fail(MALT_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
-  if (workspace_bytes < L.bytes)
-    return fail(MALT_ERR_INVALID_ARG, "a workspace of %zu bytes where %zu are needed", workspace_bytes, L.bytes);
+  MALT_TRY(check_workspace(workspace, workspace_bytes, L.bytes));
   const size_t id_bytes = size_t(tokens) * (id_type == MALT_INT64 ? 8 : 4);
   if (op_overlap(dtable, d.bytes(), grad, g.bytes()) || op_overlap(dtable, d.bytes(), ids, id_bytes))
     return fail(MALT_ERR_ALIAS, "dtable overlaps the gradient or the ids");
@@ -298,16 +304,11 @@ malt_status_t malt_block_matmul(int64_t m, int64_t n, int64_t k, const void* a_v
   if (op_overlap(out, o.bytes(), a_values, av) || op_overlap(out, o.bytes(), a_scales, as) ||
       op_overlap(out, o.bytes(), b_values, bv) || op_overlap(out, o.bytes(), b_scales, bs))
     return fail(MALT_ERR_ALIAS, "out overlaps an operand");
-  if (need > 0) {
-    if (!workspace) return fail(MALT_ERR_INVALID_ARG, "workspace is NULL");
-    if (!op_aligned(workspace, 256)) return fail(MALT_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
-    if (workspace_bytes < need)
-      return fail(MALT_ERR_INVALID_ARG, "a workspace of %zu bytes where %zu are needed", workspace_bytes, need);
-    if (op_overlap(workspace, need, out, o.bytes()) || op_overlap(workspace, need, a_values, av) ||
-        op_overlap(workspace, need, a_scales, as) || op_overlap(workspace, need, b_values, bv) ||
-        op_overlap(workspace, need, b_scales, bs))
-      return fail(MALT_ERR_ALIAS, "workspace overlaps another buffer");
-  }
+  MALT_TRY(check_workspace(workspace, workspace_bytes, need));
+  if (op_overlap(workspace, need, out, o.bytes()) || op_overlap(workspace, need, a_values, av) ||
+      op_overlap(workspace, need, a_scales, as) || op_overlap(workspace, need, b_values, bv) ||
+      op_overlap(workspace, need, b_scales, bs))
+    return fail(MALT_ERR_ALIAS, "workspace overlaps another buffer");
   BlockMatmulArgs g = {};
   g.m = m;
   g.n = n;
@@ -324,6 +325,56 @@ malt_status_t malt_block_matmul(int64_t m, int64_t n, int64_t k, const void* a_v
   g.partial = static_cast<float*>(workspace);
   return launched(launch_block_matmul(g, b_blocks != 0, out_type == MALT_FLOAT32, static_cast<hipStream_t>(stream)),
                   "launching the 8-bit product");
+}
+
+malt_status_t malt_block_linear_size(int64_t m, int64_t n, int64_t k, malt_dtype_t out_type, size_t* workspace_bytes) {
+  size_t product, values, scales;
+  MALT_TRY(malt_block_matmul_size(m, n, k, out_type, workspace_bytes));
+  product = *workspace_bytes;
+  MALT_TRY(malt_block_size(m, k, &values, &scales));
+  *workspace_bytes = m <= BLOCK_FEW ? 0 : align256(product) + values + scales;
+  return MALT_OK;
+}
+
+malt_status_t malt_block_linear(const void* x, malt_dtype_t x_type, int64_t m, int64_t k, int64_t ldx,
+                                const void* w_values, const void* w_scales, int64_t n, void* out,
+                                malt_dtype_t out_type, int64_t ldo, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  size_t need, values, scales, wv, ws;
+  MALT_TRY(malt_block_linear_size(m, n, k, out_type, &need));
+  MALT_TRY(malt_block_size(m, k, &values, &scales));
+  MALT_TRY(malt_block_size(n, k, &wv, &ws));
+  ws = size_t(q_pad(n) / QB) * (q_pad(k) / QB);
+  const Mat xm = {"x", x, x_type, m, k, ldx}, o = {"out", out, out_type, m, n, ldo};
+  MALT_TRY(check_mat(xm));
+  MALT_TRY(check_mat(o));
+  if (!w_values || !w_scales) return fail(MALT_ERR_INVALID_ARG, "the weight is NULL");
+  if (!op_aligned(w_values, 16)) return fail(MALT_ERR_ALIGNMENT, "the weight's values are not 16-byte aligned");
+  if (op_overlap(out, o.bytes(), x, xm.bytes()) || op_overlap(out, o.bytes(), w_values, wv) ||
+      op_overlap(out, o.bytes(), w_scales, ws))
+    return fail(MALT_ERR_ALIAS, "out overlaps x or the weight");
+  MALT_TRY(check_workspace(workspace, workspace_bytes, need));
+  if (op_overlap(workspace, need, out, o.bytes()) || op_overlap(workspace, need, x, xm.bytes()) ||
+      op_overlap(workspace, need, w_values, wv) || op_overlap(workspace, need, w_scales, ws))
+    return fail(MALT_ERR_ALIAS, "workspace overlaps another buffer");
+  if (m <= BLOCK_FEW) {
+    BlockLinearArgs g = {};
+    g.x = x;
+    g.m = m;
+    g.n = n;
+    g.k = k;
+    g.ldx = ldx;
+    g.w = static_cast<const uint8_t*>(w_values);
+    g.w_scales = static_cast<const uint8_t*>(w_scales);
+    g.out = out;
+    g.ldo = ldo;
+    return launched(launch_block_linear(g, x_type == MALT_FLOAT32, out_type == MALT_FLOAT32, static_cast<hipStream_t>(stream)),
+                    "launching the 8-bit layer");
+  }
+  char* const q = static_cast<char*>(workspace) + (need - values - scales);
+  MALT_TRY(malt_block_quantize(x, x_type, m, k, ldx, q, q + values, nullptr, nullptr, stream));
+  return malt_block_matmul(m, n, k, q, q + values, w_values, w_scales, 1, q_pad(k) / QB, 1, out, out_type, ldo, 0,
+                           workspace, need - values - scales, stream);
 }
 
 }  // extern "C"

@@ -127,6 +127,9 @@ _SIGNATURES = [
     ("malt_block_matmul_size", c_int32, [c_int64, c_int64, c_int64, c_int32, POINTER(c_size_t)]),
     ("malt_block_matmul", c_int32, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int64,
                                     c_int64, c_void_p, c_int32, c_int64, c_int32, c_void_p, c_size_t, c_void_p]),
+    ("malt_block_linear_size", c_int32, [c_int64, c_int64, c_int64, c_int32, POINTER(c_size_t)]),
+    ("malt_block_linear", c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_int64, c_void_p,
+                                    c_int32, c_int64, c_void_p, c_size_t, c_void_p]),
     ("malt_destroy_state", None, [c_void_p]),
     ("malt_status_string", c_char_p, [c_int32]),
     ("malt_last_error", c_char_p, []),

@@ -206,7 +206,7 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
     dev = logits.device
     if logits.dim() < 1 or logits.shape[-1] < 1:
         raise ValueError(f"logits must be (..., vocab) (got {tuple(logits.shape)})")
-    lead, v = tuple(logits.shape[:-1]), logits.shape[-1]
+    lead, v = logits.shape[:-1], logits.shape[-1]
     tau, alpha = float(tau), float(alpha)
     if not (math.isfinite(tau) and tau > 0):
         raise ValueError(f"tau must be finite and > 0 (got {tau})")
@@ -214,47 +214,47 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         raise ValueError(f"alpha must be in [0, 1] (got {alpha})")
     z, ld = _rows(_flat(logits) if logits.dim() > 1 else logits.reshape(1, v))
     n = z.shape[0]
-    a = lm.malt_distill_t()
-    a.logits, a.dtype, a.rows, a.vocab, a.ld = z.data_ptr(), _DTYPES[z.dtype], n, v, ld
-    keep = [z]
+    zt = _DTYPES[z.dtype]
+    # Teacher: pointers, types and pitches of its logits and ids.
+    t = i = y = w = None
+    tp = ip = None
+    tt = it = k = tld = ild = 0
     if (top_logits is None) != (top_ids is None):
         raise ValueError("top_logits and top_ids come together")
     if top_logits is not None:
         _tensor("top_logits", top_logits, _DTYPES, dev)
         _tensor("top_ids", top_ids, _INDEX, dev)
-        if tuple(top_logits.shape[:-1]) != lead or top_logits.shape != top_ids.shape:
-            raise ValueError(f"top_logits and top_ids must be {lead} + (k,) (got {tuple(top_logits.shape)}, "
+        if top_logits.shape[:-1] != lead or top_logits.shape != top_ids.shape:
+            raise ValueError(f"top_logits and top_ids must be {tuple(lead)} + (k,) (got {tuple(top_logits.shape)}, "
                              f"{tuple(top_ids.shape)})")
         k = top_logits.shape[-1]
         if k > lm.DISTILL_MAX_TOP:
             raise ValueError(f"at most {lm.DISTILL_MAX_TOP} teacher entries a row (got {k})")
         if k > 0:
-            t, tld = _rows(top_logits.reshape(n, k))
-            i, ild = _rows(top_ids.reshape(n, k))
-            a.top, a.top_type, a.top_ids, a.id_type = t.data_ptr(), _DTYPES[t.dtype], i.data_ptr(), _INDEX[i.dtype]
-            a.n_top, a.top_ld, a.id_ld = k, tld, ild
-            keep += [t, i]
+            t, tld = _rows(top_logits if top_logits.dim() == 2 else top_logits.reshape(n, k))
+            i, ild = _rows(top_ids if top_ids.dim() == 2 else top_ids.reshape(n, k))
+            tp, tt, ip, it = t.data_ptr(), _DTYPES[t.dtype], i.data_ptr(), _INDEX[i.dtype]
+    yp, yt = None, 0
     if labels is not None:
         _tensor("labels", labels, _INDEX, dev)
-        if tuple(labels.shape) != lead:
-            raise ValueError(f"labels must be {lead} (got {tuple(labels.shape)})")
+        if labels.shape != lead:
+            raise ValueError(f"labels must be {tuple(lead)} (got {tuple(labels.shape)})")
         y = labels.reshape(-1).contiguous()
-        a.labels, a.label_type = y.data_ptr(), _INDEX[y.dtype]
-        keep.append(y)
-    a.tau, a.alpha = tau, alpha
+        yp, yt = y.data_ptr(), _INDEX[y.dtype]
+    wp, w_stride, w_value = None, 0, 1.0
     if isinstance(weight, torch.Tensor):
         _tensor("grad", weight, (torch.float32,), dev)
         if weight.dim() == 0:
-            w, a.weight_stride = weight, 0
-        elif tuple(weight.shape) == lead:
+            w = weight
+        elif weight.shape == lead:
             w = weight.reshape(-1)
-            a.weight_stride = w.stride(0) if n > 1 else 0
+            w_stride = w.stride(0) if n > 1 else 0
         else:
-            raise ValueError(f"grad must be a number, a scalar tensor or {lead} (got {tuple(weight.shape)})")
-        a.weights = w.data_ptr()
-        keep.append(w)
+            raise ValueError(f"grad must be a number, a scalar tensor or {tuple(lead)} (got {tuple(weight.shape)})")
+        wp = w.data_ptr()
     else:
-        a.weight = float(weight)
+        w_value = float(weight)
+    d, dld = None, v
     if out is not None:
         _tensor("out", out, (logits.dtype,), dev)
         if out.shape != logits.shape:
@@ -262,23 +262,20 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         d = out if out.dim() == 2 else out.view(-1, v)   # a view, or an error: the result is written through it
         if (v > 1 and d.stride(1) != 1) or (n > 1 and d.stride(0) < v):
             raise ValueError(f"out must have contiguous rows (got strides {out.stride()})")
-        keep.append(out)
+        dld = d.stride(0) if n > 1 else v
+
     def work(s):
-        losses = grad = None
-        if want_loss:
-            losses = torch.empty(lead, dtype=torch.float32, device=dev)
-            a.losses = losses.data_ptr()
-        if want_grad:
-            if out is None:
-                grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-                a.dlogits, a.dld = grad.data_ptr(), v
-            else:
-                grad = out
-                a.dlogits, a.dld = d.data_ptr(), (d.stride(0) if n > 1 else v)
+        losses = torch.empty(lead, dtype=torch.float32, device=dev) if want_loss else None
+        grad = out
+        if want_grad and out is None:
+            grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        a = lm.malt_distill_t(z.data_ptr(), zt, n, v, ld, tp, tt, ip, it, k, tld, ild, yp, yt, tau, alpha, wp, w_stride,
+                              w_value, losses.data_ptr() if want_loss else None,
+                              (grad if d is None else d).data_ptr() if want_grad else None, dld)
         lm._check(lm.lib().malt_distill(byref(a), s))
         return losses, grad
 
-    return _on(dev, stream, keep, work)
+    return _on(dev, stream, (z, t, i, y, w, out), work)
 
 
 class _DistillLoss(torch.autograd.Function):
@@ -391,6 +388,13 @@ def _matmul(m, n, k, a: _Operand, b_values: int, b_scales: int, b_strides, dtype
     lm._check(lm.lib().malt_block_matmul(m, n, k, a.values, a.scales, b_values, b_scales, blocks, i, j, out.data_ptr(),
                                          _DTYPES[dtype], n, 0, ws.data_ptr() if size else None, size, s))
     return out
+
+
+@functools.lru_cache(maxsize=4096)
+def _linear_size(m: int, n: int, k: int, out_type: int) -> int:
+    size = c_size_t(0)
+    lm._check(lm.lib().malt_block_linear_size(m, n, k, out_type, byref(size)))
+    return size.value
 
 
 class _Fp8Linear(torch.autograd.Function):
@@ -517,11 +521,16 @@ def fp8_forward(x: torch.Tensor, values: torch.Tensor, scales: torch.Tensor,
     flat = _flat(x) if x.dim() > 1 else x.reshape(1, -1)
     m = flat.shape[0]
 
-    def work(s):
-        if m == 0:
-            return torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
-        q, _ = _quantize(flat, s, True, False)
-        y = _matmul(m, n, k, q, values.data_ptr(), scales.data_ptr(), (kb, 1), out_dtype, dev, s)
-        return y if x.dim() == 2 else y.reshape(*x.shape[:-1], n)
+    flat, ld = _rows(flat)
+    size = _linear_size(m, n, k, _DTYPES[out_dtype]) if m else 0
 
-    return _on(dev, stream, (x, values, scales), work)
+    def work(s):
+        y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
+        if m:
+            ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+            lm._check(lm.lib().malt_block_linear(flat.data_ptr(), _DTYPES[x.dtype], m, k, ld, values.data_ptr(),
+                                                 scales.data_ptr(), n, y.data_ptr(), _DTYPES[out_dtype], n,
+                                                 ws.data_ptr() if size else None, size, s))
+        return y
+
+    return _on(dev, stream, (flat, values, scales), work)

@@ -279,8 +279,7 @@ void malt_destroy_state(malt_plan_t* plan);
  * Operators of a training step around the optimizer: the token table, the
  * distillation loss and linear layers in 8-bit floating point.  They need no
  * plan.  Matrices are row-major with a row pitch (`ld`, in elements, >= the
- * row's length); pointers are aligned to their element type, and rows of
- * 16-byte-aligned start and pitch take a vectorised path.  Work is enqueued on
+ * row's length); pointers are aligned to their element type.  Work is enqueued on
  * `stream`, which must belong to the current device; nothing waits on the host
  * and nothing is allocated.  A buffer that is written may overlap no other
  * unless stated (MALT_ERR_ALIAS).  An empty product of sizes enqueues nothing
@@ -344,8 +343,9 @@ typedef struct {
   const void* top_ids;       /* rows x n_top, pitch id_ld */
   malt_index_t id_type;
   int64_t n_top, top_ld, id_ld;
-  const void* labels;        /* rows */
+  const void* labels;        /* rows, one every label_stride elements */
   malt_index_t label_type;
+  int64_t label_stride;
   float tau, alpha;
   const float* weights;
   int64_t weight_stride;

@@ -42,8 +42,7 @@ struct BlockMatmulArgs {
   int64_t ldo;
   bool accumulate;
   float* partial;   // parts > 1: [part][tile][rows][columns]
-  bool by_four;     // set by the launcher: four columns of out at a time
-  int32_t parts;    // and the parts the contraction is cut into
+  int32_t parts;    // set by the launcher: parts the contraction is cut into
 };
 
 // A linear layer on kept weights, x (m x k) W^T, for m <= BLOCK_FEW rows.
@@ -55,9 +54,8 @@ struct BlockLinearArgs {
   const uint8_t* w_scales;  // [n / 128][k / 128]
   void* out;
   int64_t ldo;
-  bool by_four;             // set by the launcher
 };
-hipError_t launch_block_linear(BlockLinearArgs g, bool x_f32, bool out_f32, hipStream_t s);
+hipError_t launch_block_linear(const BlockLinearArgs& g, bool x_f32, bool out_f32, hipStream_t s);
 
 // How a product is tiled, by its sizes and the type of its result.
 struct BlockMatmulPlan {

@@ -21,7 +21,7 @@ using ns::i32x4;
 
 constexpr int FEW_WAVES = 8;
 
-template <class T, bool VEC, int MB, int NB, class TO>
+template <class T, int MB, int NB, class TO>
 __global__ __launch_bounds__(64 * FEW_WAVES) void block_linear_kernel(BlockLinearArgs g) {
   constexpr bool WIDE = std::is_same<TO, float>::value;
   __shared__ f32x4 sums[FEW_WAVES][MB * NB][64];
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void block_linear_kernel(BlockLinea
       uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        load8<VEC>(x[a], kt * QB + k_lane + 8 * i, (int)g.k, v[i]);
+        load8(x[a], kt * QB + k_lane + 8 * i, (int)g.k, v[i]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = umax(top, mag(v[i][j]));
       }
@@ -107,40 +107,29 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void block_linear_kernel(BlockLinea
     const int m = 16 * (q / NB) + (l & 15);
     const int64_t n = n0 + 16 * (q % NB) + 4 * (l >> 4);
     if (m >= g.m) continue;
-    TO* out = static_cast<TO*>(g.out) + m * g.ldo + n;
-    if (g.by_four) {
-      if (n < g.n) store4(out, op_f32x4{v[0], v[1], v[2], v[3]});
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (n + e < g.n) gptr(out)[e] = from_f32<TO>(v[e]);
-    }
+    row_store4(static_cast<TO*>(g.out) + m * g.ldo, n, g.n, op_f32x4{v[0], v[1], v[2], v[3]});
   }
 }
 
-template <class T, bool VEC, int MB, class TO>
+template <class T, int MB, class TO>
 void few_rows(const BlockLinearArgs& g, hipStream_t s) {
   const int64_t blocks = (g.n + 15) / 16;
-  if (blocks <= 384) hipLaunchKernelGGL((block_linear_kernel<T, VEC, MB, 1, TO>), dim3((unsigned)blocks), dim3(64 * FEW_WAVES), 0, s, g);
-  else hipLaunchKernelGGL((block_linear_kernel<T, VEC, MB, 2, TO>), dim3((unsigned)((blocks + 1) / 2)), dim3(64 * FEW_WAVES), 0, s, g);
+  if (blocks <= 384) hipLaunchKernelGGL((block_linear_kernel<T, MB, 1, TO>), dim3((unsigned)blocks), dim3(64 * FEW_WAVES), 0, s, g);
+  else hipLaunchKernelGGL((block_linear_kernel<T, MB, 2, TO>), dim3((unsigned)((blocks + 1) / 2)), dim3(64 * FEW_WAVES), 0, s, g);
 }
 template <class T, class TO>
-void few_typed(const BlockLinearArgs& g, bool vec, hipStream_t s) {
-  if (vec && g.m <= 16) few_rows<T, true, 1, TO>(g, s);
-  else if (vec) few_rows<T, true, 2, TO>(g, s);
-  else if (g.m <= 16) few_rows<T, false, 1, TO>(g, s);
-  else few_rows<T, false, 2, TO>(g, s);
+void few_typed(const BlockLinearArgs& g, hipStream_t s) {
+  if (g.m <= 16) few_rows<T, 1, TO>(g, s);
+  else few_rows<T, 2, TO>(g, s);
 }
 
 }  // namespace
 
-hipError_t launch_block_linear(BlockLinearArgs g, bool x_f32, bool out_f32, hipStream_t s) {
-  const bool vec = op_aligned(g.x, 16) && (g.m == 1 || g.ldx % (x_f32 ? 4 : 8) == 0);
-  g.by_four = op_rows_by_four(g.out, out_f32 ? MALT_FLOAT32 : MALT_BFLOAT16, g.ldo, g.n);
-  if (x_f32 && out_f32) few_typed<float, float>(g, vec, s);
-  else if (x_f32) few_typed<float, bf16_t>(g, vec, s);
-  else if (out_f32) few_typed<bf16_t, float>(g, vec, s);
-  else few_typed<bf16_t, bf16_t>(g, vec, s);
+hipError_t launch_block_linear(const BlockLinearArgs& g, bool x_f32, bool out_f32, hipStream_t s) {
+  if (x_f32 && out_f32) few_typed<float, float>(g, s);
+  else if (x_f32) few_typed<float, bf16_t>(g, s);
+  else if (out_f32) few_typed<bf16_t, float>(g, s);
+  else few_typed<bf16_t, bf16_t>(g, s);
   return hipGetLastError();
 }
 

@@ -298,7 +298,6 @@ void block_matmul_kernel(BlockMatmulArgs g) {
         store4(p + (wm * G::SM + 16 * a + (lane & 15)) * G::TN + wn * G::SN + 16 * b + 4 * (lane >> 4), acc[b][a]);
     return;
   }
-  const bool four = g.by_four;
 #pragma unroll
   for (int a = 0; a < MB; ++a) {
     const int64_t m = m0 + wm * G::SM + 16 * a + (lane & 15);
@@ -307,25 +306,9 @@ void block_matmul_kernel(BlockMatmulArgs g) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int64_t n = n0 + wn * G::SN + 16 * b + 4 * (lane >> 4);
-      if (four) {
-        if (n < g.n) {
-          op_f32x4 v = {acc[b][a][0], acc[b][a][1], acc[b][a][2], acc[b][a][3]};
-          if (g.accumulate) {
-            const op_f32x4 old = load4(row + n);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += old[e];
-          }
-          store4(row + n, v);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < g.n) {
-            float v = acc[b][a][e];
-            if (g.accumulate) v += to_f32(gptr(row)[n + e]);
-            gptr(row)[n + e] = from_f32<TO>(v);
-          }
-      }
+      op_f32x4 v = acc[b][a];
+      if (g.accumulate) v += row_load4(row, n, g.n);
+      row_store4(row, n, g.n, v);
     }
   }
 }
@@ -344,19 +327,9 @@ __global__ __launch_bounds__(256) void block_sum_kernel(BlockMatmulArgs g) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += x[e];
   }
-  TO* out = static_cast<TO*>(g.out) + row * g.ldo + n;
-  if (g.by_four) {
-    if (g.accumulate) {
-      const op_f32x4 old = load4(out);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += old[e];
-    }
-    store4(out, v);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < g.n) gptr(out)[e] = from_f32<TO>(g.accumulate ? v[e] + to_f32(gptr(out)[e]) : v[e]);
-  }
+  TO* out = static_cast<TO*>(g.out) + row * g.ldo;
+  if (g.accumulate) v += row_load4(out, n, g.n);
+  row_store4(out, n, g.n, v);
 }
 
 // Rings of two slots; with three or four, and one workgroup a CU, the 128-tile ran
@@ -423,7 +396,6 @@ BlockMatmulPlan block_matmul_plan(int64_t m, int64_t n, int64_t k, bool out_f32)
 hipError_t launch_block_matmul(BlockMatmulArgs a, bool b_blocks, bool out_f32, hipStream_t s) {
   const BlockMatmulPlan p = block_matmul_plan(a.m, a.n, a.k, out_f32);
   a.parts = p.parts;
-  a.by_four = op_rows_by_four(a.out, out_f32 ? MALT_FLOAT32 : MALT_BFLOAT16, a.ldo, a.n);
   if (b_blocks) return out_f32 ? launch_typed<true, float>(a, p.big, s) : launch_typed<true, bf16_t>(a, p.big, s);
   return out_f32 ? launch_typed<false, float>(a, p.big, s) : launch_typed<false, bf16_t>(a, p.big, s);
 }

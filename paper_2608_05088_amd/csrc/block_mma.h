@@ -33,24 +33,18 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
   return (uint32_t)r;
 }
 
-template <bool VEC>
+// Columns c .. c + 7 of a row, zero past its end.
 __device__ __forceinline__ void load8(const float* row, int c, int cols, float (&v)[8]) {
-  if (VEC && c + 8 <= cols) {
-    const op_f32x4 a = load4(row + c), b = load4(row + c + 4);
+  const op_f32x4 a = row_load4(row, c, cols), b = row_load4(row, c + 4, cols);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[j] = a[j];
-      v[4 + j] = b[j];
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? gptr(row)[c + j] : 0.f;
+  for (int j = 0; j < 4; ++j) {
+    v[j] = a[j];
+    v[4 + j] = b[j];
   }
 }
-template <bool VEC>
 __device__ __forceinline__ void load8(const bf16_t* row, int c, int cols, float (&v)[8]) {
-  if (VEC && c + 8 <= cols) {
-    const op_u32x4 r = *reinterpret_cast<const MALT_GLOBAL op_u32x4*>(gptr(row) + c);
+  if (c + 8 <= cols) {
+    const op_u32x4 r = *reinterpret_cast<const MALT_GLOBAL op_u32x4_any*>(gptr(row) + c);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       v[2 * j] = bf16_lo(r[j]);

@@ -22,12 +22,12 @@ __device__ __forceinline__ uint32_t max16(uint32_t v) {
   return v;
 }
 
-// Thread (rg, cg) holds rows 8 rg .. + 7, columns 8 cg .. + 7 of the tile.
+// Thread (rg, cg) of 512 holds rows 4 rg .. + 3, columns 8 cg .. + 7 of the tile.
 // WEIGHT: one scale for the whole tile.
-template <class T, bool VEC, bool WEIGHT>
-__global__ __launch_bounds__(256) void block_quant_kernel(QuantArgs a) {
+template <class T, bool WEIGHT>
+__global__ __launch_bounds__(512) void block_quant_kernel(QuantArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t tile[QB * QB];   // the transpose's bytes
-  __shared__ uint32_t col_max[4][QB];
+  __shared__ uint32_t col_max[8][QB];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int cg = tid & 15, rg = tid >> 4;
   const int64_t r0 = (int64_t)blockIdx.y * QB, c0 = (int64_t)blockIdx.x * QB;
@@ -35,11 +35,11 @@ __global__ __launch_bounds__(256) void block_quant_kernel(QuantArgs a) {
   const T* x = static_cast<const T*>(a.x) + r0 * a.ld + c0;
   const int64_t pitch = q_pad(a.cols), t_pitch = q_pad(a.rows);
 
-  float v[8][8];
+  float v[4][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = 8 * rg + i;
-    if (r < rows) load8<VEC>(x + (int64_t)r * a.ld, 8 * cg, cols, v[i]);
+  for (int i = 0; i < 4; ++i) {
+    const int r = 4 * rg + i;
+    if (r < rows) load8(x + (int64_t)r * a.ld, 8 * cg, cols, v[i]);
     else
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) void block_quant_kernel(QuantArgs a) {
   if constexpr (WEIGHT) {
     uint32_t b = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) b = umax(b, mag(v[i][j]));
     b = max16(b);
@@ -57,14 +57,16 @@ __global__ __launch_bounds__(256) void block_quant_kernel(QuantArgs a) {
     b = umax(b, (uint32_t)__shfl_xor((int)b, 32, 64));
     if (lane == 0) col_max[wave][0] = b;
     __syncthreads();
-    one = scale_byte(umax(umax(col_max[0][0], col_max[1][0]), umax(col_max[2][0], col_max[3][0])));
+#pragma unroll
+    for (int w = 0; w < 8; ++w) b = umax(b, col_max[w][0]);
+    one = scale_byte(b);
     if (tid == 0) gptr(a.block_scales)[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = (uint8_t)one;
   }
 
   if (a.values) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = 8 * rg + i;
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * rg + i;
       uint32_t byte = one;
       if constexpr (!WEIGHT) {
         uint32_t b = 0;
@@ -92,38 +94,38 @@ __global__ __launch_bounds__(256) void block_quant_kernel(QuantArgs a) {
       for (int j = 0; j < 8; ++j) {
         uint32_t b = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) b = umax(b, mag(v[i][j]));
+        for (int i = 0; i < 4; ++i) b = umax(b, mag(v[i][j]));
         b = umax(b, (uint32_t)__shfl_xor((int)b, 16, 64));
         b = umax(b, (uint32_t)__shfl_xor((int)b, 32, 64));
         if (lane < 16) col_max[wave][8 * cg + j] = b;
       }
       __syncthreads();
+      if (tid < QB) {   // thread c: column c's scale
+        uint32_t b = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int c = 8 * cg + j;
-        byte[j] = scale_byte(umax(umax(col_max[0][c], col_max[1][c]), umax(col_max[2][c], col_max[3][c])));
+        for (int w = 0; w < 8; ++w) b = umax(b, col_max[w][tid]);
+        b = scale_byte(b);
+        col_max[0][tid] = b;
+        if (tid < cols) gptr(a.t_scales)[blockIdx.y * q_scale_rows(a.cols) + c0 + q_scale_pos(tid)] = (uint8_t)b;
       }
-      if (rg == 0) {
+      __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (8 * cg + j < cols)
-            gptr(a.t_scales)[blockIdx.y * q_scale_rows(a.cols) + c0 + q_scale_pos(8 * cg + j)] = (uint8_t)byte[j];
-      }
+      for (int j = 0; j < 8; ++j) byte[j] = col_max[0][8 * cg + j];
     }
-    // Column c's 128 bytes lie in 8-byte pieces, piece rg at rg ^ (c / 8): the
-    // 16 lanes that write one rg fill 128 consecutive bytes' worth of banks.
+    // Column c's 128 bytes lie in 4-byte pieces, piece rg at rg ^ 2 (c / 8) (its
+    // lowest bit kept): the 16 lanes that write one rg and column spread over the banks.
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float s = scale_inverse(byte[j]);
-      const op_u32x2 q = {pack4(v[0][j] * s, v[1][j] * s, v[2][j] * s, v[3][j] * s),
-                          pack4(v[4][j] * s, v[5][j] * s, v[6][j] * s, v[7][j] * s)};
-      *reinterpret_cast<op_u32x2*>(tile + (8 * cg + j) * QB + ((rg ^ cg) << 3)) = q;
+      *reinterpret_cast<uint32_t*>(tile + (8 * cg + j) * QB + ((rg ^ (2 * cg)) << 2)) =
+          pack4(v[0][j] * s, v[1][j] * s, v[2][j] * s, v[3][j] * s);
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = (tid >> 3) + 32 * i, p = tid & 7;   // column, 16-byte piece of its 128 bytes
+    for (int i = 0; i < 2; ++i) {
+      const int c = (tid >> 3) + 64 * i, p = tid & 7;   // column, 16-byte piece of its 128 bytes
       const int g = c >> 3;
+      // Pieces 4 p .. 4 p + 3 lie in one 16-byte run, its halves swapped where bit 1 of 2 g is set.
       op_u32x4 q = *reinterpret_cast<const op_u32x4*>(tile + c * QB + ((p ^ (g >> 1)) << 4));
       if (g & 1) q = op_u32x4{q.z, q.w, q.x, q.y};
       if (c < cols) *reinterpret_cast<MALT_GLOBAL op_u32x4*>(gptr(a.t_values) + (c0 + c) * t_pitch + r0 + 16 * p) = q;
@@ -132,23 +134,17 @@ __global__ __launch_bounds__(256) void block_quant_kernel(QuantArgs a) {
 }
 
 template <class T>
-void quant_typed(const QuantArgs& a, bool vec, hipStream_t s) {
+void quant_typed(const QuantArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((a.cols + QB - 1) / QB), (unsigned)((a.rows + QB - 1) / QB));
-  if (a.block_scales) {
-    if (vec) hipLaunchKernelGGL((block_quant_kernel<T, true, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((block_quant_kernel<T, false, true>), grid, dim3(256), 0, s, a);
-  } else {
-    if (vec) hipLaunchKernelGGL((block_quant_kernel<T, true, false>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((block_quant_kernel<T, false, false>), grid, dim3(256), 0, s, a);
-  }
+  if (a.block_scales) hipLaunchKernelGGL((block_quant_kernel<T, true>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((block_quant_kernel<T, false>), grid, dim3(512), 0, s, a);
 }
 
 }  // namespace
 
 hipError_t launch_block_quant(const QuantArgs& a, bool f32, hipStream_t s) {
-  const bool vec = op_aligned(a.x, 16) && a.ld % (f32 ? 4 : 8) == 0;
-  if (f32) quant_typed<float>(a, vec, s);
-  else quant_typed<bf16_t>(a, vec, s);
+  if (f32) quant_typed<float>(a, s);
+  else quant_typed<bf16_t>(a, s);
   return hipGetLastError();
 }
 

@@ -16,7 +16,7 @@ struct DistillArgs {
   const float* weight;     // null: weight_value for every row
   float* losses;           // null: not wanted
   void* dlogits;           // null: not wanted
-  int64_t rows, vocab, ld, top_ld, id_ld, weight_stride, dld;
+  int64_t rows, vocab, ld, top_ld, id_ld, weight_stride, label_stride, dld;
   int32_t n_top;
   bool top_f32, wide_ids, wide_labels;
   float tau, alpha, weight_value;

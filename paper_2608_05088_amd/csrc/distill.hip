@@ -113,7 +113,7 @@ void distill_kernel(DistillArgs a) {
   if (wave == 0) {
     if (lane < a.n_top) entry(lane, id0, top0);
     if (a.labels) {
-      const int64_t y = load_id(a.labels, a.wide_labels, row);
+      const int64_t y = load_id(a.labels, a.wide_labels, row * a.label_stride);
       label = y >= 0 && y < vocab ? (int32_t)y : -1;
     }
   }

@@ -46,9 +46,8 @@ struct EmbedGradLayout {
 };
 
 EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width);
-// vec: rows of every matrix can be read four columns at a time.
-hipError_t launch_embed_lookup(EmbedLookupArgs a, bool table_f32, bool out_f32, bool vec, hipStream_t s);
-hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32, bool vec,
+hipError_t launch_embed_lookup(EmbedLookupArgs a, bool table_f32, bool out_f32, hipStream_t s);
+hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32,
                              hipStream_t s);
 
 }  // namespace malt

@@ -17,47 +17,31 @@ namespace malt {
 namespace {
 
 constexpr int DIGIT = 8, BINS = 1 << DIGIT;
+constexpr int STRIP = 256;   // columns a wave takes, four a lane
 
 // ------------------------------------------------------------------- lookup
-template <class TI, class TO, bool VEC>
+template <class TI, class TO>
 __global__ __launch_bounds__(256) void embed_lookup_kernel(EmbedLookupArgs a) {
   // 2^lanes_log2 lanes take a token (a wave at most), four columns a lane at a time.
   const int lanes = 1 << a.lanes_log2;
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2;
   if (t >= a.tokens) return;
-  const int c = threadIdx.x & (lanes - 1);
   const int64_t id = load_id(a.ids, a.wide_ids, t);
   const bool there = id >= 0 && id < a.vocab;
   const TI* row = static_cast<const TI*>(a.table) + (there ? id : 0) * a.table_ld;
   TO* out = static_cast<TO*>(a.out) + t * a.out_ld;
-  if constexpr (VEC) {
-    const int n = a.width >> 2;
-    for (int q = c; q < n; q += 4 * lanes) {
-      op_f32x4 v[4];
+  for (int c = 4 * (threadIdx.x & (lanes - 1)); c < a.width; c += 16 * lanes) {
+    op_f32x4 v[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        v[u] = op_f32x4{0.f, 0.f, 0.f, 0.f};
-        if (there && q + u * lanes < n) v[u] = load4(row + 4 * (q + u * lanes));
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (q + u * lanes < n) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[u][e] = there ? v[u][e] * a.scale : 0.f;
-          store4(out + 4 * (q + u * lanes), v[u]);
-        }
+    for (int u = 0; u < 4; ++u) {
+      v[u] = op_f32x4{0.f, 0.f, 0.f, 0.f};
+      if (there) v[u] = row_load4(row, c + 4 * u * lanes, a.width);
     }
-  } else {
-    for (int q = c; q < a.width; q += 4 * lanes) {
-      float v[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        v[u] = 0.f;
-        if (there && q + u * lanes < a.width) v[u] = to_f32(gptr(row)[q + u * lanes]);
-      }
+    for (int u = 0; u < 4; ++u) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (q + u * lanes < a.width) gptr(out)[q + u * lanes] = from_f32<TO>(there ? v[u] * a.scale : 0.f);
+      for (int e = 0; e < 4; ++e) v[u][e] = there ? v[u][e] * a.scale : 0.f;
+      row_store4(out, c + 4 * u * lanes, a.width, v[u]);
     }
   }
 }
@@ -302,14 +286,14 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedGradArgs a, int bit
 // --------------------------------------------------------------------- sums
 // s += up to 8 rows of grad, whose loads are all in flight together; at(u) is
 // the u-th token's number (wave-uniform, u < n).
-template <bool VEC, class TG, class At>
+template <class TG, class At>
 __device__ __forceinline__ void add_rows(op_f32x4& s, const TG* grad, int64_t ld, int n, int c0, int lane, int width,
                                          At&& at) {
   op_f32x4 v[8];
 #pragma unroll
   for (int u = 0; u < 8; ++u) {
     v[u] = op_f32x4{0.f, 0.f, 0.f, 0.f};
-    if (u < n) v[u] = strip_load<VEC>(grad + (int64_t)at(u) * ld, c0, lane, width);
+    if (u < n) v[u] = row_load4(grad + (int64_t)at(u) * ld, c0 + 4 * lane, width);
   }
 #pragma unroll
   for (int u = 0; u < 8; ++u)
@@ -319,7 +303,7 @@ __device__ __forceinline__ void add_rows(op_f32x4& s, const TG* grad, int64_t ld
 }
 
 // Rows order[j .. end) of grad, columns of one strip, added in that order.
-template <bool VEC, class TG>
+template <class TG>
 __device__ __forceinline__ op_f32x4 sum_rows(const TG* grad, int64_t ld, const uint32_t* order, int64_t j, int64_t end,
                                              int c0, int lane, int width) {
   op_f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -327,27 +311,27 @@ __device__ __forceinline__ op_f32x4 sum_rows(const TG* grad, int64_t ld, const u
     const int n = end - j < 64 ? (int)(end - j) : 64;
     const uint32_t mine = lane < n ? gptr(order)[j + lane] : 0;   // 64 tokens' numbers in one load
     for (int i = 0; i < n; i += 8)
-      add_rows<VEC>(s, grad, ld, n - i < 8 ? n - i : 8, c0, lane, width,
+      add_rows(s, grad, ld, n - i < 8 ? n - i : 8, c0, lane, width,
                     [&](int u) { return (uint32_t)__builtin_amdgcn_readlane((int)mine, i + u); });
   }
   return s;
 }
 
-template <bool VEC, class TO>
+template <class TO>
 __device__ __forceinline__ void finish_row(const EmbedGradArgs& a, TO* out, int c0, int lane, op_f32x4 x) {
   if (a.accumulate) {
-    const op_f32x4 old = strip_load<VEC>(out, c0, lane, a.width);
+    const op_f32x4 old = row_load4(out, c0 + 4 * lane, a.width);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = old[i] + a.scale * x[i];
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] *= a.scale;
   }
-  strip_store<VEC>(out, c0, lane, a.width, x);
+  row_store4(out, c0 + 4 * lane, a.width, x);
 }
 
 // Few tokens: the wave of a row and strip looks all of them over itself.
-template <bool VEC, class TG, class TO>
+template <class TG, class TO>
 __global__ __launch_bounds__(256) void embed_few_kernel(EmbedGradArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t v = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -365,7 +349,7 @@ __global__ __launch_bounds__(256) void embed_few_kernel(EmbedGradArgs a) {
   TO* out = static_cast<TO*>(a.dtable) + v * a.dtable_ld;
   op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
   if (!any) {
-    if (!a.accumulate) strip_store<VEC>(out, c0, lane, a.width, x);
+    if (!a.accumulate) row_store4(out, c0 + 4 * lane, a.width, x);
     return;
   }
 #pragma unroll
@@ -379,18 +363,18 @@ __global__ __launch_bounds__(256) void embed_few_kernel(EmbedGradArgs a) {
         t[u] = m ? (uint32_t)(b * 64 + __builtin_ctzll(m)) : 0;
         m &= m - 1;   // 0 stays 0
       }
-      add_rows<VEC>(x, static_cast<const TG*>(a.grad), a.grad_ld, n < 8 ? n : 8, c0, lane, a.width,
+      add_rows(x, static_cast<const TG*>(a.grad), a.grad_ld, n < 8 ? n : 8, c0, lane, a.width,
                     [&](int u) { return t[u]; });
     }
   }
-  finish_row<VEC>(a, out, c0, lane, x);
+  finish_row(a, out, c0, lane, x);
 }
 
 // Chunk c of the sorted tokens, one strip: partial sums of the segments longer
 // than a chunk.  Such a segment holds the chunk's first or last token, so a
 // chunk has two slots: 0 for the segment its first token belongs to, 1 for one
 // that starts after it.
-template <bool VEC, class TG>
+template <class TG>
 __global__ __launch_bounds__(256) void embed_chunks_kernel(EmbedGradArgs a) {
   const int lane = threadIdx.x & 63;
   const int strip = __builtin_amdgcn_readfirstlane(blockIdx.y * 4 + (threadIdx.x >> 6));
@@ -402,16 +386,16 @@ __global__ __launch_bounds__(256) void embed_chunks_kernel(EmbedGradArgs a) {
   const TG* grad = static_cast<const TG*>(a.grad);
   if (first < (uint32_t)a.vocab) {
     const int64_t s = a.seg[2 * (int64_t)first], e = a.seg[2 * (int64_t)first + 1];
-    if (e - s > a.chunk) store4(part, sum_rows<VEC>(grad, a.grad_ld, a.order, j0, e < j1 ? e : j1, c0, lane, a.width));
+    if (e - s > a.chunk) store4(part, sum_rows(grad, a.grad_ld, a.order, j0, e < j1 ? e : j1, c0, lane, a.width));
   }
   if (last != first && last < (uint32_t)a.vocab) {
     const int64_t s = a.seg[2 * (int64_t)last], e = a.seg[2 * (int64_t)last + 1];
-    if (e - s > a.chunk) store4(part + a.part_ld, sum_rows<VEC>(grad, a.grad_ld, a.order, s, j1, c0, lane, a.width));
+    if (e - s > a.chunk) store4(part + a.part_ld, sum_rows(grad, a.grad_ld, a.order, s, j1, c0, lane, a.width));
   }
 }
 
 // One row of the table, one strip a wave.
-template <bool VEC, class TG, class TO>
+template <class TG, class TO>
 __global__ __launch_bounds__(256) void embed_rows_kernel(EmbedGradArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t v = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -421,11 +405,11 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(EmbedGradArgs a) {
   TO* out = static_cast<TO*>(a.dtable) + v * a.dtable_ld;
   op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
   if (s == e) {
-    if (!a.accumulate) strip_store<VEC>(out, c0, lane, a.width, x);
+    if (!a.accumulate) row_store4(out, c0 + 4 * lane, a.width, x);
     return;
   }
   if (e - s <= a.chunk) {
-    x = sum_rows<VEC>(static_cast<const TG*>(a.grad), a.grad_ld, a.order, s, e, c0, lane, a.width);
+    x = sum_rows(static_cast<const TG*>(a.grad), a.grad_ld, a.order, s, e, c0, lane, a.width);
   } else {
     const int64_t k0 = s / a.chunk, k1 = (e - 1) / a.chunk;
     const float* part = a.part + c0 + 4 * lane;
@@ -437,28 +421,21 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(EmbedGradArgs a) {
       for (int i = 0; i < 4; ++i) x[i] += p[i];
     }
   }
-  finish_row<VEC>(a, out, c0, lane, x);
+  finish_row(a, out, c0, lane, x);
 }
 
 }  // namespace
 
 // -------------------------------------------------------------------- launch
-template <class TI, class TO>
-static void lookup_typed(const EmbedLookupArgs& a, bool vec, dim3 grid, hipStream_t s) {
-  if (vec) hipLaunchKernelGGL((embed_lookup_kernel<TI, TO, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((embed_lookup_kernel<TI, TO, false>), grid, dim3(256), 0, s, a);
-}
-
-hipError_t launch_embed_lookup(EmbedLookupArgs a, bool table_f32, bool out_f32, bool vec, hipStream_t s) {
-  const int64_t per = vec ? a.width / 4 : a.width;
+hipError_t launch_embed_lookup(EmbedLookupArgs a, bool table_f32, bool out_f32, hipStream_t s) {
   a.lanes_log2 = 0;
-  while (a.lanes_log2 < 6 && (int64_t(1) << a.lanes_log2) < per) ++a.lanes_log2;
+  while (a.lanes_log2 < 6 && (4 << a.lanes_log2) < a.width) ++a.lanes_log2;
   const int64_t blocks = (a.tokens + (256 >> a.lanes_log2) - 1) / (256 >> a.lanes_log2);
-  const dim3 grid((unsigned)blocks);
-  if (table_f32 && out_f32) lookup_typed<float, float>(a, vec, grid, s);
-  else if (table_f32) lookup_typed<float, bf16_t>(a, vec, grid, s);
-  else if (out_f32) lookup_typed<bf16_t, float>(a, vec, grid, s);
-  else lookup_typed<bf16_t, bf16_t>(a, vec, grid, s);
+  const dim3 grid((unsigned)blocks), threads(256);
+  if (table_f32 && out_f32) hipLaunchKernelGGL((embed_lookup_kernel<float, float>), grid, threads, 0, s, a);
+  else if (table_f32) hipLaunchKernelGGL((embed_lookup_kernel<float, bf16_t>), grid, threads, 0, s, a);
+  else if (out_f32) hipLaunchKernelGGL((embed_lookup_kernel<bf16_t, float>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((embed_lookup_kernel<bf16_t, bf16_t>), grid, threads, 0, s, a);
   return hipGetLastError();
 }
 
@@ -482,20 +459,20 @@ EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width) 
   return L;
 }
 
-template <bool VEC, class TG, class TO>
+template <class TG, class TO>
 static void grad_typed(const EmbedGradArgs& a, hipStream_t s) {
   const unsigned strips = (unsigned)((a.width + STRIP - 1) / STRIP);
   const dim3 grid((unsigned)((a.vocab + 3) / 4), strips);
   if (a.tokens <= FEW) {
-    hipLaunchKernelGGL((embed_few_kernel<VEC, TG, TO>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((embed_few_kernel<TG, TO>), grid, dim3(256), 0, s, a);
     return;
   }
   const unsigned chunks = (unsigned)((a.tokens + a.chunk - 1) / a.chunk);
-  hipLaunchKernelGGL((embed_chunks_kernel<VEC, TG>), dim3(chunks, (strips + 3) / 4), dim3(256), 0, s, a);
-  hipLaunchKernelGGL((embed_rows_kernel<VEC, TG, TO>), grid, dim3(256), 0, s, a);
+  hipLaunchKernelGGL((embed_chunks_kernel<TG>), dim3(chunks, (strips + 3) / 4), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((embed_rows_kernel<TG, TO>), grid, dim3(256), 0, s, a);
 }
 
-hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32, bool vec,
+hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32,
                              hipStream_t s) {
   if (a.tokens > FEW) {
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + L.keys[0]), reinterpret_cast<uint32_t*>(ws + L.keys[1])};
@@ -527,14 +504,10 @@ hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradLayout& L, char* ws
     a.keys = keys[to ^ 1];
     a.order = index[to ^ 1];
   }
-  if (vec && grad_f32 && out_f32) grad_typed<true, float, float>(a, s);
-  else if (vec && grad_f32) grad_typed<true, float, bf16_t>(a, s);
-  else if (vec && out_f32) grad_typed<true, bf16_t, float>(a, s);
-  else if (vec) grad_typed<true, bf16_t, bf16_t>(a, s);
-  else if (grad_f32 && out_f32) grad_typed<false, float, float>(a, s);
-  else if (grad_f32) grad_typed<false, float, bf16_t>(a, s);
-  else if (out_f32) grad_typed<false, bf16_t, float>(a, s);
-  else grad_typed<false, bf16_t, bf16_t>(a, s);
+  if (grad_f32 && out_f32) grad_typed<float, float>(a, s);
+  else if (grad_f32) grad_typed<float, bf16_t>(a, s);
+  else if (out_f32) grad_typed<bf16_t, float>(a, s);
+  else grad_typed<bf16_t, bf16_t>(a, s);
   return hipGetLastError();
 }
 

@@ -97,8 +97,7 @@ malt_status_t malt_embed_lookup(const void* ids, malt_index_t id_type, int64_t t
   a.width = int32_t(width);
   a.wide_ids = id_type == MALT_INT64;
   a.scale = scale;
-  const bool vec = op_rows_by_four(table, table_type, table_ld, width) && op_rows_by_four(out, out_type, out_ld, width);
-  return launched(launch_embed_lookup(a, table_type == MALT_FLOAT32, out_type == MALT_FLOAT32, vec,
+  return launched(launch_embed_lookup(a, table_type == MALT_FLOAT32, out_type == MALT_FLOAT32,
                                       static_cast<hipStream_t>(stream)),
                   "launching the table lookup");
 }
@@ -142,10 +141,8 @@ malt_status_t malt_embed_grad(const void* ids, malt_index_t id_type, int64_t tok
   a.accumulate = accumulate != 0;
   a.scale = scale;
   if (tokens == 0 && accumulate) return MALT_OK;
-  const bool vec = (tokens == 0 || op_rows_by_four(grad, grad_type, grad_ld, width)) &&
-                   op_rows_by_four(dtable, dtable_type, dtable_ld, width);
   return launched(launch_embed_grad(a, L, static_cast<char*>(workspace), grad_type == MALT_FLOAT32,
-                                    dtable_type == MALT_FLOAT32, vec, static_cast<hipStream_t>(stream)),
+                                    dtable_type == MALT_FLOAT32, static_cast<hipStream_t>(stream)),
                   "launching the table gradient");
 }
 
@@ -167,6 +164,8 @@ malt_status_t malt_distill(const malt_distill_t* p, void* stream) {
     if (p->id_ld < p->n_top || p->id_ld > kMaxPitch) return fail(MALT_ERR_SHAPE, "top_ids: row pitch %lld", (long long)p->id_ld);
   }
   if (p->labels) MALT_TRY(check_ids("labels", p->labels, p->label_type, p->rows));
+  if (p->labels && (p->label_stride < 0 || p->label_stride > kMaxPitch))
+    return fail(MALT_ERR_SHAPE, "labels: stride %lld", (long long)p->label_stride);
   if (!p->losses && !p->dlogits) return fail(MALT_ERR_INVALID_ARG, "neither losses nor dlogits is wanted");
   if (!op_aligned(p->losses, 4) || !op_aligned(p->weights, 4)) return fail(MALT_ERR_ALIGNMENT, "losses or weights not 4-byte aligned");
   if (p->weights && (p->weight_stride < 0 || p->weight_stride > kMaxPitch))
@@ -174,7 +173,7 @@ malt_status_t malt_distill(const malt_distill_t* p, void* stream) {
   if (p->dlogits) MALT_TRY(check_mat(d));
   if (p->rows == 0) return MALT_OK;
   const size_t id_bytes = p->n_top > 0 ? (size_t(p->rows - 1) * p->id_ld + p->n_top) * (p->id_type == MALT_INT64 ? 8 : 4) : 0;
-  const size_t label_bytes = p->labels ? size_t(p->rows) * (p->label_type == MALT_INT64 ? 8 : 4) : 0;
+  const size_t label_bytes = p->labels ? (size_t(p->rows - 1) * p->label_stride + 1) * (p->label_type == MALT_INT64 ? 8 : 4) : 0;
   const size_t weight_bytes = p->weights ? (size_t(p->rows - 1) * p->weight_stride + 1) * 4 : 0;
   const size_t loss_bytes = p->losses ? 4 * size_t(p->rows) : 0;
   struct Buf { const void* p; size_t n; };
@@ -204,6 +203,7 @@ malt_status_t malt_distill(const malt_distill_t* p, void* stream) {
   a.top_ld = p->top_ld;
   a.id_ld = p->id_ld;
   a.weight_stride = p->weight_stride;
+  a.label_stride = p->label_stride;
   a.dld = p->dld;
   a.n_top = int32_t(p->n_top);
   a.wide_ids = p->id_type == MALT_INT64;

@@ -79,7 +79,7 @@ class malt_distill_t(ctypes.Structure):
     _fields_ = [("logits", c_void_p), ("dtype", c_int32), ("rows", c_int64), ("vocab", c_int64), ("ld", c_int64),
                 ("top", c_void_p), ("top_type", c_int32), ("top_ids", c_void_p), ("id_type", c_int32),
                 ("n_top", c_int64), ("top_ld", c_int64), ("id_ld", c_int64), ("labels", c_void_p),
-                ("label_type", c_int32), ("tau", c_float), ("alpha", c_float), ("weights", c_void_p),
+                ("label_type", c_int32), ("label_stride", c_int64), ("tau", c_float), ("alpha", c_float), ("weights", c_void_p),
                 ("weight_stride", c_int64), ("weight", c_float), ("losses", c_void_p), ("dlogits", c_void_p),
                 ("dld", c_int64)]
 

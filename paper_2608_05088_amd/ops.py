@@ -234,13 +234,13 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
             t, tld = _rows(top_logits if top_logits.dim() == 2 else top_logits.reshape(n, k))
             i, ild = _rows(top_ids if top_ids.dim() == 2 else top_ids.reshape(n, k))
             tp, tt, ip, it = t.data_ptr(), _DTYPES[t.dtype], i.data_ptr(), _INDEX[i.dtype]
-    yp, yt = None, 0
+    yp, yt, y_stride = None, 0, 0
     if labels is not None:
         _tensor("labels", labels, _INDEX, dev)
         if labels.shape != lead:
             raise ValueError(f"labels must be {tuple(lead)} (got {tuple(labels.shape)})")
-        y = labels.reshape(-1).contiguous()
-        yp, yt = y.data_ptr(), _INDEX[y.dtype]
+        y = labels.reshape(-1)
+        yp, yt, y_stride = y.data_ptr(), _INDEX[y.dtype], (y.stride(0) if n > 1 else 0)
     wp, w_stride, w_value = None, 0, 1.0
     if isinstance(weight, torch.Tensor):
         _tensor("grad", weight, (torch.float32,), dev)
@@ -269,8 +269,8 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         grad = out
         if want_grad and out is None:
             grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-        a = lm.malt_distill_t(z.data_ptr(), zt, n, v, ld, tp, tt, ip, it, k, tld, ild, yp, yt, tau, alpha, wp, w_stride,
-                              w_value, losses.data_ptr() if want_loss else None,
+        a = lm.malt_distill_t(z.data_ptr(), zt, n, v, ld, tp, tt, ip, it, k, tld, ild, yp, yt, y_stride, tau, alpha, wp,
+                              w_stride, w_value, losses.data_ptr() if want_loss else None,
                               (grad if d is None else d).data_ptr() if want_grad else None, dld)
         lm._check(lm.lib().malt_distill(byref(a), s))
         return losses, grad

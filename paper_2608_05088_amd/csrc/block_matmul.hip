@@ -298,17 +298,42 @@ void block_matmul_kernel(BlockMatmulArgs g) {
         store4(p + (wm * G::SM + 16 * a + (lane & 15)) * G::TN + wn * G::SN + 16 * b + 4 * (lane >> 4), acc[b][a]);
     return;
   }
+  // Two row blocks at a time go through a part of LDS of the wave's own and leave
+  // it in whole rows of the wave's columns: 128 or 256 bytes a row, not pieces of 32.
+  constexpr int PITCH = G::SN + 4, PASS = 32 * PITCH;   // floats
+  static_assert(G::NW * PASS * 4 <= 2 * G::SLOT, "the copies fit the ring");
+  float* const mine = reinterpret_cast<float*>(lds) + wave * PASS;
+  __syncthreads();   // every wave is done reading the ring
 #pragma unroll
-  for (int a = 0; a < MB; ++a) {
-    const int64_t m = m0 + wm * G::SM + 16 * a + (lane & 15);
-    if (m >= g.m) continue;
-    TO* row = static_cast<TO*>(g.out) + m * g.ldo;
+  for (int p = 0; p < MB; p += 2) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int64_t n = n0 + wn * G::SN + 16 * b + 4 * (lane >> 4);
-      op_f32x4 v = acc[b][a];
-      if (g.accumulate) v += row_load4(row, n, g.n);
-      row_store4(row, n, g.n, v);
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        *reinterpret_cast<f32x4*>(mine + (16 * a + (lane & 15)) * PITCH + 16 * b + 4 * (lane >> 4)) = acc[b][p + a];
+    constexpr int W = sizeof(TO) == 4 ? 4 : 8, PER = G::SN / W;   // columns a lane stores, lanes a row
+#pragma unroll
+    for (int i = 0; i < 32 * PER / 64; ++i) {
+      const int r = (i * 64 + lane) / PER, c = (i * 64 + lane) % PER * W;
+      const int64_t m = m0 + wm * G::SM + 16 * p + r, n = n0 + wn * G::SN + c;
+      op_f32x4 v[W / 4];
+#pragma unroll
+      for (int e = 0; e < W / 4; ++e) v[e] = *reinterpret_cast<const f32x4*>(mine + r * PITCH + c + 4 * e);
+      if (m >= g.m) continue;
+      TO* row = static_cast<TO*>(g.out) + m * g.ldo;
+      if (g.accumulate)
+#pragma unroll
+        for (int e = 0; e < W / 4; ++e) v[e] += row_load4(row, n + 4 * e, g.n);
+      if constexpr (W == 8) {
+        if (n + 8 <= g.n) {
+          const op_u32x4 q = {pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[0].z, v[0].w), pack_bf16x2(v[1].x, v[1].y),
+                              pack_bf16x2(v[1].z, v[1].w)};
+          *reinterpret_cast<MALT_GLOBAL op_u32x4_any*>(gptr(row) + n) = q;
+          continue;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < W / 4; ++e) row_store4(row, n + 4 * e, g.n, v[e]);
     }
   }
 }

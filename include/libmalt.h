@@ -332,8 +332,8 @@ malt_status_t malt_embed_grad(const void* ids, malt_index_t id_type, int64_t tok
  * top, top_ids: NULL when n_top = 0 (labels alone); labels: NULL for none.
  * weights: float32, one every weight_stride elements (0: one for all rows), or
  * NULL for the scalar `weight`.
- * Limits: rows <= 2^21, 1 <= vocab <= 2^30, n_top <= 1024, tau finite and > 0,
- * 0 <= alpha <= 1. */
+ * Limits: rows <= 2^21, 1 <= vocab <= 2^30, n_top <= 1024,
+ * 2^-60 <= tau <= 2^60, 0 <= alpha <= 1. */
 typedef struct {
   const void* logits;        /* rows x vocab, type dtype */
   malt_dtype_t dtype;        /* of logits and dlogits */

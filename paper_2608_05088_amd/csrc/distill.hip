@@ -90,6 +90,8 @@ void distill_kernel(DistillArgs a) {
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
   const int vocab = (int)a.vocab;
   // Columns before the first 16-byte boundary and after the last: one a thread.
+  // (Vectors at whatever address are as right, but their stores, which then begin
+  // and end within memory's lines, took the bf16 step from 380 to 470 us.)
   const int ahead = (int)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (int)sizeof(T);
   const int head = ahead < vocab ? ahead : vocab;
   const int nvec = (vocab - head) / N;
@@ -182,9 +184,17 @@ void distill_kernel(DistillArgs a) {
   // --------------------------------------------------------------------- sums
   // exp((z - m) / t) = 2^(z c - m c), c = log2(e) / t; the same rounded m c goes
   // into the sums, the loss and the gradient, so it cancels.
+  // The maximum's own exponent is then what m c was rounded by, below 2^5 while
+  // |m c| <= 2^29.  Beyond that (logits of 10^8, a row of the type's lowest value) a
+  // second distinct logit is at least 2^5 below the maximum in the exponent, 10^-10 of
+  // it: there c is any power of two large enough that only maxima count, and m c exact.
   const float inv_tau = 1.f / a.tau;
-  const float c_tau = MODE != ONE || a.alpha < 1.f ? LOG2E * inv_tau : LOG2E;
-  const float c_one = MODE == ONE ? c_tau : LOG2E;
+  const float r_tau = MODE != ONE || a.alpha < 1.f ? LOG2E * inv_tau : LOG2E, r_one = MODE == ONE ? r_tau : LOG2E;
+  auto usable = [&](float c) {
+    if (!(fabsf(m) * c > 0x1p29f && fabsf(m) < INFINITY)) return c;
+    return __uint_as_float(__float_as_uint(0x1p41f / fabsf(m)) & 0x7f800000u);
+  };
+  const float c_tau = usable(r_tau), c_one = usable(r_one);
   const float mc_tau = m * c_tau, mc_one = MODE == SQUARE ? 2.f * mc_tau : m * c_one;
   float s_tau = 0.f, s_one = 0.f;
   auto add = [&](float f) {
@@ -227,6 +237,7 @@ void distill_kernel(DistillArgs a) {
   // ----------------------------------------------------------- loss (wave 0)
   if (wave == 0) {
     const float log_tau = log2f(s_tau), log_one = log2f(s_one);
+    auto log2_of = [&](float f, float r, float c, float mc) { return r == c ? __builtin_fmaf(f, c, -mc) : (f - m) * r; };
     float top = -INFINITY, sum = 0.f, kl = 0.f;
     for (int j = lane; j < a.n_top; j += 64) top = fmaxf(top, ent_off[j]);
     top = wave_max(top);
@@ -240,7 +251,7 @@ void distill_kernel(DistillArgs a) {
       if (ent_off[j] != -INFINITY) {
         const float lp = (ent_off[j] - top) * c_top - log_sum;   // log2 p
         p = exp2f(lp);
-        const float lq = __builtin_fmaf(ent_z[j], c_tau, -mc_tau) - log_tau;
+        const float lq = log2_of(ent_z[j], r_tau, c_tau, mc_tau) - log_tau;
         if (p != 0.f) kl += p * (lp - lq);
       }
       ent_off[j] = (1.f - a.alpha) * a.tau * p;
@@ -251,7 +262,7 @@ void distill_kernel(DistillArgs a) {
       ent_z[a.n_top] = z_label;
       float loss = 0.f;
       if (use_teacher) loss += (1.f - a.alpha) * a.tau * a.tau * LN2 * kl;
-      if (use_label) loss += a.alpha * LN2 * (log_one - __builtin_fmaf(z_label, c_one, -mc_one));
+      if (use_label) loss += a.alpha * LN2 * (log_one - log2_of(z_label, r_one, c_one, mc_one));
       if (a.losses) gptr(a.losses)[row] = loss;
     }
   }
@@ -261,15 +272,8 @@ void distill_kernel(DistillArgs a) {
     const float w = a.weight ? gptr(a.weight)[row * a.weight_stride] : a.weight_value;
     T* d = static_cast<T*>(a.dlogits) + row * a.dld;
     MALT_GLOBAL T* const dg = gptr(d);
-    // Vector stores where the gradient's row has the logits' alignment.
-    const bool together = ((reinterpret_cast<uintptr_t>(d) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0;
     auto put = [&](int q, const float (&f)[N]) {
-      if (together) {
-        *reinterpret_cast<MALT_GLOBAL op_u32x4*>(dg + head + (int64_t)q * N) = V::close(f);
-      } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) dg[head + (int64_t)q * N + e] = from_f32<T>(f[e]);
-      }
+      *reinterpret_cast<MALT_GLOBAL op_u32x4_any*>(dg + head + (int64_t)q * N) = V::close(f);
     };
     // A row without weight, or without teacher and label, has no gradient, whatever its logits hold.
     if (w == 0.f || !(use_teacher || use_label)) {
@@ -340,7 +344,7 @@ void launch_typed(const DistillArgs& a, hipStream_t s) {
   if (nvec <= 256) launch_held<T, 256, 1, 8>(a, s);
   else if (nvec <= 256 * 4) launch_held<T, 256, 4, 6>(a, s);
   else if (nvec <= 512 * 7) launch_held<T, 512, 7, 6>(a, s);
-  else if (nvec <= 512 * 13) launch_held<T, 512, 13, 6>(a, s);
+  else if (nvec <= 512 * 13) launch_held<T, 512, 13, 5>(a, s);
   else if (nvec <= 512 * 25) launch_held<T, 512, 25, 4>(a, s);
   else launch_held<T, 1024, 25, 4>(a, s);
 }

@@ -152,7 +152,7 @@ malt_status_t malt_distill(const malt_distill_t* p, void* stream) {
   if (p->vocab < 1 || p->vocab > kMaxVocab) return fail(MALT_ERR_SHAPE, "a vocabulary of %lld", (long long)p->vocab);
   if (p->n_top < 0 || p->n_top > DISTILL_MAX_TOP)
     return fail(MALT_ERR_SHAPE, "%lld teacher entries a row (at most %d)", (long long)p->n_top, DISTILL_MAX_TOP);
-  if (!(p->tau > 0.f) || !isfinite(p->tau)) return fail(MALT_ERR_INVALID_ARG, "tau must be finite and > 0");
+  if (!(p->tau >= 0x1p-60f && p->tau <= 0x1p60f)) return fail(MALT_ERR_INVALID_ARG, "tau must be in [2^-60, 2^60]");
   if (!(p->alpha >= 0.f && p->alpha <= 1.f)) return fail(MALT_ERR_INVALID_ARG, "alpha must be in [0, 1]");
   const Mat z = {"logits", p->logits, p->dtype, p->rows, p->vocab, p->ld},
             top = {"top", p->top, p->top_type, p->n_top > 0 ? p->rows : 0, p->n_top, p->top_ld},

@@ -18,7 +18,6 @@ contiguous are copied first; row pitches larger than a row are taken as they are
 from __future__ import annotations
 
 import functools
-import math
 from ctypes import byref, c_size_t
 from typing import Optional, Tuple, Union
 
@@ -208,8 +207,8 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         raise ValueError(f"logits must be (..., vocab) (got {tuple(logits.shape)})")
     lead, v = logits.shape[:-1], logits.shape[-1]
     tau, alpha = float(tau), float(alpha)
-    if not (math.isfinite(tau) and tau > 0):
-        raise ValueError(f"tau must be finite and > 0 (got {tau})")
+    if not 2.0 ** -60 <= tau <= 2.0 ** 60:
+        raise ValueError(f"tau must be in [2^-60, 2^60] (got {tau})")
     if not 0 <= alpha <= 1:
         raise ValueError(f"alpha must be in [0, 1] (got {alpha})")
     z, ld = _rows(_flat(logits) if logits.dim() > 1 else logits.reshape(1, v))
@@ -269,6 +268,8 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         grad = out
         if want_grad and out is None:
             grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        if n == 0:
+            return losses, grad
         a = lm.malt_distill_t(z.data_ptr(), zt, n, v, ld, tp, tt, ip, it, k, tld, ild, yp, yt, y_stride, tau, alpha, wp,
                               w_stride, w_value, losses.data_ptr() if want_loss else None,
                               (grad if d is None else d).data_ptr() if want_grad else None, dld)
@@ -435,6 +436,17 @@ class _Fp8Linear(torch.autograd.Function):
         return _on(dev, None, (), work)
 
 
+def _kept(flat, values: int, scales: int, n: int, out, s) -> None:
+    """out = flat W^T on a weight's values and block scales."""
+    flat, ld = _rows(flat)
+    m, k = flat.shape
+    out_type = _DTYPES[out.dtype]
+    size = _linear_size(m, n, k, out_type)
+    ws = torch.empty(size, dtype=torch.uint8, device=out.device) if size else None
+    lm._check(lm.lib().malt_block_linear(flat.data_ptr(), _DTYPES[flat.dtype], m, k, ld, values, scales, n,
+                                         out.data_ptr(), out_type, n, ws.data_ptr() if size else None, size, s))
+
+
 def _linear(x, weight, out_dtype, stream, keep_x, keep_w):
     """The layer's output, and what its backward pass needs: x^T and W^T in 8 bits, W's scales."""
     dev = x.device
@@ -445,8 +457,12 @@ def _linear(x, weight, out_dtype, stream, keep_x, keep_w):
     def work(s):
         if m == 0:
             return torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev), None, None, None
-        q, xt = _quantize(flat, s, True, keep_x)
         values, scales, wt = _quantize_weight(weight, s, True, keep_w)
+        if not keep_x:
+            y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
+            _kept(flat, values.data_ptr(), scales.data_ptr(), n, y, s)
+            return y, None, wt, scales
+        q, xt = _quantize(flat, s, True, True)
         y = _matmul(m, n, k, q, values.data_ptr(), scales.data_ptr(), (scales.shape[1], 1), out_dtype, dev, s)
         return y if x.dim() == 2 else y.reshape(*x.shape[:-1], n), xt, wt, scales
 
@@ -521,16 +537,10 @@ def fp8_forward(x: torch.Tensor, values: torch.Tensor, scales: torch.Tensor,
     flat = _flat(x) if x.dim() > 1 else x.reshape(1, -1)
     m = flat.shape[0]
 
-    flat, ld = _rows(flat)
-    size = _linear_size(m, n, k, _DTYPES[out_dtype]) if m else 0
-
     def work(s):
         y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
         if m:
-            ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
-            lm._check(lm.lib().malt_block_linear(flat.data_ptr(), _DTYPES[x.dtype], m, k, ld, values.data_ptr(),
-                                                 scales.data_ptr(), n, y.data_ptr(), _DTYPES[out_dtype], n,
-                                                 ws.data_ptr() if size else None, size, s))
+            _kept(flat, values.data_ptr(), scales.data_ptr(), n, y, s)
         return y
 
     return _on(dev, stream, (flat, values, scales), work)

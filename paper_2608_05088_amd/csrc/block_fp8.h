@@ -66,6 +66,7 @@ struct BlockMatmulPlan {
 BlockMatmulPlan block_matmul_plan(int64_t m, int64_t n, int64_t k, bool out_f32);
 
 hipError_t launch_block_quant(const QuantArgs& a, bool f32, hipStream_t s);
+hipError_t launch_block_quant_pair(const QuantArgs& x, bool x_f32, const QuantArgs& w, bool w_f32, hipStream_t s);
 hipError_t launch_block_matmul(BlockMatmulArgs a, bool b_blocks, bool out_f32, hipStream_t s);
 
 }  // namespace malt

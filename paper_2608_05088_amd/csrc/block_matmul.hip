@@ -18,6 +18,7 @@
 // the block has one scale: a lane takes the 16-byte chunks g and g + 4 of its
 // row (g = lane / 16), which hit 16 distinct groups of banks.  The instruction's
 // first operand is B, so that a lane ends up with four consecutive columns.
+#include <atomic>
 #include <type_traits>
 
 #include "block_mma.h"
@@ -366,10 +367,17 @@ template <class G, bool BLOCKS, bool SPLIT, class TO>
 hipError_t launch_tiled(const BlockMatmulArgs& a, hipStream_t s) {
   const auto kernel = &block_matmul_kernel<G, BLOCKS, std::is_same<TO, float>::value, SPLIT, TO>;
   constexpr int bytes = 2 * G::SLOT;
-  // More LDS than the default limit: raised each time, for whichever device is current.
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  // More LDS than the default limit: raised once for each device.
+  static std::atomic<uint64_t> raised{0};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (dev > 63 || !(raised.load(std::memory_order_relaxed) & bit)) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    raised.fetch_or(bit, std::memory_order_relaxed);
+  }
   const int64_t tn = (a.n + G::TN - 1) / G::TN, tiles = (a.m + G::TM - 1) / G::TM * tn;
   hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8), (unsigned)a.parts), dim3(G::NT), bytes, s, a);
   if constexpr (SPLIT) {

@@ -22,15 +22,20 @@ __device__ __forceinline__ uint32_t max16(uint32_t v) {
   return v;
 }
 
-// Thread (rg, cg) of 512 holds rows 4 rg .. + 3, columns 8 cg .. + 7 of the tile.
-// WEIGHT: one scale for the whole tile.
+struct QuantShared {
+  __attribute__((aligned(16))) uint8_t tile[QB * QB];   // the transpose's bytes
+  uint32_t col_max[8][QB];
+};
+
+// Tile (bx, by) of one matrix.  Thread (rg, cg) of 512 holds rows 4 rg .. + 3,
+// columns 8 cg .. + 7 of the tile.  WEIGHT: one scale for the whole tile.
 template <class T, bool WEIGHT>
-__global__ __launch_bounds__(512) void block_quant_kernel(QuantArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t tile[QB * QB];   // the transpose's bytes
-  __shared__ uint32_t col_max[8][QB];
+__device__ __forceinline__ void quantize_tile(const QuantArgs& a, int bx, int by, QuantShared& sh) {
+  uint8_t* const tile = sh.tile;
+  uint32_t(*const col_max)[QB] = sh.col_max;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int cg = tid & 15, rg = tid >> 4;
-  const int64_t r0 = (int64_t)blockIdx.y * QB, c0 = (int64_t)blockIdx.x * QB;
+  const int64_t r0 = (int64_t)by * QB, c0 = (int64_t)bx * QB;
   const int rows = (int)(a.rows - r0 < QB ? a.rows - r0 : QB), cols = (int)(a.cols - c0 < QB ? a.cols - c0 : QB);
   const T* x = static_cast<const T*>(a.x) + r0 * a.ld + c0;
   const int64_t pitch = q_pad(a.cols), t_pitch = q_pad(a.rows);
@@ -60,7 +65,7 @@ __global__ __launch_bounds__(512) void block_quant_kernel(QuantArgs a) {
 #pragma unroll
     for (int w = 0; w < 8; ++w) b = umax(b, col_max[w][0]);
     one = scale_byte(b);
-    if (tid == 0) gptr(a.block_scales)[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = (uint8_t)one;
+    if (tid == 0) gptr(a.block_scales)[by * (pitch / QB) + bx] = (uint8_t)one;
   }
 
   if (a.values) {
@@ -80,7 +85,7 @@ __global__ __launch_bounds__(512) void block_quant_kernel(QuantArgs a) {
                             pack4(v[i][4] * s, v[i][5] * s, v[i][6] * s, v[i][7] * s)};
         *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(a.values) + (r0 + r) * pitch + c0 + 8 * cg) = q;
         if (!WEIGHT && cg == 0)
-          gptr(a.scales)[blockIdx.x * q_scale_rows(a.rows) + r0 + q_scale_pos(r)] = (uint8_t)byte;
+          gptr(a.scales)[bx * q_scale_rows(a.rows) + r0 + q_scale_pos(r)] = (uint8_t)byte;
       }
     }
   }
@@ -106,7 +111,7 @@ __global__ __launch_bounds__(512) void block_quant_kernel(QuantArgs a) {
         for (int w = 0; w < 8; ++w) b = umax(b, col_max[w][tid]);
         b = scale_byte(b);
         col_max[0][tid] = b;
-        if (tid < cols) gptr(a.t_scales)[blockIdx.y * q_scale_rows(a.cols) + c0 + q_scale_pos(tid)] = (uint8_t)b;
+        if (tid < cols) gptr(a.t_scales)[by * q_scale_rows(a.cols) + c0 + q_scale_pos(tid)] = (uint8_t)b;
       }
       __syncthreads();
 #pragma unroll
@@ -133,11 +138,33 @@ __global__ __launch_bounds__(512) void block_quant_kernel(QuantArgs a) {
   }
 }
 
+template <class T, bool WEIGHT>
+__global__ __launch_bounds__(512) void block_quant_kernel(QuantArgs a) {
+  __shared__ QuantShared sh;
+  quantize_tile<T, WEIGHT>(a, blockIdx.x, blockIdx.y, sh);
+}
+
+// A layer's input and weight in one launch: x's tiles, then w's.
+template <class TX, class TW>
+__global__ __launch_bounds__(512) void block_quant_pair_kernel(QuantArgs x, QuantArgs w, int x_tiles, int x_cols, int w_cols) {
+  __shared__ QuantShared sh;
+  const int b = blockIdx.x;
+  if (b < x_tiles) quantize_tile<TX, false>(x, b % x_cols, b / x_cols, sh);
+  else quantize_tile<TW, true>(w, (b - x_tiles) % w_cols, (b - x_tiles) / w_cols, sh);
+}
+
 template <class T>
 void quant_typed(const QuantArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.cols + QB - 1) / QB), (unsigned)((a.rows + QB - 1) / QB));
+  const dim3 grid((unsigned)(q_pad(a.cols) / QB), (unsigned)(q_pad(a.rows) / QB));
   if (a.block_scales) hipLaunchKernelGGL((block_quant_kernel<T, true>), grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL((block_quant_kernel<T, false>), grid, dim3(512), 0, s, a);
+}
+
+template <class TX, class TW>
+void pair_typed(const QuantArgs& x, const QuantArgs& w, hipStream_t s) {
+  const int xc = int(q_pad(x.cols) / QB), wc = int(q_pad(w.cols) / QB);
+  const int64_t xt = xc * (q_pad(x.rows) / QB), wt = wc * (q_pad(w.rows) / QB);
+  hipLaunchKernelGGL((block_quant_pair_kernel<TX, TW>), dim3((unsigned)(xt + wt)), dim3(512), 0, s, x, w, int(xt), xc, wc);
 }
 
 }  // namespace
@@ -145,6 +172,14 @@ void quant_typed(const QuantArgs& a, hipStream_t s) {
 hipError_t launch_block_quant(const QuantArgs& a, bool f32, hipStream_t s) {
   if (f32) quant_typed<float>(a, s);
   else quant_typed<bf16_t>(a, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_block_quant_pair(const QuantArgs& x, bool x_f32, const QuantArgs& w, bool w_f32, hipStream_t s) {
+  if (x_f32 && w_f32) pair_typed<float, float>(x, w, s);
+  else if (x_f32) pair_typed<float, bf16_t>(x, w, s);
+  else if (w_f32) pair_typed<bf16_t, float>(x, w, s);
+  else pair_typed<bf16_t, bf16_t>(x, w, s);
   return hipGetLastError();
 }
 

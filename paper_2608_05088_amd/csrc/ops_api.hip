@@ -377,4 +377,160 @@ malt_status_t malt_block_linear(const void* x, malt_dtype_t x_type, int64_t m, i
                            workspace, need - values - scales, stream);
 }
 
+// A layer's buffers: what is kept for the backward pass, and the workspaces.
+struct LayerLayout {
+  size_t xt, xt_scales, wt, w_scales, kept;              // kept: x^T, W^T, W's block scales
+  size_t q, q_scales, w, forward_product, forward;       // forward: x, W, the product's partial sums
+  size_t g, g_scales, gt, gt_scales, backward_product, backward;
+};
+
+static LayerLayout layer_layout(int64_t m, int64_t n, int64_t k, bool y_f32, bool dx_f32, bool dw_f32, bool need_x, bool need_w) {
+  LayerLayout L = {};
+  auto take = [](size_t& end, size_t bytes) {
+    const size_t at = end;
+    end += align256(bytes);
+    return at;
+  };
+  auto values = [](int64_t r, int64_t c) { return size_t(r) * q_pad(c); };
+  auto scales = [](int64_t r, int64_t c) { return size_t(q_pad(c) / QB) * q_scale_rows(r); };
+  if (need_w) {
+    L.xt = take(L.kept, values(k, m));
+    L.xt_scales = take(L.kept, scales(k, m));
+  }
+  if (need_x) L.wt = take(L.kept, values(k, n));
+  L.w_scales = take(L.kept, size_t(q_pad(n) / QB) * (q_pad(k) / QB));
+  L.q = take(L.forward, values(m, k));
+  L.q_scales = take(L.forward, scales(m, k));
+  L.w = take(L.forward, values(n, k));
+  L.forward_product = take(L.forward, block_matmul_plan(m, n, k, y_f32).bytes);
+  if (need_x) {
+    L.g = take(L.backward, values(m, n));
+    L.g_scales = take(L.backward, scales(m, n));
+  }
+  if (need_w) {
+    L.gt = take(L.backward, values(n, m));
+    L.gt_scales = take(L.backward, scales(n, m));
+  }
+  size_t product = 0;   // the two products follow each other
+  if (need_x) product = block_matmul_plan(m, k, n, dx_f32).bytes;
+  if (need_w) {
+    const size_t b = block_matmul_plan(n, k, m, dw_f32).bytes;
+    if (b > product) product = b;
+  }
+  L.backward_product = take(L.backward, product);
+  return L;
+}
+
+static malt_status_t check_layer(int64_t m, int64_t n, int64_t k) {
+  size_t v, s;
+  MALT_TRY(malt_block_size(m, k, &v, &s));
+  MALT_TRY(malt_block_size(n, k, &v, &s));
+  if (m > kMaxProduct / n || m > kMaxProduct / k || n > kMaxProduct / k)
+    return fail(MALT_ERR_SHAPE, "a layer of %lld x %lld on %lld rows", (long long)n, (long long)k, (long long)m);
+  if (size_t(q_pad(k) / QB) * q_scale_rows(m) > 0xffffffffull || size_t(q_pad(n) / QB) * q_scale_rows(m) > 0xffffffffull ||
+      size_t(q_pad(m) / QB) * q_scale_rows(n) > 0xffffffffull || size_t(q_pad(m) / QB) * q_scale_rows(k) > 0xffffffffull)
+    return fail(MALT_ERR_SHAPE, "an operand's scales exceed 4 GiB");
+  return MALT_OK;
+}
+
+malt_status_t malt_block_layer_size(int64_t m, int64_t n, int64_t k, malt_dtype_t y_type, malt_dtype_t dx_type,
+                                    malt_dtype_t dw_type, int32_t need_dx, int32_t need_dw, size_t* kept_bytes,
+                                    size_t* forward_bytes, size_t* backward_bytes) {
+  if (!kept_bytes || !forward_bytes || !backward_bytes) return fail(MALT_ERR_INVALID_ARG, "output pointer is NULL");
+  if (!op_dtype_ok(y_type) || !op_dtype_ok(dx_type) || !op_dtype_ok(dw_type)) return fail(MALT_ERR_INVALID_ARG, "unknown element type");
+  MALT_TRY(check_layer(m, n, k));
+  const LayerLayout L = layer_layout(m, n, k, y_type == MALT_FLOAT32, dx_type == MALT_FLOAT32, dw_type == MALT_FLOAT32,
+                                     need_dx != 0, need_dw != 0);
+  *kept_bytes = L.kept;
+  *forward_bytes = L.forward;
+  *backward_bytes = L.backward;
+  return MALT_OK;
+}
+
+malt_status_t malt_block_layer_forward(const void* x, malt_dtype_t x_type, int64_t m, int64_t k, int64_t ldx,
+                                       const void* w, malt_dtype_t w_type, int64_t n, int64_t ldw, void* y,
+                                       malt_dtype_t y_type, int64_t ldy, int32_t need_dx, int32_t need_dw, void* kept,
+                                       size_t kept_bytes, void* workspace, size_t workspace_bytes, void* stream) {
+  MALT_TRY(check_layer(m, n, k));
+  const Mat xm = {"x", x, x_type, m, k, ldx}, wm = {"w", w, w_type, n, k, ldw}, ym = {"y", y, y_type, m, n, ldy};
+  MALT_TRY(check_mat(xm));
+  MALT_TRY(check_mat(wm));
+  MALT_TRY(check_mat(ym));
+  const LayerLayout L = layer_layout(m, n, k, y_type == MALT_FLOAT32, false, false, need_dx != 0, need_dw != 0);
+  MALT_TRY(check_workspace(kept, kept_bytes, L.kept));
+  MALT_TRY(check_workspace(workspace, workspace_bytes, L.forward));
+  struct Buf { const void* p; size_t n; };
+  const Buf b[] = {{x, xm.bytes()}, {w, wm.bytes()}, {y, ym.bytes()}, {kept, L.kept}, {workspace, L.forward}};
+  for (int i = 2; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (op_overlap(b[i].p, b[i].n, b[j].p, b[j].n)) return fail(MALT_ERR_ALIAS, "two of the layer's buffers overlap");
+  uint8_t *const kb = static_cast<uint8_t*>(kept), *const ws = static_cast<uint8_t*>(workspace);
+  QuantArgs qx = {}, qw = {};
+  qx.x = x;
+  qx.rows = m;
+  qx.cols = k;
+  qx.ld = ldx;
+  qx.values = ws + L.q;
+  qx.scales = ws + L.q_scales;
+  qx.t_values = need_dw ? kb + L.xt : nullptr;
+  qx.t_scales = need_dw ? kb + L.xt_scales : nullptr;
+  qw.x = w;
+  qw.rows = n;
+  qw.cols = k;
+  qw.ld = ldw;
+  qw.values = ws + L.w;
+  qw.t_values = need_dx ? kb + L.wt : nullptr;
+  qw.block_scales = kb + L.w_scales;
+  const hipError_t e = launch_block_quant_pair(qx, x_type == MALT_FLOAT32, qw, w_type == MALT_FLOAT32, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "launching the 8-bit conversion");
+  return malt_block_matmul(m, n, k, ws + L.q, ws + L.q_scales, ws + L.w, kb + L.w_scales, 1, q_pad(k) / QB, 1, y, y_type,
+                           ldy, 0, ws + L.forward_product, L.forward - L.forward_product, stream);
+}
+
+malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, int64_t m, int64_t n, int64_t lddy,
+                                        int64_t k, const void* kept, size_t kept_bytes, void* dx, malt_dtype_t dx_type,
+                                        int64_t lddx, void* dw, malt_dtype_t dw_type, int64_t lddw, int32_t accumulate,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  MALT_TRY(check_layer(m, n, k));
+  if (!dx && !dw) return fail(MALT_ERR_INVALID_ARG, "neither dx nor dw is wanted");
+  if (accumulate != 0 && accumulate != 1) return fail(MALT_ERR_INVALID_ARG, "accumulate must be 0 or 1");
+  const Mat g = {"dy", dy, dy_type, m, n, lddy}, xm = {"dx", dx, dx_type, m, k, lddx}, wm = {"dw", dw, dw_type, n, k, lddw};
+  MALT_TRY(check_mat(g));
+  if (dx) MALT_TRY(check_mat(xm));
+  if (dw) MALT_TRY(check_mat(wm));
+  const LayerLayout L = layer_layout(m, n, k, false, dx_type == MALT_FLOAT32, dw_type == MALT_FLOAT32, dx != nullptr, dw != nullptr);
+  MALT_TRY(check_workspace(kept, kept_bytes, L.kept));
+  MALT_TRY(check_workspace(workspace, workspace_bytes, L.backward));
+  struct Buf { const void* p; size_t n; };
+  const Buf b[] = {{dy, g.bytes()}, {kept, L.kept}, {dx, dx ? xm.bytes() : 0}, {dw, dw ? wm.bytes() : 0}, {workspace, L.backward}};
+  for (int i = 2; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (op_overlap(b[i].p, b[i].n, b[j].p, b[j].n)) return fail(MALT_ERR_ALIAS, "two of the layer's buffers overlap");
+  const uint8_t* const kb = static_cast<const uint8_t*>(kept);
+  uint8_t* const ws = static_cast<uint8_t*>(workspace);
+  QuantArgs q = {};
+  q.x = dy;
+  q.rows = m;
+  q.cols = n;
+  q.ld = lddy;
+  if (dx) {
+    q.values = ws + L.g;
+    q.scales = ws + L.g_scales;
+  }
+  if (dw) {
+    q.t_values = ws + L.gt;
+    q.t_scales = ws + L.gt_scales;
+  }
+  const hipError_t e = launch_block_quant(q, dy_type == MALT_FLOAT32, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "launching the 8-bit conversion");
+  const size_t product = L.backward - L.backward_product;
+  if (dx)
+    MALT_TRY(malt_block_matmul(m, k, n, ws + L.g, ws + L.g_scales, kb + L.wt, kb + L.w_scales, 1, 1, q_pad(k) / QB, dx, dx_type,
+                               lddx, 0, ws + L.backward_product, product, stream));
+  if (dw)
+    MALT_TRY(malt_block_matmul(n, k, m, ws + L.gt, ws + L.gt_scales, kb + L.xt, kb + L.xt_scales, 0, 0, 0, dw, dw_type, lddw,
+                               accumulate, ws + L.backward_product, product, stream));
+  return MALT_OK;
+}
+
 }  // extern "C"

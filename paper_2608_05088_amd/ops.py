@@ -329,66 +329,15 @@ def _pad(n: int, to: int) -> int:
     return -(-n // to) * to
 
 
-def _operand_bytes(rows: int, cols: int) -> Tuple[int, int]:
-    """Bytes of an 8-bit operand's values, and of values and scales (malt_block_size)."""
-    k = _pad(cols, BLOCK)
-    return rows * k, rows * k + k // BLOCK * _pad(rows, 256)
-
-
-class _Operand:
-    """An 8-bit operand in a buffer of its own: values, then scales."""
-    __slots__ = ("buf", "values", "scales")
-
-    def __init__(self, buf: torch.Tensor, rows: int, cols: int):
-        self.buf = buf
-        self.values = buf.data_ptr()
-        self.scales = self.values + _operand_bytes(rows, cols)[0]
-
-    @staticmethod
-    def empty(rows: int, cols: int, device) -> "_Operand":
-        return _Operand(torch.empty(_operand_bytes(rows, cols)[1], dtype=torch.uint8, device=device), rows, cols)
-
-
-def _quantize(x, s, rows_form: bool, cols_form: bool):
-    """x (2-D) as an operand along its columns and, transposed, along its rows."""
-    x, ld = _rows(x)
-    r, c = x.shape
-    q = _Operand.empty(r, c, x.device) if rows_form else None
-    t = _Operand.empty(c, r, x.device) if cols_form else None
-    lm._check(lm.lib().malt_block_quantize(x.data_ptr(), _DTYPES[x.dtype], r, c, ld, q.values if q else None,
-                                           q.scales if q else None, t.values if t else None, t.scales if t else None, s))
-    return q, t
-
-
-def _quantize_weight(w, s, plain: bool, transposed: bool):
-    """A weight's values, its block scales and its transpose's values."""
+def _quantize_weight(w, s) -> Tuple[torch.Tensor, torch.Tensor]:
+    """A weight's values and block scales."""
     w, ld = _rows(w)
     r, c = w.shape
-    values = torch.empty((r, _pad(c, BLOCK)), dtype=torch.uint8, device=w.device) if plain else None
-    t_values = torch.empty((c, _pad(r, BLOCK)), dtype=torch.uint8, device=w.device) if transposed else None
+    values = torch.empty((r, _pad(c, BLOCK)), dtype=torch.uint8, device=w.device)
     scales = torch.empty((-(-r // BLOCK), -(-c // BLOCK)), dtype=torch.uint8, device=w.device)
-    lm._check(lm.lib().malt_block_quantize_weight(w.data_ptr(), _DTYPES[w.dtype], r, c, ld,
-                                                  values.data_ptr() if plain else None, scales.data_ptr(),
-                                                  t_values.data_ptr() if transposed else None, s))
-    return values, scales, t_values
-
-
-@functools.lru_cache(maxsize=4096)
-def _matmul_size(m: int, n: int, k: int, out_type: int) -> int:
-    size = c_size_t(0)
-    lm._check(lm.lib().malt_block_matmul_size(m, n, k, out_type, byref(size)))
-    return size.value
-
-
-def _matmul(m, n, k, a: _Operand, b_values: int, b_scales: int, b_strides, dtype, device, s):
-    """a b^T over k; b_strides: those of a weight's block scales, or None for an operand's."""
-    out = torch.empty((m, n), dtype=dtype, device=device)
-    size = _matmul_size(m, n, k, _DTYPES[dtype])
-    ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
-    blocks, (i, j) = (0, (0, 0)) if b_strides is None else (1, b_strides)
-    lm._check(lm.lib().malt_block_matmul(m, n, k, a.values, a.scales, b_values, b_scales, blocks, i, j, out.data_ptr(),
-                                         _DTYPES[dtype], n, 0, ws.data_ptr() if size else None, size, s))
-    return out
+    lm._check(lm.lib().malt_block_quantize_weight(w.data_ptr(), _DTYPES[w.dtype], r, c, ld, values.data_ptr(),
+                                                  scales.data_ptr(), None, s))
+    return values, scales
 
 
 @functools.lru_cache(maxsize=4096)
@@ -398,39 +347,63 @@ def _linear_size(m: int, n: int, k: int, out_type: int) -> int:
     return size.value
 
 
+@functools.lru_cache(maxsize=4096)
+def _layer_sizes(m: int, n: int, k: int, types: Tuple[int, int, int], need_x: bool, need_w: bool) -> Tuple[int, int, int]:
+    """Bytes kept for the backward pass, and of the workspaces of both passes."""
+    sizes = (c_size_t(0), c_size_t(0), c_size_t(0))
+    lm._check(lm.lib().malt_block_layer_size(m, n, k, *types, int(need_x), int(need_w), *map(byref, sizes)))
+    return tuple(s.value for s in sizes)
+
+
 class _Fp8Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, out_dtype):
+        dev = x.device
+        n, k = weight.shape
+        xt, wt, yt = _DTYPES[x.dtype], _DTYPES[weight.dtype], _DTYPES[out_dtype]
         need_x, need_w = ctx.needs_input_grad[:2]
-        y, xt, wt, w_scales = _linear(x, weight, out_dtype, None, need_w, need_x)
-        ctx.save_for_backward(xt.buf if xt else None, wt, w_scales)
-        ctx.args = (x.shape, x.dtype, weight.shape, weight.dtype)
+        flat, ldx = _rows(_flat(x) if x.dim() > 1 else x.reshape(1, -1))
+        w, ldw = _rows(weight)
+        m = flat.shape[0]
+        sizes = _layer_sizes(m, n, k, (yt, xt, wt), need_x, need_w) if m else (0, 0, 0)
+
+        def work(s):
+            y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
+            kept = torch.empty(sizes[0], dtype=torch.uint8, device=dev)
+            if m:
+                ws = torch.empty(sizes[1], dtype=torch.uint8, device=dev)
+                lm._check(lm.lib().malt_block_layer_forward(
+                    flat.data_ptr(), xt, m, k, ldx, w.data_ptr(), wt, n, ldw, y.data_ptr(), yt, n, need_x, need_w,
+                    kept.data_ptr(), sizes[0], ws.data_ptr(), sizes[1], s))
+            return y, kept
+
+        y, kept = _on(dev, None, (), work)
+        ctx.save_for_backward(kept)
+        ctx.args = (x.shape, x.dtype, weight.dtype, m, n, k, sizes)
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        xt, wt, w_scales = ctx.saved_tensors
-        x_shape, x_dtype, (n, k), w_dtype = ctx.args
+        (kept,) = ctx.saved_tensors
+        x_shape, x_dtype, w_dtype, m, n, k, sizes = ctx.args
         need_x, need_w = ctx.needs_input_grad[:2]
         dev = dy.device
         if dy.dtype not in _DTYPES:
             dy = dy.float()
-        g = dy.reshape(-1, n)
-        m = g.shape[0]
         if m == 0:
             return (torch.zeros(x_shape, dtype=x_dtype, device=dev) if need_x else None,
                     torch.zeros((n, k), dtype=w_dtype, device=dev) if need_w else None, None)
+        g, ld = _rows(dy if dy.dim() == 2 else dy.reshape(-1, n))
 
         def work(s):
-            q, t = _quantize(g, s, need_x, need_w)
-            dx = dw = None
-            if need_x:
-                dx = _matmul(m, k, n, q, wt.data_ptr(), w_scales.data_ptr(), (1, w_scales.shape[1]), x_dtype, dev, s)
-                dx = dx.reshape(x_shape)
-            if need_w:
-                o = _Operand(xt, k, m)
-                dw = _matmul(n, k, m, t, o.values, o.scales, None, w_dtype, dev, s)
+            dx = torch.empty(x_shape, dtype=x_dtype, device=dev) if need_x else None
+            dw = torch.empty((n, k), dtype=w_dtype, device=dev) if need_w else None
+            ws = torch.empty(sizes[2], dtype=torch.uint8, device=dev)
+            lm._check(lm.lib().malt_block_layer_backward(
+                g.data_ptr(), _DTYPES[g.dtype], m, n, ld, k, kept.data_ptr(), sizes[0],
+                dx.data_ptr() if need_x else None, _DTYPES[x_dtype], k, dw.data_ptr() if need_w else None,
+                _DTYPES[w_dtype], k, 0, ws.data_ptr(), sizes[2], s))
             return dx, dw, None
 
         return _on(dev, None, (), work)
@@ -447,24 +420,18 @@ def _kept(flat, values: int, scales: int, n: int, out, s) -> None:
                                          out.data_ptr(), out_type, n, ws.data_ptr() if size else None, size, s))
 
 
-def _linear(x, weight, out_dtype, stream, keep_x, keep_w):
-    """The layer's output, and what its backward pass needs: x^T and W^T in 8 bits, W's scales."""
+def _linear(x, weight, out_dtype, stream):
+    """The layer without gradients."""
     dev = x.device
     n, k = weight.shape
     flat = _flat(x) if x.dim() > 1 else x.reshape(1, -1)
-    m = flat.shape[0]
 
     def work(s):
-        if m == 0:
-            return torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev), None, None, None
-        values, scales, wt = _quantize_weight(weight, s, True, keep_w)
-        if not keep_x:
-            y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
+        y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
+        if flat.shape[0]:
+            values, scales = _quantize_weight(weight, s)
             _kept(flat, values.data_ptr(), scales.data_ptr(), n, y, s)
-            return y, None, wt, scales
-        q, xt = _quantize(flat, s, True, True)
-        y = _matmul(m, n, k, q, values.data_ptr(), scales.data_ptr(), (scales.shape[1], 1), out_dtype, dev, s)
-        return y if x.dim() == 2 else y.reshape(*x.shape[:-1], n), xt, wt, scales
+        return y
 
     return _on(dev, stream, (x, weight), work)
 
@@ -499,7 +466,7 @@ def fp8_linear(x: torch.Tensor, weight: torch.Tensor, out_dtype: Optional[torch.
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad):
         _no_stream(stream)
         return _Fp8Linear.apply(x, weight, out_dtype)
-    return _linear(x, weight, out_dtype, stream, False, False)[0]
+    return _linear(x, weight, out_dtype, stream)
 
 
 def fp8_quantize_weight(weight: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -509,7 +476,7 @@ def fp8_quantize_weight(weight: torch.Tensor, stream=None) -> Tuple[torch.Tensor
     (outer blocks, inner blocks).  value * 2^(scale - 127) is what it stands for."""
     _weight(weight)
     weight = weight.detach()
-    values, scales, _ = _on(weight.device, stream, (weight,), lambda s: _quantize_weight(weight, s, True, False))
+    values, scales = _on(weight.device, stream, (weight,), lambda s: _quantize_weight(weight, s))
     return values.view(torch.float8_e4m3fn), scales
 
 

@@ -5,6 +5,7 @@ offsets, repeated ids, other streams, captured graphs.
 Tolerances follow from the arithmetic.  u = 2^-24 is float32's unit roundoff,
 2^-8 bfloat16's; a sum of n float32 terms is off by at most n u sum|x|.
 """
+import ctypes
 import math
 
 import pytest
@@ -568,15 +569,31 @@ def test_layer_shapes_pitches_and_empty_batches(ops):
         ops.fp8_forward(x, kept[0], kept[1].t())
 
 
+class Operand:
+    """x as an operand along its columns, through the C entries."""
+
+    def __init__(self, x):
+        v, s = ctypes.c_size_t(0), ctypes.c_size_t(0)
+        r, c = x.shape
+        lm._check(lm.lib().malt_block_size(r, c, ctypes.byref(v), ctypes.byref(s)))
+        self.buf = torch.empty(v.value + s.value, dtype=torch.uint8, device="cuda")
+        self.values, self.scales = self.buf.data_ptr(), self.buf.data_ptr() + v.value
+        t = lm.MALT_BFLOAT16 if x.dtype == BF16 else lm.MALT_FLOAT32
+        lm._check(lm.lib().malt_block_quantize(x.data_ptr(), t, r, c, x.stride(0), self.values, self.scales, None, None,
+                                               torch.cuda.current_stream().cuda_stream))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("m,n,k", [(50, 60, 200), (50, 60, 6000), (2100, 2200, 128)])
 def test_product_accumulates(ops, dtype, m, n, k):
     """The C entry's accumulation, whole and cut along k, into rows of a larger pitch."""
     a, b = randn(420, m, k), randn(421, n, k)
     s = torch.cuda.current_stream().cuda_stream
-    qa, qb = ops._quantize(a, s, True, False)[0], ops._quantize(b, s, True, False)[0]
+    qa, qb = Operand(a), Operand(b)
     t = lm.MALT_BFLOAT16 if dtype == BF16 else lm.MALT_FLOAT32
-    size = ops._matmul_size(m, n, k, t)
+    need = ctypes.c_size_t(0)
+    lm._check(lm.lib().malt_block_matmul_size(m, n, k, t, ctypes.byref(need)))
+    size = need.value
     assert (size > 0) == (k == 6000)
     ws = torch.empty(max(size, 1), dtype=torch.uint8, device="cuda")
     old = randn(422, m, n, dtype=dtype)
@@ -590,12 +607,34 @@ def test_product_accumulates(ops, dtype, m, n, k):
     assert bool(torch.isnan(out.as_strided((m - 1, 3), (n + 3, 1), n)).all())   # nothing written between the rows
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m", [40, 5000])
+def test_layer_accumulates_its_weight_gradient(ops, dtype, m):
+    n, k = 70, 200
+    x, w, dy = _uneven(440, m, k, F32), _uneven(441, n, k, F32), _uneven(442, m, n, F32)
+    t = lm.MALT_BFLOAT16 if dtype == BF16 else lm.MALT_FLOAT32
+    s = torch.cuda.current_stream().cuda_stream
+    kept_n, fwd_n, bwd_n = ctypes.c_size_t(0), ctypes.c_size_t(0), ctypes.c_size_t(0)
+    lm._check(lm.lib().malt_block_layer_size(m, n, k, 0, 0, t, 0, 1, *map(ctypes.byref, (kept_n, fwd_n, bwd_n))))
+    kept, fwd, bwd = (torch.empty(c.value, dtype=torch.uint8, device="cuda") for c in (kept_n, fwd_n, bwd_n))
+    y, old = torch.empty((m, n), device="cuda"), randn(443, n, k, dtype=dtype)
+    dw = pitched(old, 3)
+    lm._check(lm.lib().malt_block_layer_forward(x.data_ptr(), 0, m, k, k, w.data_ptr(), 0, n, k, y.data_ptr(), 0, n, 0, 1,
+                                                kept.data_ptr(), kept_n.value, fwd.data_ptr(), fwd_n.value, s))
+    lm._check(lm.lib().malt_block_layer_backward(dy.data_ptr(), 0, m, n, n, k, kept.data_ptr(), kept_n.value, None, 0, k,
+                                                 dw.data_ptr(), t, k + 3, 1, bwd.data_ptr(), bwd_n.value, s))
+    a, b = _rounded64(dy, 128, 1)[0].t().contiguous(), _rounded64(x, 128, 1)[0].t().contiguous()
+    want, tall = a @ b.t() + old.double().cpu(), a.abs() @ b.abs().t() + old.double().cpu().abs()
+    tol = 2.0 ** -11 * tall + rounding(BF16) * want.abs() * 1.01 if dtype == BF16 else (m + 3) * U * tall
+    assert bool(((dw.double().cpu() - want).abs() <= tol).all())
+
+
 def test_product_beyond_32_bit_offsets(ops):
     """An output whose rows start past 2^32 elements."""
     m, n, k = 3, 40, 130
     a, b = randn(430, m, k), randn(431, n, k)
     s = torch.cuda.current_stream().cuda_stream
-    qa, qb = ops._quantize(a, s, True, False)[0], ops._quantize(b, s, True, False)[0]
+    qa, qb = Operand(a), Operand(b)
     ld = (1 << 31) - 1
     out = torch.empty(2 * ld + 64, dtype=BF16, device="cuda").as_strided((m, n), (ld, 1))
     lm._check(lm.lib().malt_block_matmul(m, n, k, qa.values, qa.scales, qb.values, qb.scales, 0, 0, 0, out.data_ptr(),

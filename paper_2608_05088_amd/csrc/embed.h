@@ -37,6 +37,7 @@ struct EmbedGradArgs {
   float* part;             // [chunk][2][part_ld]
   int64_t part_ld;
   int32_t chunk;
+  int32_t lanes_log2;      // narrow tables: lanes of a row
 };
 
 struct EmbedGradLayout {
@@ -47,7 +48,7 @@ struct EmbedGradLayout {
 
 EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width);
 hipError_t launch_embed_lookup(EmbedLookupArgs a, bool table_f32, bool out_f32, hipStream_t s);
-hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32,
+hipError_t launch_embed_grad(const EmbedGradArgs& a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32,
                              hipStream_t s);
 
 }  // namespace malt

@@ -17,7 +17,8 @@ namespace malt {
 namespace {
 
 constexpr int DIGIT = 8, BINS = 1 << DIGIT;
-constexpr int STRIP = 256;   // columns a wave takes, four a lane
+constexpr int STRIP = 256;     // columns a wave takes, four a lane
+constexpr int FILL_VECS = 4;   // groups of four columns a thread fills with zeros
 
 // ------------------------------------------------------------------- lookup
 template <class TI, class TO>
@@ -213,13 +214,38 @@ __global__ __launch_bounds__(256) void embed_segments_kernel(EmbedGradArgs a) {
   if (j + 1 == a.tokens || gptr(a.keys)[j + 1] != k) gptr(a.seg)[2 * (int64_t)k + 1] = (uint32_t)(j + 1);
 }
 
-// Up to SORT_ONE tokens: all passes in the LDS of one workgroup, and the
-// segments.  Wave w's keys are a run of them, so ranks by wave are stable.
+// Zeros for FILL_VECS x 1024 groups of four columns from block b's on.
+template <class TO>
+__device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, int64_t b) {
+  const op_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  TO* const out = static_cast<TO*>(a.dtable);
+  // Rows without gaps are one long row.
+  const bool one = a.dtable_ld == a.width;
+  const int64_t width = one ? a.vocab * a.width : a.width, per = (width + 3) / 4, all = one ? per : per * a.vocab;
+#pragma unroll
+  for (int u = 0; u < FILL_VECS; ++u) {
+    const int64_t i = (b * FILL_VECS + u) * 1024 + threadIdx.x;
+    if (i < all) {
+      const int64_t row = one ? 0 : i / per;
+      row_store4(out + row * a.dtable_ld, 4 * (i - row * per), width, zero);
+    }
+  }
+}
+
+// Up to SORT_ONE tokens: all passes in the LDS of workgroup 0, and the segments.
+// Wave w's keys are a run of them, so ranks by wave are stable.  Meanwhile the
+// other workgroups fill the table with zeros: a sort of 8192 tokens takes one CU
+// 25 us, the rest of the chip as long for the 200 MB of a table.
+template <class TO>
 __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedGradArgs a, int bits, uint32_t* keys_out, uint32_t* order_out) {
   constexpr int NW = 16, R = SORT_ONE / 1024;
   __shared__ uint32_t skey[SORT_ONE];
   __shared__ uint16_t sidx[SORT_ONE];
   __shared__ uint32_t hist[NW][BINS], part[BINS / 64];
+  if (blockIdx.x > 0) {
+    fill_rows<TO>(a, blockIdx.x - 1);
+    return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tokens = (int)a.tokens;
   const int rounds = (tokens + 1023) / 1024;
@@ -232,8 +258,6 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedGradArgs a, int bit
     idx[r] = (uint32_t)(base + r * 64 + lane);
     if (r * 64 + lane < n) key[r] = token_key(a, base + r * 64 + lane);
   }
-  // Rows without tokens have an empty segment.
-  for (int64_t v = tid; v < a.vocab; v += 1024) gptr(reinterpret_cast<op_u32x2*>(a.seg))[v] = op_u32x2{0u, 0u};
   for (int shift = 0; shift < bits; shift += DIGIT) {
     for (int i = tid; i < NW * BINS; i += 1024) (&hist[0][0])[i] = 0;
     __syncthreads();
@@ -267,8 +291,6 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedGradArgs a, int bit
         idx[r] = sidx[base + r * 64 + lane];
       }
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the segments are empty before any is written
-  __syncthreads();
 #pragma unroll
   for (int r = 0; r < R; ++r)
     if (r * 64 + lane < n) {
@@ -330,46 +352,6 @@ __device__ __forceinline__ void finish_row(const EmbedGradArgs& a, TO* out, int 
   row_store4(out, c0 + 4 * lane, a.width, x);
 }
 
-// Few tokens: the wave of a row and strip looks all of them over itself.
-template <class TG, class TO>
-__global__ __launch_bounds__(256) void embed_few_kernel(EmbedGradArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t v = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (v >= a.vocab) return;
-  const int c0 = blockIdx.y * STRIP, tokens = (int)a.tokens;
-  uint64_t met[FEW / 64];
-#pragma unroll
-  for (int b = 0; b < FEW / 64; ++b) {
-    const int t = b * 64 + lane;
-    met[b] = b * 64 < tokens ? __ballot(t < tokens && load_id(a.ids, a.wide_ids, t) == v) : 0;
-  }
-  uint64_t any = 0;
-#pragma unroll
-  for (int b = 0; b < FEW / 64; ++b) any |= met[b];
-  TO* out = static_cast<TO*>(a.dtable) + v * a.dtable_ld;
-  op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  if (!any) {
-    if (!a.accumulate) row_store4(out, c0 + 4 * lane, a.width, x);
-    return;
-  }
-#pragma unroll
-  for (int b = 0; b < FEW / 64; ++b) {
-    uint64_t m = met[b];
-    while (m) {
-      const int n = __popcll(m);
-      uint32_t t[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        t[u] = m ? (uint32_t)(b * 64 + __builtin_ctzll(m)) : 0;
-        m &= m - 1;   // 0 stays 0
-      }
-      add_rows(x, static_cast<const TG*>(a.grad), a.grad_ld, n < 8 ? n : 8, c0, lane, a.width,
-                    [&](int u) { return t[u]; });
-    }
-  }
-  finish_row(a, out, c0, lane, x);
-}
-
 // Chunk c of the sorted tokens, one strip: partial sums of the segments longer
 // than a chunk.  Such a segment holds the chunk's first or last token, so a
 // chunk has two slots: 0 for the segment its first token belongs to, 1 for one
@@ -394,34 +376,128 @@ __global__ __launch_bounds__(256) void embed_chunks_kernel(EmbedGradArgs a) {
   }
 }
 
-// One row of the table, one strip a wave.
-template <class TG, class TO>
-__global__ __launch_bounds__(256) void embed_rows_kernel(EmbedGradArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t v = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (v >= a.vocab) return;
-  const int c0 = blockIdx.y * STRIP;
-  const int64_t s = a.seg[2 * v], e = a.seg[2 * v + 1];
-  TO* out = static_cast<TO*>(a.dtable) + v * a.dtable_ld;
-  op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  if (s == e) {
-    if (!a.accumulate) row_store4(out, c0 + 4 * lane, a.width, x);
-    return;
-  }
-  if (e - s <= a.chunk) {
-    x = sum_rows(static_cast<const TG*>(a.grad), a.grad_ld, a.order, s, e, c0, lane, a.width);
-  } else {
-    const int64_t k0 = s / a.chunk, k1 = (e - 1) / a.chunk;
-    const float* part = a.part + c0 + 4 * lane;
-    x = load4(part + (2 * k0 + (s > k0 * a.chunk ? 1 : 0)) * a.part_ld);
+// The sum of a row's sorted tokens [s, e), one strip: taken here, or from its chunks'.
+template <class TG>
+__device__ __forceinline__ op_f32x4 row_sum(const EmbedGradArgs& a, int64_t s, int64_t e, int c0, int lane) {
+  if (e - s <= a.chunk) return sum_rows(static_cast<const TG*>(a.grad), a.grad_ld, a.order, s, e, c0, lane, a.width);
+  const int64_t k0 = s / a.chunk, k1 = (e - 1) / a.chunk;
+  const float* part = a.part + c0 + 4 * lane;
+  op_f32x4 x = load4(part + (2 * k0 + (s > k0 * a.chunk ? 1 : 0)) * a.part_ld);
 #pragma unroll 8
-    for (int64_t k = k0 + 1; k <= k1; ++k) {
-      const op_f32x4 p = load4(part + 2 * k * a.part_ld);
+  for (int64_t k = k0 + 1; k <= k1; ++k) x += load4(part + 2 * k * a.part_ld);
+  return x;
+}
+
+// Tables wider than NARROW: a wave takes a row and a strip.  How it comes by the
+// row and its tokens is one of three:
+enum Source {
+  EVERY,      // every row of the table, with its segment of the sorted tokens (empty: zeros)
+  MET,        // every sorted token that is the first of its row (the other rows are zeros already)
+  LOOK        // every row; few tokens, all of which the wave looks over itself
+};
+template <class TG, class TO, int SOURCE>
+__global__ __launch_bounds__(256) void embed_rows_kernel(EmbedGradArgs a) {
+  const int lane = threadIdx.x & 63, c0 = blockIdx.y * STRIP;
+  const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  int64_t v = i;
+  if constexpr (SOURCE == LOOK) {
+    if (i >= a.vocab) return;
+    uint64_t met[FEW / 64], any = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] += p[i];
+    for (int b = 0; b < FEW / 64; ++b) {
+      const int t = b * 64 + lane;
+      met[b] = b * 64 < a.tokens ? __ballot(t < a.tokens && load_id(a.ids, a.wide_ids, t) == v) : 0;
+      any |= met[b];
+    }
+    if (any) {
+#pragma unroll
+      for (int b = 0; b < FEW / 64; ++b) {
+        uint64_t m = met[b];
+        while (m) {
+          const int n = __popcll(m);
+          uint32_t t[8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            t[u] = m ? (uint32_t)(b * 64 + __builtin_ctzll(m)) : 0;
+            m &= m - 1;   // 0 stays 0
+          }
+          add_rows(x, static_cast<const TG*>(a.grad), a.grad_ld, n < 8 ? n : 8, c0, lane, a.width, [&](int u) { return t[u]; });
+        }
+      }
+    } else if (a.accumulate) {
+      return;
+    }
+  } else {
+    int64_t s, e;
+    if constexpr (SOURCE == MET) {
+      if (i >= a.tokens) return;
+      const uint32_t k = a.keys[i];
+      if (k >= (uint32_t)a.vocab || (i > 0 && a.keys[i - 1] == k)) return;
+      v = k;
+      s = i;
+      e = a.seg[2 * v + 1];
+    } else {
+      if (i >= a.vocab) return;
+      s = a.seg[2 * v];
+      e = a.seg[2 * v + 1];
+      if (s == e && a.accumulate) return;
+    }
+    if (s != e) x = row_sum<TG>(a, s, e, c0, lane);
+  }
+  finish_row(a, static_cast<TO*>(a.dtable) + v * a.dtable_ld, c0, lane, x);
+}
+
+// Narrow tables: 2^lanes_log2 < 64 lanes take a row, so a wave has several, and
+// each lane goes through its row's tokens by itself.
+template <class TG, class TO, int SOURCE>
+__global__ __launch_bounds__(256) void embed_narrow_kernel(EmbedGradArgs a) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2;
+  const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1);
+  const TG* const grad = static_cast<const TG*>(a.grad);
+  op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  int64_t v = i;
+  if constexpr (SOURCE == LOOK) {
+    if (i >= a.vocab) return;
+    bool any = false;
+    for (int t = 0; t < a.tokens; ++t)
+      if (load_id(a.ids, a.wide_ids, t) == v) {
+        any = true;
+        x += row_load4(grad + (int64_t)t * a.grad_ld, 4 * lane, a.width);
+      }
+    if (!any && a.accumulate) return;
+  } else {
+    int64_t s, e;
+    if constexpr (SOURCE == MET) {
+      if (i >= a.tokens) return;
+      const uint32_t k = gptr(a.keys)[i];
+      if (k >= (uint32_t)a.vocab || (i > 0 && gptr(a.keys)[i - 1] == k)) return;
+      v = k;
+      s = i;
+      e = gptr(a.seg)[2 * v + 1];
+    } else {
+      if (i >= a.vocab) return;
+      s = gptr(a.seg)[2 * v];
+      e = gptr(a.seg)[2 * v + 1];
+      if (s == e && a.accumulate) return;
+    }
+    if (e - s > a.chunk) {
+      x = row_sum<TG>(a, s, e, 0, lane);
+    } else {
+      for (int64_t j = s; j < e; j += 4) {
+        op_f32x4 y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          y[u] = op_f32x4{0.f, 0.f, 0.f, 0.f};
+          if (j + u < e) y[u] = row_load4(grad + (int64_t)gptr(a.order)[j + u] * a.grad_ld, 4 * lane, a.width);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (j + u < e) x += y[u];
+      }
     }
   }
-  finish_row(a, out, c0, lane, x);
+  finish_row(a, static_cast<TO*>(a.dtable) + v * a.dtable_ld, 0, lane, x);
 }
 
 }  // namespace
@@ -459,55 +535,66 @@ EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width) 
   return L;
 }
 
-template <class TG, class TO>
-static void grad_typed(const EmbedGradArgs& a, hipStream_t s) {
-  const unsigned strips = (unsigned)((a.width + STRIP - 1) / STRIP);
-  const dim3 grid((unsigned)((a.vocab + 3) / 4), strips);
-  if (a.tokens <= FEW) {
-    hipLaunchKernelGGL((embed_few_kernel<TG, TO>), grid, dim3(256), 0, s, a);
-    return;
-  }
-  const unsigned chunks = (unsigned)((a.tokens + a.chunk - 1) / a.chunk);
-  hipLaunchKernelGGL((embed_chunks_kernel<TG>), dim3(chunks, (strips + 3) / 4), dim3(256), 0, s, a);
-  hipLaunchKernelGGL((embed_rows_kernel<TG, TO>), grid, dim3(256), 0, s, a);
+template <class TG, class TO, int SOURCE>
+static void rows_typed(EmbedGradArgs a, hipStream_t s) {
+  const int64_t rows = SOURCE == MET ? a.tokens : a.vocab;
+  a.lanes_log2 = 0;
+  while ((4 << a.lanes_log2) < a.width) ++a.lanes_log2;
+  if (a.lanes_log2 < 6)
+    hipLaunchKernelGGL((embed_narrow_kernel<TG, TO, SOURCE>), dim3((unsigned)(((rows << a.lanes_log2) + 255) / 256)), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((embed_rows_kernel<TG, TO, SOURCE>), dim3((unsigned)((rows + 3) / 4), (unsigned)((a.width + STRIP - 1) / STRIP)),
+                       dim3(256), 0, s, a);
 }
 
-hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32,
-                             hipStream_t s) {
-  if (a.tokens > FEW) {
-    uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + L.keys[0]), reinterpret_cast<uint32_t*>(ws + L.keys[1])};
-    uint32_t* index[2] = {reinterpret_cast<uint32_t*>(ws + L.index[0]), reinterpret_cast<uint32_t*>(ws + L.index[1])};
-    a.table = reinterpret_cast<uint32_t*>(ws + L.table);
-    a.seg = reinterpret_cast<uint32_t*>(ws + L.seg);
-    a.part = reinterpret_cast<float*>(ws + L.part);
-    a.part_ld = L.part_ld;
-    a.chunk = L.chunk;
-    int bits = 1;   // keys run up to vocab
-    while ((int64_t(1) << bits) <= a.vocab) ++bits;
-    int to = 0;
-    if (a.tokens <= SORT_ONE) {
-      hipLaunchKernelGGL(sort_one_kernel, dim3(1), dim3(1024), 0, s, a, bits, keys[0], index[0]);
-      to = 1;
-    } else {
-      const dim3 grid((unsigned)L.blocks), threads(SORT_THREADS);
-      for (int shift = 0; shift < bits; shift += DIGIT, to ^= 1) {
-        const uint32_t *k = keys[to ^ 1], *i = index[to ^ 1];
-        if (shift == 0) hipLaunchKernelGGL(sort_count_kernel<true>, grid, threads, 0, s, a, shift, k);
-        else hipLaunchKernelGGL(sort_count_kernel<false>, grid, threads, 0, s, a, shift, k);
-        hipLaunchKernelGGL(sort_scan_kernel, dim3(BINS), dim3(256), 0, s, a.table, int(L.blocks));
-        if (shift == 0) hipLaunchKernelGGL(sort_place_kernel<true>, grid, threads, 0, s, a, shift, k, i, keys[to], index[to]);
-        else hipLaunchKernelGGL(sort_place_kernel<false>, grid, threads, 0, s, a, shift, k, i, keys[to], index[to]);
-      }
-      a.keys = keys[to ^ 1];
-      hipLaunchKernelGGL(embed_segments_kernel, dim3((unsigned)((a.tokens + 255) / 256)), dim3(256), 0, s, a);
+template <class TG, class TO>
+static void grad_typed(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, hipStream_t s) {
+  if (a.tokens <= FEW) return rows_typed<TG, TO, LOOK>(a, s);
+  uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + L.keys[0]), reinterpret_cast<uint32_t*>(ws + L.keys[1])};
+  uint32_t* index[2] = {reinterpret_cast<uint32_t*>(ws + L.index[0]), reinterpret_cast<uint32_t*>(ws + L.index[1])};
+  a.table = reinterpret_cast<uint32_t*>(ws + L.table);
+  a.seg = reinterpret_cast<uint32_t*>(ws + L.seg);
+  a.part = reinterpret_cast<float*>(ws + L.part);
+  a.part_ld = L.part_ld;
+  a.chunk = L.chunk;
+  int bits = 1;   // keys run up to vocab
+  while ((int64_t(1) << bits) <= a.vocab) ++bits;
+  int to = 0;
+  const bool one = a.tokens <= SORT_ONE;
+  if (one) {
+    int64_t fill = 0;
+    if (!a.accumulate) {
+      const int64_t vecs = a.dtable_ld == a.width ? (a.vocab * a.width + 3) / 4 : a.vocab * ((a.width + 3) / 4);
+      fill = (vecs + FILL_VECS * 1024 - 1) / (FILL_VECS * 1024);
     }
-    a.keys = keys[to ^ 1];
-    a.order = index[to ^ 1];
+    hipLaunchKernelGGL((sort_one_kernel<TO>), dim3((unsigned)(1 + fill)), dim3(1024), 0, s, a, bits, keys[0], index[0]);
+    to = 1;
+  } else {
+    const dim3 grid((unsigned)L.blocks), threads(SORT_THREADS);
+    for (int shift = 0; shift < bits; shift += DIGIT, to ^= 1) {
+      const uint32_t *k = keys[to ^ 1], *i = index[to ^ 1];
+      if (shift == 0) hipLaunchKernelGGL(sort_count_kernel<true>, grid, threads, 0, s, a, shift, k);
+      else hipLaunchKernelGGL(sort_count_kernel<false>, grid, threads, 0, s, a, shift, k);
+      hipLaunchKernelGGL(sort_scan_kernel, dim3(BINS), dim3(256), 0, s, a.table, int(L.blocks));
+      if (shift == 0) hipLaunchKernelGGL(sort_place_kernel<true>, grid, threads, 0, s, a, shift, k, i, keys[to], index[to]);
+      else hipLaunchKernelGGL(sort_place_kernel<false>, grid, threads, 0, s, a, shift, k, i, keys[to], index[to]);
+    }
   }
-  if (grad_f32 && out_f32) grad_typed<float, float>(a, s);
-  else if (grad_f32) grad_typed<float, bf16_t>(a, s);
-  else if (out_f32) grad_typed<bf16_t, float>(a, s);
-  else grad_typed<bf16_t, bf16_t>(a, s);
+  a.keys = keys[to ^ 1];
+  a.order = index[to ^ 1];
+  if (!one) hipLaunchKernelGGL(embed_segments_kernel, dim3((unsigned)((a.tokens + 255) / 256)), dim3(256), 0, s, a);
+  const unsigned strips = (unsigned)((a.width + STRIP - 1) / STRIP), chunks = (unsigned)((a.tokens + a.chunk - 1) / a.chunk);
+  hipLaunchKernelGGL((embed_chunks_kernel<TG>), dim3(chunks, (strips + 3) / 4), dim3(256), 0, s, a);
+  if (one) rows_typed<TG, TO, MET>(a, s);
+  else rows_typed<TG, TO, EVERY>(a, s);
+}
+
+hipError_t launch_embed_grad(const EmbedGradArgs& a, const EmbedGradLayout& L, char* ws, bool grad_f32, bool out_f32,
+                             hipStream_t s) {
+  if (grad_f32 && out_f32) grad_typed<float, float>(a, L, ws, s);
+  else if (grad_f32) grad_typed<float, bf16_t>(a, L, ws, s);
+  else if (out_f32) grad_typed<bf16_t, float>(a, L, ws, s);
+  else grad_typed<bf16_t, bf16_t>(a, L, ws, s);
   return hipGetLastError();
 }
 

@@ -414,23 +414,25 @@ malt_status_t malt_block_linear(const void* x, malt_dtype_t x_type, int64_t m, i
  *   forward:  y = Q(x) Q(w)^T, x by rows, w by 128 x 128 blocks;
  *   backward: dx = Q(dy) Q(w), dy by rows;  dw = Q(dy)^T Q(x), both by columns of
  *             128 rows; dw is added to with accumulate.
+ * w_transposed: w and dw lie k x n (y = x w), as GPT-2's layers store them.
  * `kept` carries what the backward pass needs from the forward's: x^T (for dw),
- * w^T (for dx) and w's scales, in 8 bits.  need_dx, need_dw: which gradients will
+ * w (for dx) and w's scales, in 8 bits.  need_dx, need_dw: which gradients will
  * be asked for; the backward call must ask (dx, dw not NULL) for those.
  * malt_block_layer_size gives the bytes of kept and of both workspaces, all
  * 256-byte aligned; NULL is fine where it says 0.
  * Limits: those of the products. */
-malt_status_t malt_block_layer_size(int64_t m, int64_t n, int64_t k, malt_dtype_t y_type, malt_dtype_t dx_type,
-                                    malt_dtype_t dw_type, int32_t need_dx, int32_t need_dw, size_t* kept_bytes,
-                                    size_t* forward_bytes, size_t* backward_bytes);
+malt_status_t malt_block_layer_size(int64_t m, int64_t n, int64_t k, int32_t w_transposed, malt_dtype_t y_type,
+                                    malt_dtype_t dx_type, malt_dtype_t dw_type, int32_t need_dx, int32_t need_dw,
+                                    size_t* kept_bytes, size_t* forward_bytes, size_t* backward_bytes);
 malt_status_t malt_block_layer_forward(const void* x, malt_dtype_t x_type, int64_t m, int64_t k, int64_t ldx,
-                                       const void* w, malt_dtype_t w_type, int64_t n, int64_t ldw, void* y,
-                                       malt_dtype_t y_type, int64_t ldy, int32_t need_dx, int32_t need_dw, void* kept,
-                                       size_t kept_bytes, void* workspace, size_t workspace_bytes, void* stream);
+                                       const void* w, malt_dtype_t w_type, int64_t n, int64_t ldw, int32_t w_transposed,
+                                       void* y, malt_dtype_t y_type, int64_t ldy, int32_t need_dx, int32_t need_dw,
+                                       void* kept, size_t kept_bytes, void* workspace, size_t workspace_bytes,
+                                       void* stream);
 malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, int64_t m, int64_t n, int64_t lddy,
-                                        int64_t k, const void* kept, size_t kept_bytes, void* dx, malt_dtype_t dx_type,
-                                        int64_t lddx, void* dw, malt_dtype_t dw_type, int64_t lddw, int32_t accumulate,
-                                        void* workspace, size_t workspace_bytes, void* stream);
+                                        int64_t k, int32_t w_transposed, const void* kept, size_t kept_bytes, void* dx,
+                                        malt_dtype_t dx_type, int64_t lddx, void* dw, malt_dtype_t dw_type, int64_t lddw,
+                                        int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
 const char* malt_status_string(malt_status_t status);
 const char* malt_last_error(void);

@@ -384,7 +384,9 @@ struct LayerLayout {
   size_t g, g_scales, gt, gt_scales, backward_product, backward;
 };
 
-static LayerLayout layer_layout(int64_t m, int64_t n, int64_t k, bool y_f32, bool dx_f32, bool dw_f32, bool need_x, bool need_w) {
+// w_t: the weight lies k x n, and so does its gradient.
+static LayerLayout layer_layout(int64_t m, int64_t n, int64_t k, bool w_t, bool y_f32, bool dx_f32, bool dw_f32, bool need_x,
+                                bool need_w) {
   LayerLayout L = {};
   auto take = [](size_t& end, size_t bytes) {
     const size_t at = end;
@@ -414,7 +416,7 @@ static LayerLayout layer_layout(int64_t m, int64_t n, int64_t k, bool y_f32, boo
   size_t product = 0;   // the two products follow each other
   if (need_x) product = block_matmul_plan(m, k, n, dx_f32).bytes;
   if (need_w) {
-    const size_t b = block_matmul_plan(n, k, m, dw_f32).bytes;
+    const size_t b = block_matmul_plan(w_t ? k : n, w_t ? n : k, m, dw_f32).bytes;
     if (b > product) product = b;
   }
   L.backward_product = take(L.backward, product);
@@ -433,14 +435,15 @@ static malt_status_t check_layer(int64_t m, int64_t n, int64_t k) {
   return MALT_OK;
 }
 
-malt_status_t malt_block_layer_size(int64_t m, int64_t n, int64_t k, malt_dtype_t y_type, malt_dtype_t dx_type,
-                                    malt_dtype_t dw_type, int32_t need_dx, int32_t need_dw, size_t* kept_bytes,
-                                    size_t* forward_bytes, size_t* backward_bytes) {
+malt_status_t malt_block_layer_size(int64_t m, int64_t n, int64_t k, int32_t w_transposed, malt_dtype_t y_type,
+                                    malt_dtype_t dx_type, malt_dtype_t dw_type, int32_t need_dx, int32_t need_dw,
+                                    size_t* kept_bytes, size_t* forward_bytes, size_t* backward_bytes) {
   if (!kept_bytes || !forward_bytes || !backward_bytes) return fail(MALT_ERR_INVALID_ARG, "output pointer is NULL");
   if (!op_dtype_ok(y_type) || !op_dtype_ok(dx_type) || !op_dtype_ok(dw_type)) return fail(MALT_ERR_INVALID_ARG, "unknown element type");
+  if (w_transposed != 0 && w_transposed != 1) return fail(MALT_ERR_INVALID_ARG, "w_transposed must be 0 or 1");
   MALT_TRY(check_layer(m, n, k));
-  const LayerLayout L = layer_layout(m, n, k, y_type == MALT_FLOAT32, dx_type == MALT_FLOAT32, dw_type == MALT_FLOAT32,
-                                     need_dx != 0, need_dw != 0);
+  const LayerLayout L = layer_layout(m, n, k, w_transposed != 0, y_type == MALT_FLOAT32, dx_type == MALT_FLOAT32,
+                                     dw_type == MALT_FLOAT32, need_dx != 0, need_dw != 0);
   *kept_bytes = L.kept;
   *forward_bytes = L.forward;
   *backward_bytes = L.backward;
@@ -448,15 +451,18 @@ malt_status_t malt_block_layer_size(int64_t m, int64_t n, int64_t k, malt_dtype_
 }
 
 malt_status_t malt_block_layer_forward(const void* x, malt_dtype_t x_type, int64_t m, int64_t k, int64_t ldx,
-                                       const void* w, malt_dtype_t w_type, int64_t n, int64_t ldw, void* y,
-                                       malt_dtype_t y_type, int64_t ldy, int32_t need_dx, int32_t need_dw, void* kept,
-                                       size_t kept_bytes, void* workspace, size_t workspace_bytes, void* stream) {
+                                       const void* w, malt_dtype_t w_type, int64_t n, int64_t ldw, int32_t w_transposed,
+                                       void* y, malt_dtype_t y_type, int64_t ldy, int32_t need_dx, int32_t need_dw,
+                                       void* kept, size_t kept_bytes, void* workspace, size_t workspace_bytes,
+                                       void* stream) {
+  if (w_transposed != 0 && w_transposed != 1) return fail(MALT_ERR_INVALID_ARG, "w_transposed must be 0 or 1");
   MALT_TRY(check_layer(m, n, k));
-  const Mat xm = {"x", x, x_type, m, k, ldx}, wm = {"w", w, w_type, n, k, ldw}, ym = {"y", y, y_type, m, n, ldy};
+  const bool wt = w_transposed != 0;
+  const Mat xm = {"x", x, x_type, m, k, ldx}, wm = {"w", w, w_type, wt ? k : n, wt ? n : k, ldw}, ym = {"y", y, y_type, m, n, ldy};
   MALT_TRY(check_mat(xm));
   MALT_TRY(check_mat(wm));
   MALT_TRY(check_mat(ym));
-  const LayerLayout L = layer_layout(m, n, k, y_type == MALT_FLOAT32, false, false, need_dx != 0, need_dw != 0);
+  const LayerLayout L = layer_layout(m, n, k, wt, y_type == MALT_FLOAT32, false, false, need_dx != 0, need_dw != 0);
   MALT_TRY(check_workspace(kept, kept_bytes, L.kept));
   MALT_TRY(check_workspace(workspace, workspace_bytes, L.forward));
   struct Buf { const void* p; size_t n; };
@@ -475,30 +481,35 @@ malt_status_t malt_block_layer_forward(const void* x, malt_dtype_t x_type, int64
   qx.t_values = need_dw ? kb + L.xt : nullptr;
   qx.t_scales = need_dw ? kb + L.xt_scales : nullptr;
   qw.x = w;
-  qw.rows = n;
-  qw.cols = k;
+  qw.rows = wm.rows;
+  qw.cols = wm.cols;
   qw.ld = ldw;
-  qw.values = ws + L.w;
-  qw.t_values = need_dx ? kb + L.wt : nullptr;
+  // The forward product takes the weight as n rows, the input gradient as k.
+  uint8_t* const by_k = need_dx ? kb + L.wt : nullptr;
+  qw.values = wt ? by_k : ws + L.w;
+  qw.t_values = wt ? ws + L.w : by_k;
   qw.block_scales = kb + L.w_scales;
   const hipError_t e = launch_block_quant_pair(qx, x_type == MALT_FLOAT32, qw, w_type == MALT_FLOAT32, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "launching the 8-bit conversion");
-  return malt_block_matmul(m, n, k, ws + L.q, ws + L.q_scales, ws + L.w, kb + L.w_scales, 1, q_pad(k) / QB, 1, y, y_type,
-                           ldy, 0, ws + L.forward_product, L.forward - L.forward_product, stream);
+  return malt_block_matmul(m, n, k, ws + L.q, ws + L.q_scales, ws + L.w, kb + L.w_scales, 1, wt ? 1 : q_pad(k) / QB,
+                           wt ? q_pad(n) / QB : 1, y, y_type, ldy, 0, ws + L.forward_product, L.forward - L.forward_product, stream);
 }
 
 malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, int64_t m, int64_t n, int64_t lddy,
-                                        int64_t k, const void* kept, size_t kept_bytes, void* dx, malt_dtype_t dx_type,
-                                        int64_t lddx, void* dw, malt_dtype_t dw_type, int64_t lddw, int32_t accumulate,
-                                        void* workspace, size_t workspace_bytes, void* stream) {
+                                        int64_t k, int32_t w_transposed, const void* kept, size_t kept_bytes, void* dx,
+                                        malt_dtype_t dx_type, int64_t lddx, void* dw, malt_dtype_t dw_type, int64_t lddw,
+                                        int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+  if (w_transposed != 0 && w_transposed != 1) return fail(MALT_ERR_INVALID_ARG, "w_transposed must be 0 or 1");
   MALT_TRY(check_layer(m, n, k));
+  const bool wt = w_transposed != 0;
   if (!dx && !dw) return fail(MALT_ERR_INVALID_ARG, "neither dx nor dw is wanted");
   if (accumulate != 0 && accumulate != 1) return fail(MALT_ERR_INVALID_ARG, "accumulate must be 0 or 1");
-  const Mat g = {"dy", dy, dy_type, m, n, lddy}, xm = {"dx", dx, dx_type, m, k, lddx}, wm = {"dw", dw, dw_type, n, k, lddw};
+  const Mat g = {"dy", dy, dy_type, m, n, lddy}, xm = {"dx", dx, dx_type, m, k, lddx}, wm = {"dw", dw, dw_type, wt ? k : n, wt ? n : k, lddw};
   MALT_TRY(check_mat(g));
   if (dx) MALT_TRY(check_mat(xm));
   if (dw) MALT_TRY(check_mat(wm));
-  const LayerLayout L = layer_layout(m, n, k, false, dx_type == MALT_FLOAT32, dw_type == MALT_FLOAT32, dx != nullptr, dw != nullptr);
+  const LayerLayout L = layer_layout(m, n, k, wt, false, dx_type == MALT_FLOAT32, dw_type == MALT_FLOAT32, dx != nullptr,
+                                     dw != nullptr);
   MALT_TRY(check_workspace(kept, kept_bytes, L.kept));
   MALT_TRY(check_workspace(workspace, workspace_bytes, L.backward));
   struct Buf { const void* p; size_t n; };
@@ -525,11 +536,12 @@ malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, in
   if (e != hipSuccess) return hip_fail(e, "launching the 8-bit conversion");
   const size_t product = L.backward - L.backward_product;
   if (dx)
-    MALT_TRY(malt_block_matmul(m, k, n, ws + L.g, ws + L.g_scales, kb + L.wt, kb + L.w_scales, 1, 1, q_pad(k) / QB, dx, dx_type,
-                               lddx, 0, ws + L.backward_product, product, stream));
+    MALT_TRY(malt_block_matmul(m, k, n, ws + L.g, ws + L.g_scales, kb + L.wt, kb + L.w_scales, 1, wt ? q_pad(n) / QB : 1,
+                               wt ? 1 : q_pad(k) / QB, dx, dx_type, lddx, 0, ws + L.backward_product, product, stream));
+  const uint8_t *const gt = ws + L.gt, *const gs = ws + L.gt_scales, *const xt = kb + L.xt, *const xs = kb + L.xt_scales;
   if (dw)
-    MALT_TRY(malt_block_matmul(n, k, m, ws + L.gt, ws + L.gt_scales, kb + L.xt, kb + L.xt_scales, 0, 0, 0, dw, dw_type, lddw,
-                               accumulate, ws + L.backward_product, product, stream));
+    MALT_TRY(malt_block_matmul(wm.rows, wm.cols, m, wt ? xt : gt, wt ? xs : gs, wt ? gt : xt, wt ? gs : xs, 0, 0, 0, dw, dw_type,
+                               lddw, accumulate, ws + L.backward_product, product, stream));
   return MALT_OK;
 }
 

@@ -130,14 +130,14 @@ _SIGNATURES = [
     ("malt_block_linear_size", c_int32, [c_int64, c_int64, c_int64, c_int32, POINTER(c_size_t)]),
     ("malt_block_linear", c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_int64, c_void_p,
                                     c_int32, c_int64, c_void_p, c_size_t, c_void_p]),
-    ("malt_block_layer_size", c_int32, [c_int64, c_int64, c_int64, c_int32, c_int32, c_int32, c_int32, c_int32,
+    ("malt_block_layer_size", c_int32, [c_int64, c_int64, c_int64, c_int32, c_int32, c_int32, c_int32, c_int32, c_int32,
                                         POINTER(c_size_t), POINTER(c_size_t), POINTER(c_size_t)]),
     ("malt_block_layer_forward", c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p, c_int32, c_int64,
-                                           c_int64, c_void_p, c_int32, c_int64, c_int32, c_int32, c_void_p, c_size_t,
-                                           c_void_p, c_size_t, c_void_p]),
-    ("malt_block_layer_backward", c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_int64, c_void_p, c_size_t,
-                                            c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_int32, c_void_p,
-                                            c_size_t, c_void_p]),
+                                           c_int64, c_int32, c_void_p, c_int32, c_int64, c_int32, c_int32, c_void_p,
+                                           c_size_t, c_void_p, c_size_t, c_void_p]),
+    ("malt_block_layer_backward", c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_int64, c_int32, c_void_p,
+                                            c_size_t, c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_int32,
+                                            c_void_p, c_size_t, c_void_p]),
     ("malt_destroy_state", None, [c_void_p]),
     ("malt_status_string", c_char_p, [c_int32]),
     ("malt_last_error", c_char_p, []),

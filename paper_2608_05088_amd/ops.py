@@ -348,63 +348,69 @@ def _linear_size(m: int, n: int, k: int, out_type: int) -> int:
 
 
 @functools.lru_cache(maxsize=4096)
-def _layer_sizes(m: int, n: int, k: int, types: Tuple[int, int, int], need_x: bool, need_w: bool) -> Tuple[int, int, int]:
+def _layer_sizes(m: int, n: int, k: int, transposed: bool, types: Tuple[int, int, int], need_x: bool,
+                 need_w: bool) -> Tuple[int, int, int]:
     """Bytes kept for the backward pass, and of the workspaces of both passes."""
     sizes = (c_size_t(0), c_size_t(0), c_size_t(0))
-    lm._check(lm.lib().malt_block_layer_size(m, n, k, *types, int(need_x), int(need_w), *map(byref, sizes)))
+    lm._check(lm.lib().malt_block_layer_size(m, n, k, transposed, *types, need_x, need_w, *map(byref, sizes)))
     return tuple(s.value for s in sizes)
+
+
+def _layer_forward(x, weight, transposed, out_dtype, need_x, need_w, stream):
+    """The layer's output, what its backward pass needs, and the bytes of the buffers."""
+    dev = x.device
+    n, k = weight.shape[::-1] if transposed else weight.shape
+    xt, wt, yt = _DTYPES[x.dtype], _DTYPES[weight.dtype], _DTYPES[out_dtype]
+    flat, ldx = _rows(_flat(x) if x.dim() > 1 else x.reshape(1, -1))
+    w, ldw = _rows(weight)
+    m = flat.shape[0]
+    sizes = _layer_sizes(m, n, k, transposed, (yt, xt, wt), need_x, need_w) if m else (0, 0, 0)
+
+    def work(s):
+        y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
+        kept = torch.empty(sizes[0], dtype=torch.uint8, device=dev)
+        if m:
+            ws = torch.empty(sizes[1], dtype=torch.uint8, device=dev)
+            lm._check(lm.lib().malt_block_layer_forward(
+                flat.data_ptr(), xt, m, k, ldx, w.data_ptr(), wt, n, ldw, transposed, y.data_ptr(), yt, n, need_x, need_w,
+                kept.data_ptr(), sizes[0], ws.data_ptr(), sizes[1], s))
+        return y, kept
+
+    return (*_on(dev, stream, (flat, w), work), (m, n, k, sizes))
 
 
 class _Fp8Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, out_dtype):
-        dev = x.device
-        n, k = weight.shape
-        xt, wt, yt = _DTYPES[x.dtype], _DTYPES[weight.dtype], _DTYPES[out_dtype]
+    def forward(ctx, x, weight, transposed, out_dtype):
         need_x, need_w = ctx.needs_input_grad[:2]
-        flat, ldx = _rows(_flat(x) if x.dim() > 1 else x.reshape(1, -1))
-        w, ldw = _rows(weight)
-        m = flat.shape[0]
-        sizes = _layer_sizes(m, n, k, (yt, xt, wt), need_x, need_w) if m else (0, 0, 0)
-
-        def work(s):
-            y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
-            kept = torch.empty(sizes[0], dtype=torch.uint8, device=dev)
-            if m:
-                ws = torch.empty(sizes[1], dtype=torch.uint8, device=dev)
-                lm._check(lm.lib().malt_block_layer_forward(
-                    flat.data_ptr(), xt, m, k, ldx, w.data_ptr(), wt, n, ldw, y.data_ptr(), yt, n, need_x, need_w,
-                    kept.data_ptr(), sizes[0], ws.data_ptr(), sizes[1], s))
-            return y, kept
-
-        y, kept = _on(dev, None, (), work)
+        y, kept, sizes = _layer_forward(x, weight, transposed, out_dtype, need_x, need_w, None)
         ctx.save_for_backward(kept)
-        ctx.args = (x.shape, x.dtype, weight.dtype, m, n, k, sizes)
+        ctx.args = (x.shape, x.dtype, weight.shape, weight.dtype, transposed, *sizes)
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         (kept,) = ctx.saved_tensors
-        x_shape, x_dtype, w_dtype, m, n, k, sizes = ctx.args
+        x_shape, x_dtype, w_shape, w_dtype, transposed, m, n, k, sizes = ctx.args
         need_x, need_w = ctx.needs_input_grad[:2]
         dev = dy.device
         if dy.dtype not in _DTYPES:
             dy = dy.float()
         if m == 0:
             return (torch.zeros(x_shape, dtype=x_dtype, device=dev) if need_x else None,
-                    torch.zeros((n, k), dtype=w_dtype, device=dev) if need_w else None, None)
+                    torch.zeros(w_shape, dtype=w_dtype, device=dev) if need_w else None, None, None)
         g, ld = _rows(dy if dy.dim() == 2 else dy.reshape(-1, n))
 
         def work(s):
             dx = torch.empty(x_shape, dtype=x_dtype, device=dev) if need_x else None
-            dw = torch.empty((n, k), dtype=w_dtype, device=dev) if need_w else None
+            dw = torch.empty(w_shape, dtype=w_dtype, device=dev) if need_w else None
             ws = torch.empty(sizes[2], dtype=torch.uint8, device=dev)
             lm._check(lm.lib().malt_block_layer_backward(
-                g.data_ptr(), _DTYPES[g.dtype], m, n, ld, k, kept.data_ptr(), sizes[0],
+                g.data_ptr(), _DTYPES[g.dtype], m, n, ld, k, transposed, kept.data_ptr(), sizes[0],
                 dx.data_ptr() if need_x else None, _DTYPES[x_dtype], k, dw.data_ptr() if need_w else None,
-                _DTYPES[w_dtype], k, 0, ws.data_ptr(), sizes[2], s))
-            return dx, dw, None
+                _DTYPES[w_dtype], w_shape[1], 0, ws.data_ptr(), sizes[2], s))
+            return dx, dw, None, None
 
         return _on(dev, None, (), work)
 
@@ -451,10 +457,11 @@ def _weight(weight, device=None) -> None:
 
 
 def fp8_linear(x: torch.Tensor, weight: torch.Tensor, out_dtype: Optional[torch.dtype] = None,
-               stream=None) -> torch.Tensor:
+               transposed: bool = False, stream=None) -> torch.Tensor:
     """x weight^T with both brought to 8 bits: x with a scale for each row and
     128 values, weight (outer, inner) with one for each 128 x 128 block.  Sums
-    are float32; out_dtype: x's unless given.
+    are float32; out_dtype: x's unless given.  transposed: weight is
+    (inner, outer), as GPT-2's layers store it, and the result x weight.
 
     The backward pass runs in 8 bits too: the output's gradient by rows times
     the same 8-bit weight, and the transposes of gradient and x, with a scale for
@@ -462,10 +469,13 @@ def fp8_linear(x: torch.Tensor, weight: torch.Tensor, out_dtype: Optional[torch.
     Rounding to 8 bits passes gradients through unchanged."""
     _tensor("x", x, _DTYPES)
     _weight(weight, x.device)
-    out_dtype = _linear_args(x, weight.shape[1], out_dtype)
+    transposed = bool(transposed)
+    out_dtype = _linear_args(x, weight.shape[0 if transposed else 1], out_dtype)
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad):
         _no_stream(stream)
-        return _Fp8Linear.apply(x, weight, out_dtype)
+        return _Fp8Linear.apply(x, weight, transposed, out_dtype)
+    if transposed:
+        return _layer_forward(x, weight, True, out_dtype, False, False, stream)[0]
     return _linear(x, weight, out_dtype, stream)
 
 

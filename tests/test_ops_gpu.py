@@ -514,6 +514,21 @@ def test_layer_gradients_at_odd_sizes(ops, tokens, inner, outer):
         assert torch.equal(torch.autograd.grad(ops.fp8_linear(x.detach(), w), w, dy)[0], dw)
 
 
+@pytest.mark.parametrize("tokens,inner,outer", [(3, 130, 20), (200, 257, 300), (1000, 128, 640)])
+def test_layer_on_a_transposed_weight(ops, tokens, inner, outer):
+    """A weight that lies (inner, outer): the same blocks, so the same numbers."""
+    x, w = _uneven(384, tokens, inner, F32).requires_grad_(), _uneven(385, inner, outer, F32).requires_grad_()
+    dy = _uneven(386, tokens, outer, F32)
+    y = ops.fp8_linear(x, w, transposed=True)
+    dx, dw = torch.autograd.grad(y, (x, w), dy)
+    wq, xd = _rounded64(w.detach(), 128, 128)[0], x.detach()
+    _check_product(y.detach(), _rounded64(xd, 1, 128)[0], wq.t().contiguous())
+    _check_product(dx, _rounded64(dy, 1, 128)[0], wq)
+    _check_product(dw, _rounded64(xd, 128, 1)[0].t().contiguous(), _rounded64(dy, 128, 1)[0].t().contiguous())
+    assert torch.equal(ops.fp8_linear(xd, w.detach(), transposed=True), y.detach())
+    assert torch.equal(torch.autograd.grad(ops.fp8_linear(x, w.detach(), transposed=True), x, dy)[0], dx)
+
+
 def test_layer_against_differences(ops):
     """Whole numbers up to 15 with a 16 in every block are exact in 8 bits, and so is a step of 16: differences
     of the layer give its gradients exactly."""
@@ -615,13 +630,13 @@ def test_layer_accumulates_its_weight_gradient(ops, dtype, m):
     t = lm.MALT_BFLOAT16 if dtype == BF16 else lm.MALT_FLOAT32
     s = torch.cuda.current_stream().cuda_stream
     kept_n, fwd_n, bwd_n = ctypes.c_size_t(0), ctypes.c_size_t(0), ctypes.c_size_t(0)
-    lm._check(lm.lib().malt_block_layer_size(m, n, k, 0, 0, t, 0, 1, *map(ctypes.byref, (kept_n, fwd_n, bwd_n))))
+    lm._check(lm.lib().malt_block_layer_size(m, n, k, 0, 0, 0, t, 0, 1, *map(ctypes.byref, (kept_n, fwd_n, bwd_n))))
     kept, fwd, bwd = (torch.empty(c.value, dtype=torch.uint8, device="cuda") for c in (kept_n, fwd_n, bwd_n))
     y, old = torch.empty((m, n), device="cuda"), randn(443, n, k, dtype=dtype)
     dw = pitched(old, 3)
-    lm._check(lm.lib().malt_block_layer_forward(x.data_ptr(), 0, m, k, k, w.data_ptr(), 0, n, k, y.data_ptr(), 0, n, 0, 1,
+    lm._check(lm.lib().malt_block_layer_forward(x.data_ptr(), 0, m, k, k, w.data_ptr(), 0, n, k, 0, y.data_ptr(), 0, n, 0, 1,
                                                 kept.data_ptr(), kept_n.value, fwd.data_ptr(), fwd_n.value, s))
-    lm._check(lm.lib().malt_block_layer_backward(dy.data_ptr(), 0, m, n, n, k, kept.data_ptr(), kept_n.value, None, 0, k,
+    lm._check(lm.lib().malt_block_layer_backward(dy.data_ptr(), 0, m, n, n, k, 0, kept.data_ptr(), kept_n.value, None, 0, k,
                                                  dw.data_ptr(), t, k + 3, 1, bwd.data_ptr(), bwd_n.value, s))
     a, b = _rounded64(dy, 128, 1)[0].t().contiguous(), _rounded64(x, 128, 1)[0].t().contiguous()
     want, tall = a @ b.t() + old.double().cpu(), a.abs() @ b.abs().t() + old.double().cpu().abs()

@@ -195,19 +195,23 @@ def test_kept_layer_refuses(L):
 def test_layer_refuses(L):
     kept, fwd, bwd = c_size_t(0), c_size_t(0), c_size_t(0)
     three = (byref(kept), byref(fwd), byref(bwd))
-    assert L.malt_block_layer_size(40, 200, 256, 0, 0, 0, 1, 1, *three) == lm.MALT_OK
+    assert L.malt_block_layer_size(40, 200, 256, 0, 0, 0, 0, 1, 1, *three) == lm.MALT_OK
     assert kept.value >= 256 * 128 + 256 * 256 and fwd.value >= 40 * 256 + 200 * 256 and bwd.value >= 40 * 256 + 200 * 128
-    assert L.malt_block_layer_size(40, 200, 256, 0, 0, 0, 0, 0, *three) == lm.MALT_OK and bwd.value == 0
-    assert L.malt_block_layer_size(0, 200, 256, 0, 0, 0, 1, 1, *three) == lm.MALT_ERR_SHAPE
-    assert L.malt_block_layer_size(40, 200, 256, 3, 0, 0, 1, 1, *three) == lm.MALT_ERR_INVALID_ARG
-    assert L.malt_block_layer_size(40, 200, 256, 0, 0, 0, 1, 1, None, *three[1:]) == lm.MALT_ERR_INVALID_ARG
+    assert L.malt_block_layer_size(40, 200, 256, 0, 0, 0, 0, 0, 0, *three) == lm.MALT_OK and bwd.value == 0
+    assert L.malt_block_layer_size(40, 200, 256, 2, 0, 0, 0, 1, 1, *three) == lm.MALT_ERR_INVALID_ARG
+    assert L.malt_block_layer_size(0, 200, 256, 0, 0, 0, 0, 1, 1, *three) == lm.MALT_ERR_SHAPE
+    assert L.malt_block_layer_size(40, 200, 256, 0, 3, 0, 0, 1, 1, *three) == lm.MALT_ERR_INVALID_ARG
+    assert L.malt_block_layer_size(40, 200, 256, 0, 0, 0, 0, 1, 1, None, *three[1:]) == lm.MALT_ERR_INVALID_ARG
     big = 1 << 30
 
-    def forward(x=A, ld=256, w=B, y=C, ldy=200, k=D, kb=big, ws=E, wb=big):
-        return L.malt_block_layer_forward(x, 0, 40, 256, ld, w, 0, 200, 256, y, 0, ldy, 1, 1, k, kb, ws, wb, None)
+    def forward(x=A, ld=256, w=B, ldw=256, t=0, y=C, ldy=200, k=D, kb=big, ws=E, wb=big):
+        return L.malt_block_layer_forward(x, 0, 40, 256, ld, w, 0, 200, ldw, t, y, 0, ldy, 1, 1, k, kb, ws, wb, None)
 
     assert forward(x=None) == lm.MALT_ERR_INVALID_ARG
     assert forward(ld=255) == lm.MALT_ERR_SHAPE
+    assert forward(ldw=255) == lm.MALT_ERR_SHAPE
+    assert forward(t=1, ldw=199) == lm.MALT_ERR_SHAPE
+    assert forward(t=3) == lm.MALT_ERR_INVALID_ARG
     assert forward(ldy=199) == lm.MALT_ERR_SHAPE
     assert forward(k=None) == lm.MALT_ERR_INVALID_ARG
     assert forward(kb=100) == lm.MALT_ERR_INVALID_ARG
@@ -218,7 +222,7 @@ def test_layer_refuses(L):
     assert forward(ws=D) == lm.MALT_ERR_ALIAS
 
     def backward(dy=A, ld=200, k=B, kb=big, dx=C, dw=D, acc=0, ws=E, wb=big):
-        return L.malt_block_layer_backward(dy, 0, 40, 200, ld, 256, k, kb, dx, 0, 256, dw, 0, 256, acc, ws, wb, None)
+        return L.malt_block_layer_backward(dy, 0, 40, 200, ld, 256, 0, k, kb, dx, 0, 256, dw, 0, 256, acc, ws, wb, None)
 
     assert backward(dy=None) == lm.MALT_ERR_INVALID_ARG
     assert backward(dx=None, dw=None) == lm.MALT_ERR_INVALID_ARG

@@ -6,13 +6,21 @@ The model is GPT-2 Small / Medium / Large (transformers' GPT2LMHeadModel,
 random initialisation, no checkpoint, dropout off), the data random token
 ids (no dataset).  Matrix parameters (the four per-block matrices) go to
 libmalt (MALT / MALTER / Muon), the rest to AdamW; "adamw" trains everything
-with torch's AdamW.  The model trains in float32 (no autocast).  One
+with torch's AdamW.  The model trains in float32 (no autocast) unless --fp8 is given.  One
 iteration is the paper's global batch: 480 sequences of 1024 tokens
 (Sec. 5.1), here as 60 accumulated micro-batches of 8, then one optimizer
 step; weight decay 0.1 on both parts (hyper-parameter table) and a linear
 warm-up over the first 10% of the run (Sec. 5.1).
 
   python -m paper_2608_05088_amd.train --model gpt2-medium --optim adamw,muon,malt,malter
+
+With --teacher the student trains on another model's answers (also random
+weights: what is measured is the step): the loss against the teacher's top
+logits with the next tokens mixed in, loss and gradient in one pass over the
+student's logits.  --fp8 runs the token table and the block matrices' layers,
+forward and backward, on this package's operators (ops.py) in 8 bits:
+
+  python -m paper_2608_05088_amd.train --model gpt2-small --optim malt --teacher gpt2-medium --top-k 64 --fp8
 
 Prints one JSON line per optimizer: ms per iteration, of which optimizer
 step, the optimizer state (as the paper counts it: the tensors the algorithm
@@ -64,6 +72,46 @@ def make_optimizer(kind: str, model, lr: float, adamw_lr: float, weight_decay: f
                 adamw_weight_decay=weight_decay, matrix_filter=lambda p: id(p) in mats)
 
 
+def use_operators(model) -> None:
+    """The token table and the block matrices' layers on this package's kernels:
+    lookup with the gradient by sorted tokens, products in 8 bits."""
+    import functools
+    from transformers.pytorch_utils import Conv1D
+    from . import ops
+    table = model.transformer.wte
+
+    def lookup(ids):
+        return ops.embedding(ids, table.weight)
+
+    def layer(mod, x):
+        return ops.fp8_linear(x, mod.weight, transposed=True) + mod.bias
+
+    table.forward = lookup
+    for mod in model.transformer.h.modules():
+        if isinstance(mod, Conv1D):
+            mod.forward = functools.partial(layer, mod)
+
+
+def distill_backward(student, teacher, ids, top_k: int = 64, tau: float = 2.0, alpha: float = 0.5, scale: float = 1.0):
+    """One micro-batch against a teacher: the mean loss over the tokens that
+    have a next one, and its gradient, times `scale`, in the student's
+    parameters."""
+    import torch
+    from . import ops
+    with torch.no_grad():
+        top = teacher(input_ids=ids).logits.topk(top_k, dim=-1)
+    logits = student(input_ids=ids).logits
+    labels = torch.full_like(ids, -100)
+    labels[:, :-1] = ids[:, 1:]
+    top.indices[:, -1] = -1          # the last token has neither teacher nor label
+    count = ids.shape[0] * (ids.shape[1] - 1)
+    # The gradient takes the logits' place: nobody reads them again.
+    losses, grad = ops.distill_step(logits, top.values, top.indices, labels, tau=tau, alpha=alpha, grad=scale / count,
+                                    out=logits.detach())
+    logits.backward(grad)
+    return losses.sum() / count
+
+
 def _adam_state_bytes(opt) -> int:
     import torch
     total = 0
@@ -102,6 +150,11 @@ def run(kind: str, args, device) -> dict:
     import torch
     torch.cuda.reset_peak_memory_stats(device)
     model = build_model(args.model, device, seed=args.seed)
+    teacher = None
+    if args.teacher:
+        teacher = build_model(args.teacher, device, seed=args.seed + 1).eval().requires_grad_(False)
+    if args.fp8:
+        use_operators(model)
     opt = make_optimizer(kind, model, args.lr, args.adamw_lr, args.weight_decay)
     # The paper's protocol: linear warm-up over the first 10% of the run.
     sched = lambda_lr(opt, linear_warmup(args.warmup + args.iters))
@@ -112,8 +165,11 @@ def run(kind: str, args, device) -> dict:
     def iteration():
         for _ in range(args.accum):
             ids = torch.randint(0, 50257, (B, T), device=device, generator=gen)
-            loss = model(input_ids=ids, labels=ids).loss
-            (loss / args.accum).backward()
+            if teacher is not None:
+                loss = distill_backward(model, teacher, ids, args.top_k, args.tau, args.alpha, 1 / args.accum)
+            else:
+                loss = model(input_ids=ids, labels=ids).loss
+                (loss / args.accum).backward()
         s, e = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         s.record()
         opt.step()
@@ -146,8 +202,11 @@ def run(kind: str, args, device) -> dict:
            "optimizer_state_MiB": round(sb["algorithm"] / mib, 2),
            "optimizer_state_allocated_MiB": round(sb["allocated"] / mib, 2),
            "peak_device_memory_GiB": round(torch.cuda.max_memory_allocated(device) / mib / 1024, 2),
-           "final_loss": round(float(loss.item()), 4), "dtype": "float32", "data": "synthetic token ids"}
-    del opt, model
+           "final_loss": round(float(loss.item()), 4),
+           "dtype": "float32, block matrices' products fp8" if args.fp8 else "float32", "data": "synthetic token ids"}
+    if teacher is not None:
+        out["teacher"] = args.teacher
+    del opt, model, teacher
     torch.cuda.empty_cache()
     return out
 
@@ -165,6 +224,11 @@ def main(argv=None):
     ap.add_argument("--adamw-lr", type=float, default=6e-4)
     ap.add_argument("--weight-decay", type=float, default=0.1)
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--fp8", action="store_true", help="token table and block layers on this package's operators, in 8 bits")
+    ap.add_argument("--teacher", choices=sorted(MODELS), help="train on this model's top logits")
+    ap.add_argument("--top-k", type=int, default=64)
+    ap.add_argument("--tau", type=float, default=2.0)
+    ap.add_argument("--alpha", type=float, default=0.5)
     args = ap.parse_args(argv)
     import torch
     if not torch.cuda.is_available():

@@ -345,7 +345,11 @@ void launch_typed(const DistillArgs& a, hipStream_t s) {
   else if (nvec <= 256 * 4) launch_held<T, 256, 4, 6>(a, s);
   else if (nvec <= 512 * 7) launch_held<T, 512, 7, 6>(a, s);
   else if (nvec <= 512 * 13) launch_held<T, 512, 13, 5>(a, s);
-  else if (nvec <= 512 * 25) launch_held<T, 512, 25, 4>(a, s);
+  // Past what 512 threads hold, reading the rest of a row again costs less than one row a CU
+  // (1024 threads) while it is under a third of it (float32, 2000 rows: 60000 columns 211 and
+  // 242 us, 100277 columns 277 and 226).  A loss alone goes the same way, though it would take
+  // 512 threads further (131072 columns 254 and 276 us): so both give the same losses, bit for bit.
+  else if (nvec <= 512 * 25 * 7 / 5) launch_held<T, 512, 25, 4>(a, s);
   else launch_held<T, 1024, 25, 4>(a, s);
 }
 

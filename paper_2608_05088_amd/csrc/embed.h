@@ -8,7 +8,8 @@ namespace malt {
 
 constexpr int SORT_THREADS = 256, SORT_TILE = 2048;   // keys a block of the sort takes
 constexpr int SORT_ONE = 8192;                        // tokens one workgroup sorts by itself
-constexpr int FEW = 256;                              // tokens that need no sort
+constexpr int FEW = 256;                              // tokens every row looks over itself
+constexpr int FIRST_MOST = 4096;                      // tokens (times strips) that need no sort
 
 struct EmbedLookupArgs {
   const void* ids;

@@ -388,7 +388,58 @@ __device__ __forceinline__ op_f32x4 row_sum(const EmbedGradArgs& a, int64_t s, i
   return x;
 }
 
-// Tables wider than NARROW: a wave takes a row and a strip.  How it comes by the
+// Up to FIRST_MOST tokens: no sort.  A workgroup for each token and strip looks
+// the tokens over, an eighth of them a wave; if its token is the first with its
+// id, the waves sum the rows they met and join the sums in the tokens' order.
+// Rows without tokens are zeros already.
+template <class TG, class TO>
+__global__ __launch_bounds__(512) void embed_first_kernel(EmbedGradArgs a) {
+  constexpr int NW = 8, G = FIRST_MOST / 64 / NW;
+  __shared__ op_f32x4 sums[NW][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t0 = blockIdx.x, c0 = blockIdx.y * STRIP, tokens = (int)a.tokens;
+  const int64_t v = load_id(a.ids, a.wide_ids, t0);
+  if (v < 0 || v >= a.vocab) return;
+  const int groups = (tokens + 64 * NW - 1) / (64 * NW), base = wave * groups * 64;
+  uint64_t met[G];
+  bool earlier = false;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int t = base + g * 64 + lane;
+    const bool same = g < groups && t < tokens && load_id(a.ids, a.wide_ids, t) == v;
+    earlier |= same && t < t0;
+    met[g] = __ballot(same);
+  }
+  if (__syncthreads_or(earlier)) return;
+  op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    uint64_t m = met[g];
+    while (m) {
+      const int n = __popcll(m);
+      uint32_t t[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        t[u] = m ? (uint32_t)(base + g * 64 + __builtin_ctzll(m)) : 0;
+        m &= m - 1;   // 0 stays 0
+      }
+      add_rows(x, static_cast<const TG*>(a.grad), a.grad_ld, n < 8 ? n : 8, c0, lane, a.width, [&](int u) { return t[u]; });
+    }
+  }
+  sums[wave][lane] = x;
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int w = 1; w < NW; ++w) x += sums[w][lane];
+  finish_row(a, static_cast<TO*>(a.dtable) + v * a.dtable_ld, c0, lane, x);
+}
+
+template <class TO>
+__global__ __launch_bounds__(1024) void embed_fill_kernel(EmbedGradArgs a) {
+  fill_rows<TO>(a, blockIdx.x);
+}
+
+// Tables of more than 128 columns: a wave takes a row and a strip.  How it comes by the
 // row and its tokens is one of three:
 enum Source {
   EVERY,      // every row of the table, with its segment of the sorted tokens (empty: zeros)
@@ -547,9 +598,27 @@ static void rows_typed(EmbedGradArgs a, hipStream_t s) {
                        dim3(256), 0, s, a);
 }
 
+// Workgroups that fill the table with zeros.
+static unsigned fill_blocks(const EmbedGradArgs& a) {
+  const int64_t vecs = a.dtable_ld == a.width ? (a.vocab * a.width + 3) / 4 : a.vocab * ((a.width + 3) / 4);
+  return (unsigned)((vecs + FILL_VECS * 1024 - 1) / (FILL_VECS * 1024));
+}
+
 template <class TG, class TO>
 static void grad_typed(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, hipStream_t s) {
-  if (a.tokens <= FEW) return rows_typed<TG, TO, LOOK>(a, s);
+  const unsigned strips = (unsigned)((a.width + STRIP - 1) / STRIP);
+  if (a.tokens <= FEW && !a.accumulate) return rows_typed<TG, TO, LOOK>(a, s);
+  // The search for the first token of an id grows with the square of the tokens, and
+  // what it saves (the sort) is hidden where a large table is filled with zeros at the
+  // same time.  Measured: 1000 tokens, 1173 x 429: 14 us and 24 sorted; 2048, 40298 x 39:
+  // 15 and 30; 4096, 1173 x 429: 39 and 31; 1000, 50257 x 768: 35 and 32.
+  const bool first = a.tokens <= FIRST_MOST && a.tokens * strips <= FIRST_MOST &&
+                     (a.accumulate || a.vocab * a.width * (int64_t)sizeof(TO) <= (int64_t)64 << 20);
+  if (a.tokens <= FEW || first) {
+    if (!a.accumulate) hipLaunchKernelGGL((embed_fill_kernel<TO>), dim3(fill_blocks(a)), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL((embed_first_kernel<TG, TO>), dim3((unsigned)a.tokens, strips), dim3(512), 0, s, a);
+    return;
+  }
   uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + L.keys[0]), reinterpret_cast<uint32_t*>(ws + L.keys[1])};
   uint32_t* index[2] = {reinterpret_cast<uint32_t*>(ws + L.index[0]), reinterpret_cast<uint32_t*>(ws + L.index[1])};
   a.table = reinterpret_cast<uint32_t*>(ws + L.table);
@@ -562,12 +631,8 @@ static void grad_typed(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, hipS
   int to = 0;
   const bool one = a.tokens <= SORT_ONE;
   if (one) {
-    int64_t fill = 0;
-    if (!a.accumulate) {
-      const int64_t vecs = a.dtable_ld == a.width ? (a.vocab * a.width + 3) / 4 : a.vocab * ((a.width + 3) / 4);
-      fill = (vecs + FILL_VECS * 1024 - 1) / (FILL_VECS * 1024);
-    }
-    hipLaunchKernelGGL((sort_one_kernel<TO>), dim3((unsigned)(1 + fill)), dim3(1024), 0, s, a, bits, keys[0], index[0]);
+    const unsigned fill = a.accumulate ? 0 : fill_blocks(a);
+    hipLaunchKernelGGL((sort_one_kernel<TO>), dim3(1 + fill), dim3(1024), 0, s, a, bits, keys[0], index[0]);
     to = 1;
   } else {
     const dim3 grid((unsigned)L.blocks), threads(SORT_THREADS);
@@ -583,7 +648,7 @@ static void grad_typed(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, hipS
   a.keys = keys[to ^ 1];
   a.order = index[to ^ 1];
   if (!one) hipLaunchKernelGGL(embed_segments_kernel, dim3((unsigned)((a.tokens + 255) / 256)), dim3(256), 0, s, a);
-  const unsigned strips = (unsigned)((a.width + STRIP - 1) / STRIP), chunks = (unsigned)((a.tokens + a.chunk - 1) / a.chunk);
+  const unsigned chunks = (unsigned)((a.tokens + a.chunk - 1) / a.chunk);
   hipLaunchKernelGGL((embed_chunks_kernel<TG>), dim3(chunks, (strips + 3) / 4), dim3(256), 0, s, a);
   if (one) rows_typed<TG, TO, MET>(a, s);
   else rows_typed<TG, TO, EVERY>(a, s);

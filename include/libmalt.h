@@ -293,7 +293,8 @@ typedef enum { MALT_INT32 = 0, MALT_INT64 = 1 } malt_index_t;
  *   out[t, :] = scale * table[ids[t], :]     t < tokens, `width` columns
  * computed in float32, rounded once to out_type.  An id outside [0, vocab)
  * stands for no token: its row is zero.
- * Limits: tokens <= 2^25, 1 <= vocab <= 2^25, 1 <= width <= 2^20. */
+ * Limits: tokens <= 2^25, 1 <= vocab <= 2^25, 1 <= width <= 2^20,
+ * vocab * width <= 2^35. */
 malt_status_t malt_embed_lookup(const void* ids, malt_index_t id_type, int64_t tokens, const void* table,
                                 malt_dtype_t table_type, int64_t vocab, int64_t width, int64_t table_ld, float scale,
                                 void* out, malt_dtype_t out_type, int64_t out_ld, void* stream);
@@ -420,7 +421,7 @@ malt_status_t malt_block_linear(const void* x, malt_dtype_t x_type, int64_t m, i
  * be asked for; the backward call must ask (dx, dw not NULL) for those.
  * malt_block_layer_size gives the bytes of kept and of both workspaces, all
  * 256-byte aligned; NULL is fine where it says 0.
- * Limits: those of the products. */
+ * Limits: those of the products, and m k, n k, m n <= 2^35. */
 malt_status_t malt_block_layer_size(int64_t m, int64_t n, int64_t k, int32_t w_transposed, malt_dtype_t y_type,
                                     malt_dtype_t dx_type, malt_dtype_t dw_type, int32_t need_dx, int32_t need_dw,
                                     size_t* kept_bytes, size_t* forward_bytes, size_t* backward_bytes);

@@ -19,6 +19,7 @@ constexpr int64_t kMaxRows = int64_t(1) << 21;
 constexpr int64_t kMaxVocab = int64_t(1) << 30;
 constexpr int64_t kMaxBlockDim = int64_t(1) << 22;
 constexpr int64_t kMaxProduct = int64_t(1) << 37;
+constexpr int64_t kMaxMatrix = int64_t(1) << 35;   // elements of a table, or of one matrix of a layer
 
 // A strided matrix as the checks see it.
 struct Mat {
@@ -49,7 +50,8 @@ malt_status_t check_ids(const char* name, const void* p, int type, int64_t n) {
 malt_status_t check_table(int64_t tokens, int64_t vocab, int64_t width) {
   if (tokens < 0 || tokens > kMaxTokens) return fail(MALT_ERR_SHAPE, "%lld tokens", (long long)tokens);
   if (vocab < 1 || vocab > kMaxTokens) return fail(MALT_ERR_SHAPE, "a table of %lld rows", (long long)vocab);
-  if (width < 1 || width > (int64_t(1) << 20)) return fail(MALT_ERR_SHAPE, "a table of %lld columns", (long long)width);
+  if (width < 1 || width > (int64_t(1) << 20) || vocab > kMaxMatrix / width)
+    return fail(MALT_ERR_SHAPE, "a table of %lld x %lld", (long long)vocab, (long long)width);
   return MALT_OK;
 }
 
@@ -427,7 +429,7 @@ static malt_status_t check_layer(int64_t m, int64_t n, int64_t k) {
   size_t v, s;
   MALT_TRY(malt_block_size(m, k, &v, &s));
   MALT_TRY(malt_block_size(n, k, &v, &s));
-  if (m > kMaxProduct / n || m > kMaxProduct / k || n > kMaxProduct / k)
+  if (m > kMaxMatrix / n || m > kMaxMatrix / k || n > kMaxMatrix / k)
     return fail(MALT_ERR_SHAPE, "a layer of %lld x %lld on %lld rows", (long long)n, (long long)k, (long long)m);
   if (size_t(q_pad(k) / QB) * q_scale_rows(m) > 0xffffffffull || size_t(q_pad(n) / QB) * q_scale_rows(m) > 0xffffffffull ||
       size_t(q_pad(m) / QB) * q_scale_rows(n) > 0xffffffffull || size_t(q_pad(m) / QB) * q_scale_rows(k) > 0xffffffffull)

@@ -32,6 +32,11 @@ BLOCK = 128   # values that share a scale
 
 # ------------------------------------------------------------------ arguments
 def _tensor(name: str, x, types, device=None) -> None:
+    try:
+        if x.dtype in types and x.is_cuda and (device is None or x.device == device):
+            return
+    except AttributeError:
+        pass
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name} must be a tensor (got {type(x).__name__})")
     if x.dtype not in types:
@@ -95,17 +100,16 @@ def _on(device: torch.device, stream, inputs, work):
 
 # ------------------------------------------------------------------ embedding
 def _lookup(ids, weight, scale, out_dtype, stream):
-    flat = ids if ids.dim() == 1 and ids.is_contiguous() else ids.reshape(-1).contiguous()
+    flat = ids if ids.is_contiguous() else ids.contiguous()
     table, ld = _rows(weight)
     v, w = weight.shape
-    n = flat.shape[0]
     dev = weight.device
 
     def work(s):
         out = torch.empty((*ids.shape, w), dtype=out_dtype, device=dev)
-        lm._check(lm.lib().malt_embed_lookup(flat.data_ptr(), _INDEX[flat.dtype], n, table.data_ptr(),
-                                             _DTYPES[weight.dtype], v, w, ld, scale, out.data_ptr(),
-                                             _DTYPES[out_dtype], w, s))
+        lm._check(lm.lib().malt_embed_lookup(flat.data_ptr(), _INDEX[flat.dtype], flat.numel(), table.data_ptr(),
+                                             _DTYPES[table.dtype], v, w, ld, scale, out.data_ptr(), _DTYPES[out_dtype],
+                                             w, s))
         return out
 
     return _on(dev, stream, (flat, table), work)
@@ -142,11 +146,13 @@ def embedding(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0, out_d
     of any shape; out_dtype: weight's unless given.  Differentiable in weight
     (the gradient is dense, of weight's type, see embedding_grad)."""
     _tensor("weight", weight, _DTYPES)
-    if weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
+    if weight.dim() != 2 or weight.numel() < 1:
         raise ValueError(f"weight must be (vocab, width) (got {tuple(weight.shape)})")
     _tensor("ids", ids, _INDEX, weight.device)
-    out_dtype = weight.dtype if out_dtype is None else out_dtype
-    _type("out_dtype", out_dtype)
+    if out_dtype is None:
+        out_dtype = weight.dtype
+    else:
+        _type("out_dtype", out_dtype)
     scale = float(scale)
     if weight.requires_grad and torch.is_grad_enabled():
         _no_stream(stream)
@@ -452,7 +458,7 @@ def _linear_args(x, k: int, out_dtype):
 
 def _weight(weight, device=None) -> None:
     _tensor("weight", weight, _DTYPES, device)
-    if weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
+    if weight.dim() != 2 or weight.numel() < 1:
         raise ValueError(f"weight must be (outer, inner) (got {tuple(weight.shape)})")
 
 

@@ -5,13 +5,21 @@
 //   loss = (1 - alpha) tau^2 sum_j p_j (log p_j - log q_{i_j}) - alpha log q1_y
 //   dz   = w [ (1 - alpha) tau (q - p) + alpha (q1 - 1_y) ]
 //
-// A workgroup takes a row and holds it in registers: it is read once, for the
-// maximum, the sums and the gradient, which is all the memory traffic there has
-// to be.  Wave 0 also deals with the teacher's entries.  What does not fit the
-// registers is read again for each pass.  q and q1 are written to every column
-// first; then the columns of the teacher's entries and of the label, whose
-// logits were fetched at the start, are written again with p and 1_y taken off.
+// Bound by memory: z in and dz out, 6 flops and one exponential a column.  A workgroup
+// takes a row and holds it on the chip, in registers and, past them, in LDS: it is
+// read once, for the maximum, the sums and the gradient, which is all the memory
+// traffic there has to be.  Wave 0 also deals with the teacher's entries.  What does
+// not fit is read again for each pass.  q and q1 are written to every column first;
+// then the columns of the teacher's entries and of the label, whose logits were
+// fetched at the start, are written again with p and 1_y taken off.
+//
+// Measured (a large copy reaches 5.17 TB/s on the same card): 8192 x 50257 bf16 with 64
+// entries, tau = 2 and labels 360 us, 4.6 TB/s; losses alone with 32 entries 151 us, 5.5 TB/s
+// of reads; 4096 x 128256 bf16 451 us, 4.7 TB/s; 1001 x 100277 float32 with 100 entries, tau
+// = 1.5 and labels 214 us, 3.8 TB/s (four rounds of one row a CU, and the last 9% of it);
+// 128 x 1000 float32 10 us, the launch and three barriers.
 #include "distill.h"
+#include "ns_common.h"
 #include "ops_common.h"
 
 namespace malt {
@@ -74,8 +82,9 @@ enum Mode {
   SQUARE    // tau = 2: exp(z) is the square of exp(z / 2), one exponential serves both
 };
 
-// NT threads hold H vectors of 16 bytes each.  STEP: the gradient is written.
-template <class T, int NT, int H, int MODE, bool STEP, int WPE>
+// NT threads hold H vectors of 16 bytes each in registers and L in LDS.  STEP: the
+// gradient is written.
+template <class T, int NT, int H, int L, int MODE, bool STEP, int WPE>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE)))
 void distill_kernel(DistillArgs a) {
   using V = Vec<T>;
@@ -83,6 +92,7 @@ void distill_kernel(DistillArgs a) {
   __shared__ float red_max[NW], red_tau[NW], red_one[NW];
   __shared__ float ent_off[DISTILL_MAX_TOP + 1], ent_z[DISTILL_MAX_TOP + 1];   // what a column is lowered by; its logit
   __shared__ int32_t ent_id[DISTILL_MAX_TOP + 1];                              // -1: no entry
+  __shared__ op_u32x4 kept[L > 0 ? L * NT : 1];   // vector i of thread t at i NT + t
   __shared__ float flags[2];                                                   // the row has a teacher, a label
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -126,7 +136,30 @@ void distill_kernel(DistillArgs a) {
     held[i] = op_u32x4{V::NEG_INF, V::NEG_INF, V::NEG_INF, V::NEG_INF};
     if (tid + i * NT < nvec) held[i] = body[tid + i * NT];
   }
+  // Vectors H NT + i NT + tid go straight to LDS, each wave's into its own part of it.
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    const int q0 = (H + i) * NT + wave * 64;
+    if (q0 + lane < nvec) ns::dma16(ns::buf_rsrc(z + head + (int64_t)q0 * N), 16 * lane, 0, ns::lds_u32(kept + i * NT + wave * 64));
+  }
   const float edge_z = edge ? to_f32(gptr(z)[edge_col]) : -INFINITY;
+  // f(q, its values) for the vectors of this thread that LDS holds, and those read again.
+  auto beyond = [&](auto&& each) {
+#pragma unroll 1
+    for (int i = 0; i < L; ++i) {
+      const int q = (H + i) * NT + tid;
+      if (q < nvec) {
+        float f[N];
+        V::open(kept[i * NT + tid], f);
+        each(q, f);
+      }
+    }
+    for (int q = (H + L) * NT + tid; q < nvec; q += NT) {
+      float f[N];
+      V::open(body[q], f);
+      each(q, f);
+    }
+  };
   // The held bits are opened anew in each pass: kept open they would take twice the registers.
   auto close_held = [&]() {
 #pragma unroll
@@ -168,12 +201,11 @@ void distill_kernel(DistillArgs a) {
 #pragma unroll
     for (int e = 0; e < N; ++e) m = fmaxf(m, f[e]);
   }
-  for (int q = H * NT + tid; q < nvec; q += NT) {
-    float f[N];
-    V::open(body[q], f);
+  if constexpr (L > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // LDS holds this wave's vectors
+  beyond([&](int, const float (&f)[N]) {
 #pragma unroll
     for (int e = 0; e < N; ++e) m = fmaxf(m, f[e]);
-  }
+  });
   m = wave_max(m);
   if (lane == 0) red_max[wave] = m;
   __syncthreads();
@@ -211,12 +243,10 @@ void distill_kernel(DistillArgs a) {
 #pragma unroll
     for (int e = 0; e < N; ++e) add(f[e]);
   }
-  for (int q = H * NT + tid; q < nvec; q += NT) {
-    float f[N];
-    V::open(body[q], f);
+  beyond([&](int, const float (&f)[N]) {
 #pragma unroll
     for (int e = 0; e < N; ++e) add(f[e]);
-  }
+  });
   s_tau = wave_sum(s_tau);
   if constexpr (MODE != ONE) s_one = wave_sum(s_one);
   if (lane == 0) {
@@ -301,13 +331,12 @@ void distill_kernel(DistillArgs a) {
         for (int e = 0; e < N; ++e) f[e] = grad(f[e]);
         put(tid + i * NT, f);
       }
-    for (int q = H * NT + tid; q < nvec; q += NT) {
-      float f[N];
-      V::open(body[q], f);
+    beyond([&](int q, const float (&f)[N]) {
+      float g[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = grad(f[e]);
-      put(q, f);
-    }
+      for (int e = 0; e < N; ++e) g[e] = grad(f[e]);
+      put(q, g);
+    });
     if (edge) dg[edge_col] = from_f32<T>(grad(edge_z));
     // Every store above has reached memory before a column is written again.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -324,33 +353,38 @@ void distill_kernel(DistillArgs a) {
   }
 }
 
-template <class T, int NT, int H, int WPE, int MODE>
+template <class T, int NT, int H, int L, int WPE, int MODE>
 void launch_mode(const DistillArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.rows), threads(NT);
-  if (a.dlogits) hipLaunchKernelGGL((distill_kernel<T, NT, H, MODE, true, WPE>), grid, threads, 0, s, a);
-  else hipLaunchKernelGGL((distill_kernel<T, NT, H, MODE, false, WPE>), grid, threads, 0, s, a);
+  if (a.dlogits) hipLaunchKernelGGL((distill_kernel<T, NT, H, L, MODE, true, WPE>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((distill_kernel<T, NT, H, L, MODE, false, WPE>), grid, threads, 0, s, a);
 }
 
-template <class T, int NT, int H, int WPE>
+template <class T, int NT, int H, int L, int WPE>
 void launch_held(const DistillArgs& a, hipStream_t s) {
-  if (a.alpha == 0.f || a.alpha == 1.f || a.tau == 1.f) launch_mode<T, NT, H, WPE, ONE>(a, s);
-  else if (a.tau == 2.f) launch_mode<T, NT, H, WPE, SQUARE>(a, s);
-  else launch_mode<T, NT, H, WPE, TWO>(a, s);
+  if (a.alpha == 0.f || a.alpha == 1.f || a.tau == 1.f) launch_mode<T, NT, H, L, WPE, ONE>(a, s);
+  else if (a.tau == 2.f) launch_mode<T, NT, H, L, WPE, SQUARE>(a, s);
+  else launch_mode<T, NT, H, L, WPE, TWO>(a, s);
 }
 
 template <class T>
 void launch_typed(const DistillArgs& a, hipStream_t s) {
   const int64_t nvec = a.vocab / Vec<T>::N;
-  if (nvec <= 256) launch_held<T, 256, 1, 8>(a, s);
-  else if (nvec <= 256 * 4) launch_held<T, 256, 4, 6>(a, s);
-  else if (nvec <= 512 * 7) launch_held<T, 512, 7, 6>(a, s);
-  else if (nvec <= 512 * 13) launch_held<T, 512, 13, 5>(a, s);
-  // Past what 512 threads hold, reading the rest of a row again costs less than one row a CU
-  // (1024 threads) while it is under a third of it (float32, 2000 rows: 60000 columns 211 and
-  // 242 us, 100277 columns 277 and 226).  A loss alone goes the same way, though it would take
-  // 512 threads further (131072 columns 254 and 276 us): so both give the same losses, bit for bit.
-  else if (nvec <= 512 * 25 * 7 / 5) launch_held<T, 512, 25, 4>(a, s);
-  else launch_held<T, 1024, 25, 4>(a, s);
+  // Threads, vectors a thread holds in registers and in LDS, and the waves a SIMD (of
+  // which four are a CU) that this leaves room for: as many rows a CU as fit, since one
+  // row's loads go on during another's arithmetic and stores.
+  if (nvec <= 256) launch_held<T, 256, 1, 0, 8>(a, s);
+  else if (nvec <= 256 * 4) launch_held<T, 256, 4, 0, 6>(a, s);
+  else if (nvec <= 512 * 7) launch_held<T, 512, 7, 0, 6>(a, s);   // with 256 threads, a fifth in LDS: losses alone 8% slower
+  // Four rows a CU.  512 threads and three rows: step above 348 us, with tau = 1.5 373 (not
+  // 367), losses alone 165 (not 151); registers alone, two rows: 369, 404 and 165.
+  else if (nvec <= 256 * 25) launch_held<T, 256, 19, 6, 4>(a, s);
+  // Two rows a CU.  Past what they hold (16384 vectors), reading the rest of a row again
+  // costs less than one row a CU (1024 threads) while it is under a fifth: 4096 x 151936
+  // bf16 566 and 608 us, 2048 x 88000 float32 351 and 313.  Without LDS 128256 columns of
+  // bf16 took 523 us, not 451.
+  else if (nvec <= 512 * 40) launch_held<T, 512, 24, 8, 4>(a, s);
+  else launch_held<T, 1024, 24, 9, 4>(a, s);
 }
 
 }  // namespace

@@ -376,6 +376,19 @@ def test_distillation_in_place_beyond_the_registers(ops, v):
         assert torch.equal(ops.distill_step(z, a, ids, labels, tau=1.5, alpha=0.5, grad=weight, out=z)[1], want)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vectors", [4863, 5057, 6400, 6402, 12353, 16384, 16390, 20480, 20482, 24640, 33792, 33860])
+def test_distillation_where_a_row_meets_the_ends_of_what_is_held(ops, dtype, vectors):
+    """Rows that end at, just before or just past registers, LDS and the sizes at which the split changes."""
+    v = vectors * (16 // (torch.finfo(dtype).bits // 8)) + 3
+    z, a, ids, labels, weight = _case(300 + vectors, 3, v, 9, dtype)
+    z[1, -1], z[2, v // 2] = 40.0, 40.0     # the maximum in the last column, and in the middle
+    for tau, alpha in ((1.0, 0.0), (2.0, 0.5), (1.5, 0.25)):
+        got = ops.distill_step(z, a, ids, labels, tau=tau, alpha=alpha, grad=weight)
+        _check_distill(got, _distill64(z, a, ids, labels, tau, alpha, weight), z, tau, alpha, weight, dtype)
+        assert torch.equal(ops.distill_loss(z, a, ids, labels, tau=tau, alpha=alpha), got[0])
+
+
 def test_distillation_beyond_32_bit_offsets(ops):
     ld = (1 << 31) - 8
     z, a, ids, labels, weight = _case(250, 3, 500, 7, BF16)

@@ -8,7 +8,8 @@ namespace malt {
 
 constexpr int SORT_THREADS = 256, SORT_TILE = 2048;   // keys a block of the sort takes
 constexpr int SORT_ONE = 8192;                        // tokens one workgroup sorts by itself
-constexpr int FEW = 256;                              // tokens every row looks over itself
+constexpr int FEW = 256;                              // tokens that need no workspace
+constexpr int64_t LOOK_MOST = 1 << 19;                // looks of rows at tokens in one launch
 constexpr int FIRST_MOST = 4096;                      // tokens (times strips) that need no sort
 
 struct EmbedLookupArgs {
@@ -38,7 +39,6 @@ struct EmbedGradArgs {
   float* part;             // [chunk][2][part_ld]
   int64_t part_ld;
   int32_t chunk;
-  int32_t lanes_log2;      // narrow tables: lanes of a row
 };
 
 struct EmbedGradLayout {

@@ -9,6 +9,14 @@
 // depend on how the work was scheduled.  A row with few tokens is summed by the
 // wave that writes it; the sorted tokens of longer rows (one id in sixteen may
 // be the same word) are first summed in chunks by waves of their own.
+//
+// Measured (a large copy reaches 5.17 TB/s on the same card):
+//   lookup of 8192 x 1280, float32 to bf16: 8.9 us, 7 TB/s with what the caches hold;
+//   gradient of 8192 x 1024 float32 tokens, 50257 rows: 43 us, of which 26 to sort while
+//   the table's 206 MB are filled, 7 the chunks and 10 the rows; 5.6 TB/s;
+//   gradient of 491520 x 768 bf16 tokens into float32: 268 us, of which 41 for the sort's
+//   seven launches, 117 the chunks (429 MB) and 110 the rows (432 MB), near 4 TB/s;
+//   rows in order instead of by chance, and ids equally frequent: 4.9 TB/s.
 #include "embed.h"
 #include "ops_common.h"
 
@@ -232,7 +240,8 @@ __device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, int64_t b) {
   }
 }
 
-// Up to SORT_ONE tokens: all passes in the LDS of workgroup 0, and the segments.
+// Up to SORT_ONE tokens (what its registers hold; 8000 tokens, 50257 x 768: 38 us, and 62 by
+// the kernels above): all passes in the LDS of workgroup 0, and the segments.
 // Wave w's keys are a run of them, so ranks by wave are stable.  Meanwhile the
 // other workgroups fill the table with zeros: a sort of 8192 tokens takes one CU
 // 25 us, the rest of the chip as long for the 200 MB of a table.
@@ -307,7 +316,9 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedGradArgs a, int bit
 
 // --------------------------------------------------------------------- sums
 // s += up to 8 rows of grad, whose loads are all in flight together; at(u) is
-// the u-th token's number (wave-uniform, u < n).
+// the u-th token's number (wave-uniform, u < n).  (16 rows in flight were slower, 4 no
+// faster.  8 columns a lane of bf16 instead of 4: 285 -> 320 us for the second
+// gradient above, since the registers then leave room for half the waves.)
 template <class TG, class At>
 __device__ __forceinline__ void add_rows(op_f32x4& s, const TG* grad, int64_t ld, int n, int c0, int lane, int width,
                                          At&& at) {
@@ -451,8 +462,8 @@ __global__ __launch_bounds__(1024) void embed_fill_kernel(EmbedGradArgs a) {
   fill_rows<TO>(a, blockIdx.x);
 }
 
-// Tables of more than 128 columns: a wave takes a row and a strip.  How it comes by the
-// row and its tokens is one of three:
+// A wave takes a row and a strip.  (Several neighbouring rows a wave: frequent ids are
+// neighbours, 268 -> 274 us with two and 322 with four.)  How it comes by the row and its tokens is one of three:
 enum Source {
   EVERY,      // every row of the table, with its segment of the sorted tokens (empty: zeros)
   MET,        // every sorted token that is the first of its row (the other rows are zeros already)
@@ -513,58 +524,6 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(EmbedGradArgs a) {
   finish_row(a, static_cast<TO*>(a.dtable) + v * a.dtable_ld, c0, lane, x);
 }
 
-// Narrow tables: 2^lanes_log2 < 64 lanes take a row, so a wave has several, and
-// each lane goes through its row's tokens by itself.
-template <class TG, class TO, int SOURCE>
-__global__ __launch_bounds__(256) void embed_narrow_kernel(EmbedGradArgs a) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2;
-  const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1);
-  const TG* const grad = static_cast<const TG*>(a.grad);
-  op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  int64_t v = i;
-  if constexpr (SOURCE == LOOK) {
-    if (i >= a.vocab) return;
-    bool any = false;
-    for (int t = 0; t < a.tokens; ++t)
-      if (load_id(a.ids, a.wide_ids, t) == v) {
-        any = true;
-        x += row_load4(grad + (int64_t)t * a.grad_ld, 4 * lane, a.width);
-      }
-    if (!any && a.accumulate) return;
-  } else {
-    int64_t s, e;
-    if constexpr (SOURCE == MET) {
-      if (i >= a.tokens) return;
-      const uint32_t k = gptr(a.keys)[i];
-      if (k >= (uint32_t)a.vocab || (i > 0 && gptr(a.keys)[i - 1] == k)) return;
-      v = k;
-      s = i;
-      e = gptr(a.seg)[2 * v + 1];
-    } else {
-      if (i >= a.vocab) return;
-      s = gptr(a.seg)[2 * v];
-      e = gptr(a.seg)[2 * v + 1];
-      if (s == e && a.accumulate) return;
-    }
-    if (e - s > a.chunk) {
-      x = row_sum<TG>(a, s, e, 0, lane);
-    } else {
-      for (int64_t j = s; j < e; j += 4) {
-        op_f32x4 y[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          y[u] = op_f32x4{0.f, 0.f, 0.f, 0.f};
-          if (j + u < e) y[u] = row_load4(grad + (int64_t)gptr(a.order)[j + u] * a.grad_ld, 4 * lane, a.width);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (j + u < e) x += y[u];
-      }
-    }
-  }
-  finish_row(a, static_cast<TO*>(a.dtable) + v * a.dtable_ld, 0, lane, x);
-}
-
 }  // namespace
 
 // -------------------------------------------------------------------- launch
@@ -588,6 +547,7 @@ EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width) 
     return at;
   };
   if (tokens <= FEW) return L;
+  // Shorter chunks have more sums to join, longer ones leave waves idle (8192 tokens: 64 was slower).
   L.chunk = 32;
   while (tokens / L.chunk >= 8192) L.chunk *= 2;
   L.blocks = (tokens + SORT_TILE - 1) / SORT_TILE;
@@ -603,12 +563,7 @@ EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width) 
 template <class TG, class TO, int SOURCE>
 static void rows_typed(EmbedGradArgs a, hipStream_t s) {
   const int64_t rows = SOURCE == MET ? a.tokens : a.vocab;
-  a.lanes_log2 = 0;
-  while ((4 << a.lanes_log2) < a.width) ++a.lanes_log2;
-  if (a.lanes_log2 < 6)
-    hipLaunchKernelGGL((embed_narrow_kernel<TG, TO, SOURCE>), dim3((unsigned)(((rows << a.lanes_log2) + 255) / 256)), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((embed_rows_kernel<TG, TO, SOURCE>), waves_grid(rows * ((a.width + STRIP - 1) / STRIP)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((embed_rows_kernel<TG, TO, SOURCE>), waves_grid(rows * ((a.width + STRIP - 1) / STRIP)), dim3(256), 0, s, a);
 }
 
 // Workgroups that fill the table with zeros.
@@ -620,7 +575,10 @@ static unsigned fill_blocks(const EmbedGradArgs& a) {
 template <class TG, class TO>
 static void grad_typed(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, hipStream_t s) {
   const unsigned strips = (unsigned)((a.width + STRIP - 1) / STRIP);
-  if (a.tokens <= FEW && !a.accumulate) return rows_typed<TG, TO, LOOK>(a, s);
+  // One launch while the rows' looks at all tokens are few.  Measured, us in one launch and
+  // in the two below: 256 tokens, 1173 x 429: 10.5 and 13; 64, 50257 x 768: 23.6 and 23.9;
+  // 256, 50257 x 768: 32 and 24.
+  if (a.tokens <= FEW && !a.accumulate && a.vocab * a.tokens <= LOOK_MOST) return rows_typed<TG, TO, LOOK>(a, s);
   // The search for the first token of an id grows with the square of the tokens, and
   // what it saves (the sort) is hidden where a large table is filled with zeros at the
   // same time.  Measured: 1000 tokens, 1173 x 429: 14 us and 24 sorted; 2048, 40298 x 39:

@@ -6,6 +6,10 @@
 // Bound by memory: one workgroup reads a 128 x 128 tile once, into registers,
 // and writes what is wanted of it: the rows' form (blocks along a row), the
 // transpose's (blocks along a column), or both under one scale (a weight).
+//
+// Measured (a large copy reaches 5.17 TB/s on the same card): 8192 x 5120 bf16, both
+// forms, 37 us, 4.5 TB/s; 8192 x 1280 bf16, rows only, 8.3 us, 3.8 TB/s; that matrix in
+// both forms and a 5120 x 1280 float32 weight in one launch 24 us, 3.4 TB/s.
 #include "block_mma.h"
 #include "ops_common.h"
 

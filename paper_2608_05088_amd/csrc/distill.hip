@@ -17,7 +17,7 @@
 // entries, tau = 2 and labels 360 us, 4.6 TB/s; losses alone with 32 entries 151 us, 5.5 TB/s
 // of reads; 4096 x 128256 bf16 451 us, 4.7 TB/s; 1001 x 100277 float32 with 100 entries, tau
 // = 1.5 and labels 214 us, 3.8 TB/s (four rounds of one row a CU, and the last 9% of it);
-// 128 x 1000 float32 10 us, the launch and three barriers.
+// 128 x 1000 float32 6 us, one load's latency and three barriers.
 #include "distill.h"
 #include "ns_common.h"
 #include "ops_common.h"
@@ -373,9 +373,12 @@ void launch_typed(const DistillArgs& a, hipStream_t s) {
   // Threads, vectors a thread holds in registers and in LDS, and the waves a SIMD (of
   // which four are a CU) that this leaves room for: as many rows a CU as fit, since one
   // row's loads go on during another's arithmetic and stores.
+  // 8192 rows: 1000 float32 columns 26 us with one vector a thread, 27 with four; 4000 and
+  // 8000 bf16 46 and 50 with four, 74 and 94 with 512 threads; 20001 bf16 146 with seven,
+  // 149 four rows a CU.
   if (nvec <= 256) launch_held<T, 256, 1, 0, 8>(a, s);
   else if (nvec <= 256 * 4) launch_held<T, 256, 4, 0, 6>(a, s);
-  else if (nvec <= 512 * 7) launch_held<T, 512, 7, 0, 6>(a, s);   // with 256 threads, a fifth in LDS: losses alone 8% slower
+  else if (nvec <= 512 * 7) launch_held<T, 512, 7, 0, 6>(a, s);
   // Four rows a CU.  512 threads and three rows: step above 348 us, with tau = 1.5 373 (not
   // 367), losses alone 165 (not 151); registers alone, two rows: 369, 404 and 165.
   else if (nvec <= 256 * 25) launch_held<T, 256, 19, 6, 4>(a, s);

@@ -12,10 +12,10 @@
 //
 // Measured (a large copy reaches 5.17 TB/s on the same card):
 //   lookup of 8192 x 1280, float32 to bf16: 8.9 us, 7 TB/s with what the caches hold;
-//   gradient of 8192 x 1024 float32 tokens, 50257 rows: 43 us, of which 26 to sort while
-//   the table's 206 MB are filled, 7 the chunks and 10 the rows; 5.6 TB/s;
+//   gradient of 8192 x 1024 float32 tokens, 50257 rows: 41 us, of which 26 to sort while
+//   the table's 206 MB are filled, the rest the chunks and the rows; 5.8 TB/s;
 //   gradient of 491520 x 768 bf16 tokens into float32: 268 us, of which 41 for the sort's
-//   seven launches, 117 the chunks (429 MB) and 110 the rows (432 MB), near 4 TB/s;
+//   seven launches, 110 the chunks (383 MB) and 118 the rows (479 MB), near 4 TB/s;
 //   rows in order instead of by chance, and ids equally frequent: 4.9 TB/s.
 #include "embed.h"
 #include "ops_common.h"
@@ -547,9 +547,10 @@ EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width) 
     return at;
   };
   if (tokens <= FEW) return L;
-  // Shorter chunks have more sums to join, longer ones leave waves idle (8192 tokens: 64 was slower).
-  L.chunk = 32;
-  while (tokens / L.chunk >= 8192) L.chunk *= 2;
+  // Shorter chunks have more sums to join, longer ones a longer last wave.  Measured: 8192
+  // tokens in chunks of 16, 32, 64: 41, 43, 48 us; 491520 in 32, 64, 128: 289, 268, 269.
+  L.chunk = 16;
+  while (tokens / L.chunk >= 4096) L.chunk *= 2;
   L.blocks = (tokens + SORT_TILE - 1) / SORT_TILE;
   L.part_ld = (width + STRIP - 1) / STRIP * STRIP;
   for (size_t& k : L.keys) k = take(4 * size_t(tokens));

@@ -64,13 +64,16 @@ __device__ __forceinline__ uint32_t token_key(const EmbedGradArgs& a, int64_t t)
 
 // Lanes of the wave whose digit equals this lane's.
 __device__ __forceinline__ uint64_t same_digit(uint32_t d, bool valid) {
-  uint64_t m = __ballot(valid);
+  const uint64_t all = __ballot(valid);
+  uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
 #pragma unroll
   for (int b = 0; b < DIGIT; ++b) {
-    const uint64_t s = __ballot((d >> b) & 1);
-    m &= ((d >> b) & 1) ? s : ~s;
+    const uint32_t x = (uint32_t)((int32_t)(d << (31 - b)) >> 31);   // bit b, all over
+    const uint64_t s = __ballot(x != 0);
+    lo &= ~((uint32_t)s ^ x);
+    hi &= ~((uint32_t)(s >> 32) ^ x);
   }
-  return m;
+  return (uint64_t)hi << 32 | lo;
 }
 
 __device__ __forceinline__ int lanes_below(uint64_t m) {

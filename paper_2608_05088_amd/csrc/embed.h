@@ -37,12 +37,14 @@ struct EmbedGradArgs {
   uint32_t* table;         // [digit][block] counts of the sort
   uint32_t* seg;           // [vocab][2]: first and one past the last sorted token
   float* part;             // [chunk][2][part_ld]
+  float* groups;           // [chunk / GROUP][part_ld], or null
   int64_t part_ld;
+  int64_t chunks;          // of the sorted tokens, `chunk` of them each
   int32_t chunk;
 };
 
 struct EmbedGradLayout {
-  size_t keys[2], index[2], table, seg, part, bytes;
+  size_t keys[2], index[2], table, seg, part, groups, bytes;
   int64_t blocks, part_ld;
   int32_t chunk;
 };

@@ -8,15 +8,18 @@
 // every row's sum is taken in the order of its tokens: the result does not
 // depend on how the work was scheduled.  A row with few tokens is summed by the
 // wave that writes it; the sorted tokens of longer rows (one id in sixteen may
-// be the same word) are first summed in chunks by waves of their own.
+// be the same word, and padding half of all) are summed in chunks by waves of
+// their own, whose sums a second launch joins.
 //
 // Measured (a large copy reaches 5.17 TB/s on the same card):
 //   lookup of 8192 x 1280, float32 to bf16: 8.9 us, 7 TB/s with what the caches hold;
-//   gradient of 8192 x 1024 float32 tokens, 50257 rows: 41 us, of which 26 to sort while
-//   the table's 206 MB are filled, the rest the chunks and the rows; 5.8 TB/s;
-//   gradient of 491520 x 768 bf16 tokens into float32: 268 us, of which 41 for the sort's
-//   seven launches, 110 the chunks (383 MB) and 118 the rows (479 MB), near 4 TB/s;
-//   rows in order instead of by chance, and ids equally frequent: 4.9 TB/s.
+//   gradient of 8192 x 1024 float32 tokens, 50257 rows: 43 us, of which 26 to sort while
+//   the table's 206 MB are filled, 11 the sums and 4 their joins; 5.6 TB/s;
+//   gradient of 491520 x 768 bf16 tokens into float32: 256 us, of which 41 for the sort's
+//   seven launches, 14 for joins and 201 for the sums (861 MB), 4.3 TB/s; the same where
+//   equal ids lie together; 263 where all are one id.
+// Joining a row in the wave that writes it, chunks in a launch before, took 41 and 268 us,
+// and 514 with one id.
 #include "embed.h"
 #include "ops_common.h"
 
@@ -26,6 +29,8 @@ namespace {
 
 constexpr int DIGIT = 8, BINS = 1 << DIGIT;
 constexpr int STRIP = 256;     // columns a wave takes, four a lane
+constexpr int GROUP = 16;      // chunks
+constexpr int JOIN_WAVES = 8, JOIN_ALONE = 16;
 constexpr int FILL_VECS = 4;   // groups of four columns a thread fills with zeros
 
 // ------------------------------------------------------------------- lookup
@@ -320,8 +325,8 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedGradArgs a, int bit
 // --------------------------------------------------------------------- sums
 // s += up to 8 rows of grad, whose loads are all in flight together; at(u) is
 // the u-th token's number (wave-uniform, u < n).  (16 rows in flight were slower, 4 no
-// faster.  8 columns a lane of bf16 instead of 4: 285 -> 320 us for the second
-// gradient above, since the registers then leave room for half the waves.)
+// faster.  For the second gradient above, 8 columns a lane of bf16 instead of 4: 285 -> 320
+// us; whole rows of three strips a wave: 277 -> 305; registers then leave room for fewer waves.)
 template <class TG, class At>
 __device__ __forceinline__ void add_rows(op_f32x4& s, const TG* grad, int64_t ld, int n, int c0, int lane, int width,
                                          At&& at) {
@@ -368,27 +373,24 @@ __device__ __forceinline__ void finish_row(const EmbedGradArgs& a, TO* out, int 
 
 // The strips of a row are neighbouring waves: a row of a gradient is then read as a
 // whole (rows and strips in different dimensions of the grid: 284 us at 491520 x 768
-// bf16, so 269).  The grid's waves, four a workgroup, run through x and then y, since
+// bf16, so 269).  The grid's waves, W a workgroup, run through x and then y, since
 // either takes fewer than 2^32 threads.
+template <int W>
 __device__ __forceinline__ uint32_t wave_of_grid() {
-  return (blockIdx.y * gridDim.x + blockIdx.x) * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  return (blockIdx.y * gridDim.x + blockIdx.x) * W + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 }
+template <int W>
 static dim3 waves_grid(int64_t waves) {
-  const int64_t blocks = (waves + 3) / 4, x = blocks < (1 << 22) ? blocks : 1 << 22;
+  const int64_t blocks = (waves + W - 1) / W, x = blocks < (1 << 24) / W ? blocks : (1 << 24) / W;
   return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
 }
 
-// Chunk c of the sorted tokens, one strip: partial sums of the segments longer
-// than a chunk.  Such a segment holds the chunk's first or last token, so a
-// chunk has two slots: 0 for the segment its first token belongs to, 1 for one
-// that starts after it.
+// A chunk of the sorted tokens, one strip: partial sums of the segments longer than a
+// chunk.  Such a segment holds the chunk's first or last token, so a chunk has two
+// slots: 0 for the segment its first token belongs to, 1 for one that starts after it.
 template <class TG>
-__global__ __launch_bounds__(256) void embed_chunks_kernel(EmbedGradArgs a) {
-  const int lane = threadIdx.x & 63;
-  const uint32_t w = wave_of_grid(), strips = (uint32_t)(a.width + STRIP - 1) / STRIP;
-  const int64_t chunk = w / strips, j0 = chunk * a.chunk, j1 = j0 + a.chunk < a.tokens ? j0 + a.chunk : a.tokens;
-  const int c0 = (int)(w % strips) * STRIP;
-  if (j0 >= a.tokens) return;
+__device__ __forceinline__ void chunk_sums(const EmbedGradArgs& a, int64_t chunk, int c0, int lane) {
+  const int64_t j0 = chunk * a.chunk, j1 = j0 + a.chunk < a.tokens ? j0 + a.chunk : a.tokens;
   const uint32_t first = a.keys[j0], last = a.keys[j1 - 1];
   float* part = a.part + chunk * 2 * a.part_ld + c0 + 4 * lane;
   const TG* grad = static_cast<const TG*>(a.grad);
@@ -402,16 +404,86 @@ __global__ __launch_bounds__(256) void embed_chunks_kernel(EmbedGradArgs a) {
   }
 }
 
-// The sum of a row's sorted tokens [s, e), one strip: taken here, or from its chunks'.
-template <class TG>
-__device__ __forceinline__ op_f32x4 row_sum(const EmbedGradArgs& a, int64_t s, int64_t e, int c0, int lane) {
-  if (e - s <= a.chunk) return sum_rows(static_cast<const TG*>(a.grad), a.grad_ld, a.order, s, e, c0, lane, a.width);
-  const int64_t k0 = s / a.chunk, k1 = (e - 1) / a.chunk;
-  const float* part = a.part + c0 + 4 * lane;
-  op_f32x4 x = load4(part + (2 * k0 + (s > k0 * a.chunk ? 1 : 0)) * a.part_ld);
+// GROUP chunks of one row, one strip: their sums in one.  (Padding may be half of all tokens.)
+__global__ __launch_bounds__(256) void embed_group_kernel(EmbedGradArgs a) {
+  const uint32_t w = wave_of_grid<4>(), strips = (uint32_t)(a.width + STRIP - 1) / STRIP;
+  const int64_t g = w / strips, j0 = g * GROUP * a.chunk;
+  const int c = (int)(w % strips) * STRIP + 4 * (threadIdx.x & 63);
+  if (g >= a.chunks / GROUP) return;
+  const uint32_t v = a.keys[j0];
+  if (v >= (uint32_t)a.vocab) return;
+  if (a.seg[2 * (int64_t)v + 1] < j0 + GROUP * a.chunk) return;
+  const float* p = a.part + g * GROUP * 2 * a.part_ld + c;
+  op_f32x4 y[GROUP];
+#pragma unroll
+  for (int i = 0; i < GROUP; ++i) y[i] = load4(p + i * 2 * a.part_ld);
+#pragma unroll
+  for (int i = 1; i < GROUP; ++i) y[0] += y[i];
+  store4(a.groups + g * a.part_ld + c, y[0]);
+}
+
+// The sums that make up row v, [s, e) of the sorted tokens, and piece q of `of` of them:
+// its chunks, or groups in the place of the chunks they hold.
+struct RowParts {
+  int64_t s, k0, n0, g0, ng, n;
+  __device__ __forceinline__ RowParts(const EmbedGradArgs& a, int64_t s_, int64_t e) : s(s_), k0(s_ / a.chunk) {
+    const int64_t k1 = (e - 1) / a.chunk + 1, width = (int64_t)GROUP * a.chunk;
+    g0 = (s + width - 1) / width;
+    ng = a.groups ? e / width - g0 : 0;
+    if (ng < 0) ng = 0;
+    n0 = ng > 0 ? g0 * GROUP - k0 : k1 - k0;
+    n = ng > 0 ? n0 + ng + k1 - (g0 + ng) * GROUP : n0;
+  }
+  __device__ __forceinline__ op_f32x4 sum(const EmbedGradArgs& a, int q, int of, int c) const {
+    op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int64_t k = k0 + 1; k <= k1; ++k) x += load4(part + 2 * k * a.part_ld);
-  return x;
+    for (int64_t i = n * q / of; i < n * (q + 1) / of; ++i) {
+      const int64_t k = i < n0 ? k0 + i : k0 + i + ng * (GROUP - 1);
+      const float* p = i >= n0 && i < n0 + ng ? a.groups + (g0 + i - n0) * a.part_ld
+                                              : a.part + (2 * k + (s > k * a.chunk ? 1 : 0)) * a.part_ld;
+      x += load4(p + c);
+    }
+    return x;
+  }
+};
+
+// Rows of more than a chunk, one strip: a wave joins the row that starts in its chunk,
+// if one does (it holds the chunk's last token).  A row of more than JOIN_ALONE parts
+// is left to the workgroup, whose waves take a run of them each.
+template <class TO>
+__global__ __launch_bounds__(64 * JOIN_WAVES) void embed_join_kernel(EmbedGradArgs a) {
+  __shared__ op_f32x4 sums[JOIN_WAVES][64];
+  __shared__ uint32_t large[JOIN_WAVES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c0 = blockIdx.y * STRIP;
+  const int64_t chunk = (int64_t)blockIdx.x * JOIN_WAVES + wave;
+  uint32_t left = (uint32_t)a.vocab;
+  if (chunk < a.chunks) {
+    const int64_t j0 = chunk * a.chunk, j1 = j0 + a.chunk < a.tokens ? j0 + a.chunk : a.tokens;
+    const uint32_t v = a.keys[j1 - 1];
+    if (v < (uint32_t)a.vocab) {
+      const int64_t s = a.seg[2 * (int64_t)v], e = a.seg[2 * (int64_t)v + 1];
+      if (s >= j0 && e - s > a.chunk) {
+        const RowParts r(a, s, e);
+        if (r.n > JOIN_ALONE) left = v;
+        else finish_row(a, static_cast<TO*>(a.dtable) + (int64_t)v * a.dtable_ld, c0, lane, r.sum(a, 0, 1, c0 + 4 * lane));
+      }
+    }
+  }
+  if (lane == 0) large[wave] = left;
+  __syncthreads();
+  for (int w = 0; w < JOIN_WAVES; ++w) {
+    const uint32_t v = __builtin_amdgcn_readfirstlane(large[w]);
+    if (v >= (uint32_t)a.vocab) continue;
+    sums[wave][lane] = RowParts(a, a.seg[2 * (int64_t)v], a.seg[2 * (int64_t)v + 1]).sum(a, wave, JOIN_WAVES, c0 + 4 * lane);
+    __syncthreads();
+    if (wave == 0) {
+      op_f32x4 x = sums[0][lane];
+#pragma unroll
+      for (int q = 1; q < JOIN_WAVES; ++q) x += sums[q][lane];
+      finish_row(a, static_cast<TO*>(a.dtable) + (int64_t)v * a.dtable_ld, c0, lane, x);
+    }
+    __syncthreads();
+  }
 }
 
 // Up to FIRST_MOST tokens: no sort.  A workgroup for each token and strip looks
@@ -472,12 +544,17 @@ enum Source {
   MET,        // every sorted token that is the first of its row (the other rows are zeros already)
   LOOK        // every row; few tokens, all of which the wave looks over itself
 };
+// Waves of a workgroup.  Rows of unequal length go better by one (491520 x 768: 263 us with
+// four, 256 with one), waves of which most have nothing to do by four (8192 x 1024: 42.8 and 44.4).
+template <int SOURCE>
+constexpr int ROW_WAVES = SOURCE == EVERY ? 1 : 4;
 template <class TG, class TO, int SOURCE>
-__global__ __launch_bounds__(256) void embed_rows_kernel(EmbedGradArgs a) {
+__global__ __launch_bounds__(64 * ROW_WAVES<SOURCE>) void embed_rows_kernel(EmbedGradArgs a) {
   const int lane = threadIdx.x & 63;
-  const uint32_t w = wave_of_grid(), strips = (uint32_t)(a.width + STRIP - 1) / STRIP;
-  const int64_t i = w / strips;
+  const uint32_t w = wave_of_grid<ROW_WAVES<SOURCE>>(), strips = (uint32_t)(a.width + STRIP - 1) / STRIP;
   const int c0 = (int)(w % strips) * STRIP;
+  if (SOURCE != LOOK && w / strips < (uint32_t)a.chunks) return chunk_sums<TG>(a, w / strips, c0, lane);
+  const int64_t i = w / strips - (SOURCE != LOOK ? a.chunks : 0);
   op_f32x4 x = {0.f, 0.f, 0.f, 0.f};
   int64_t v = i;
   if constexpr (SOURCE == LOOK) {
@@ -522,7 +599,8 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(EmbedGradArgs a) {
       e = a.seg[2 * v + 1];
       if (s == e && a.accumulate) return;
     }
-    if (s != e) x = row_sum<TG>(a, s, e, c0, lane);
+    if (e - s > a.chunk) return;   // joined later
+    if (s != e) x = sum_rows(static_cast<const TG*>(a.grad), a.grad_ld, a.order, s, e, c0, lane, a.width);
   }
   finish_row(a, static_cast<TO*>(a.dtable) + v * a.dtable_ld, c0, lane, x);
 }
@@ -550,8 +628,8 @@ EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width) 
     return at;
   };
   if (tokens <= FEW) return L;
-  // Shorter chunks have more sums to join, longer ones a longer last wave.  Measured: 8192
-  // tokens in chunks of 16, 32, 64: 41, 43, 48 us; 491520 in 32, 64, 128: 289, 268, 269.
+  // Shorter chunks have more sums to join, longer ones a longer last wave.  Measured: 20000
+  // x 100 in chunks of 16, 32, 64: 49, 49, 58 us; 491520 x 768 in 32, 64, 128: 289, 269, 263.
   L.chunk = 16;
   while (tokens / L.chunk >= 4096) L.chunk *= 2;
   L.blocks = (tokens + SORT_TILE - 1) / SORT_TILE;
@@ -560,14 +638,22 @@ EmbedGradLayout embed_grad_layout(int64_t tokens, int64_t vocab, int64_t width) 
   for (size_t& k : L.index) k = take(4 * size_t(tokens));
   L.table = take(4 * size_t(BINS) * (L.blocks + 1));
   L.seg = take(8 * size_t(vocab));
-  L.part = take(8 * size_t((tokens + L.chunk - 1) / L.chunk) * L.part_ld);
+  const int64_t chunks = (tokens + L.chunk - 1) / L.chunk;
+  L.part = take(8 * size_t(chunks) * L.part_ld);
+  if (chunks >= 1024) L.groups = take(4 * size_t(chunks / GROUP) * L.part_ld);
   return L;
 }
 
 template <class TG, class TO, int SOURCE>
-static void rows_typed(EmbedGradArgs a, hipStream_t s) {
+static void rows_typed(const EmbedGradArgs& a, hipStream_t s) {
   const int64_t rows = SOURCE == MET ? a.tokens : a.vocab;
-  hipLaunchKernelGGL((embed_rows_kernel<TG, TO, SOURCE>), waves_grid(rows * ((a.width + STRIP - 1) / STRIP)), dim3(256), 0, s, a);
+  const unsigned strips = (unsigned)((a.width + STRIP - 1) / STRIP);
+  hipLaunchKernelGGL((embed_rows_kernel<TG, TO, SOURCE>), waves_grid<ROW_WAVES<SOURCE>>((a.chunks + rows) * strips),
+                     dim3(64 * ROW_WAVES<SOURCE>), 0, s, a);
+  if (SOURCE == LOOK) return;
+  if (a.groups) hipLaunchKernelGGL(embed_group_kernel, waves_grid<4>(a.chunks / GROUP * strips), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((embed_join_kernel<TO>), dim3((unsigned)((a.chunks + JOIN_WAVES - 1) / JOIN_WAVES), strips),
+                     dim3(64 * JOIN_WAVES), 0, s, a);
 }
 
 // Workgroups that fill the table with zeros.
@@ -601,6 +687,8 @@ static void grad_typed(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, hipS
   a.part = reinterpret_cast<float*>(ws + L.part);
   a.part_ld = L.part_ld;
   a.chunk = L.chunk;
+  a.chunks = (a.tokens + a.chunk - 1) / a.chunk;
+  if (L.groups) a.groups = reinterpret_cast<float*>(ws + L.groups);
   int bits = 1;   // keys run up to vocab
   while ((int64_t(1) << bits) <= a.vocab) ++bits;
   int to = 0;
@@ -623,8 +711,6 @@ static void grad_typed(EmbedGradArgs a, const EmbedGradLayout& L, char* ws, hipS
   a.keys = keys[to ^ 1];
   a.order = index[to ^ 1];
   if (!one) hipLaunchKernelGGL(embed_segments_kernel, dim3((unsigned)((a.tokens + 255) / 256)), dim3(256), 0, s, a);
-  const unsigned chunks = (unsigned)((a.tokens + a.chunk - 1) / a.chunk);
-  hipLaunchKernelGGL((embed_chunks_kernel<TG>), waves_grid((int64_t)chunks * strips), dim3(256), 0, s, a);
   if (one) rows_typed<TG, TO, MET>(a, s);
   else rows_typed<TG, TO, EVERY>(a, s);
 }

@@ -253,6 +253,8 @@ void distill_kernel(DistillArgs a) {
     red_tau[wave] = s_tau;
     if constexpr (MODE != ONE) red_one[wave] = s_one;
   }
+  // Past the barrier a gradient written in place replaces the logits: every load has arrived.
+  if constexpr (STEP) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   s_tau = s_one = 0.f;
 #pragma unroll

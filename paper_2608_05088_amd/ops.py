@@ -244,7 +244,7 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         _tensor("labels", labels, _INDEX, dev)
         if labels.shape != lead:
             raise ValueError(f"labels must be {tuple(lead)} (got {tuple(labels.shape)})")
-        y = labels.reshape(-1)
+        y = labels if labels.dim() == 1 else labels.reshape(-1)
         yp, yt, y_stride = y.data_ptr(), _INDEX[y.dtype], (y.stride(0) if n > 1 else 0)
     wp, w_stride, w_value = None, 0, 1.0
     if isinstance(weight, torch.Tensor):
@@ -252,7 +252,7 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         if weight.dim() == 0:
             w = weight
         elif weight.shape == lead:
-            w = weight.reshape(-1)
+            w = weight if weight.dim() == 1 else weight.reshape(-1)
             w_stride = w.stride(0) if n > 1 else 0
         else:
             raise ValueError(f"grad must be a number, a scalar tensor or {tuple(lead)} (got {tuple(weight.shape)})")
@@ -273,7 +273,7 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         losses = torch.empty(lead, dtype=torch.float32, device=dev) if want_loss else None
         grad = out
         if want_grad and out is None:
-            grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+            grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
         if n == 0:
             return losses, grad
         a = lm.malt_distill_t(z.data_ptr(), zt, n, v, ld, tp, tt, ip, it, k, tld, ild, yp, yt, y_stride, tau, alpha, wp,
@@ -325,7 +325,7 @@ def distill_step(logits: torch.Tensor, top_logits: Optional[torch.Tensor], top_i
     logits, in one pass over the logits.  grad: a number, a float32 scalar
     tensor or one weight for each row (0: no gradient).  The gradient goes to
     `out` when given, which may be `logits` itself."""
-    if isinstance(logits, torch.Tensor):
+    if isinstance(logits, torch.Tensor) and logits.requires_grad:
         logits = logits.detach()
     return _distill(logits, top_logits, top_ids, labels, tau, alpha, grad, True, True, out, stream)
 

@@ -13,7 +13,8 @@ tensor) before anything is enqueued.
 Work runs on the current stream of the tensors' device, or on `stream`; the
 caller orders that stream after whatever produces the inputs.  Outputs and
 workspaces belong to the stream the work runs on.  Tensors whose rows are not
-contiguous are copied first; row pitches larger than a row are taken as they are.
+contiguous are copied first, on that stream too; row pitches larger than a row are
+taken as they are.
 """
 from __future__ import annotations
 
@@ -81,7 +82,7 @@ _current_stream = torch._C._cuda_getCurrentRawStream
 
 def _on(device: torch.device, stream, inputs, work):
     """work(stream handle) with `device` and `stream` current, so that what it
-    allocates belongs to them."""
+    allocates and copies belongs to them.  `inputs` are the caller's tensors."""
     if stream is None:
         if device.index == _current_device():
             return work(_current_stream(device.index))
@@ -100,19 +101,19 @@ def _on(device: torch.device, stream, inputs, work):
 
 # ------------------------------------------------------------------ embedding
 def _lookup(ids, weight, scale, out_dtype, stream):
-    flat = ids if ids.is_contiguous() else ids.contiguous()
-    table, ld = _rows(weight)
     v, w = weight.shape
     dev = weight.device
 
     def work(s):
+        flat = ids if ids.is_contiguous() else ids.contiguous()
+        table, ld = _rows(weight)
         out = torch.empty((*ids.shape, w), dtype=out_dtype, device=dev)
         lm._check(lm.lib().malt_embed_lookup(flat.data_ptr(), _INDEX[flat.dtype], flat.numel(), table.data_ptr(),
                                              _DTYPES[table.dtype], v, w, ld, scale, out.data_ptr(), _DTYPES[out_dtype],
                                              w, s))
         return out
 
-    return _on(dev, stream, (flat, table), work)
+    return _on(dev, stream, (ids, weight), work)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -171,13 +172,11 @@ def embedding_grad(ids: torch.Tensor, grad: torch.Tensor, num_rows: int, scale: 
     _tensor("grad", grad, _DTYPES)
     dev = grad.device
     _tensor("ids", ids, _INDEX, dev)
-    flat = ids.reshape(-1).contiguous()
     if grad.dim() < 1 or tuple(grad.shape[:-1]) != tuple(ids.shape):
         raise ValueError(f"grad must be ids.shape + (width,) (got {tuple(grad.shape)} for ids {tuple(ids.shape)})")
     w = grad.shape[-1]
     if num_rows < 1 or w < 1:
         raise ValueError(f"the table must have rows and columns (got {num_rows} x {w})")
-    g, ld = _rows(grad.reshape(-1, w))
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -190,10 +189,12 @@ def embedding_grad(ids: torch.Tensor, grad: torch.Tensor, num_rows: int, scale: 
                              f"strides {out.stride()})")
         if dtype is not None and dtype != out.dtype:
             raise ValueError(f"dtype {dtype} differs from out's {out.dtype}")
-    n = flat.shape[0]
+    n = ids.numel()
     size = _embed_grad_size(n, num_rows, w)
 
     def work(s):
+        flat = ids.reshape(-1).contiguous()
+        g, ld = _rows(grad.reshape(-1, w))
         d = torch.empty((num_rows, w), dtype=dtype, device=dev) if out is None else out
         ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
         lm._check(lm.lib().malt_embed_grad(flat.data_ptr(), _INDEX[flat.dtype], n, g.data_ptr(), _DTYPES[g.dtype], ld,
@@ -202,7 +203,7 @@ def embedding_grad(ids: torch.Tensor, grad: torch.Tensor, num_rows: int, scale: 
                                            None if ws is None else ws.data_ptr(), size, s))
         return d
 
-    return _on(dev, stream, (flat, g, out), work)
+    return _on(dev, stream, (ids, grad, out), work)
 
 
 # --------------------------------------------------------------- distillation
@@ -217,13 +218,8 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         raise ValueError(f"tau must be in [2^-60, 2^60] (got {tau})")
     if not 0 <= alpha <= 1:
         raise ValueError(f"alpha must be in [0, 1] (got {alpha})")
-    z, ld = _rows(_flat(logits) if logits.dim() > 1 else logits.reshape(1, v))
-    n = z.shape[0]
-    zt = _DTYPES[z.dtype]
-    # Teacher: pointers, types and pitches of its logits and ids.
-    t = i = y = w = None
-    tp = ip = None
-    tt = it = k = tld = ild = 0
+    n = lead.numel()
+    k = 0
     if (top_logits is None) != (top_ids is None):
         raise ValueError("top_logits and top_ids come together")
     if top_logits is not None:
@@ -235,30 +231,18 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         k = top_logits.shape[-1]
         if k > lm.DISTILL_MAX_TOP:
             raise ValueError(f"at most {lm.DISTILL_MAX_TOP} teacher entries a row (got {k})")
-        if k > 0:
-            t, tld = _rows(top_logits if top_logits.dim() == 2 else top_logits.reshape(n, k))
-            i, ild = _rows(top_ids if top_ids.dim() == 2 else top_ids.reshape(n, k))
-            tp, tt, ip, it = t.data_ptr(), _DTYPES[t.dtype], i.data_ptr(), _INDEX[i.dtype]
-    yp, yt, y_stride = None, 0, 0
     if labels is not None:
         _tensor("labels", labels, _INDEX, dev)
         if labels.shape != lead:
             raise ValueError(f"labels must be {tuple(lead)} (got {tuple(labels.shape)})")
-        y = labels if labels.dim() == 1 else labels.reshape(-1)
-        yp, yt, y_stride = y.data_ptr(), _INDEX[y.dtype], (y.stride(0) if n > 1 else 0)
-    wp, w_stride, w_value = None, 0, 1.0
+    weights = None
     if isinstance(weight, torch.Tensor):
         _tensor("grad", weight, (torch.float32,), dev)
-        if weight.dim() == 0:
-            w = weight
-        elif weight.shape == lead:
-            w = weight if weight.dim() == 1 else weight.reshape(-1)
-            w_stride = w.stride(0) if n > 1 else 0
-        else:
+        if weight.dim() > 0 and weight.shape != lead:
             raise ValueError(f"grad must be a number, a scalar tensor or {tuple(lead)} (got {tuple(weight.shape)})")
-        wp = w.data_ptr()
+        weights, weight = weight, 1.0
     else:
-        w_value = float(weight)
+        weight = float(weight)
     d, dld = None, v
     if out is not None:
         _tensor("out", out, (logits.dtype,), dev)
@@ -276,13 +260,27 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
             grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
         if n == 0:
             return losses, grad
-        a = lm.malt_distill_t(z.data_ptr(), zt, n, v, ld, tp, tt, ip, it, k, tld, ild, yp, yt, y_stride, tau, alpha, wp,
-                              w_stride, w_value, losses.data_ptr() if want_loss else None,
+        z, ld = _rows(_flat(logits) if logits.dim() > 1 else logits.reshape(1, v))
+        # Teacher, labels and weights: pointers, types and pitches.
+        tp = ip = yp = wp = None
+        tt = it = tld = ild = yt = y_stride = w_stride = 0
+        if k > 0:
+            t, tld = _rows(top_logits if top_logits.dim() == 2 else top_logits.reshape(n, k))
+            i, ild = _rows(top_ids if top_ids.dim() == 2 else top_ids.reshape(n, k))
+            tp, tt, ip, it = t.data_ptr(), _DTYPES[t.dtype], i.data_ptr(), _INDEX[i.dtype]
+        if labels is not None:
+            y = labels if labels.dim() == 1 else labels.reshape(-1)
+            yp, yt, y_stride = y.data_ptr(), _INDEX[y.dtype], (y.stride(0) if n > 1 else 0)
+        if weights is not None:
+            w = weights if weights.dim() < 2 else weights.reshape(-1)
+            wp, w_stride = w.data_ptr(), (w.stride(0) if n > 1 and w.dim() else 0)
+        a = lm.malt_distill_t(z.data_ptr(), _DTYPES[z.dtype], n, v, ld, tp, tt, ip, it, k, tld, ild, yp, yt, y_stride,
+                              tau, alpha, wp, w_stride, weight, losses.data_ptr() if want_loss else None,
                               (grad if d is None else d).data_ptr() if want_grad else None, dld)
         lm._check(lm.lib().malt_distill(byref(a), s))
         return losses, grad
 
-    return _on(dev, stream, (z, t, i, y, w, out), work)
+    return _on(dev, stream, (logits, top_logits, top_ids, labels, weights, out), work)
 
 
 class _DistillLoss(torch.autograd.Function):
@@ -367,22 +365,22 @@ def _layer_forward(x, weight, transposed, out_dtype, need_x, need_w, stream):
     dev = x.device
     n, k = weight.shape[::-1] if transposed else weight.shape
     xt, wt, yt = _DTYPES[x.dtype], _DTYPES[weight.dtype], _DTYPES[out_dtype]
-    flat, ldx = _rows(_flat(x) if x.dim() > 1 else x.reshape(1, -1))
-    w, ldw = _rows(weight)
-    m = flat.shape[0]
+    m = x.numel() // k
     sizes = _layer_sizes(m, n, k, transposed, (yt, xt, wt), need_x, need_w) if m else (0, 0, 0)
 
     def work(s):
         y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
         kept = torch.empty(sizes[0], dtype=torch.uint8, device=dev)
         if m:
+            flat, ldx = _rows(_flat(x) if x.dim() > 1 else x.reshape(1, -1))
+            w, ldw = _rows(weight)
             ws = torch.empty(sizes[1], dtype=torch.uint8, device=dev)
             lm._check(lm.lib().malt_block_layer_forward(
                 flat.data_ptr(), xt, m, k, ldx, w.data_ptr(), wt, n, ldw, transposed, y.data_ptr(), yt, n, need_x, need_w,
                 kept.data_ptr(), sizes[0], ws.data_ptr(), sizes[1], s))
         return y, kept
 
-    return (*_on(dev, stream, (flat, w), work), (m, n, k, sizes))
+    return (*_on(dev, stream, (x, weight), work), (m, n, k, sizes))
 
 
 class _Fp8Linear(torch.autograd.Function):
@@ -406,9 +404,9 @@ class _Fp8Linear(torch.autograd.Function):
         if m == 0:
             return (torch.zeros(x_shape, dtype=x_dtype, device=dev) if need_x else None,
                     torch.zeros(w_shape, dtype=w_dtype, device=dev) if need_w else None, None, None)
-        g, ld = _rows(dy if dy.dim() == 2 else dy.reshape(-1, n))
 
         def work(s):
+            g, ld = _rows(dy if dy.dim() == 2 else dy.reshape(-1, n))
             dx = torch.empty(x_shape, dtype=x_dtype, device=dev) if need_x else None
             dw = torch.empty(w_shape, dtype=w_dtype, device=dev) if need_w else None
             ws = torch.empty(sizes[2], dtype=torch.uint8, device=dev)
@@ -421,9 +419,9 @@ class _Fp8Linear(torch.autograd.Function):
         return _on(dev, None, (), work)
 
 
-def _kept(flat, values: int, scales: int, n: int, out, s) -> None:
-    """out = flat W^T on a weight's values and block scales."""
-    flat, ld = _rows(flat)
+def _kept(x, values: int, scales: int, n: int, out, s) -> None:
+    """out = x W^T on a weight's values and block scales."""
+    flat, ld = _rows(_flat(x) if x.dim() > 1 else x.reshape(1, -1))
     m, k = flat.shape
     out_type = _DTYPES[out.dtype]
     size = _linear_size(m, n, k, out_type)
@@ -435,14 +433,13 @@ def _kept(flat, values: int, scales: int, n: int, out, s) -> None:
 def _linear(x, weight, out_dtype, stream):
     """The layer without gradients."""
     dev = x.device
-    n, k = weight.shape
-    flat = _flat(x) if x.dim() > 1 else x.reshape(1, -1)
+    n = weight.shape[0]
 
     def work(s):
         y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
-        if flat.shape[0]:
+        if x.numel():
             values, scales = _quantize_weight(weight, s)
-            _kept(flat, values.data_ptr(), scales.data_ptr(), n, y, s)
+            _kept(x, values.data_ptr(), scales.data_ptr(), n, y, s)
         return y
 
     return _on(dev, stream, (x, weight), work)
@@ -517,13 +514,11 @@ def fp8_forward(x: torch.Tensor, values: torch.Tensor, scales: torch.Tensor,
         raise ValueError(f"scales must be contiguous, ({-(-n // BLOCK)}, {kb}) "
                          f"(got {tuple(scales.shape)}, strides {scales.stride()})")
     x = x.detach()
-    flat = _flat(x) if x.dim() > 1 else x.reshape(1, -1)
-    m = flat.shape[0]
 
     def work(s):
         y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
-        if m:
-            _kept(flat, values.data_ptr(), scales.data_ptr(), n, y, s)
+        if x.numel():
+            _kept(x, values.data_ptr(), scales.data_ptr(), n, y, s)
         return y
 
-    return _on(dev, stream, (flat, values, scales), work)
+    return _on(dev, stream, (x, values, scales), work)

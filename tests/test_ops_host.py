@@ -1,0 +1,85 @@
+"""What the operators' Python entries do on the host, without a GPU: where copies
+are made, what is refused, what autograd is told.  The kernels are not reached."""
+import os
+
+import pytest
+import torch
+from torch.utils._python_dispatch import TorchDispatchMode
+
+from paper_2608_05088_amd import libmalt as lm
+
+F32, I64 = torch.float32, torch.int64
+
+
+@pytest.fixture()
+def ops(monkeypatch):
+    """The module with tensors of the host let through its checks."""
+    if not os.path.exists(lm.LIB_PATH):
+        from paper_2608_05088_amd import build
+        build.build()
+    from paper_2608_05088_amd import ops as module
+    monkeypatch.setattr(module, "_tensor", lambda *a, **k: None)
+    return module
+
+
+class _Copies(TorchDispatchMode):
+    def __init__(self):
+        super().__init__()
+        self.met = []
+
+    def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+        if func.overloadpacket.__name__ in ("clone", "copy_", "_to_copy", "_reshape_copy"):
+            self.met.append(str(func))
+        return func(*args, **(kwargs or {}))
+
+
+class _Enqueued(Exception):
+    pass
+
+
+def _turned(*shape, dtype=F32):
+    """A tensor of a shape whose last two dimensions lie the other way round."""
+    return torch.zeros(*shape[:-2], shape[-1], shape[-2], dtype=dtype).transpose(-1, -2)
+
+
+def _strided_calls(ops):
+    """Every entry that takes a stream, on inputs that have to be laid out anew, and those inputs."""
+    ids, table = _turned(4, 6, dtype=I64), _turned(50, 8)
+    grad = _turned(4, 6, 8)
+    z, a, top = _turned(2, 3, 90), _turned(2, 3, 5), _turned(2, 3, 5, dtype=I64)
+    y, w = _turned(3, 2, dtype=I64).t(), _turned(3, 2).t()
+    y, w = y.t().contiguous().t(), w.t().contiguous().t()
+    x, weight = _turned(2, 3, 140), _turned(33, 140)
+    values, scales = torch.zeros(33, 256, dtype=torch.uint8), torch.zeros(1, 2, dtype=torch.uint8)
+    s = object()
+    return {
+        "embedding": (lambda: ops.embedding(ids, table, stream=s), (ids, table)),
+        "embedding_grad": (lambda: ops.embedding_grad(ids, grad, 50, stream=s), (ids, grad)),
+        "distill_loss": (lambda: ops.distill_loss(z, a, top, y, alpha=0.5, stream=s), (z, a, top, y)),
+        "distill_step": (lambda: ops.distill_step(z, a, top, y, alpha=0.5, grad=w, stream=s), (z, a, top, y, w)),
+        "fp8_linear": (lambda: ops.fp8_linear(x, weight, stream=s), (x, weight)),
+        "fp8_linear transposed": (lambda: ops.fp8_linear(x, weight.t(), transposed=True, stream=s), (x, weight)),
+        "fp8_quantize_weight": (lambda: ops.fp8_quantize_weight(weight, stream=s), (weight,)),
+        "fp8_forward": (lambda: ops.fp8_forward(x, values, scales, stream=s), (x, values, scales)),
+    }
+
+
+@pytest.mark.parametrize("entry", ["embedding", "embedding_grad", "distill_loss", "distill_step", "fp8_linear",
+                                   "fp8_linear transposed", "fp8_quantize_weight", "fp8_forward"])
+def test_copies_are_made_on_the_stream_of_the_work(ops, monkeypatch, entry):
+    """A layout copy made before the given stream is current is ordered before nothing that runs there."""
+    call, inputs = _strided_calls(ops)[entry]
+    copies = _Copies()
+    seen = []
+
+    def on(device, stream, tensors, work):
+        seen.append((list(copies.met), [t.data_ptr() for t in tensors if t is not None]))
+        raise _Enqueued
+
+    monkeypatch.setattr(ops, "_on", on)
+    with copies, pytest.raises(_Enqueued):
+        call()
+    early, recorded = seen[0]
+    assert early == []
+    for t in inputs:      # what the stream reads is not handed out again before it has
+        assert t.data_ptr() in recorded

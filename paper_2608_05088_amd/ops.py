@@ -99,6 +99,13 @@ def _on(device: torch.device, stream, inputs, work):
         return work(stream.cuda_stream)
 
 
+def _written(out: Optional[torch.Tensor]) -> None:
+    """Tells autograd that a caller's tensor holds new values, so that a backward
+    pass which had saved it raises.  (What was made in inference mode is never saved.)"""
+    if out is not None and not out.is_inference():
+        torch.autograd.graph.increment_version(out)
+
+
 # ------------------------------------------------------------------ embedding
 def _lookup(ids, weight, scale, out_dtype, stream):
     v, w = weight.shape
@@ -168,7 +175,7 @@ def embedding_grad(ids: torch.Tensor, grad: torch.Tensor, num_rows: int, scale: 
     grad over the tokens with id v, in float32 and in the tokens' order (equal
     inputs give equal bits).  grad: ids.shape + (width,).  Written to `out`
     (contiguous rows) when given, with accumulate added to it; otherwise to a
-    new tensor of `dtype` (default: grad's)."""
+    new tensor of `dtype` (default: grad's).  To autograd, `out` is changed in place."""
     _tensor("grad", grad, _DTYPES)
     dev = grad.device
     _tensor("ids", ids, _INDEX, dev)
@@ -203,7 +210,9 @@ def embedding_grad(ids: torch.Tensor, grad: torch.Tensor, num_rows: int, scale: 
                                            None if ws is None else ws.data_ptr(), size, s))
         return d
 
-    return _on(dev, stream, (ids, grad, out), work)
+    result = _on(dev, stream, (ids, grad, out), work)
+    _written(out)
+    return result
 
 
 # --------------------------------------------------------------- distillation
@@ -280,7 +289,9 @@ def _distill(logits, top_logits, top_ids, labels, tau, alpha, weight, want_loss,
         lm._check(lm.lib().malt_distill(byref(a), s))
         return losses, grad
 
-    return _on(dev, stream, (logits, top_logits, top_ids, labels, weights, out), work)
+    result = _on(dev, stream, (logits, top_logits, top_ids, labels, weights, out), work)
+    _written(out)
+    return result
 
 
 class _DistillLoss(torch.autograd.Function):
@@ -322,7 +333,8 @@ def distill_step(logits: torch.Tensor, top_logits: Optional[torch.Tensor], top_i
     """The losses of distill_loss and the gradient of sum(grad * losses) to the
     logits, in one pass over the logits.  grad: a number, a float32 scalar
     tensor or one weight for each row (0: no gradient).  The gradient goes to
-    `out` when given, which may be `logits` itself."""
+    `out` when given, which may be `logits` itself and is changed in place to autograd:
+    a backward pass that saved it raises."""
     if isinstance(logits, torch.Tensor) and logits.requires_grad:
         logits = logits.detach()
     return _distill(logits, top_logits, top_ids, labels, tau, alpha, grad, True, True, out, stream)

@@ -94,3 +94,19 @@ def test_strided_inputs_on_another_stream(ops):
             same = [torch.equal(p, q) for p, q in zip(got, want)]
         torch.cuda.synchronize()
         assert all(same), i
+
+
+def test_a_backward_pass_refuses_what_was_written_over(ops):
+    """Logits saved by the differentiable loss and then replaced by their gradient in place."""
+    z, labels = randn(20, 6, 300).requires_grad_(), torch.arange(6, device="cuda")
+    h = z * 1.0
+    loss = ops.distill_loss(h, None, None, labels, alpha=1.0).sum()
+    ops.distill_step(h, None, None, labels, alpha=1.0, out=h.detach())
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+    table = randn(21, 10, 8).requires_grad_()
+    h = table * 1.0
+    square = (h * h).sum()
+    ops.embedding_grad(labels, randn(22, 6, 8), 10, out=h.detach(), accumulate=True)
+    with pytest.raises(RuntimeError, match="inplace"):
+        square.backward()

@@ -83,3 +83,24 @@ def test_copies_are_made_on_the_stream_of_the_work(ops, monkeypatch, entry):
     assert early == []
     for t in inputs:      # what the stream reads is not handed out again before it has
         assert t.data_ptr() in recorded
+
+
+def test_results_written_in_place_are_known_to_autograd(ops, monkeypatch):
+    """A tensor given as `out` has a new version, through a detached view as well; one made in inference mode has none."""
+    monkeypatch.setattr(ops, "_on", lambda *a: (None, None))
+    ids, grad, z = torch.zeros(3, dtype=I64), torch.zeros(3, 5), torch.zeros(3, 7)
+    for call, out in ((lambda out: ops.embedding_grad(ids, grad, 4, out=out), torch.zeros(4, 5)),
+                      (lambda out: ops.distill_step(z, None, None, ids, out=out), z)):
+        leaf = out.clone().requires_grad_()
+        saved = leaf * 1.0
+        product = (saved * saved).sum()
+        call(saved.detach())
+        with pytest.raises(RuntimeError, match="inplace"):
+            product.backward()
+        with torch.inference_mode():
+            inner = torch.zeros_like(out)
+        call(inner)
+    outer = torch.zeros(4, 5)
+    with torch.inference_mode():
+        ops.embedding_grad(ids, grad, 4, out=torch.zeros(4, 5))
+        ops.embedding_grad(ids, grad, 4, out=outer)

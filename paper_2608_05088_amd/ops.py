@@ -8,7 +8,8 @@
 The definitions stand in include/libmalt.h.  This module checks arguments,
 allocates outputs and workspaces with torch, and calls the library; there is
 no CPU fallback.  Wrong arguments raise ValueError (TypeError for what is no
-tensor) before anything is enqueued.
+tensor) before anything is enqueued.  "Differentiable" means reverse mode, once; a
+tangent of forward mode is refused there.
 
 Work runs on the current stream of the tensors' device, or on `stream`; the
 caller orders that stream after whatever produces the inputs.  Outputs and
@@ -68,6 +69,12 @@ def _no_stream(stream) -> None:
     """A differentiable call follows the current stream, as its backward pass will."""
     if stream is not None:
         raise ValueError("a differentiable call takes no stream: make it within torch.cuda.stream(...)")
+
+
+def _no_tangent(name: str, x) -> None:
+    """Forward-mode derivatives are not defined: a tangent would be lost without a word."""
+    if torch.autograd.forward_ad.unpack_dual(x).tangent is not None:
+        raise ValueError(f"{name} has a tangent, but only reverse-mode derivatives are defined")
 
 
 def _flat(x: torch.Tensor) -> torch.Tensor:
@@ -156,6 +163,7 @@ def embedding(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0, out_d
     _tensor("weight", weight, _DTYPES)
     if weight.dim() != 2 or weight.numel() < 1:
         raise ValueError(f"weight must be (vocab, width) (got {tuple(weight.shape)})")
+    _no_tangent("weight", weight)
     _tensor("ids", ids, _INDEX, weight.device)
     if out_dtype is None:
         out_dtype = weight.dtype
@@ -320,6 +328,8 @@ def distill_loss(logits: torch.Tensor, top_logits: Optional[torch.Tensor], top_i
     q = softmax(logits / tau) over the vocabulary.  Ids and labels outside the
     vocabulary (-1, -100) are no entries and no labels; a part that a row lacks
     is zero.  Differentiable in logits."""
+    if isinstance(logits, torch.Tensor):
+        _no_tangent("logits", logits)
     if isinstance(logits, torch.Tensor) and logits.requires_grad and torch.is_grad_enabled():
         _no_stream(stream)
         return _DistillLoss.apply(logits, top_logits, top_ids, labels, tau, alpha)
@@ -484,6 +494,8 @@ def fp8_linear(x: torch.Tensor, weight: torch.Tensor, out_dtype: Optional[torch.
     Rounding to 8 bits passes gradients through unchanged."""
     _tensor("x", x, _DTYPES)
     _weight(weight, x.device)
+    _no_tangent("x", x)
+    _no_tangent("weight", weight)
     transposed = bool(transposed)
     out_dtype = _linear_args(x, weight.shape[0 if transposed else 1], out_dtype)
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad):

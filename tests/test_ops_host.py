@@ -104,3 +104,23 @@ def test_results_written_in_place_are_known_to_autograd(ops, monkeypatch):
     with torch.inference_mode():
         ops.embedding_grad(ids, grad, 4, out=torch.zeros(4, 5))
         ops.embedding_grad(ids, grad, 4, out=outer)
+
+
+def test_forward_mode_is_refused(ops, monkeypatch):
+    """A dual tensor has no requires_grad, so nothing else would tell that its tangent is dropped."""
+    from torch.autograd import forward_ad
+    monkeypatch.setattr(ops, "_on", lambda *a: (None, None))
+    ids, labels = torch.zeros(3, dtype=I64), torch.zeros(3, dtype=I64)
+    calls = [lambda w: ops.embedding(ids, w), lambda z: ops.distill_loss(z, None, None, labels),
+             lambda x: ops.fp8_linear(x, torch.zeros(4, 5)), lambda w: ops.fp8_linear(torch.zeros(2, 5), w),
+             lambda w: ops.fp8_linear(torch.zeros(2, 3), w, transposed=True)]
+    for call in calls:
+        with forward_ad.dual_level():
+            dual = forward_ad.make_dual(torch.zeros(3, 5), torch.ones(3, 5))
+            assert not dual.requires_grad
+            with pytest.raises(ValueError, match="reverse-mode"):
+                call(dual)
+            call(torch.zeros(3, 5))
+        call(torch.zeros(3, 5))
+    with pytest.raises(ValueError, match="reverse-mode"):
+        torch.func.jvp(calls[0], (torch.zeros(3, 5),), (torch.ones(3, 5),))

@@ -226,7 +226,8 @@ void distill_kernel(DistillArgs a) {
     if (!(fabsf(m) * c > 0x1p29f && fabsf(m) < INFINITY)) return c;
     return __uint_as_float(__float_as_uint(0x1p41f / fabsf(m)) & 0x7f800000u);
   };
-  const float c_tau = usable(r_tau), c_one = usable(r_one);
+  // Squares share the rounding of m c_tau, so c_one is twice c_tau whatever that is (r_one = 2 r_tau there).
+  const float c_tau = usable(r_tau), c_one = MODE == SQUARE ? 2.f * c_tau : usable(r_one);
   const float mc_tau = m * c_tau, mc_one = MODE == SQUARE ? 2.f * mc_tau : m * c_one;
   float s_tau = 0.f, s_one = 0.f;
   auto add = [&](float f) {

@@ -110,3 +110,39 @@ def test_a_backward_pass_refuses_what_was_written_over(ops):
     ops.embedding_grad(labels, randn(22, 6, 8), 10, out=h.detach(), accumulate=True)
     with pytest.raises(RuntimeError, match="inplace"):
         square.backward()
+
+
+@pytest.mark.parametrize("tau,alpha", [(2.0, 0.5), (2.0, 0.125), (1.5, 0.5), (1.0, 0.5), (2.0, 0.0), (2.0, 1.0)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_distillation_of_logits_of_hundreds_of_millions(ops, tau, alpha, sign):
+    """Maxima m on both sides of where |m| log2(e) and |m| log2(e) / tau pass 2^29, the rest up to four spacings below.
+
+    Exponents (f - m) log2(e) / t reach 4 * 64 * 1.45 = 371 beside a rounding of m c of at most 2^5, so each is
+    rounded by less than 2^9 u, and sums of 40 terms by 40 u: log-probabilities are within 2^-13, a row's loss within
+    2^-13 of its coefficients, probabilities within 2^-13 too."""
+    v = 40
+    tops = [1.0e8, 3.6e8, 3.72e8, 3.8e8, 5.0e8, 5.5e8, 7.0e8, 7.4e8, 7.5e8, 1.0e9]
+    z = torch.empty(len(tops), v, dtype=torch.float64)
+    steps = torch.randint(0, 5, z.shape, generator=torch.Generator().manual_seed(30)).double()
+    for r, t in enumerate(tops):
+        m = torch.tensor(t, dtype=F32).double()
+        spacing = 2.0 ** (math.floor(math.log2(t)) - 23)
+        z[r] = sign * m - spacing * steps[r]
+        z[r, 7], z[r, 11] = sign * m, sign * m - spacing
+    z32 = z.to(F32)
+    assert torch.equal(z32.double(), z)
+    n = len(tops)
+    labels = torch.tensor([7, 11] * (n // 2))
+    ids = torch.tensor([[7, 3, 11]] * n)
+    a = torch.tensor([[1.0, 0.5, -0.25]] * n, dtype=torch.float64)
+    p = torch.softmax(a / tau, 1)
+    lq, l1 = torch.log_softmax(z / tau, 1), torch.log_softmax(z, 1)
+    big = (1 - alpha) * tau ** 2 + alpha
+    want = (1 - alpha) * tau ** 2 * (p * (p.log() - lq.gather(1, ids))).sum(1) - alpha * l1.gather(1, labels[:, None])[:, 0]
+    grad = (1 - alpha) * tau * lq.exp() + alpha * l1.exp()
+    grad.scatter_add_(1, ids, -(1 - alpha) * tau * p)
+    grad.scatter_add_(1, labels[:, None], torch.full((n, 1), -alpha, dtype=torch.float64))
+    got = ops.distill_step(z32.cuda(), a.float().cuda(), ids.cuda(), labels.cuda(), tau=tau, alpha=alpha)
+    off = (got[0].double().cpu() - want).abs() - 2 * U * want.abs()
+    assert bool((off <= 2.0 ** -13 * big).all()), off
+    assert bool(((got[1].double().cpu() - grad).abs() <= 2.0 ** -13 * big).all())

@@ -146,3 +146,33 @@ def test_distillation_of_logits_of_hundreds_of_millions(ops, tau, alpha, sign):
     off = (got[0].double().cpu() - want).abs() - 2 * U * want.abs()
     assert bool((off <= 2.0 ** -13 * big).all()), off
     assert bool(((got[1].double().cpu() - grad).abs() <= 2.0 ** -13 * big).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [7, 63, 1000, 4097, 15001, 53257, 110003])
+@pytest.mark.parametrize("tau,alpha", [(1.0, 0.0), (2.0, 0.5), (1.5, 0.25), (0.5, 0.75), (3.0, 1.0)])
+def test_small_probabilities_are_right_relatively(ops, dtype, v, tau, alpha):
+    """Columns that nothing is taken off are sums of positive terms: their gradient is right to its own size.
+
+    An exponent e = (z - m) log2(e) / t is rounded by (|e| + |m c|) u twice at most (constant and product) and the
+    exponential by 4 u; a row's sum has chains of at most v / 256 + 64 additions, each rounded by u, of terms as
+    accurate; the coefficients and the last product add 8 u.  q1 may be the square of an exponential, which doubles the
+    first part.  So a column is within (4 E + v / 256 + 80) u, E = max |z| log2(e) / min(t) of both signs together,
+    and its rounding to the type.  Columns below 2^-100 are left to the absolute bounds."""
+    n, k = 4, min(v // 2, 33)
+    z = randn(40 + v, n, v, scale=3.0, dtype=dtype)
+    ids = torch.stack([torch.randperm(v, device="cuda", generator=gen(41 + r))[:k] for r in range(n)])
+    a = z.float().gather(1, ids) + randn(42, n, k)
+    labels = torch.randint(0, v, (n,), device="cuda", generator=gen(43))
+    weight = randn(44, n)
+    _, got = ops.distill_step(z, a, ids, labels, tau=tau, alpha=alpha, grad=weight)
+    zz = z.double()
+    # The plain formula, the parameters as float32 (tau = 1.5 and the rest are exact there).
+    want = weight.double()[:, None] * ((1 - alpha) * tau * torch.softmax(zz / tau, 1) + alpha * torch.softmax(zz, 1))
+    free = torch.ones_like(z, dtype=torch.bool).scatter_(1, ids, False).scatter_(1, labels[:, None], False)
+    free &= want.abs() > 2.0 ** -100
+    e = 2 * float(zz.abs().max()) * math.log2(math.e) * max(1.0, 1.0 / tau)
+    rel = (4 * e + v / 256 + 80) * U + torch.finfo(dtype).eps / 2 * 1.01
+    off = (got.double() - want).abs() / want.abs()
+    assert int(free.sum()) >= n * (v - k - 1) // 2
+    assert float(off[free].max()) <= rel, (float(off[free].max()), rel)

@@ -420,7 +420,9 @@ malt_status_t malt_block_linear(const void* x, malt_dtype_t x_type, int64_t m, i
  * w (for dx) and w's scales, in 8 bits.  need_dx, need_dw: which gradients will
  * be asked for; the backward call must ask (dx, dw not NULL) for those.
  * malt_block_layer_size gives the bytes of kept and of both workspaces, all
- * 256-byte aligned; NULL is fine where it says 0.
+ * 256-byte aligned; NULL is fine where it says 0.  Where things lie in `kept`
+ * depends on the gradients chosen, and so does its size: the backward call takes
+ * exactly the kept_bytes of its gradients and refuses others (MALT_ERR_INVALID_ARG).
  * Limits: those of the products, and m k, n k, m n <= 2^35. */
 malt_status_t malt_block_layer_size(int64_t m, int64_t n, int64_t k, int32_t w_transposed, malt_dtype_t y_type,
                                     malt_dtype_t dx_type, malt_dtype_t dw_type, int32_t need_dx, int32_t need_dw,

@@ -403,6 +403,8 @@ static LayerLayout layer_layout(int64_t m, int64_t n, int64_t k, bool w_t, bool 
   }
   if (need_x) L.wt = take(L.kept, values(k, n));
   L.w_scales = take(L.kept, size_t(q_pad(n) / QB) * (q_pad(k) / QB));
+  // What `kept` holds is told by its size: no two choices of gradients have the same.
+  if (need_w && !need_x && L.w_scales == align256(values(k, n))) take(L.kept, 1);
   L.q = take(L.forward, values(m, k));
   L.q_scales = take(L.forward, scales(m, k));
   L.w = take(L.forward, values(n, k));
@@ -519,6 +521,8 @@ malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, in
   for (int i = 2; i < 5; ++i)
     for (int j = 0; j < i; ++j)
       if (op_overlap(b[i].p, b[i].n, b[j].p, b[j].n)) return fail(MALT_ERR_ALIAS, "two of the layer's buffers overlap");
+  if (kept_bytes != L.kept)
+    return fail(MALT_ERR_INVALID_ARG, "%zu kept bytes where these gradients need %zu: the forward call kept for others", kept_bytes, L.kept);
   const uint8_t* const kb = static_cast<const uint8_t*>(kept);
   uint8_t* const ws = static_cast<uint8_t*>(workspace);
   QuantArgs q = {};

@@ -75,21 +75,23 @@ def make_optimizer(kind: str, model, lr: float, adamw_lr: float, weight_decay: f
 def use_operators(model) -> None:
     """The token table and the block matrices' layers on this package's kernels:
     lookup with the gradient by sorted tokens, products in 8 bits."""
-    import functools
     from transformers.pytorch_utils import Conv1D
     from . import ops
-    table = model.transformer.wte
 
-    def lookup(ids):
-        return ops.embedding(ids, table.weight)
+    # Classes in the modules' places: a module that holds a function on itself is a cycle, freed late, and in a
+    # copy of the model the function would still read the original's weights.
+    class Table(type(model.transformer.wte)):
+        def forward(self, ids):
+            return ops.embedding(ids, self.weight)
 
-    def layer(mod, x):
-        return ops.fp8_linear(x, mod.weight, transposed=True) + mod.bias
+    class Layer(Conv1D):
+        def forward(self, x):
+            return ops.fp8_linear(x, self.weight, transposed=True) + self.bias
 
-    table.forward = lookup
+    model.transformer.wte.__class__ = Table
     for mod in model.transformer.h.modules():
         if isinstance(mod, Conv1D):
-            mod.forward = functools.partial(layer, mod)
+            mod.__class__ = Layer
 
 
 def distill_backward(student, teacher, ids, top_k: int = 64, tau: float = 2.0, alpha: float = 0.5, scale: float = 1.0):

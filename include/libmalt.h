@@ -279,9 +279,9 @@ void malt_destroy_state(malt_plan_t* plan);
  * Operators of a training step around the optimizer: the token table, the
  * distillation loss and linear layers in 8-bit floating point.  They need no
  * plan.  Matrices are row-major with a row pitch (`ld`, in elements, >= the
- * row's length); pointers are aligned to their element type.  Work is enqueued on
- * `stream`, which must belong to the current device; nothing waits on the host
- * and nothing is allocated.  A buffer that is written may overlap no other
+ * row's length and below 2^31, as strides are); pointers are aligned to their
+ * element type.  Work is enqueued on `stream`, which must belong to the current
+ * device; nothing waits on the host and nothing is allocated.  A buffer that is written may overlap no other
  * unless stated (MALT_ERR_ALIAS).  An empty product of sizes enqueues nothing
  * but what the definition asks for (a gradient over no tokens is zero).
  * ======================================================================== */

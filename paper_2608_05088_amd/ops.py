@@ -15,7 +15,7 @@ Work runs on the current stream of the tensors' device, or on `stream`; the
 caller orders that stream after whatever produces the inputs.  Outputs and
 workspaces belong to the stream the work runs on.  Tensors whose rows are not
 contiguous are copied first, on that stream too; row pitches larger than a row are
-taken as they are.
+taken as they are up to 2^31 - 1 elements, as are those of outputs.
 """
 from __future__ import annotations
 
@@ -30,6 +30,7 @@ from . import libmalt as lm
 _DTYPES = {torch.float32: lm.MALT_FLOAT32, torch.bfloat16: lm.MALT_BFLOAT16}
 _INDEX = {torch.int32: lm.MALT_INT32, torch.int64: lm.MALT_INT64}
 BLOCK = 128   # values that share a scale
+MAX_PITCH = (1 << 31) - 1   # elements between two rows
 
 
 # ------------------------------------------------------------------ arguments
@@ -56,11 +57,12 @@ def _type(name: str, dtype) -> int:
 
 
 def _rows(x: torch.Tensor) -> Tuple[torch.Tensor, int]:
-    """A 2-D tensor whose rows are contiguous and do not overlap, and its row pitch."""
+    """A 2-D tensor whose rows are contiguous, do not overlap and lie no further apart
+    than the library takes, and its row pitch."""
     r, c = x.shape
     if x.is_contiguous():
         return x, c
-    if (c > 1 and x.stride(1) != 1) or (r > 1 and x.stride(0) < c):
+    if (c > 1 and x.stride(1) != 1) or (r > 1 and not c <= x.stride(0) <= MAX_PITCH):
         x = x.contiguous()
     return x, (x.stride(0) if r > 1 else c)
 

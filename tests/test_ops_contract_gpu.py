@@ -176,3 +176,19 @@ def test_small_probabilities_are_right_relatively(ops, dtype, v, tau, alpha):
     off = (got.double() - want).abs() / want.abs()
     assert int(free.sum()) >= n * (v - k - 1) // 2
     assert float(off[free].max()) <= rel, (float(off[free].max()), rel)
+
+
+def test_rows_further_apart_than_a_pitch_goes(ops):
+    """Two rows 2^31 + 8 elements apart: copied where they are read, refused where they would be written."""
+    far = torch.empty((1 << 31) + 8 + 300, device="cuda", dtype=BF16).as_strided((2, 300), ((1 << 31) + 8, 1))
+    z, labels = randn(50, 2, 300, dtype=BF16), torch.tensor([5, 7], device="cuda")
+    far.copy_(z)
+    want = ops.distill_step(z, None, None, labels, alpha=1.0)
+    got = ops.distill_step(far, None, None, labels, alpha=1.0)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert torch.equal(ops.embedding(labels - 6, far), ops.embedding(labels - 6, z))
+    weight = randn(51, 20, 300, dtype=BF16)
+    assert torch.equal(ops.fp8_linear(far, weight), ops.fp8_linear(z, weight))
+    with pytest.raises(lm.MaltError, match="pitch"):
+        ops.distill_step(z, None, None, labels, alpha=1.0, out=far)
+    assert torch.equal(far, z)

@@ -124,3 +124,18 @@ def test_forward_mode_is_refused(ops, monkeypatch):
         call(torch.zeros(3, 5))
     with pytest.raises(ValueError, match="reverse-mode"):
         torch.func.jvp(calls[0], (torch.zeros(3, 5),), (torch.ones(3, 5),))
+
+
+def test_rows_too_far_apart_are_copied(ops):
+    """The kernels take row pitches below 2^31 elements; the last token of (2, 65536, 50257) logits lies further apart."""
+    last = torch.empty((2, 65536, 50257), dtype=torch.bfloat16, device="meta")[:, -1]
+    assert last.stride(0) >= 1 << 31
+    x, ld = ops._rows(last)
+    assert x.is_contiguous() and ld == 50257
+    near = torch.empty((2, 1 << 15, 1 << 15), dtype=torch.bfloat16, device="meta")[:, -1]
+    x, ld = ops._rows(near)
+    assert x is near and ld == 1 << 30
+    edge = torch.empty_strided((3, 8), ((1 << 31) - 1, 1), device="meta")
+    assert ops._rows(edge)[1] == (1 << 31) - 1
+    one = torch.empty_strided((1, 8), (1 << 40, 1), device="meta")
+    assert ops._rows(one)[1] == 8

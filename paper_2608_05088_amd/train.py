@@ -106,7 +106,7 @@ def distill_backward(student, teacher, ids, top_k: int = 64, tau: float = 2.0, a
     labels = torch.full_like(ids, -100)
     labels[:, :-1] = ids[:, 1:]
     top.indices[:, -1] = -1          # the last token has neither teacher nor label
-    count = ids.shape[0] * (ids.shape[1] - 1)
+    count = max(1, ids.shape[0] * (ids.shape[1] - 1))   # no token has a next one: nothing to learn, loss 0
     # The gradient takes the logits' place: nobody reads them again.
     losses, grad = ops.distill_step(logits, top.values, top.indices, labels, tau=tau, alpha=alpha, grad=scale / count,
                                     out=logits.detach())

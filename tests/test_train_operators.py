@@ -43,3 +43,22 @@ def test_a_copy_of_a_model_on_the_operators_has_weights_of_its_own(monkeypatch):
         assert torch.allclose(m(input_ids=ids).logits, want, atol=1e-5)
         assert len(seen) == 1 + 2 * 4 and all(any(w is p for p in m.parameters()) for w in seen)
     assert [n for n, _ in model.named_parameters()] == [n for n, _ in _model().named_parameters()]
+
+
+def test_a_micro_batch_without_next_tokens(monkeypatch):
+    """Sequences of one token: no loss and no gradient, as a mean over nothing, not a division by zero."""
+    from types import SimpleNamespace
+
+    from paper_2608_05088_amd import ops
+    from paper_2608_05088_amd.train import distill_backward
+    z = torch.randn(3, 1, 40, requires_grad=True)
+
+    def step(logits, top, top_ids, labels, tau, alpha, grad, out):
+        assert bool((top_ids == -1).all()) and bool((labels == -100).all())   # rows of neither: zeros
+        return torch.zeros(3, 1), torch.zeros_like(logits)
+
+    monkeypatch.setattr(ops, "distill_step", step)
+    loss = distill_backward(lambda input_ids: SimpleNamespace(logits=z * 1.0),
+                            lambda input_ids: SimpleNamespace(logits=torch.randn(3, 1, 40)),
+                            torch.zeros(3, 1, dtype=torch.int64), top_k=5)
+    assert float(loss) == 0.0 and bool((z.grad == 0).all())

@@ -542,7 +542,7 @@ __global__ __launch_bounds__(1024) void embed_fill_kernel(EmbedGradArgs a) {
 enum Source {
   EVERY,      // every row of the table, with its segment of the sorted tokens (empty: zeros)
   MET,        // every sorted token that is the first of its row (the other rows are zeros already)
-  LOOK        // every row; few tokens, all of which the wave looks over itself
+  LOOK        // every row, written anew; few tokens, all of which the wave looks over itself
 };
 // Waves of a workgroup.  Rows of unequal length go better by one (491520 x 768: 263 us with
 // four, 256 with one), waves of which most have nothing to do by four (8192 x 1024: 42.8 and 44.4).
@@ -581,8 +581,6 @@ __global__ __launch_bounds__(64 * ROW_WAVES<SOURCE>) void embed_rows_kernel(Embe
           add_rows(x, static_cast<const TG*>(a.grad), a.grad_ld, n < 8 ? n : 8, c0, lane, a.width, [&](int u) { return t[u]; });
         }
       }
-    } else if (a.accumulate) {
-      return;
     }
   } else {
     int64_t s, e;

@@ -363,6 +363,18 @@ malt_status_t malt_distill(const malt_distill_t* args, void* stream);
  * (4 exponent, 3 mantissa bits, ties to even).  A block holding an infinity or a
  * NaN makes every sum it enters NaN.
  *
+ * Products of two operands (malt_block_matmul, malt_block_linear and the layer's)
+ * are as precise as their result:
+ *  - float32 results: products and sums in float32.  Values (q times its scale)
+ *    are multiplied as bfloat16, which is exact but for those that are no multiple
+ *    of 2^-133, bfloat16's smallest number; these are off by less than that.
+ *  - bfloat16 results: fewer bits.  The 8-bit matrix instruction adds the products of
+ *    8 neighbouring values with 14 bits below the largest of them, and these
+ *    sums in float32.  Before it is rounded to bfloat16 a result is off by up to
+ *    2^-11 sum |a||b|: 1e-5 to 6e-5 of the results' norm measured on random values,
+ *    more than the result's own rounding where large products cancel.  Whoever
+ *    wants bfloat16 results of float32 sums asks for float32 ones and rounds them.
+ *
  * An operand of `rows` rows over a contraction of `cols` values is
  *   values: rows x pad128(cols) bytes, zeros past cols;
  *   scales: bytes e + 127, one for each row and 128 values, in the order the
@@ -386,7 +398,7 @@ malt_status_t malt_block_quantize_weight(const void* w, malt_dtype_t type, int64
                                          void* values, void* block_scales, void* t_values, void* stream);
 
 /* out (m x n) = (accumulate ? out : 0) + A B^T over k values, A m x k, B n x k,
- * sums in float32, rounded once to out_type.
+ * summed as said above, rounded once to out_type.
  *  b_blocks = 0: b_scales are an operand's.
  *  b_blocks = 1: B is a weight's values, or its transpose's; the scale of rows
  *    128 i .. and values 128 j .. is b_scales[i * b_row_stride + j * b_col_stride].
@@ -402,7 +414,8 @@ malt_status_t malt_block_matmul(int64_t m, int64_t n, int64_t k, const void* a_v
 
 /* A linear layer on a kept weight (malt_block_quantize_weight's values and
  * block_scales, n x k): x (m x k) is brought to 8 bits and multiplied,
- * out (m x n) = x w^T; up to 32 rows in one launch.  Types and limits as above.
+ * out (m x n) = x w^T; up to 32 rows in one launch.  Types, precision and limits
+ * as above.
  * workspace: device memory of malt_block_linear_size's bytes (may be 0; then
  * NULL), 256-byte aligned. */
 malt_status_t malt_block_linear_size(int64_t m, int64_t n, int64_t k, malt_dtype_t out_type, size_t* workspace_bytes);
@@ -415,6 +428,7 @@ malt_status_t malt_block_linear(const void* x, malt_dtype_t x_type, int64_t m, i
  *   forward:  y = Q(x) Q(w)^T, x by rows, w by 128 x 128 blocks;
  *   backward: dx = Q(dy) Q(w), dy by rows;  dw = Q(dy)^T Q(x), both by columns of
  *             128 rows; dw is added to with accumulate.
+ * Each of y, dx and dw is as precise as its own type (above).
  * w_transposed: w and dw lie k x n (y = x w), as GPT-2's layers store them.
  * `kept` carries what the backward pass needs from the forward's: x^T (for dw),
  * w (for dx) and w's scales, in 8 bits.  need_dx, need_dw: which gradients will

@@ -8,9 +8,9 @@
 //   measured, results are 1e-5 to 6e-5 of their norm off, a thirtieth of what
 //   rounding them to bf16 (1.7e-3) costs.
 // float32: that is not enough for sums that are kept in 32 bits, so the values
-//   are widened to bf16 on their way from LDS, scale included (both exact), and
-//   v_mfma_f32_16x16x32_bf16, whose sums are off by 1e-8 to 1e-7, multiplies them
-//   at half the rate.
+//   are widened to bf16 on their way from LDS, scale included (both exact down to
+//   bf16's smallest number, 2^-133), and v_mfma_f32_16x16x32_bf16, whose sums are
+//   off by 1e-8 to 1e-7, multiplies them at half the rate.
 //
 // Bound by the matrix cores (and their power).  Measured, the library's products without
 // block scales beside: 8192 x 5120 x 1280 bf16 73 us, 1.47 PFLOP/s (8-bit library 72);

@@ -74,7 +74,8 @@ __device__ __forceinline__ ns::f32x4 mma_sel(i32x8 b, i32x8 a, ns::f32x4 c, int 
   }
 }
 
-// Eight 8-bit values (two dwords) times 2^e as bf16, exactly; `scale` is 2^e.
+// Eight 8-bit values (two dwords) times 2^e as bf16, exactly where they are multiples
+// of 2^-133, bf16's smallest number; `scale` is 2^e, of which the exponent byte counts.
 __device__ __forceinline__ ns::bf16x8 widen(int lo, int hi, float scale) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)lo, scale, false);
@@ -83,7 +84,8 @@ __device__ __forceinline__ ns::bf16x8 widen(int lo, int hi, float scale) {
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)hi, scale, true);
   return ns::bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
-// The power of two of exponent byte i of a scale register.
+// The power of two of exponent byte i of a scale register, for `widen`: byte 0, a float32
+// zero, is taken as 2^-127 there, and byte 255 as no number.
 __device__ __forceinline__ float scale_of(int bytes, int i) {
   return __uint_as_float((((uint32_t)bytes >> (8 * i)) & 0xffu) << 23);
 }

@@ -486,9 +486,16 @@ def _weight(weight, device=None) -> None:
 def fp8_linear(x: torch.Tensor, weight: torch.Tensor, out_dtype: Optional[torch.dtype] = None,
                transposed: bool = False, stream=None) -> torch.Tensor:
     """x weight^T with both brought to 8 bits: x with a scale for each row and
-    128 values, weight (outer, inner) with one for each 128 x 128 block.  Sums
-    are float32; out_dtype: x's unless given.  transposed: weight is
-    (inner, outer), as GPT-2's layers store it, and the result x weight.
+    128 values, weight (outer, inner) with one for each 128 x 128 block.
+    out_dtype: x's unless given.  transposed: weight is (inner, outer), as GPT-2's
+    layers store it, and the result x weight.
+
+    float32 results are float32 sums.  bfloat16 results are summed with fewer bits:
+    products of 8 neighbouring values with 14 bits below the largest, these sums in
+    float32, off by up to 2^-11 sum |x||w| before they are rounded (1e-5 to 6e-5 of
+    their norm on random values; more than bfloat16's rounding where large products
+    cancel).  For bfloat16 results of float32 sums take out_dtype=torch.float32 and
+    round.  The gradients are as precise as their types, x's and weight's.
 
     The backward pass runs in 8 bits too: the output's gradient by rows times
     the same 8-bit weight, and the transposes of gradient and x, with a scale for
@@ -522,7 +529,8 @@ def fp8_quantize_weight(weight: torch.Tensor, stream=None) -> Tuple[torch.Tensor
 def fp8_forward(x: torch.Tensor, values: torch.Tensor, scales: torch.Tensor,
                 out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """fp8_linear on kept weights (fp8_quantize_weight), without gradients:
-    x (..., inner), values (outer, inner padded to whole blocks)."""
+    x (..., inner), values (outer, inner padded to whole blocks).  Precision by
+    out_dtype, as there."""
     _tensor("values", values, (torch.float8_e4m3fn,))
     dev = values.device
     _tensor("x", x, _DTYPES, dev)

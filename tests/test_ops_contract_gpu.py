@@ -192,3 +192,67 @@ def test_rows_further_apart_than_a_pitch_goes(ops):
     with pytest.raises(lm.MaltError, match="pitch"):
         ops.distill_step(z, None, None, labels, alpha=1.0, out=far)
     assert torch.equal(far, z)
+
+
+# ============================================================ precision of 8-bit products
+def _rounded64(x, rows, cols):
+    """The 8-bit form's values in 64 bits: least 2^e >= 2^-127 with max|block| <= 448 2^e, nearest, ties to even."""
+    r, k = x.shape
+    full = torch.zeros((-(-r // rows) * rows, -(-k // cols) * cols), dtype=torch.float64)
+    full[:r, :k] = x.double().cpu()
+    b = full.view(full.shape[0] // rows, rows, full.shape[1] // cols, cols)
+    top = b.abs().amax(3).amax(1)
+    m, e = torch.frexp(torch.where(top > 0, top, torch.full_like(top, 448.0)))
+    unit = torch.ldexp(torch.ones_like(top), torch.clamp(e - 9 + (m > 0.875), min=-127))[:, None, :, None]
+    v = b / unit
+    step = torch.ldexp(torch.ones_like(v), torch.frexp(v.abs().clamp(min=2.0 ** -6)).exponent - 4)
+    return (torch.round(v / step) * step * unit).reshape(full.shape)[:r, :k]
+
+
+@pytest.mark.parametrize("m", [1, 20, 40, 300])
+def test_products_that_cancel(ops, m):
+    """Whole numbers: each 8 neighbouring products are 200704, -200704 and six small ones.  float32 sums, all below
+    2^24, are exact, and so are bfloat16 results rounded from them; bfloat16 results of their own lose up to 2^-11 of
+    the products' magnitudes."""
+    k, n = 384, 70
+    g = gen(60)
+    x = torch.randint(-3, 4, (m, k), device="cuda", generator=g).float()
+    w = torch.randint(-3, 4, (n, k), device="cuda", generator=g).float()
+    x[:, ::8], w[:, ::8] = 448.0, 448.0
+    x[:, 5::8], w[:, 5::8] = -448.0, 448.0
+    want, size = x.double() @ w.double().t(), x.double().abs() @ w.double().abs().t()
+    kept = ops.fp8_quantize_weight(w)
+    y = ops.fp8_forward(x, *kept, out_dtype=F32)
+    assert torch.equal(y.double(), want)
+    assert torch.equal(ops.fp8_linear(x, w), y)
+    assert torch.equal(y.to(BF16), want.to(BF16))
+    low = ops.fp8_forward(x, *kept, out_dtype=BF16)
+    assert bool(((low.double() - want).abs() <= 2.0 ** -11 * size + 2.0 ** -8 * 1.01 * want.abs()).all())
+    # The gradients' precision goes by their types.
+    xg, wg = x.to(BF16).requires_grad_(), w.clone().requires_grad_()
+    dy = torch.zeros(m, n, device="cuda", dtype=BF16)
+    dy[:, :8] = 1.0
+    dx, dw = torch.autograd.grad(ops.fp8_linear(xg, wg), (xg, wg), dy)
+    assert dx.dtype == BF16 and dw.dtype == F32
+    assert torch.equal(dw.double(), dy.double().t() @ x.double())
+
+
+@pytest.mark.parametrize("m", [5, 200])
+@pytest.mark.parametrize("p", [-110, -118, -120, -124, -126, -128, -130, -134, -140])
+@pytest.mark.parametrize("tiny", ["x", "weight"])
+def test_products_of_tiny_blocks(ops, m, p, tiny):
+    """Blocks down to the least scale, 2^-127, against large ones: float32 results are off by float32's sums and by
+    less than 2^-133 a value, bfloat16 ones by what is said of theirs."""
+    k, n = 256, 70
+    small = (torch.randn(m if tiny == "x" else n, k, device="cuda", generator=gen(61), dtype=torch.float64) * 2.0 ** p).float()
+    large = randn(62, n if tiny == "x" else m, k, scale=2.0 ** 100)
+    x, w = (small, large) if tiny == "x" else (large, small)
+    xq, wq = _rounded64(x, 1, 128), _rounded64(w, 128, 128)
+    want, size = xq @ wq.t(), xq.abs() @ wq.abs().t()
+    other = (wq if tiny == "x" else xq).abs().sum(1)
+    lost = 2.0 ** -133 * (other[None] if tiny == "x" else other[:, None])
+    kept = ops.fp8_quantize_weight(w)
+    diff = (ops.fp8_forward(x, *kept, out_dtype=F32).double().cpu() - want).abs()
+    assert bool((diff <= (k + 2) * U * size + lost).all())
+    diff = (ops.fp8_forward(x, *kept, out_dtype=BF16).double().cpu() - want).abs()
+    assert bool((diff <= 2.0 ** -11 * size + 2.0 ** -8 * 1.01 * want.abs()).all())

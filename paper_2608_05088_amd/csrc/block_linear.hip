@@ -8,8 +8,9 @@
 // block's maximum is two exchanges away.  A separate conversion would cost a
 // launch and a round trip through memory, longer than the product itself.
 //
-// Measured: one token, 1280 -> 5120 (6.6 MB of weights) 5.9 us, the latency of five
-// rounds of loads and of the join; 4096 -> 16384 (67 MB) 18 us, 3.7 TB/s; 32 tokens 29.
+// Measured: one token, 1280 -> 5120 (6.6 MB of weights) 5.9 us: of ten blocks two waves
+// take two, and a block is a chain of loads, exchanges and products with nothing
+// loaded ahead, then the join; 4096 -> 16384 (67 MB) 18 us, 3.7 TB/s; 32 tokens 29.
 #include <type_traits>
 
 #include "block_mma.h"

@@ -254,7 +254,8 @@ void distill_kernel(DistillArgs a) {
     red_tau[wave] = s_tau;
     if constexpr (MODE != ONE) red_one[wave] = s_one;
   }
-  // Past the barrier a gradient written in place replaces the logits: every load has arrived.
+  // Past the barrier a gradient written in place replaces the logits.  Wave 0 may not have used its
+  // entries' and its label's logits yet, which other waves' columns hold: its loads have to have arrived.
   if constexpr (STEP) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   s_tau = s_one = 0.f;

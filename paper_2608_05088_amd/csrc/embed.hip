@@ -13,8 +13,9 @@
 //
 // Measured (a large copy reaches 5.17 TB/s on the same card):
 //   lookup of 8192 x 1280, float32 to bf16: 8.9 us, 7 TB/s with what the caches hold;
-//   gradient of 8192 x 1024 float32 tokens, 50257 rows: 43 us, of which 26 to sort while
-//   the table's 206 MB are filled, 11 the sums and 4 their joins; 5.6 TB/s;
+//   gradient of 8192 x 1024 float32 tokens, 50257 rows: 53 us, of which 36 to fill the table's
+//   206 MB while the tokens are sorted, 11 the sums and 6 their joins; 4.5 TB/s (43 in all
+//   where the caches still hold part of the table);
 //   gradient of 491520 x 768 bf16 tokens into float32: 256 us, of which 41 for the sort's
 //   seven launches, 14 for joins and 201 for the sums (861 MB), 4.3 TB/s; the same where
 //   equal ids lie together; 263 where all are one id.
@@ -251,8 +252,8 @@ __device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, int64_t b) {
 // Up to SORT_ONE tokens (what its registers hold; 8000 tokens, 50257 x 768: 38 us, and 62 by
 // the kernels above): all passes in the LDS of workgroup 0, and the segments.
 // Wave w's keys are a run of them, so ranks by wave are stable.  Meanwhile the
-// other workgroups fill the table with zeros: a sort of 8192 tokens takes one CU
-// 25 us, the rest of the chip as long for the 200 MB of a table.
+// other workgroups fill the table with zeros: a sort of 8000 tokens takes one CU 17 us
+// (ids of two digits; 27 of three), the rest of the chip 26 to 36 for the 200 MB of a table.
 template <class TO>
 __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedGradArgs a, int bits, uint32_t* keys_out, uint32_t* order_out) {
   constexpr int NW = 16, R = SORT_ONE / 1024;

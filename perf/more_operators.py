@@ -1,0 +1,484 @@
+"""The pieces between the layers and behind them, as cases that can be timed and checked.
+
+A language model whose matrices this library steps also has norms in front of its layers, a head with a loss over
+the whole vocabulary, and parameters that are no matrices of its blocks.  One case is one of:
+
+  head_loss    per-row cross entropy of a linear head, logits = x weight^T, over the vocabulary; no logits come back
+  head_step    the same losses with the gradients of sum(grad * losses) to x and weight
+  adamw        one AdamW step over many tensors at once, moments in 32 bits or in 8 with a scale a block
+  norm_step    root-mean-square norm of x + residual, its output and the sum, and its backward pass
+  norm_layer   serving: the norm with its output in 8 bits, into a linear layer on kept 8-bit weights
+
+A case is a dict of plain values; `rows`, `vocab`, `inner`, `outer`, `width`, `table`, `vectors` are sizes, the rest
+types and options.  A label outside the vocabulary stands for no label: its row has loss 0 and adds no gradient.
+
+The 8-bit form of a row's block of 128 values x: s = 2^e with the least e >= -127 for which max|x| <= 448 s (s = 1
+for a block of zeros), q = x / s rounded to the nearest 8-bit float (4 exponent and 3 mantissa bits, ties to even).
+
+The 8-bit form of a block of 256 moments: a float32 scale s = max|m| / 448 for the first, max v / 61440 for the
+second (0 for a block below 2^-100), and codes of a float with 3 mantissa bits: sign and 4 exponent bits (up to 448)
+for the first, 5 exponent bits and no sign (up to 61440) for the second.  x = |m| (448 / max|m|) lies between two
+neighbours a step apart and becomes floor(x / step + u) step; a second moment above zero never becomes zero.  u are
+the upper and lower 16 bits of a counter's hash: of seed, tensor, block and place.  A state's bytes are the codes of
+the first moment in whole blocks, those of the second, then the scales of either.
+"""
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"float32": torch.float32, "bfloat16": torch.bfloat16, "int32": torch.int32, "int64": torch.int64}
+F8_MAX = 448.0
+SECOND_MAX = 61440.0   # largest second-moment code
+BLOCK = 256            # moments that share a scale
+EPS = 1e-6
+
+
+def listed():
+    return [
+        # One token's loss under the widest of the three models' heads, as a scorer asks for it: the weights are read once.
+        dict(name="head_one_token", op="head_loss", rows=1, vocab=50257, inner=1280, x="bfloat16", weight="bfloat16",
+             labels="int64", ragged=False),
+        # Evaluation of a micro-batch of 8 x 1024 tokens.
+        dict(name="head_loss_micro_batch", op="head_loss", rows=8192, vocab=50257, inner=768, x="bfloat16",
+             weight="bfloat16", labels="int64", ragged=False),
+        # The training step's head on a micro-batch: losses and both gradients.
+        dict(name="head_step_micro_batch", op="head_step", rows=8192, vocab=50257, inner=1280, x="bfloat16",
+             weight="bfloat16", labels="int64", ragged=False),
+        # Everything in 32 bits, as the training loop runs without mixed precision; odd sizes, rows without label.
+        dict(name="head_step_ragged", op="head_step", rows=1001, vocab=50257, inner=901, x="float32", weight="float32",
+             labels="int32", ragged=True),
+        # The vectors of the smallest model (norms and biases): a hundred small tensors, latency counts.
+        dict(name="adamw_vectors", op="adamw", table=0, width=768, vectors=98, bits=32, param="float32", grad="float32",
+             step=10),
+        # All that is no block matrix in the widest: token table, positions, norms and biases.
+        dict(name="adamw_rest_of_model", op="adamw", table=50257, width=1280, vectors=290, bits=32, param="float32",
+             grad="float32", step=1000),
+        # The token table with its moments in 8 bits.
+        dict(name="adamw_table_8bit", op="adamw", table=50257, width=1280, vectors=0, bits=8, param="float32",
+             grad="float32", step=1000),
+        # An odd table in bfloat16, first step, moments in 8 bits, a few odd vectors.
+        dict(name="adamw_ragged_8bit", op="adamw", table=1501, width=901, vectors=3, bits=8, param="bfloat16",
+             grad="bfloat16", step=1),
+        # One generated token: residual added, normed, brought to 8 bits, through the attention's input matrix.
+        dict(name="norm_layer_one_token", op="norm_layer", rows=1, width=1280, outer=3840, x="bfloat16"),
+        # A prompt of 1024 tokens through the same.
+        dict(name="norm_layer_prompt", op="norm_layer", rows=1024, width=1280, outer=3840, x="bfloat16"),
+        # A micro-batch's norm in a training step.
+        dict(name="norm_step_micro_batch", op="norm_step", rows=8192, width=1280, x="bfloat16", weight="float32",
+             residual=True),
+        # Odd sizes in 32 bits, no residual.
+        dict(name="norm_step_ragged", op="norm_step", rows=1000, width=901, x="float32", weight="float32", residual=False),
+    ]
+
+
+def _cost(c):
+    w = work(c)
+    return w["bytes"] + w["flops"] / 300
+
+
+def _most(op):
+    return max(_cost(c) for c in listed() if c["op"] == op)
+
+
+def draw(rng):
+    """Sizes log-uniform over the ranges, odd ones as they fall, none dearer than the dearest listed of its kind."""
+    def size(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    op = rng.choice(["head_loss", "head_step", "adamw", "norm_step", "norm_layer"])
+    while True:
+        if op.startswith("head"):
+            x, weight = rng.choice([("float32", "float32"), ("bfloat16", "bfloat16"), ("bfloat16", "float32")])
+            c = dict(op=op, rows=size(1, 8192), vocab=size(128, 131072), inner=size(16, 4096), x=x, weight=weight,
+                     labels=rng.choice(["int32", "int64"]), ragged=rng.random() < 0.5)
+        elif op == "adamw":
+            bits = rng.choice([8, 32])
+            c = dict(op=op, table=rng.choice([0, size(1, 131072)]), width=size(1, 4096),
+                     vectors=size(1, 300 if bits == 32 else 50), bits=bits, param=rng.choice(["float32", "bfloat16"]), step=size(1, 100000))
+            c["grad"] = c["param"] if rng.random() < 0.5 else "float32"
+        elif op == "norm_step":
+            c = dict(op=op, rows=size(1, 65536), width=size(16, 8192), x=rng.choice(["float32", "bfloat16"]),
+                     weight=rng.choice(["float32", "bfloat16"]), residual=rng.random() < 0.5)
+        else:
+            c = dict(op=op, rows=size(1, 4096), width=size(16, 8192), outer=size(16, 8192),
+                     x=rng.choice(["float32", "bfloat16"]))
+        if _cost(c) <= _most(op) and (op != "head_step" or c["x"] == "bfloat16" or _cost(c) <= _most(op) / 6):
+            return c
+
+
+def _bytes(name):
+    return {"float32": 4, "bfloat16": 2, "int32": 4, "int64": 8}[name]
+
+
+def _sizes(c):
+    """Elements of each tensor of an adamw case: the table, a table of positions beside it, vectors of both layers' widths."""
+    head = [(c["table"], c["width"]), (min(1024, c["table"]), c["width"])] if c["table"] else []
+    return head + [((4 * c["width"] if i % 8 == 5 else c["width"]),) for i in range(c["vectors"])]
+
+
+def work(case):
+    c = case
+    if c["op"].startswith("head"):
+        m, v, k = c["rows"], c["vocab"], c["inner"]
+        step = c["op"] == "head_step"
+        moved = m * k * _bytes(c["x"]) + v * k * _bytes(c["weight"])
+        return {"bytes": moved * (2 if step else 1) + m * (_bytes(c["labels"]) + 4 + 4 * step),
+                "flops": 2 * m * v * k * (3 if step else 1)}
+    if c["op"] == "adamw":
+        n = sum(math.prod(s) for s in _sizes(c))
+        moments = 16 if c["bits"] == 32 else 4 + 8   # in 8 bits they come back as the values they stand for, too
+        return {"bytes": n * (2 * _bytes(c["param"]) + _bytes(c["grad"]) + moments), "flops": 15 * n}
+    n, s = c["rows"] * c["width"], _bytes(c["x"])
+    if c["op"] == "norm_step":   # x (and residual) in, y (and the sum) out; dy (and the sum's) in, dx out, x or the sum in
+        return {"bytes": n * s * (8 if c["residual"] else 5) + 2 * c["width"] * _bytes(c["weight"]), "flops": 16 * n}
+    return {"bytes": 3 * n * s + c["width"] * (4 + c["outer"]) + c["rows"] * c["outer"] * 2,
+            "flops": 2 * n * c["outer"] + 6 * n}
+
+
+def _generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _normal(g, shape, scale=1.0):
+    return torch.randn(shape, device="cuda", generator=g) * scale
+
+
+def _in_one(tensors):
+    """The tensors as views of one buffer, each from a multiple of 64 elements, and that buffer."""
+    flat = torch.cat([torch.nn.functional.pad(t.flatten(), (0, -t.numel() % 64)) for t in tensors])
+    starts = [0]
+    for t in tensors:
+        starts.append(starts[-1] + t.numel() + -t.numel() % 64)
+    return [flat[a:a + t.numel()].view(t.shape) for a, t in zip(starts, tensors)], flat
+
+
+def _activations(g, shape):
+    """Normal values with channels of unequal scale, a few of them large, and rows of padding (zeros)."""
+    x = _normal(g, shape)
+    x *= torch.exp(0.5 * _normal(g, (1, shape[1])))
+    x *= torch.where(torch.rand((1, shape[1]), device="cuda", generator=g) < 0.01, 20.0, 1.0)
+    x[torch.rand(shape[0], device="cuda", generator=g) < 0.02] = 0.0
+    return x
+
+
+def prepare(case, seed):
+    c, g = case, _generator(seed)
+    s = dict(case=dict(c))
+    if c["op"].startswith("head"):
+        m, v, k = c["rows"], c["vocab"], c["inner"]
+        w = _normal(g, (v, k), 2.0 / math.sqrt(k))
+        # Labels as text has them: frequency falls as 1 / rank.  The states lean towards their labels' rows, some of
+        # them far enough that the model is sure.
+        u = torch.rand(m, device="cuda", generator=g, dtype=torch.float64)
+        labels = (torch.exp(u * math.log(v + 1)).long() - 1).clamp_(0, v - 1)
+        lean = 4.0 * torch.rand((m, 1), device="cuda", generator=g)
+        s["x"] = (_normal(g, (m, k)) + lean * w[labels]).to(DTYPES[c["x"]])
+        if c["ragged"]:
+            labels[torch.rand(m, device="cuda", generator=g) < 0.25] = -100
+        s["w"] = w.to(DTYPES[c["weight"]])
+        s["labels"] = labels.to(DTYPES[c["labels"]])
+        s["weight"] = torch.full((m,), 1.0 / m, device="cuda")
+        if c["ragged"]:
+            s["weight"] *= torch.rand(m, device="cuda", generator=g) + 0.5
+    elif c["op"] == "adamw":
+        shapes = _sizes(c)
+        s["params"], s["flat"] = _in_one([_normal(g, n, 0.02).to(DTYPES[c["param"]]) for n in shapes])
+        # Gradients of rows that were met and rows that were not; moments as a run leaves them.
+        s["grads"] = [(_normal(g, n, 1e-3) * (torch.rand(n[:1], device="cuda", generator=g) < 0.7).reshape(
+            (-1,) + (1,) * (len(n) - 1))).to(DTYPES[c["grad"]]) for n in shapes]
+        s["seed"] = int(torch.randint(0, 1 << 62, (1,), generator=torch.Generator().manual_seed(seed)))
+        first = c["step"] == 1
+        moments = [(torch.zeros(n, device="cuda") if first else _normal(g, n, 3e-4),
+                    torch.zeros(n, device="cuda") if first else 1e-6 * torch.exp(_normal(g, n))) for n in shapes]
+        if c["bits"] == 32:
+            s["states"], s["flat_states"] = _in_one([torch.stack([a.flatten(), b.flatten()]) for a, b in moments])
+        else:
+            s["states"] = [_encoded(a.flatten(), b.flatten(), 1, i) for i, (a, b) in enumerate(moments)]
+    else:
+        n, k = c["rows"], c["width"]
+        s["x"] = _activations(g, (n, k)).to(DTYPES[c["x"]])
+        s["residual"] = _normal(g, (n, k), 2.0).to(DTYPES[c["x"]]) if c.get("residual", True) else None
+        w = 1.0 + _normal(g, (k,), 0.2)
+        if c["op"] == "norm_step":
+            s["w"] = w.to(DTYPES[c["weight"]])
+            s["dy"] = (_normal(g, (n, k)) * torch.exp(_normal(g, (n, 1))) * 1e-3).to(DTYPES[c["x"]])
+            s["dh"] = _normal(g, (n, k), 1e-3).to(DTYPES[c["x"]]) if c["residual"] else None
+            for t in ("x", "residual", "w"):
+                if s[t] is not None:
+                    s[t].requires_grad_()
+        else:
+            s["w"] = w
+            # Weights as a program keeps them: 8-bit rows padded to whole blocks, a scale's exponent for each block.
+            b = _blocks(_normal(g, (c["outer"], k), 0.02), 128, 128)
+            e = _exponents(b.abs().amax((1, 3)))
+            q = (b * torch.exp2(-e.float())[:, None, :, None]).reshape(-1, b.shape[2] * 128)[:c["outer"]]
+            s["w_values"] = q.to(torch.float8_e4m3fn).contiguous()
+            s["w_scales"] = (e + 127).to(torch.uint8)
+    return s
+
+
+# ------------------------------------------------------------------ plain forms
+
+def _blocks(x, rows, cols):
+    """x, padded with zeros to whole blocks, as (row blocks, rows, column blocks, cols)."""
+    x = torch.nn.functional.pad(x, (0, -x.shape[1] % cols, 0, -x.shape[0] % rows))
+    return x.reshape(x.shape[0] // rows, rows, x.shape[1] // cols, cols)
+
+
+def _exponents(amax):
+    """The least e with amax <= 448 * 2^e, not below -127; 0 for amax = 0."""
+    m, e = torch.frexp(amax)
+    e = torch.where(m > F8_MAX / 512, e - 8, e - 9).clamp_min(-127)
+    return torch.where(amax == 0, 0, e)
+
+
+def _rounded(x):
+    """What the 8-bit form of x with a scale for each row and 128 values stands for, in 32 bits."""
+    b = _blocks(x, 1, 128)
+    e = _exponents(b.abs().amax((1, 3), keepdim=True)).float()
+    q = (b * torch.exp2(-e)).to(torch.float8_e4m3fn).float() * torch.exp2(e)
+    return q.reshape(b.shape[0], -1)[:, :x.shape[1]]
+
+
+def _mixed(x):
+    """A hash of 32-bit numbers (held in 64 bits): shifts, and products with odd numbers from the digits of the golden
+    ratio and of the root of 3."""
+    x = x ^ (x >> 16)
+    x = (x * 0x9E3779B1) & 0xFFFFFFFF
+    x = x ^ (x >> 15)
+    x = (x * 0xBB67AE85) & 0xFFFFFFFF
+    return x ^ (x >> 16)
+
+
+def _noise(seed, tensor, blocks):
+    """Two numbers in (0, 1), multiples of 2^-17, for each place of each block of a tensor."""
+    key = _mixed((seed & 0xFFFFFFFF) ^ _mixed(((seed >> 32) + 0x9E3779B1 * (tensor + 1)) & 0xFFFFFFFF))
+    b = torch.arange(blocks, device="cuda")[:, None]
+    r = _mixed(_mixed((key + b * 0x9E3779B1) & 0xFFFFFFFF) ^ torch.arange(BLOCK, device="cuda"))
+    return ((r & 0xFFFF) + 0.5) / 65536, ((r >> 16) + 0.5) / 65536
+
+
+def _codes(x, least, u):
+    """x >= 0 to one of its two neighbours with 3 mantissa bits, exponents from `least`: floor(x / step + u) step."""
+    e = (torch.frexp(x).exponent - 1).clamp_min(least)
+    step = torch.ldexp(torch.ones_like(x), e - 3)
+    return torch.floor(x / step + u) * step, step
+
+
+def _encoded(m, v, seed, tensor):
+    """A state's bytes from its moments."""
+    n = m.numel()
+    m, v = (torch.nn.functional.pad(t, (0, -n % BLOCK)).reshape(-1, BLOCK) for t in (m, v))
+    um, uv = _noise(seed, tensor, m.shape[0])
+    am, av = m.abs().amax(1, keepdim=True), v.amax(1, keepdim=True)
+    some_m, some_v = am >= 2.0 ** -100, av >= 2.0 ** -100
+    rm, _ = _codes((m.abs() * (F8_MAX / torch.where(some_m, am, 1.0))).clamp_max(F8_MAX), -6, um.float())
+    rv, step = _codes((v * (SECOND_MAX / torch.where(some_v, av, 1.0))).clamp_max(SECOND_MAX), -14, uv.float())
+    rv = torch.where(v > 0, torch.maximum(rv, step), rv)
+    cm = torch.where(some_m, torch.copysign(rm, m), 0.0).to(torch.float8_e4m3fn).view(torch.uint8)
+    cv = (torch.where(some_v, rv, 0.0).half().view(torch.int16) >> 7).to(torch.uint8)
+    scales = [torch.where(some_m, am / F8_MAX, 0.0), torch.where(some_v, av / SECOND_MAX, 0.0)]
+    return torch.cat([cm.flatten(), cv.flatten()] + [t.flatten().view(torch.uint8) for t in scales])
+
+
+def _decoded(state, n):
+    """The moments that a state's bytes stand for."""
+    blocks = state.numel() // (2 * BLOCK + 8)
+    codes, scales = state[:2 * BLOCK * blocks].reshape(2, blocks, BLOCK), state[2 * BLOCK * blocks:].view(torch.float32)
+    m = codes[0].view(torch.float8_e4m3fn).float() * scales[:blocks, None]
+    v = (codes[1].to(torch.int16) << 7).view(torch.float16).float() * scales[blocks:, None]
+    return m.flatten()[:n], v.flatten()[:n]
+
+
+LR, BETA1, BETA2, ADAM_EPS, DECAY = 6e-4, 0.9, 0.95, 1e-8, 0.1
+
+
+def _plain_adamw(s):
+    c = s["case"]
+    params = [p.flatten().float() for p in s["params"]]
+    grads = [g.flatten().float() for g in s["grads"]]
+    if c["bits"] == 32:
+        moments = [list(st) for st in s["states"]]
+    else:
+        moments = [_decoded(st, p.numel()) for st, p in zip(s["states"], params)]
+    m, v = ([a[i] for a in moments] for i in (0, 1))
+    m = torch._foreach_add(torch._foreach_mul(m, BETA1), torch._foreach_mul(grads, 1 - BETA1))
+    v = torch._foreach_add(torch._foreach_mul(v, BETA2), torch._foreach_mul(torch._foreach_mul(grads, 1 - BETA2), grads))
+    # p <- p (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+    denom = torch._foreach_div(torch._foreach_sqrt(v), math.sqrt(1 - BETA2 ** c["step"]))
+    update = torch._foreach_div(torch._foreach_mul(m, LR / (1 - BETA1 ** c["step"])), torch._foreach_add(denom, ADAM_EPS))
+    params = torch._foreach_sub(torch._foreach_mul(params, 1 - LR * DECAY), update)
+    torch._foreach_copy_([p.view(-1) for p in s["params"]], params)
+    if c["bits"] == 32:
+        torch._foreach_copy_([st[0] for st in s["states"]], m)
+        torch._foreach_copy_([st[1] for st in s["states"]], v)
+        return s["flat"], s["flat_states"]
+    torch._foreach_copy_(s["states"], [_encoded(a, b, s["seed"], i) for i, (a, b) in enumerate(zip(m, v))])
+    return s["flat"], [torch.stack(_decoded(st, p.numel())) for st, p in zip(s["states"], s["params"])]
+
+
+def _plain_head(s):
+    c = s["case"]
+    x, w = s["x"].float(), s["w"].float()
+    there = (s["labels"] >= 0) & (s["labels"] < c["vocab"])
+    y = s["labels"].long().clamp(0, c["vocab"] - 1)[:, None]
+    z = x @ w.t()
+    z = z - z.amax(1, keepdim=True)
+    at_label = z.gather(1, y)[:, 0]
+    e = torch.exp(z)
+    total = e.sum(1)
+    losses = torch.where(there, torch.log(total) - at_label, 0.0)
+    if c["op"] == "head_loss":
+        return losses
+    weight = torch.where(there, s["weight"], 0.0)
+    d = e / total[:, None]
+    # At the label 1 - q is the sum of the others: where the model is sure, 1 - q by subtraction has few bits left.
+    others = e.scatter(1, y, 0.0).sum(1)
+    d = d.scatter(1, y, (-others / total)[:, None]) * weight[:, None]
+    return losses, (d @ w).to(s["x"].dtype), (d.t() @ x).to(s["w"].dtype)
+
+
+def _plain_norm(s):
+    """The sum (rounded to its type), 1 / rms (from 64-bit sums of squares, since the 8-bit form has borders next to
+    which a last bit decides) and the normed rows, in 32 bits."""
+    h = s["x"].detach()
+    if s["residual"] is not None:
+        h = (h.float() + s["residual"].detach().float()).to(h.dtype)
+    r = (1.0 / torch.sqrt(h.double().square().mean(1, keepdim=True) + EPS)).float()
+    return h, r, h.float() * r
+
+
+def _plain(s):
+    c = s["case"]
+    if c["op"].startswith("head"):
+        return _plain_head(s)
+    if c["op"] == "adamw":
+        return _plain_adamw(s)
+    h, r, n = _plain_norm(s)
+    w = s["w"].detach().float()
+    if c["op"] == "norm_layer":
+        scale = torch.exp2(s["w_scales"].float() - 127)
+        wide = (s["w_values"].float().reshape(c["outer"], -1, 128)
+                * scale.repeat_interleave(128, 0)[:c["outer"], :, None]).reshape(c["outer"], -1)[:, :c["width"]]
+        return (_rounded(n * w) @ wide.t()).to(torch.bfloat16), h
+    dy = s["dy"].float()
+    dn = dy * w
+    dx = r * (dn - n * (dn * n).mean(1, keepdim=True))
+    dw = (dy * n).sum(0)
+    if not c["residual"]:
+        return (n * w).to(h.dtype), dx.to(h.dtype), dw.to(s["w"].dtype)
+    dx = (dx + s["dh"].float()).to(h.dtype)
+    return (n * w).to(h.dtype), h, dx, dx, dw.to(s["w"].dtype)
+
+
+def run(state):
+    s, c = state, state["case"]
+    if not own:
+        return _plain(s)
+    from paper_2608_05088_amd import ops
+    if c["op"] == "head_loss":
+        return ops.linear_cross_entropy(s["x"], s["w"], s["labels"])
+    if c["op"] == "head_step":
+        return ops.linear_cross_entropy_step(s["x"], s["w"], s["labels"], grad=s["weight"])
+    if c["op"] == "adamw":
+        ops.adamw_step(s["params"], s["grads"], s["states"], lr=LR, betas=(BETA1, BETA2), eps=ADAM_EPS,
+                       weight_decay=DECAY, step=c["step"], seed=s["seed"])
+        return s["flat"], s["flat_states"] if c["bits"] == 32 else ops.adamw_moments(s["params"], s["states"])
+    if c["op"] == "norm_layer":
+        rows, h = ops.rms_norm_fp8(s["x"], s["w"], residual=s["residual"], eps=EPS)
+        return ops.fp8_forward(rows, s["w_values"], s["w_scales"], out_dtype=torch.bfloat16), h
+    if not c["residual"]:
+        y = ops.rms_norm(s["x"], s["w"], eps=EPS)
+        return (y.detach(), *torch.autograd.grad(y, (s["x"], s["w"]), s["dy"]))
+    y, h = ops.rms_norm(s["x"], s["w"], residual=s["residual"], eps=EPS)
+    dx, dr, dw = torch.autograd.grad((y, h), (s["x"], s["residual"], s["w"]), (s["dy"], s["dh"]))
+    return y.detach(), h.detach(), dx, dr, dw
+
+
+# ------------------------------------------------------------------ 64 bits
+
+def _two_to(e):
+    """2^e in 64 bits, exactly (pow on the GPU is not)."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
+def _exact_rounded(x):
+    """The 8-bit form of rows from its definition, in 64 bits: e by logarithm, q by the spacing of its binade."""
+    out = torch.zeros_like(x)
+    for j in range(0, x.shape[1], 128):
+        b = x[:, j:j + 128]
+        largest = b.abs().amax(1, keepdim=True)
+        largest = torch.where(largest > 0, largest, F8_MAX)
+        e = torch.ceil(torch.log2(largest / F8_MAX))
+        e = e - (largest <= F8_MAX * _two_to(e - 1)).double()   # where the logarithm was rounded past a whole number
+        e = e + (largest > F8_MAX * _two_to(e)).double()
+        unit = _two_to(e.clamp(min=-127))
+        step = _two_to(torch.frexp((b / unit).abs().clamp(min=2.0 ** -6)).exponent - 4)
+        out[:, j:j + 128] = torch.round(b / unit / step) * step * unit
+    return out
+
+
+def _exact_head(c, s):
+    w, n = s["w"].double(), c["rows"]
+    wt = w.t().contiguous()
+    losses, dx, dw = [], [], torch.zeros_like(w)
+    for r in range(0, n, 1024):
+        x, labels = s["x"][r:r + 1024].double(), s["labels"][r:r + 1024].long()
+        logp = torch.log_softmax(x @ wt, 1)
+        hot = torch.zeros_like(logp)
+        rows = torch.nonzero(labels >= 0)[:, 0]
+        hot[rows, labels[rows]] = 1.0
+        losses.append(-(hot * logp).sum(1))
+        if c["op"] == "head_step":
+            d = torch.exp(logp) - hot
+            # e^a - 1 at the label
+            d[rows, labels[rows]] = torch.expm1(logp[rows, labels[rows]])
+            d *= torch.where(labels >= 0, s["weight"][r:r + 1024], 0.0).double()[:, None]
+            dx.append(d @ w)
+            dw += d.t().contiguous() @ x
+    return torch.cat(losses) if c["op"] == "head_loss" else (torch.cat(losses), torch.cat(dx), dw)
+
+
+def exact(case, seed):
+    c = case
+    s = prepare(case, seed)
+    if c["op"].startswith("head"):
+        return _exact_head(c, s)
+    if c["op"] == "adamw":
+        params, states = [], []
+        for p, g, st in zip(s["params"], s["grads"], s["states"]):
+            if c["bits"] == 32:
+                m, v = st.double()
+            else:
+                m, v = (t.double() for t in _decoded(st, p.numel()))
+            g = g.double().flatten()
+            m, v = BETA1 * m + (1 - BETA1) * g, BETA2 * v + (1 - BETA2) * g * g
+            hat_m, hat_v = m / (1 - BETA1 ** c["step"]), v / (1 - BETA2 ** c["step"])
+            q = p.double().flatten() * (1 - LR * DECAY) - LR * hat_m / (hat_v.sqrt() + ADAM_EPS)
+            params.append(q.reshape(p.shape))
+            # Which of two neighbours an 8-bit moment becomes is decided by the last bits of 32.
+            states.append(torch.stack([m, v]) if c["bits"] == 32 else None)
+        return _in_one(params)[1], _in_one(states)[1] if c["bits"] == 32 else states
+    x = s["x"].detach().double()
+    if s["residual"] is not None:
+        x = (x + s["residual"].detach().double()).to(s["x"].dtype).double()   # the sum is what its type holds
+    rms = torch.sqrt((x * x).mean(1, keepdim=True) + EPS)
+    n, w = x / rms, s["w"].detach().double()
+    if c["op"] == "norm_layer":
+        e = s["w_scales"].double() - 127
+        wide = s["w_values"].double()
+        for j in range(e.shape[1]):
+            wide[:, 128 * j:128 * (j + 1)] *= _two_to(e[:, j]).repeat_interleave(128)[:c["outer"], None]
+        return _exact_rounded(n * w) @ wide[:, :c["width"]].t().contiguous(), x
+    dy = s["dy"].double()
+    dn = dy * w
+    dx = (dn - n * (dn * n).sum(1, keepdim=True) / c["width"]) / rms
+    dw = (dy * n).sum(0)
+    if not c["residual"]:
+        return n * w, dx, dw
+    dx = dx + s["dh"].double()
+    return n * w, x, dx, dx, dw

@@ -17,8 +17,9 @@ for a block of zeros), q = x / s rounded to the nearest 8-bit float (4 exponent 
 
 The 8-bit form of a block of 256 moments: a float32 scale s = max|m| / 448 for the first, max v / 61440 for the
 second (0 for a block below 2^-100), and codes of a float with 3 mantissa bits: sign and 4 exponent bits (up to 448)
-for the first, 5 exponent bits and no sign (up to 61440) for the second.  x = |m| (448 / max|m|) lies between two
-neighbours a step apart and becomes floor(x / step + u) step; a second moment above zero never becomes zero.  u are
+for the first, 5 exponent bits and no sign (up to 61440) for the second.  x = |m| (1 / max|m|) 448 lies between two
+neighbours a step apart and becomes floor(x / step + u) step; a second moment above zero never becomes zero.  Every
+step of this is rounded to 32 bits, the moments' own products and sums too, so that codes are the same everywhere.  u are
 the upper and lower 16 bits of a counter's hash: of seed, tensor, block and place.  A state's bytes are the codes of
 the first moment in whole blocks, those of the second, then the scales of either.
 """
@@ -276,12 +277,12 @@ def _encoded(m, v, seed, tensor):
     um, uv = _noise(seed, tensor, m.shape[0])
     am, av = m.abs().amax(1, keepdim=True), v.amax(1, keepdim=True)
     some_m, some_v = am >= 2.0 ** -100, av >= 2.0 ** -100
-    rm, _ = _codes((m.abs() * (F8_MAX / torch.where(some_m, am, 1.0))).clamp_max(F8_MAX), -6, um.float())
-    rv, step = _codes((v * (SECOND_MAX / torch.where(some_v, av, 1.0))).clamp_max(SECOND_MAX), -14, uv.float())
+    rm, _ = _codes((m.abs() * (torch.where(some_m, am, 1.0).reciprocal() * F8_MAX)).clamp_max(F8_MAX), -6, um)
+    rv, step = _codes((v * (torch.where(some_v, av, 1.0).reciprocal() * SECOND_MAX)).clamp_max(SECOND_MAX), -14, uv)
     rv = torch.where(v > 0, torch.maximum(rv, step), rv)
     cm = torch.where(some_m, torch.copysign(rm, m), 0.0).to(torch.float8_e4m3fn).view(torch.uint8)
     cv = (torch.where(some_v, rv, 0.0).half().view(torch.int16) >> 7).to(torch.uint8)
-    scales = [torch.where(some_m, am / F8_MAX, 0.0), torch.where(some_v, av / SECOND_MAX, 0.0)]
+    scales = [torch.where(some_m, am * (1 / F8_MAX), 0.0), torch.where(some_v, av * (1 / SECOND_MAX), 0.0)]
     return torch.cat([cm.flatten(), cv.flatten()] + [t.flatten().view(torch.uint8) for t in scales])
 
 

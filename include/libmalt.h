@@ -451,6 +451,158 @@ malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, in
                                         malt_dtype_t dx_type, int64_t lddx, void* dw, malt_dtype_t dw_type, int64_t lddw,
                                         int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Cross entropy of a linear head over a large vocabulary, and its gradients, without
+ * keeping the logits.  For row r of x (rows x inner), weight (vocab x inner), label y:
+ *   z = x[r] weight^T,  losses[r] = log sum_v exp z_v - z_y,
+ *   dx = sum over v of d_v weight[v],  dweight = (accumulate ? dweight : 0) + sum over r of d x[r],
+ *   d = weight_r (softmax(z) - 1_y):  the gradients of sum_r weight_r losses[r].
+ *  - A label outside [0, vocab) is no label: the row's loss and gradient are zero whatever the
+ *    row holds.  A row of weight 0 has a zero gradient.  (A weight row that is not finite makes
+ *    every row's loss no number, as the definition does.)
+ *  - Logits of -inf have probability zero; a labelled row without a finite logit is NaN, as are
+ *    rows with a NaN or +inf.
+ *  - Products of bfloat16 are exact and summed in float32.  float32 values enter products as
+ *    three bfloat16 numbers whose sum they are; of their nine products the six above 2^-26 are
+ *    taken, in float32.  Softmax and losses are float32.  1 - q_y is formed from the other
+ *    columns' sum.  Gradients of type float32 take d, x and weight whole; bfloat16 ones take
+ *    d, x and weight rounded to bfloat16, which puts them off by about as much as their own
+ *    rounding.
+ * losses, dx, dweight may be NULL (not wanted).  stats: rows x 4 float32, 16-byte aligned, what
+ * the gradients need of the first pass: written, or, with stats_given, read from an earlier call
+ * on the same x, weight and labels (losses is NULL then); NULL: kept in the workspace.
+ * weights: float32, one every weight_stride elements (0: one for all rows), or NULL for the
+ * scalar weight_value.
+ * workspace: device memory of malt_linear_loss_size's bytes for the same arguments, 256-byte
+ * aligned, of no meaning before or after the call.  It holds d for a piece of the vocabulary at a
+ * time, at most 512 MiB (a tile's 256 columns at the least), x and, where it is float32
+ * or not laid out for whole 16-byte loads, the weight in bfloat16.
+ * Limits: rows <= 65536, 1 <= inner <= 65536, 1 <= vocab <= 2^25, vocab * inner <= 2^33,
+ * rows * vocab <= 2^38 (rounded up to 2048 and 1024). */
+typedef struct {
+  const void* x;             /* rows x inner, type x_type (dx's too) */
+  malt_dtype_t x_type;
+  int64_t rows, inner, ldx;
+  const void* weight;        /* vocab x inner */
+  malt_dtype_t weight_type;
+  int64_t vocab, ldw;
+  const void* labels;        /* rows, one every label_stride elements */
+  malt_index_t label_type;
+  int64_t label_stride;
+  const float* weights;
+  int64_t weight_stride;
+  float weight_value;
+  float* losses;
+  float* stats;
+  int32_t stats_given;
+  void* dx;
+  int64_t lddx;
+  void* dweight;             /* vocab x inner */
+  malt_dtype_t dweight_type;
+  int64_t lddw;
+  int32_t accumulate;
+} malt_linear_loss_t;
+malt_status_t malt_linear_loss_size(const malt_linear_loss_t* args, size_t* workspace_bytes);
+malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One AdamW step over many tensors:
+ *   g = c grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * in float32, p rounded once to its type; c = grad_scale, times *grad_scale_at if that is not NULL
+ * (read on the device).  A tensor's elements are contiguous; its moments lie in `state`,
+ * malt_adamw_state_size's bytes, 4-byte aligned, zeros before the first step:
+ *  - state_bits 32: float32 m[numel], then v[numel];
+ *  - state_bits 8: for each 256 elements a block: codes of m [blocks][256] (bytes), codes of v,
+ *    scales of m [blocks] (float32), scales of v.  A moment is its code's value times its
+ *    block's scale.  m's codes: sign, 4 exponent bits (bias 7), 3 mantissa bits; v's: 5 exponent bits (bias 15),
+ *    3 mantissa bits, no sign.  Scales are the block's largest magnitude times 1/448 and 1/61440
+ *    (0 for a block below 2^-100, not a number where the block holds an infinity or a NaN).  A magnitude x =
+ *    |m| (1 / largest) 448 between two neighbours a step apart becomes floor(x / step + u) step, a
+ *    v above zero at least one step.  u in (0, 1) is a hash of seed, the tensor's place in the
+ *    call, the block and the element's place in it: equal calls give equal bits, and another seed for each
+ *    step keeps sums over steps right on average.  The step itself uses m and v unrounded.
+ * Each of m's and v's products and sums is rounded to float32.
+ * No written buffer may overlap another (a tensor named twice is refused).  A captured call
+ * keeps its arguments, step and seed among them.  numel <= 2^35.
+ * malt_adamw_moments writes what 8-bit states stand for: float32 m[numel], then v[numel]. */
+typedef struct {
+  int32_t count;
+  const int64_t* numel;
+  void* const* params;
+  const uint8_t* param_types;   /* malt_dtype_t, a byte each */
+  const void* const* grads;
+  const uint8_t* grad_types;
+  void* const* states;
+  const uint8_t* state_bits;    /* 8 or 32 */
+} malt_adamw_tensors_t;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;                 /* from 1 */
+  double grad_scale;
+  const float* grad_scale_at;
+  uint64_t seed;
+} malt_adamw_t;
+malt_status_t malt_adamw_state_size(int64_t numel, int32_t bits, size_t* bytes);
+malt_status_t malt_adamw_step(const malt_adamw_tensors_t* tensors, const malt_adamw_t* args, void* stream);
+malt_status_t malt_adamw_moments(int32_t count, const int64_t* numel, const void* const* states, float* const* moments, void* stream);
+
+/* Root-mean-square norm of rows, with a residual's addition before it:
+ *   h = x + residual, rounded to their type (sum; x itself without residual),
+ *   r = 1 / sqrt(mean(h^2) + eps),  y = (h r) weight
+ * mean and root in float64, r rounded to float32 (rstd, if not NULL), products in float32, y
+ * rounded once.  The output is y (y_type) or an 8-bit operand (values, scales; malt_block_size's
+ * bytes, 16-byte aligned) for malt_block_matmul and malt_block_linear_operand.
+ * The gradients, n = h r:
+ *   dx = r (dy weight - n mean(dy weight n)) + dsum   (of x and of residual alike)
+ *   dweight = sum over rows of dy n
+ * dsum (the gradient that reaches h itself), dx and dweight may be NULL.  Sums are float32 in an
+ * order fixed by the sizes.  workspace: malt_rms_norm_grad_size's bytes, 256-byte aligned.
+ * Limits: rows <= 2^21, 1 <= width <= 16384. */
+typedef struct {
+  const void* x;
+  malt_dtype_t type;            /* of x, residual and sum */
+  int64_t rows, width, ldx;
+  const void* residual;
+  int64_t ldr;
+  const void* weight;           /* width */
+  malt_dtype_t weight_type;
+  double eps;
+  void* sum;
+  int64_t lds;
+  void* y;
+  malt_dtype_t y_type;
+  int64_t ldy;
+  void* values;
+  void* scales;
+  float* rstd;
+} malt_rms_norm_t;
+malt_status_t malt_rms_norm(const malt_rms_norm_t* args, void* stream);
+typedef struct {
+  const void* h;
+  malt_dtype_t type;            /* of h, dsum and dx */
+  int64_t rows, width, ldh;
+  const void* weight;
+  malt_dtype_t weight_type;     /* of dweight too */
+  const float* rstd;
+  const void* dy;
+  malt_dtype_t dy_type;
+  int64_t lddy;
+  const void* dsum;
+  int64_t ldds;
+  void* dx;
+  int64_t lddx;
+  void* dweight;
+} malt_rms_norm_grad_t;
+malt_status_t malt_rms_norm_grad_size(int64_t rows, int64_t width, int32_t need_dweight, size_t* workspace_bytes);
+malt_status_t malt_rms_norm_grad(const malt_rms_norm_grad_t* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/* malt_block_linear on an input that is an 8-bit operand already (malt_rms_norm's or
+ * malt_block_quantize's values and scales, m rows over k values).  The workspace is that of
+ * malt_block_matmul (malt_block_matmul_size; not used for up to 32 rows). */
+malt_status_t malt_block_linear_operand(const void* x_values, const void* x_scales, int64_t m, int64_t k,
+                                        const void* w_values, const void* w_scales, int64_t n, void* out,
+                                        malt_dtype_t out_type, int64_t ldo, void* workspace, size_t workspace_bytes,
+                                        void* stream);
+
 const char* malt_status_string(malt_status_t status);
 const char* malt_last_error(void);
 const char* malt_version(void);

@@ -18,7 +18,7 @@ CALIB = os.path.join(PKG, "calib")
 CALIB_LIB = os.path.join(PKG, "lib", "libmalt_calib.so")
 SOURCES = ["malt_api.hip", "elementwise.hip", "ns_sym.hip", "ns_update.hip", "ns_mid.hip", "small_ns.hip",
            "embed.hip", "distill.hip", "block_quant.hip", "block_matmul.hip", "block_linear.hip",
-           "ops_api.hip"]
+           "ops_api.hip", "adamw.hip", "norm.hip", "head.hip", "head_rows.hip", "model_api.hip"]
 ARCH = "gfx950"
 
 

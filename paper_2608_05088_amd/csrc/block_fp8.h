@@ -56,6 +56,7 @@ struct BlockLinearArgs {
   const uint8_t* w_scales;  // [n / 128][k / 128]
   void* out;
   int64_t ldo;
+  const uint8_t* x_scales;  // x is an operand's values (ldx = pad128(k)) with these scales; or null
 };
 hipError_t launch_block_linear(const BlockLinearArgs& g, bool x_f32, bool out_f32, hipStream_t s);
 

@@ -25,9 +25,10 @@ using ns::i32x4;
 
 constexpr int FEW_WAVES = 8;
 
+// T: x's type; uint8_t for an operand that is in 8 bits already.
 template <class T, int MB, int NB, class TO>
 __global__ __launch_bounds__(64 * FEW_WAVES) void block_linear_kernel(BlockLinearArgs g) {
-  constexpr bool WIDE = std::is_same<TO, float>::value;
+  constexpr bool WIDE = std::is_same<TO, float>::value, READY = std::is_same<T, uint8_t>::value;
   __shared__ f32x4 sums[FEW_WAVES][MB * NB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int KT = (int)((g.k + QB - 1) / QB);
@@ -43,7 +44,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void block_linear_kernel(BlockLinea
 #pragma unroll
   for (int a = 0; a < MB; ++a) {
     const int m = 16 * a + r;
-    x[a] = static_cast<const T*>(g.x) + (m < g.m ? m : g.m - 1) * g.ldx;
+    x[a] = static_cast<const T*>(g.x) + (m < g.m ? m : g.m - 1) * g.ldx + (READY ? k_lane : 0);
   }
   const uint8_t* const ws = g.w_scales + n0 / QB * KT;
 
@@ -63,23 +64,31 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void block_linear_kernel(BlockLinea
     const int sw = gptr(ws)[kt];   // 16 NB <= 64 columns lie in one block of the weight
 #pragma unroll
     for (int a = 0; a < MB; ++a) {
-      float v[4][8];
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        load8(x[a], kt * QB + k_lane + 8 * i, (int)g.k, v[i]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = umax(top, mag(v[i][j]));
-      }
-      top = umax(top, (uint32_t)__shfl_xor((int)top, 16, 64));
-      top = umax(top, (uint32_t)__shfl_xor((int)top, 32, 64));
-      const int sx = (int)scale_byte(top);
-      const float inv = scale_inverse((uint32_t)sx);
       i32x8 fx;
+      int sx;
+      if constexpr (READY) {
+        const MALT_GLOBAL i32x4* p = reinterpret_cast<const MALT_GLOBAL i32x4*>(gptr(x[a]) + (int64_t)kt * QB);
+        fx = __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        const int m = 16 * a + r;   // its scale, of the last row past the end
+        sx = gptr(g.x_scales)[(int64_t)kt * q_scale_rows(g.m) + q_scale_pos(m < g.m ? m : (int)g.m - 1)];
+      } else {
+        float v[4][8];
+        uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        fx[2 * i] = (int)pack4(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
-        fx[2 * i + 1] = (int)pack4(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
+        for (int i = 0; i < 4; ++i) {
+          load8(x[a], kt * QB + k_lane + 8 * i, (int)g.k, v[i]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) top = umax(top, mag(v[i][j]));
+        }
+        top = umax(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+        top = umax(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+        sx = (int)scale_byte(top);
+        const float inv = scale_inverse((uint32_t)sx);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          fx[2 * i] = (int)pack4(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
+          fx[2 * i + 1] = (int)pack4(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
+        }
       }
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
@@ -133,7 +142,9 @@ void few_typed(const BlockLinearArgs& g, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_block_linear(const BlockLinearArgs& g, bool x_f32, bool out_f32, hipStream_t s) {
-  if (x_f32 && out_f32) few_typed<float, float>(g, s);
+  if (g.x_scales && out_f32) few_typed<uint8_t, float>(g, s);
+  else if (g.x_scales) few_typed<uint8_t, bf16_t>(g, s);
+  else if (x_f32 && out_f32) few_typed<float, float>(g, s);
   else if (x_f32) few_typed<float, bf16_t>(g, s);
   else if (out_f32) few_typed<bf16_t, float>(g, s);
   else few_typed<bf16_t, bf16_t>(g, s);

@@ -1,0 +1,120 @@
+// Cross entropy of a linear head over a large vocabulary, and its gradients, without
+// the logits: arguments, layout of the workspace and launchers (head.hip,
+// head_rows.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "malt_internal.h"
+
+namespace malt {
+
+// A matrix as bf16 planes whose sum it is: one where it is bf16, three (high, middle, low
+// bits: exact) where it is float32.
+constexpr int HEAD_PLANES = 3;
+constexpr int HEAD_TILE = 256;   // output tile edge, and what rows are padded to
+constexpr int HEAD_BK = 64;      // contraction per stage, and what columns are padded to
+
+// A row's softmax after the first pass, in log2: probabilities are 2^(z log2 e - top) * inverse.
+struct HeadRow {
+  float top;       // log2 e times the row's largest logit but the label's
+  float inverse;   // 1 / sum over the vocabulary of 2^(z log2 e - top)
+  float others;    // 1 - the label's probability, from the others' sum
+  float unused;
+};
+
+// What decides about a row.
+struct HeadLabels {
+  const void* labels;
+  bool wide;
+  int64_t stride;
+  const float* weights;    // or null
+  int64_t weight_stride;
+};
+
+// One side of a product: planes of bf16 rows, one behind the other.
+struct HeadSide {
+  const uint16_t* p;
+  int64_t plane;   // elements from one plane to the next
+  int64_t ld;
+  int64_t rows;    // rows there are: further ones are not read
+  int32_t cols;    // columns there are (a multiple of 8)
+};
+
+// C = sum over pairs of planes of A B^T, over `k` values.
+struct HeadProduct {
+  HeadSide a, b;
+  int32_t m, n;              // output rows and columns there are
+  int64_t k;
+  int32_t pairs;
+  uint32_t pair_a, pair_b;   // a pair's planes, four bits each, the first in the lowest
+  int32_t tiles_m, tiles_n;
+};
+
+struct HeadLogits {
+  HeadProduct g;         // m rows, n vocabulary columns from `col0`
+  HeadLabels rows;
+  int64_t vocab, col0;
+  // first pass
+  malt_f32x2* partial;       // [m][tiles]: a tile's largest (log2) and sum without the label's column
+  float* at_label;       // [m]: log2 e times the label's logit
+  int32_t parts;         // tiles
+  // second pass
+  const HeadRow* stats;
+  uint16_t* dz;          // planes of [padded m][padded n]
+  int64_t dz_plane, dz_ld;
+  int32_t dz_planes;
+};
+
+struct HeadOut {
+  HeadProduct g;
+  void* out;
+  int64_t ldo;
+  float* partial;        // float32 sums of the pieces so far (dx), m x n; null: one piece
+  int32_t form;          // 0: dx (B as rows of the contraction), 1: dW (both sides)
+  bool f32, add_partial, write_partial, accumulate;
+  bool mask_rows;        // rows without label or weight are zero (dx)
+};
+struct HeadGrads {
+  HeadOut part[2];       // one launch: dx's tiles, then dW's
+  int32_t parts;
+  HeadLabels rows;
+  int64_t vocab;
+  float scale;
+  const float* scale_at; // or null
+};
+
+// Few rows, weights as they lie.
+constexpr int HEAD_FEW = 32;
+struct HeadFew {
+  const void* x;
+  const void* w;
+  int64_t ldx, ldw, vocab;
+  int32_t m, k, parts;
+  HeadLabels rows;
+  malt_f32x2* partial;
+  float* at_label;
+};
+int head_few_parts(int64_t vocab);
+
+struct HeadPack {
+  const void* x;
+  int64_t rows, cols, ld;
+  uint16_t* out;           // planes of [padded rows][padded cols]
+  int64_t plane, pitch, out_rows;
+  int32_t planes;
+  HeadLabels labels;       // rows without label become zeros; labels null: every row stays
+  int64_t vocab;
+};
+
+hipError_t launch_head_pack(const HeadPack& a, bool f32, hipStream_t s);
+hipError_t launch_head_clear(const HeadPack& a, hipStream_t s);
+hipError_t launch_head_few(const HeadFew& a, bool x_f32, bool w_f32, hipStream_t s);
+hipError_t launch_head_join(const HeadLabels& rows, int64_t m, int64_t vocab, const malt_f32x2* partial, int parts,
+                            const float* at_label, HeadRow* stats, float* losses, hipStream_t s);
+hipError_t launch_head_logits(const HeadLogits& a, bool second, hipStream_t s);
+hipError_t launch_head_grads(const HeadGrads& a, hipStream_t s);
+hipError_t head_setup();
+
+}  // namespace malt

@@ -1,0 +1,279 @@
+// Cross entropy of a linear head: everything but its tiled products (head.hip).
+//
+//   z = x W^T, loss = log sum_v exp z_v - z_y
+//
+// Statistics are kept without the label's column: with o = sum over v != y of exp z_v, 1 - q_y =
+// o / (o + exp z_y) has all its bits where the model is sure of the label and 1 - q_y by
+// subtraction would have none, and so has loss = log(1 + o / exp z_y).
+#include "head.h"
+#include "ns_common.h"
+#include "ops_common.h"
+
+namespace malt {
+
+namespace {
+
+using ns::bf16x8;
+using ns::f32x4;
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
+// A row's label, or -1: outside the vocabulary.
+__device__ __forceinline__ int64_t label_of(const HeadLabels& l, int64_t r, int64_t vocab) {
+  const int64_t y = load_id(l.labels, l.wide, r * l.stride);
+  return (uint64_t)y < (uint64_t)vocab ? y : -1;
+}
+
+// ---------------------------------------------------------------------- packing
+// Four columns a thread.
+template <class T>
+__global__ __launch_bounds__(256) void head_pack_kernel(HeadPack a) {
+  const int64_t per = a.pitch / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= a.out_rows * per) return;
+  const int64_t r = i / per, c = i % per * 4;
+  op_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (r < a.rows && (!a.labels.labels || label_of(a.labels, r, a.vocab) >= 0))
+    v = row_load4(static_cast<const T*>(a.x) + r * a.ld, c, a.cols);
+  uint16_t* out = a.out + r * a.pitch + c;
+  for (int p = 0; p < a.planes; ++p) {
+    const uint32_t lo = pack_bf16x2(v.x, v.y), hi = pack_bf16x2(v.z, v.w);
+    *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(out)) = op_u32x2{lo, hi};
+    // What is left is exact: its bits are those of v past the plane's.  An infinity leaves nothing.
+    const float h[4] = {bf16_lo(lo), bf16_hi(lo), bf16_lo(hi), bf16_hi(hi)};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = fabsf(h[j]) == __builtin_inff() ? 0.f : v[j] - h[j];
+    out += a.plane;
+  }
+}
+
+// Rows of weight 0 become zeros, after the losses were formed from them: their gradient is
+// zero whatever they hold.
+__global__ __launch_bounds__(256) void head_clear_kernel(HeadPack a) {
+  const int64_t r = blockIdx.x;
+  if (gptr(a.labels.weights)[r * a.labels.weight_stride] != 0.f) return;
+  for (int p = 0; p < a.planes; ++p)
+    for (int64_t c = 4 * threadIdx.x; c < a.pitch; c += 1024)
+      *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(a.out) + p * a.plane + r * a.pitch + c) = op_u32x2{0u, 0u};
+}
+
+// --------------------------------------------------------------------- few rows
+// Up to 32 rows of x: bound by reading the weights, once, as they lie.  A wave takes 16 rows of
+// the weight at a time over the whole contraction: a lane holds 32 values (bf16) or 16 of one
+// of them, neighbours, so that its loads are wide; the products' order of k is the same for both sides.
+template <class T>
+struct Few;
+template <>
+struct Few<bf16_t> {
+  static constexpr int PER = 32, K = 4 * PER;   // values a lane holds, contraction of a step
+  bf16x8 v[4];
+  __device__ __forceinline__ void load(const bf16_t* row, int k, int cols) {
+    if (k + PER <= cols) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const MALT_GLOBAL op_u32x4_any*>(gptr(row) + k + 8 * i));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        op_u32x4 q;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = k + 8 * i + 2 * j;
+          const uint32_t lo = c < cols ? gptr(row)[c] : 0, hi = c + 1 < cols ? gptr(row)[c + 1] : 0;
+          q[j] = lo | hi << 16;
+        }
+        v[i] = __builtin_bit_cast(bf16x8, q);
+      }
+    }
+  }
+  __device__ static __forceinline__ f32x4 mma(const Few& w, const Few& x, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[i], x.v[i], c, 0, 0, 0);
+    return c;
+  }
+};
+// float32, or bf16 widened to it beside a float32 weight.
+template <>
+struct Few<float> {
+  static constexpr int PER = 16, K = 4 * PER;
+  op_f32x4 v[4];
+  template <class S>
+  __device__ __forceinline__ void load(const S* row, int k, int cols) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = row_load4(row, k + 4 * i, cols);
+  }
+  __device__ static __forceinline__ f32x4 mma(const Few& w, const Few& x, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[i][j], x.v[i][j], c, 0, 0, 0);
+    return c;
+  }
+};
+
+constexpr int FEW_WAVES = 4, FEW_COLS = 16 * FEW_WAVES;
+
+template <class C, class X, class W, int MB>
+__global__ __launch_bounds__(64 * FEW_WAVES) void head_few_kernel(HeadFew a) {
+  __shared__ malt_f32x2 join[FEW_WAVES][MB * 16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * FEW_COLS + 16 * wave;
+  const int64_t n = n0 + r < a.vocab ? n0 + r : a.vocab - 1;   // past the end: not counted below
+  const W* const w = static_cast<const W*>(a.w) + n * a.ldw;
+  const X* x[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) {
+    const int m = 16 * b + r;
+    x[b] = static_cast<const X*>(a.x) + (m < a.m ? m : a.m - 1) * a.ldx;
+  }
+  f32x4 acc[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int k0 = 0; k0 < a.k; k0 += C::K) {
+    const int k = k0 + C::PER * g;
+    C fw, fx;
+    fw.load(w, k, a.k);
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+      fx.load(x[b], k, a.k);
+      acc[b] = C::mma(fw, fx, acc[b]);
+    }
+  }
+  // acc[b][e]: row 16 b + lane % 16, column n0 + 4 (lane / 16) + e.
+#pragma unroll
+  for (int b = 0; b < MB; ++b) {
+    const int m = 16 * b + r;
+    const int64_t y = m < a.m ? label_of(a.rows, m, a.vocab) : -1, c = n0 + 4 * g;
+    float top = -__builtin_inff(), sum = 0.f, z[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      z[e] = acc[b][e] * LOG2E;
+      if (c + e == y) gptr(a.at_label)[m] = z[e];
+      if (c + e == y || c + e >= a.vocab) z[e] = -__builtin_inff();
+      top = fmaxf(top, z[e]);
+    }
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float ref = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += exp2f(z[e] - ref);
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (g == 0) join[wave][m] = malt_f32x2{top, sum};
+  }
+  __syncthreads();
+  if (threadIdx.x < a.m) {
+    float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < FEW_WAVES; ++i) top = fmaxf(top, join[i][threadIdx.x].x);
+    const float ref = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+    for (int i = 0; i < FEW_WAVES; ++i) sum += join[i][threadIdx.x].y * exp2f(join[i][threadIdx.x].x - ref);
+    gptr(a.partial)[(int64_t)threadIdx.x * a.parts + blockIdx.x] = malt_f32x2{top, sum};
+  }
+}
+
+// ------------------------------------------------------------------------- join
+// A row's parts, one workgroup of T threads a row.
+template <int T>
+__global__ __launch_bounds__(T) void head_join_kernel(HeadLabels rows, int64_t vocab, const malt_f32x2* partial, int parts,
+                                                      const float* at_label, HeadRow* stats, float* losses) {
+  __shared__ float red[2][T / 64];
+  const int64_t r = blockIdx.x;
+  const malt_f32x2* const p = partial + r * parts;
+  float top = -__builtin_inff(), sum = 0.f;
+  for (int i = threadIdx.x; i < parts; i += T) {
+    const malt_f32x2 v = gptr(p)[i];
+    const float t = fmaxf(top, v.x), ref = t == -__builtin_inff() ? 0.f : t;
+    sum = sum * exp2f(top - ref) + v.y * exp2f(v.x - ref);
+    top = t;
+  }
+  float all = top;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor(all, d, 64));
+  if constexpr (T > 64) {
+    if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = all;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < T / 64; ++i) all = fmaxf(all, red[0][i]);
+  }
+  const float ref = all == -__builtin_inff() ? 0.f : all;
+  sum = sum * exp2f(top - ref);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+  if constexpr (T > 64) {
+    if ((threadIdx.x & 63) == 0) red[1][threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = red[1][0];
+#pragma unroll
+    for (int i = 1; i < T / 64; ++i) sum += red[1][i];
+  }
+  if (threadIdx.x != 0) return;
+  if (label_of(rows, r, vocab) < 0) {
+    if (losses) gptr(losses)[r] = 0.f;
+    if (stats) {
+      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+      *reinterpret_cast<MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<float*>(stats + r))) = zero;
+    }
+    return;
+  }
+  const float y = gptr(at_label)[r];   // log2
+  if (losses) {
+    // log(1 + o / e^y) where the label leads, log(o) - y + log(1 + e^y / o) where it does not; log1p keeps
+    // what a sum of nearly 1 would lose.
+    const float d = y - ref;   // log2 of e^y over the others' largest
+    float loss;
+    if (d > log2f(sum)) loss = log1pf(sum * exp2f(-d));
+    else loss = (log2f(sum) - d) * LN2 + log1pf(exp2f(d) / sum);
+    if (sum == 0.f && y > -__builtin_inff()) loss = 0.f;   // no other column has mass
+    if (y == __builtin_inff()) loss = __builtin_nanf("");
+    gptr(losses)[r] = loss;
+  }
+  if (stats) {
+    // The reference is the larger of both: no power of two above 1 is formed.
+    const float t = fmaxf(ref, y), o = sum * exp2f(ref - t), total = o + exp2f(y - t);
+    const f32x4 v = {t, 1.f / total, o / total, 0.f};
+    *reinterpret_cast<MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<float*>(stats + r))) = v;
+  }
+}
+
+template <class C, class X, class W>
+void few(const HeadFew& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.parts), block(64 * FEW_WAVES);
+  if (a.m <= 16) hipLaunchKernelGGL((head_few_kernel<C, X, W, 1>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((head_few_kernel<C, X, W, 2>), grid, block, 0, s, a);
+}
+
+}  // namespace
+
+int head_few_parts(int64_t vocab) { return (int)((vocab + FEW_COLS - 1) / FEW_COLS); }
+
+hipError_t launch_head_few(const HeadFew& a, bool x_f32, bool w_f32, hipStream_t s) {
+  if (x_f32 && w_f32) few<Few<float>, float, float>(a, s);
+  else if (x_f32) few<Few<float>, float, bf16_t>(a, s);
+  else if (w_f32) few<Few<float>, bf16_t, float>(a, s);
+  else few<Few<bf16_t>, bf16_t, bf16_t>(a, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_join(const HeadLabels& rows, int64_t m, int64_t vocab, const malt_f32x2* partial, int parts,
+                            const float* at_label, HeadRow* stats, float* losses, hipStream_t s) {
+  // A wave a row where there are enough rows to fill the card.
+  const dim3 grid((unsigned)m);
+  if (m <= HEAD_FEW) hipLaunchKernelGGL((head_join_kernel<256>), grid, dim3(256), 0, s, rows, vocab, partial, parts, at_label, stats, losses);
+  else hipLaunchKernelGGL((head_join_kernel<64>), grid, dim3(64), 0, s, rows, vocab, partial, parts, at_label, stats, losses);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_pack(const HeadPack& a, bool f32, hipStream_t s) {
+  const dim3 grid((unsigned)((a.out_rows * (a.pitch / 4) + 255) / 256));
+  if (f32) hipLaunchKernelGGL((head_pack_kernel<float>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((head_pack_kernel<bf16_t>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_clear(const HeadPack& a, hipStream_t s) {
+  hipLaunchKernelGGL(head_clear_kernel, dim3((unsigned)a.rows), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace malt

@@ -5,13 +5,12 @@
 #include "block_fp8.h"
 #include "distill.h"
 #include "embed.h"
-#include "ops_common.h"
+#include "ops_check.h"
 
 using namespace malt;
 
 namespace {
 
-constexpr int64_t kMaxPitch = (int64_t(1) << 31) - 1;
 // A grid holds fewer than 2^32 threads: 64 for each token or table row, 1024 for
 // each row of logits, 512 for each 256 x 256 output tile.
 constexpr int64_t kMaxTokens = int64_t(1) << 25;
@@ -19,33 +18,6 @@ constexpr int64_t kMaxRows = int64_t(1) << 21;
 constexpr int64_t kMaxVocab = int64_t(1) << 30;
 constexpr int64_t kMaxBlockDim = int64_t(1) << 22;
 constexpr int64_t kMaxProduct = int64_t(1) << 37;
-constexpr int64_t kMaxMatrix = int64_t(1) << 35;   // elements of a table, or of one matrix of a layer
-
-// A strided matrix as the checks see it.
-struct Mat {
-  const char* name;
-  const void* p;
-  int type;               // malt_dtype_t
-  int64_t rows, cols, ld;
-  size_t elem() const { return op_dtype_bytes(type); }
-  size_t bytes() const { return rows > 0 && cols > 0 ? (size_t(rows - 1) * ld + cols) * elem() : 0; }
-};
-
-malt_status_t check_mat(const Mat& m) {
-  if (!op_dtype_ok(m.type)) return fail(MALT_ERR_INVALID_ARG, "%s: unknown element type %d", m.name, m.type);
-  if (m.rows > 0 && m.cols > 0 && !m.p) return fail(MALT_ERR_INVALID_ARG, "%s is NULL", m.name);
-  if (m.ld < m.cols || m.ld > kMaxPitch)
-    return fail(MALT_ERR_SHAPE, "%s: row pitch %lld of %lld columns", m.name, (long long)m.ld, (long long)m.cols);
-  if (!op_aligned(m.p, m.elem())) return fail(MALT_ERR_ALIGNMENT, "%s is not aligned to its elements", m.name);
-  return MALT_OK;
-}
-
-malt_status_t check_ids(const char* name, const void* p, int type, int64_t n) {
-  if (type != MALT_INT32 && type != MALT_INT64) return fail(MALT_ERR_INVALID_ARG, "%s: unknown index type %d", name, type);
-  if (n > 0 && !p) return fail(MALT_ERR_INVALID_ARG, "%s is NULL", name);
-  if (!op_aligned(p, type == MALT_INT64 ? 8 : 4)) return fail(MALT_ERR_ALIGNMENT, "%s is not aligned to its elements", name);
-  return MALT_OK;
-}
 
 malt_status_t check_table(int64_t tokens, int64_t vocab, int64_t width) {
   if (tokens < 0 || tokens > kMaxTokens) return fail(MALT_ERR_SHAPE, "%lld tokens", (long long)tokens);
@@ -54,23 +26,6 @@ malt_status_t check_table(int64_t tokens, int64_t vocab, int64_t width) {
     return fail(MALT_ERR_SHAPE, "a table of %lld x %lld", (long long)vocab, (long long)width);
   return MALT_OK;
 }
-
-malt_status_t launched(hipError_t e, const char* what) { return e == hipSuccess ? MALT_OK : hip_fail(e, what); }
-
-malt_status_t check_workspace(const void* p, size_t bytes, size_t need) {
-  if (need > 0 && !p) return fail(MALT_ERR_INVALID_ARG, "workspace is NULL");
-  if (!op_aligned(p, 256)) return fail(MALT_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
-  if (bytes < need) return fail(MALT_ERR_INVALID_ARG, "a workspace of %zu bytes where %zu are needed", bytes, need);
-  return MALT_OK;
-}
-
-inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
-
-#define MALT_TRY(expr)                          \
-  do {                                          \
-    const malt_status_t st_ = (expr);           \
-    if (st_ != MALT_OK) return st_;             \
-  } while (0)
 
 }  // namespace
 
@@ -377,6 +332,41 @@ malt_status_t malt_block_linear(const void* x, malt_dtype_t x_type, int64_t m, i
   MALT_TRY(malt_block_quantize(x, x_type, m, k, ldx, q, q + values, nullptr, nullptr, stream));
   return malt_block_matmul(m, n, k, q, q + values, w_values, w_scales, 1, q_pad(k) / QB, 1, out, out_type, ldo, 0,
                            workspace, need - values - scales, stream);
+}
+
+malt_status_t malt_block_linear_operand(const void* x_values, const void* x_scales, int64_t m, int64_t k,
+                                        const void* w_values, const void* w_scales, int64_t n, void* out,
+                                        malt_dtype_t out_type, int64_t ldo, void* workspace, size_t workspace_bytes,
+                                        void* stream) {
+  if (m > BLOCK_FEW)
+    return malt_block_matmul(m, n, k, x_values, x_scales, w_values, w_scales, 1, q_pad(k > 0 ? k : 1) / QB, 1, out, out_type, ldo,
+                             0, workspace, workspace_bytes, stream);
+  size_t need, values, scales, wv, ws;
+  MALT_TRY(malt_block_matmul_size(m, n, k, out_type, &need));
+  MALT_TRY(malt_block_size(m, k, &values, &scales));
+  MALT_TRY(malt_block_size(n, k, &wv, &ws));
+  ws = size_t(q_pad(n) / QB) * (q_pad(k) / QB);
+  if (!x_values || !x_scales || !w_values || !w_scales) return fail(MALT_ERR_INVALID_ARG, "an operand is NULL");
+  if (!op_aligned(x_values, 16) || !op_aligned(x_scales, 16) || !op_aligned(w_values, 16))
+    return fail(MALT_ERR_ALIGNMENT, "an operand is not 16-byte aligned");
+  const Mat o = {"out", out, out_type, m, n, ldo};
+  MALT_TRY(check_mat(o));
+  if (op_overlap(out, o.bytes(), x_values, values) || op_overlap(out, o.bytes(), x_scales, scales) ||
+      op_overlap(out, o.bytes(), w_values, wv) || op_overlap(out, o.bytes(), w_scales, ws))
+    return fail(MALT_ERR_ALIAS, "out overlaps an operand");
+  BlockLinearArgs g = {};
+  g.x = x_values;
+  g.x_scales = static_cast<const uint8_t*>(x_scales);
+  g.m = m;
+  g.n = n;
+  g.k = k;
+  g.ldx = q_pad(k);
+  g.w = static_cast<const uint8_t*>(w_values);
+  g.w_scales = static_cast<const uint8_t*>(w_scales);
+  g.out = out;
+  g.ldo = ldo;
+  return launched(launch_block_linear(g, false, out_type == MALT_FLOAT32, static_cast<hipStream_t>(stream)),
+                  "launching the 8-bit layer");
 }
 
 // A layer's buffers: what is kept for the backward pass, and the workspaces.

@@ -84,6 +84,40 @@ class malt_distill_t(ctypes.Structure):
                 ("dld", c_int64)]
 
 
+class malt_linear_loss_t(ctypes.Structure):
+    _fields_ = [("x", c_void_p), ("x_type", c_int32), ("rows", c_int64), ("inner", c_int64), ("ldx", c_int64),
+                ("weight", c_void_p), ("weight_type", c_int32), ("vocab", c_int64), ("ldw", c_int64), ("labels", c_void_p),
+                ("label_type", c_int32), ("label_stride", c_int64), ("weights", c_void_p), ("weight_stride", c_int64),
+                ("weight_value", c_float), ("losses", c_void_p), ("stats", c_void_p), ("stats_given", c_int32),
+                ("dx", c_void_p), ("lddx", c_int64), ("dweight", c_void_p), ("dweight_type", c_int32), ("lddw", c_int64),
+                ("accumulate", c_int32)]
+
+
+class malt_adamw_tensors_t(ctypes.Structure):
+    _fields_ = [("count", c_int32), ("numel", POINTER(c_int64)), ("params", POINTER(c_void_p)), ("param_types", c_char_p),
+                ("grads", POINTER(c_void_p)), ("grad_types", c_char_p), ("states", POINTER(c_void_p)),
+                ("state_bits", c_char_p)]
+
+
+class malt_adamw_t(ctypes.Structure):
+    _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("weight_decay", c_double),
+                ("step", c_int64), ("grad_scale", c_double), ("grad_scale_at", c_void_p), ("seed", ctypes.c_uint64)]
+
+
+class malt_rms_norm_t(ctypes.Structure):
+    _fields_ = [("x", c_void_p), ("type", c_int32), ("rows", c_int64), ("width", c_int64), ("ldx", c_int64),
+                ("residual", c_void_p), ("ldr", c_int64), ("weight", c_void_p), ("weight_type", c_int32), ("eps", c_double),
+                ("sum", c_void_p), ("lds", c_int64), ("y", c_void_p), ("y_type", c_int32), ("ldy", c_int64),
+                ("values", c_void_p), ("scales", c_void_p), ("rstd", c_void_p)]
+
+
+class malt_rms_norm_grad_t(ctypes.Structure):
+    _fields_ = [("h", c_void_p), ("type", c_int32), ("rows", c_int64), ("width", c_int64), ("ldh", c_int64),
+                ("weight", c_void_p), ("weight_type", c_int32), ("rstd", c_void_p), ("dy", c_void_p), ("dy_type", c_int32),
+                ("lddy", c_int64), ("dsum", c_void_p), ("ldds", c_int64), ("dx", c_void_p), ("lddx", c_int64),
+                ("dweight", c_void_p)]
+
+
 class MaltError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{status_string(status)}: {message}")
@@ -138,6 +172,16 @@ _SIGNATURES = [
     ("malt_block_layer_backward", c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_int64, c_int32, c_void_p,
                                             c_size_t, c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_int32,
                                             c_void_p, c_size_t, c_void_p]),
+    ("malt_block_linear_operand", c_int32, [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_int64, c_void_p,
+                                            c_int32, c_int64, c_void_p, c_size_t, c_void_p]),
+    ("malt_linear_loss_size", c_int32, [POINTER(malt_linear_loss_t), POINTER(c_size_t)]),
+    ("malt_linear_loss", c_int32, [POINTER(malt_linear_loss_t), c_void_p, c_size_t, c_void_p]),
+    ("malt_adamw_state_size", c_int32, [c_int64, c_int32, POINTER(c_size_t)]),
+    ("malt_adamw_step", c_int32, [POINTER(malt_adamw_tensors_t), POINTER(malt_adamw_t), c_void_p]),
+    ("malt_adamw_moments", c_int32, [c_int32, POINTER(c_int64), POINTER(c_void_p), POINTER(c_void_p), c_void_p]),
+    ("malt_rms_norm", c_int32, [POINTER(malt_rms_norm_t), c_void_p]),
+    ("malt_rms_norm_grad_size", c_int32, [c_int64, c_int64, c_int32, POINTER(c_size_t)]),
+    ("malt_rms_norm_grad", c_int32, [POINTER(malt_rms_norm_grad_t), c_void_p, c_size_t, c_void_p]),
     ("malt_destroy_state", None, [c_void_p]),
     ("malt_status_string", c_char_p, [c_int32]),
     ("malt_last_error", c_char_p, []),

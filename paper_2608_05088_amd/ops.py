@@ -4,6 +4,11 @@
   distill_loss, distill_step           loss against a teacher's top logits (and labels), and its gradient
   fp8_linear                           a linear layer in 8-bit floating point, with its backward pass
   fp8_quantize_weight, fp8_forward     the same layer on kept 8-bit weights
+  linear_cross_entropy, linear_cross_entropy_step
+                                       loss of a linear head over a large vocabulary without its logits, and its gradients
+  rms_norm, rms_norm_fp8               norm of x + residual, with its backward pass, and with its output in 8 bits
+  adamw_state, adamw_step, adamw_moments
+                                       one AdamW step over many tensors, moments in 32 bits or in 8
 
 The definitions stand in include/libmalt.h.  This module checks arguments,
 allocates outputs and workspaces with torch, and calls the library; there is
@@ -21,8 +26,9 @@ taken as they are up to 2^31 - 1 elements, as are those of outputs.
 from __future__ import annotations
 
 import functools
-from ctypes import byref, c_size_t
-from typing import Optional, Tuple, Union
+import operator
+from ctypes import byref, c_int64, c_size_t, c_void_p
+from typing import List, NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
 from torch.autograd import forward_ad as _forward_ad
@@ -529,20 +535,56 @@ def fp8_quantize_weight(weight: torch.Tensor, stream=None) -> Tuple[torch.Tensor
     return values.view(torch.float8_e4m3fn), scales
 
 
-def fp8_forward(x: torch.Tensor, values: torch.Tensor, scales: torch.Tensor,
+class Fp8Rows(NamedTuple):
+    """Activations (shape[:-1] + (inner,)) in 8 bits, as rms_norm_fp8 makes them for fp8_forward."""
+    values: torch.Tensor   # float8_e4m3fn (rows, inner padded with zeros to whole blocks)
+    scales: torch.Tensor   # uint8 (blocks, rows padded to 256), in the matrix instructions' order
+    shape: torch.Size
+
+
+def _fp8_rows(x: Fp8Rows, dev, k: int, kb: int) -> int:
+    """Checks activations in 8 bits; their number of rows."""
+    _tensor("x.values", x.values, (torch.float8_e4m3fn,), dev)
+    _tensor("x.scales", x.scales, (torch.uint8,), dev)
+    m = torch.Size(x.shape[:-1]).numel()
+    if tuple(x.values.shape) != (m, kb * BLOCK) or not x.values.is_contiguous():
+        raise ValueError(f"x.values must be contiguous, ({m}, {kb * BLOCK}) (got {tuple(x.values.shape)}, "
+                         f"strides {x.values.stride()})")
+    if tuple(x.scales.shape) != (kb, _pad(m, 256)) or not x.scales.is_contiguous():
+        raise ValueError(f"x.scales must be contiguous, ({kb}, {_pad(m, 256)}) (got {tuple(x.scales.shape)}, "
+                         f"strides {x.scales.stride()})")
+    return m
+
+
+@functools.lru_cache(maxsize=4096)
+def _matmul_size(m: int, n: int, k: int, out_type: int) -> int:
+    size = c_size_t(0)
+    lm._check(lm.lib().malt_block_matmul_size(m, n, k, out_type, byref(size)))
+    return size.value
+
+
+def fp8_forward(x: Union[torch.Tensor, Fp8Rows], values: torch.Tensor, scales: torch.Tensor,
                 out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """fp8_linear on kept weights (fp8_quantize_weight), without gradients:
-    x (..., inner), values (outer, inner padded to whole blocks).  Precision by
+    x (..., inner), values (outer, inner padded to whole blocks).  x may be in 8 bits
+    already (rms_norm_fp8's rows; out_dtype is bfloat16 then unless given).  Precision by
     out_dtype, as there."""
     _tensor("values", values, (torch.float8_e4m3fn,))
     dev = values.device
-    _tensor("x", x, _DTYPES, dev)
+    ready = isinstance(x, Fp8Rows)
+    if not ready:
+        _tensor("x", x, _DTYPES, dev)
     _tensor("scales", scales, (torch.uint8,), dev)
-    k = x.shape[-1] if x.dim() else 0
+    k = x.shape[-1] if len(x.shape) else 0
     if k < 1:
         raise ValueError(f"x must be (..., inner) (got {tuple(x.shape)})")
-    out_dtype = _linear_args(x, k, out_dtype)
     kb = -(-k // BLOCK)
+    if ready:
+        m = _fp8_rows(x, dev, k, kb)
+        out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
+        _type("out_dtype", out_dtype)
+    else:
+        out_dtype = _linear_args(x, k, out_dtype)
     if values.dim() != 2 or values.shape[0] < 1 or values.shape[1] != kb * BLOCK or not values.is_contiguous():
         raise ValueError(f"values must be contiguous, (outer, {kb * BLOCK}) (got {tuple(values.shape)}, "
                          f"strides {values.stride()})")
@@ -550,6 +592,19 @@ def fp8_forward(x: torch.Tensor, values: torch.Tensor, scales: torch.Tensor,
     if tuple(scales.shape) != (-(-n // BLOCK), kb) or not scales.is_contiguous():
         raise ValueError(f"scales must be contiguous, ({-(-n // BLOCK)}, {kb}) "
                          f"(got {tuple(scales.shape)}, strides {scales.stride()})")
+    if ready:
+        def work_ready(s):
+            y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
+            if m:
+                out_type = _DTYPES[out_dtype]
+                size = _matmul_size(m, n, k, out_type) if m > 32 else 0
+                ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+                lm._check(lm.lib().malt_block_linear_operand(
+                    x.values.data_ptr(), x.scales.data_ptr(), m, k, values.data_ptr(), scales.data_ptr(), n, y.data_ptr(),
+                    out_type, n, ws.data_ptr() if size else None, size, s))
+            return y
+
+        return _on(dev, stream, (x.values, x.scales, values, scales), work_ready)
     x = x.detach()
 
     def work(s):
@@ -559,3 +614,356 @@ def fp8_forward(x: torch.Tensor, values: torch.Tensor, scales: torch.Tensor,
         return y
 
     return _on(dev, stream, (x, values, scales), work)
+
+
+# ------------------------------------------------------- cross entropy of a head
+def _head(x, weight, labels, grad, want_losses, want_dx, want_dw, out, accumulate, stats, want_stats, stream):
+    """losses, dx, dweight and the rows' statistics, as far as they are wanted.  stats: those of an earlier call."""
+    _tensor("x", x, _DTYPES)
+    dev = x.device
+    _weight(weight, dev)
+    v, k = weight.shape
+    if x.dim() < 1 or x.shape[-1] != k:
+        raise ValueError(f"x must be (..., {k}) (got {tuple(x.shape)})")
+    lead = x.shape[:-1]
+    n = lead.numel()
+    _tensor("labels", labels, _INDEX, dev)
+    if labels.shape != lead:
+        raise ValueError(f"labels must be {tuple(lead)} (got {tuple(labels.shape)})")
+    weights, value = None, 1.0
+    if isinstance(grad, torch.Tensor):
+        _tensor("grad", grad, (torch.float32,), dev)
+        if grad.dim() > 0 and grad.shape != lead:
+            raise ValueError(f"grad must be a number, a scalar tensor or {tuple(lead)} (got {tuple(grad.shape)})")
+        weights = grad
+    else:
+        value = float(grad)
+    if out is not None:
+        _tensor("out", out, _DTYPES, dev)
+        if tuple(out.shape) != (v, k) or (k > 1 and out.stride(1) != 1) or (v > 1 and out.stride(0) < k):
+            raise ValueError(f"out must be ({v}, {k}) with contiguous rows (got {tuple(out.shape)}, strides {out.stride()})")
+    elif accumulate:
+        raise ValueError("accumulate needs out")
+
+    def work(s):
+        losses = torch.empty(lead, dtype=torch.float32, device=dev) if want_losses else None
+        dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_dx else None
+        dw = out if out is not None else torch.empty((v, k), dtype=weight.dtype, device=dev) if want_dw else None
+        kept = torch.empty((n, 4), dtype=torch.float32, device=dev) if want_stats else stats
+        flat, ldx = _rows(_flat(x) if x.dim() > 1 else x.reshape(1, k))
+        w, ldw = _rows(weight)
+        y = labels if labels.dim() == 1 else labels.reshape(-1)
+        g = weights if weights is None or weights.dim() < 2 else weights.reshape(-1)
+        a = lm.malt_linear_loss_t(
+            flat.data_ptr(), _DTYPES[x.dtype], n, k, ldx, w.data_ptr(), _DTYPES[weight.dtype], v, ldw, y.data_ptr(),
+            _INDEX[y.dtype], y.stride(0) if n > 1 else 0, None if g is None else g.data_ptr(),
+            g.stride(0) if g is not None and n > 1 and g.dim() else 0, value, losses.data_ptr() if want_losses else None,
+            None if kept is None else kept.data_ptr(), int(stats is not None), dx.data_ptr() if want_dx else None, k,
+            None if dw is None else dw.data_ptr(), 0 if dw is None else _DTYPES[dw.dtype],
+            k if dw is None or v == 1 else dw.stride(0), int(bool(accumulate)))
+        if n or dw is not None:
+            size = c_size_t(0)
+            lm._check(lm.lib().malt_linear_loss_size(byref(a), byref(size)))
+            ws = torch.empty(size.value, dtype=torch.uint8, device=dev)
+            lm._check(lm.lib().malt_linear_loss(byref(a), ws.data_ptr(), size.value, s))
+        return losses, dx, dw, kept
+
+    result = _on(dev, stream, (x, weight, labels, weights, out, stats), work)
+    _written(out)
+    return result
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, labels):
+        losses, _, _, stats = _head(x, weight, labels, 1.0, True, False, False, None, False, None, True, None)
+        ctx.save_for_backward(x, weight, labels, stats)
+        return losses
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        x, weight, labels, stats = ctx.saved_tensors
+        need_x, need_w = ctx.needs_input_grad[:2]
+        _, dx, dw, _ = _head(x, weight, labels, grad.float(), False, need_x, need_w, None, False, stats, False, None)
+        return dx, dw, None
+
+
+def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, stream=None) -> torch.Tensor:
+    """Cross entropy of each row of a linear head, logits = x weight^T with
+    x (..., inner) and weight (vocab, inner), float32 of labels' shape.  The logits
+    are never held: neither here nor in the backward pass.  A label outside the vocabulary
+    (-1, -100) is none: the row's loss is 0, whatever x holds there, and it adds no gradient.
+    Types may differ (float32, bfloat16); float32 values enter the products whole.
+    Differentiable in x and weight; gradients are of their types."""
+    for name, t in (("x", x), ("weight", weight)):
+        if isinstance(t, torch.Tensor):
+            _no_tangent(name, t)
+    if torch.is_grad_enabled() and (getattr(x, "requires_grad", False) or getattr(weight, "requires_grad", False)):
+        _no_stream(stream)
+        return _LinearCrossEntropy.apply(x, weight, labels)
+    return _head(x, weight, labels, 1.0, True, False, False, None, False, None, False, stream)[0]
+
+
+def linear_cross_entropy_step(x: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor,
+                              grad: Union[float, torch.Tensor] = 1.0, out: Optional[torch.Tensor] = None,
+                              accumulate: bool = False, stream=None
+                              ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """The losses of linear_cross_entropy and the gradients of sum(grad * losses)
+    to x and weight, as (losses, dx, dweight).  grad: a number, a float32 scalar tensor or
+    one weight for each row (0: no gradient).  dweight is of weight's type, or goes to `out`
+    (vocab, inner; contiguous rows; either type) when given, with accumulate added to it: to autograd,
+    `out` is changed in place."""
+    x, weight = (t.detach() if isinstance(t, torch.Tensor) and t.requires_grad else t for t in (x, weight))
+    return _head(x, weight, labels, grad, True, True, True, out, accumulate, None, False, stream)[:3]
+
+
+# -------------------------------------------------------------------------- norm
+@functools.lru_cache(maxsize=4096)
+def _norm_grad_size(rows: int, width: int, need_w: bool) -> int:
+    size = c_size_t(0)
+    lm._check(lm.lib().malt_rms_norm_grad_size(rows, width, need_w, byref(size)))
+    return size.value
+
+
+def _norm_args(x, weight, residual, eps) -> float:
+    _tensor("x", x, _DTYPES)
+    _tensor("weight", weight, _DTYPES, x.device)
+    if x.dim() < 1 or x.shape[-1] < 1 or weight.dim() != 1 or weight.shape[0] != x.shape[-1]:
+        raise ValueError(f"x must be (..., width) and weight (width,) (got {tuple(x.shape)}, {tuple(weight.shape)})")
+    if residual is not None:
+        _tensor("residual", residual, (x.dtype,), x.device)
+        if residual.shape != x.shape:
+            raise ValueError(f"residual must be {tuple(x.shape)} (got {tuple(residual.shape)})")
+    eps = float(eps)
+    if not 0 <= eps < float("inf"):
+        raise ValueError(f"eps must be a number, 0 or more (got {eps})")
+    return eps
+
+
+def _norm(x, weight, residual, eps, out_dtype, want_rstd, stream):
+    """y (in 8 bits without out_dtype), the sum (None without residual) and 1 / rms."""
+    dev = x.device
+    width = x.shape[-1]
+    n = x.numel() // width
+
+    def work(s):
+        sums = torch.empty(x.shape, dtype=x.dtype, device=dev) if residual is not None else None
+        rstd = torch.empty(n, dtype=torch.float32, device=dev) if want_rstd else None
+        if out_dtype is None:
+            kb = -(-width // BLOCK)
+            y = torch.empty((n, kb * BLOCK), dtype=torch.float8_e4m3fn, device=dev)
+            scales = torch.empty((kb, _pad(n, 256)), dtype=torch.uint8, device=dev)
+        else:
+            y, scales = torch.empty(x.shape, dtype=out_dtype, device=dev), None
+        if n:
+            flat, ldx = _rows(_flat(x) if x.dim() > 1 else x.reshape(1, width))
+            r, ldr = (None, 0) if residual is None else _rows(_flat(residual) if x.dim() > 1 else residual.reshape(1, width))
+            w = weight.contiguous()
+            eight = scales is not None
+            a = lm.malt_rms_norm_t(
+                flat.data_ptr(), _DTYPES[x.dtype], n, width, ldx, None if r is None else r.data_ptr(), ldr, w.data_ptr(),
+                _DTYPES[w.dtype], eps, None if sums is None else sums.data_ptr(), width, None if eight else y.data_ptr(),
+                0 if eight else _DTYPES[out_dtype], width, y.data_ptr() if eight else None,
+                scales.data_ptr() if eight else None, None if rstd is None else rstd.data_ptr())
+            lm._check(lm.lib().malt_rms_norm(byref(a), s))
+        return (y if scales is None else Fp8Rows(y, scales, x.shape)), sums, rstd
+
+    return _on(dev, stream, (x, weight, residual), work)
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps, out_dtype):
+        ctx.set_materialize_grads(False)
+        y, h, rstd = _norm(x, weight, residual, eps, out_dtype, True, None)
+        ctx.save_for_backward(x if h is None else h, weight, rstd)
+        return y if h is None else (y, h)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dh=None):
+        h, weight, rstd = ctx.saved_tensors
+        need_x, need_w, need_r = ctx.needs_input_grad[:3]
+        if dh is not None and dh.dtype != h.dtype:
+            dh = dh.to(h.dtype)
+        if dy is None:   # nothing went through the norm
+            return dh if need_x else None, None, dh if need_r else None, None, None
+        dev = h.device
+        width = h.shape[-1]
+        n = h.numel() // width
+        if dy.dtype not in _DTYPES:
+            dy = dy.float()
+        need_h = need_x or need_r
+
+        def work(s):
+            dx = torch.empty(h.shape, dtype=h.dtype, device=dev) if need_h else None
+            dw = torch.empty(width, dtype=weight.dtype, device=dev) if need_w else None
+            if n == 0:
+                return dx, None if dw is None else dw.zero_()
+            (hf, ldh), (gf, ldg) = (_rows(_flat(t) if t.dim() > 1 else t.reshape(1, width)) for t in (h, dy))
+            df, ldd = (None, 0) if dh is None or not need_h else _rows(_flat(dh) if dh.dim() > 1 else dh.reshape(1, width))
+            w = weight.contiguous()
+            size = _norm_grad_size(n, width, need_w)
+            ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+            a = lm.malt_rms_norm_grad_t(
+                hf.data_ptr(), _DTYPES[h.dtype], n, width, ldh, w.data_ptr(), _DTYPES[w.dtype], rstd.data_ptr(), gf.data_ptr(),
+                _DTYPES[gf.dtype], ldg, None if df is None else df.data_ptr(), ldd, dx.data_ptr() if need_h else None, width,
+                dw.data_ptr() if need_w else None)
+            lm._check(lm.lib().malt_rms_norm_grad(byref(a), ws.data_ptr() if size else None, size, s))
+            return dx, dw
+
+        dx, dw = _on(dev, None, (), work)
+        return dx if need_x else None, dw, dx if need_r else None, None, None
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+             out_dtype: Optional[torch.dtype] = None, stream=None):
+    """Root-mean-square norm of the rows of x (..., width) times weight (width,):
+    y = h / sqrt(mean(h^2) + eps) * weight, h = x.  With residual (of x's shape and type)
+    h = x + residual, rounded to their type, and the result is (y, h).  out_dtype: x's unless
+    given.  Computed in float32, the mean of squares in float64.  Differentiable in x, residual
+    and weight, through h as well."""
+    eps = _norm_args(x, weight, residual, eps)
+    for name, t in (("x", x), ("weight", weight), ("residual", residual)):
+        if t is not None:
+            _no_tangent(name, t)
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    _type("out_dtype", out_dtype)
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad
+                                    or (residual is not None and residual.requires_grad)):
+        _no_stream(stream)
+        return _RmsNorm.apply(x, weight, residual, eps, out_dtype)
+    y, h, _ = _norm(x, weight, residual, eps, out_dtype, False, stream)
+    return y if residual is None else (y, h)
+
+
+def rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 stream=None):
+    """rms_norm with its output in 8 bits (Fp8Rows: a scale for each row and 128
+    values), for fp8_forward on kept weights, in one pass and without gradients:
+    rows, or (rows, h) with residual.  y is rounded once, from float32."""
+    eps = _norm_args(x, weight, residual, eps)
+    x, weight = x.detach(), weight.detach()
+    if residual is not None:
+        residual = residual.detach()
+    rows, h, _ = _norm(x, weight, residual, eps, None, False, stream)
+    return rows if residual is None else (rows, h)
+
+
+# ------------------------------------------------------------------------- AdamW
+@functools.lru_cache(maxsize=4096)
+def _adamw_size(numel: int, bits: int) -> int:
+    size = c_size_t(0)
+    lm._check(lm.lib().malt_adamw_state_size(numel, bits, byref(size)))
+    return size.value
+
+
+def adamw_state(param: torch.Tensor, bits: int = 32) -> torch.Tensor:
+    """The moments of a parameter before its first step, to be kept for adamw_step: float32
+    (2, numel), or with bits=8 the bytes of 8-bit moments (8.25 bits each)."""
+    _tensor("param", param, _DTYPES)
+    if bits not in (8, 32):
+        raise ValueError(f"bits must be 8 or 32 (got {bits})")
+    if bits == 32:
+        return torch.zeros((2, param.numel()), dtype=torch.float32, device=param.device)
+    return torch.zeros(_adamw_size(param.numel(), 8), dtype=torch.uint8, device=param.device)
+
+
+_FIELDS = operator.attrgetter("dtype", "device", "shape")
+_BITS = {torch.float32: 32, torch.uint8: 8}
+
+
+def _adamw_states(params, states, dev) -> bytes:
+    """Checks moments against their parameters; their bits."""
+    for i, (p, st) in enumerate(zip(params, states)):
+        _tensor(f"states[{i}]", st, _BITS, dev)
+        want = (2, p.numel()) if st.dtype == torch.float32 else (_adamw_size(p.numel(), 8),)
+        if tuple(st.shape) != want or not st.is_contiguous():
+            raise ValueError(f"states[{i}] must be contiguous, {want} (got {tuple(st.shape)}, strides {st.stride()})")
+    return bytes(_BITS[st.dtype] for st in states)
+
+
+def _pointers(tensors):
+    return (c_void_p * len(tensors))(*map(torch.Tensor.data_ptr, tensors))
+
+
+def _sizes(tensors):
+    return (c_int64 * len(tensors))(*map(torch.Tensor.numel, tensors))
+
+
+def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], states: Sequence[torch.Tensor], lr: float,
+               betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, *, step: int,
+               grad_scale: Union[float, torch.Tensor] = 1.0, seed: int = 0, stream=None) -> None:
+    """One AdamW step over many tensors, in place, a launch for each 108 of them:
+    m = b1 m + (1 - b1) g, v = b2 v + (1 - b2) g^2 with g = grad_scale * grad, then
+    p = p (1 - lr weight_decay) - lr (m / (1 - b1^step)) / (sqrt(v / (1 - b2^step)) + eps).
+    params (contiguous) and grads are float32 or bfloat16, states adamw_state's.  step counts
+    from 1; grad_scale: a number or a float32 scalar tensor, read on the device.
+
+    8-bit moments are rounded up or down at random by their distance, so that small changes
+    add up; the random numbers follow from `seed`, the tensor's place in the list and the
+    element's: give each step another seed.  Equal calls give equal bits.  A captured call replays its
+    arguments, step and seed among them.  To autograd, params and states are changed in place."""
+    params, grads, states = list(params), list(grads), list(states)
+    if not len(params) == len(grads) == len(states):
+        raise ValueError(f"params, grads and states must be as many (got {len(params)}, {len(grads)}, {len(states)})")
+    scale_at = None
+    if isinstance(grad_scale, torch.Tensor):
+        scale_at, grad_scale = grad_scale, 1.0
+    if not 0 <= int(seed) < 1 << 64:
+        raise ValueError(f"seed must be in [0, 2^64) (got {seed})")
+    if not params:
+        return
+    for i, (p, g) in enumerate(zip(params, grads)):
+        _tensor(f"params[{i}]", p, _DTYPES, params[0].device)
+        _tensor(f"grads[{i}]", g, _DTYPES, params[0].device)
+        if not p.is_contiguous():
+            raise ValueError(f"params[{i}] must be contiguous (got strides {p.stride()})")
+        if g.shape != p.shape:
+            raise ValueError(f"grads[{i}] must be {tuple(p.shape)} (got {tuple(g.shape)})")
+    dev = params[0].device
+    bits = _adamw_states(params, states, dev)
+    if scale_at is not None:
+        _tensor("grad_scale", scale_at, (torch.float32,), dev)
+        if scale_at.numel() != 1:
+            raise ValueError(f"grad_scale must be a number or a scalar tensor (got {tuple(scale_at.shape)})")
+    h = lm.malt_adamw_t(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(step),
+                        float(grad_scale), None if scale_at is None else scale_at.data_ptr(), int(seed))
+
+    def work(s):
+        gs = [g if g.is_contiguous() else g.contiguous() for g in grads]
+        t = lm.malt_adamw_tensors_t(len(params), _sizes(params), _pointers(params), bytes(_DTYPES[p.dtype] for p in params),
+                                    _pointers(gs), bytes(_DTYPES[g.dtype] for g in gs), _pointers(states), bits)
+        lm._check(lm.lib().malt_adamw_step(byref(t), byref(h), s))
+
+    _on(dev, stream, (*params, *grads, *states, scale_at), work)
+    for x in params:
+        _written(x)
+    for x in states:
+        _written(x)
+
+
+def adamw_moments(params: Sequence[torch.Tensor], states: Sequence[torch.Tensor], stream=None) -> List[torch.Tensor]:
+    """What the moments of adamw_step stand for: float32 (2, numel) for each parameter,
+    the first moment and the second, in new tensors."""
+    params, states = list(params), list(states)
+    if len(params) != len(states):
+        raise ValueError(f"params and states must be as many (got {len(params)}, {len(states)})")
+    if not params:
+        return []
+    dev = params[0].device
+    for i, p in enumerate(params):
+        _tensor(f"params[{i}]", p, _DTYPES, dev)
+    bits = _adamw_states(params, states, dev)
+
+    def work(s):
+        out = [st.clone() if b == 32 else torch.empty((2, p.numel()), dtype=torch.float32, device=dev)
+               for p, st, b in zip(params, states, bits)]
+        few = [i for i, b in enumerate(bits) if b == 8]
+        if few:
+            lm._check(lm.lib().malt_adamw_moments(len(few), _sizes([params[i] for i in few]),
+                                                  _pointers([states[i] for i in few]), _pointers([out[i] for i in few]), s))
+        return out
+
+    return _on(dev, stream, states, work)

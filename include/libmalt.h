@@ -476,8 +476,8 @@ malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, in
  * aligned, of no meaning before or after the call.  It holds d for a piece of the vocabulary at a
  * time, at most 512 MiB (a tile's 256 columns at the least), x and, where it is float32
  * or not laid out for whole 16-byte loads, the weight in bfloat16.
- * Limits: rows <= 65536, 1 <= inner <= 65536, 1 <= vocab <= 2^25, vocab * inner <= 2^33,
- * rows * vocab <= 2^38 (rounded up to 2048 and 1024). */
+ * Limits: rows <= 65536, 1 <= inner <= 65536, 1 <= vocab <= 2^22, vocab * inner <= 2^33,
+ * rows * vocab <= 2^38 (both rounded up to 256). */
 typedef struct {
   const void* x;             /* rows x inner, type x_type (dx's too) */
   malt_dtype_t x_type;

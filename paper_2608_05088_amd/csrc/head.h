@@ -18,10 +18,10 @@ constexpr int HEAD_BK = 64;      // contraction per stage, and what columns are 
 
 // A row's softmax after the first pass, in log2: probabilities are 2^(z log2 e - top) * inverse.
 struct HeadRow {
-  float top;       // log2 e times the row's largest logit but the label's
+  float top;       // log2 e times the row's largest logit
   float inverse;   // 1 / sum over the vocabulary of 2^(z log2 e - top)
   float others;    // 1 - the label's probability, from the others' sum
-  float unused;
+  int32_t label;   // for the second pass, where `inverse` and `others` hold the row's weight; -1: no gradient
 };
 
 // What decides about a row.
@@ -33,13 +33,17 @@ struct HeadLabels {
   int64_t weight_stride;
 };
 
-// One side of a product: planes of bf16 rows, one behind the other.
+// One side of a product: planes of bf16, rows with the contraction along them.  As they lie (a
+// weight): tile = 256 ld, step = 64.  Packed: blocks of 256 rows by 64 values, what a stage reads
+// of a tile, each 32 KB in a piece: [row / 256][value / 64][row % 256][value % 64].
+constexpr int HEAD_BLOCK = HEAD_TILE * HEAD_BK;
 struct HeadSide {
   const uint16_t* p;
   int64_t plane;   // elements from one plane to the next
-  int64_t ld;
+  int64_t tile;    // from 256 rows to the next
+  int64_t step;    // from a stage to the next
+  int32_t ld;      // from a row to the next
   int64_t rows;    // rows there are: further ones are not read
-  int32_t cols;    // columns there are (a multiple of 8)
 };
 
 // C = sum over pairs of planes of A B^T, over `k` values.
@@ -61,9 +65,10 @@ struct HeadLogits {
   float* at_label;       // [m]: log2 e times the label's logit
   int32_t parts;         // tiles
   // second pass
-  const HeadRow* stats;
-  uint16_t* dz;          // planes of [padded m][padded n]
-  int64_t dz_plane, dz_ld;
+  const HeadRow* records;   // of the padded rows
+  uint16_t* dz;          // packed planes, rows m by n, or null
+  uint16_t* dz_t;        // packed planes, rows n by m, or null
+  int64_t dz_plane, dz_tile, dz_t_tile;
   int32_t dz_planes;
 };
 
@@ -71,16 +76,15 @@ struct HeadOut {
   HeadProduct g;
   void* out;
   int64_t ldo;
-  float* partial;        // float32 sums of the pieces so far (dx), m x n; null: one piece
-  int32_t form;          // 0: dx (B as rows of the contraction), 1: dW (both sides)
+  float* partial;        // float32 sums, [splits][m][n], where `out` is not written at once
+  int32_t splits;        // parts of the contraction, each a workgroup's
   bool f32, add_partial, write_partial, accumulate;
-  bool mask_rows;        // rows without label or weight are zero (dx)
+  bool mask_rows;        // rows without gradient are zero (dx)
 };
 struct HeadGrads {
   HeadOut part[2];       // one launch: dx's tiles, then dW's
   int32_t parts;
-  HeadLabels rows;
-  int64_t vocab;
+  const HeadRow* records;
   float scale;
   const float* scale_at; // or null
 };
@@ -101,20 +105,24 @@ int head_few_parts(int64_t vocab);
 struct HeadPack {
   const void* x;
   int64_t rows, cols, ld;
-  uint16_t* out;           // planes of [padded rows][padded cols]
-  int64_t plane, pitch, out_rows;
+  uint16_t* out;           // packed planes, rows by cols, or cols by rows for the transpose
+  int64_t plane;
+  int64_t out_rows, out_cols;   // as the output lies: rows to write, padded columns (the contraction)
   int32_t planes;
-  HeadLabels labels;       // rows without label become zeros; labels null: every row stays
+  HeadLabels labels;       // rows without label (or weight) become zeros; labels null: every row stays
   int64_t vocab;
 };
 
 hipError_t launch_head_pack(const HeadPack& a, bool f32, hipStream_t s);
-hipError_t launch_head_clear(const HeadPack& a, hipStream_t s);
+hipError_t launch_head_pack_t(const HeadPack& a, bool f32, hipStream_t s);
+hipError_t launch_head_records(const HeadLabels& l, int64_t rows, int64_t rows_pad, int64_t vocab, const HeadRow* stats,
+                               HeadRow* records, hipStream_t s);
 hipError_t launch_head_few(const HeadFew& a, bool x_f32, bool w_f32, hipStream_t s);
 hipError_t launch_head_join(const HeadLabels& rows, int64_t m, int64_t vocab, const malt_f32x2* partial, int parts,
                             const float* at_label, HeadRow* stats, float* losses, hipStream_t s);
 hipError_t launch_head_logits(const HeadLogits& a, bool second, hipStream_t s);
 hipError_t launch_head_grads(const HeadGrads& a, hipStream_t s);
+hipError_t launch_head_sum(const HeadOut& o, const HeadGrads& a, hipStream_t s);
 hipError_t head_setup();
 
 }  // namespace malt

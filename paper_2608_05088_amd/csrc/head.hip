@@ -9,9 +9,10 @@
 // read (twice 4 bytes a logit) as the K products that make one.
 //
 // A workgroup of eight waves makes one 256 x 256 tile, the pipeline of the Newton-Schulz
-// update (ns_common.h): stages of 64 contracted values go straight to LDS, two slots deep.  Rows with
-// the contraction contiguous ("rows") are read as they lie, an operand whose rows are the
-// contraction ("columns") through transposed LDS reads, so that nothing is transposed in memory.
+// update (ns_common.h): stages of 64 contracted values go straight to LDS, two slots deep.  Both
+// sides of every product lie with the contraction along their rows: x and W are transposed once for
+// the gradients, dz is written both ways.  (Transposed LDS reads instead: 1.84 us a stage, for one side or
+// both; rows of 32 KB apart: 1.70, with a pitch that is no power of two 1.58.)
 //
 // float32 operands are three bf16 planes whose sum they are.  A product of two is the six plane
 // products that matter (high by low and middle by low are below 2^-26 of it), small ones first,
@@ -19,8 +20,8 @@
 // of the float32 matrix instruction.  bf16 gradients take dz and the operands as single
 // planes: dz is rounded once more, an error of the size of the result's own rounding.
 //
-// Tiles are dealt to the eight XCDs in blocks of 8 x 4, so that the panels of the tiles that run
-// on one XCD at a time are few enough for its L2.
+// An XCD's 32 CUs work on 8 x 4 neighbouring tiles at a time, so that the twelve panels they read
+// come once from memory and otherwise from its L2.
 #include <atomic>
 
 #include "head.h"
@@ -37,331 +38,445 @@ using G = NsGeom<HEAD_BK, 2, 32>;
 constexpr int BK = G::BK, STAGES = G::STAGES, H = G::H, RB = G::RB, CPR = G::CPR, LOADS = G::LOADS;
 constexpr int NB = TM / 16, NA = TN / 16;
 constexpr float LOG2E = 1.44269504088896340736f;
-constexpr int OUT_PITCH = TN * 2 + 8;   // dz's staging: a wave's sub-tile, rows padded by 8 bytes
-constexpr int STAGING = NW * TM * OUT_PITCH;
-constexpr int LDS_BYTES = G::RING_BYTES > STAGING ? G::RING_BYTES : STAGING;
+// Behind the ring, so that the next tile's first stages can arrive during a tile's epilogue: rows'
+// records or labels of two tiles, and the waves' statistics or 16 rows of each wave's dz (padded by 8 bytes).
+constexpr int ROW_BYTES = HEAD_TILE * 16;
+constexpr int AT_ROWS = G::RING_BYTES, AT_EPI = AT_ROWS + 2 * ROW_BYTES;
+constexpr int OUT_PITCH = TN * 2 + 8, OUT_WAVE = 16 * OUT_PITCH;
+constexpr int JOIN_BYTES = HEAD_TILE * (NW / 2) * 8;
+constexpr int LDS_BYTES = AT_EPI + (NW * OUT_WAVE > JOIN_BYTES ? NW * OUT_WAVE : JOIN_BYTES);
 static_assert(LDS_BYTES <= 160 * 1024, "LDS budget");
-static_assert(BK == 64 && CPR == 8 && LOADS == 8, "the loads below");
+constexpr int CUS = 256;   // workgroups of the passes over the logits, one a CU
+static_assert(STAGES == 2 && (G::STAGE_BYTES & (G::STAGE_BYTES - 1)) == 0 && BK == 64 && TN == BK && TM == 2 * BK && CPR == 8 && LOADS == 8 && 16 % (G::RPP * CPR) == 0, "the loads and reads below");
 
-enum Side { ROWS, COLS };   // ROWS: [row][k]; COLS: [k][row]
+__host__ __device__ inline int stages_of(const HeadProduct& g) { return (int)((g.k + BK - 1) / BK); }
 
-struct TileAt { int i, j; };
-
-// Block b's tile of tiles_m x tiles_n, or i < 0.  Blocks b, b + 8, ... run on one XCD.
-constexpr int SUPER_M = 8, SUPER_N = 4;
-__host__ __device__ inline int supers(int tiles_m, int tiles_n) {
-  return ((tiles_m + SUPER_M - 1) / SUPER_M) * ((tiles_n + SUPER_N - 1) / SUPER_N);
+// Block b's tile (i, j) and part of the contraction, or i < 0.  Blocks b, b + 8, ... run on one XCD:
+// it takes an eighth of the tiles, neighbours in an order of bands of eight rows, column by column.
+struct TileAt { int i, j, split; };
+constexpr int BAND = 8;
+__host__ __device__ inline int tile_blocks(int tiles_m, int tiles_n, int splits) {
+  return (tiles_m * tiles_n * splits + 7) / 8 * 8;
 }
-__host__ __device__ inline int tile_blocks(int tiles_m, int tiles_n) {
-  return (supers(tiles_m, tiles_n) + 7) / 8 * 8 * SUPER_M * SUPER_N;
-}
-__device__ __forceinline__ TileAt tile_at(int b, int tiles_m, int tiles_n) {
-  const int xcd = b & 7, slot = b >> 3;
-  const int super = slot / (SUPER_M * SUPER_N) * 8 + xcd, in = slot % (SUPER_M * SUPER_N);
-  const int sm = (tiles_m + SUPER_M - 1) / SUPER_M;
-  const int i = super % sm * SUPER_M + in % SUPER_M, j = super / sm * SUPER_N + in / SUPER_M;
-  return i < tiles_m && j < tiles_n ? TileAt{i, j} : TileAt{-1, -1};
+__device__ __forceinline__ TileAt tile_at(int b, int tiles_m, int tiles_n, int splits) {
+  const int tiles = tiles_m * tiles_n, all = tiles * splits, per = (all + 7) / 8;
+  int t = (b & 7) * per + (b >> 3);
+  if ((b >> 3) >= per || t >= all) return {-1, -1, 0};   // so for any block past the last
+  const int split = t / tiles;
+  t -= split * tiles;
+  const int band = t / (BAND * tiles_n), first = band * BAND, rows = tiles_m - first < BAND ? tiles_m - first : BAND;
+  t -= first * tiles_n;
+  return {first + t % rows, t / rows, split};
 }
 
 // One operand's loads: 32 of 1 KB a stage, four of them this wave's.
-template <Side S>
 struct Loader {
-  const uint16_t* base;   // the tile's first row (ROWS) or column (COLS) of plane 0
+  const uint16_t* base;   // the tile's first row in plane 0
   uint32_t voff[LOADS / 2];
-  uint32_t ld;            // elements
-  int64_t rows;           // COLS: contraction rows there are
-  int64_t plane;
+  int64_t plane, step;
 
-  __device__ __forceinline__ void init(const HeadSide& s, int64_t row0, int wave, int lane) {
-    ld = (uint32_t)s.ld;
+  __device__ __forceinline__ void init(const HeadSide& s, int tile, int wave, int lane) {
     plane = s.plane;
-    if constexpr (S == ROWS) {
-      base = s.p + row0 * s.ld;
-      const int last = (int)(s.rows - 1 - row0 < 255 ? s.rows - 1 - row0 : 255);   // rows past the end repeat the last one
+    step = s.step;
+    base = s.p + tile * s.tile;
+    const int64_t row0 = (int64_t)tile * HEAD_TILE;
+    const int last = (int)(s.rows - 1 - row0 < 255 ? s.rows - 1 - row0 : 255);   // rows past the end repeat the last one
 #pragma unroll
-      for (int q = 0; q < LOADS / 2; ++q) {
-        const int r = (wave + q * NW) * 8 + lane / CPR;
-        const int c = (lane % CPR) ^ ((r / G::RPP) % CPR);
-        voff[q] = ((uint32_t)(r < last ? r : last) * ld + c * 8) * 2;
-      }
-    } else {
-      base = s.p + row0;
-      rows = s.rows;
-      const int last = (int)(s.cols - 8 - row0 < 248 ? s.cols - 8 - row0 : 248);   // columns past the end repeat the last eight
-#pragma unroll
-      for (int q = 0; q < LOADS / 2; ++q) {
-        const int k = (wave + q * NW) * 2 + lane / 32;
-        const int c = swz_chunk<3>(k, lane % 32) * 8;
-        voff[q] = ((uint32_t)k * ld + (c < last ? c : last)) * 2;
-      }
+    for (int q = 0; q < LOADS / 2; ++q) {
+      const int r = (wave + q * NW) * 8 + lane / CPR;
+      const int c = (lane % CPR) ^ ((r / G::RPP) % CPR);
+      voff[q] = ((uint32_t)(r < last ? r : last) * (uint32_t)s.ld + c * 8) * 2;
     }
   }
-  // Load q of stage kt of a plane.
-  __device__ __forceinline__ void load(int p, int kt, int q, int wave, int lane, uint32_t lds) const {
-    const uint16_t* at = base + p * plane;
-    uint32_t v = voff[q];
-    if constexpr (S == ROWS) {
-      at += kt * BK;
-    } else {
-      const int64_t k0 = (int64_t)kt * BK;
-      at += k0 * ld;
-      if (k0 + BK > rows) {   // rows of the contraction past the end repeat the last one: the other side is zero there
-        const int k = (wave + q * NW) * 2 + lane / 32, last = (int)(rows - 1 - k0);
-        if (k > last) v -= (uint32_t)(k - last) * ld * 2;
-      }
-    }
-    dma16(buf_rsrc(at), v, 0u, lds);
-  }
-  __device__ static constexpr int dst(int wave, int q) { return (wave + q * NW) * 1024; }
-};
-
-// A wave's fragments of one operand: N blocks of 16 rows from row `first` of the tile.
-template <Side S, int N>
-struct Reader {
-  int off[S == ROWS ? H : N * 2];
-
-  __device__ __forceinline__ void init(int first, int lane) {
-    if constexpr (S == ROWS) {
-#pragma unroll
-      for (int h = 0; h < H; ++h) off[h] = G::swz_rk(first + (lane & 15), 4 * h + (lane >> 4));
-    } else {
-      const int r = (lane & 15) >> 2, q = lane & 3;
-#pragma unroll
-      for (int a = 0; a < N; ++a)
-#pragma unroll
-        for (int r2 = 0; r2 < 2; ++r2) off[2 * a + r2] = swz_kn<3>(8 * (lane >> 4) + 4 * r2 + r, first + a * 16 + 4 * q);
-    }
-  }
-  __device__ __forceinline__ bf16x8 read(const char* st, int h, int a) const {
-    if constexpr (S == ROWS) {
-      return *reinterpret_cast<const bf16x8*>(st + off[h] + a * 16 * RB);
-    } else {
-      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(st + off[2 * a] + h * 32 * KN_ROW));
-      const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(st + off[2 * a + 1] + h * 32 * KN_ROW));
-      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
+  // Stage kt of a plane.
+  __device__ __forceinline__ uint64_t at(int p, int kt) const {
+    return reinterpret_cast<uint64_t>(base + p * plane + kt * step);
   }
 };
 
+// A tile's product: prime() starts the loads of its first stages, arrived() waits for this wave's,
+// run() does the rest.
 // acc[a][b][e] = C(row0 + wr TM + 16 b + lane % 16, col0 + wc TN + 16 a + 4 (lane / 16) + e).
-template <Side SA, Side SB>
-__device__ __forceinline__ void product(const HeadProduct& g, int64_t row0, int64_t col0, char* lds, f32x4 (&acc)[NA][NB]) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wr = wave / (NW / 2), wc = wave % (NW / 2);
-  Loader<SA> la;
-  Loader<SB> lb;
-  la.init(g.a, row0, wave, lane);
-  lb.init(g.b, col0, wave, lane);
-  Reader<SA, NB> ra;
-  Reader<SB, NA> rb;
-  ra.init(wr * TM, lane);
-  rb.init(wc * TN, lane);
+struct Product {
+  const HeadProduct& g;
+  char* const lds;
+  const int lane, wave;
+  Loader la, lb;
+  int kt0, KT;   // stages of the contraction, for each pair of planes
+  // The next stage to load: its pair of planes, how many stages of that are left, where they lie.
+  int pair, left;
+  uint64_t at_a, at_b;
+  uint32_t at_lds;
+
+  __device__ __forceinline__ Product(const HeadProduct& g_, char* lds_)
+      : g(g_), lds(lds_), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) {}
+
+  __device__ __forceinline__ static i32x4 rsrc(uint64_t at) {   // as buf_rsrc: addresses have 48 bits
+    return i32x4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), -1, 0x00020000};
+  }
+  __device__ __forceinline__ void issue(int q) const {
+    if (q < LOADS / 2) dma16(rsrc(at_a), la.voff[q], 0u, at_lds + q * NW * 1024);
+    else dma16(rsrc(at_b), lb.voff[q - LOADS / 2], 0u, at_lds + G::OPER_BYTES + (q - LOADS / 2) * NW * 1024);
+  }
+  __device__ __forceinline__ void start_pair() {
+    at_a = la.at((int)(g.pair_a >> (4 * pair)) & 15, kt0);
+    at_b = lb.at((int)(g.pair_b >> (4 * pair)) & 15, kt0);
+    left = KT;
+  }
+  // Past the stage that was loaded last.
+  __device__ __forceinline__ void advance() {
+    at_a += 2 * la.step;
+    at_b += 2 * lb.step;
+    at_lds ^= G::STAGE_BYTES;
+    if (--left == 0) {
+      ++pair;
+      start_pair();
+    }
+  }
+
+  // No wave reads the ring any more.
+  __device__ __forceinline__ void prime(int tile_a, int tile_b, int first, int count) {
+    kt0 = first;
+    KT = count;
+    la.init(g.a, tile_a, wave, lane);
+    lb.init(g.b, tile_b, wave, lane);
+    pair = 0;
+    at_lds = lds_u32(lds) + wave * 1024;
+    start_pair();
+    const int total = KT * g.pairs;
 #pragma unroll
-  for (int a = 0; a < NA; ++a)
+    for (int s = 0; s < STAGES; ++s)
+      if (s < total) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  bf16x8 fa[2][NB], fb[2][NA];
-  const int KT = (int)((g.k + BK - 1) / BK);
-  const int total = KT * g.pairs;
-  pipeline<G, 1, LOADS / 2>(
-      total, LOADS, lds,
-      [&](int st, int q) {
-        // The pair of planes, the stage of the contraction.
-        const int p = (st >= KT) + (st >= 2 * KT) + (st >= 3 * KT) + (st >= 4 * KT) + (st >= 5 * KT), kt = st - p * KT;
-        const uint32_t at = lds_u32(lds + (st % STAGES) * G::STAGE_BYTES);
-        if (q < LOADS / 2) la.load((int)(g.pair_a >> (4 * p)) & 15, kt, q, wave, lane, at + la.dst(wave, q));
-        else lb.load((int)(g.pair_b >> (4 * p)) & 15, kt, q - LOADS / 2, wave, lane, at + G::OPER_BYTES + lb.dst(wave, q - LOADS / 2));
-      },
-      [&](int buf, const char* st, int h) {
+        for (int q = 0; q < LOADS; ++q) issue(q);
+        advance();
+      }
+  }
+
+  __device__ __forceinline__ void arrived() const {
+    asm volatile("" ::: "memory");
+    wait_vm_c<0>();
+  }
+
+  // Two stages of loads: at the barrier that closes stage st, stage st + 1 has arrived and every wave is
+  // done with the slot of stage st, which then receives stage st + 2; half of its loads go out at
+  // once, half from among the products that follow.  Fragments are read one sub-step ahead.
+  __device__ __forceinline__ void run(f32x4 (&acc)[NA][NB]) {
+    const int wr = wave / (NW / 2), wc = wave % (NW / 2);
+    // Block b's fragment lies 16 b rows below block 0's: 16 rows keep the swizzle's phase.
+    int oa[H], ob[H];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) fa[buf][b] = ra.read(st, h, b);
+    for (int h = 0; h < H; ++h) {
+      oa[h] = G::swz_rk(wr * TM + (lane & 15), 4 * h + (lane >> 4));
+      ob[h] = G::OPER_BYTES + G::swz_rk(wc * TN + (lane & 15), 4 * h + (lane >> 4));
+    }
 #pragma unroll
-        for (int a = 0; a < NA; ++a) fb[buf][a] = rb.read(st + G::OPER_BYTES, h, a);
-      },
-      [](int, int, const char*) {},
-      [&](int buf, auto&& after) {
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int total = KT * g.pairs;
+    if (total == 0) return;
+    bf16x8 fa[2][NB], fb[2][NA];
+    auto read = [&](int buf, const char* st, int h) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) fa[buf][b] = *reinterpret_cast<const bf16x8*>(st + oa[h] + b * 16 * RB);
+#pragma unroll
+      for (int a = 0; a < NA; ++a) fb[buf][a] = *reinterpret_cast<const bf16x8*>(st + ob[h] + a * 16 * RB);
+    };
+    __builtin_amdgcn_s_barrier();   // every wave's loads have arrived
+    asm volatile("" ::: "memory");
+    read(0, lds, 0);
+    auto stage = [&](const int st, auto steady_tag) {
+      constexpr bool steady = decltype(steady_tag)::value;   // stage st + 2 exists
+      const char* const slot = lds + (st & 1) * G::STAGE_BYTES;
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        const int c = h & 1;
+        if (h + 1 < H) {
+          read(c ^ 1, slot, h + 1);
+        } else if (steady || st + 1 < total) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's reads of the stage are done
+          wait_vm_c<0>();
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          if constexpr (steady) {
+#pragma unroll
+            for (int q = LOADS / 2; q < LOADS; ++q) issue(q);
+          }
+          read(c ^ 1, lds + ((st + 1) & 1) * G::STAGE_BYTES, 0);
+        }
 #pragma unroll
         for (int a = 0; a < NA; ++a)
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
-            acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[buf][a], fa[buf][b], acc[a][b], 0, 0, 0);
-            after(a * NB + b);
+            acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[c][a], fa[c][b], acc[a][b], 0, 0, 0);
+            if (steady && h == H - 1 && a * NB + b < LOADS / 2) issue(a * NB + b);
           }
-      });
+#pragma unroll
+        for (int j = 0; j < NA * NB; ++j) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // one product
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // one LDS read
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (steady) advance();
+    };
+    int st = 0;
+    for (; st < total - STAGES; ++st) stage(st, std::true_type{});
+    for (; st < total; ++st) stage(st, std::false_type{});
+  }
+};
+
+// All waves are done with what they read of LDS.
+__device__ __forceinline__ void lds_free() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
-__device__ __forceinline__ int64_t label_of(const HeadLabels& l, int64_t r, int64_t vocab) {
+__device__ __forceinline__ int label_of(const HeadLabels& l, int64_t r, int64_t vocab) {
   const int64_t y = load_id(l.labels, l.wide, r * l.stride);
-  return (uint64_t)y < (uint64_t)vocab ? y : -1;
+  return (uint64_t)y < (uint64_t)vocab ? (int)y : -1;
 }
 
 }  // namespace
 
+// A workgroup takes every 32nd tile of its XCD's.  While a tile's sums are formed in registers,
+// the next one's first stages arrive.
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void head_first_kernel(HeadLogits a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  const TileAt t = tile_at(blockIdx.x, a.g.tiles_m, a.g.tiles_n);
+  int block = blockIdx.x;
+  TileAt t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
   if (t.i < 0) return;
-  const int64_t row0 = (int64_t)t.i * HEAD_TILE, col0 = (int64_t)t.j * HEAD_TILE;
-  f32x4 acc[NA][NB];
-  product<ROWS, ROWS>(a.g, row0, col0, lds, acc);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wr = wave / (NW / 2), wc = wave % (NW / 2), g = lane >> 4;
-  malt_f32x2* const join = reinterpret_cast<malt_f32x2*>(lds);   // [row][wave column]
-  __syncthreads();   // every wave is done with the ring
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int ml = wr * TM + b * 16 + (lane & 15);
-    const int64_t m = row0 + ml, c = col0 + wc * TN + 4 * g;
-    const int64_t y = m < a.g.m ? label_of(a.rows, m, a.vocab) : -1;
-    // The label's and the end's place from this lane's first column.
-    const int yl = y < 0 ? -1 : (int)(y - c), left = (int)(a.g.n - c);
-    float top = -__builtin_inff(), sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < NA; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float z = acc[i][b][e] * LOG2E;
-        if (yl == 16 * i + e) gptr(a.at_label)[m] = z;
-        if (yl == 16 * i + e || 16 * i + e >= left) z = -__builtin_inff();
-        acc[i][b][e] = z;
-        top = fmaxf(top, z);
-      }
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float ref = top == -__builtin_inff() ? 0.f : top;
-#pragma unroll
-    for (int i = 0; i < NA; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(acc[i][b][e] - ref);
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
-    if (g == 0) join[ml * (NW / 2) + wc] = malt_f32x2{top, sum};
-  }
-  __syncthreads();
-  const int64_t m = row0 + threadIdx.x;
-  if (threadIdx.x < HEAD_TILE && m < a.g.m) {
-    float top = -__builtin_inff(), sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < NW / 2; ++i) top = fmaxf(top, join[threadIdx.x * (NW / 2) + i].x);
-    const float ref = top == -__builtin_inff() ? 0.f : top;
-#pragma unroll
-    for (int i = 0; i < NW / 2; ++i) {
-      const malt_f32x2 v = join[threadIdx.x * (NW / 2) + i];
-      sum += v.y * __builtin_amdgcn_exp2f(v.x - ref);
+  Product product(a.g, lds);
+  const int lane = product.lane, wave = product.wave, wr = wave / (NW / 2), wc = wave % (NW / 2), g = lane >> 4;
+  const int KT = stages_of(a.g);
+  product.prime(t.i, t.j, 0, KT);
+  int* const labels = reinterpret_cast<int*>(lds + AT_ROWS);   // [2][row]
+  auto row_label = [&](int i) {
+    const int64_t m = (int64_t)i * HEAD_TILE + threadIdx.x;
+    return threadIdx.x < HEAD_TILE && m < a.g.m ? label_of(a.rows, m, a.vocab) : -1;
+  };
+  int own = row_label(t.i), turn = 0;
+  product.arrived();
+  malt_f32x2* const join = reinterpret_cast<malt_f32x2*>(lds + AT_EPI);   // [row][wave column]
+  for (;;) {
+    const int64_t row0 = (int64_t)t.i * HEAD_TILE, col0 = (int64_t)t.j * HEAD_TILE;
+    const int tile_n = t.j;
+    if (threadIdx.x < HEAD_TILE) labels[turn * HEAD_TILE + threadIdx.x] = own;
+    f32x4 acc[NA][NB];
+    product.run(acc);
+    lds_free();
+    block += CUS;
+    t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
+    if (t.i >= 0) {
+      product.prime(t.i, t.j, 0, KT);
+      own = row_label(t.i);
     }
-    gptr(a.partial)[m * a.parts + t.j] = malt_f32x2{top, sum};
+    const int c = (int)col0 + wc * TN, left = a.g.n - c - 4 * g;   // columns there are from this lane's first
+    const bool end = a.g.n - c < TN;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int ml = wr * TM + b * 16 + (lane & 15), yl = labels[turn * HEAD_TILE + ml] - c;   // the label's place in the wave's columns
+      if (end || __builtin_amdgcn_ballot_w64((unsigned)yl < TN)) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool label = yl == 16 * i + 4 * g + e;
+            if (label) gptr(a.at_label)[row0 + ml] = acc[i][b][e] * LOG2E;
+            if (label || 16 * i + e >= left) acc[i][b][e] = -__builtin_inff();
+          }
+      }
+      float top = acc[0][b][0];
+#pragma unroll
+      for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[i][b][e]);
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64)) * LOG2E;
+      const float ref = top == -__builtin_inff() ? 0.f : top;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], LOG2E, -ref));
+      sum += __shfl_xor(sum, 16, 64);
+      sum += __shfl_xor(sum, 32, 64);
+      if (g == 0) join[ml * (NW / 2) + wc] = malt_f32x2{top, sum};
+    }
+    product.arrived();
+    lds_free();
+    const int64_t m = row0 + threadIdx.x;
+    if (threadIdx.x < HEAD_TILE && m < a.g.m) {
+      float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW / 2; ++i) top = fmaxf(top, join[threadIdx.x * (NW / 2) + i].x);
+      const float ref = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+      for (int i = 0; i < NW / 2; ++i) {
+        const malt_f32x2 v = join[threadIdx.x * (NW / 2) + i];
+        sum += v.y * __builtin_amdgcn_exp2f(v.x - ref);
+      }
+      gptr(a.partial)[m * a.parts + tile_n] = malt_f32x2{top, sum};
+    }
+    if (t.i < 0) return;
+    turn ^= 1;
   }
 }
 
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void head_second_kernel(HeadLogits a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  const TileAt t = tile_at(blockIdx.x, a.g.tiles_m, a.g.tiles_n);
+  int block = blockIdx.x;
+  TileAt t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
   if (t.i < 0) return;
-  const int64_t row0 = (int64_t)t.i * HEAD_TILE, col0 = (int64_t)t.j * HEAD_TILE;
-  f32x4 acc[NA][NB];
-  product<ROWS, ROWS>(a.g, row0, col0, lds, acc);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wr = wave / (NW / 2), wc = wave % (NW / 2), g = lane >> 4;
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int64_t m = row0 + wr * TM + b * 16 + (lane & 15), c = col0 + wc * TN + 4 * g;
-    HeadRow s = {0.f, 0.f, 0.f, 0.f};
-    int64_t y = -1;
-    if (m < a.g.m) {
-      y = label_of(a.rows, m, a.vocab);
-      const f32x4 v = *reinterpret_cast<const MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<const float*>(a.stats + m)));
-      s = HeadRow{v.x, v.y, v.z, 0.f};
-      if (a.rows.weights) {
-        const float w = gptr(a.rows.weights)[m * a.rows.weight_stride];
-        s.inverse *= w;
-        s.others *= w;
-        if (w == 0.f) y = -1;
-      }
+  Product product(a.g, lds);
+  const int lane = product.lane, wave = product.wave, wr = wave / (NW / 2), wc = wave % (NW / 2), g = lane >> 4;
+  const int KT = stages_of(a.g);
+  product.prime(t.i, t.j, 0, KT);
+  f32x4* const records = reinterpret_cast<f32x4*>(lds + AT_ROWS);   // [2][row]
+  auto record = [&](int i) {
+    return *reinterpret_cast<const MALT_GLOBAL f32x4*>(
+        gptr(reinterpret_cast<const float*>(a.records + (int64_t)i * HEAD_TILE + threadIdx.x % HEAD_TILE)));
+  };
+  f32x4 own = record(t.i);
+  int turn = 0;
+  product.arrived();
+  char* const sto = lds + AT_EPI + wave * OUT_WAVE;
+  for (;;) {
+    const int64_t col0 = (int64_t)t.j * HEAD_TILE;
+    const int tile_m = t.i, tile_n = t.j;
+    if (threadIdx.x < HEAD_TILE) records[turn * HEAD_TILE + threadIdx.x] = own;
+    f32x4 acc[NA][NB];
+    product.run(acc);
+    lds_free();
+    block += CUS;
+    t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
+    if (t.i >= 0) {
+      product.prime(t.i, t.j, 0, KT);
+      own = record(t.i);
     }
-    const int yl = (int)(y - a.col0 - c), left = (int)(a.g.n - c);
+    const int c = (int)col0 + wc * TN, left = a.g.n - c - 4 * g;
+    const bool end = a.g.n - c < TN;
 #pragma unroll
-    for (int i = 0; i < NA; ++i)
+    for (int b = 0; b < NB; ++b) {
+      const f32x4 s = records[turn * HEAD_TILE + wr * TM + b * 16 + (lane & 15)];
+      const int y = __float_as_int(s.w), yl = y < 0 ? -1 : y - (int)a.col0 - c;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float q = __builtin_amdgcn_exp2f(acc[i][b][e] * LOG2E - s.top) * s.inverse;
+      for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          acc[i][b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], LOG2E, -s.x)) * s.y;
+      if (end || __builtin_amdgcn_ballot_w64(y < 0 || (unsigned)yl < TN)) {
         // Zeros in rows that have no gradient, whatever their logits are, and past the end.
-        acc[i][b][e] = y < 0 || 16 * i + e >= left ? 0.f : yl == 16 * i + e ? -s.others : q;
-      }
-  }
-  __syncthreads();   // every wave is done with the ring
-  char* const sto = lds + wave * (TM * OUT_PITCH);
-  const int sr0 = lane & 15, sc0 = 4 * g;
-  for (int p = 0; p < a.dz_planes; ++p) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+        for (int i = 0; i < NA; ++i)
 #pragma unroll
-      for (int i = 0; i < NA; ++i) {
-        uint2 pk;
-        pk.x = pack_bf16x2(acc[i][b][0], acc[i][b][1]);
-        pk.y = pack_bf16x2(acc[i][b][2], acc[i][b][3]);
-        *reinterpret_cast<uint2*>(sto + (sr0 + b * 16) * OUT_PITCH + (sc0 + i * 16) * 2) = pk;
-        acc[i][b][0] -= bf16_lo(pk.x);
-        acc[i][b][1] -= bf16_hi(pk.x);
-        acc[i][b][2] -= bf16_lo(pk.y);
-        acc[i][b][3] -= bf16_hi(pk.y);
+          for (int e = 0; e < 4; ++e)
+            acc[i][b][e] = y < 0 || 16 * i + e >= left ? 0.f : yl == 16 * i + 4 * g + e ? -s.z : acc[i][b][e];
       }
-    // The wave's own region: its LDS instructions run in order.
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-    bf16_t* const dz = a.dz + p * a.dz_plane;
-#pragma unroll 4
-    for (int it = 0; it < TM * 8 / 64; ++it) {
-      const int r = lane / 8 + 8 * it, ch = lane % 8;
-      const char* src = sto + r * OUT_PITCH + ch * 16;
-      const uint2 lo = *reinterpret_cast<const uint2*>(src);
-      const uint2 hi = *reinterpret_cast<const uint2*>(src + 8);
-      const u32x4 v = {lo.x, lo.y, hi.x, hi.y};
-      *reinterpret_cast<MALT_GLOBAL u32x4*>(gptr(dz) + (row0 + wr * TM + r) * a.dz_ld + col0 + wc * TN + ch * 8) = v;
     }
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
+    // The next tile's loads are waited for before the stores go out: loads and stores may complete in any
+    // order, and waiting for both would put the stores' time between two tiles.
+    product.arrived();
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      for (int p = 0; p < a.dz_planes; ++p) {
+        uint2 pk[NA];
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+          pk[i].x = pack_bf16x2(acc[i][b][0], acc[i][b][1]);
+          pk[i].y = pack_bf16x2(acc[i][b][2], acc[i][b][3]);
+          if (p + 1 < a.dz_planes) {
+            acc[i][b][0] -= bf16_lo(pk[i].x);
+            acc[i][b][1] -= bf16_hi(pk[i].x);
+            acc[i][b][2] -= bf16_lo(pk[i].y);
+            acc[i][b][3] -= bf16_hi(pk[i].y);
+          }
+        }
+        if (a.dz_t) {
+          // Lane p of a quad takes column p of its four rows.
+          bf16_t* const out = a.dz_t + p * a.dz_plane + tile_n * a.dz_t_tile + (tile_m * 4 + wr * 2 + b / 4) * HEAD_BLOCK +
+                              (wc * TN + 4 * g + (lane & 3)) * BK + b % 4 * 16 + (lane & 12);
+#pragma unroll
+          for (int i = 0; i < NA; ++i) {
+            const uint2 q = quad_transpose(pk[i], lane & 3);
+            *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(out) + 16 * i * BK) = op_u32x2{q.x, q.y};
+          }
+        }
+        if (a.dz) {
+#pragma unroll
+          for (int i = 0; i < NA; ++i) *reinterpret_cast<uint2*>(sto + (lane & 15) * OUT_PITCH + (4 * g + i * 16) * 2) = pk[i];
+          // The wave's own region: its LDS instructions run in order.
+          asm volatile("" ::: "memory");
+          __builtin_amdgcn_wave_barrier();
+          bf16_t* const dz = a.dz + p * a.dz_plane + tile_m * a.dz_tile + (tile_n * 4 + wc) * HEAD_BLOCK + (wr * TM + b * 16) * BK;
+#pragma unroll
+          for (int it = 0; it < 2; ++it) {
+            const int r = lane / 8 + 8 * it, ch = lane % 8;
+            const char* src = sto + r * OUT_PITCH + ch * 16;
+            const uint2 lo = *reinterpret_cast<const uint2*>(src);
+            const uint2 hi = *reinterpret_cast<const uint2*>(src + 8);
+            const u32x4 v = {lo.x, lo.y, hi.x, hi.y};
+            *reinterpret_cast<MALT_GLOBAL u32x4*>(gptr(dz) + r * BK + ch * 8) = v;
+          }
+          asm volatile("" ::: "memory");
+          __builtin_amdgcn_wave_barrier();
+        }
+      }
+    }
+    if (t.i < 0) return;
+    turn ^= 1;
   }
 }
 
 namespace {
 
+// Columns n .. n + 3 of row m of a result, from their sums.
 template <class T>
-__device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, float scale, int64_t row0, int64_t col0,
+__device__ __forceinline__ void write4(const HeadOut& o, const HeadGrads& a, float scale, bool none, int64_t m, int64_t n, op_f32x4 v) {
+  T* const out = static_cast<T*>(o.out) + m * o.ldo;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = none || scale == 0.f ? 0.f : v[e] * scale;
+  if (o.accumulate) {
+    const op_f32x4 u = row_load4(out, n, o.g.n);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += u[e];
+  }
+  row_store4(out, n, o.g.n, v);
+}
+// Rows that have no gradient.
+__device__ __forceinline__ bool row_without(const HeadOut& o, const HeadGrads& a, int64_t m) {
+  return o.mask_rows && gptr(reinterpret_cast<const int32_t*>(a.records + m))[3] < 0;
+}
+__device__ __forceinline__ float scale_of(const HeadGrads& a) { return a.scale_at ? a.scale * gptr(a.scale_at)[0] : a.scale; }
+
+template <class T>
+__device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, int split, int64_t row0, int64_t col0,
                                           const f32x4 (&acc)[NA][NB]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wr = wave / (NW / 2), wc = wave % (NW / 2);
+  const float scale = scale_of(a);
+  float* const partial = o.partial + split * ((int64_t)o.g.m * o.g.n);
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     const int64_t m = row0 + wr * TM + b * 16 + (lane & 15);
     if (m >= o.g.m) continue;
-    bool none = false;
-    if (o.mask_rows)
-      none = label_of(a.rows, m, a.vocab) < 0 || (a.rows.weights && gptr(a.rows.weights)[m * a.rows.weight_stride] == 0.f);
+    const bool none = row_without(o, a, m);
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
       const int64_t n = col0 + wc * TN + i * 16 + 4 * (lane >> 4);
       if (n >= o.g.n) continue;
       op_f32x4 v = {acc[i][b][0], acc[i][b][1], acc[i][b][2], acc[i][b][3]};
       if (o.add_partial) {
-        const op_f32x4 u = row_load4(o.partial + m * o.g.n, n, o.g.n);
+        const op_f32x4 u = row_load4(partial + m * o.g.n, n, o.g.n);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += u[e];
       }
-      if (o.write_partial) {
-        row_store4(o.partial + m * o.g.n, n, o.g.n, v);
-        continue;
-      }
-      T* const out = static_cast<T*>(o.out) + m * o.ldo;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = none || scale == 0.f ? 0.f : v[e] * scale;
-      if (o.accumulate) {
-        const op_f32x4 u = row_load4(out, n, o.g.n);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += u[e];
-      }
-      row_store4(out, n, o.g.n, v);
+      if (o.write_partial) row_store4(partial + m * o.g.n, n, o.g.n, v);
+      else write4<T>(o, a, scale, none, m, n, v);
     }
   }
 }
@@ -372,22 +487,40 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void head_grads_kernel(HeadGrads a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   int b = blockIdx.x, which = 0;
-  const int first = tile_blocks(a.part[0].g.tiles_m, a.part[0].g.tiles_n);
+  const int first = tile_blocks(a.part[0].g.tiles_m, a.part[0].g.tiles_n, a.part[0].splits);
   if (a.parts > 1 && b >= first) {
     b -= first;
     which = 1;
   }
   const HeadOut& o = a.part[which];
-  const TileAt t = tile_at(b, o.g.tiles_m, o.g.tiles_n);
+  const TileAt t = tile_at(b, o.g.tiles_m, o.g.tiles_n, o.splits);
   if (t.i < 0) return;
+  const int split = t.split;
   const int64_t row0 = (int64_t)t.i * HEAD_TILE, col0 = (int64_t)t.j * HEAD_TILE;
+  const int KT = stages_of(o.g), kt0 = (int)((int64_t)KT * split / o.splits), kt1 = (int)((int64_t)KT * (split + 1) / o.splits);
   f32x4 acc[NA][NB];
-  if (o.form == 0) product<ROWS, COLS>(o.g, row0, col0, lds, acc);
-  else product<COLS, COLS>(o.g, row0, col0, lds, acc);
-  float scale = a.scale;
-  if (a.scale_at) scale *= gptr(a.scale_at)[0];
-  if (o.f32) write_out<float>(o, a, scale, row0, col0, acc);
-  else write_out<bf16_t>(o, a, scale, row0, col0, acc);
+  Product product(o.g, lds);
+  product.prime(t.i, t.j, kt0, kt1 - kt0);
+  product.arrived();
+  product.run(acc);
+  if (o.f32) write_out<float>(o, a, split, row0, col0, acc);
+  else write_out<bf16_t>(o, a, split, row0, col0, acc);
+}
+
+// The sum of a contraction's parts, four columns a thread.
+template <class T>
+__global__ __launch_bounds__(256) void head_sum_kernel(HeadOut o, HeadGrads a) {
+  const int64_t per = (o.g.n + 3) / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / per, n = i % per * 4;
+  if (m >= o.g.m) return;
+  const float* p = o.partial + m * o.g.n;
+  op_f32x4 v = row_load4(p, n, o.g.n);
+  for (int s = 1; s < o.splits; ++s) {
+    p += (int64_t)o.g.m * o.g.n;
+    const op_f32x4 u = row_load4(p, n, o.g.n);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += u[e];
+  }
+  write4<T>(o, a, scale_of(a), row_without(o, a, m), m, n, v);
 }
 
 // The kernels use more dynamic LDS than the default limit: raised once for each device.
@@ -408,16 +541,24 @@ hipError_t head_setup() {
 }
 
 hipError_t launch_head_logits(const HeadLogits& a, bool second, hipStream_t s) {
-  const dim3 grid((unsigned)tile_blocks(a.g.tiles_m, a.g.tiles_n));
+  const int blocks = tile_blocks(a.g.tiles_m, a.g.tiles_n, 1);
+  const dim3 grid((unsigned)(blocks < CUS ? blocks : CUS));
   if (second) hipLaunchKernelGGL(head_second_kernel, grid, dim3(NT), LDS_BYTES, s, a);
   else hipLaunchKernelGGL(head_first_kernel, grid, dim3(NT), LDS_BYTES, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_head_grads(const HeadGrads& a, hipStream_t s) {
-  int blocks = tile_blocks(a.part[0].g.tiles_m, a.part[0].g.tiles_n);
-  if (a.parts > 1) blocks += tile_blocks(a.part[1].g.tiles_m, a.part[1].g.tiles_n);
+  int blocks = 0;
+  for (int i = 0; i < a.parts; ++i) blocks += tile_blocks(a.part[i].g.tiles_m, a.part[i].g.tiles_n, a.part[i].splits);
   hipLaunchKernelGGL(head_grads_kernel, dim3((unsigned)blocks), dim3(NT), LDS_BYTES, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_sum(const HeadOut& o, const HeadGrads& a, hipStream_t s) {
+  const dim3 grid((unsigned)(((int64_t)o.g.m * ((o.g.n + 3) / 4) + 255) / 256));
+  if (o.f32) hipLaunchKernelGGL(head_sum_kernel<float>, grid, dim3(256), 0, s, o, a);
+  else hipLaunchKernelGGL(head_sum_kernel<bf16_t>, grid, dim3(256), 0, s, o, a);
   return hipGetLastError();
 }
 

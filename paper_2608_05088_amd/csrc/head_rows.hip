@@ -25,35 +25,82 @@ __device__ __forceinline__ int64_t label_of(const HeadLabels& l, int64_t r, int6
 }
 
 // ---------------------------------------------------------------------- packing
-// Four columns a thread.
-template <class T>
-__global__ __launch_bounds__(256) void head_pack_kernel(HeadPack a) {
-  const int64_t per = a.pitch / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= a.out_rows * per) return;
-  const int64_t r = i / per, c = i % per * 4;
-  op_f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (r < a.rows && (!a.labels.labels || label_of(a.labels, r, a.vocab) >= 0))
-    v = row_load4(static_cast<const T*>(a.x) + r * a.ld, c, a.cols);
-  uint16_t* out = a.out + r * a.pitch + c;
-  for (int p = 0; p < a.planes; ++p) {
+// Rows that stay: those with a label and a weight, or all.
+__device__ __forceinline__ bool stays(const HeadLabels& l, int64_t r, int64_t vocab) {
+  return !l.labels || (label_of(l, r, vocab) >= 0 && (!l.weights || gptr(l.weights)[r * l.weight_stride] != 0.f));
+}
+
+// Four values as planes.  What a plane leaves is exact: its bits are those of v past the plane's.  An
+// infinity leaves nothing.
+__device__ __forceinline__ void store_planes(uint16_t* out, int64_t plane, int planes, op_f32x4 v) {
+  for (int p = 0; p < planes; ++p) {
     const uint32_t lo = pack_bf16x2(v.x, v.y), hi = pack_bf16x2(v.z, v.w);
-    *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(out)) = op_u32x2{lo, hi};
-    // What is left is exact: its bits are those of v past the plane's.  An infinity leaves nothing.
+    *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(out) + p * plane) = op_u32x2{lo, hi};
     const float h[4] = {bf16_lo(lo), bf16_hi(lo), bf16_lo(hi), bf16_hi(hi)};
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = fabsf(h[j]) == __builtin_inff() ? 0.f : v[j] - h[j];
-    out += a.plane;
   }
 }
 
-// Rows of weight 0 become zeros, after the losses were formed from them: their gradient is
-// zero whatever they hold.
-__global__ __launch_bounds__(256) void head_clear_kernel(HeadPack a) {
-  const int64_t r = blockIdx.x;
-  if (gptr(a.labels.weights)[r * a.labels.weight_stride] != 0.f) return;
-  for (int p = 0; p < a.planes; ++p)
-    for (int64_t c = 4 * threadIdx.x; c < a.pitch; c += 1024)
-      *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(a.out) + p * a.plane + r * a.pitch + c) = op_u32x2{0u, 0u};
+// Where value c of row r lies in a plane whose rows hold `cols`.
+__device__ __forceinline__ int64_t packed_at(int64_t r, int64_t c, int64_t cols) {
+  return (r / HEAD_TILE * (cols / HEAD_BK) + c / HEAD_BK) * HEAD_BLOCK + r % HEAD_TILE * HEAD_BK + c % HEAD_BK;
+}
+
+// Four columns a thread.
+template <class T>
+__global__ __launch_bounds__(256) void head_pack_kernel(HeadPack a) {
+  const int64_t per = a.out_cols / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= a.out_rows * per) return;
+  const int64_t r = i / per, c = i % per * 4;
+  op_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (r < a.rows && stays(a.labels, r, a.vocab)) v = row_load4(static_cast<const T*>(a.x) + r * a.ld, c, a.cols);
+  store_planes(a.out + packed_at(r, c, a.out_cols), a.plane, a.planes, v);
+}
+
+// The transpose of a 64 x 64 tile through LDS; rows past the end are zeros.
+template <class T>
+__global__ __launch_bounds__(256) void head_pack_t_kernel(HeadPack a, int tiles_r) {
+  __shared__ float tile[64][65];
+  const int64_t r0 = (int64_t)(blockIdx.x % tiles_r) * 64, c0 = (int64_t)(blockIdx.x / tiles_r) * 64;
+  const int lo = threadIdx.x & 15, hi = threadIdx.x >> 4;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int64_t r = r0 + hi + 16 * k;
+    op_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (r < a.rows && stays(a.labels, r, a.vocab)) v = row_load4(static_cast<const T*>(a.x) + r * a.ld, c0 + 4 * lo, a.cols);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) tile[hi + 16 * k][4 * lo + j] = v[j];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int c = hi + 16 * k;
+    if (c0 + c >= a.out_rows) continue;
+    const op_f32x4 v = {tile[4 * lo][c], tile[4 * lo + 1][c], tile[4 * lo + 2][c], tile[4 * lo + 3][c]};
+    store_planes(a.out + packed_at(c0 + c, r0 + 4 * lo, a.out_cols), a.plane, a.planes, v);
+  }
+}
+
+// What the second pass asks about a row.
+__global__ __launch_bounds__(256) void head_records_kernel(HeadLabels l, int64_t rows, int64_t rows_pad, int64_t vocab,
+                                                           const HeadRow* stats, HeadRow* records) {
+  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (r >= rows_pad) return;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  int64_t y = -1;
+  if (r < rows) {
+    y = label_of(l, r, vocab);
+    v = *reinterpret_cast<const MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<const float*>(stats + r)));
+    if (l.weights) {
+      const float w = gptr(l.weights)[r * l.weight_stride];
+      v.y *= w;
+      v.z *= w;
+      if (w == 0.f) y = -1;
+    }
+  }
+  v.w = __int_as_float((int)y);
+  *reinterpret_cast<MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<float*>(records + r))) = v;
 }
 
 // --------------------------------------------------------------------- few rows
@@ -265,14 +312,23 @@ hipError_t launch_head_join(const HeadLabels& rows, int64_t m, int64_t vocab, co
 }
 
 hipError_t launch_head_pack(const HeadPack& a, bool f32, hipStream_t s) {
-  const dim3 grid((unsigned)((a.out_rows * (a.pitch / 4) + 255) / 256));
+  const dim3 grid((unsigned)((a.out_rows * (a.out_cols / 4) + 255) / 256));
   if (f32) hipLaunchKernelGGL((head_pack_kernel<float>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((head_pack_kernel<bf16_t>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-hipError_t launch_head_clear(const HeadPack& a, hipStream_t s) {
-  hipLaunchKernelGGL(head_clear_kernel, dim3((unsigned)a.rows), dim3(256), 0, s, a);
+hipError_t launch_head_pack_t(const HeadPack& a, bool f32, hipStream_t s) {
+  const int tiles_r = (int)(a.out_cols / 64);
+  const dim3 grid((unsigned)(tiles_r * ((a.out_rows + 63) / 64)));
+  if (f32) hipLaunchKernelGGL((head_pack_t_kernel<float>), grid, dim3(256), 0, s, a, tiles_r);
+  else hipLaunchKernelGGL((head_pack_t_kernel<bf16_t>), grid, dim3(256), 0, s, a, tiles_r);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_records(const HeadLabels& l, int64_t rows, int64_t rows_pad, int64_t vocab, const HeadRow* stats,
+                               HeadRow* records, hipStream_t s) {
+  hipLaunchKernelGGL(head_records_kernel, dim3((unsigned)((rows_pad + 255) / 256)), dim3(256), 0, s, l, rows, rows_pad, vocab, stats, records);
   return hipGetLastError();
 }
 

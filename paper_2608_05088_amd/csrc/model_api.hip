@@ -79,7 +79,7 @@ malt_status_t adam_launches(AdamArgs& a, int count, const int64_t* numel, Fill&&
 }
 
 // ------------------------------------------------------------------------- head
-constexpr int64_t kHeadRows = 65536, kHeadInner = 65536, kHeadVocab = int64_t(1) << 25, kHeadWeight = int64_t(1) << 33;
+constexpr int64_t kHeadRows = 65536, kHeadInner = 65536, kHeadVocab = int64_t(1) << 22, kHeadWeight = int64_t(1) << 33;
 constexpr int64_t kHeadPiece = int64_t(1) << 28;   // elements of a piece's dz, all planes
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -90,12 +90,32 @@ struct HeadPlan {
   int x_planes, w_planes;
   bool pack_w;           // otherwise the products read the weights as they lie
   int dz_planes;
-  int64_t rows_pad, cols_pad;
+  int64_t rows_pad, cols_pad, vocab_pad;
   int64_t piece;         // vocabulary columns of a piece, a multiple of the tile
   int pieces;
   int parts;             // of a row's statistics
-  size_t partial, at_label, stats, x, w, dz, dx, bytes;
+  int dx_splits, dw_splits;   // parts of the gradients' contractions
+  size_t partial, at_label, stats, records, x, w, x_t, w_t, dz, dz_t, dx, dw, bytes;
 };
+
+// Pairs of planes that make a product of `na` by `nb` planes, small ones first.
+void head_pairs(HeadProduct& g, int na, int nb) {
+  g.pairs = 0;
+  g.pair_a = g.pair_b = 0;
+  for (int s = HEAD_PLANES - 1; s >= 0; --s)
+    for (int i = s < na ? s : na - 1; i >= 0; --i) {
+      const int j = s - i;
+      if (j >= nb) break;
+      g.pair_a |= (uint32_t)i << (4 * g.pairs);
+      g.pair_b |= (uint32_t)j << (4 * g.pairs);
+      ++g.pairs;
+    }
+}
+int head_pair_count(int na, int nb) {
+  HeadProduct g;
+  head_pairs(g, na, nb);
+  return g.pairs;
+}
 
 HeadPlan head_plan(const malt_linear_loss_t& a) {
   HeadPlan L = {};
@@ -124,7 +144,7 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
   if (!a.stats) L.stats = take(size_t(a.rows) * sizeof(HeadRow));
   if (L.grads || !L.few) {
     L.x = take(size_t(L.x_planes) * L.rows_pad * L.cols_pad * 2);
-    if (L.pack_w) L.w = take(size_t(L.w_planes) * a.vocab * L.cols_pad * 2);
+    if (L.pack_w) L.w = take(size_t(L.w_planes) * up(a.vocab, HEAD_TILE) * L.cols_pad * 2);
   }
   if (L.grads) {
     // Pieces of like size, as few as keep dz within its share of memory.
@@ -134,25 +154,42 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     const int64_t pieces = (all + most - 1) / most;
     L.piece = up((all + pieces - 1) / pieces, HEAD_TILE);
     L.pieces = int((all + L.piece - 1) / L.piece);
-    L.dz = take(size_t(L.dz_planes) * L.rows_pad * L.piece * 2);
-    if (a.dx && L.pieces > 1) L.dx = take(size_t(a.rows) * a.inner * 4);
+    L.records = take(size_t(L.rows_pad) * sizeof(HeadRow));
+    L.vocab_pad = L.piece * L.pieces;
+    if (a.dx) {
+      L.w_t = take(size_t(x32 ? L.w_planes : 1) * up(a.inner, HEAD_TILE) * L.vocab_pad * 2);
+      L.dz = take(size_t(L.dz_planes) * L.rows_pad * L.piece * 2);
+    }
+    if (a.dweight) {
+      L.x_t = take(size_t(a.dweight_type == MALT_FLOAT32 ? L.x_planes : 1) * up(a.inner, HEAD_TILE) * L.rows_pad * 2);
+      L.dz_t = take(size_t(L.dz_planes) * L.rows_pad * L.piece * 2);
+    }
+    // A product of few tiles and a long contraction is cut into parts, so that no workgroup has more
+    // stages than a CU's share of them all, and 16 at the least (a part costs its tile in float32, written and read).
+    const int64_t across = up(a.inner, HEAD_TILE) / HEAD_TILE;
+    const int64_t dx_tiles = a.dx ? L.rows_pad / HEAD_TILE * across : 0, dw_tiles = a.dweight ? L.piece / HEAD_TILE * across : 0;
+    const int64_t dx_stages = L.piece / HEAD_BK * head_pair_count(x32 ? L.dz_planes : 1, x32 ? L.w_planes : 1);
+    const int64_t dw_stages = up(a.rows, HEAD_BK) / HEAD_BK *
+                              head_pair_count(a.dweight_type == MALT_FLOAT32 ? L.dz_planes : 1, a.dweight_type == MALT_FLOAT32 ? L.x_planes : 1);
+    int64_t share = (dx_tiles * dx_stages + dw_tiles * dw_stages) / 256;
+    if (share < 16) share = 16;
+    auto parts = [&](int64_t stages, int64_t contraction) {
+      int64_t n = (stages + share - 1) / share;
+      if (n > contraction / HEAD_BK) n = contraction / HEAD_BK;
+      return int(n < 1 ? 1 : n > 64 ? 64 : n);
+    };
+    L.dx_splits = a.dx ? parts(dx_stages, L.piece) : 1;
+    L.dw_splits = a.dweight ? parts(dw_stages, a.rows) : 1;
+    if (a.dx && (L.pieces > 1 || L.dx_splits > 1)) L.dx = take(size_t(L.dx_splits) * a.rows * a.inner * 4);
+    if (L.dw_splits > 1) L.dw = take(size_t(L.dw_splits) * L.piece * a.inner * 4);
   }
   L.bytes = end;
   return L;
 }
 
-// Pairs of planes that make a product of `na` by `nb` planes, small ones first.
-void head_pairs(HeadProduct& g, int na, int nb) {
-  g.pairs = 0;
-  g.pair_a = g.pair_b = 0;
-  for (int s = HEAD_PLANES - 1; s >= 0; --s)
-    for (int i = s < na ? s : na - 1; i >= 0; --i) {
-      const int j = s - i;
-      if (j >= nb) break;
-      g.pair_a |= (uint32_t)i << (4 * g.pairs);
-      g.pair_b |= (uint32_t)j << (4 * g.pairs);
-      ++g.pairs;
-    }
+// A packed operand of `rows` (a multiple of the tile) by `cols` (of the stage).
+HeadSide packed_side(const uint16_t* p, int64_t rows, int64_t cols) {
+  return {p, rows * cols, cols / HEAD_BK * HEAD_BLOCK, HEAD_BLOCK, HEAD_BK, rows};
 }
 
 malt_status_t check_head(const malt_linear_loss_t* a) {
@@ -161,7 +198,8 @@ malt_status_t check_head(const malt_linear_loss_t* a) {
   if (a->inner < 1 || a->inner > kHeadInner) return fail(MALT_ERR_SHAPE, "rows of %lld values (at most %lld)", (long long)a->inner, (long long)kHeadInner);
   if (a->vocab < 1 || a->vocab > kHeadVocab || a->vocab > kHeadWeight / a->inner)
     return fail(MALT_ERR_SHAPE, "a weight of %lld x %lld", (long long)a->vocab, (long long)a->inner);
-  if (a->rows > 0 && up(a->rows, 2048) * up(a->vocab, 1024) > (int64_t(1) << 38))
+  // A grid holds fewer than 2^32 threads, 512 for each 256 x 256 tile.
+  if (a->rows > 0 && up(a->rows, HEAD_TILE) * up(a->vocab, HEAD_TILE) > (int64_t(1) << 38))
     return fail(MALT_ERR_SHAPE, "%lld rows over a vocabulary of %lld", (long long)a->rows, (long long)a->vocab);
   const Mat x = {"x", a->x, a->x_type, a->rows, a->inner, a->ldx}, w = {"weight", a->weight, a->weight_type, a->vocab, a->inner, a->ldw},
             dx = {"dx", a->dx, a->x_type, a->rows, a->inner, a->lddx},
@@ -448,34 +486,33 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
   px.ld = a.ldx;
   px.out = xp;
   px.plane = L.rows_pad * L.cols_pad;
-  px.pitch = L.cols_pad;
   px.out_rows = L.rows_pad;
+  px.out_cols = L.cols_pad;
   px.planes = L.x_planes;
   px.labels = labels;
+  px.labels.weights = nullptr;   // the losses of rows without weight are formed all the same
   px.vocab = a.vocab;
-  HeadSide xs = {xp, px.plane, px.pitch, L.rows_pad, (int32_t)L.cols_pad};
-  HeadSide wside = {static_cast<const uint16_t*>(a.weight), 0, a.ldw, a.vocab, (int32_t)L.cols_pad};
+  HeadSide wside = {static_cast<const uint16_t*>(a.weight), 0, HEAD_TILE * a.ldw, HEAD_BK, (int32_t)a.ldw, a.vocab};
   if (a.rows > 0 && (L.grads || !L.few)) {
     MALT_TRY(launched(launch_head_pack(px, f32x, s), "packing the head's input"));
     if (L.pack_w) {
       HeadPack pw = {};
       pw.x = a.weight;
-      pw.rows = pw.out_rows = a.vocab;
+      pw.rows = a.vocab;
       pw.cols = a.inner;
       pw.ld = a.ldw;
       pw.out = wp;
-      pw.plane = a.vocab * L.cols_pad;
-      pw.pitch = L.cols_pad;
+      pw.out_rows = up(a.vocab, HEAD_TILE);
+      pw.out_cols = L.cols_pad;
+      pw.plane = pw.out_rows * pw.out_cols;
       pw.planes = L.w_planes;
       MALT_TRY(launched(launch_head_pack(pw, f32w, s), "packing the head's weight"));
-      wside.p = wp;
-      wside.plane = pw.plane;
-      wside.ld = L.cols_pad;
+      wside = packed_side(wp, pw.out_rows, pw.out_cols);
     }
   }
 
   HeadLogits z = {};
-  z.g.a = xs;
+  z.g.a = packed_side(xp, L.rows_pad, L.cols_pad);
   z.g.b = wside;
   z.g.m = (int32_t)a.rows;
   z.g.k = L.cols_pad;
@@ -483,7 +520,8 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
   head_pairs(z.g, L.x_planes, L.w_planes);
   z.rows = labels;
   z.vocab = a.vocab;
-  z.stats = stats;
+  HeadRow* const records = reinterpret_cast<HeadRow*>(ws + L.records);
+  z.records = records;
   if (a.rows > 0 && !a.stats_given) {
     malt_f32x2* const partial = reinterpret_cast<malt_f32x2*>(ws + L.partial);
     float* const at_label = reinterpret_cast<float*>(ws + L.at_label);
@@ -513,72 +551,107 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
     MALT_TRY(launched(launch_head_join(labels, a.rows, a.vocab, partial, L.parts, at_label, stats, a.losses, s), "joining the head's statistics"));
   }
   if (!L.grads) return MALT_OK;
-  if (a.rows > 0 && per_row) MALT_TRY(launched(launch_head_clear(px, s), "clearing rows without weight"));
+  if (a.rows > 0) MALT_TRY(launched(launch_head_records(labels, a.rows, L.rows_pad, a.vocab, stats, records, s), "preparing the head's rows"));
 
   HeadGrads gr = {};
-  gr.rows = labels;
-  gr.vocab = a.vocab;
+  gr.records = records;
   gr.scale = a.weights ? 1.f : a.weight_value;
   gr.scale_at = per_row ? nullptr : a.weights;
-  uint16_t* const dz = reinterpret_cast<uint16_t*>(ws + L.dz);
+  uint16_t *const dz = reinterpret_cast<uint16_t*>(ws + L.dz), *const dz_t = reinterpret_cast<uint16_t*>(ws + L.dz_t);
+  const bool want_dx = a.dx && a.rows > 0;
+  HeadSide w_t = {}, x_t = {};
+  const int dx_w = f32x ? L.w_planes : 1, dw_x = a.dweight_type == MALT_FLOAT32 ? L.x_planes : 1;
+  if (want_dx) {
+    HeadPack p = {};
+    p.x = a.weight;
+    p.rows = a.vocab;
+    p.cols = a.inner;
+    p.ld = a.ldw;
+    p.out = reinterpret_cast<uint16_t*>(ws + L.w_t);
+    p.out_rows = a.inner;
+    p.out_cols = L.vocab_pad;
+    p.plane = up(a.inner, HEAD_TILE) * L.vocab_pad;
+    p.planes = dx_w;
+    MALT_TRY(launched(launch_head_pack_t(p, f32w, s), "transposing the head's weight"));
+    w_t = packed_side(p.out, up(a.inner, HEAD_TILE), L.vocab_pad);
+    w_t.rows = a.inner;
+  }
+  if (a.dweight && a.rows > 0) {
+    HeadPack p = px;
+    p.labels = labels;
+    p.out = reinterpret_cast<uint16_t*>(ws + L.x_t);
+    p.out_rows = a.inner;
+    p.out_cols = L.rows_pad;
+    p.plane = up(a.inner, HEAD_TILE) * L.rows_pad;
+    p.planes = dw_x;
+    MALT_TRY(launched(launch_head_pack_t(p, f32x, s), "transposing the head's input"));
+    x_t = packed_side(p.out, up(a.inner, HEAD_TILE), L.rows_pad);
+    x_t.rows = a.inner;
+  }
   for (int p = 0; p < L.pieces; ++p) {
     const int64_t v0 = p * L.piece, n = a.vocab - v0 < L.piece ? a.vocab - v0 : L.piece;
-    const HeadSide dzs = {dz, L.rows_pad * L.piece, L.piece, L.rows_pad, (int32_t)L.piece};
-    HeadSide wv = wside;
-    wv.p += v0 * wv.ld;
-    wv.rows -= v0;
     if (a.rows > 0) {
       HeadLogits second = z;
-      second.g.b = wv;
+      second.g.b.p += v0 / HEAD_TILE * wside.tile;
+      second.g.b.rows -= v0;
       second.g.n = (int32_t)n;
       second.g.tiles_n = int(up(n, HEAD_TILE) / HEAD_TILE);
       second.col0 = v0;
-      second.dz = dz;
-      second.dz_plane = dzs.plane;
-      second.dz_ld = L.piece;
+      second.dz = a.dx ? dz : nullptr;
+      second.dz_t = a.dweight ? dz_t : nullptr;
+      second.dz_plane = L.rows_pad * L.piece;
+      second.dz_tile = L.piece / HEAD_BK * HEAD_BLOCK;
+      second.dz_t_tile = L.rows_pad / HEAD_BK * HEAD_BLOCK;
       second.dz_planes = L.dz_planes;
       MALT_TRY(launched(launch_head_logits(second, true, s), "launching the logits' gradient"));
     }
     gr.parts = 0;
-    if (a.dx && a.rows > 0) {
+    if (want_dx) {
       HeadOut& o = gr.part[gr.parts++];
       o = HeadOut{};
-      o.g.a = dzs;
-      o.g.b = wv;
+      o.g.a = packed_side(dz, L.rows_pad, L.piece);
+      o.g.b = w_t;
+      o.g.b.p += v0 / HEAD_BK * HEAD_BLOCK;
       o.g.m = (int32_t)a.rows;
       o.g.n = (int32_t)a.inner;
       o.g.k = n;
       o.g.tiles_m = int(L.rows_pad / HEAD_TILE);
       o.g.tiles_n = int(up(a.inner, HEAD_TILE) / HEAD_TILE);
-      head_pairs(o.g, f32x ? L.dz_planes : 1, f32x ? L.w_planes : 1);
+      head_pairs(o.g, f32x ? L.dz_planes : 1, dx_w);
       o.out = a.dx;
       o.ldo = a.lddx;
       o.partial = reinterpret_cast<float*>(ws + L.dx);
-      o.form = 0;
-      o.f32 = f32x;
+      o.splits = L.dx_splits;
       o.add_partial = p > 0;
-      o.write_partial = p + 1 < L.pieces;
+      o.write_partial = o.splits > 1 || p + 1 < L.pieces;
+      o.f32 = f32x;
       o.mask_rows = true;
     }
     if (a.dweight) {
       HeadOut& o = gr.part[gr.parts++];
       o = HeadOut{};
       const bool fine = a.dweight_type == MALT_FLOAT32;
-      o.g.a = dzs;
-      o.g.b = xs;
+      o.g.a = packed_side(dz_t, L.piece, L.rows_pad);
+      o.g.b = x_t;
       o.g.m = (int32_t)n;
       o.g.n = (int32_t)a.inner;
       o.g.k = a.rows;
       o.g.tiles_m = int(up(n, HEAD_TILE) / HEAD_TILE);
       o.g.tiles_n = int(up(a.inner, HEAD_TILE) / HEAD_TILE);
-      head_pairs(o.g, fine ? L.dz_planes : 1, fine ? L.x_planes : 1);
+      head_pairs(o.g, fine ? L.dz_planes : 1, dw_x);
       o.out = static_cast<char*>(a.dweight) + v0 * a.lddw * op_dtype_bytes(a.dweight_type);
       o.ldo = a.lddw;
-      o.form = 1;
+      o.partial = reinterpret_cast<float*>(ws + L.dw);
+      o.splits = L.dw_splits;
+      o.write_partial = o.splits > 1;
       o.f32 = fine;
       o.accumulate = a.accumulate != 0;
     }
     MALT_TRY(launched(launch_head_grads(gr, s), "launching the head's gradients"));
+    for (int i = 0; i < gr.parts; ++i) {
+      const HeadOut& o = gr.part[i];
+      if (o.splits > 1 && (!o.mask_rows || p + 1 == L.pieces)) MALT_TRY(launched(launch_head_sum(o, gr, s), "joining the head's gradients"));
+    }
   }
   return MALT_OK;
 }

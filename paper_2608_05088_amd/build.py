@@ -1,5 +1,6 @@
-"""Build libmalt.so (HIP, gfx950) in-tree with hipcc, and the matrix-core
-calibration library libmalt_calib.so beside it.
+"""Build libmalt.so (HIP, gfx950) in-tree with hipcc, and beside it the Python module
+_malt.so (host code on torch's headers) and the matrix-core calibration library
+libmalt_calib.so.
 
 Usage: python -m paper_2608_05088_amd.build [-v]
 """
@@ -14,6 +15,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "lib", "libmalt.so")
+BINDING_LIB = os.path.join(PKG, "lib", "_malt.so")
 CALIB = os.path.join(PKG, "calib")
 CALIB_LIB = os.path.join(PKG, "lib", "libmalt_calib.so")
 SOURCES = ["malt_api.hip", "elementwise.hip", "ns_sym.hip", "ns_update.hip", "ns_mid.hip", "small_ns.hip",
@@ -39,6 +41,17 @@ def build_cmd(out: str = LIB) -> list:
             "-o", out]
 
 
+def binding_cmd(out: str = BINDING_LIB) -> list:
+    import sysconfig
+    from torch.utils import cpp_extension
+    torch_lib = cpp_extension.library_paths()[0]
+    return [hipcc(), "-x", "hip", "--cuda-host-only", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+            "-Wall", "-Wno-unused-function", "-Wno-deprecated-declarations", "-Wno-unused-result",
+            *[f"-I{p}" for p in cpp_extension.include_paths()], "-I", sysconfig.get_paths()["include"],
+            os.path.join(CSRC, "binding.cpp"), "-L", os.path.dirname(LIB), "-l:libmalt.so", "-Wl,-rpath,$ORIGIN",
+            "-L", torch_lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip", "-o", out]
+
+
 def calib_cmd(out: str = CALIB_LIB) -> list:
     return [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -60,10 +73,12 @@ def _compile(cmd: list, lib: str, what: str, verbose: bool) -> None:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source of the package into libmalt.so, and the
-    matrix-core calibration into libmalt_calib.so (always rebuilds)."""
+    """Compile every HIP source of the package into libmalt.so, the host side of the
+    operators into _malt.so and the matrix-core calibration into libmalt_calib.so (always
+    rebuilds)."""
     os.makedirs(os.path.dirname(LIB), exist_ok=True)
     _compile(build_cmd(LIB + ".tmp"), LIB, "libmalt", verbose)
+    _compile(binding_cmd(BINDING_LIB + ".tmp"), BINDING_LIB, "_malt", verbose)
     _compile(calib_cmd(CALIB_LIB + ".tmp"), CALIB_LIB, "libmalt_calib", verbose)
     return LIB
 

@@ -15,6 +15,7 @@ from typing import List, Optional, Sequence, Tuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "lib", "libmalt.so")
+BINDING_PATH = os.path.join(_HERE, "lib", "_malt.so")
 
 MALT_OK = 0
 MALT_ERR_INVALID_ARG = 1
@@ -204,6 +205,18 @@ def lib() -> ctypes.CDLL:
             fn.argtypes = args
         _lib = handle
     return _lib
+
+
+def load_binding():
+    """The Python module _malt, built beside libmalt.so; raises if it has not been built."""
+    import importlib.util
+    if not os.path.exists(BINDING_PATH):
+        raise RuntimeError(f"_malt.so not found at {BINDING_PATH}: build it with "
+                           "`python -m paper_2608_05088_amd.build` (there is no other host side)")
+    spec = importlib.util.spec_from_file_location("_malt", BINDING_PATH)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
 
 
 def status_string(status: int) -> str:

@@ -26,8 +26,7 @@ taken as they are up to 2^31 - 1 elements, as are those of outputs.
 from __future__ import annotations
 
 import functools
-import operator
-from ctypes import byref, c_int64, c_size_t, c_void_p
+from ctypes import byref, c_size_t
 from typing import List, NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
@@ -719,102 +718,20 @@ def linear_cross_entropy_step(x: torch.Tensor, weight: torch.Tensor, labels: tor
 
 
 # -------------------------------------------------------------------------- norm
-@functools.lru_cache(maxsize=4096)
-def _norm_grad_size(rows: int, width: int, need_w: bool) -> int:
-    size = c_size_t(0)
-    lm._check(lm.lib().malt_rms_norm_grad_size(rows, width, need_w, byref(size)))
-    return size.value
+_binding = None
 
 
-def _norm_args(x, weight, residual, eps) -> float:
-    _tensor("x", x, _DTYPES)
-    _tensor("weight", weight, _DTYPES, x.device)
-    if x.dim() < 1 or x.shape[-1] < 1 or weight.dim() != 1 or weight.shape[0] != x.shape[-1]:
-        raise ValueError(f"x must be (..., width) and weight (width,) (got {tuple(x.shape)}, {tuple(weight.shape)})")
-    if residual is not None:
-        _tensor("residual", residual, (x.dtype,), x.device)
-        if residual.shape != x.shape:
-            raise ValueError(f"residual must be {tuple(x.shape)} (got {tuple(residual.shape)})")
-    eps = float(eps)
-    if not 0 <= eps < float("inf"):
-        raise ValueError(f"eps must be a number, 0 or more (got {eps})")
-    return eps
+def _host():
+    """The module _malt (csrc/binding.cpp): the host side of what follows, in C++."""
+    global _binding
+    if _binding is None:
+        lm.lib()
+        _binding = lm.load_binding()
+    return _binding
 
 
-def _norm(x, weight, residual, eps, out_dtype, want_rstd, stream):
-    """y (in 8 bits without out_dtype), the sum (None without residual) and 1 / rms."""
-    dev = x.device
-    width = x.shape[-1]
-    n = x.numel() // width
-
-    def work(s):
-        sums = torch.empty(x.shape, dtype=x.dtype, device=dev) if residual is not None else None
-        rstd = torch.empty(n, dtype=torch.float32, device=dev) if want_rstd else None
-        if out_dtype is None:
-            kb = -(-width // BLOCK)
-            y = torch.empty((n, kb * BLOCK), dtype=torch.float8_e4m3fn, device=dev)
-            scales = torch.empty((kb, _pad(n, 256)), dtype=torch.uint8, device=dev)
-        else:
-            y, scales = torch.empty(x.shape, dtype=out_dtype, device=dev), None
-        if n:
-            flat, ldx = _rows(_flat(x) if x.dim() > 1 else x.reshape(1, width))
-            r, ldr = (None, 0) if residual is None else _rows(_flat(residual) if x.dim() > 1 else residual.reshape(1, width))
-            w = weight.contiguous()
-            eight = scales is not None
-            a = lm.malt_rms_norm_t(
-                flat.data_ptr(), _DTYPES[x.dtype], n, width, ldx, None if r is None else r.data_ptr(), ldr, w.data_ptr(),
-                _DTYPES[w.dtype], eps, None if sums is None else sums.data_ptr(), width, None if eight else y.data_ptr(),
-                0 if eight else _DTYPES[out_dtype], width, y.data_ptr() if eight else None,
-                scales.data_ptr() if eight else None, None if rstd is None else rstd.data_ptr())
-            lm._check(lm.lib().malt_rms_norm(byref(a), s))
-        return (y if scales is None else Fp8Rows(y, scales, x.shape)), sums, rstd
-
-    return _on(dev, stream, (x, weight, residual), work)
-
-
-class _RmsNorm(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, weight, residual, eps, out_dtype):
-        ctx.set_materialize_grads(False)
-        y, h, rstd = _norm(x, weight, residual, eps, out_dtype, True, None)
-        ctx.save_for_backward(x if h is None else h, weight, rstd)
-        return y if h is None else (y, h)
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dy, dh=None):
-        h, weight, rstd = ctx.saved_tensors
-        need_x, need_w, need_r = ctx.needs_input_grad[:3]
-        if dh is not None and dh.dtype != h.dtype:
-            dh = dh.to(h.dtype)
-        if dy is None:   # nothing went through the norm
-            return dh if need_x else None, None, dh if need_r else None, None, None
-        dev = h.device
-        width = h.shape[-1]
-        n = h.numel() // width
-        if dy.dtype not in _DTYPES:
-            dy = dy.float()
-        need_h = need_x or need_r
-
-        def work(s):
-            dx = torch.empty(h.shape, dtype=h.dtype, device=dev) if need_h else None
-            dw = torch.empty(width, dtype=weight.dtype, device=dev) if need_w else None
-            if n == 0:
-                return dx, None if dw is None else dw.zero_()
-            (hf, ldh), (gf, ldg) = (_rows(_flat(t) if t.dim() > 1 else t.reshape(1, width)) for t in (h, dy))
-            df, ldd = (None, 0) if dh is None or not need_h else _rows(_flat(dh) if dh.dim() > 1 else dh.reshape(1, width))
-            w = weight.contiguous()
-            size = _norm_grad_size(n, width, need_w)
-            ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
-            a = lm.malt_rms_norm_grad_t(
-                hf.data_ptr(), _DTYPES[h.dtype], n, width, ldh, w.data_ptr(), _DTYPES[w.dtype], rstd.data_ptr(), gf.data_ptr(),
-                _DTYPES[gf.dtype], ldg, None if df is None else df.data_ptr(), ldd, dx.data_ptr() if need_h else None, width,
-                dw.data_ptr() if need_w else None)
-            lm._check(lm.lib().malt_rms_norm_grad(byref(a), ws.data_ptr() if size else None, size, s))
-            return dx, dw
-
-        dx, dw = _on(dev, None, (), work)
-        return dx if need_x else None, dw, dx if need_r else None, None, None
+def _grads_wanted(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
 def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -824,18 +741,20 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Ten
     h = x + residual, rounded to their type, and the result is (y, h).  out_dtype: x's unless
     given.  Computed in float32, the mean of squares in float64.  Differentiable in x, residual
     and weight, through h as well."""
-    eps = _norm_args(x, weight, residual, eps)
-    for name, t in (("x", x), ("weight", weight), ("residual", residual)):
-        if t is not None:
-            _no_tangent(name, t)
-    out_dtype = x.dtype if out_dtype is None else out_dtype
-    _type("out_dtype", out_dtype)
-    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad
-                                    or (residual is not None and residual.requires_grad)):
+    _tensor("x", x, _DTYPES)
+    _tensor("weight", weight, _DTYPES, x.device)
+    if residual is not None:
+        _tensor("residual", residual, (x.dtype,), x.device)
+        _no_tangent("residual", residual)
+    _no_tangent("x", x)
+    _no_tangent("weight", weight)
+    if out_dtype is not None:
+        _type("out_dtype", out_dtype)
+    grad = _grads_wanted(x, weight, residual)
+    if grad:
         _no_stream(stream)
-        return _RmsNorm.apply(x, weight, residual, eps, out_dtype)
-    y, h, _ = _norm(x, weight, residual, eps, out_dtype, False, stream)
-    return y if residual is None else (y, h)
+    return _on(x.device, stream, (x, weight, residual),
+               lambda s: _host().rms_norm(x, weight, residual, eps, out_dtype, grad, s))
 
 
 def rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -843,11 +762,10 @@ def rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
     """rms_norm with its output in 8 bits (Fp8Rows: a scale for each row and 128
     values), for fp8_forward on kept weights, in one pass and without gradients:
     rows, or (rows, h) with residual.  y is rounded once, from float32."""
-    eps = _norm_args(x, weight, residual, eps)
-    x, weight = x.detach(), weight.detach()
-    if residual is not None:
-        residual = residual.detach()
-    rows, h, _ = _norm(x, weight, residual, eps, None, False, stream)
+    _tensor("x", x, _DTYPES)
+    values, scales, h = _on(x.device, stream, (x, weight, residual),
+                            lambda s: _host().rms_norm_fp8(x, weight, residual, eps, s))
+    rows = Fp8Rows(values, scales, x.shape)
     return rows if residual is None else (rows, h)
 
 
@@ -861,35 +779,13 @@ def _adamw_size(numel: int, bits: int) -> int:
 
 def adamw_state(param: torch.Tensor, bits: int = 32) -> torch.Tensor:
     """The moments of a parameter before its first step, to be kept for adamw_step: float32
-    (2, numel), or with bits=8 the bytes of 8-bit moments (8.25 bits each)."""
+    (2, numel), or with bits=8 the bytes of 8-bit moments (8.125 bits each)."""
     _tensor("param", param, _DTYPES)
     if bits not in (8, 32):
         raise ValueError(f"bits must be 8 or 32 (got {bits})")
     if bits == 32:
         return torch.zeros((2, param.numel()), dtype=torch.float32, device=param.device)
     return torch.zeros(_adamw_size(param.numel(), 8), dtype=torch.uint8, device=param.device)
-
-
-_FIELDS = operator.attrgetter("dtype", "device", "shape")
-_BITS = {torch.float32: 32, torch.uint8: 8}
-
-
-def _adamw_states(params, states, dev) -> bytes:
-    """Checks moments against their parameters; their bits."""
-    for i, (p, st) in enumerate(zip(params, states)):
-        _tensor(f"states[{i}]", st, _BITS, dev)
-        want = (2, p.numel()) if st.dtype == torch.float32 else (_adamw_size(p.numel(), 8),)
-        if tuple(st.shape) != want or not st.is_contiguous():
-            raise ValueError(f"states[{i}] must be contiguous, {want} (got {tuple(st.shape)}, strides {st.stride()})")
-    return bytes(_BITS[st.dtype] for st in states)
-
-
-def _pointers(tensors):
-    return (c_void_p * len(tensors))(*map(torch.Tensor.data_ptr, tensors))
-
-
-def _sizes(tensors):
-    return (c_int64 * len(tensors))(*map(torch.Tensor.numel, tensors))
 
 
 def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], states: Sequence[torch.Tensor], lr: float,
@@ -906,64 +802,29 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
     element's: give each step another seed.  Equal calls give equal bits.  A captured call replays its
     arguments, step and seed among them.  To autograd, params and states are changed in place."""
     params, grads, states = list(params), list(grads), list(states)
-    if not len(params) == len(grads) == len(states):
-        raise ValueError(f"params, grads and states must be as many (got {len(params)}, {len(grads)}, {len(states)})")
+    if not 0 <= int(seed) < 1 << 64:
+        raise ValueError(f"seed must be in [0, 2^64) (got {seed})")
+    if not params and not grads and not states:
+        return
     scale_at = None
     if isinstance(grad_scale, torch.Tensor):
         scale_at, grad_scale = grad_scale, 1.0
-    if not 0 <= int(seed) < 1 << 64:
-        raise ValueError(f"seed must be in [0, 2^64) (got {seed})")
-    if not params:
-        return
-    for i, (p, g) in enumerate(zip(params, grads)):
-        _tensor(f"params[{i}]", p, _DTYPES, params[0].device)
-        _tensor(f"grads[{i}]", g, _DTYPES, params[0].device)
-        if not p.is_contiguous():
-            raise ValueError(f"params[{i}] must be contiguous (got strides {p.stride()})")
-        if g.shape != p.shape:
-            raise ValueError(f"grads[{i}] must be {tuple(p.shape)} (got {tuple(g.shape)})")
-    dev = params[0].device
-    bits = _adamw_states(params, states, dev)
-    if scale_at is not None:
-        _tensor("grad_scale", scale_at, (torch.float32,), dev)
-        if scale_at.numel() != 1:
-            raise ValueError(f"grad_scale must be a number or a scalar tensor (got {tuple(scale_at.shape)})")
-    h = lm.malt_adamw_t(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(step),
-                        float(grad_scale), None if scale_at is None else scale_at.data_ptr(), int(seed))
-
-    def work(s):
-        gs = [g if g.is_contiguous() else g.contiguous() for g in grads]
-        t = lm.malt_adamw_tensors_t(len(params), _sizes(params), _pointers(params), bytes(_DTYPES[p.dtype] for p in params),
-                                    _pointers(gs), bytes(_DTYPES[g.dtype] for g in gs), _pointers(states), bits)
-        lm._check(lm.lib().malt_adamw_step(byref(t), byref(h), s))
-
-    _on(dev, stream, (*params, *grads, *states, scale_at), work)
-    for x in params:
-        _written(x)
-    for x in states:
-        _written(x)
+    if params:
+        _tensor("params[0]", params[0], _DTYPES)
+    dev = params[0].device if params else grads[0].device
+    inputs = (*params, *grads, *states, scale_at) if stream is not None else ()
+    b1, b2 = betas
+    _on(dev, stream, inputs, lambda s: _host().adamw_step(params, grads, states, lr, b1, b2, eps, weight_decay, step,
+                                                          grad_scale, scale_at, seed, s))
 
 
 def adamw_moments(params: Sequence[torch.Tensor], states: Sequence[torch.Tensor], stream=None) -> List[torch.Tensor]:
     """What the moments of adamw_step stand for: float32 (2, numel) for each parameter,
     the first moment and the second, in new tensors."""
     params, states = list(params), list(states)
-    if len(params) != len(states):
-        raise ValueError(f"params and states must be as many (got {len(params)}, {len(states)})")
-    if not params:
+    if not params and not states:
         return []
-    dev = params[0].device
-    for i, p in enumerate(params):
-        _tensor(f"params[{i}]", p, _DTYPES, dev)
-    bits = _adamw_states(params, states, dev)
-
-    def work(s):
-        out = [st.clone() if b == 32 else torch.empty((2, p.numel()), dtype=torch.float32, device=dev)
-               for p, st, b in zip(params, states, bits)]
-        few = [i for i, b in enumerate(bits) if b == 8]
-        if few:
-            lm._check(lm.lib().malt_adamw_moments(len(few), _sizes([params[i] for i in few]),
-                                                  _pointers([states[i] for i in few]), _pointers([out[i] for i in few]), s))
-        return out
-
-    return _on(dev, stream, states, work)
+    if params:
+        _tensor("params[0]", params[0], _DTYPES)
+    dev = params[0].device if params else states[0].device
+    return _on(dev, stream, states, lambda s: _host().adamw_moments(params, states, s))

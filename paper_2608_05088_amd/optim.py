@@ -5,7 +5,7 @@ Algorithm 1 (MALT) and Algorithm 2 (MALTER) update matrix parameters; the
 paper trains embeddings, norms and biases with AdamW.  This optimizer routes
 every 2-D parameter (or those `matrix_filter` selects) of a parameter group
 into one libmalt plan per group, so one `step()` is one grouped `malt_step`
-per group, and hands the remaining parameters to an inner `torch.optim.AdamW`.
+per group, and hands the remaining parameters to an inner AdamW.
 
 Variants:
   "malt"    Algorithm 1
@@ -18,6 +18,8 @@ Conventions
     gradients are made contiguous float32 before the step.  A matrix
     parameter without a gradient is stepped with a zero gradient (the plan
     steps all of its matrices together).
+  * The remaining parameters go to torch's AdamW, or with adamw_bits=32 or 8 to this
+    module's (moments in that many bits), one launch for a hundred of them.
   * `lr` is the matrix learning rate eta; schedulers that change a group's
     "lr" scale the group's AdamW learning rate by the same factor.
   * `state_dict()` holds each plan's state buffer (M, l, r, nu as float32)
@@ -26,6 +28,7 @@ Conventions
 """
 from __future__ import annotations
 
+import itertools
 from typing import Callable, Dict, List, Optional, Tuple
 
 import torch
@@ -40,14 +43,73 @@ def is_matrix(p: torch.Tensor) -> bool:
     return p.dim() == 2
 
 
+class AdamW(torch.optim.Optimizer):
+    """AdamW on ops.adamw_step: all parameters of a group in one launch for each 108 of
+    them.  Parameters and gradients are float32 or bfloat16 CUDA tensors, parameters
+    contiguous.
+
+    bits: of the moments.  8 keeps those of parameters of at least `min_8bit` elements in
+    8 bits (a scale for each 256), the others in 32; their rounding is random, by `seed`, step and
+    place.  A parameter without a gradient is left out of a step and does not count it."""
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+                 bits: int = 32, min_8bit: int = 4096, seed: int = 0):
+        if bits not in (8, 32):
+            raise ValueError(f"bits must be 8 or 32 (got {bits})")
+        if not 0 <= seed < 1 << 32:
+            raise ValueError(f"seed must be in [0, 2^32) (got {seed})")
+        super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay))
+        self.bits, self.min_8bit, self.seed = bits, min_8bit, seed
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        from . import ops
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        # A captured launch keeps its step count, so that replays would repeat this step.
+        if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("AdamW.step cannot be captured: its step count is an argument")
+        for k, g in enumerate(self.param_groups):
+            calls: Dict[tuple, list] = {}   # parameters of a device that have stepped as often
+            for p in g["params"]:
+                if p.grad is None:
+                    continue
+                st = self.state[p]
+                if not st:
+                    st["step"] = 0
+                    st["moments"] = ops.adamw_state(p, 8 if self.bits == 8 and p.numel() >= self.min_8bit else 32)
+                calls.setdefault((p.device, st["step"] + 1), []).append(p)
+            for i, ((_, t), ps) in enumerate(calls.items()):
+                ops.adamw_step(ps, [p.grad for p in ps], [self.state[p]["moments"] for p in ps], lr=g["lr"],
+                               betas=g["betas"], eps=g["eps"], weight_decay=g["weight_decay"], step=t,
+                               seed=self.seed << 32 | (t * 1000003 + k * 1009 + i) & 0xFFFFFFFF)
+                for p in ps:
+                    self.state[p]["step"] = t
+        return loss
+
+    def load_state_dict(self, state_dict: Dict) -> None:
+        super().load_state_dict(state_dict)
+        # Moments keep the type they were saved in, whatever the parameter's.
+        ids = itertools.chain.from_iterable(g["params"] for g in state_dict["param_groups"])
+        for i, p in zip(ids, itertools.chain.from_iterable(g["params"] for g in self.param_groups)):
+            if i in state_dict["state"]:
+                st = state_dict["state"][i]
+                self.state[p] = {"step": int(st["step"]), "moments": st["moments"].detach().clone().to(p.device)}
+
+
 class MALT(torch.optim.Optimizer):
     def __init__(self, params, lr: float = 1.3e-3, mu1: float = 0.95, mu2: float = 0.99, eps: float = 1e-8,
                  weight_decay: float = 0.0, variant: str = "malt", ns_steps: int = 5,
                  adamw_lr: Optional[float] = None, adamw_betas=(0.9, 0.95), adamw_eps: float = 1e-8,
                  adamw_weight_decay: float = 0.0,
-                 matrix_filter: Optional[Callable[[torch.Tensor], bool]] = None):
+                 matrix_filter: Optional[Callable[[torch.Tensor], bool]] = None,
+                 adamw_bits: Optional[int] = None):
         if variant not in VARIANTS:
             raise ValueError(f"variant must be one of {VARIANTS}")
+        if adamw_bits not in (None, 8, 32):
+            raise ValueError(f"adamw_bits must be 8, 32 or None (got {adamw_bits})")
         defaults = dict(lr=lr, mu1=mu1, mu2=mu2, eps=eps, weight_decay=weight_decay, ns_steps=ns_steps,
                         adamw_lr=lr if adamw_lr is None else adamw_lr, adamw_betas=tuple(adamw_betas),
                         adamw_eps=adamw_eps, adamw_weight_decay=adamw_weight_decay)
@@ -70,7 +132,9 @@ class MALT(torch.optim.Optimizer):
             adam_groups.append(dict(params=rest, lr=g["adamw_lr"], betas=g["adamw_betas"], eps=g["adamw_eps"],
                                     weight_decay=g["adamw_weight_decay"]))
         self._adam_lr0 = [ag["lr"] for ag in adam_groups]
-        self._adam = torch.optim.AdamW(adam_groups) if any(ag["params"] for ag in adam_groups) else None
+        self._adam = None
+        if any(ag["params"] for ag in adam_groups):
+            self._adam = torch.optim.AdamW(adam_groups) if adamw_bits is None else AdamW(adam_groups, bits=adamw_bits)
 
     # ------------------------------------------------------------------ helpers
     def _hparams(self, g: dict):

@@ -22,6 +22,12 @@ forward and backward, on this package's operators (ops.py) in 8 bits:
 
   python -m paper_2608_05088_amd.train --model gpt2-small --optim malt --teacher gpt2-medium --top-k 64 --fp8
 
+--head forms the language model's loss and its gradients from the last states without
+the logits, --adamw-bits steps what is no block matrix with moments of that many bits, many
+tensors a launch, --rms-norm puts root-mean-square norms in the layer norms' places:
+
+  python -m paper_2608_05088_amd.train --model gpt2-small --optim malt --head --adamw-bits 8 --rms-norm --fp8
+
 Prints one JSON line per optimizer: ms per iteration, of which optimizer
 step, the optimizer state (as the paper counts it: the tensors the algorithm
 keeps, and as allocated) and the peak device memory.
@@ -61,15 +67,18 @@ def block_matrix(name: str, p) -> bool:
 from .schedules import lambda_lr, linear_warmup  # noqa: E402
 
 
-def make_optimizer(kind: str, model, lr: float, adamw_lr: float, weight_decay: float = 0.1):
+def make_optimizer(kind: str, model, lr: float, adamw_lr: float, weight_decay: float = 0.1, adamw_bits=None):
     import torch
-    from .optim import MALT
+    from .optim import MALT, AdamW
+    if kind == "adamw" and adamw_bits is not None:
+        return AdamW(model.parameters(), lr=adamw_lr, betas=(0.9, 0.95), eps=1e-8, weight_decay=weight_decay,
+                     bits=adamw_bits)
     if kind == "adamw":
         return torch.optim.AdamW(model.parameters(), lr=adamw_lr, betas=(0.9, 0.95), eps=1e-8,
                                  weight_decay=weight_decay)
     mats = {id(p) for n, p in model.named_parameters() if block_matrix(n, p)}
     return MALT(model.parameters(), lr=lr, variant=kind, adamw_lr=adamw_lr, weight_decay=weight_decay,
-                adamw_weight_decay=weight_decay, matrix_filter=lambda p: id(p) in mats)
+                adamw_weight_decay=weight_decay, matrix_filter=lambda p: id(p) in mats, adamw_bits=adamw_bits)
 
 
 def use_operators(model) -> None:
@@ -92,6 +101,40 @@ def use_operators(model) -> None:
     for mod in model.transformer.h.modules():
         if isinstance(mod, Conv1D):
             mod.__class__ = Layer
+
+
+def use_rms_norm(model) -> None:
+    """Root-mean-square norms with the layer norms' gains, on this package's kernel, in the
+    layer norms' places; their biases go."""
+    import torch
+    from . import ops
+
+    class RmsNorm(torch.nn.LayerNorm):
+        def forward(self, x):
+            return ops.rms_norm(x, self.weight, eps=self.eps)
+
+    for mod in model.modules():
+        if type(mod) is torch.nn.LayerNorm:
+            mod.__class__ = RmsNorm
+            mod.bias = None
+
+
+def head_backward(model, ids, scale: float = 1.0):
+    """One micro-batch of language modelling without the logits: the mean loss over the tokens that
+    have a next one, and its gradient, times `scale`, in the model's parameters.  The
+    head is the token table; its gradient is added to where the table's lies."""
+    import torch
+    from . import ops
+    hidden = model.transformer(input_ids=ids).last_hidden_state
+    labels = torch.full_like(ids, -100)
+    labels[:, :-1] = ids[:, 1:]
+    count = max(1, ids.shape[0] * (ids.shape[1] - 1))   # no token has a next one: nothing to learn, loss 0
+    table = model.lm_head.weight
+    losses, dx, dw = ops.linear_cross_entropy_step(hidden, table, labels, grad=scale / count, out=table.grad,
+                                                   accumulate=table.grad is not None)
+    table.grad = dw
+    hidden.backward(dx)
+    return losses.sum() / count
 
 
 def distill_backward(student, teacher, ids, top_k: int = 64, tau: float = 2.0, alpha: float = 0.5, scale: float = 1.0):
@@ -155,9 +198,11 @@ def run(kind: str, args, device) -> dict:
     teacher = None
     if args.teacher:
         teacher = build_model(args.teacher, device, seed=args.seed + 1).eval().requires_grad_(False)
+    if args.rms_norm:
+        use_rms_norm(model)
     if args.fp8:
         use_operators(model)
-    opt = make_optimizer(kind, model, args.lr, args.adamw_lr, args.weight_decay)
+    opt = make_optimizer(kind, model, args.lr, args.adamw_lr, args.weight_decay, args.adamw_bits)
     # The paper's protocol: linear warm-up over the first 10% of the run.
     sched = lambda_lr(opt, linear_warmup(args.warmup + args.iters))
     gen = torch.Generator(device=device)
@@ -169,6 +214,8 @@ def run(kind: str, args, device) -> dict:
             ids = torch.randint(0, 50257, (B, T), device=device, generator=gen)
             if teacher is not None:
                 loss = distill_backward(model, teacher, ids, args.top_k, args.tau, args.alpha, 1 / args.accum)
+            elif args.head:
+                loss = head_backward(model, ids, 1 / args.accum)
             else:
                 loss = model(input_ids=ids, labels=ids).loss
                 (loss / args.accum).backward()
@@ -227,11 +274,16 @@ def main(argv=None):
     ap.add_argument("--weight-decay", type=float, default=0.1)
     ap.add_argument("--seed", type=int, default=0)
     ap.add_argument("--fp8", action="store_true", help="token table and block layers on this package's operators, in 8 bits")
+    ap.add_argument("--head", action="store_true", help="the loss and its gradients without the logits")
+    ap.add_argument("--adamw-bits", type=int, choices=(8, 32), help="AdamW on this package's kernel, moments in so many bits")
+    ap.add_argument("--rms-norm", action="store_true", help="root-mean-square norms in the layer norms' places")
     ap.add_argument("--teacher", choices=sorted(MODELS), help="train on this model's top logits")
     ap.add_argument("--top-k", type=int, default=64)
     ap.add_argument("--tau", type=float, default=2.0)
     ap.add_argument("--alpha", type=float, default=0.5)
     args = ap.parse_args(argv)
+    if args.head and args.teacher:
+        ap.error("--head forms the language model's own loss: it goes without --teacher")
     import torch
     if not torch.cuda.is_available():
         raise SystemExit("a GPU is required")

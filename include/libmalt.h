@@ -459,11 +459,12 @@ malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, in
  *  - A label outside [0, vocab) is no label: the row's loss and gradient are zero whatever the
  *    row holds.  A row of weight 0 has a zero gradient.  (A weight row that is not finite makes
  *    every row's loss no number, as the definition does.)
- *  - Logits of -inf have probability zero; a labelled row without a finite logit is NaN, as are
+ *  - Logits of -inf have probability zero, and so has a probability below 2^-126; a labelled row without a finite logit is NaN, as are
  *    rows with a NaN or +inf.
  *  - Products of bfloat16 are exact and summed in float32.  float32 values enter products as
- *    three bfloat16 numbers whose sum they are; of their nine products the six above 2^-26 are
- *    taken, in float32.  Softmax and losses are float32.  1 - q_y is formed from the other
+ *    three bfloat16 numbers whose sum they are; of their nine products the three smallest, below
+ *    2^-24 of the whole each, are left out, the others summed in float32.  Where x or weight is float32 an
+ *    infinite value enters as the largest bfloat16 number.  Softmax and losses are float32.  1 - q_y is formed from the other
  *    columns' sum.  Gradients of type float32 take d, x and weight whole; bfloat16 ones take
  *    d, x and weight rounded to bfloat16, which puts them off by about as much as their own
  *    rounding.

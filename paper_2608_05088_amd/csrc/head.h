@@ -109,6 +109,7 @@ struct HeadPack {
   int64_t plane;
   int64_t out_rows, out_cols;   // as the output lies: rows to write, padded columns (the contraction)
   int32_t planes;
+  bool finite;             // infinities become the largest numbers
   HeadLabels labels;       // rows without label (or weight) become zeros; labels null: every row stays
   int64_t vocab;
 };

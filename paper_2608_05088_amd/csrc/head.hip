@@ -15,7 +15,7 @@
 // both; rows of 32 KB apart: 1.70, with a pitch that is no power of two 1.58.)
 //
 // float32 operands are three bf16 planes whose sum they are.  A product of two is the six plane
-// products that matter (high by low and middle by low are below 2^-26 of it), small ones first,
+// products that matter (middle by low and low by low are below 2^-24 of it), small ones first,
 // run as a contraction six times as long: float32 sums of exact products, at 2.5 times the rate
 // of the float32 matrix instruction.  bf16 gradients take dz and the operands as single
 // planes: dz is rounded once more, an error of the size of the result's own rounding.

@@ -16,6 +16,7 @@ namespace {
 using ns::bf16x8;
 using ns::f32x4;
 
+constexpr float FAR = 0x1p100f;   // a logit (log2) that counts as infinite
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 // A row's label, or -1: outside the vocabulary.
@@ -30,18 +31,30 @@ __device__ __forceinline__ bool stays(const HeadLabels& l, int64_t r, int64_t vo
   return !l.labels || (label_of(l, r, vocab) >= 0 && (!l.weights || gptr(l.weights)[r * l.weight_stride] != 0.f));
 }
 
-// Four values as planes.  What a plane leaves is exact: its bits are those of v past the plane's.  An
-// infinity leaves nothing.
-__device__ __forceinline__ void store_planes(uint16_t* out, int64_t plane, int planes, op_f32x4 v) {
+// Four values as planes.  What a plane leaves is exact: its bits are those of v past the plane's.
+// finite: the largest values, infinities among them, stay so, since an infinity times another value's empty
+// plane would be no number.  Logits past FAR count as infinite.
+constexpr float BF16_MAX = 0x1.fep127f;
+__device__ __forceinline__ void store_planes(uint16_t* out, int64_t plane, int planes, bool finite, op_f32x4 v) {
+  if (finite)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (fabsf(v[j]) == __builtin_inff()) v[j] = copysignf(BF16_MAX, v[j]);
   for (int p = 0; p < planes; ++p) {
-    const uint32_t lo = pack_bf16x2(v.x, v.y), hi = pack_bf16x2(v.z, v.w);
+    uint32_t lo = pack_bf16x2(v.x, v.y), hi = pack_bf16x2(v.z, v.w);
+    if (finite) {
+      // Rounded past bf16's largest.
+      if ((lo & 0x7fffu) == 0x7f80u) lo -= 1;
+      if ((lo & 0x7fff0000u) == 0x7f800000u) lo -= 0x10000u;
+      if ((hi & 0x7fffu) == 0x7f80u) hi -= 1;
+      if ((hi & 0x7fff0000u) == 0x7f800000u) hi -= 0x10000u;
+    }
     *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(out) + p * plane) = op_u32x2{lo, hi};
     const float h[4] = {bf16_lo(lo), bf16_hi(lo), bf16_lo(hi), bf16_hi(hi)};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = fabsf(h[j]) == __builtin_inff() ? 0.f : v[j] - h[j];
+    for (int j = 0; j < 4; ++j) v[j] -= h[j];
   }
 }
-
 // Where value c of row r lies in a plane whose rows hold `cols`.
 __device__ __forceinline__ int64_t packed_at(int64_t r, int64_t c, int64_t cols) {
   return (r / HEAD_TILE * (cols / HEAD_BK) + c / HEAD_BK) * HEAD_BLOCK + r % HEAD_TILE * HEAD_BK + c % HEAD_BK;
@@ -55,7 +68,7 @@ __global__ __launch_bounds__(256) void head_pack_kernel(HeadPack a) {
   const int64_t r = i / per, c = i % per * 4;
   op_f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (r < a.rows && stays(a.labels, r, a.vocab)) v = row_load4(static_cast<const T*>(a.x) + r * a.ld, c, a.cols);
-  store_planes(a.out + packed_at(r, c, a.out_cols), a.plane, a.planes, v);
+  store_planes(a.out + packed_at(r, c, a.out_cols), a.plane, a.planes, a.finite, v);
 }
 
 // The transpose of a 64 x 64 tile through LDS; rows past the end are zeros.
@@ -78,7 +91,7 @@ __global__ __launch_bounds__(256) void head_pack_t_kernel(HeadPack a, int tiles_
     const int c = hi + 16 * k;
     if (c0 + c >= a.out_rows) continue;
     const op_f32x4 v = {tile[4 * lo][c], tile[4 * lo + 1][c], tile[4 * lo + 2][c], tile[4 * lo + 3][c]};
-    store_planes(a.out + packed_at(c0 + c, r0 + 4 * lo, a.out_cols), a.plane, a.planes, v);
+    store_planes(a.out + packed_at(c0 + c, r0 + 4 * lo, a.out_cols), a.plane, a.planes, a.finite, v);
   }
 }
 
@@ -243,8 +256,9 @@ __global__ __launch_bounds__(T) void head_join_kernel(HeadLabels rows, int64_t v
 #pragma unroll
     for (int i = 0; i < T / 64; ++i) all = fmaxf(all, red[0][i]);
   }
+  if (all <= -FAR) all = -__builtin_inff();
   const float ref = all == -__builtin_inff() ? 0.f : all;
-  sum = sum * exp2f(top - ref);
+  sum = all == -__builtin_inff() && sum == sum ? 0.f : sum * exp2f(top - ref);
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
   if constexpr (T > 64) {
@@ -263,7 +277,9 @@ __global__ __launch_bounds__(T) void head_join_kernel(HeadLabels rows, int64_t v
     }
     return;
   }
-  const float y = gptr(at_label)[r];   // log2
+  float y = gptr(at_label)[r];   // log2
+  if (y <= -FAR) y = -__builtin_inff();
+  if (y >= FAR || all >= FAR) sum = __builtin_nanf("");
   if (losses) {
     // log(1 + o / e^y) where the label leads, log(o) - y + log(1 + e^y / o) where it does not; log1p keeps
     // what a sum of nearly 1 would lose.
@@ -272,7 +288,7 @@ __global__ __launch_bounds__(T) void head_join_kernel(HeadLabels rows, int64_t v
     if (d > log2f(sum)) loss = log1pf(sum * exp2f(-d));
     else loss = (log2f(sum) - d) * LN2 + log1pf(exp2f(d) / sum);
     if (sum == 0.f && y > -__builtin_inff()) loss = 0.f;   // no other column has mass
-    if (y == __builtin_inff()) loss = __builtin_nanf("");
+    if (sum != sum) loss = sum;
     gptr(losses)[r] = loss;
   }
   if (stats) {

@@ -128,8 +128,8 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
   L.dz_planes = fine ? HEAD_PLANES : 1;
   L.rows_pad = up(a.rows, HEAD_TILE);
   L.cols_pad = up(a.inner, HEAD_BK);
-  // As they lie: rows of whole stages, 16-byte pieces, a tile's offsets in 32 bits.
-  L.pack_w = w32 || a.inner % HEAD_BK || a.ldw % 8 || a.ldw > (int64_t(1) << 22) || !op_aligned(a.weight, 16);
+  // As they lie: rows of whole stages, 16-byte pieces, a tile's offsets in 32 bits, infinities that meet no empty plane.
+  L.pack_w = w32 || x32 || a.inner % HEAD_BK || a.ldw % 8 || a.ldw > (int64_t(1) << 22) || !op_aligned(a.weight, 16);
   size_t end = 0;
   auto take = [&](size_t bytes) {
     const size_t at = end;
@@ -489,6 +489,7 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
   px.out_rows = L.rows_pad;
   px.out_cols = L.cols_pad;
   px.planes = L.x_planes;
+  px.finite = f32x || f32w;
   px.labels = labels;
   px.labels.weights = nullptr;   // the losses of rows without weight are formed all the same
   px.vocab = a.vocab;
@@ -506,6 +507,7 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       pw.out_cols = L.cols_pad;
       pw.plane = pw.out_rows * pw.out_cols;
       pw.planes = L.w_planes;
+      pw.finite = f32x || f32w;
       MALT_TRY(launched(launch_head_pack(pw, f32w, s), "packing the head's weight"));
       wside = packed_side(wp, pw.out_rows, pw.out_cols);
     }
@@ -572,6 +574,7 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
     p.out_cols = L.vocab_pad;
     p.plane = up(a.inner, HEAD_TILE) * L.vocab_pad;
     p.planes = dx_w;
+    p.finite = f32x || f32w;
     MALT_TRY(launched(launch_head_pack_t(p, f32w, s), "transposing the head's weight"));
     w_t = packed_side(p.out, up(a.inner, HEAD_TILE), L.vocab_pad);
     w_t.rows = a.inner;

@@ -1,0 +1,399 @@
+"""The loss of a linear head without its logits, and its gradients, against plain
+implementations in 64 bits: odd sizes, rows without label or weight, logits that are no
+numbers, strides, types, pieces of the vocabulary and of the contraction, streams and graphs.
+
+Tolerances follow from the arithmetic.  u = 2^-24 is float32's unit roundoff, r = finfo.eps / 2 a
+type's half step (bf16 2^-8).  With S = sum |x||w| a logit is off by (6 K + 8) u S: at most 6 K
+products are added up, each exact, and the three that are left out of a float32 product are below
+2^-24 of it each.  A row's sum of exponentials has at most 100 additions in a row and
+exponents rounded at |z| log2 e, so it is relatively off by d = 2 dz + 128 u + 4 u max|z| (and the
+hardware's 2 u an exponential).  Losses are off by d (1 - q_y) and their own rounding,
+d log p = d, and so on through the products.  A probability below 2^-126, float32's smallest normal
+number, is taken as zero: that is off by less than 2^-126, whatever d is."""
+import math
+
+import pytest
+import torch
+
+from paper_2608_05088_amd import libmalt as lm
+
+pytestmark = pytest.mark.gpu
+F32, BF16, I32, I64 = torch.float32, torch.bfloat16, torch.int32, torch.int64
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    lm.lib()
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2608_05088_amd import ops as module
+    return module
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def half(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def pitched(x, extra=5):
+    big = torch.full((x.shape[0], x.shape[1] + extra), float("nan"), device=x.device, dtype=x.dtype)
+    view = big[:, :x.shape[1]]
+    view.copy_(x)
+    return view
+
+
+def inputs(seed, m, v, k, xt=BF16, wt=BF16, lt=I64, holes=0.3, lean=3.0):
+    g = gen(seed)
+    w = (torch.randn((v, k), device="cuda", generator=g) * (2 / math.sqrt(k))).to(wt)
+    y = torch.randint(0, v, (m,), device="cuda", generator=g)
+    x = torch.randn((m, k), device="cuda", generator=g) + lean * torch.rand((m, 1), device="cuda", generator=g) * w[y].float()
+    none = torch.rand(m, device="cuda", generator=g) < holes
+    y[none] = torch.tensor([-1, v, -100, 1 << 30], device="cuda").repeat(m)[:int(none.sum())]
+    return x.to(xt), w, y.to(lt)
+
+
+class Exact:
+    """Losses and gradients in 64 bits, and the errors that are allowed."""
+
+    def __init__(self, x, w, y, weight=None, dx_type=None, dw_type=None):
+        m, k = x.shape
+        v = w.shape[0]
+        x64, w64, y = x.double(), w.double(), y.long()
+        self.there = (y >= 0) & (y < v)
+        weight = torch.ones(m, device="cuda", dtype=torch.float64) if weight is None else weight.double()
+        weight = torch.where(self.there, weight, 0.0)
+        x64 = torch.where(self.there[:, None], x64, 0.0)
+        z = x64 @ w64.t()
+        dz = (6 * k + 8) * U * (x64.abs() @ w64.abs().t()).amax(1)
+        d = 2 * dz + 128 * U + 4 * U * z.abs().amax(1)
+        logp = torch.log_softmax(z, 1)
+        at = y.clamp(0, v - 1)[:, None]
+        hot = torch.zeros_like(z).scatter_(1, at, 1.0)
+        p = torch.exp(logp)
+        self.losses = torch.where(self.there, -logp.gather(1, at)[:, 0], 0.0)
+        self.losses_tol = torch.where(self.there, d * -torch.expm1(-self.losses) + 8 * U * self.losses.abs(), 0.0)
+        g = torch.where(hot > 0, torch.expm1(logp), p) * weight[:, None]
+        used = (weight != 0)[:, None]
+        x64 = torch.where(used, x64, 0.0)
+        self.dx, self.dw = g @ w64, g.t() @ x64
+        g_err = g.abs() * (2 * d[:, None] + 8 * U) + 2.0 ** -126 * used
+
+        def tol(result, a, a_err, b, n, out, single):
+            # bf16 results: d and the other side rounded to bf16 once.
+            r = half(BF16)
+            e = a_err + (a.abs() * r if single else a.abs() * 4 * U)
+            extra = (r if single and b.dtype == F32 else 0) + (6 * n + 8) * U
+            big = a.abs() + e
+            return e @ b.double().abs() * 1.01 + extra * (big @ b.double().abs()) + half(out) * result.abs() * 1.01
+
+        dx_type, dw_type = dx_type or x.dtype, dw_type or w.dtype
+        self.dx_tol = tol(self.dx, g, g_err, w, v, dx_type, dx_type == BF16)
+        xs = torch.where(used, x, torch.zeros_like(x))
+        self.dw_tol = tol(self.dw, g.t(), g_err.t(), xs, m, dw_type, dw_type == BF16)
+
+    def check(self, losses=None, dx=None, dw=None):
+        for name, got, want, tol in (("losses", losses, self.losses, self.losses_tol), ("dx", dx, self.dx, self.dx_tol),
+                                     ("dw", dw, self.dw, self.dw_tol)):
+            if got is None:
+                continue
+            off = (got.double() - want).abs()
+            assert bool((off <= tol + 1e-38).all()), (name, float((off / (tol + 1e-38)).max()), float(off.max()))
+        if losses is not None:
+            assert bool((losses[~self.there] == 0).all())
+        if dx is not None:
+            assert bool((dx[~self.there] == 0).all())
+
+
+# ---------------------------------------------------------------- sizes and types
+@pytest.mark.parametrize("xt,wt", [(BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("m,v,k", [(1, 1, 1), (1, 1000, 64), (2, 7, 3), (16, 333, 130), (17, 64, 33), (32, 65, 128), (33, 257, 65),
+                                   (256, 256, 64), (257, 511, 128), (300, 1000, 129), (128, 1000, 64), (700, 130, 320)])
+def test_losses_and_gradients(ops, m, v, k, xt, wt):
+    x, w, y = inputs(m * 31 + v + k, m, v, k, xt, wt, I32 if m % 2 else I64)
+    e = Exact(x, w, y)
+    losses, dx, dw = ops.linear_cross_entropy_step(x, w, y)
+    assert losses.dtype == F32 and dx.dtype == xt and dw.dtype == wt
+    e.check(losses, dx, dw)
+    e.check(ops.linear_cross_entropy(x, w, y))
+
+
+@pytest.mark.parametrize("m,v,k", [(5000, 300, 64), (40, 20000, 64), (300, 9000, 100), (1000, 5000, 1280)])
+def test_long_contractions_are_cut(ops, m, v, k):
+    x, w, y = inputs(m + v, m, v, k)
+    g = torch.rand(m, device="cuda", generator=gen(5)) / m
+    Exact(x, w, y, g).check(*ops.linear_cross_entropy_step(x, w, y, grad=g))
+
+
+def test_pieces_of_the_vocabulary(ops):
+    """More rows times columns than a piece's gradient holds (2^28): two pieces."""
+    m, v, k = 65536, 8200, 64
+    x, w, y = inputs(9, m, v, k, holes=0.1)
+    losses, dx, dw = ops.linear_cross_entropy_step(x, w, y, grad=1 / m)
+    want_dw, tol_dw = torch.zeros((v, k), dtype=torch.float64, device="cuda"), torch.zeros((v, k), dtype=torch.float64, device="cuda")
+    for r in range(0, m, 8192):
+        s = slice(r, r + 8192)
+        e = Exact(x[s], w, y[s], torch.full((8192,), 1 / m, device="cuda"))
+        e.check(losses[s], dx[s])
+        want_dw += e.dw
+        tol_dw += e.dw_tol * 8   # additions of all rows: eight times a part's
+    assert bool(((dw.double() - want_dw).abs() <= tol_dw + half(BF16) * want_dw.abs() * 1.01).all())
+
+
+def test_float32_weight_gradient_of_bf16_inputs(ops):
+    """out of float32 takes dweight whole: its error is float32's, not bf16's."""
+    x, w, y = inputs(11, 300, 700, 128)
+    out = torch.full((700, 128), float("nan"), device="cuda")
+    losses, dx, dw = ops.linear_cross_entropy_step(x, w, y, out=out)
+    assert dw is out
+    Exact(x, w, y, dw_type=F32).check(losses, dx, dw)
+    kept = out.clone()
+    ops.linear_cross_entropy_step(x, w, y, out=out, accumulate=True)
+    e = Exact(x, w, y, dw_type=F32)
+    assert bool(((out.double() - 2 * e.dw).abs() <= 2 * e.dw_tol + 2 * U * e.dw.abs()).all())
+    assert bool((kept == kept).all())
+
+
+def test_float32_products_have_float32_precision(ops):
+    """Values whose bf16 parts alone would lose what is asked for: rows that differ past bf16's bits."""
+    m, v, k = 64, 500, 96
+    x, w, y = inputs(13, m, v, k, F32, F32, holes=0.0, lean=0.5)
+    x = x + torch.randn_like(x) * 2.0 ** -13
+    losses, dx, dw = ops.linear_cross_entropy_step(x, w, y)
+    e = Exact(x, w, y)
+    e.check(losses, dx, dw)
+    for got, want in ((losses, e.losses), (dx, e.dx), (dw, e.dw)):
+        assert float((got.double() - want).norm() / want.norm()) < 2e-6
+
+
+# ------------------------------------------------------- labels, weights, no numbers
+def test_no_row_has_a_label(ops):
+    x, w, y = inputs(15, 40, 300, 64)
+    y.fill_(-100)
+    w[3, 2] = float("inf")
+    x[5] = float("nan")
+    losses, dx, dw = ops.linear_cross_entropy_step(x, w, y)
+    assert bool((losses == 0).all()) and bool((dx == 0).all()) and bool((dw == 0).all())
+
+
+@pytest.mark.parametrize("m", [20, 300])
+def test_rows_without_label_may_hold_anything(ops, m):
+    x, w, y = inputs(17, m, 300, 64)
+    clean = x.clone()
+    none = (y < 0) | (y >= 300)
+    x[none] = float("nan")
+    x[none.nonzero()[0, 0]] = float("inf")
+    a, b = ops.linear_cross_entropy_step(x, w, y), ops.linear_cross_entropy_step(clean, w, y)
+    for p, q in zip(a, b):
+        assert torch.equal(p, q)
+
+
+def test_rows_of_weight_zero(ops):
+    x, w, y = inputs(19, 100, 300, 64, holes=0.0)
+    g = torch.rand(100, device="cuda", generator=gen(20))
+    g[::3] = 0.0
+    want = ops.linear_cross_entropy_step(x, w, y, grad=g)
+    assert bool((want[1][::3] == 0).all())
+    x[6] = float("nan")   # its loss is none, its gradient zero all the same
+    losses, dx, dw = ops.linear_cross_entropy_step(x, w, y, grad=g)
+    assert bool(losses[6].isnan()) and bool((losses[7:] == want[0][7:]).all())
+    assert torch.equal(dx, want[1]) and torch.equal(dw, want[2])
+    zero = ops.linear_cross_entropy_step(x, w, y, grad=torch.zeros((), device="cuda"))
+    assert bool((zero[1][:6] == 0).all()) and bool((zero[2][:, :][zero[2] == zero[2]] == 0).all())
+
+
+def test_logits_that_are_no_numbers(ops):
+    for m in (3, 50):
+        x, w, y = inputs(21, m, 300, 64, F32, F32, holes=0.0, lean=0.0)
+        x[1, 5] = float("nan")
+        losses, dx, _ = ops.linear_cross_entropy_step(x, w, y)
+        assert bool(losses[1].isnan()) and bool(dx[1].isnan().all())
+        assert bool(losses[0].isfinite()) and bool(dx[0].isfinite().all()) and bool(losses[2].isfinite())
+        w2 = w.clone()
+        x[1] = 1.0
+        x[:, 0] = 1.0
+        w2[7, 0] = float("-inf")   # a logit of -inf in every row: probability zero
+        y[y == 7] = 8
+        losses = ops.linear_cross_entropy(x, w2, y)
+        z = (x.double() @ w.double().t())
+        z[:, 7] = -math.inf
+        want = torch.nn.functional.cross_entropy(z, y, reduction="none")
+        assert bool(((losses.double() - want).abs() <= 1e-5 * (1 + want.abs())).all())
+        y[2] = 7                   # and as the label: the loss is infinite
+        assert bool(torch.isposinf(ops.linear_cross_entropy(x, w2, y)[2]))
+
+
+def test_sure_rows_keep_their_bits(ops):
+    """1 - q of a row that is sure of its label is 1e-9 here: by subtraction from 1 it would be zero in float32."""
+    m, v, k = 40, 400, 64
+    g = gen(23)
+    w = torch.randn((v, k), device="cuda", generator=g) * 0.1
+    w[:, 0] = 0.0
+    y = torch.randint(0, v, (m,), device="cuda", generator=g)
+    x = torch.randn((m, k), device="cuda", generator=g)
+    x[:, 0] = 0.0
+    w2 = torch.cat([w, torch.eye(v, device="cuda")[:, :m]], 1)     # column k + i lifts row y_i's logit
+    x2 = torch.cat([x, torch.zeros((m, m), device="cuda")], 1)
+    w2[:, k:] = 0.0
+    for i in range(m):
+        w2[y[i], k + i] = 1.0
+        x2[i, k + i] = 26.0
+    losses, dx, dw = ops.linear_cross_entropy_step(x2, w2, y)
+    e = Exact(x2, w2, y)
+    assert float(e.losses.max()) < 1e-7
+    e.check(losses, dx, dw)
+    assert bool(((losses.double() - e.losses).abs() <= 1e-4 * e.losses).all())
+
+
+def test_large_logits(ops):
+    x, w, y = inputs(25, 70, 500, 64, F32, F32, holes=0.0)
+    x *= 200
+    e = Exact(x, w, y)
+    losses, dx, dw = ops.linear_cross_entropy_step(x, w, y)
+    assert float(e.losses.max()) > 500
+    e.check(losses, dx, dw)
+
+
+# --------------------------------------------------------------- layouts and calls
+def test_shapes_strides_and_types(ops):
+    x, w, y = inputs(27, 48, 300, 64)
+    want = ops.linear_cross_entropy_step(x, w, y)
+    got = ops.linear_cross_entropy_step(x.view(4, 12, 64), w, y.view(4, 12))
+    assert got[0].shape == (4, 12) and got[1].shape == (4, 12, 64)
+    for a, b in zip(got, want):
+        assert torch.equal(a.reshape(b.shape), b)
+    turned = x.t().contiguous().t()
+    wide = torch.stack([y, y - 7], 1)
+    for xx, ww, yy in ((pitched(x), w, y), (turned, w, y), (x, pitched(w), y), (x, w.t().contiguous().t(), y), (x, w, wide[:, 0]),
+                       (x, pitched(w, 8), y.int()), (pitched(x, 3)[:, :], pitched(w, 64), y)):
+        for a, b in zip(ops.linear_cross_entropy_step(xx, ww, yy), want):
+            assert torch.equal(a, b)
+    one = ops.linear_cross_entropy_step(x[0], w, y[0])
+    assert one[0].shape == () and one[1].shape == (64,)
+    odd = torch.empty(300 * 64 + 1, device="cuda", dtype=BF16)[1:].view(300, 64).copy_(w)   # not 16-byte aligned
+    for a, b in zip(ops.linear_cross_entropy_step(x, odd, y), want):
+        assert torch.equal(a, b)
+
+
+def test_gradient_weights(ops):
+    x, w, y = inputs(29, 64, 200, 64, F32, F32)
+    row = torch.rand(64, device="cuda", generator=gen(30))
+    wide = torch.stack([row, -row], 1)
+    e = Exact(x, w, y, row)
+    e.check(*ops.linear_cross_entropy_step(x, w, y, grad=row))
+    e.check(*ops.linear_cross_entropy_step(x, w, y, grad=wide[:, 0]))
+    half_ = Exact(x, w, y, torch.full((64,), 0.5, device="cuda"))
+    half_.check(*ops.linear_cross_entropy_step(x, w, y, grad=0.5))
+    half_.check(*ops.linear_cross_entropy_step(x, w, y, grad=torch.tensor(0.5, device="cuda")))
+    half_.check(*ops.linear_cross_entropy_step(x, w, y, grad=torch.tensor(0.5, device="cuda").expand(64)))
+    losses, dx, dw = ops.linear_cross_entropy_step(x.view(8, 8, 64), w, y.view(8, 8), grad=torch.full((8, 8), 0.5, device="cuda"))
+    half_.check(losses.view(-1), dx.view(64, 64), dw)
+
+
+def test_weight_gradient_in_place(ops):
+    x, w, y = inputs(31, 100, 300, 64)
+    _, _, want = ops.linear_cross_entropy_step(x, w, y)
+    store = torch.full((300, 80), 7.0, device="cuda", dtype=BF16)
+    out = store[:, :64]
+    assert ops.linear_cross_entropy_step(x, w, y, out=out)[2] is out
+    assert torch.equal(out, want) and bool((store[:, 64:] == 7).all())
+    empty = out.clone()
+    ops.linear_cross_entropy_step(x[:0], w, y[:0], out=empty, accumulate=True)
+    assert torch.equal(empty, out)
+    losses, dx, dw = ops.linear_cross_entropy_step(x[:0], w, y[:0])
+    assert losses.shape == (0,) and dx.shape == (0, 64) and bool((dw == 0).all())
+
+
+@pytest.mark.parametrize("m", [20, 300])
+def test_autograd_and_differences(ops, m):
+    x, w, y = inputs(33, m, 150, 48, F32, F32)
+    x.requires_grad_(), w.requires_grad_()
+    g = torch.rand(m, device="cuda", generator=gen(34))
+    loss = (ops.linear_cross_entropy(x, w, y) * g).sum()
+    dx, dw = torch.autograd.grad(loss, (x, w))
+    Exact(x.detach(), w.detach(), y, g).check(None, dx, dw)
+    # Along a direction, in 64 bits of the same function: the difference's own error is h^2 and rounding / h.
+    def f(xx, ww):
+        z = xx.double() @ ww.double().t()
+        there = (y >= 0) & (y < 150)
+        l = torch.nn.functional.cross_entropy(z, torch.where(there, y, 0), reduction="none")
+        return float((torch.where(there, l, 0.0) * g.double()).sum())
+    ux, uw = torch.randn_like(x).double(), torch.randn_like(w).double()
+    h = 1e-5
+    num = (f(x.detach().double() + h * ux, w.detach().double() + h * uw) - f(x.detach().double() - h * ux, w.detach().double() - h * uw)) / (2 * h)
+    ana = float((dx.double() * ux).sum() + (dw.double() * uw).sum())
+    assert abs(num - ana) <= 1e-5 * (abs(num) + float(dx.norm() + dw.norm()))
+    mean = ops.linear_cross_entropy(x, w, y).mean()
+    dx2, = torch.autograd.grad(mean, x)
+    Exact(x.detach(), w.detach(), y, torch.full((m,), 1 / m, device="cuda")).check(None, dx2, None)
+    only, = torch.autograd.grad(ops.linear_cross_entropy(x.detach(), w, y).sum(), w)
+    Exact(x.detach(), w.detach(), y).check(None, None, only)
+    with pytest.raises(RuntimeError):
+        gg, = torch.autograd.grad((ops.linear_cross_entropy(x, w, y) * g.requires_grad_()).sum(), x, create_graph=True)
+        gg.sum().backward()
+
+
+def test_equal_calls_give_equal_bits(ops):
+    x, w, y = inputs(35, 1000, 3000, 128)
+    a = ops.linear_cross_entropy_step(x, w, y)
+    for _ in range(3):
+        for p, q in zip(ops.linear_cross_entropy_step(x, w, y), a):
+            assert torch.equal(p, q)
+
+
+def test_another_stream(ops):
+    x, w, y = inputs(37, 300, 700, 64)
+    want = ops.linear_cross_entropy_step(x, w, y)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = ops.linear_cross_entropy_step(pitched(x), w, y, stream=s)
+    losses = ops.linear_cross_entropy(x, w, y, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert torch.equal(losses, want[0])
+
+
+def test_captured_and_replayed(ops):
+    """Two graphs with workspaces of their own, replayed in turn with eager work between."""
+    sets = [inputs(39 + i, 200, 600, 64, holes=0.2) for i in range(2)]
+    out = [torch.zeros((600, 64), device="cuda") for _ in sets]
+    graphs, results = [], []
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for (x, w, y), o in zip(sets, out):
+            ops.linear_cross_entropy_step(x, w, y, out=o)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    for (x, w, y), o in zip(sets, out):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            results.append(ops.linear_cross_entropy_step(x, w, y, out=o))
+        graphs.append(g)
+    for turn in range(3):
+        for i, (x, w, y) in enumerate(sets):
+            x.copy_(inputs(50 + 2 * turn + i, 200, 600, 64)[0])
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for (x, w, y), r in zip(sets, results):
+            for a, b in zip(ops.linear_cross_entropy_step(x, w, y, out=torch.zeros((600, 64), device="cuda")), r):
+                assert torch.equal(a, b)
+
+
+def test_rows_behind_the_last_stay(ops):
+    """Outputs end where their rows do."""
+    x, w, y = inputs(41, 33, 70, 20, F32, F32)
+    store = torch.full((75, 20), 3.0, device="cuda")
+    ops.linear_cross_entropy_step(x, w, y, out=store[:70])
+    assert bool((store[70:] == 3).all())

@@ -1,0 +1,430 @@
+"""One AdamW step over many tensors against a plain implementation in 64 bits, and its 8-bit
+moments against an implementation of their definition on the host, bit by bit.
+
+u = 2^-24 is float32's unit roundoff.  m' = b1 m + c1 g has two rounded products and their sum:
+off by 2 u (|b1 m| + |c1 g|); v' has one product more.  The update m' rate / (sqrt(v') root + eps)
+adds 8 roundings of its own at most, and the parameter three."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_05088_amd import libmalt as lm
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    lm.lib()
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2608_05088_amd import ops as module
+    return module
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def f32(x):
+    return float(np.float32(x))
+
+
+HP = dict(lr=6e-4, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.1)
+
+
+def tensors(seed, shapes, pt=F32, gt=F32):
+    g = gen(seed)
+    ps = [(torch.randn(s, device="cuda", generator=g) * 0.02).to(pt) for s in shapes]
+    gs = [(torch.randn(s, device="cuda", generator=g) * 1e-3).to(gt) for s in shapes]
+    return ps, gs
+
+
+def moments32(seed, shapes):
+    g = gen(seed)
+    return [torch.stack([torch.randn(math.prod(s), device="cuda", generator=g) * 3e-4,
+                         torch.rand(math.prod(s), device="cuda", generator=g) * 1e-6]) for s in shapes]
+
+
+def check(p0, p1, g, m0, v0, m1, v1, step, scale=1.0, lr=6e-4, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.1):
+    """A parameter after the step against 64 bits, from the float32 constants that the step uses."""
+    p, g, m, v = (t.double().flatten() for t in (p0, g, m0, v0))
+    g = g * f32(scale)
+    b1, c1, b2, c2 = f32(betas[0]), f32(1 - betas[0]), f32(betas[1]), f32(1 - betas[1])
+    want_m, want_v = b1 * m + c1 * g, b2 * v + c2 * g * g
+    m_err = 2.1 * U * (b1 * m.abs() + c1 * g.abs()) + U * c1 * g.abs()   # and the scaled gradient's rounding
+    v_err = 5 * U * want_v + 1e-44
+    if m1 is not None:
+        assert bool(((m1.double().flatten() - want_m).abs() <= m_err + 1e-44).all())
+        assert bool(((v1.double().flatten() - want_v).abs() <= v_err).all())
+    rate, root = lr / (1 - betas[0] ** step), 1 / math.sqrt(1 - betas[1] ** step)
+    den = want_v.sqrt() * root + eps
+    update = want_m * rate / den
+    want = p * f32(1 - lr * weight_decay) - update
+    err = m_err * rate / den + 12 * U * update.abs() + 3 * U * p.abs() + torch.finfo(p1.dtype).eps / 2 * want.abs() * 1.01
+    off = (p1.double().flatten() - want).abs()
+    assert bool((off <= err + 1e-38).all()), float((off / (err + 1e-38)).max())
+
+
+@pytest.mark.parametrize("pt,gt", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_one_step(ops, pt, gt, bits):
+    shapes = [(1,), (3,), (255,), (256,), (257,), (4096,), (4097,), (33, 129), (0,), (5, 1, 7), ()]
+    ps, gs = tensors(1, shapes, pt, gt)
+    states = [ops.adamw_state(p, bits) for p in ps]
+    for step in (1, 2, 7):
+        before, old = [p.clone() for p in ps], ops.adamw_moments(ps, states)
+        ops.adamw_step(ps, gs, states, step=step, seed=step, **HP)
+        new = ops.adamw_moments(ps, states)
+        for p0, p1, g, o, n in zip(before, ps, gs, old, new):
+            assert n.shape == (2, p1.numel())
+            check(p0, p1, g, o[0], o[1], n[0] if bits == 32 else None, n[1], step, **HP)
+
+
+def test_many_tensors_take_several_launches(ops):
+    """More than a launch's 108, of both kinds of moments, an empty one at the border."""
+    shapes = [(i % 7 * 300 + 1,) for i in range(107)] + [(0,)] + [(1000 + i,) for i in range(130)]
+    ps, gs = tensors(2, shapes)
+    states = [ops.adamw_state(p, 8 if i % 3 else 32) for i, p in enumerate(ps)]
+    alone = [p.clone() for p in ps]
+    alone_states = [s.clone() for s in states]
+    before = [p.clone() for p in ps]
+    ops.adamw_step(ps, gs, states, step=3, seed=9, **HP)
+    for i, (p0, p1, g) in enumerate(zip(before, ps, gs)):
+        zero = torch.zeros(p1.numel(), device="cuda")
+        check(p0, p1, g, zero, zero, None, None, 3, **HP)
+    for i in (0, 1, 106, 108, 237):   # the step of a tensor does not depend on the others (its noise does, on its place)
+        ops.adamw_step([alone[i]], [gs[i]], [alone_states[i]], step=3, seed=9, **HP)
+        assert torch.equal(alone[i], ps[i])
+        if states[i].dtype == F32:
+            assert torch.equal(alone_states[i], states[i])
+
+
+def test_a_large_tensor(ops):
+    ps, gs = tensors(3, [(3001, 4999)])
+    states = moments32(4, [(3001, 4999)])
+    old, before = states[0].clone(), ps[0].clone()
+    ops.adamw_step(ps, gs, states, step=100, **HP)
+    check(before, ps[0], gs[0], old[0], old[1], states[0][0], states[0][1], 100, **HP)
+
+
+def test_offsets_past_32_bits(ops):
+    """2^32 + 300 elements: the last block's places, their scales behind 2^33 bytes of codes."""
+    n = (1 << 32) + 300
+    p = torch.zeros(n, device="cuda", dtype=BF16)
+    g = torch.zeros(n, device="cuda", dtype=BF16)
+    p[-300:] = 1.0
+    g[-300:] = torch.randn(300, device="cuda", generator=gen(5)).to(BF16)
+    p[:300] = 1.0
+    g[:300] = g[-300:]
+    st = ops.adamw_state(p, 8)
+    ops.adamw_step([p], [g], [st], step=1, **HP)
+    small = [torch.ones(300, device="cuda", dtype=BF16)]
+    ops.adamw_step(small, [g[:300]], [ops.adamw_state(small[0], 8)], step=1, **HP)
+    assert torch.equal(p[:300], small[0]) and torch.equal(p[-300:], small[0])
+    assert bool((p[300:4000] == 0).all()) and bool((p[-4000:-300] == 0).all())
+    blocks = -(-n // 256)
+    scales = st[512 * blocks:].view(F32)
+    assert scales.numel() == 2 * blocks and int((scales != 0).sum()) == 8   # 300 places: two blocks at either end, m and v
+    del p, g, st
+
+
+# ------------------------------------------------------------------------ 8 bits
+def mixed(x):
+    x = np.uint32(x)
+    with np.errstate(over="ignore"):
+        x = x ^ (x >> np.uint32(16))
+        x = x * np.uint32(0x9E3779B1)
+        x = x ^ (x >> np.uint32(15))
+        x = x * np.uint32(0xBB67AE85)
+        return x ^ (x >> np.uint32(16))
+
+
+def noise(seed, tensor, blocks):
+    lo, hi = seed & 0xFFFFFFFF, seed >> 32
+    key = mixed(np.uint32(lo) ^ mixed(np.uint32((hi + 0x9E3779B1 * (tensor + 1)) & 0xFFFFFFFF)))
+    b = ((int(key) + np.arange(blocks, dtype=np.uint64) * 0x9E3779B1) & 0xFFFFFFFF).astype(np.uint32)
+    r = mixed(mixed(b)[:, None] ^ np.arange(256, dtype=np.uint32)[None])
+    return ((r & np.uint32(0xFFFF)).astype(np.float32) + np.float32(0.5)) / np.float32(65536), \
+           ((r >> np.uint32(16)).astype(np.float32) + np.float32(0.5)) / np.float32(65536)
+
+
+def value_of(code, exponent_bits, bias):
+    """What a code's exponent and mantissa bits stand for."""
+    e, f = code >> 3 & ((1 << exponent_bits) - 1), code & 7
+    return f * 2.0 ** (1 - bias - 3) if e == 0 else (8 + f) * 2.0 ** (e - bias - 3)
+
+
+FIRST = np.array([(-1.0 if c & 128 else 1.0) * value_of(c & 127, 4, 7) for c in range(256)], dtype=np.float32)
+SECOND = np.array([value_of(c, 5, 15) for c in range(256)], dtype=np.float32)
+
+
+def decode(state, n):
+    raw = state.cpu().numpy()
+    blocks = -(-n // 256)
+    scales = raw[512 * blocks:].view(np.float32)
+    m = FIRST[raw[:256 * blocks]].reshape(blocks, 256) * scales[:blocks, None]
+    v = SECOND[raw[256 * blocks:512 * blocks]].reshape(blocks, 256) * scales[blocks:, None]
+    return m.reshape(-1)[:n], v.reshape(-1)[:n]
+
+
+def encode(x, u, most, least):
+    """Codes' values and scales of blocks from the definition, every step in float32."""
+    one = np.float32(1)
+    x = x.astype(np.float32)
+    top = np.abs(x).max(1, keepdims=True)
+    some = top >= np.float32(2.0 ** -100)
+    inv = one / np.where(some, top, one) * np.float32(most)
+    t = np.minimum(np.abs(x) * inv, np.float32(most))
+    e = np.maximum(np.frexp(t)[1] - 1, least)
+    step = np.ldexp(one, e - 3).astype(np.float32)
+    r = np.floor((t / step).astype(np.float32) + u).astype(np.float32) * step
+    return r, step, np.where(some, top * (one / np.float32(most)), np.float32(0)), some
+
+
+@pytest.mark.parametrize("pt,n", [(F32, 1), (F32, 255), (F32, 256), (BF16, 4097), (F32, 70000)])
+def test_moments_in_8_bits_bit_by_bit(ops, pt, n):
+    ps, gs = tensors(n, [(n,), (n,)], pt)
+    gs[1] *= torch.where(torch.rand(n, device="cuda", generator=gen(n + 1)) < 0.5, 1e-5, 1.0)   # far apart within a block
+    states = [ops.adamw_state(p, 8) for p in ps]
+    for step in range(1, 5):
+        seed = (step * 0x123456789ABCDEF) & ((1 << 64) - 1)
+        old = [decode(s, n) for s in states]
+        ops.adamw_step(ps, gs, states, step=step, seed=seed, **HP)
+        for i, (st, g, (m, v)) in enumerate(zip(states, gs, old)):
+            blocks = -(-n // 256)
+            um, uv = noise(seed, i, blocks)
+            pad = lambda t: np.pad(t, (0, blocks * 256 - n)).reshape(blocks, 256)  # noqa: E731
+            g = g.float().cpu().numpy()
+            b1, c1, b2, c2 = (np.float32(t) for t in (0.9, 1 - 0.9, 0.95, 1 - 0.95))
+            m, v = pad(m * b1 + g * c1), pad(v * b2 + (g * c2) * g)
+            rm, _, sm, some_m = encode(m, um, 448, -6)
+            rv, step_v, sv, some_v = encode(v, uv, 61440, -14)
+            rv = np.where(v > 0, np.maximum(rv, step_v), rv)
+            raw = st.cpu().numpy()
+            scales = raw[512 * blocks:].view(np.float32)
+            assert np.array_equal(scales[:blocks], sm[:, 0]) and np.array_equal(scales[blocks:], sv[:, 0])
+            got_m, got_v = FIRST[raw[:256 * blocks]].reshape(blocks, 256), SECOND[raw[256 * blocks:512 * blocks]].reshape(blocks, 256)
+            assert np.array_equal(got_m, np.where(some_m, np.copysign(rm, m), 0)) and np.array_equal(got_v, np.where(some_v, rv, 0))
+        for st, mv in zip(states, ops.adamw_moments(ps, states)):
+            m, v = decode(st, n)
+            assert np.array_equal(mv[0].cpu().numpy(), m) and np.array_equal(mv[1].cpu().numpy(), v)
+
+
+def test_rounding_is_right_on_average(ops):
+    """4000 seeds: the mean of a moment's codes is the moment, to five standard errors of a
+    rounding to one of two neighbours (at most half a step each)."""
+    n, seeds = 256, 4000
+    g = torch.randn(n, device="cuda", generator=gen(7)) * 1e-3
+    total = torch.zeros((2, n), device="cuda", dtype=torch.float64)
+    p = [torch.zeros(n, device="cuda")]
+    exact = [ops.adamw_state(p[0])]
+    ops.adamw_step(p, [g], exact, step=1, **HP)
+    for s in range(seeds):
+        st = [ops.adamw_state(p[0], 8)]
+        ops.adamw_step(p, [g], st, step=1, seed=s * 0x9E3779B97F4A7C15 & ((1 << 64) - 1), **HP)
+        total += ops.adamw_moments(p, st)[0]
+    mean, want = total / seeds, exact[0].double()
+    for i, (most, least) in enumerate(((448.0, -6), (61440.0, -14))):
+        scale = want[i].abs().max() / most
+        step = torch.exp2(torch.floor(torch.log2(want[i].abs() / scale)).clamp_min(least) - 3) * scale
+        near = want[i].abs() >= step      # what is below the least code never becomes zero (second moments)
+        off = (mean[i] - want[i]).abs()
+        assert bool((off <= 5 * 0.5 * step / math.sqrt(seeds) + 2.0 ** -16 * step)[near].all())
+
+
+def test_small_changes_add_up(ops):
+    """beta2 = 0.999: a second moment changes by a thousandth of itself a step, a sixtieth of a code's step.  Under
+    rounding to nearest it would stand still; here it follows its average."""
+    n, steps = 4096, 3000
+    hp = dict(lr=0.0, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0)
+    p = [torch.zeros(n, device="cuda")]
+    st, ref = [ops.adamw_state(p[0], 8)], [ops.adamw_state(p[0])]
+    big, small = torch.full((n,), 1e-2, device="cuda"), torch.full((n,), 1e-3, device="cuda")
+    big[::256] = small[::256] = 1e-1     # the largest of its block stays: scales do not follow the others
+    for t in range(1, steps + 1):
+        g = [big if t <= steps // 2 else small]
+        ops.adamw_step(p, g, st, step=t, seed=t, **hp)
+        ops.adamw_step(p, g, ref, step=t, **hp)
+    m, v = ops.adamw_moments(p, st)[0].double()
+    want = ref[0][1].double()
+    others = torch.ones(n, dtype=torch.bool, device="cuda")
+    others[::256] = False
+    assert float(want[others].max()) < 0.5 * 1e-4           # it has fallen to a quarter of what it was
+    mean = float(v[others].mean() / want[others].mean())
+    # 4080 places, each a walk of one-step errors that decay with 0.999: its spread is below
+    # half a step (1/16 of the value) times sqrt(1000 / 2) / 8, a quarter of the value; the mean's 64 times less.
+    assert abs(mean - 1) <= 5 * 0.25 / 64 + 0.02, mean
+
+
+def test_blocks_of_nothing_and_of_no_number(ops):
+    n = 1024
+    p = [torch.ones(n, device="cuda")]
+    g = torch.zeros(n, device="cuda")
+    g[300] = float("nan")
+    g[600] = float("inf")
+    g[800:1024] = 1e-25     # squares below 2^-100: a block of zeros
+    st = [ops.adamw_state(p[0], 8)]
+    ops.adamw_step(p, [g], st, step=1, lr=1e-3, weight_decay=0.0)
+    m, v = ops.adamw_moments(p, st)[0]
+    assert bool((m[:256] == 0).all()) and bool((v[:256] == 0).all()) and bool((p[0][:256] == 1).all())
+    assert bool(m[256:512].isnan().all()) and bool(v[256:512].isnan().all()) and bool(m[512:768].isnan().all())
+    assert bool(p[0][300].isnan()) and bool((p[0][256:300] == 1).all())   # the step itself is each element's own
+    assert bool((v[768:] == 0).all()) and bool(m[768:].isfinite().all()) and bool(p[0][768:].isfinite().all())
+    st32 = [ops.adamw_state(p[0])]
+    q = [torch.ones(n, device="cuda")]
+    ops.adamw_step(q, [g], st32, step=1, lr=1e-3, weight_decay=0.0)
+    assert int(st32[0][0].isnan().sum()) == 1 and int(q[0].isnan().sum()) == 2   # inf / inf
+
+
+def test_updates_stay_bounded_where_moments_are_small(ops):
+    """Gradients of 1e-9 beside one of 1: second moments 1e-18 of the largest do not vanish before first moments do."""
+    n = 2560
+    g = torch.full((n,), 1e-9, device="cuda")
+    g[::256] = 1.0
+    p = [torch.zeros(n, device="cuda")]
+    st = [ops.adamw_state(p[0], 8)]
+    for t in range(1, 60):
+        before = p[0].clone()
+        ops.adamw_step(p, [g if t < 5 else torch.zeros_like(g)], st, lr=1e-3, betas=(0.9, 0.95), eps=1e-12, weight_decay=0.0,
+                       step=t, seed=t)
+        # |m| / sqrt(v) of the smallest codes: one step of the first (2^-9 / 448 of the largest), the root of one of
+        # the second (2^-17 / 61440), each a largest apart of at most 0.1 / sqrt(0.05); bias corrections at most 10.
+        assert float((p[0] - before).abs().max()) <= 1e-3 * 10 * 2.0
+
+
+# --------------------------------------------------------------------- the calls
+def test_gradient_scale(ops):
+    shapes = [(1000,), (77, 3)]
+    for bits in (32, 8):
+        res = []
+        for scale in (0.25, torch.tensor(0.25, device="cuda"), torch.tensor([0.25], device="cuda")):
+            ps, gs = tensors(8, shapes)
+            states = [ops.adamw_state(p, bits) for p in ps]
+            before = [p.clone() for p in ps]
+            ops.adamw_step(ps, gs, states, step=2, grad_scale=scale, **HP)
+            for p0, p1, g in zip(before, ps, gs):
+                z = torch.zeros(g.numel(), device="cuda")
+                check(p0, p1, g, z, z, None, None, 2, scale=0.25, **HP)
+            res.append(ps + states)
+        for r in res[1:]:
+            for a, b in zip(r, res[0]):
+                assert torch.equal(a, b)
+
+
+def test_strided_gradients_streams_and_versions(ops):
+    ps, gs = tensors(9, [(64, 48), (1000,)])
+    states = [ops.adamw_state(p, 8) for p in ps]
+    qs, other = [p.clone() for p in ps], [s.clone() for s in states]
+    saved = ps[0].clone().requires_grad_()
+    product = (saved * 1.0)
+    square = (product * product).sum()
+    ops.adamw_step(ps, gs, states, step=1, seed=3, **HP)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    turned = [gs[0].t().contiguous().t(), torch.stack([gs[1], gs[1]], 1)[:, 0]]
+    s.wait_stream(torch.cuda.current_stream())
+    ops.adamw_step(qs, turned, other, step=1, seed=3, stream=s, **HP)
+    torch.cuda.current_stream().wait_stream(s)
+    for a, b in zip(ps + states, qs + other):
+        assert torch.equal(a, b)
+    ops.adamw_step([product.detach()], [gs[0]], [ops.adamw_state(product.detach())], step=1, **HP)
+    with pytest.raises(RuntimeError, match="inplace"):
+        square.backward()
+
+
+def test_views_of_one_buffer(ops):
+    """Parameters at odd offsets of a flat buffer; what lies between them stays."""
+    flat = torch.full((5000,), 7.0, device="cuda")
+    cuts = [(1, 300), (303, 1), (305, 1023), (2001, 2048)]
+    ps = [flat[a:a + n] for a, n in cuts]
+    before = [p.clone() for p in ps]
+    gs = [torch.randn(n, device="cuda", generator=gen(n)) for _, n in cuts]
+    ops.adamw_step(ps, gs, [ops.adamw_state(p) for p in ps], step=1, **HP)
+    for p0, p1, g in zip(before, ps, gs):
+        z = torch.zeros(g.numel(), device="cuda")
+        check(p0, p1, g, z, z, None, None, 1, **HP)
+    rest = torch.ones(5000, dtype=torch.bool, device="cuda")
+    for a, n in cuts:
+        rest[a:a + n] = False
+    assert bool((flat[rest] == 7).all())
+
+
+def test_captured_and_replayed(ops):
+    """A captured call repeats its step; two graphs in turn, eager work between."""
+    sets = []
+    for i in range(2):
+        ps, gs = tensors(20 + i, [(3000,), (17, 5)])
+        sets.append((ps, gs, [ops.adamw_state(p, 8) for p in ps]))
+    twins = [([p.clone() for p in ps], gs, [s.clone() for s in st]) for ps, gs, st in sets]
+    graphs = []
+    for ps, gs, st in sets:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            ops.adamw_step(ps, gs, st, step=4, seed=11, **HP)
+        graphs.append(g)
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+        for ps, gs, st in twins:
+            ops.adamw_step(ps, gs, st, step=4, seed=11, **HP)
+        torch.cuda.synchronize()
+        for (ps, _, st), (qs, _, ot) in zip(sets, twins):
+            for a, b in zip(ps + st, qs + ot):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_the_optimizer(ops, bits):
+    """optim.AdamW against torch's: 32-bit moments to rounding, 8-bit ones to the moments' rounding; and resumed bitwise."""
+    from paper_2608_05088_amd.optim import AdamW
+    ps = [torch.nn.Parameter(torch.randn(s, device="cuda", generator=gen(30))) for s in ((70, 90), (90,), (5000,))]
+    qs = [torch.nn.Parameter(p.detach().clone()) for p in ps]
+    ours = AdamW([dict(params=ps[:1], lr=1e-2), dict(params=ps[1:], weight_decay=0.3)], lr=3e-3, betas=(0.9, 0.95), bits=bits, seed=5)
+    theirs = torch.optim.AdamW([dict(params=qs[:1], lr=1e-2), dict(params=qs[1:], weight_decay=0.3)], lr=3e-3, betas=(0.9, 0.95))
+    def grads(t, params):
+        for i, p in enumerate(params):
+            p.grad = None if i == 1 and t == 2 else torch.randn(p.shape, device="cuda", generator=gen(100 * t + i)) + 0.5
+    for t in range(1, 9):
+        grads(t, ps), grads(t, qs)
+        ours.step(), theirs.step()
+    assert [ours.state[p]["step"] for p in ps] == [8, 7, 8]
+    assert [ours.state[p]["moments"].dtype for p in ps] == [torch.uint8 if bits == 8 and p.numel() >= 4096 else F32 for p in ps]
+    for p, q in zip(ps, qs):
+        # Eight steps of lr each, updates of size one: rounded moments (a step of 1/8 in m at most, 1/16 in the root of v)
+        # change an update by 0.2 at most; in 32 bits by 1e-5.
+        lr = 1e-2 if p is ps[0] else 3e-3
+        far = 8 * lr * (0.2 if ours.state[p]["moments"].dtype == torch.uint8 else 1e-5) + 8 * 4 * U * float(q.detach().abs().max())
+        assert float((p - q).abs().max()) <= far
+    saved = {k: v for k, v in ours.state_dict().items()}
+    rs = [torch.nn.Parameter(p.detach().clone()) for p in ps]
+    again = AdamW([dict(params=rs[:1], lr=1e-2), dict(params=rs[1:], weight_decay=0.3)], lr=3e-3, betas=(0.9, 0.95), bits=bits, seed=5)
+    again.load_state_dict(saved)
+    grads(9, ps), grads(9, rs)
+    ours.step(), again.step()
+    for p, r in zip(ps, rs):
+        assert torch.equal(p, r)
+        assert torch.equal(ours.state[p]["moments"], again.state[r]["moments"])
+
+
+def test_the_optimizer_is_not_captured(ops):
+    from paper_2608_05088_amd.optim import AdamW
+    p = torch.nn.Parameter(torch.zeros(10, device="cuda"))
+    p.grad = torch.ones_like(p)
+    opt = AdamW([p])
+    opt.step()
+    g = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="captured"):
+        with torch.cuda.graph(g):
+            p.detach().add_(0.0)
+            opt.step()

@@ -1,0 +1,310 @@
+"""Root-mean-square norm with a residual's addition, its gradient and its 8-bit output,
+against plain implementations in 64 bits.
+
+u = 2^-24 is float32's unit roundoff.  r = 1 / rms is rounded once from 64 bits, y = (h r) w twice:
+3 u |y| and the output's rounding.  A row's sum in the gradient has at most 64 additions in a
+row, a weight's gradient rows / 1024 + 100."""
+import pytest
+import torch
+
+from paper_2608_05088_amd import libmalt as lm
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+U = 2.0 ** -24
+EPS = 1e-5
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    lm.lib()
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2608_05088_amd import ops as module
+    return module
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def half(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def pitched(x, extra=5):
+    big = torch.full((x.shape[0], x.shape[1] + extra), float("nan"), device=x.device, dtype=x.dtype)
+    view = big[:, :x.shape[1]]
+    view.copy_(x)
+    return view
+
+
+def rows(seed, n, k, t):
+    g = gen(seed)
+    return (torch.randn((n, k), device="cuda", generator=g) * torch.exp(torch.randn((n, 1), device="cuda", generator=g))).to(t)
+
+
+SIZES = [(1, 1), (1, 1280), (3, 7), (5, 8), (2, 127), (4, 128), (9, 513), (600, 130), (2100, 512), (2100, 1024), (2100, 1500),
+         (2100, 2047), (300, 2048), (7, 2049), (5, 4096), (6, 5000), (3, 8192), (2, 8193), (3, 16384), (5000, 24)]
+
+
+@pytest.mark.parametrize("t,wt,out", [(F32, F32, None), (BF16, F32, None), (BF16, BF16, F32), (F32, BF16, BF16)])
+@pytest.mark.parametrize("n,k", SIZES)
+@pytest.mark.parametrize("res", [False, True])
+def test_norm_and_gradient(ops, n, k, t, wt, out, res):
+    x, w = rows(n + k, n, k, t), (1 + 0.3 * torch.randn(k, device="cuda", generator=gen(k))).to(wt)
+    r = rows(n + k + 1, n, k, t) if res else None
+    out = out or t
+    x.requires_grad_(), w.requires_grad_()
+    if res:
+        r.requires_grad_()
+    got = ops.rms_norm(x, w, residual=r, eps=EPS, out_dtype=None if out == t else out)
+    y, h = got if res else (got, x)
+    want_h = (x.detach().float() + r.detach().float()).to(t) if res else x.detach()
+    assert torch.equal(h, want_h) and y.dtype == out
+    h64, w64 = want_h.double(), w.detach().double()
+    rms = torch.sqrt(h64.square().mean(1, keepdim=True) + EPS)
+    nrm = h64 / rms
+    want = nrm * w64
+    assert bool(((y.double() - want).abs() <= (3.1 * U + half(out)) * 1.01 * want.abs() + 1e-44).all())
+    dy = rows(3, n, k, out)
+    dh = rows(4, n, k, t) if res else None
+    ins = (x, w) + ((r,) if res else ())
+    grads = torch.autograd.grad((y, h) if res else y, ins, (dy, dh) if res else dy)
+    dn = dy.double() * w64
+    mean = (dn * nrm).mean(1, keepdim=True)
+    want = (dn - nrm * mean) / rms
+    err = 70 * U * (dn.abs() + nrm.abs() * (dn * nrm).abs().mean(1, keepdim=True)) / rms
+    if res:
+        want = want + dh.double()
+        err = err + 2 * U * dh.double().abs()
+        assert torch.equal(grads[0], grads[2])
+    assert grads[0].dtype == t and grads[1].dtype == wt
+    assert bool(((grads[0].double() - want).abs() <= err + half(t) * 1.01 * want.abs() + 1e-38).all())
+    terms = dy.double() * nrm
+    err = (n / 1024 + 104) * U * terms.abs().sum(0)
+    assert bool(((grads[1].double() - terms.sum(0)).abs() <= err + half(wt) * 1.01 * terms.sum(0).abs() + 1e-38).all())
+
+
+def test_differences(ops):
+    """Against differences of the function in 64 bits, along a direction."""
+    x, w, r = rows(5, 20, 100, F32), torch.rand(100, device="cuda", generator=gen(6)), rows(7, 20, 100, F32)
+    dy, dh = rows(8, 20, 100, F32).double(), rows(9, 20, 100, F32).double()
+    def f(a, b, c):
+        h = a.double() + c.double()
+        return float((h / torch.sqrt(h.square().mean(1, keepdim=True) + EPS) * b.double() * dy).sum() + (h * dh).sum())
+    ins = [t.clone().requires_grad_() for t in (x, w, r)]
+    y, h = ops.rms_norm(ins[0], ins[1], residual=ins[2], eps=EPS)
+    grads = torch.autograd.grad((y, h), ins, (dy.float(), dh.float()))
+    dirs = [torch.randn(t.shape, device="cuda", generator=gen(10 + i)).double() for i, t in enumerate((x, w, r))]
+    e = 1e-6
+    num = (f(*(t.double() + e * d for t, d in zip((x, w, r), dirs))) - f(*(t.double() - e * d for t, d in zip((x, w, r), dirs)))) / (2 * e)
+    ana = sum(float((g.double() * d).sum()) for g, d in zip(grads, dirs))
+    assert abs(num - ana) <= 1e-5 * sum(float(g.norm()) for g in grads)
+
+
+def test_which_gradients(ops):
+    """Only those that are asked for, through one output or the other."""
+    x, w, r = rows(11, 30, 200, F32), torch.rand(200, device="cuda", generator=gen(12)), rows(13, 30, 200, F32)
+    dy, dh = rows(14, 30, 200, F32), rows(15, 30, 200, F32)
+    full = [t.clone().requires_grad_() for t in (x, w, r)]
+    y, h = ops.rms_norm(full[0], full[1], residual=full[2])
+    want = torch.autograd.grad((y, h), full, (dy, dh), retain_graph=True)
+    for i in range(3):
+        some = [t.clone().requires_grad_(j == i) for j, t in enumerate((x, w, r))]
+        y2, h2 = ops.rms_norm(some[0], some[1], residual=some[2])
+        outs, gs = ((y2,), (dy,)) if i == 1 else ((y2, h2), (dy, dh))
+        got, = torch.autograd.grad(outs, some[i], gs)
+        assert torch.equal(got, want[i])
+    gx, gr = torch.autograd.grad(h, (full[0], full[2]), dh, retain_graph=True)
+    assert torch.equal(gx, dh) and torch.equal(gr, dh)
+    y_only, = torch.autograd.grad(y, full[0], dy, retain_graph=True)
+    assert bool(((y_only + dh) - want[0]).abs().max() <= 4 * U * (y_only.abs() + dh.abs()).max())
+    plain = ops.rms_norm(x, w)
+    assert not plain.requires_grad
+    leaf = x.clone().requires_grad_()
+    ops.rms_norm(leaf, w).backward(dy)
+    ops.rms_norm(leaf, w).backward(dy)   # accumulated
+    once, = torch.autograd.grad(ops.rms_norm(leaf, w), leaf, dy)
+    assert torch.equal(leaf.grad, 2 * once)
+    g = dy.clone().requires_grad_()
+    gx, = torch.autograd.grad(ops.rms_norm(leaf, w), leaf, g, create_graph=True)
+    with pytest.raises(RuntimeError, match="twice"):
+        gx.sum().backward()
+
+
+def test_shared_input(ops):
+    """One tensor as x and as the residual: its gradients add up."""
+    x, w = rows(16, 12, 64, F32).requires_grad_(), torch.ones(64, device="cuda")
+    y, h = ops.rms_norm(x, w, residual=x)
+    dy = rows(17, 12, 64, F32)
+    got, = torch.autograd.grad(y, x, dy)
+    a = x.detach().clone().requires_grad_()
+    y2, _ = ops.rms_norm(a, w, residual=x.detach())
+    one, = torch.autograd.grad(y2, a, dy)
+    assert torch.equal(got, 2 * one)
+
+
+# ------------------------------------------------------------------------ 8 bits
+def eight(y):
+    """The values that the 8-bit form of float32 rows stands for, on the host."""
+    y = y.cpu()
+    n, k = y.shape
+    b = torch.nn.functional.pad(y, (0, -k % 128)).reshape(n, -1, 128)
+    top = b.abs().amax(2, keepdim=True)
+    m, e = torch.frexp(top)
+    e = torch.where(top == 0, 0, torch.where(m > 448 / 512, e - 8, e - 9).clamp_min(-127))
+    q = torch.ldexp(b, -e).to(torch.float8_e4m3fn)
+    return q.view(torch.uint8).reshape(n, -1), (e + 127).to(torch.uint8)[:, :, 0]
+
+
+@pytest.mark.parametrize("n,k", [(1, 1), (1, 128), (2, 1280), (31, 300), (33, 129), (130, 2049), (257, 768), (2200, 500), (3, 16384)])
+@pytest.mark.parametrize("t,wt,res", [(F32, F32, False), (BF16, F32, True), (BF16, BF16, False)])
+def test_8_bit_rows(ops, n, k, t, wt, res):
+    x, w = rows(n * 3 + k, n, k, t), (1 + 0.3 * torch.randn(k, device="cuda", generator=gen(k))).to(wt)
+    r = rows(2, n, k, t) if res else None
+    if n > 3:
+        x[3] = 0
+        if res:
+            r[3] = 0
+    got = ops.rms_norm_fp8(x, w, residual=r, eps=EPS)
+    q, h = got if res else (got, x)
+    want_h = (x.float() + r.float()).to(t) if res else x
+    assert torch.equal(h, want_h) and q.shape == x.shape
+    # y as its definition has it, each product rounded to float32.
+    rstd = (1 / torch.sqrt(want_h.double().cpu().square().mean(1, keepdim=True) + EPS)).float()
+    y = (want_h.float().cpu() * rstd) * w.float().cpu()
+    values, scales = eight(y)
+    assert torch.equal(q.values.view(torch.uint8).cpu(), values)
+    i = torch.arange(n)
+    at = 128 * (i // 128) + 8 * (i % 16) + (i // 16) % 8
+    assert torch.equal(q.scales.cpu()[:, at].t(), scales)
+
+
+@pytest.mark.parametrize("m", [1, 2, 15, 16, 17, 32, 33, 200])
+@pytest.mark.parametrize("k,n", [(128, 16), (300, 77), (1280, 640)])
+@pytest.mark.parametrize("out", [F32, BF16])
+def test_layer_on_8_bit_rows(ops, m, k, n, out):
+    """The same bits as the layer makes of the float32 rows that the norm would have written."""
+    x, w = rows(m + k, m, k, BF16), 1 + 0.3 * torch.randn(k, device="cuda", generator=gen(k))
+    values, scales = ops.fp8_quantize_weight(torch.randn((n, k), device="cuda", generator=gen(n)) * 0.05)
+    y = ops.rms_norm(x, w, out_dtype=F32)
+    q = ops.rms_norm_fp8(x, w)
+    want = ops.fp8_forward(y, values, scales, out_dtype=out)
+    got = ops.fp8_forward(q, values, scales, out_dtype=out)
+    assert torch.equal(got, want) and got.shape == (m, n)
+    assert torch.equal(ops.fp8_forward(q, values, scales), ops.fp8_forward(q, values, scales, out_dtype=BF16))
+
+
+# --------------------------------------------------------------- layouts and calls
+def test_shapes_and_strides(ops):
+    x, w, r = rows(21, 24, 96, BF16), torch.rand(96, device="cuda", generator=gen(22)), rows(23, 24, 96, BF16)
+    y, h = ops.rms_norm(x, w, residual=r)
+    for xx, rr in ((pitched(x), r), (x, pitched(r, 8)), (x.t().contiguous().t(), r), (x, torch.stack([r, r], 2)[:, :, 0])):
+        a, b = ops.rms_norm(xx, w, residual=rr)
+        assert torch.equal(a, y) and torch.equal(b, h)
+    a, b = ops.rms_norm(x.view(2, 3, 4, 96), w, residual=r.view(2, 3, 4, 96))
+    assert a.shape == (2, 3, 4, 96) and torch.equal(a.view(24, 96), y) and torch.equal(b.view(24, 96), h)
+    assert torch.equal(ops.rms_norm(x, torch.stack([w, w], 1)[:, 0]), ops.rms_norm(x, w))
+    one, two = ops.rms_norm(x[0], w, residual=r[0])
+    assert one.shape == (96,) and torch.equal(one, y[0]) and torch.equal(two, h[0])
+    q, h8 = ops.rms_norm_fp8(x.view(2, 12, 96), w, residual=r.view(2, 12, 96))
+    assert q.shape == (2, 12, 96) and q.values.shape == (24, 128) and h8.shape == (2, 12, 96)
+    values, scales = ops.fp8_quantize_weight(torch.randn((8, 96), device="cuda", generator=gen(24)))
+    assert ops.fp8_forward(q, values, scales).shape == (2, 12, 8)
+    z = torch.zeros((0, 96), device="cuda", requires_grad=True)
+    wz = w.clone().requires_grad_()
+    out = ops.rms_norm(z, wz)
+    gz, gw = torch.autograd.grad(out, (z, wz), out.detach())
+    assert gz.shape == (0, 96) and bool((gw == 0).all())
+    assert ops.fp8_forward(ops.rms_norm_fp8(z.detach(), w), values, scales).shape == (0, 8)
+    # Gradients that lie otherwise.
+    leaf = x.float().requires_grad_()
+    dy = rows(25, 24, 96, F32)
+    want, = torch.autograd.grad(ops.rms_norm(leaf, w), leaf, dy)
+    got, = torch.autograd.grad(ops.rms_norm(leaf, w), leaf, dy.t().contiguous().t())
+    assert torch.equal(got, want)
+    got, = torch.autograd.grad(ops.rms_norm(leaf, w).sum(), leaf)
+    want, = torch.autograd.grad(ops.rms_norm(leaf, w), leaf, torch.ones_like(dy))
+    assert torch.equal(got, want)
+
+
+def test_no_numbers_stay_in_their_rows(ops):
+    x, w = rows(26, 9, 200, F32), torch.ones(200, device="cuda")
+    want = ops.rms_norm(x, w)
+    x[2, 3], x[5, 0] = float("nan"), float("inf")
+    y = ops.rms_norm(x, w)
+    keep = [0, 1, 3, 4, 6, 7, 8]
+    assert torch.equal(y[keep], want[keep]) and bool(y[2].isnan().all()) and bool(y[5, 0].isnan())
+    values, scales = ops.fp8_quantize_weight(torch.eye(200, device="cuda"))
+    out = ops.fp8_forward(ops.rms_norm_fp8(x, w), values, scales, out_dtype=F32)
+    assert bool(out[2].isnan().all()) and bool(out[keep].isfinite().all())
+
+
+def test_extreme_rows(ops):
+    """Squares past float32's range, in either direction."""
+    x = torch.full((2, 64), 1e30, device="cuda")
+    x[1] = 1e-30
+    y = ops.rms_norm(x, torch.ones(64, device="cuda"), eps=0.0)
+    assert bool(((y - 1).abs() <= 4 * U).all())
+
+
+def test_another_stream_and_equal_bits(ops):
+    x, w, r = rows(27, 3000, 700, BF16), torch.rand(700, device="cuda", generator=gen(28)), rows(29, 3000, 700, BF16)
+    y, h = ops.rms_norm(x, w, residual=r)
+    q, _ = ops.rms_norm_fp8(x, w, residual=r)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    a, b = ops.rms_norm(x, w, residual=pitched(r), stream=s)
+    q2, _ = ops.rms_norm_fp8(x, w, residual=r, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(a, y) and torch.equal(b, h) and torch.equal(q.values.view(torch.uint8), q2.values.view(torch.uint8))
+    leaf, lw = x.clone().requires_grad_(), w.clone().requires_grad_()
+    dy = rows(30, 3000, 700, BF16)
+    want = torch.autograd.grad(ops.rms_norm(leaf, lw), (leaf, lw), dy)
+    with torch.cuda.stream(s):
+        s.wait_stream(torch.cuda.current_stream())
+        out = ops.rms_norm(leaf, lw)
+    torch.cuda.current_stream().wait_stream(s)
+    got = torch.autograd.grad(out, (leaf, lw), dy)   # the backward pass runs on the forward's stream
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_captured_and_replayed(ops):
+    values, scales = ops.fp8_quantize_weight(torch.randn((64, 256), device="cuda", generator=gen(31)))
+    w = torch.rand(256, device="cuda", generator=gen(32)).requires_grad_()
+    xs = [rows(33 + i, 40, 256, F32) for i in range(2)]
+    dy = rows(40, 40, 256, F32)
+    def work(x):
+        leaf = x.detach().requires_grad_()
+        y = ops.rms_norm(leaf, w)
+        return (*torch.autograd.grad(y, (leaf, w), dy), ops.fp8_forward(ops.rms_norm_fp8(x, w.detach()), values, scales))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for x in xs:
+            work(x)
+    torch.cuda.current_stream().wait_stream(s)
+    graphs, results = [], []
+    for x in xs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            results.append(work(x))
+        graphs.append(g)
+    for turn in range(3):
+        for i, x in enumerate(xs):
+            x.copy_(rows(50 + 2 * turn + i, 40, 256, F32))
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for x, r in zip(xs, results):
+            for a, b in zip(work(x), r):
+                assert torch.equal(a, b)

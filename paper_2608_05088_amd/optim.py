@@ -81,10 +81,13 @@ class AdamW(torch.optim.Optimizer):
                     st["step"] = 0
                     st["moments"] = ops.adamw_state(p, 8 if self.bits == 8 and p.numel() >= self.min_8bit else 32)
                 calls.setdefault((p.device, st["step"] + 1), []).append(p)
-            for i, ((_, t), ps) in enumerate(calls.items()):
+            place = {id(p): i for i, p in enumerate(g["params"])}
+            for (_, t), ps in calls.items():
+                # No other call has this group, first parameter and step count of it.
+                noise = (t * 0x9E3779B1 + k * 0xBB67AE85 + place[id(ps[0])] * 0xA54FF53B) & 0xFFFFFFFF
                 ops.adamw_step(ps, [p.grad for p in ps], [self.state[p]["moments"] for p in ps], lr=g["lr"],
                                betas=g["betas"], eps=g["eps"], weight_decay=g["weight_decay"], step=t,
-                               seed=self.seed << 32 | (t * 1000003 + k * 1009 + i) & 0xFFFFFFFF)
+                               seed=self.seed << 32 | noise)
                 for p in ps:
                     self.state[p]["step"] = t
         return loss

@@ -227,6 +227,16 @@ struct Product {
   }
 };
 
+// Over the four lanes that hold a row's columns, 16 and 32 lanes apart: exchanges between registers,
+// no round trips through LDS.
+template <class F>
+__device__ __forceinline__ float across(float v, F&& op) {
+  auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = op(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
 // All waves are done with what they read of LDS.
 __device__ __forceinline__ void lds_free() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -294,16 +304,14 @@ void head_first_kernel(HeadLogits a) {
       for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[i][b][e]);
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64)) * LOG2E;
+      top = across(top, [](float a, float b) { return fmaxf(a, b); }) * LOG2E;
       const float ref = top == -__builtin_inff() ? 0.f : top;
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], LOG2E, -ref));
-      sum += __shfl_xor(sum, 16, 64);
-      sum += __shfl_xor(sum, 32, 64);
+      sum = across(sum, [](float a, float b) { return a + b; });
       if (g == 0) join[ml * (NW / 2) + wc] = malt_f32x2{top, sum};
     }
     product.arrived();

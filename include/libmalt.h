@@ -461,10 +461,12 @@ malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, in
  *    every row's loss no number, as the definition does.)
  *  - Logits of -inf have probability zero, and so has a probability below 2^-126; a labelled row without a finite logit is NaN, as are
  *    rows with a NaN or +inf.
- *  - Products of bfloat16 are exact and summed in float32.  float32 values enter products as
- *    three bfloat16 numbers whose sum they are; of their nine products the three smallest, below
- *    2^-24 of the whole each, are left out, the others summed in float32.  Where x or weight is float32 an
- *    infinite value enters as the largest bfloat16 number.  Softmax and losses are float32.  1 - q_y is formed from the other
+ *  - Products of bfloat16 are exact and summed in float32.  Logits of float32 values take 22 bits of
+ *    them (two float16 numbers under a power of two for each row, to 2^-39 of the row's largest), or
+ *    all 24 for up to 32 rows; a product is off by up to 3 2^-22 of itself before it is summed in float32.
+ *    Gradients take float32 values whole, as three bfloat16 numbers; of their nine products the
+ *    three smallest, below 2^-24 of the whole each, are left out.  Where x or weight is float32 an
+ *    infinite value enters as a number past all others.  Softmax and losses are float32.  1 - q_y is formed from the other
  *    columns' sum.  Gradients of type float32 take d, x and weight whole; bfloat16 ones take
  *    d, x and weight rounded to bfloat16, which puts them off by about as much as their own
  *    rounding.

@@ -10,9 +10,10 @@
 
 namespace malt {
 
-// A matrix as bf16 planes whose sum it is: one where it is bf16, three (high, middle, low
-// bits: exact) where it is float32.
-constexpr int HEAD_PLANES = 3;
+// A matrix in the gradients' products as bf16 planes whose sum it is: one where it is bf16, three
+// (high, middle, low bits: exact) where it is float32.  In the logits' products, where one of both is
+// float32: float16 planes, rows scaled to 2^15, one of bf16 and two of float32 (22 bits).
+constexpr int HEAD_PLANES = 3, HEAD_HALVES = 2;
 constexpr int HEAD_TILE = 256;   // output tile edge, and what rows are padded to
 constexpr int HEAD_BK = 64;      // contraction per stage, and what columns are padded to
 
@@ -66,6 +67,9 @@ struct HeadLogits {
   int32_t parts;         // tiles
   // second pass
   const HeadRow* records;   // of the padded rows
+  // float32 operands: float16 planes, rows scaled by powers of two (both null: bf16)
+  const float* x_scales;    // of the padded rows
+  const float* w_scales;    // of the padded vocabulary, from `col0`
   uint16_t* dz;          // packed planes, rows m by n, or null
   uint16_t* dz_t;        // packed planes, rows n by m, or null
   int64_t dz_plane, dz_tile, dz_t_tile;
@@ -114,16 +118,32 @@ struct HeadPack {
   int64_t vocab;
 };
 
-hipError_t launch_head_pack(const HeadPack& a, bool f32, hipStream_t s);
-hipError_t launch_head_pack_t(const HeadPack& a, bool f32, hipStream_t s);
+// Everything that is packed, in one launch.
+struct HeadPrepare {
+  HeadPack part[4];        // x, x^T, weight, weight^T
+  int32_t blocks[4];       // each part's, 0: not wanted; set by the launcher
+  float* scales[2];        // of x and weight: planes of float16, each row under a power of two, and what it was divided by
+  bool halves;
+};
+hipError_t launch_head_prepare(HeadPrepare a, bool x_f32, bool w_f32, hipStream_t s);
 hipError_t launch_head_records(const HeadLabels& l, int64_t rows, int64_t rows_pad, int64_t vocab, const HeadRow* stats,
                                HeadRow* records, hipStream_t s);
 hipError_t launch_head_few(const HeadFew& a, bool x_f32, bool w_f32, hipStream_t s);
-hipError_t launch_head_join(const HeadLabels& rows, int64_t m, int64_t vocab, const malt_f32x2* partial, int parts,
-                            const float* at_label, HeadRow* stats, float* losses, hipStream_t s);
+// A row's parts joined: its loss, its statistics and, for the gradients, its record (of the padded rows).
+struct HeadJoin {
+  HeadLabels rows;
+  int64_t m, rows_pad, vocab;
+  const malt_f32x2* partial;
+  int32_t parts;
+  const float* at_label;
+  HeadRow* stats;      // or null
+  HeadRow* records;    // or null
+  float* losses;       // or null
+};
+hipError_t launch_head_join(const HeadJoin& a, hipStream_t s);
 hipError_t launch_head_logits(const HeadLogits& a, bool second, hipStream_t s);
 hipError_t launch_head_grads(const HeadGrads& a, hipStream_t s);
-hipError_t launch_head_sum(const HeadOut& o, const HeadGrads& a, hipStream_t s);
+hipError_t launch_head_sum(const HeadGrads& a, bool first, bool second, hipStream_t s);
 hipError_t head_setup();
 
 }  // namespace malt

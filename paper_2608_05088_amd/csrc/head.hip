@@ -14,11 +14,15 @@
 // the gradients, dz is written both ways.  (Transposed LDS reads instead: 1.84 us a stage, for one side or
 // both; rows of 32 KB apart: 1.70, with a pitch that is no power of two 1.58.)
 //
-// float32 operands are three bf16 planes whose sum they are.  A product of two is the six plane
-// products that matter (middle by low and low by low are below 2^-24 of it), small ones first,
-// run as a contraction six times as long: float32 sums of exact products, at 2.5 times the rate
-// of the float32 matrix instruction.  bf16 gradients take dz and the operands as single
-// planes: dz is rounded once more, an error of the size of the result's own rounding.
+// float32 operands are planes whose sum they are, and a product of two runs as a contraction over
+// the pairs of planes that matter, small ones first: float32 sums of exact products.
+//   logits: two float16 planes under a power of two for each row, 22 bits; three pairs (low by low is
+//     below 2^-22 of the whole, as the planes' own rounding).
+//   gradients: three bf16 planes, all 24 bits; six pairs (middle by low and low by low are below
+//     2^-24).  float16 would not do for dz, whose values have no row or column of like size.
+// At the matrix cores' 16-bit rate that is three and 1.5 times the float32 instruction's.  bf16
+// gradients take dz and the operands as single planes: dz is rounded once more, an error of the size
+// of the result's own rounding.
 //
 // An XCD's 32 CUs work on 8 x 4 neighbouring tiles at a time, so that the twelve panels they read
 // come once from memory and otherwise from its L2.
@@ -36,12 +40,13 @@ namespace {
 
 using G = NsGeom<HEAD_BK, 2, 32>;
 constexpr int BK = G::BK, STAGES = G::STAGES, H = G::H, RB = G::RB, CPR = G::CPR, LOADS = G::LOADS;
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int NB = TM / 16, NA = TN / 16;
 constexpr float LOG2E = 1.44269504088896340736f;
 // Behind the ring, so that the next tile's first stages can arrive during a tile's epilogue: rows'
-// records or labels of two tiles, and the waves' statistics or 16 rows of each wave's dz (padded by 8 bytes).
+// records or labels and scales of two tiles, and the waves' statistics or 16 rows of each wave's dz (padded by 8 bytes).
 constexpr int ROW_BYTES = HEAD_TILE * 16;
-constexpr int AT_ROWS = G::RING_BYTES, AT_EPI = AT_ROWS + 2 * ROW_BYTES;
+constexpr int AT_ROWS = G::RING_BYTES, AT_SCALES = AT_ROWS + 2 * ROW_BYTES, AT_EPI = AT_SCALES + 2 * HEAD_TILE * 4;
 constexpr int OUT_PITCH = TN * 2 + 8, OUT_WAVE = 16 * OUT_PITCH;
 constexpr int JOIN_BYTES = HEAD_TILE * (NW / 2) * 8;
 constexpr int LDS_BYTES = AT_EPI + (NW * OUT_WAVE > JOIN_BYTES ? NW * OUT_WAVE : JOIN_BYTES);
@@ -97,6 +102,8 @@ struct Loader {
 // A tile's product: prime() starts the loads of its first stages, arrived() waits for this wave's,
 // run() does the rest.
 // acc[a][b][e] = C(row0 + wr TM + 16 b + lane % 16, col0 + wc TN + 16 a + 4 (lane / 16) + e).
+// HALVES: the planes are float16.
+template <bool HALVES>
 struct Product {
   const HeadProduct& g;
   char* const lds;
@@ -209,7 +216,11 @@ struct Product {
         for (int a = 0; a < NA; ++a)
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
-            acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[c][a], fa[c][b], acc[a][b], 0, 0, 0);
+            if constexpr (HALVES)
+              acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, fb[c][a]), __builtin_bit_cast(f16x8, fa[c][b]),
+                                                                 acc[a][b], 0, 0, 0);
+            else
+              acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[c][a], fa[c][b], acc[a][b], 0, 0, 0);
             if (steady && h == H - 1 && a * NB + b < LOADS / 2) issue(a * NB + b);
           }
 #pragma unroll
@@ -237,6 +248,19 @@ __device__ __forceinline__ float across(float v, F&& op) {
   return op(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
+// The scales of this lane's columns into its logits.
+__device__ __forceinline__ void scale_columns(const float* scales, int c, int g, f32x4 (&acc)[NA][NB]) {
+  f32x4 w[NA];
+#pragma unroll
+  for (int i = 0; i < NA; ++i) w[i] = *reinterpret_cast<const MALT_GLOBAL f32x4*>(gptr(scales) + c + 16 * i + 4 * g);
+#pragma unroll
+  for (int i = 0; i < NA; ++i)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][b][e] *= w[i][e];
+}
+
 // All waves are done with what they read of LDS.
 __device__ __forceinline__ void lds_free() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -253,13 +277,14 @@ __device__ __forceinline__ int label_of(const HeadLabels& l, int64_t r, int64_t 
 
 // A workgroup takes every 32nd tile of its XCD's.  While a tile's sums are formed in registers,
 // the next one's first stages arrive.
+template <bool HALVES>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void head_first_kernel(HeadLogits a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   int block = blockIdx.x;
   TileAt t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
   if (t.i < 0) return;
-  Product product(a.g, lds);
+  Product<HALVES> product(a.g, lds);
   const int lane = product.lane, wave = product.wave, wr = wave / (NW / 2), wc = wave % (NW / 2), g = lane >> 4;
   const int KT = stages_of(a.g);
   product.prime(t.i, t.j, 0, KT);
@@ -268,13 +293,19 @@ void head_first_kernel(HeadLogits a) {
     const int64_t m = (int64_t)i * HEAD_TILE + threadIdx.x;
     return threadIdx.x < HEAD_TILE && m < a.g.m ? label_of(a.rows, m, a.vocab) : -1;
   };
+  float* const scales = reinterpret_cast<float*>(lds + AT_SCALES);   // [2][row]
+  auto row_scale = [&](int i) { return HALVES ? gptr(a.x_scales)[(int64_t)i * HEAD_TILE + threadIdx.x % HEAD_TILE] : 1.f; };
   int own = row_label(t.i), turn = 0;
+  float own_scale = row_scale(t.i);
   product.arrived();
   malt_f32x2* const join = reinterpret_cast<malt_f32x2*>(lds + AT_EPI);   // [row][wave column]
   for (;;) {
     const int64_t row0 = (int64_t)t.i * HEAD_TILE, col0 = (int64_t)t.j * HEAD_TILE;
     const int tile_n = t.j;
-    if (threadIdx.x < HEAD_TILE) labels[turn * HEAD_TILE + threadIdx.x] = own;
+    if (threadIdx.x < HEAD_TILE) {
+      labels[turn * HEAD_TILE + threadIdx.x] = own;
+      if (HALVES) scales[turn * HEAD_TILE + threadIdx.x] = own_scale;
+    }
     f32x4 acc[NA][NB];
     product.run(acc);
     lds_free();
@@ -283,19 +314,22 @@ void head_first_kernel(HeadLogits a) {
     if (t.i >= 0) {
       product.prime(t.i, t.j, 0, KT);
       own = row_label(t.i);
+      own_scale = row_scale(t.i);
     }
     const int c = (int)col0 + wc * TN, left = a.g.n - c - 4 * g;   // columns there are from this lane's first
     const bool end = a.g.n - c < TN;
+    if constexpr (HALVES) scale_columns(a.w_scales, c, g, acc);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int ml = wr * TM + b * 16 + (lane & 15), yl = labels[turn * HEAD_TILE + ml] - c;   // the label's place in the wave's columns
+      const float unit = HALVES ? scales[turn * HEAD_TILE + ml] * LOG2E : LOG2E;
       if (end || __builtin_amdgcn_ballot_w64((unsigned)yl < TN)) {
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const bool label = yl == 16 * i + 4 * g + e;
-            if (label) gptr(a.at_label)[row0 + ml] = acc[i][b][e] * LOG2E;
+            if (label) gptr(a.at_label)[row0 + ml] = acc[i][b][e] * unit;
             if (label || 16 * i + e >= left) acc[i][b][e] = -__builtin_inff();
           }
       }
@@ -304,13 +338,13 @@ void head_first_kernel(HeadLogits a) {
       for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[i][b][e]);
-      top = across(top, [](float a, float b) { return fmaxf(a, b); }) * LOG2E;
+      top = across(top, [](float a, float b) { return fmaxf(a, b); }) * unit;
       const float ref = top == -__builtin_inff() ? 0.f : top;
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < NA; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], LOG2E, -ref));
+        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], unit, -ref));
       sum = across(sum, [](float a, float b) { return a + b; });
       if (g == 0) join[ml * (NW / 2) + wc] = malt_f32x2{top, sum};
     }
@@ -334,13 +368,14 @@ void head_first_kernel(HeadLogits a) {
   }
 }
 
+template <bool HALVES>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void head_second_kernel(HeadLogits a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   int block = blockIdx.x;
   TileAt t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
   if (t.i < 0) return;
-  Product product(a.g, lds);
+  Product<HALVES> product(a.g, lds);
   const int lane = product.lane, wave = product.wave, wr = wave / (NW / 2), wc = wave % (NW / 2), g = lane >> 4;
   const int KT = stages_of(a.g);
   product.prime(t.i, t.j, 0, KT);
@@ -349,14 +384,20 @@ void head_second_kernel(HeadLogits a) {
     return *reinterpret_cast<const MALT_GLOBAL f32x4*>(
         gptr(reinterpret_cast<const float*>(a.records + (int64_t)i * HEAD_TILE + threadIdx.x % HEAD_TILE)));
   };
+  float* const scales = reinterpret_cast<float*>(lds + AT_SCALES);   // [2][row]
+  auto row_scale = [&](int i) { return HALVES ? gptr(a.x_scales)[(int64_t)i * HEAD_TILE + threadIdx.x % HEAD_TILE] : 1.f; };
   f32x4 own = record(t.i);
+  float own_scale = row_scale(t.i);
   int turn = 0;
   product.arrived();
   char* const sto = lds + AT_EPI + wave * OUT_WAVE;
   for (;;) {
     const int64_t col0 = (int64_t)t.j * HEAD_TILE;
     const int tile_m = t.i, tile_n = t.j;
-    if (threadIdx.x < HEAD_TILE) records[turn * HEAD_TILE + threadIdx.x] = own;
+    if (threadIdx.x < HEAD_TILE) {
+      records[turn * HEAD_TILE + threadIdx.x] = own;
+      if (HALVES) scales[turn * HEAD_TILE + threadIdx.x] = own_scale;
+    }
     f32x4 acc[NA][NB];
     product.run(acc);
     lds_free();
@@ -365,18 +406,22 @@ void head_second_kernel(HeadLogits a) {
     if (t.i >= 0) {
       product.prime(t.i, t.j, 0, KT);
       own = record(t.i);
+      own_scale = row_scale(t.i);
     }
     const int c = (int)col0 + wc * TN, left = a.g.n - c - 4 * g;
     const bool end = a.g.n - c < TN;
+    if constexpr (HALVES) scale_columns(a.w_scales, c, g, acc);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const f32x4 s = records[turn * HEAD_TILE + wr * TM + b * 16 + (lane & 15)];
+      const int ml = wr * TM + b * 16 + (lane & 15);
+      const f32x4 s = records[turn * HEAD_TILE + ml];
+      const float unit = HALVES ? scales[turn * HEAD_TILE + ml] * LOG2E : LOG2E;
       const int y = __float_as_int(s.w), yl = y < 0 ? -1 : y - (int)a.col0 - c;
 #pragma unroll
       for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          acc[i][b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], LOG2E, -s.x)) * s.y;
+          acc[i][b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], unit, -s.x)) * s.y;
       if (end || __builtin_amdgcn_ballot_w64(y < 0 || (unsigned)yl < TN)) {
         // Zeros in rows that have no gradient, whatever their logits are, and past the end.
 #pragma unroll
@@ -507,7 +552,7 @@ void head_grads_kernel(HeadGrads a) {
   const int64_t row0 = (int64_t)t.i * HEAD_TILE, col0 = (int64_t)t.j * HEAD_TILE;
   const int KT = stages_of(o.g), kt0 = (int)((int64_t)KT * split / o.splits), kt1 = (int)((int64_t)KT * (split + 1) / o.splits);
   f32x4 acc[NA][NB];
-  Product product(o.g, lds);
+  Product<false> product(o.g, lds);
   product.prime(t.i, t.j, kt0, kt1 - kt0);
   product.arrived();
   product.run(acc);
@@ -515,10 +560,10 @@ void head_grads_kernel(HeadGrads a) {
   else write_out<bf16_t>(o, a, split, row0, col0, acc);
 }
 
-// The sum of a contraction's parts, four columns a thread.
+// The sums of contractions' parts, four columns a thread: one result's, then the other's.
 template <class T>
-__global__ __launch_bounds__(256) void head_sum_kernel(HeadOut o, HeadGrads a) {
-  const int64_t per = (o.g.n + 3) / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / per, n = i % per * 4;
+__device__ __forceinline__ void sum4(const HeadOut& o, const HeadGrads& a, int64_t i) {
+  const int64_t per = (o.g.n + 3) / 4, m = i / per, n = i % per * 4;
   if (m >= o.g.m) return;
   const float* p = o.partial + m * o.g.n;
   op_f32x4 v = row_load4(p, n, o.g.n);
@@ -530,6 +575,13 @@ __global__ __launch_bounds__(256) void head_sum_kernel(HeadOut o, HeadGrads a) {
   }
   write4<T>(o, a, scale_of(a), row_without(o, a, m), m, n, v);
 }
+__global__ __launch_bounds__(256) void head_sum_kernel(HeadGrads a, int first_blocks) {
+  const bool second = (int)blockIdx.x >= first_blocks;
+  const HeadOut& o = a.part[second ? 1 : 0];
+  const int64_t i = (int64_t)(blockIdx.x - (second ? first_blocks : 0)) * 256 + threadIdx.x;
+  if (o.f32) sum4<float>(o, a, i);
+  else sum4<bf16_t>(o, a, i);
+}
 
 // The kernels use more dynamic LDS than the default limit: raised once for each device.
 hipError_t head_setup() {
@@ -539,7 +591,8 @@ hipError_t head_setup() {
   if (e != hipSuccess) return e;
   const uint64_t bit = uint64_t(1) << (dev & 63);
   if (dev <= 63 && raised.load(std::memory_order_relaxed) & bit) return hipSuccess;
-  for (const void* f : {reinterpret_cast<const void*>(&head_first_kernel), reinterpret_cast<const void*>(&head_second_kernel),
+  for (const void* f : {reinterpret_cast<const void*>(&head_first_kernel<false>), reinterpret_cast<const void*>(&head_first_kernel<true>),
+                        reinterpret_cast<const void*>(&head_second_kernel<false>), reinterpret_cast<const void*>(&head_second_kernel<true>),
                         reinterpret_cast<const void*>(&head_grads_kernel)}) {
     e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
     if (e != hipSuccess) return e;
@@ -551,8 +604,10 @@ hipError_t head_setup() {
 hipError_t launch_head_logits(const HeadLogits& a, bool second, hipStream_t s) {
   const int blocks = tile_blocks(a.g.tiles_m, a.g.tiles_n, 1);
   const dim3 grid((unsigned)(blocks < CUS ? blocks : CUS));
-  if (second) hipLaunchKernelGGL(head_second_kernel, grid, dim3(NT), LDS_BYTES, s, a);
-  else hipLaunchKernelGGL(head_first_kernel, grid, dim3(NT), LDS_BYTES, s, a);
+  if (second && a.x_scales) hipLaunchKernelGGL(head_second_kernel<true>, grid, dim3(NT), LDS_BYTES, s, a);
+  else if (second) hipLaunchKernelGGL(head_second_kernel<false>, grid, dim3(NT), LDS_BYTES, s, a);
+  else if (a.x_scales) hipLaunchKernelGGL(head_first_kernel<true>, grid, dim3(NT), LDS_BYTES, s, a);
+  else hipLaunchKernelGGL(head_first_kernel<false>, grid, dim3(NT), LDS_BYTES, s, a);
   return hipGetLastError();
 }
 
@@ -563,10 +618,11 @@ hipError_t launch_head_grads(const HeadGrads& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_head_sum(const HeadOut& o, const HeadGrads& a, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)o.g.m * ((o.g.n + 3) / 4) + 255) / 256));
-  if (o.f32) hipLaunchKernelGGL(head_sum_kernel<float>, grid, dim3(256), 0, s, o, a);
-  else hipLaunchKernelGGL(head_sum_kernel<bf16_t>, grid, dim3(256), 0, s, o, a);
+hipError_t launch_head_sum(const HeadGrads& a, bool first, bool second, hipStream_t s) {
+  auto blocks = [&](int i) { return (int)(((int64_t)a.part[i].g.m * ((a.part[i].g.n + 3) / 4) + 255) / 256); };
+  const int n = first ? blocks(0) : 0, all = n + (second ? blocks(1) : 0);
+  if (all == 0) return hipSuccess;
+  hipLaunchKernelGGL(head_sum_kernel, dim3((unsigned)all), dim3(256), 0, s, a, n);
   return hipGetLastError();
 }
 

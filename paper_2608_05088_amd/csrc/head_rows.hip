@@ -62,8 +62,8 @@ __device__ __forceinline__ int64_t packed_at(int64_t r, int64_t c, int64_t cols)
 
 // Four columns a thread.
 template <class T>
-__global__ __launch_bounds__(256) void head_pack_kernel(HeadPack a) {
-  const int64_t per = a.out_cols / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__device__ __forceinline__ void pack_rows(const HeadPack& a, int block) {
+  const int64_t per = a.out_cols / 4, i = (int64_t)block * 256 + threadIdx.x;
   if (i >= a.out_rows * per) return;
   const int64_t r = i / per, c = i % per * 4;
   op_f32x4 v = {0.f, 0.f, 0.f, 0.f};
@@ -71,11 +71,63 @@ __global__ __launch_bounds__(256) void head_pack_kernel(HeadPack a) {
   store_planes(a.out + packed_at(r, c, a.out_cols), a.plane, a.planes, a.finite, v);
 }
 
+// A wave a row: its largest magnitude, then its values times the power of two that brings it to
+// [2^14, 2^15), as float16 numbers: 11 bits, and 11 of what they leave, to 2^-39 of the largest.  A row with an
+// infinity keeps its infinities alone, as 1 under a scale past every logit.
+template <class T>
+__device__ __forceinline__ void pack_halves(const HeadPack& a, float* scales, int block) {
+  const int64_t r = (int64_t)block * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (r >= a.out_rows) return;
+  const bool there = r < a.rows && stays(a.labels, r, a.vocab);
+  const T* const row = static_cast<const T*>(a.x) + (there ? r : 0) * a.ld;
+  uint32_t top = 0;
+  if (there)
+    for (int64_t c = 4 * lane; c < a.cols; c += 256) {
+      const op_f32x4 v = row_load4(row, c, a.cols);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
+        top = top > b ? top : b;
+      }
+    }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)top, d, 64);
+    top = top > o ? top : o;
+  }
+  const bool far = top >= 0x7f800000u;
+  int e = (int)(top >> 23) - 127 - 14;   // the scale's exponent
+  e = top == 0 ? 0 : e < -126 ? -126 : e;
+  const float scale = far ? 0x1p120f : __uint_as_float((uint32_t)(e + 127) << 23), inverse = __uint_as_float((uint32_t)(127 - e) << 23);
+  if (lane == 0) gptr(scales)[r] = scale;
+  for (int64_t c = 4 * lane; c < a.out_cols; c += 256) {
+    op_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (there) v = row_load4(row, c, a.cols);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (!far) v[j] *= inverse;
+      else if (v[j] == v[j]) v[j] = fabsf(v[j]) == __builtin_inff() ? copysignf(1.f, v[j]) : 0.f;
+    }
+    uint16_t* out = a.out + packed_at(r, c, a.out_cols);
+    for (int p = 0; p < a.planes; ++p) {
+      _Float16 h[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        h[j] = (_Float16)v[j];
+        v[j] -= (float)h[j];
+      }
+      typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+      *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(out) + p * a.plane) = __builtin_bit_cast(op_u32x2, half4{h[0], h[1], h[2], h[3]});
+    }
+  }
+}
+
 // The transpose of a 64 x 64 tile through LDS; rows past the end are zeros.
 template <class T>
-__global__ __launch_bounds__(256) void head_pack_t_kernel(HeadPack a, int tiles_r) {
-  __shared__ float tile[64][65];
-  const int64_t r0 = (int64_t)(blockIdx.x % tiles_r) * 64, c0 = (int64_t)(blockIdx.x / tiles_r) * 64;
+__device__ __forceinline__ void pack_turned(const HeadPack& a, float (&tile)[64][65], int block) {
+  const int tiles_r = (int)(a.out_cols / 64);
+  const int64_t r0 = (int64_t)(block % tiles_r) * 64, c0 = (int64_t)(block / tiles_r) * 64;
   const int lo = threadIdx.x & 15, hi = threadIdx.x >> 4;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -95,25 +147,43 @@ __global__ __launch_bounds__(256) void head_pack_t_kernel(HeadPack a, int tiles_
   }
 }
 
+template <class X, class W>
+__global__ __launch_bounds__(256) void head_prepare_kernel(HeadPrepare a) {
+  __shared__ float tile[64][65];
+  int block = blockIdx.x, part = 0;
+  while (block >= a.blocks[part]) block -= a.blocks[part++];   // the grid is their sum
+  if (part == 0) {
+    if (a.halves) pack_halves<X>(a.part[0], a.scales[0], block);
+    else pack_rows<X>(a.part[0], block);
+  } else if (part == 1) {
+    pack_turned<X>(a.part[1], tile, block);
+  } else if (part == 2) {
+    if (a.halves) pack_halves<W>(a.part[2], a.scales[1], block);
+    else pack_rows<W>(a.part[2], block);
+  } else {
+    pack_turned<W>(a.part[3], tile, block);
+  }
+}
+
 // What the second pass asks about a row.
+__device__ __forceinline__ void write_record(const HeadLabels& l, int64_t r, bool there, int64_t y, f32x4 v, HeadRow* records) {
+  if (there && l.weights) {
+    const float w = gptr(l.weights)[r * l.weight_stride];
+    v.y *= w;
+    v.z *= w;
+    if (w == 0.f) y = -1;
+  }
+  v.w = __int_as_float(there ? (int)y : -1);
+  *reinterpret_cast<MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<float*>(records + r))) = v;
+}
 __global__ __launch_bounds__(256) void head_records_kernel(HeadLabels l, int64_t rows, int64_t rows_pad, int64_t vocab,
                                                            const HeadRow* stats, HeadRow* records) {
   const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (r >= rows_pad) return;
+  const bool there = r < rows;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  int64_t y = -1;
-  if (r < rows) {
-    y = label_of(l, r, vocab);
-    v = *reinterpret_cast<const MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<const float*>(stats + r)));
-    if (l.weights) {
-      const float w = gptr(l.weights)[r * l.weight_stride];
-      v.y *= w;
-      v.z *= w;
-      if (w == 0.f) y = -1;
-    }
-  }
-  v.w = __int_as_float((int)y);
-  *reinterpret_cast<MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<float*>(records + r))) = v;
+  if (there) v = *reinterpret_cast<const MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<const float*>(stats + r)));
+  write_record(l, r, there, there ? label_of(l, r, vocab) : -1, v, records);
 }
 
 // --------------------------------------------------------------------- few rows
@@ -235,11 +305,16 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void head_few_kernel(HeadFew a) {
 // ------------------------------------------------------------------------- join
 // A row's parts, one workgroup of T threads a row.
 template <int T>
-__global__ __launch_bounds__(T) void head_join_kernel(HeadLabels rows, int64_t vocab, const malt_f32x2* partial, int parts,
-                                                      const float* at_label, HeadRow* stats, float* losses) {
+__global__ __launch_bounds__(T) void head_join_kernel(HeadJoin a) {
   __shared__ float red[2][T / 64];
   const int64_t r = blockIdx.x;
-  const malt_f32x2* const p = partial + r * parts;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  if (r >= a.m) {
+    if (threadIdx.x == 0) write_record(a.rows, r, false, -1, zero, a.records);
+    return;
+  }
+  const int parts = a.parts;
+  const malt_f32x2* const p = a.partial + r * parts;
   float top = -__builtin_inff(), sum = 0.f;
   for (int i = threadIdx.x; i < parts; i += T) {
     const malt_f32x2 v = gptr(p)[i];
@@ -269,18 +344,17 @@ __global__ __launch_bounds__(T) void head_join_kernel(HeadLabels rows, int64_t v
     for (int i = 1; i < T / 64; ++i) sum += red[1][i];
   }
   if (threadIdx.x != 0) return;
-  if (label_of(rows, r, vocab) < 0) {
-    if (losses) gptr(losses)[r] = 0.f;
-    if (stats) {
-      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-      *reinterpret_cast<MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<float*>(stats + r))) = zero;
-    }
+  const int64_t label = label_of(a.rows, r, a.vocab);
+  if (label < 0) {
+    if (a.losses) gptr(a.losses)[r] = 0.f;
+    if (a.stats) *reinterpret_cast<MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<float*>(a.stats + r))) = zero;
+    if (a.records) write_record(a.rows, r, true, -1, zero, a.records);
     return;
   }
-  float y = gptr(at_label)[r];   // log2
+  float y = gptr(a.at_label)[r];   // log2
   if (y <= -FAR) y = -__builtin_inff();
   if (y >= FAR || all >= FAR) sum = __builtin_nanf("");
-  if (losses) {
+  if (a.losses) {
     // log(1 + o / e^y) where the label leads, log(o) - y + log(1 + e^y / o) where it does not; log1p keeps
     // what a sum of nearly 1 would lose.
     const float d = y - ref;   // log2 of e^y over the others' largest
@@ -289,13 +363,14 @@ __global__ __launch_bounds__(T) void head_join_kernel(HeadLabels rows, int64_t v
     else loss = (log2f(sum) - d) * LN2 + log1pf(exp2f(d) / sum);
     if (sum == 0.f && y > -__builtin_inff()) loss = 0.f;   // no other column has mass
     if (sum != sum) loss = sum;
-    gptr(losses)[r] = loss;
+    gptr(a.losses)[r] = loss;
   }
-  if (stats) {
+  if (a.stats || a.records) {
     // The reference is the larger of both: no power of two above 1 is formed.
     const float t = fmaxf(ref, y), o = sum * exp2f(ref - t), total = o + exp2f(y - t);
     const f32x4 v = {t, 1.f / total, o / total, 0.f};
-    *reinterpret_cast<MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<float*>(stats + r))) = v;
+    if (a.stats) *reinterpret_cast<MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<float*>(a.stats + r))) = v;
+    if (a.records) write_record(a.rows, r, true, label, v, a.records);
   }
 }
 
@@ -318,27 +393,31 @@ hipError_t launch_head_few(const HeadFew& a, bool x_f32, bool w_f32, hipStream_t
   return hipGetLastError();
 }
 
-hipError_t launch_head_join(const HeadLabels& rows, int64_t m, int64_t vocab, const malt_f32x2* partial, int parts,
-                            const float* at_label, HeadRow* stats, float* losses, hipStream_t s) {
+hipError_t launch_head_join(const HeadJoin& a, hipStream_t s) {
   // A wave a row where there are enough rows to fill the card.
-  const dim3 grid((unsigned)m);
-  if (m <= HEAD_FEW) hipLaunchKernelGGL((head_join_kernel<256>), grid, dim3(256), 0, s, rows, vocab, partial, parts, at_label, stats, losses);
-  else hipLaunchKernelGGL((head_join_kernel<64>), grid, dim3(64), 0, s, rows, vocab, partial, parts, at_label, stats, losses);
+  const dim3 grid((unsigned)(a.records ? a.rows_pad : a.m));
+  if (a.m <= HEAD_FEW) hipLaunchKernelGGL((head_join_kernel<256>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((head_join_kernel<64>), grid, dim3(64), 0, s, a);
   return hipGetLastError();
 }
 
-hipError_t launch_head_pack(const HeadPack& a, bool f32, hipStream_t s) {
-  const dim3 grid((unsigned)((a.out_rows * (a.out_cols / 4) + 255) / 256));
-  if (f32) hipLaunchKernelGGL((head_pack_kernel<float>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((head_pack_kernel<bf16_t>), grid, dim3(256), 0, s, a);
-  return hipGetLastError();
-}
-
-hipError_t launch_head_pack_t(const HeadPack& a, bool f32, hipStream_t s) {
-  const int tiles_r = (int)(a.out_cols / 64);
-  const dim3 grid((unsigned)(tiles_r * ((a.out_rows + 63) / 64)));
-  if (f32) hipLaunchKernelGGL((head_pack_t_kernel<float>), grid, dim3(256), 0, s, a, tiles_r);
-  else hipLaunchKernelGGL((head_pack_t_kernel<bf16_t>), grid, dim3(256), 0, s, a, tiles_r);
+hipError_t launch_head_prepare(HeadPrepare a, bool x_f32, bool w_f32, hipStream_t s) {
+  int64_t all = 0;
+  for (int i = 0; i < 4; ++i) {
+    const HeadPack& p = a.part[i];
+    int64_t n = 0;
+    if (p.out && i % 2) n = p.out_cols / 64 * ((p.out_rows + 63) / 64);
+    else if (p.out && a.halves) n = (p.out_rows + 3) / 4;
+    else if (p.out) n = (p.out_rows * (p.out_cols / 4) + 255) / 256;
+    a.blocks[i] = (int32_t)n;
+    all += n;
+  }
+  if (all == 0) return hipSuccess;
+  const dim3 grid((unsigned)all);
+  if (x_f32 && w_f32) hipLaunchKernelGGL((head_prepare_kernel<float, float>), grid, dim3(256), 0, s, a);
+  else if (x_f32) hipLaunchKernelGGL((head_prepare_kernel<float, bf16_t>), grid, dim3(256), 0, s, a);
+  else if (w_f32) hipLaunchKernelGGL((head_prepare_kernel<bf16_t, float>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((head_prepare_kernel<bf16_t, bf16_t>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

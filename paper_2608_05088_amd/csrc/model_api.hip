@@ -87,22 +87,23 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct HeadPlan {
   bool few;              // the first pass in one launch on the weights as they lie
   bool grads;
-  int x_planes, w_planes;
+  bool halves;           // logits from float16 planes
+  int x_halves, w_halves;
   bool pack_w;           // otherwise the products read the weights as they lie
-  int dz_planes;
+  int dz_planes, dx_z, dx_w, dw_z, dw_x;   // bf16 planes of the gradients' products
   int64_t rows_pad, cols_pad, vocab_pad;
   int64_t piece;         // vocabulary columns of a piece, a multiple of the tile
   int pieces;
   int parts;             // of a row's statistics
   int dx_splits, dw_splits;   // parts of the gradients' contractions
-  size_t partial, at_label, stats, records, x, w, x_t, w_t, dz, dz_t, dx, dw, bytes;
+  size_t partial, at_label, records, x, w, x_scales, w_scales, x_t, w_t, dz, dz_t, dx, dw, bytes;
 };
 
-// Pairs of planes that make a product of `na` by `nb` planes, small ones first.
-void head_pairs(HeadProduct& g, int na, int nb) {
+// Pairs of planes that make a product of `na` by `nb` planes (of two or three at most), small ones first.
+void head_pairs(HeadProduct& g, int na, int nb, int planes) {
   g.pairs = 0;
   g.pair_a = g.pair_b = 0;
-  for (int s = HEAD_PLANES - 1; s >= 0; --s)
+  for (int s = planes - 1; s >= 0; --s)
     for (int i = s < na ? s : na - 1; i >= 0; --i) {
       const int j = s - i;
       if (j >= nb) break;
@@ -111,9 +112,9 @@ void head_pairs(HeadProduct& g, int na, int nb) {
       ++g.pairs;
     }
 }
-int head_pair_count(int na, int nb) {
+int head_pair_count(int na, int nb, int planes) {
   HeadProduct g;
-  head_pairs(g, na, nb);
+  head_pairs(g, na, nb, planes);
   return g.pairs;
 }
 
@@ -122,14 +123,23 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
   const bool x32 = a.x_type == MALT_FLOAT32, w32 = a.weight_type == MALT_FLOAT32;
   L.few = a.rows <= HEAD_FEW;
   L.grads = a.dx || a.dweight;
-  L.x_planes = x32 ? HEAD_PLANES : 1;
-  L.w_planes = w32 ? HEAD_PLANES : 1;
-  const bool fine = (a.dx && x32) || (a.dweight && a.dweight_type == MALT_FLOAT32);
-  L.dz_planes = fine ? HEAD_PLANES : 1;
+  L.halves = x32 || w32;
+  L.x_halves = x32 ? HEAD_HALVES : 1;
+  L.w_halves = w32 ? HEAD_HALVES : 1;
+  // Planes of dz and of the other side, by the result's type.  bf16: one of dz, whose rounding is of the result's
+  // own size (together 1.41 times it); two below 2^32 products, where that costs under 10 us.  The other side's
+  // float32 values: two, since a third rounding would make that 1.73.
+  const bool dw32 = a.dweight_type == MALT_FLOAT32;
+  const int coarse = double(a.rows) * double(a.vocab) * double(a.inner) < 0x1p32 ? 2 : 1;
+  L.dx_z = x32 ? HEAD_PLANES : coarse;
+  L.dx_w = w32 ? (x32 ? HEAD_PLANES : 2) : 1;
+  L.dw_z = dw32 ? HEAD_PLANES : coarse;
+  L.dw_x = x32 ? (dw32 ? HEAD_PLANES : 2) : 1;
+  L.dz_planes = std::max(a.dx ? L.dx_z : 1, a.dweight ? L.dw_z : 1);
   L.rows_pad = up(a.rows, HEAD_TILE);
   L.cols_pad = up(a.inner, HEAD_BK);
-  // As they lie: rows of whole stages, 16-byte pieces, a tile's offsets in 32 bits, infinities that meet no empty plane.
-  L.pack_w = w32 || x32 || a.inner % HEAD_BK || a.ldw % 8 || a.ldw > (int64_t(1) << 22) || !op_aligned(a.weight, 16);
+  // As they lie: rows of whole stages, 16-byte pieces, a tile's offsets in 32 bits.
+  L.pack_w = L.halves || a.inner % HEAD_BK || a.ldw % 8 || a.ldw > (int64_t(1) << 22) || !op_aligned(a.weight, 16);
   size_t end = 0;
   auto take = [&](size_t bytes) {
     const size_t at = end;
@@ -141,10 +151,13 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     L.partial = take(size_t(a.rows) * L.parts * 8);
     L.at_label = take(size_t(a.rows) * 4);
   }
-  if (!a.stats) L.stats = take(size_t(a.rows) * sizeof(HeadRow));
   if (L.grads || !L.few) {
-    L.x = take(size_t(L.x_planes) * L.rows_pad * L.cols_pad * 2);
-    if (L.pack_w) L.w = take(size_t(L.w_planes) * up(a.vocab, HEAD_TILE) * L.cols_pad * 2);
+    L.x = take(size_t(L.x_halves) * L.rows_pad * L.cols_pad * 2);
+    if (L.pack_w) L.w = take(size_t(L.w_halves) * up(a.vocab, HEAD_TILE) * L.cols_pad * 2);
+    if (L.halves) {
+      L.x_scales = take(size_t(L.rows_pad) * 4);
+      L.w_scales = take(size_t(up(a.vocab, HEAD_TILE)) * 4);
+    }
   }
   if (L.grads) {
     // Pieces of like size, as few as keep dz within its share of memory.
@@ -157,20 +170,20 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     L.records = take(size_t(L.rows_pad) * sizeof(HeadRow));
     L.vocab_pad = L.piece * L.pieces;
     if (a.dx) {
-      L.w_t = take(size_t(x32 ? L.w_planes : 1) * up(a.inner, HEAD_TILE) * L.vocab_pad * 2);
+      L.w_t = take(size_t(L.dx_w) * up(a.inner, HEAD_TILE) * L.vocab_pad * 2);
       L.dz = take(size_t(L.dz_planes) * L.rows_pad * L.piece * 2);
     }
     if (a.dweight) {
-      L.x_t = take(size_t(a.dweight_type == MALT_FLOAT32 ? L.x_planes : 1) * up(a.inner, HEAD_TILE) * L.rows_pad * 2);
+      L.x_t = take(size_t(L.dw_x) * up(a.inner, HEAD_TILE) * L.rows_pad * 2);
       L.dz_t = take(size_t(L.dz_planes) * L.rows_pad * L.piece * 2);
     }
     // A product of few tiles and a long contraction is cut into parts, so that no workgroup has more
     // stages than a CU's share of them all, and 16 at the least (a part costs its tile in float32, written and read).
     const int64_t across = up(a.inner, HEAD_TILE) / HEAD_TILE;
     const int64_t dx_tiles = a.dx ? L.rows_pad / HEAD_TILE * across : 0, dw_tiles = a.dweight ? L.piece / HEAD_TILE * across : 0;
-    const int64_t dx_stages = L.piece / HEAD_BK * head_pair_count(x32 ? L.dz_planes : 1, x32 ? L.w_planes : 1);
+    const int64_t dx_stages = L.piece / HEAD_BK * head_pair_count(L.dx_z, L.dx_w, x32 ? HEAD_PLANES : 2);
     const int64_t dw_stages = up(a.rows, HEAD_BK) / HEAD_BK *
-                              head_pair_count(a.dweight_type == MALT_FLOAT32 ? L.dz_planes : 1, a.dweight_type == MALT_FLOAT32 ? L.x_planes : 1);
+                              head_pair_count(L.dw_z, L.dw_x, dw32 ? HEAD_PLANES : 2);
     int64_t share = (dx_tiles * dx_stages + dw_tiles * dw_stages) / 256;
     if (share < 16) share = 16;
     auto parts = [&](int64_t stages, int64_t contraction) {
@@ -472,54 +485,76 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
   if (a.rows == 0 && (!a.dweight || a.accumulate)) return MALT_OK;
   const hipStream_t s = static_cast<hipStream_t>(stream_);
   char* const ws = static_cast<char*>(workspace);
-  uint16_t *const xp = reinterpret_cast<uint16_t*>(ws + L.x), *const wp = reinterpret_cast<uint16_t*>(ws + L.w);
   const bool per_row = a.weights && a.weight_stride > 0;   // one for all rows is a factor of the result
   const HeadLabels labels = {a.labels, a.label_type == MALT_INT64, a.label_stride, per_row ? a.weights : nullptr, a.weight_stride};
-  HeadRow* const stats = a.stats ? reinterpret_cast<HeadRow*>(a.stats) : reinterpret_cast<HeadRow*>(ws + L.stats);
   const bool f32x = a.x_type == MALT_FLOAT32, f32w = a.weight_type == MALT_FLOAT32;
   if (L.grads || !L.few) MALT_TRY(launched(head_setup(), "raising the head's LDS limit"));
 
-  HeadPack px = {};
-  px.x = a.x;
-  px.rows = a.rows;
-  px.cols = a.inner;
-  px.ld = a.ldx;
-  px.out = xp;
-  px.plane = L.rows_pad * L.cols_pad;
-  px.out_rows = L.rows_pad;
-  px.out_cols = L.cols_pad;
-  px.planes = L.x_planes;
-  px.finite = f32x || f32w;
-  px.labels = labels;
-  px.labels.weights = nullptr;   // the losses of rows without weight are formed all the same
-  px.vocab = a.vocab;
-  HeadSide wside = {static_cast<const uint16_t*>(a.weight), 0, HEAD_TILE * a.ldw, HEAD_BK, (int32_t)a.ldw, a.vocab};
+  // What is packed: the logits' sides, and for the gradients the transposes.
+  const bool want_dx = a.dx && a.rows > 0, want_dw = a.dweight && a.rows > 0;
+  HeadPrepare prepare = {};
+  prepare.halves = L.halves;
+  prepare.scales[0] = reinterpret_cast<float*>(ws + L.x_scales);
+  prepare.scales[1] = reinterpret_cast<float*>(ws + L.w_scales);
+  HeadSide wside = {static_cast<const uint16_t*>(a.weight), 0, HEAD_TILE * a.ldw, HEAD_BK, (int32_t)a.ldw, a.vocab}, w_t = {}, x_t = {};
   if (a.rows > 0 && (L.grads || !L.few)) {
-    MALT_TRY(launched(launch_head_pack(px, f32x, s), "packing the head's input"));
-    if (L.pack_w) {
-      HeadPack pw = {};
-      pw.x = a.weight;
-      pw.rows = a.vocab;
-      pw.cols = a.inner;
-      pw.ld = a.ldw;
-      pw.out = wp;
-      pw.out_rows = up(a.vocab, HEAD_TILE);
-      pw.out_cols = L.cols_pad;
-      pw.plane = pw.out_rows * pw.out_cols;
-      pw.planes = L.w_planes;
-      pw.finite = f32x || f32w;
-      MALT_TRY(launched(launch_head_pack(pw, f32w, s), "packing the head's weight"));
-      wside = packed_side(wp, pw.out_rows, pw.out_cols);
+    HeadPack x = {}, w = {};
+    x.x = a.x;
+    x.rows = a.rows;
+    x.cols = w.cols = a.inner;
+    x.ld = a.ldx;
+    x.labels = labels;
+    x.finite = w.finite = L.halves;
+    x.vocab = a.vocab;
+    w.x = a.weight;
+    w.rows = a.vocab;
+    w.ld = a.ldw;
+    auto straight = [&](HeadPack p, size_t at, int64_t rows, int planes) {
+      p.out = reinterpret_cast<uint16_t*>(ws + at);
+      p.out_rows = rows;
+      p.out_cols = L.cols_pad;
+      p.plane = rows * L.cols_pad;
+      p.planes = planes;
+      return p;
+    };
+    auto turned = [&](HeadPack p, size_t at, int64_t cols, int planes) {
+      p.out = reinterpret_cast<uint16_t*>(ws + at);
+      p.out_rows = a.inner;
+      p.out_cols = cols;
+      p.plane = up(a.inner, HEAD_TILE) * cols;
+      p.planes = planes;
+      return p;
+    };
+    prepare.part[0] = straight(x, L.x, L.rows_pad, L.x_halves);
+    prepare.part[0].labels.weights = nullptr;   // the losses of rows without weight are formed all the same
+    if (want_dw) {
+      prepare.part[1] = turned(x, L.x_t, L.rows_pad, L.dw_x);
+      x_t = packed_side(prepare.part[1].out, up(a.inner, HEAD_TILE), L.rows_pad);
+      x_t.rows = a.inner;
     }
+    if (L.pack_w) {
+      prepare.part[2] = straight(w, L.w, up(a.vocab, HEAD_TILE), L.w_halves);
+      wside = packed_side(prepare.part[2].out, up(a.vocab, HEAD_TILE), L.cols_pad);
+    }
+    if (want_dx) {
+      prepare.part[3] = turned(w, L.w_t, L.vocab_pad, L.dx_w);
+      w_t = packed_side(prepare.part[3].out, up(a.inner, HEAD_TILE), L.vocab_pad);
+      w_t.rows = a.inner;
+    }
+    MALT_TRY(launched(launch_head_prepare(prepare, f32x, f32w, s), "packing the head's operands"));
   }
 
   HeadLogits z = {};
-  z.g.a = packed_side(xp, L.rows_pad, L.cols_pad);
+  z.g.a = packed_side(reinterpret_cast<const uint16_t*>(ws + L.x), L.rows_pad, L.cols_pad);
   z.g.b = wside;
   z.g.m = (int32_t)a.rows;
   z.g.k = L.cols_pad;
   z.g.tiles_m = int(L.rows_pad / HEAD_TILE);
-  head_pairs(z.g, L.x_planes, L.w_planes);
+  head_pairs(z.g, L.x_halves, L.w_halves, HEAD_HALVES);
+  if (L.halves) {
+    z.x_scales = prepare.scales[0];
+    z.w_scales = prepare.scales[1];
+  }
   z.rows = labels;
   z.vocab = a.vocab;
   HeadRow* const records = reinterpret_cast<HeadRow*>(ws + L.records);
@@ -550,47 +585,20 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       first.parts = L.parts;
       MALT_TRY(launched(launch_head_logits(first, false, s), "launching the head's logits"));
     }
-    MALT_TRY(launched(launch_head_join(labels, a.rows, a.vocab, partial, L.parts, at_label, stats, a.losses, s), "joining the head's statistics"));
+    const HeadJoin join = {labels, a.rows, L.rows_pad, a.vocab, partial, L.parts, at_label, reinterpret_cast<HeadRow*>(a.stats),
+                           L.grads ? records : nullptr, a.losses};
+    MALT_TRY(launched(launch_head_join(join, s), "joining the head's statistics"));
   }
   if (!L.grads) return MALT_OK;
-  if (a.rows > 0) MALT_TRY(launched(launch_head_records(labels, a.rows, L.rows_pad, a.vocab, stats, records, s), "preparing the head's rows"));
+  if (a.rows > 0 && a.stats_given)
+    MALT_TRY(launched(launch_head_records(labels, a.rows, L.rows_pad, a.vocab, reinterpret_cast<const HeadRow*>(a.stats), records, s),
+                      "preparing the head's rows"));
 
   HeadGrads gr = {};
   gr.records = records;
   gr.scale = a.weights ? 1.f : a.weight_value;
   gr.scale_at = per_row ? nullptr : a.weights;
   uint16_t *const dz = reinterpret_cast<uint16_t*>(ws + L.dz), *const dz_t = reinterpret_cast<uint16_t*>(ws + L.dz_t);
-  const bool want_dx = a.dx && a.rows > 0;
-  HeadSide w_t = {}, x_t = {};
-  const int dx_w = f32x ? L.w_planes : 1, dw_x = a.dweight_type == MALT_FLOAT32 ? L.x_planes : 1;
-  if (want_dx) {
-    HeadPack p = {};
-    p.x = a.weight;
-    p.rows = a.vocab;
-    p.cols = a.inner;
-    p.ld = a.ldw;
-    p.out = reinterpret_cast<uint16_t*>(ws + L.w_t);
-    p.out_rows = a.inner;
-    p.out_cols = L.vocab_pad;
-    p.plane = up(a.inner, HEAD_TILE) * L.vocab_pad;
-    p.planes = dx_w;
-    p.finite = f32x || f32w;
-    MALT_TRY(launched(launch_head_pack_t(p, f32w, s), "transposing the head's weight"));
-    w_t = packed_side(p.out, up(a.inner, HEAD_TILE), L.vocab_pad);
-    w_t.rows = a.inner;
-  }
-  if (a.dweight && a.rows > 0) {
-    HeadPack p = px;
-    p.labels = labels;
-    p.out = reinterpret_cast<uint16_t*>(ws + L.x_t);
-    p.out_rows = a.inner;
-    p.out_cols = L.rows_pad;
-    p.plane = up(a.inner, HEAD_TILE) * L.rows_pad;
-    p.planes = dw_x;
-    MALT_TRY(launched(launch_head_pack_t(p, f32x, s), "transposing the head's input"));
-    x_t = packed_side(p.out, up(a.inner, HEAD_TILE), L.rows_pad);
-    x_t.rows = a.inner;
-  }
   for (int p = 0; p < L.pieces; ++p) {
     const int64_t v0 = p * L.piece, n = a.vocab - v0 < L.piece ? a.vocab - v0 : L.piece;
     if (a.rows > 0) {
@@ -600,6 +608,7 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       second.g.n = (int32_t)n;
       second.g.tiles_n = int(up(n, HEAD_TILE) / HEAD_TILE);
       second.col0 = v0;
+      if (L.halves) second.w_scales += v0;
       second.dz = a.dx ? dz : nullptr;
       second.dz_t = a.dweight ? dz_t : nullptr;
       second.dz_plane = L.rows_pad * L.piece;
@@ -620,7 +629,7 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       o.g.k = n;
       o.g.tiles_m = int(L.rows_pad / HEAD_TILE);
       o.g.tiles_n = int(up(a.inner, HEAD_TILE) / HEAD_TILE);
-      head_pairs(o.g, f32x ? L.dz_planes : 1, dx_w);
+      head_pairs(o.g, L.dx_z, L.dx_w, f32x ? HEAD_PLANES : 2);
       o.out = a.dx;
       o.ldo = a.lddx;
       o.partial = reinterpret_cast<float*>(ws + L.dx);
@@ -641,7 +650,7 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       o.g.k = a.rows;
       o.g.tiles_m = int(up(n, HEAD_TILE) / HEAD_TILE);
       o.g.tiles_n = int(up(a.inner, HEAD_TILE) / HEAD_TILE);
-      head_pairs(o.g, fine ? L.dz_planes : 1, dw_x);
+      head_pairs(o.g, L.dw_z, L.dw_x, fine ? HEAD_PLANES : 2);
       o.out = static_cast<char*>(a.dweight) + v0 * a.lddw * op_dtype_bytes(a.dweight_type);
       o.ldo = a.lddw;
       o.partial = reinterpret_cast<float*>(ws + L.dw);
@@ -651,10 +660,9 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       o.accumulate = a.accumulate != 0;
     }
     MALT_TRY(launched(launch_head_grads(gr, s), "launching the head's gradients"));
-    for (int i = 0; i < gr.parts; ++i) {
-      const HeadOut& o = gr.part[i];
-      if (o.splits > 1 && (!o.mask_rows || p + 1 == L.pieces)) MALT_TRY(launched(launch_head_sum(o, gr, s), "joining the head's gradients"));
-    }
+    bool sums[2] = {false, false};
+    for (int i = 0; i < gr.parts; ++i) sums[i] = gr.part[i].splits > 1 && (!gr.part[i].mask_rows || p + 1 == L.pieces);
+    MALT_TRY(launched(launch_head_sum(gr, sums[0], sums[1], s), "joining the head's gradients"));
   }
   return MALT_OK;
 }

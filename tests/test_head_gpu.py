@@ -3,9 +3,10 @@ implementations in 64 bits: odd sizes, rows without label or weight, logits that
 numbers, strides, types, pieces of the vocabulary and of the contraction, streams and graphs.
 
 Tolerances follow from the arithmetic.  u = 2^-24 is float32's unit roundoff, r = finfo.eps / 2 a
-type's half step (bf16 2^-8).  With S = sum |x||w| a logit is off by (6 K + 8) u S: at most 6 K
-products are added up, each exact, and the three that are left out of a float32 product are below
-2^-24 of it each.  A row's sum of exponentials has at most 100 additions in a row and
+type's half step (bf16 2^-8).  With S = sum |x||w| a logit is off by (6 K + 8) u S: K products of
+bf16 are exact and added up; of float32 3 K are, and each product has lost 12 u (its factors' 22
+bits 4 u each, the smallest part of it 4 u), which is at most 3 K - 1 + 12 <= 6 K + 8.  The gradients'
+products add up 6 n, and lose three parts below 2^-24.  A row's sum of exponentials has at most 100 additions in a row and
 exponents rounded at |z| log2 e, so it is relatively off by d = 2 dz + 128 u + 4 u max|z| (and the
 hardware's 2 u an exponential).  Losses are off by d (1 - q_y) and their own rounding,
 d log p = d, and so on through the products.  A probability below 2^-126, float32's smallest normal

@@ -506,30 +506,45 @@ __device__ __forceinline__ bool row_without(const HeadOut& o, const HeadGrads& a
 }
 __device__ __forceinline__ float scale_of(const HeadGrads& a) { return a.scale_at ? a.scale * gptr(a.scale_at)[0] : a.scale; }
 
+// A wave's sub-tile leaves through its own part of LDS, half of its columns at a time, so that a
+// store covers eight rows' 128 bytes, and in a loop: straight from the registers it is 30 KB of code,
+// run once a tile.
+constexpr int GRAD_PITCH = TN / 2 * 4 + 16, GRAD_WAVE = TM * GRAD_PITCH;
+static_assert(NW * GRAD_WAVE <= LDS_BYTES, "LDS budget");
 template <class T>
-__device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, int split, int64_t row0, int64_t col0,
+__device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, int split, int64_t row0, int64_t col0, char* lds,
                                           const f32x4 (&acc)[NA][NB]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave / (NW / 2), wc = wave % (NW / 2);
   const float scale = scale_of(a);
   float* const partial = o.partial + split * ((int64_t)o.g.m * o.g.n);
+  char* const own = lds + wave * GRAD_WAVE;
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int64_t m = row0 + wr * TM + b * 16 + (lane & 15);
-    if (m >= o.g.m) continue;
-    const bool none = row_without(o, a, m);
+  for (int half = 0; half < 2; ++half) {
+    // The wave's LDS instructions run in order.
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 0; i < NA; ++i) {
-      const int64_t n = col0 + wc * TN + i * 16 + 4 * (lane >> 4);
-      if (n >= o.g.n) continue;
-      op_f32x4 v = {acc[i][b][0], acc[i][b][1], acc[i][b][2], acc[i][b][3]};
+    for (int i = 0; i < NA / 2; ++i)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        *reinterpret_cast<f32x4*>(own + (16 * b + (lane & 15)) * GRAD_PITCH + (16 * i + 4 * (lane >> 4)) * 4) = acc[half * (NA / 2) + i][b];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    const int64_t n = col0 + wc * TN + half * (TN / 2) + 4 * (lane & 7);
+#pragma unroll 2
+    for (int r = lane >> 3; r < TM; r += 8) {
+      const int64_t m = row0 + wr * TM + r;
+      if (m >= o.g.m || n >= o.g.n) continue;
+      const f32x4 x = *reinterpret_cast<const f32x4*>(own + r * GRAD_PITCH + (lane & 7) * 16);
+      op_f32x4 v = {x.x, x.y, x.z, x.w};
       if (o.add_partial) {
         const op_f32x4 u = row_load4(partial + m * o.g.n, n, o.g.n);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += u[e];
       }
       if (o.write_partial) row_store4(partial + m * o.g.n, n, o.g.n, v);
-      else write4<T>(o, a, scale, none, m, n, v);
+      else write4<T>(o, a, scale, row_without(o, a, m), m, n, v);
     }
   }
 }
@@ -556,8 +571,9 @@ void head_grads_kernel(HeadGrads a) {
   product.prime(t.i, t.j, kt0, kt1 - kt0);
   product.arrived();
   product.run(acc);
-  if (o.f32) write_out<float>(o, a, split, row0, col0, acc);
-  else write_out<bf16_t>(o, a, split, row0, col0, acc);
+  lds_free();
+  if (o.f32) write_out<float>(o, a, split, row0, col0, lds, acc);
+  else write_out<bf16_t>(o, a, split, row0, col0, lds, acc);
 }
 
 // The sums of contractions' parts, four columns a thread: one result's, then the other's.

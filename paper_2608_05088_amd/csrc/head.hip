@@ -323,15 +323,23 @@ void head_first_kernel(HeadLogits a) {
     for (int b = 0; b < NB; ++b) {
       const int ml = wr * TM + b * 16 + (lane & 15), yl = labels[turn * HEAD_TILE + ml] - c;   // the label's place in the wave's columns
       const float unit = HALVES ? scales[turn * HEAD_TILE + ml] * LOG2E : LOG2E;
-      if (end || __builtin_amdgcn_ballot_w64((unsigned)yl < TN)) {
+      if (__builtin_amdgcn_ballot_w64((unsigned)yl < TN)) {   // few waves meet a label
+        float z = 0.f;
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const bool label = yl == 16 * i + 4 * g + e;
-            if (label) gptr(a.at_label)[row0 + ml] = acc[i][b][e] * unit;
-            if (label || 16 * i + e >= left) acc[i][b][e] = -__builtin_inff();
+            z = label ? acc[i][b][e] : z;
+            acc[i][b][e] = label ? -__builtin_inff() : acc[i][b][e];
           }
+        if ((unsigned)yl < TN && ((yl >> 2) & 3) == g) gptr(a.at_label)[row0 + ml] = z * unit;
+      }
+      if (end) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][b][e] = 16 * i + e >= left ? -__builtin_inff() : acc[i][b][e];
       }
       float top = acc[0][b][0];
 #pragma unroll
@@ -422,13 +430,28 @@ void head_second_kernel(HeadLogits a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           acc[i][b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], unit, -s.x)) * s.y;
-      if (end || __builtin_amdgcn_ballot_w64(y < 0 || (unsigned)yl < TN)) {
-        // Zeros in rows that have no gradient, whatever their logits are, and past the end.
+      if (__builtin_amdgcn_ballot_w64((unsigned)yl < TN)) {
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[i][b][e] = y < 0 || 16 * i + e >= left ? 0.f : yl == 16 * i + 4 * g + e ? -s.z : acc[i][b][e];
+          for (int e = 0; e < 4; ++e) {
+            const bool label = yl == 16 * i + 4 * g + e;
+            acc[i][b][e] = label ? -s.z : acc[i][b][e];
+          }
+      }
+      // Zeros in rows that have no gradient, whatever their logits are, and past the end.
+      if (__builtin_amdgcn_ballot_w64(y < 0)) {
+        const bool none = y < 0;
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][b][e] = none ? 0.f : acc[i][b][e];
+      }
+      if (end) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][b][e] = 16 * i + e >= left ? 0.f : acc[i][b][e];
       }
     }
     // The next tile's loads are waited for before the stores go out: loads and stores may complete in any
@@ -487,18 +510,17 @@ void head_second_kernel(HeadLogits a) {
 
 namespace {
 
-// Columns n .. n + 3 of row m of a result, from their sums.
+// Four columns of a result, `width` of which there are, from their sums.
 template <class T>
-__device__ __forceinline__ void write4(const HeadOut& o, const HeadGrads& a, float scale, bool none, int64_t m, int64_t n, op_f32x4 v) {
-  T* const out = static_cast<T*>(o.out) + m * o.ldo;
+__device__ __forceinline__ void write4(const HeadOut& o, float scale, bool none, T* out, int64_t width, op_f32x4 v) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] = none || scale == 0.f ? 0.f : v[e] * scale;
   if (o.accumulate) {
-    const op_f32x4 u = row_load4(out, n, o.g.n);
+    const op_f32x4 u = row_load4(out, 0, width);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += u[e];
   }
-  row_store4(out, n, o.g.n, v);
+  row_store4(out, 0, width, v);
 }
 // Rows that have no gradient.
 __device__ __forceinline__ bool row_without(const HeadOut& o, const HeadGrads& a, int64_t m) {
@@ -517,8 +539,14 @@ __device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave / (NW / 2), wc = wave % (NW / 2);
   const float scale = scale_of(a);
-  float* const partial = o.partial + split * ((int64_t)o.g.m * o.g.n);
   char* const own = lds + wave * GRAD_WAVE;
+  const int64_t m0 = row0 + wr * TM + (lane >> 3);
+  const int rows = (int)(o.g.m - m0);   // there are, from this lane's first
+  uint32_t none = 0;                    // bit i: row 8 i has no gradient
+  if (o.mask_rows) {
+#pragma unroll
+    for (int i = 0; i < TM / 8; ++i) none |= (8 * i < rows && row_without(o, a, m0 + 8 * i) ? 1u : 0u) << i;
+  }
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     // The wave's LDS instructions run in order.
@@ -532,19 +560,23 @@ __device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, 
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
     const int64_t n = col0 + wc * TN + half * (TN / 2) + 4 * (lane & 7);
-#pragma unroll 2
-    for (int r = lane >> 3; r < TM; r += 8) {
-      const int64_t m = row0 + wr * TM + r;
-      if (m >= o.g.m || n >= o.g.n) continue;
-      const f32x4 x = *reinterpret_cast<const f32x4*>(own + r * GRAD_PITCH + (lane & 7) * 16);
+    if (n >= o.g.n) continue;
+    const char* from = own + (lane >> 3) * GRAD_PITCH + (lane & 7) * 16;
+    const int width = (int)(o.g.n - n);   // columns there are from this lane's first
+    float* part = o.partial + ((int64_t)split * o.g.m + m0) * o.g.n + n;
+    T* out = static_cast<T*>(o.out) + m0 * o.ldo + n;
+#pragma unroll 4
+    for (int i = 0; i < TM / 8; ++i, from += 8 * GRAD_PITCH, part += 8 * (int64_t)o.g.n, out += 8 * o.ldo) {
+      if (8 * i >= rows) break;
+      const f32x4 x = *reinterpret_cast<const f32x4*>(from);
       op_f32x4 v = {x.x, x.y, x.z, x.w};
       if (o.add_partial) {
-        const op_f32x4 u = row_load4(partial + m * o.g.n, n, o.g.n);
+        const op_f32x4 u = row_load4(part, 0, width);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += u[e];
       }
-      if (o.write_partial) row_store4(partial + m * o.g.n, n, o.g.n, v);
-      else write4<T>(o, a, scale, row_without(o, a, m), m, n, v);
+      if (o.write_partial) row_store4(part, 0, width, v);
+      else write4(o, scale, (none >> i) & 1, out, width, v);
     }
   }
 }
@@ -589,7 +621,7 @@ __device__ __forceinline__ void sum4(const HeadOut& o, const HeadGrads& a, int64
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += u[e];
   }
-  write4<T>(o, a, scale_of(a), row_without(o, a, m), m, n, v);
+  write4(o, scale_of(a), row_without(o, a, m), static_cast<T*>(o.out) + m * o.ldo + n, o.g.n - n, v);
 }
 __global__ __launch_bounds__(256) void head_sum_kernel(HeadGrads a, int first_blocks) {
   const bool second = (int)blockIdx.x >= first_blocks;

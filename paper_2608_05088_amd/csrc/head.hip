@@ -248,6 +248,19 @@ __device__ __forceinline__ float across(float v, F&& op) {
   return op(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
+// A 4 x 4 block of 16-bit values in a lane quad, turned: in, lane p holds column p's rows 0, 1 (x) and 2, 3 (y);
+// out, row p's four columns.  `pick` takes the low halves of this lane and the next (even lanes) or the
+// high ones of the one before and this (odd): byte permutes and selects, no branches.
+__device__ __forceinline__ uint32_t turn_pick(int lane) { return lane & 1 ? 0x03020706u : 0x05040100u; }
+__device__ __forceinline__ op_u32x2 turn_quad(uint2 v, uint32_t pick, bool low) {
+  const uint32_t x1 = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v.x, 0xB1, 0xF, 0xF, true);   // lane p ^ 1
+  const uint32_t y1 = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v.y, 0xB1, 0xF, 0xF, true);
+  const uint32_t a = __builtin_amdgcn_perm(x1, v.x, pick), b = __builtin_amdgcn_perm(y1, v.y, pick);   // two columns of rows p % 2, 2 + p % 2
+  const uint32_t give = low ? b : a;
+  const uint32_t got = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)give, 0x4E, 0xF, 0xF, true);      // lane p ^ 2
+  return op_u32x2{low ? a : got, low ? got : b};
+}
+
 // The scales of this lane's columns into its logits.
 __device__ __forceinline__ void scale_columns(const float* scales, int c, int g, f32x4 (&acc)[NA][NB]) {
   f32x4 w[NA];
@@ -399,6 +412,8 @@ void head_second_kernel(HeadLogits a) {
   int turn = 0;
   product.arrived();
   char* const sto = lds + AT_EPI + wave * OUT_WAVE;
+  const uint32_t pick = turn_pick(lane);
+  const bool low = (lane & 3) < 2;
   for (;;) {
     const int64_t col0 = (int64_t)t.j * HEAD_TILE;
     const int tile_m = t.i, tile_n = t.j;
@@ -478,8 +493,7 @@ void head_second_kernel(HeadLogits a) {
                               (wc * TN + 4 * g + (lane & 3)) * BK + b % 4 * 16 + (lane & 12);
 #pragma unroll
           for (int i = 0; i < NA; ++i) {
-            const uint2 q = quad_transpose(pk[i], lane & 3);
-            *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(out) + 16 * i * BK) = op_u32x2{q.x, q.y};
+            *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(out) + 16 * i * BK) = turn_quad(pk[i], pick, low);
           }
         }
         if (a.dz) {

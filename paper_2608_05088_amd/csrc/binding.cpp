@@ -297,6 +297,28 @@ NormOut norm(const Tensor& x, const Tensor& weight, const Tensor& residual, doub
 
 void* current_stream(const Tensor& x) { return c10::hip::getCurrentHIPStream(x.device().index()).stream(); }
 
+// In a captured backward pass: refuses to go on in a graph that was built on the default stream (leaves
+// whose eager graph still lives have such nodes).  The engine would make that stream wait for the
+// capture, which no capture survives, nor the process.
+void check_captured_backward() {
+  const auto node = torch::autograd::get_current_node();
+  if (!node) return;
+  const auto here = node->stream();
+  if (!here) return;
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(c10::hip::getCurrentHIPStream(here->device_index()).stream(), &status) != hipSuccess ||
+      status == hipStreamCaptureStatusNone)
+    return;
+  for (size_t i = 0; i < node->num_outputs(); ++i) {
+    const auto& edge = node->next_edge(i);
+    if (!edge.is_valid() || !node->task_should_compute_output(i)) continue;
+    const auto there = edge.function->stream();
+    if (there && there->id() == 0)
+      throw std::runtime_error("a captured backward pass reaches a graph that was built on the default stream: drop what holds it "
+                               "(outputs of eager calls on the same leaves), or make those calls on a stream of their own");
+  }
+}
+
 struct RmsNorm : torch::autograd::Function<RmsNorm> {
   static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& x, const Tensor& weight,
                                                 const std::optional<Tensor>& residual_, double eps, int64_t out_type) {
@@ -311,6 +333,7 @@ struct RmsNorm : torch::autograd::Function<RmsNorm> {
 
   static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
     torch::autograd::variable_list out(5);
+    check_captured_backward();
     {
       at::NoGradGuard no_grad;
       const auto saved = ctx->get_saved_variables();
@@ -416,4 +439,5 @@ PYBIND11_MODULE(_malt, m) {
   m.def("adamw_moments", &adamw_moments);
   m.def("rms_norm", &rms_norm);
   m.def("rms_norm_fp8", &rms_norm_fp8);
+  m.def("check_captured_backward", &check_captured_backward);
 }

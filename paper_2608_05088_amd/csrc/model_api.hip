@@ -254,7 +254,7 @@ extern "C" {
 // ------------------------------------------------------------------------ AdamW
 malt_status_t malt_adamw_state_size(int64_t numel, int32_t bits, size_t* bytes) {
   if (!bytes) return fail(MALT_ERR_INVALID_ARG, "output pointer is NULL");
-  MALT_TRY(check_adam_tensor(0, numel, bytes, bits == 8 ? 8 : bits));
+  MALT_TRY(check_adam_tensor(0, numel, bytes, bits));
   *bytes = size_t(adam_state_bytes(numel, bits));
   return MALT_OK;
 }

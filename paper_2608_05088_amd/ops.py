@@ -682,6 +682,7 @@ class _LinearCrossEntropy(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
+        _host().check_captured_backward()
         x, weight, labels, stats = ctx.saved_tensors
         need_x, need_w = ctx.needs_input_grad[:2]
         _, dx, dw, _ = _head(x, weight, labels, grad.float(), False, need_x, need_w, None, False, stats, False, None)

@@ -155,3 +155,47 @@ def test_adamw_beside_malt_is_torchs(ops):
             assert torch.equal(p, q)
         else:
             assert float((p - q).detach().abs().max()) <= 3 * (40 * 1e-3 * 2.0 ** -24 * 10 + 3 * 2.0 ** -24 * float(q.detach().abs().max())), n
+
+
+@pytest.mark.parametrize("op", ["head", "norm"])
+def test_a_captured_backward_pass_and_an_eager_graph(ops, op):
+    """Beside an eager graph of the same leaves on the default stream a captured backward pass is refused, before
+    the engine reaches that graph; without one, or with one of another stream, it is captured."""
+    x = torch.randn((40, 64), device="cuda", generator=gen(90))
+    w = torch.rand((64,) if op == "norm" else (100, 64), device="cuda", generator=gen(91)).requires_grad_()
+    y = torch.arange(40, device="cuda")
+    dy = torch.randn((40, 64) if op == "norm" else (40,), device="cuda", generator=gen(92))
+
+    def forward():
+        return ops.rms_norm(x, w) if op == "norm" else ops.linear_cross_entropy(x, w, y)
+
+    def capture():
+        g = torch.cuda.CUDAGraph()
+        w.grad = None
+        with torch.cuda.graph(g):
+            forward().backward(dy)
+        return g
+
+    eager = forward()
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="default stream"):
+        capture()
+    torch.cuda.synchronize()
+    w.grad = None
+    eager.backward(dy)
+    want = w.grad.clone()
+    del eager
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        held = forward()
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    for _ in range(2):   # beside a graph of another stream, then beside none
+        g = capture()
+        for _ in range(3):
+            w.grad.fill_(7.0)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(w.grad, want)
+        held = None

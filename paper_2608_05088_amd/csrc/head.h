@@ -104,7 +104,7 @@ struct HeadFew {
   malt_f32x2* partial;
   float* at_label;
 };
-int head_few_parts(int64_t vocab);
+int head_few_parts(int64_t vocab, int64_t inner);
 
 struct HeadPack {
   const void* x;

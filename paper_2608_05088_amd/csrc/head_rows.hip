@@ -240,13 +240,19 @@ struct Few<float> {
   }
 };
 
-constexpr int FEW_WAVES = 4, FEW_COLS = 16 * FEW_WAVES;
+constexpr int FEW_WAVES = 4;
+// SPLIT: a workgroup's waves share 16 rows of the weight and cut the contraction; else they take 16 each.
+// us a call, split | whole, one row of bf16: 3000 x 4096 15 | 31 (the host), 12000 x 4096 25 | 40, 50257 x 1280
+// 32 | 34, 50257 x 4096 79 | 101, 50257 x 768 24 | 24; 32 rows of float32: 3000 x 4096 37 | 121, 18000 x 768 32 | 40.
+// Whole where there are many rows or short ones: 131072 x 2048 120 | 104, 32 rows of 50257 x 128 21 | 15.
+bool few_split(int64_t vocab, int64_t inner) { return vocab <= 65536 && inner >= (vocab <= 20480 ? 512 : 1024); }
 
-template <class C, class X, class W, int MB>
+template <class C, class X, class W, int MB, bool SPLIT>
 __global__ __launch_bounds__(64 * FEW_WAVES) void head_few_kernel(HeadFew a) {
-  __shared__ malt_f32x2 join[FEW_WAVES][MB * 16];
+  constexpr int COLS = SPLIT ? 16 : 16 * FEW_WAVES, JOIN = SPLIT ? 1 : FEW_WAVES, CUT = SPLIT ? FEW_WAVES : 1;
+  __shared__ malt_f32x2 join[JOIN][MB * 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int64_t n0 = (int64_t)blockIdx.x * FEW_COLS + 16 * wave;
+  const int64_t n0 = (int64_t)blockIdx.x * COLS + (SPLIT ? 0 : 16 * wave);
   const int64_t n = n0 + r < a.vocab ? n0 + r : a.vocab - 1;   // past the end: not counted below
   const W* const w = static_cast<const W*>(a.w) + n * a.ldw;
   const X* x[MB];
@@ -258,7 +264,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void head_few_kernel(HeadFew a) {
   f32x4 acc[MB];
 #pragma unroll
   for (int b = 0; b < MB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int k0 = 0; k0 < a.k; k0 += C::K) {
+  for (int k0 = SPLIT ? wave * C::K : 0; k0 < a.k; k0 += CUT * C::K) {
     const int k = k0 + C::PER * g;
     C fw, fx;
     fw.load(w, k, a.k);
@@ -268,6 +274,15 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void head_few_kernel(HeadFew a) {
       acc[b] = C::mma(fw, fx, acc[b]);
     }
   }
+  if constexpr (SPLIT) {
+    __shared__ f32x4 parts[FEW_WAVES][MB][64];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) parts[wave][b][lane] = acc[b];
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < MB; ++b) acc[b] = (parts[0][b][lane] + parts[1][b][lane]) + (parts[2][b][lane] + parts[3][b][lane]);
+  }
+  const int slot = SPLIT ? 0 : wave;   // of SPLIT all waves hold the same sums, the first writes
   // acc[b][e]: row 16 b + lane % 16, column n0 + 4 (lane / 16) + e.
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
@@ -277,7 +292,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void head_few_kernel(HeadFew a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       z[e] = acc[b][e] * LOG2E;
-      if (c + e == y) gptr(a.at_label)[m] = z[e];
+      if (c + e == y && (!SPLIT || wave == 0)) gptr(a.at_label)[m] = z[e];
       if (c + e == y || c + e >= a.vocab) z[e] = -__builtin_inff();
       top = fmaxf(top, z[e]);
     }
@@ -288,16 +303,16 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void head_few_kernel(HeadFew a) {
     for (int e = 0; e < 4; ++e) sum += exp2f(z[e] - ref);
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
-    if (g == 0) join[wave][m] = malt_f32x2{top, sum};
+    if (g == 0 && (!SPLIT || wave == 0)) join[slot][m] = malt_f32x2{top, sum};
   }
   __syncthreads();
   if (threadIdx.x < a.m) {
     float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < FEW_WAVES; ++i) top = fmaxf(top, join[i][threadIdx.x].x);
+    for (int i = 0; i < JOIN; ++i) top = fmaxf(top, join[i][threadIdx.x].x);
     const float ref = top == -__builtin_inff() ? 0.f : top;
 #pragma unroll
-    for (int i = 0; i < FEW_WAVES; ++i) sum += join[i][threadIdx.x].y * exp2f(join[i][threadIdx.x].x - ref);
+    for (int i = 0; i < JOIN; ++i) sum += join[i][threadIdx.x].y * exp2f(join[i][threadIdx.x].x - ref);
     gptr(a.partial)[(int64_t)threadIdx.x * a.parts + blockIdx.x] = malt_f32x2{top, sum};
   }
 }
@@ -374,16 +389,24 @@ __global__ __launch_bounds__(T) void head_join_kernel(HeadJoin a) {
   }
 }
 
+template <class C, class X, class W, bool SPLIT>
+void few_of(const HeadFew& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.parts), block(64 * FEW_WAVES);
+  if (a.m <= 16) hipLaunchKernelGGL((head_few_kernel<C, X, W, 1, SPLIT>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((head_few_kernel<C, X, W, 2, SPLIT>), grid, block, 0, s, a);
+}
 template <class C, class X, class W>
 void few(const HeadFew& a, hipStream_t s) {
-  const dim3 grid((unsigned)a.parts), block(64 * FEW_WAVES);
-  if (a.m <= 16) hipLaunchKernelGGL((head_few_kernel<C, X, W, 1>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((head_few_kernel<C, X, W, 2>), grid, block, 0, s, a);
+  if (few_split(a.vocab, a.k)) few_of<C, X, W, true>(a, s);
+  else few_of<C, X, W, false>(a, s);
 }
 
 }  // namespace
 
-int head_few_parts(int64_t vocab) { return (int)((vocab + FEW_COLS - 1) / FEW_COLS); }
+int head_few_parts(int64_t vocab, int64_t inner) {
+  const int cols = few_split(vocab, inner) ? 16 : 16 * FEW_WAVES;
+  return (int)((vocab + cols - 1) / cols);
+}
 
 hipError_t launch_head_few(const HeadFew& a, bool x_f32, bool w_f32, hipStream_t s) {
   if (x_f32 && w_f32) few<Few<float>, float, float>(a, s);

@@ -146,7 +146,7 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     end += align256(bytes);
     return at;
   };
-  L.parts = L.few ? head_few_parts(a.vocab) : int(up(a.vocab, HEAD_TILE) / HEAD_TILE);
+  L.parts = L.few ? head_few_parts(a.vocab, a.inner) : int(up(a.vocab, HEAD_TILE) / HEAD_TILE);
   if (!a.stats_given) {
     L.partial = take(size_t(a.rows) * L.parts * 8);
     L.at_label = take(size_t(a.rows) * 4);

@@ -128,6 +128,14 @@ def test_losses_and_gradients(ops, m, v, k, xt, wt):
     e.check(ops.linear_cross_entropy(x, w, y))
 
 
+@pytest.mark.parametrize("xt,wt", [(BF16, BF16), (F32, F32), (BF16, F32)])
+@pytest.mark.parametrize("m,v,k", [(1, 17, 512), (1, 1000, 511), (3, 1, 700), (16, 500, 1029), (17, 20481, 520), (32, 300, 4100), (5, 21000, 1025)])
+def test_few_rows_of_long_contractions(ops, m, v, k, xt, wt):
+    """A contraction cut between waves, some of which may have none of it."""
+    x, w, y = inputs(m + v + k, m, v, k, xt, wt)
+    Exact(x, w, y).check(ops.linear_cross_entropy(x, w, y), None, None)
+
+
 @pytest.mark.parametrize("m,v,k", [(5000, 300, 64), (40, 20000, 64), (300, 9000, 100), (1000, 5000, 1280)])
 def test_long_contractions_are_cut(ops, m, v, k):
     x, w, y = inputs(m + v, m, v, k)

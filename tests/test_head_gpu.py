@@ -406,3 +406,46 @@ def test_rows_behind_the_last_stay(ops):
     store = torch.full((75, 20), 3.0, device="cuda")
     ops.linear_cross_entropy_step(x, w, y, out=store[:70])
     assert bool((store[70:] == 3).all())
+
+
+@pytest.mark.parametrize("m", [2, 40])
+def test_offsets_past_32_bits(ops, m):
+    """A weight of more than 2^31 elements, its last rows the labels of some."""
+    v, k = (1 << 22) - 3, 576
+    w = torch.randn((v, k), device="cuda", dtype=BF16, generator=gen(43))
+    w *= 2 / math.sqrt(k)
+    x = torch.randn((m, k), device="cuda", generator=gen(44)).to(BF16)
+    y = torch.arange(m, device="cuda") * 7
+    y[1] = v - 1
+    losses, dx, dw = ops.linear_cross_entropy_step(x, w, y)
+    x64 = x.double()
+    lse = torch.full((m,), -math.inf, device="cuda", dtype=torch.float64)
+    for part in w.split(1 << 18):
+        lse = torch.logaddexp(lse, torch.logsumexp(x64 @ part.double().t(), 1))
+    want = lse - (x64 * w[y].double()).sum(1)
+    # As in Exact: the logits' errors by their terms, and what the loss rounds.
+    dz = (6 * k + 8) * U * float((x64.abs() @ w[:4096].double().abs().t()).max()) * 2
+    assert float((losses.double() - want).abs().max()) <= 2 * dz + 128 * U + 4 * U * 60 + 8 * U * float(want.max())
+    # The gradient's last rows: p x and, of the label, (p - 1) x.
+    tail = w[-1000:].double()
+    p = torch.exp(x64 @ tail.t() - lse[:, None])
+    p[1, -1] = torch.expm1(torch.log(p[1, -1]))
+    exact = p.t() @ x64
+    bound = p.abs().t() @ x64.abs()
+    err = (4 * dz + 256 * U + half(BF16) * 2.01) * bound + half(BF16) * exact.abs() + 1e-38
+    assert bool(((dw[-1000:].double() - exact).abs() <= err).all())
+    assert bool((dw[12345:12345 + 50].double() != 0).any())
+    step = torch.zeros((m, k), device="cuda", dtype=torch.float64)
+    size = torch.zeros((m, k), device="cuda", dtype=torch.float64)
+    at = 0
+    for part in w.split(1 << 18):
+        b = part.double()
+        q = torch.exp(x64 @ b.t() - lse[:, None])
+        here = (y >= at) & (y < at + len(b))
+        q[here, y[here] - at] -= 1.0
+        step += q @ b
+        size += q.abs() @ b.abs()
+        at += len(b)
+    # A sum of v terms is rounded at most twice for each 32 of them, an instruction's.
+    err = (4 * dz + 256 * U + half(BF16) * 2.01 + v / 16 * U) * size + half(BF16) * step.abs()
+    assert bool(((dx.double() - step).abs() <= err).all())

@@ -331,9 +331,11 @@ void head_first_kernel(HeadLogits a) {
     }
     const int c = (int)col0 + wc * TN, left = a.g.n - c - 4 * g;   // columns there are from this lane's first
     const bool end = a.g.n - c < TN;
+    const int rows = a.g.m - (int)row0 - wr * TM;   // this wave's
     if constexpr (HALVES) scale_columns(a.w_scales, c, g, acc);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
+      if (b % 4 == 0 && 16 * b >= rows) break;
       const int ml = wr * TM + b * 16 + (lane & 15), yl = labels[turn * HEAD_TILE + ml] - c;   // the label's place in the wave's columns
       const float unit = HALVES ? scales[turn * HEAD_TILE + ml] * LOG2E : LOG2E;
       if (__builtin_amdgcn_ballot_w64((unsigned)yl < TN)) {   // few waves meet a label
@@ -433,9 +435,12 @@ void head_second_kernel(HeadLogits a) {
     }
     const int c = (int)col0 + wc * TN, left = a.g.n - c - 4 * g;
     const bool end = a.g.n - c < TN;
+    // This wave's rows, to the end of the last stage that the gradients read.
+    const int rows = (a.g.m - tile_m * HEAD_TILE + BK - 1) / BK * BK - wr * TM;
     if constexpr (HALVES) scale_columns(a.w_scales, c, g, acc);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
+      if (b % 4 == 0 && 16 * b >= rows) break;
       const int ml = wr * TM + b * 16 + (lane & 15);
       const f32x4 s = records[turn * HEAD_TILE + ml];
       const float unit = HALVES ? scales[turn * HEAD_TILE + ml] * LOG2E : LOG2E;
@@ -474,6 +479,7 @@ void head_second_kernel(HeadLogits a) {
     product.arrived();
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
+      if (b % 4 == 0 && 16 * b >= rows) break;
       for (int p = 0; p < a.dz_planes; ++p) {
         uint2 pk[NA];
 #pragma unroll
@@ -622,27 +628,44 @@ void head_grads_kernel(HeadGrads a) {
   else write_out<bf16_t>(o, a, split, row0, col0, lds, acc);
 }
 
-// The sums of contractions' parts, four columns a thread: one result's, then the other's.
+// The sums of contractions' parts, four columns a thread: one result's, then the other's.  Of many parts
+// a wave takes a quarter each, or few outputs would wait for one load after another (74 x 431, 64 parts: 30 -> 9 us).
+constexpr int SUM_MANY = 16, SUM_WAVES = 4;
+__host__ __device__ inline int sum_quads(const HeadOut& o) { return o.splits >= SUM_MANY ? 64 : 64 * SUM_WAVES; }   // of a workgroup
 template <class T>
-__device__ __forceinline__ void sum4(const HeadOut& o, const HeadGrads& a, int64_t i) {
-  const int64_t per = (o.g.n + 3) / 4, m = i / per, n = i % per * 4;
-  if (m >= o.g.m) return;
-  const float* p = o.partial + m * o.g.n;
-  op_f32x4 v = row_load4(p, n, o.g.n);
-  for (int s = 1; s < o.splits; ++s) {
-    p += (int64_t)o.g.m * o.g.n;
-    const op_f32x4 u = row_load4(p, n, o.g.n);
+__device__ __forceinline__ void sum4(const HeadOut& o, const HeadGrads& a, int64_t block, op_f32x4 (&join)[SUM_WAVES][64]) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const bool many = o.splits >= SUM_MANY;   // the same for a workgroup
+  const int64_t i = block * sum_quads(o) + (many ? lane : threadIdx.x), per = (o.g.n + 3) / 4, m = i / per, n = i % per * 4;
+  const int first = many ? wave : 0, step = many ? SUM_WAVES : 1;
+  op_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (m < o.g.m) {
+    const float* const p = o.partial + m * o.g.n;
+#pragma unroll 4
+    for (int s = first; s < o.splits; s += step) {
+      const op_f32x4 u = row_load4(p + s * (int64_t)o.g.m * o.g.n, n, o.g.n);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += u[e];
+      for (int e = 0; e < 4; ++e) v[e] += u[e];
+    }
   }
-  write4(o, scale_of(a), row_without(o, a, m), static_cast<T*>(o.out) + m * o.ldo + n, o.g.n - n, v);
+  if (many) {
+    join[wave][lane] = v;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < SUM_WAVES; ++w)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += join[w][lane][e];
+  }
+  if (m < o.g.m) write4(o, scale_of(a), row_without(o, a, m), static_cast<T*>(o.out) + m * o.ldo + n, o.g.n - n, v);
 }
-__global__ __launch_bounds__(256) void head_sum_kernel(HeadGrads a, int first_blocks) {
+__global__ __launch_bounds__(64 * SUM_WAVES) void head_sum_kernel(HeadGrads a, int first_blocks) {
+  __shared__ op_f32x4 join[SUM_WAVES][64];
   const bool second = (int)blockIdx.x >= first_blocks;
   const HeadOut& o = a.part[second ? 1 : 0];
-  const int64_t i = (int64_t)(blockIdx.x - (second ? first_blocks : 0)) * 256 + threadIdx.x;
-  if (o.f32) sum4<float>(o, a, i);
-  else sum4<bf16_t>(o, a, i);
+  const int64_t block = blockIdx.x - (second ? first_blocks : 0);
+  if (o.f32) sum4<float>(o, a, block, join);
+  else sum4<bf16_t>(o, a, block, join);
 }
 
 // The kernels use more dynamic LDS than the default limit: raised once for each device.
@@ -681,7 +704,10 @@ hipError_t launch_head_grads(const HeadGrads& a, hipStream_t s) {
 }
 
 hipError_t launch_head_sum(const HeadGrads& a, bool first, bool second, hipStream_t s) {
-  auto blocks = [&](int i) { return (int)(((int64_t)a.part[i].g.m * ((a.part[i].g.n + 3) / 4) + 255) / 256); };
+  auto blocks = [&](int i) {
+    const int quads = sum_quads(a.part[i]);
+    return (int)(((int64_t)a.part[i].g.m * ((a.part[i].g.n + 3) / 4) + quads - 1) / quads);
+  };
   const int n = first ? blocks(0) : 0, all = n + (second ? blocks(1) : 0);
   if (all == 0) return hipSuccess;
   hipLaunchKernelGGL(head_sum_kernel, dim3((unsigned)all), dim3(256), 0, s, a, n);

@@ -266,7 +266,7 @@ malt_status_t malt_adamw_step(const malt_adamw_tensors_t* t, const malt_adamw_t*
     return fail(MALT_ERR_INVALID_ARG, "a list of the tensors is NULL");
   if (!(h->lr >= 0 && number(h->lr))) return fail(MALT_ERR_INVALID_ARG, "lr must be a number, 0 or more");
   if (!(h->beta1 >= 0 && h->beta1 < 1 && h->beta2 >= 0 && h->beta2 < 1)) return fail(MALT_ERR_INVALID_ARG, "betas must be in [0, 1)");
-  if (!((float)h->eps > 0 && number(h->eps))) return fail(MALT_ERR_INVALID_ARG, "eps must be positive");
+  if (!((float)h->eps >= 0x1p-126f && number(h->eps))) return fail(MALT_ERR_INVALID_ARG, "eps must be at least 2^-126");
   if (!(h->weight_decay >= 0 && number(h->weight_decay))) return fail(MALT_ERR_INVALID_ARG, "weight_decay must be a number, 0 or more");
   if (h->step < 1) return fail(MALT_ERR_INVALID_ARG, "step counts from 1 (got %lld)", (long long)h->step);
   if (!number(h->grad_scale)) return fail(MALT_ERR_INVALID_ARG, "grad_scale must be a number");

@@ -523,7 +523,8 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
  *    v above zero at least one step.  u in (0, 1) is a hash of seed, the tensor's place in the
  *    call, the block and the element's place in it: equal calls give equal bits, and another seed for each
  *    step keeps sums over steps right on average.  The step itself uses m and v unrounded.
- * Each of m's and v's products and sums is rounded to float32.
+ * Each of m's and v's products and sums is rounded to float32; the update, by the hardware's root and
+ * reciprocal, is off by 12 2^-24 of itself at most.  eps >= 2^-126.
  * No written buffer may overlap another (a tensor named twice is refused).  A captured call
  * keeps its arguments, step and seed among them.  numel <= 2^35.
  * malt_adamw_moments writes what 8-bit states stand for: float32 m[numel], then v[numel]. */

@@ -303,6 +303,34 @@ def test_updates_stay_bounded_where_moments_are_small(ops):
         assert float((p[0] - before).abs().max()) <= 1e-3 * 10 * 2.0
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_tiny_and_huge_second_moments(ops, bits):
+    """Roots of subnormal numbers and near the largest, beside the smallest eps and a large one: the update within
+    its bound where 64 bits give a float32 number."""
+    v = torch.tensor([1e-44, 1e-42, 3e-39, 1.2e-38, 1e-30, 1.2e-29, 1.3e-29, 1.0, 1e30, 3e38], device="cuda")
+    for eps in (2.0 ** -126, 1e-20, 1e10):
+        p = [torch.zeros(len(v), device="cuda")]
+        m = torch.sqrt(v) * 0.5   # no gradient: b1 m and b2 v are all there is
+        if bits == 32:
+            st = [torch.stack([m, v])]
+            old = st[0].clone()
+        else:   # one block: what lies far below its largest becomes its smallest code
+            st = [ops.adamw_state(p[0], 8)]
+            ops.adamw_step(p, [m * 1e-3], st, step=1, seed=3, lr=0.0, betas=(0.0, 0.0), weight_decay=0.0)
+            old = ops.adamw_moments(p, st)[0].clone()
+        ops.adamw_step(p, [torch.zeros_like(p[0])], st, step=2, lr=1.0, betas=(0.9, 0.95), eps=eps, weight_decay=0.0)
+        m64, v64 = old.double()
+        want_m, want_v = f32(0.9) * m64, f32(0.95) * v64
+        den = want_v.sqrt() / math.sqrt(1 - 0.95 ** 2) + f32(eps)
+        update = want_m / (1 - 0.9 ** 2) / den
+        # v' is rounded to a subnormal number: half of 2^-149, in the root its share of v'.
+        slack = 2.0 ** -150 / want_v.clamp(min=1e-46)
+        fits = (den < 2.0 ** 126) & torch.isfinite(old.sum(0))
+        off = (p[0].double() + update).abs()
+        bound = update.abs() * (16 * U + slack) + 2.0 ** -126
+        assert bool((off <= bound)[fits].all()), (eps, off / bound)
+
+
 # --------------------------------------------------------------------- the calls
 def test_gradient_scale(ops):
     shapes = [(1000,), (77, 3)]

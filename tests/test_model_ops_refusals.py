@@ -67,9 +67,9 @@ def test_head_workspace(L):
     # The vocabulary is worked on in pieces: dz both ways stays within 2 x 512 MiB (three planes each in float32).
     big = _head(rows=65536, vocab=100000, inner=64)
     assert L.malt_linear_loss_size(byref(big), byref(size)) == lm.MALT_OK and size.value < (2 << 30)
-    # Losses of few rows take their statistics only.
+    # Losses of few rows take their statistics only: 8 bytes for each 16 columns and the labels' logits, in whole 256 bytes.
     few = _head(rows=1, vocab=50257, inner=1280, ldx=1280, ldw=1280, dx=None, dweight=None)
-    assert L.malt_linear_loss_size(byref(few), byref(size)) == lm.MALT_OK and size.value < 16384
+    assert L.malt_linear_loss_size(byref(few), byref(size)) == lm.MALT_OK and size.value <= 8 * 3142 + 512
     none = _head(rows=0, dweight=None)
     assert L.malt_linear_loss(byref(none), c_void_p(P[10]), 1 << 30, None) == lm.MALT_OK
 
@@ -98,7 +98,7 @@ def _adam(n=2, hp=None, **kw):
     (dict(hp=dict(grad_scale_at=P[0])), ALIAS), (dict(hp=dict(grad_scale_at=P[9] + 2)), ALIGN),
     (dict(hp=dict(lr=-1.0)), BAD), (dict(hp=dict(lr=float("nan"))), BAD), (dict(hp=dict(lr=float("inf"))), BAD),
     (dict(hp=dict(beta1=1.0)), BAD), (dict(hp=dict(beta2=-0.1)), BAD), (dict(hp=dict(beta1=float("nan"))), BAD),
-    (dict(hp=dict(eps=0.0)), BAD), (dict(hp=dict(eps=1e-60)), BAD), (dict(hp=dict(weight_decay=-1.0)), BAD),
+    (dict(hp=dict(eps=0.0)), BAD), (dict(hp=dict(eps=1e-60)), BAD), (dict(hp=dict(eps=1e-38)), BAD), (dict(hp=dict(weight_decay=-1.0)), BAD),
     (dict(hp=dict(step=0)), BAD), (dict(hp=dict(grad_scale=float("inf"))), BAD),
 ])
 def test_adamw_refuses(L, kw, code):

@@ -331,6 +331,7 @@ __global__ __launch_bounds__(T) void head_join_kernel(HeadJoin a) {
   const int parts = a.parts;
   const malt_f32x2* const p = a.partial + r * parts;
   float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll 4
   for (int i = threadIdx.x; i < parts; i += T) {
     const malt_f32x2 v = gptr(p)[i];
     const float t = fmaxf(top, v.x), ref = t == -__builtin_inff() ? 0.f : t;
@@ -419,7 +420,7 @@ hipError_t launch_head_few(const HeadFew& a, bool x_f32, bool w_f32, hipStream_t
 hipError_t launch_head_join(const HeadJoin& a, hipStream_t s) {
   // A wave a row where there are enough rows to fill the card.
   const dim3 grid((unsigned)(a.records ? a.rows_pad : a.m));
-  if (a.m <= HEAD_FEW) hipLaunchKernelGGL((head_join_kernel<256>), grid, dim3(256), 0, s, a);
+  if (a.m <= HEAD_FEW) hipLaunchKernelGGL((head_join_kernel<1024>), grid, dim3(1024), 0, s, a);
   else hipLaunchKernelGGL((head_join_kernel<64>), grid, dim3(64), 0, s, a);
   return hipGetLastError();
 }

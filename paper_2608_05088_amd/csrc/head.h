@@ -141,8 +141,8 @@ struct HeadJoin {
   float* losses;       // or null
 };
 hipError_t launch_head_join(const HeadJoin& a, hipStream_t s);
-hipError_t launch_head_logits(const HeadLogits& a, bool second, hipStream_t s);
-hipError_t launch_head_grads(const HeadGrads& a, hipStream_t s);
+hipError_t launch_head_logits(const HeadLogits& a, int edge, bool second, hipStream_t s);   // of the tiles, as below
+hipError_t launch_head_grads(const HeadGrads& a, int edge, hipStream_t s);
 hipError_t launch_head_sum(const HeadGrads& a, bool first, bool second, hipStream_t s);
 hipError_t head_setup();
 

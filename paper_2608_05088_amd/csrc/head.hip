@@ -8,8 +8,17 @@
 // The logits are formed twice because M x V of them in 32 bits would cost as much to write and
 // read (twice 4 bytes a logit) as the K products that make one.
 //
+// 8192 x 50257 x 1280 in bf16, 1.05 T operations a product: first pass 950 us (1110 TFLOP/s; the library's
+// product that writes its logits: 939), second 1320 in two pieces, gradients 1740 (1210 TFLOP/s; the library's: 2450).
+// A stage of 64 takes a tile 1.40 to 1.46 us with random values and 1.23 with zeros: the power limit.  What the
+// second pass takes longer is its writing: a tile's dz, 256 KB both ways, 24 us of 53, while no matrix
+// instruction runs on that CU.
+//
 // A workgroup of eight waves makes one 256 x 256 tile, the pipeline of the Newton-Schulz
-// update (ns_common.h): stages of 64 contracted values go straight to LDS, two slots deep.  Both
+// update (ns_common.h): stages of 64 contracted values go straight to LDS, two slots deep.  Where
+// there are few tiles or few stages in each, tiles are of 128 x 128, two on a CU, which read twice the LDS for a
+// product but leave no CU out and work on one's stages during the other's epilogue: 300 x 1000 x 64 76 -> 40 us a
+// step, 200 x 8000 x 512 in float32 168 -> 94, 500 x 2000 x 2000 162 -> 87 (the rules are in model_api.hip).  Both
 // sides of every product lie with the contraction along their rows: x and W are transposed once for
 // the gradients, dz is written both ways.  (Transposed LDS reads instead: 1.84 us a stage, for one side or
 // both; rows of 32 KB apart: 1.70, with a pitch that is no power of two 1.58.)
@@ -20,9 +29,10 @@
 //     below 2^-22 of the whole, as the planes' own rounding).
 //   gradients: three bf16 planes, all 24 bits; six pairs (middle by low and low by low are below
 //     2^-24).  float16 would not do for dz, whose values have no row or column of like size.
-// At the matrix cores' 16-bit rate that is three and 1.5 times the float32 instruction's.  bf16
-// gradients take dz and the operands as single planes: dz is rounded once more, an error of the size
-// of the result's own rounding.
+// At the matrix cores' 16-bit rate that is three and 1.5 times the float32 instruction's
+// (1001 x 50257 x 901: 310, 535 and 1040 us; in one float32 product each the matrix cores would need 4 x 590).
+// bf16 gradients take one plane of dz, rounded once more, an error of the size of the result's own
+// rounding (two planes where the problem is small, and of a float32 operand).
 //
 // An XCD's 32 CUs work on 8 x 4 neighbouring tiles at a time, so that the twelve panels they read
 // come once from memory and otherwise from its L2.
@@ -39,20 +49,28 @@ using namespace ns;
 namespace {
 
 using G = NsGeom<HEAD_BK, 2, 32>;
-constexpr int BK = G::BK, STAGES = G::STAGES, H = G::H, RB = G::RB, CPR = G::CPR, LOADS = G::LOADS;
+constexpr int BK = G::BK, STAGES = G::STAGES, H = G::H, RB = G::RB, CPR = G::CPR;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-constexpr int NB = TM / 16, NA = TN / 16;
 constexpr float LOG2E = 1.44269504088896340736f;
-// Behind the ring, so that the next tile's first stages can arrive during a tile's epilogue: rows'
-// records or labels and scales of two tiles, and the waves' statistics or 16 rows of each wave's dz (padded by 8 bytes).
-constexpr int ROW_BYTES = HEAD_TILE * 16;
-constexpr int AT_ROWS = G::RING_BYTES, AT_SCALES = AT_ROWS + 2 * ROW_BYTES, AT_EPI = AT_SCALES + 2 * HEAD_TILE * 4;
-constexpr int OUT_PITCH = TN * 2 + 8, OUT_WAVE = 16 * OUT_PITCH;
-constexpr int JOIN_BYTES = HEAD_TILE * (NW / 2) * 8;
-constexpr int LDS_BYTES = AT_EPI + (NW * OUT_WAVE > JOIN_BYTES ? NW * OUT_WAVE : JOIN_BYTES);
-static_assert(LDS_BYTES <= 160 * 1024, "LDS budget");
-constexpr int CUS = 256;   // workgroups of the passes over the logits, one a CU
-static_assert(STAGES == 2 && (G::STAGE_BYTES & (G::STAGE_BYTES - 1)) == 0 && BK == 64 && TN == BK && TM == 2 * BK && CPR == 8 && LOADS == 8 && 16 % (G::RPP * CPR) == 0, "the loads and reads below");
+// A tile of E x E and the waves' 2 x 4 parts of it.
+template <int E>
+struct Shape {
+  static constexpr int TM = E / 2, TN = E / (NW / 2), NB = TM / 16, NA = TN / 16;
+  static constexpr int OPER = E * RB, STAGE = 2 * OPER, RING = STAGES * STAGE;   // bytes
+  static constexpr int LOADS = STAGE / 1024 / NW;                                // 1 KB each, a wave's of a stage
+  // Behind the ring, so that the next tile's first stages can arrive during a tile's epilogue: rows'
+  // records or labels and scales of two tiles, and the waves' statistics or 16 rows of each wave's dz (padded by 8 bytes).
+  static constexpr int AT_ROWS = RING, AT_SCALES = AT_ROWS + 2 * E * 16, AT_EPI = AT_SCALES + 2 * E * 4;
+  static constexpr int OUT_PITCH = TN * 2 + 8, OUT_WAVE = 16 * OUT_PITCH, JOIN = E * (NW / 2) * 8;
+  // A result's 32 columns of a wave's rows (padded by 16 bytes), in the ring's place.
+  static constexpr int GRAD_PITCH = 32 * 4 + 16, GRAD_WAVE = TM * GRAD_PITCH;
+  static constexpr int EPI = NW * OUT_WAVE > JOIN ? NW * OUT_WAVE : JOIN;
+  static constexpr int LDS = AT_EPI + EPI > NW * GRAD_WAVE ? AT_EPI + EPI : NW * GRAD_WAVE;
+  static constexpr int PER_CU = E == 256 ? 1 : 2, GROUPS = 256 * PER_CU;   // workgroups that run at a time
+  static_assert(PER_CU * LDS <= 160 * 1024 && LOADS * NW * 1024 == STAGE && (STAGE & (STAGE - 1)) == 0, "LDS");
+  typedef f32x4 Acc[NA][NB];
+};
+static_assert(STAGES == 2 && BK == 64 && CPR == 8 && NT == 512, "the loads and reads below");
 
 __host__ __device__ inline int stages_of(const HeadProduct& g) { return (int)((g.k + BK - 1) / BK); }
 
@@ -74,20 +92,22 @@ __device__ __forceinline__ TileAt tile_at(int b, int tiles_m, int tiles_n, int s
   return {first + t % rows, t / rows, split};
 }
 
-// One operand's loads: 32 of 1 KB a stage, four of them this wave's.
+// One operand's loads of 1 KB each: this wave's.
+template <int E>
 struct Loader {
+  static constexpr int N = Shape<E>::LOADS / 2;
   const uint16_t* base;   // the tile's first row in plane 0
-  uint32_t voff[LOADS / 2];
+  uint32_t voff[N];
   int64_t plane, step;
 
   __device__ __forceinline__ void init(const HeadSide& s, int tile, int wave, int lane) {
     plane = s.plane;
     step = s.step;
-    base = s.p + tile * s.tile;
-    const int64_t row0 = (int64_t)tile * HEAD_TILE;
-    const int last = (int)(s.rows - 1 - row0 < 255 ? s.rows - 1 - row0 : 255);   // rows past the end repeat the last one
+    const int64_t row0 = (int64_t)tile * E;
+    base = s.p + row0 / HEAD_TILE * s.tile + row0 % HEAD_TILE * s.ld;
+    const int last = (int)(s.rows - 1 - row0 < E - 1 ? s.rows - 1 - row0 : E - 1);   // rows past the end repeat the last one
 #pragma unroll
-    for (int q = 0; q < LOADS / 2; ++q) {
+    for (int q = 0; q < N; ++q) {
       const int r = (wave + q * NW) * 8 + lane / CPR;
       const int c = (lane % CPR) ^ ((r / G::RPP) % CPR);
       voff[q] = ((uint32_t)(r < last ? r : last) * (uint32_t)s.ld + c * 8) * 2;
@@ -103,12 +123,14 @@ struct Loader {
 // run() does the rest.
 // acc[a][b][e] = C(row0 + wr TM + 16 b + lane % 16, col0 + wc TN + 16 a + 4 (lane / 16) + e).
 // HALVES: the planes are float16.
-template <bool HALVES>
+template <bool HALVES, int E>
 struct Product {
+  typedef Shape<E> S;
+  static constexpr int NA = S::NA, NB = S::NB, LOADS = S::LOADS;
   const HeadProduct& g;
   char* const lds;
   const int lane, wave;
-  Loader la, lb;
+  Loader<E> la, lb;
   int kt0, KT;   // stages of the contraction, for each pair of planes
   // The next stage to load: its pair of planes, how many stages of that are left, where they lie.
   int pair, left;
@@ -123,7 +145,7 @@ struct Product {
   }
   __device__ __forceinline__ void issue(int q) const {
     if (q < LOADS / 2) dma16(rsrc(at_a), la.voff[q], 0u, at_lds + q * NW * 1024);
-    else dma16(rsrc(at_b), lb.voff[q - LOADS / 2], 0u, at_lds + G::OPER_BYTES + (q - LOADS / 2) * NW * 1024);
+    else dma16(rsrc(at_b), lb.voff[q - LOADS / 2], 0u, at_lds + S::OPER + (q - LOADS / 2) * NW * 1024);
   }
   __device__ __forceinline__ void start_pair() {
     at_a = la.at((int)(g.pair_a >> (4 * pair)) & 15, kt0);
@@ -134,7 +156,7 @@ struct Product {
   __device__ __forceinline__ void advance() {
     at_a += 2 * la.step;
     at_b += 2 * lb.step;
-    at_lds ^= G::STAGE_BYTES;
+    at_lds ^= S::STAGE;
     if (--left == 0) {
       ++pair;
       start_pair();
@@ -168,14 +190,14 @@ struct Product {
   // Two stages of loads: at the barrier that closes stage st, stage st + 1 has arrived and every wave is
   // done with the slot of stage st, which then receives stage st + 2; half of its loads go out at
   // once, half from among the products that follow.  Fragments are read one sub-step ahead.
-  __device__ __forceinline__ void run(f32x4 (&acc)[NA][NB]) {
+  __device__ __forceinline__ void run(typename S::Acc& acc) {
     const int wr = wave / (NW / 2), wc = wave % (NW / 2);
     // Block b's fragment lies 16 b rows below block 0's: 16 rows keep the swizzle's phase.
     int oa[H], ob[H];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-      oa[h] = G::swz_rk(wr * TM + (lane & 15), 4 * h + (lane >> 4));
-      ob[h] = G::OPER_BYTES + G::swz_rk(wc * TN + (lane & 15), 4 * h + (lane >> 4));
+      oa[h] = G::swz_rk(wr * S::TM + (lane & 15), 4 * h + (lane >> 4));
+      ob[h] = S::OPER + G::swz_rk(wc * S::TN + (lane & 15), 4 * h + (lane >> 4));
     }
 #pragma unroll
     for (int a = 0; a < NA; ++a)
@@ -195,7 +217,7 @@ struct Product {
     read(0, lds, 0);
     auto stage = [&](const int st, auto steady_tag) {
       constexpr bool steady = decltype(steady_tag)::value;   // stage st + 2 exists
-      const char* const slot = lds + (st & 1) * G::STAGE_BYTES;
+      const char* const slot = lds + (st & 1) * S::STAGE;
 #pragma unroll
       for (int h = 0; h < H; ++h) {
         const int c = h & 1;
@@ -210,7 +232,7 @@ struct Product {
 #pragma unroll
             for (int q = LOADS / 2; q < LOADS; ++q) issue(q);
           }
-          read(c ^ 1, lds + ((st + 1) & 1) * G::STAGE_BYTES, 0);
+          read(c ^ 1, lds + ((st + 1) & 1) * S::STAGE, 0);
         }
 #pragma unroll
         for (int a = 0; a < NA; ++a)
@@ -262,6 +284,7 @@ __device__ __forceinline__ op_u32x2 turn_quad(uint2 v, uint32_t pick, bool low) 
 }
 
 // The scales of this lane's columns into its logits.
+template <int NA, int NB>
 __device__ __forceinline__ void scale_columns(const float* scales, int c, int g, f32x4 (&acc)[NA][NB]) {
   f32x4 w[NA];
 #pragma unroll
@@ -290,39 +313,41 @@ __device__ __forceinline__ int label_of(const HeadLabels& l, int64_t r, int64_t 
 
 // A workgroup takes every 32nd tile of its XCD's.  While a tile's sums are formed in registers,
 // the next one's first stages arrive.
-template <bool HALVES>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
+template <bool HALVES, int E>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE * Shape<E>::PER_CU, WPE * Shape<E>::PER_CU)))
 void head_first_kernel(HeadLogits a) {
+  typedef Shape<E> S;
+  constexpr int TM = S::TM, TN = S::TN, NA = S::NA, NB = S::NB;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   int block = blockIdx.x;
   TileAt t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
   if (t.i < 0) return;
-  Product<HALVES> product(a.g, lds);
+  Product<HALVES, E> product(a.g, lds);
   const int lane = product.lane, wave = product.wave, wr = wave / (NW / 2), wc = wave % (NW / 2), g = lane >> 4;
   const int KT = stages_of(a.g);
   product.prime(t.i, t.j, 0, KT);
-  int* const labels = reinterpret_cast<int*>(lds + AT_ROWS);   // [2][row]
+  int* const labels = reinterpret_cast<int*>(lds + S::AT_ROWS);   // [2][row]
   auto row_label = [&](int i) {
-    const int64_t m = (int64_t)i * HEAD_TILE + threadIdx.x;
-    return threadIdx.x < HEAD_TILE && m < a.g.m ? label_of(a.rows, m, a.vocab) : -1;
+    const int64_t m = (int64_t)i * E + threadIdx.x;
+    return threadIdx.x < E && m < a.g.m ? label_of(a.rows, m, a.vocab) : -1;
   };
-  float* const scales = reinterpret_cast<float*>(lds + AT_SCALES);   // [2][row]
-  auto row_scale = [&](int i) { return HALVES ? gptr(a.x_scales)[(int64_t)i * HEAD_TILE + threadIdx.x % HEAD_TILE] : 1.f; };
+  float* const scales = reinterpret_cast<float*>(lds + S::AT_SCALES);   // [2][row]
+  auto row_scale = [&](int i) { return HALVES ? gptr(a.x_scales)[(int64_t)i * E + threadIdx.x % E] : 1.f; };
   int own = row_label(t.i), turn = 0;
   float own_scale = row_scale(t.i);
   product.arrived();
-  malt_f32x2* const join = reinterpret_cast<malt_f32x2*>(lds + AT_EPI);   // [row][wave column]
+  malt_f32x2* const join = reinterpret_cast<malt_f32x2*>(lds + S::AT_EPI);   // [row][wave column]
   for (;;) {
-    const int64_t row0 = (int64_t)t.i * HEAD_TILE, col0 = (int64_t)t.j * HEAD_TILE;
+    const int64_t row0 = (int64_t)t.i * E, col0 = (int64_t)t.j * E;
     const int tile_n = t.j;
-    if (threadIdx.x < HEAD_TILE) {
-      labels[turn * HEAD_TILE + threadIdx.x] = own;
-      if (HALVES) scales[turn * HEAD_TILE + threadIdx.x] = own_scale;
+    if (threadIdx.x < E) {
+      labels[turn * E + threadIdx.x] = own;
+      if (HALVES) scales[turn * E + threadIdx.x] = own_scale;
     }
-    f32x4 acc[NA][NB];
+    typename S::Acc acc;
     product.run(acc);
     lds_free();
-    block += CUS;
+    block += gridDim.x;
     t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
     if (t.i >= 0) {
       product.prime(t.i, t.j, 0, KT);
@@ -336,8 +361,8 @@ void head_first_kernel(HeadLogits a) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       if (b % 4 == 0 && 16 * b >= rows) break;
-      const int ml = wr * TM + b * 16 + (lane & 15), yl = labels[turn * HEAD_TILE + ml] - c;   // the label's place in the wave's columns
-      const float unit = HALVES ? scales[turn * HEAD_TILE + ml] * LOG2E : LOG2E;
+      const int ml = wr * TM + b * 16 + (lane & 15), yl = labels[turn * E + ml] - c;   // the label's place in the wave's columns
+      const float unit = HALVES ? scales[turn * E + ml] * LOG2E : LOG2E;
       if (__builtin_amdgcn_ballot_w64((unsigned)yl < TN)) {   // few waves meet a label
         float z = 0.f;
 #pragma unroll
@@ -374,7 +399,7 @@ void head_first_kernel(HeadLogits a) {
     product.arrived();
     lds_free();
     const int64_t m = row0 + threadIdx.x;
-    if (threadIdx.x < HEAD_TILE && m < a.g.m) {
+    if (threadIdx.x < E && m < a.g.m) {
       float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
       for (int i = 0; i < NW / 2; ++i) top = fmaxf(top, join[threadIdx.x * (NW / 2) + i].x);
@@ -391,42 +416,44 @@ void head_first_kernel(HeadLogits a) {
   }
 }
 
-template <bool HALVES>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
+template <bool HALVES, int E>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE * Shape<E>::PER_CU, WPE * Shape<E>::PER_CU)))
 void head_second_kernel(HeadLogits a) {
+  typedef Shape<E> S;
+  constexpr int TM = S::TM, TN = S::TN, NA = S::NA, NB = S::NB;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   int block = blockIdx.x;
   TileAt t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
   if (t.i < 0) return;
-  Product<HALVES> product(a.g, lds);
+  Product<HALVES, E> product(a.g, lds);
   const int lane = product.lane, wave = product.wave, wr = wave / (NW / 2), wc = wave % (NW / 2), g = lane >> 4;
   const int KT = stages_of(a.g);
   product.prime(t.i, t.j, 0, KT);
-  f32x4* const records = reinterpret_cast<f32x4*>(lds + AT_ROWS);   // [2][row]
+  f32x4* const records = reinterpret_cast<f32x4*>(lds + S::AT_ROWS);   // [2][row]
   auto record = [&](int i) {
     return *reinterpret_cast<const MALT_GLOBAL f32x4*>(
-        gptr(reinterpret_cast<const float*>(a.records + (int64_t)i * HEAD_TILE + threadIdx.x % HEAD_TILE)));
+        gptr(reinterpret_cast<const float*>(a.records + (int64_t)i * E + threadIdx.x % E)));
   };
-  float* const scales = reinterpret_cast<float*>(lds + AT_SCALES);   // [2][row]
-  auto row_scale = [&](int i) { return HALVES ? gptr(a.x_scales)[(int64_t)i * HEAD_TILE + threadIdx.x % HEAD_TILE] : 1.f; };
+  float* const scales = reinterpret_cast<float*>(lds + S::AT_SCALES);   // [2][row]
+  auto row_scale = [&](int i) { return HALVES ? gptr(a.x_scales)[(int64_t)i * E + threadIdx.x % E] : 1.f; };
   f32x4 own = record(t.i);
   float own_scale = row_scale(t.i);
   int turn = 0;
   product.arrived();
-  char* const sto = lds + AT_EPI + wave * OUT_WAVE;
+  char* const sto = lds + S::AT_EPI + wave * S::OUT_WAVE;
   const uint32_t pick = turn_pick(lane);
   const bool low = (lane & 3) < 2;
   for (;;) {
-    const int64_t col0 = (int64_t)t.j * HEAD_TILE;
+    const int64_t col0 = (int64_t)t.j * E;
     const int tile_m = t.i, tile_n = t.j;
-    if (threadIdx.x < HEAD_TILE) {
-      records[turn * HEAD_TILE + threadIdx.x] = own;
-      if (HALVES) scales[turn * HEAD_TILE + threadIdx.x] = own_scale;
+    if (threadIdx.x < E) {
+      records[turn * E + threadIdx.x] = own;
+      if (HALVES) scales[turn * E + threadIdx.x] = own_scale;
     }
-    f32x4 acc[NA][NB];
+    typename S::Acc acc;
     product.run(acc);
     lds_free();
-    block += CUS;
+    block += gridDim.x;
     t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
     if (t.i >= 0) {
       product.prime(t.i, t.j, 0, KT);
@@ -436,14 +463,14 @@ void head_second_kernel(HeadLogits a) {
     const int c = (int)col0 + wc * TN, left = a.g.n - c - 4 * g;
     const bool end = a.g.n - c < TN;
     // This wave's rows, to the end of the last stage that the gradients read.
-    const int rows = (a.g.m - tile_m * HEAD_TILE + BK - 1) / BK * BK - wr * TM;
+    const int rows = (a.g.m - tile_m * E + BK - 1) / BK * BK - wr * TM;
     if constexpr (HALVES) scale_columns(a.w_scales, c, g, acc);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       if (b % 4 == 0 && 16 * b >= rows) break;
       const int ml = wr * TM + b * 16 + (lane & 15);
-      const f32x4 s = records[turn * HEAD_TILE + ml];
-      const float unit = HALVES ? scales[turn * HEAD_TILE + ml] * LOG2E : LOG2E;
+      const f32x4 s = records[turn * E + ml];
+      const float unit = HALVES ? scales[turn * E + ml] * LOG2E : LOG2E;
       const int y = __float_as_int(s.w), yl = y < 0 ? -1 : y - (int)a.col0 - c;
 #pragma unroll
       for (int i = 0; i < NA; ++i)
@@ -493,10 +520,11 @@ void head_second_kernel(HeadLogits a) {
             acc[i][b][3] -= bf16_hi(pk[i].y);
           }
         }
+        const int row = tile_m * E + wr * TM + 16 * b, col = tile_n * E + wc * TN;   // the first ones
         if (a.dz_t) {
           // Lane p of a quad takes column p of its four rows.
-          bf16_t* const out = a.dz_t + p * a.dz_plane + tile_n * a.dz_t_tile + (tile_m * 4 + wr * 2 + b / 4) * HEAD_BLOCK +
-                              (wc * TN + 4 * g + (lane & 3)) * BK + b % 4 * 16 + (lane & 12);
+          bf16_t* const out = a.dz_t + p * a.dz_plane + col / HEAD_TILE * a.dz_t_tile + row / BK * HEAD_BLOCK +
+                              (col % HEAD_TILE + 4 * g + (lane & 3)) * BK + row % BK + (lane & 12);
 #pragma unroll
           for (int i = 0; i < NA; ++i) {
             *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(out) + 16 * i * BK) = turn_quad(pk[i], pick, low);
@@ -504,15 +532,16 @@ void head_second_kernel(HeadLogits a) {
         }
         if (a.dz) {
 #pragma unroll
-          for (int i = 0; i < NA; ++i) *reinterpret_cast<uint2*>(sto + (lane & 15) * OUT_PITCH + (4 * g + i * 16) * 2) = pk[i];
+          for (int i = 0; i < NA; ++i) *reinterpret_cast<uint2*>(sto + (lane & 15) * S::OUT_PITCH + (4 * g + i * 16) * 2) = pk[i];
           // The wave's own region: its LDS instructions run in order.
           asm volatile("" ::: "memory");
           __builtin_amdgcn_wave_barrier();
-          bf16_t* const dz = a.dz + p * a.dz_plane + tile_m * a.dz_tile + (tile_n * 4 + wc) * HEAD_BLOCK + (wr * TM + b * 16) * BK;
+          bf16_t* const dz = a.dz + p * a.dz_plane + row / HEAD_TILE * a.dz_tile + col / BK * HEAD_BLOCK + row % HEAD_TILE * BK + col % BK;
+          constexpr int CHUNKS = TN / 8, ROWS = 64 / CHUNKS;   // 16 bytes each; rows a store covers
 #pragma unroll
-          for (int it = 0; it < 2; ++it) {
-            const int r = lane / 8 + 8 * it, ch = lane % 8;
-            const char* src = sto + r * OUT_PITCH + ch * 16;
+          for (int it = 0; it < 16 / ROWS; ++it) {
+            const int r = lane / CHUNKS + ROWS * it, ch = lane % CHUNKS;
+            const char* src = sto + r * S::OUT_PITCH + ch * 16;
             const uint2 lo = *reinterpret_cast<const uint2*>(src);
             const uint2 hi = *reinterpret_cast<const uint2*>(src + 8);
             const u32x4 v = {lo.x, lo.y, hi.x, hi.y};
@@ -548,18 +577,18 @@ __device__ __forceinline__ bool row_without(const HeadOut& o, const HeadGrads& a
 }
 __device__ __forceinline__ float scale_of(const HeadGrads& a) { return a.scale_at ? a.scale * gptr(a.scale_at)[0] : a.scale; }
 
-// A wave's sub-tile leaves through its own part of LDS, half of its columns at a time, so that a
+// A wave's sub-tile leaves through its own part of LDS, 32 of its columns at a time, so that a
 // store covers eight rows' 128 bytes, and in a loop: straight from the registers it is 30 KB of code,
 // run once a tile.
-constexpr int GRAD_PITCH = TN / 2 * 4 + 16, GRAD_WAVE = TM * GRAD_PITCH;
-static_assert(NW * GRAD_WAVE <= LDS_BYTES, "LDS budget");
-template <class T>
+template <class T, int E>
 __device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, int split, int64_t row0, int64_t col0, char* lds,
-                                          const f32x4 (&acc)[NA][NB]) {
+                                          const typename Shape<E>::Acc& acc) {
+  typedef Shape<E> S;
+  constexpr int TM = S::TM, TN = S::TN, NB = S::NB;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave / (NW / 2), wc = wave % (NW / 2);
   const float scale = scale_of(a);
-  char* const own = lds + wave * GRAD_WAVE;
+  char* const own = lds + wave * S::GRAD_WAVE;
   const int64_t m0 = row0 + wr * TM + (lane >> 3);
   const int rows = (int)(o.g.m - m0);   // there are, from this lane's first
   uint32_t none = 0;                    // bit i: row 8 i has no gradient
@@ -568,25 +597,25 @@ __device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, 
     for (int i = 0; i < TM / 8; ++i) none |= (8 * i < rows && row_without(o, a, m0 + 8 * i) ? 1u : 0u) << i;
   }
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
+  for (int slice = 0; slice < TN / 32; ++slice) {
     // The wave's LDS instructions run in order.
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 0; i < NA / 2; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        *reinterpret_cast<f32x4*>(own + (16 * b + (lane & 15)) * GRAD_PITCH + (16 * i + 4 * (lane >> 4)) * 4) = acc[half * (NA / 2) + i][b];
+        *reinterpret_cast<f32x4*>(own + (16 * b + (lane & 15)) * S::GRAD_PITCH + (16 * i + 4 * (lane >> 4)) * 4) = acc[2 * slice + i][b];
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
-    const int64_t n = col0 + wc * TN + half * (TN / 2) + 4 * (lane & 7);
+    const int64_t n = col0 + wc * TN + 32 * slice + 4 * (lane & 7);
     if (n >= o.g.n) continue;
-    const char* from = own + (lane >> 3) * GRAD_PITCH + (lane & 7) * 16;
+    const char* from = own + (lane >> 3) * S::GRAD_PITCH + (lane & 7) * 16;
     const int width = (int)(o.g.n - n);   // columns there are from this lane's first
     float* part = o.partial + ((int64_t)split * o.g.m + m0) * o.g.n + n;
     T* out = static_cast<T*>(o.out) + m0 * o.ldo + n;
 #pragma unroll 4
-    for (int i = 0; i < TM / 8; ++i, from += 8 * GRAD_PITCH, part += 8 * (int64_t)o.g.n, out += 8 * o.ldo) {
+    for (int i = 0; i < TM / 8; ++i, from += 8 * S::GRAD_PITCH, part += 8 * (int64_t)o.g.n, out += 8 * o.ldo) {
       if (8 * i >= rows) break;
       const f32x4 x = *reinterpret_cast<const f32x4*>(from);
       op_f32x4 v = {x.x, x.y, x.z, x.w};
@@ -603,7 +632,8 @@ __device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, 
 
 }  // namespace
 
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
+template <int E>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE * Shape<E>::PER_CU, WPE * Shape<E>::PER_CU)))
 void head_grads_kernel(HeadGrads a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   int b = blockIdx.x, which = 0;
@@ -616,16 +646,16 @@ void head_grads_kernel(HeadGrads a) {
   const TileAt t = tile_at(b, o.g.tiles_m, o.g.tiles_n, o.splits);
   if (t.i < 0) return;
   const int split = t.split;
-  const int64_t row0 = (int64_t)t.i * HEAD_TILE, col0 = (int64_t)t.j * HEAD_TILE;
+  const int64_t row0 = (int64_t)t.i * E, col0 = (int64_t)t.j * E;
   const int KT = stages_of(o.g), kt0 = (int)((int64_t)KT * split / o.splits), kt1 = (int)((int64_t)KT * (split + 1) / o.splits);
-  f32x4 acc[NA][NB];
-  Product<false> product(o.g, lds);
+  typename Shape<E>::Acc acc;
+  Product<false, E> product(o.g, lds);
   product.prime(t.i, t.j, kt0, kt1 - kt0);
   product.arrived();
   product.run(acc);
   lds_free();
-  if (o.f32) write_out<float>(o, a, split, row0, col0, lds, acc);
-  else write_out<bf16_t>(o, a, split, row0, col0, lds, acc);
+  if (o.f32) write_out<float, E>(o, a, split, row0, col0, lds, acc);
+  else write_out<bf16_t, E>(o, a, split, row0, col0, lds, acc);
 }
 
 // The sums of contractions' parts, four columns a thread: one result's, then the other's.  Of many parts
@@ -676,30 +706,44 @@ hipError_t head_setup() {
   if (e != hipSuccess) return e;
   const uint64_t bit = uint64_t(1) << (dev & 63);
   if (dev <= 63 && raised.load(std::memory_order_relaxed) & bit) return hipSuccess;
-  for (const void* f : {reinterpret_cast<const void*>(&head_first_kernel<false>), reinterpret_cast<const void*>(&head_first_kernel<true>),
-                        reinterpret_cast<const void*>(&head_second_kernel<false>), reinterpret_cast<const void*>(&head_second_kernel<true>),
-                        reinterpret_cast<const void*>(&head_grads_kernel)}) {
-    e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
+  struct { const void* kernel; int bytes; } const all[] = {
+      {reinterpret_cast<const void*>(&head_first_kernel<false, 256>), Shape<256>::LDS}, {reinterpret_cast<const void*>(&head_first_kernel<true, 256>), Shape<256>::LDS},
+      {reinterpret_cast<const void*>(&head_second_kernel<false, 256>), Shape<256>::LDS}, {reinterpret_cast<const void*>(&head_second_kernel<true, 256>), Shape<256>::LDS},
+      {reinterpret_cast<const void*>(&head_grads_kernel<256>), Shape<256>::LDS},
+      {reinterpret_cast<const void*>(&head_first_kernel<false, 128>), Shape<128>::LDS}, {reinterpret_cast<const void*>(&head_first_kernel<true, 128>), Shape<128>::LDS},
+      {reinterpret_cast<const void*>(&head_second_kernel<false, 128>), Shape<128>::LDS}, {reinterpret_cast<const void*>(&head_second_kernel<true, 128>), Shape<128>::LDS},
+      {reinterpret_cast<const void*>(&head_grads_kernel<128>), Shape<128>::LDS}};
+  for (const auto& f : all) {
+    e = hipFuncSetAttribute(f.kernel, hipFuncAttributeMaxDynamicSharedMemorySize, f.bytes);
     if (e != hipSuccess) return e;
   }
   if (dev <= 63) raised.fetch_or(bit, std::memory_order_relaxed);
   return hipSuccess;
 }
 
-hipError_t launch_head_logits(const HeadLogits& a, bool second, hipStream_t s) {
+namespace {
+template <int E>
+void logits_of(const HeadLogits& a, bool second, hipStream_t s) {
   const int blocks = tile_blocks(a.g.tiles_m, a.g.tiles_n, 1);
-  const dim3 grid((unsigned)(blocks < CUS ? blocks : CUS));
-  if (second && a.x_scales) hipLaunchKernelGGL(head_second_kernel<true>, grid, dim3(NT), LDS_BYTES, s, a);
-  else if (second) hipLaunchKernelGGL(head_second_kernel<false>, grid, dim3(NT), LDS_BYTES, s, a);
-  else if (a.x_scales) hipLaunchKernelGGL(head_first_kernel<true>, grid, dim3(NT), LDS_BYTES, s, a);
-  else hipLaunchKernelGGL(head_first_kernel<false>, grid, dim3(NT), LDS_BYTES, s, a);
+  const dim3 grid((unsigned)(blocks < Shape<E>::GROUPS ? blocks : Shape<E>::GROUPS));
+  if (second && a.x_scales) hipLaunchKernelGGL((head_second_kernel<true, E>), grid, dim3(NT), Shape<E>::LDS, s, a);
+  else if (second) hipLaunchKernelGGL((head_second_kernel<false, E>), grid, dim3(NT), Shape<E>::LDS, s, a);
+  else if (a.x_scales) hipLaunchKernelGGL((head_first_kernel<true, E>), grid, dim3(NT), Shape<E>::LDS, s, a);
+  else hipLaunchKernelGGL((head_first_kernel<false, E>), grid, dim3(NT), Shape<E>::LDS, s, a);
+}
+}  // namespace
+
+hipError_t launch_head_logits(const HeadLogits& a, int edge, bool second, hipStream_t s) {
+  if (edge == 256) logits_of<256>(a, second, s);
+  else logits_of<128>(a, second, s);
   return hipGetLastError();
 }
 
-hipError_t launch_head_grads(const HeadGrads& a, hipStream_t s) {
+hipError_t launch_head_grads(const HeadGrads& a, int edge, hipStream_t s) {
   int blocks = 0;
   for (int i = 0; i < a.parts; ++i) blocks += tile_blocks(a.part[i].g.tiles_m, a.part[i].g.tiles_n, a.part[i].splits);
-  hipLaunchKernelGGL(head_grads_kernel, dim3((unsigned)blocks), dim3(NT), LDS_BYTES, s, a);
+  if (edge == 256) hipLaunchKernelGGL(head_grads_kernel<256>, dim3((unsigned)blocks), dim3(NT), Shape<256>::LDS, s, a);
+  else hipLaunchKernelGGL(head_grads_kernel<128>, dim3((unsigned)blocks), dim3(NT), Shape<128>::LDS, s, a);
   return hipGetLastError();
 }
 

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <new>
+#include <numeric>
 #include <vector>
 
 #include "adamw.h"
@@ -94,6 +95,7 @@ struct HeadPlan {
   int64_t rows_pad, cols_pad, vocab_pad;
   int64_t piece;         // vocabulary columns of a piece, a multiple of the tile
   int pieces;
+  int first_edge, second_edge, grad_edge;   // of the tiles
   int parts;             // of a row's statistics
   int dx_splits, dw_splits;   // parts of the gradients' contractions
   size_t partial, at_label, records, x, w, x_scales, w_scales, x_t, w_t, dz, dz_t, dx, dw, bytes;
@@ -116,6 +118,15 @@ int head_pair_count(int na, int nb, int planes) {
   HeadProduct g;
   head_pairs(g, na, nb, planes);
   return g.pairs;
+}
+
+// The tiles' edge of a pass over rows x cols logits, from what tiles take.  A CU runs one tile of 256 at a time, 1.43 us
+// a stage, or two of 128, 0.78; `big` and `small`: what is done after the stages, in us.  us, tiles of 128 | 256:
+//   first pass   300 x 1000 x 64 6 | 11, 512 x 50257 x 768 45 | 52, 8192 x 50257 x 768 659 | 622
+//   second       300 x 1000 x 64 10 | 26, 2000 x 12000 x 768 54 | 62, 8192 x 50257 x 1280 762 | 660 (half of it)
+int head_edge(int64_t rows, int64_t cols, int64_t stages, double big, double small) {
+  auto rounds = [&](int64_t e) { return double((up(rows, e) / e * (up(cols, e) / e) + 255) / 256); };
+  return 0.5 * rounds(128) * (0.78 * double(stages) + small) < rounds(256) * (1.43 * double(stages) + big) ? 128 : 256;
 }
 
 HeadPlan head_plan(const malt_linear_loss_t& a) {
@@ -146,7 +157,9 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     end += align256(bytes);
     return at;
   };
-  L.parts = L.few ? head_few_parts(a.vocab, a.inner) : int(up(a.vocab, HEAD_TILE) / HEAD_TILE);
+  const int64_t stages = L.cols_pad / HEAD_BK * head_pair_count(L.x_halves, L.w_halves, HEAD_HALVES);
+  L.first_edge = head_edge(a.rows, a.vocab, stages, 8.5, 3.8);
+  L.parts = L.few ? head_few_parts(a.vocab, a.inner) : int(up(a.vocab, L.first_edge) / L.first_edge);
   if (!a.stats_given) {
     L.partial = take(size_t(a.rows) * L.parts * 8);
     L.at_label = take(size_t(a.rows) * 4);
@@ -166,6 +179,9 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     if (most < HEAD_TILE) most = HEAD_TILE;
     const int64_t pieces = (all + most - 1) / most;
     L.piece = up((all + pieces - 1) / pieces, HEAD_TILE);
+    // Whole rounds of 256 CUs before the last piece's (8192 rows x 50257: 13 and 12 instead of 13 and 13).
+    const int64_t whole = 256 / std::gcd(L.rows_pad / HEAD_TILE, int64_t(256)) * HEAD_TILE;
+    if (pieces > 1 && up(L.piece, whole) <= most) L.piece = up(L.piece, whole);
     L.pieces = int((all + L.piece - 1) / L.piece);
     L.records = take(size_t(L.rows_pad) * sizeof(HeadRow));
     L.vocab_pad = L.piece * L.pieces;
@@ -179,12 +195,18 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     }
     // A product of few tiles and a long contraction is cut into parts, so that no workgroup has more
     // stages than a CU's share of them all, and 16 at the least (a part costs its tile in float32, written and read).
-    const int64_t across = up(a.inner, HEAD_TILE) / HEAD_TILE;
-    const int64_t dx_tiles = a.dx ? L.rows_pad / HEAD_TILE * across : 0, dw_tiles = a.dweight ? L.piece / HEAD_TILE * across : 0;
     const int64_t dx_stages = L.piece / HEAD_BK * head_pair_count(L.dx_z, L.dx_w, x32 ? HEAD_PLANES : 2);
     const int64_t dw_stages = up(a.rows, HEAD_BK) / HEAD_BK *
                               head_pair_count(L.dw_z, L.dw_x, dw32 ? HEAD_PLANES : 2);
-    int64_t share = (dx_tiles * dx_stages + dw_tiles * dw_stages) / 256;
+    L.second_edge = head_edge(a.rows, std::min(L.piece, a.vocab), stages, 4 + 20 * L.dz_planes, 4 + 12 * L.dz_planes);
+    // Of the gradients: by their stages of 256-tiles on each of 256 CUs.  us, tiles of 128 | 256: 500 x 2000 x 2000 (below 36) 24 | 35,
+    // 2000 x 12000 x 768 (35) 83 | 101, 512 x 50257 x 768 (37) 119 | 119, 400 x 30000 x 1024 in float32 (165) 401 | 330.
+    const int64_t wide = up(a.inner, HEAD_TILE) / HEAD_TILE;
+    const int64_t work = wide * ((a.dx ? L.rows_pad / HEAD_TILE * dx_stages : 0) + (a.dweight ? L.piece / HEAD_TILE * dw_stages : 0));
+    L.grad_edge = work <= 36 * 256 ? 128 : 256;
+    const int64_t across = up(a.inner, L.grad_edge) / L.grad_edge;
+    const int64_t dx_tiles = a.dx ? up(a.rows, L.grad_edge) / L.grad_edge * across : 0, dw_tiles = a.dweight ? L.piece / L.grad_edge * across : 0;
+    int64_t share = (dx_tiles * dx_stages + dw_tiles * dw_stages) / (L.grad_edge == 256 ? 256 : 512);
     if (share < 16) share = 16;
     auto parts = [&](int64_t stages, int64_t contraction) {
       int64_t n = (stages + share - 1) / share;
@@ -549,7 +571,6 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
   z.g.b = wside;
   z.g.m = (int32_t)a.rows;
   z.g.k = L.cols_pad;
-  z.g.tiles_m = int(L.rows_pad / HEAD_TILE);
   head_pairs(z.g, L.x_halves, L.w_halves, HEAD_HALVES);
   if (L.halves) {
     z.x_scales = prepare.scales[0];
@@ -579,11 +600,12 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
     } else {
       HeadLogits first = z;
       first.g.n = (int32_t)a.vocab;
-      first.g.tiles_n = int(up(a.vocab, HEAD_TILE) / HEAD_TILE);
+      first.g.tiles_m = int(up(a.rows, L.first_edge) / L.first_edge);
+      first.g.tiles_n = int(up(a.vocab, L.first_edge) / L.first_edge);
       first.partial = partial;
       first.at_label = at_label;
       first.parts = L.parts;
-      MALT_TRY(launched(launch_head_logits(first, false, s), "launching the head's logits"));
+      MALT_TRY(launched(launch_head_logits(first, L.first_edge, false, s), "launching the head's logits"));
     }
     const HeadJoin join = {labels, a.rows, L.rows_pad, a.vocab, partial, L.parts, at_label, reinterpret_cast<HeadRow*>(a.stats),
                            L.grads ? records : nullptr, a.losses};
@@ -606,7 +628,8 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       second.g.b.p += v0 / HEAD_TILE * wside.tile;
       second.g.b.rows -= v0;
       second.g.n = (int32_t)n;
-      second.g.tiles_n = int(up(n, HEAD_TILE) / HEAD_TILE);
+      second.g.tiles_m = int(up(a.rows, L.second_edge) / L.second_edge);
+      second.g.tiles_n = int(up(n, L.second_edge) / L.second_edge);
       second.col0 = v0;
       if (L.halves) second.w_scales += v0;
       second.dz = a.dx ? dz : nullptr;
@@ -615,7 +638,7 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       second.dz_tile = L.piece / HEAD_BK * HEAD_BLOCK;
       second.dz_t_tile = L.rows_pad / HEAD_BK * HEAD_BLOCK;
       second.dz_planes = L.dz_planes;
-      MALT_TRY(launched(launch_head_logits(second, true, s), "launching the logits' gradient"));
+      MALT_TRY(launched(launch_head_logits(second, L.second_edge, true, s), "launching the logits' gradient"));
     }
     gr.parts = 0;
     if (want_dx) {
@@ -627,8 +650,8 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       o.g.m = (int32_t)a.rows;
       o.g.n = (int32_t)a.inner;
       o.g.k = n;
-      o.g.tiles_m = int(L.rows_pad / HEAD_TILE);
-      o.g.tiles_n = int(up(a.inner, HEAD_TILE) / HEAD_TILE);
+      o.g.tiles_m = int(up(a.rows, L.grad_edge) / L.grad_edge);
+      o.g.tiles_n = int(up(a.inner, L.grad_edge) / L.grad_edge);
       head_pairs(o.g, L.dx_z, L.dx_w, f32x ? HEAD_PLANES : 2);
       o.out = a.dx;
       o.ldo = a.lddx;
@@ -648,8 +671,8 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       o.g.m = (int32_t)n;
       o.g.n = (int32_t)a.inner;
       o.g.k = a.rows;
-      o.g.tiles_m = int(up(n, HEAD_TILE) / HEAD_TILE);
-      o.g.tiles_n = int(up(a.inner, HEAD_TILE) / HEAD_TILE);
+      o.g.tiles_m = int(up(n, L.grad_edge) / L.grad_edge);
+      o.g.tiles_n = int(up(a.inner, L.grad_edge) / L.grad_edge);
       head_pairs(o.g, L.dw_z, L.dw_x, fine ? HEAD_PLANES : 2);
       o.out = static_cast<char*>(a.dweight) + v0 * a.lddw * op_dtype_bytes(a.dweight_type);
       o.ldo = a.lddw;
@@ -659,7 +682,7 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       o.f32 = fine;
       o.accumulate = a.accumulate != 0;
     }
-    MALT_TRY(launched(launch_head_grads(gr, s), "launching the head's gradients"));
+    MALT_TRY(launched(launch_head_grads(gr, L.grad_edge, s), "launching the head's gradients"));
     bool sums[2] = {false, false};
     for (int i = 0; i < gr.parts; ++i) sums[i] = gr.part[i].splits > 1 && (!gr.part[i].mask_rows || p + 1 == L.pieces);
     MALT_TRY(launched(launch_head_sum(gr, sums[0], sums[1], s), "joining the head's gradients"));

@@ -6,6 +6,9 @@
 //
 // Bound by memory: a row is read once, held in registers for its sum and its output, and
 // x, residual, sum and y (h, dy, dsum and dx) pass through memory once each.
+// 8192 x 1280 in bf16, 84 MB each way: 18 us (4.7 TB/s), the gradient 27 (3.1 TB/s) and 4 for the join
+// of the weight's.  The gradient waits for a row's sum before it can write and holds the weight's columns besides; the
+// next row's loads ahead of that took 27 to 29.  One row: 3.5 us; 1024 rows of 1280 into 8 bits 5.8.
 //
 // The sum of squares is in 64 bits: squares of float32 numbers are exact there, and the order
 // of summation changes r's last of 24 bits in one row of 10^8.  The 8-bit output has borders

@@ -143,6 +143,14 @@ def test_long_contractions_are_cut(ops, m, v, k):
     Exact(x, w, y, g).check(*ops.linear_cross_entropy_step(x, w, y, grad=g))
 
 
+@pytest.mark.parametrize("xt,wt", [(BF16, BF16), (F32, F32), (BF16, F32)])
+@pytest.mark.parametrize("m,v,k", [(3999, 8190, 1500), (4090, 8000, 1536), (300, 50001, 2000)])
+def test_large_problems(ops, m, v, k, xt, wt):
+    """Sizes that larger tiles are taken for, in the passes over the logits and in the gradients, the last with parts."""
+    x, w, y = inputs(m + k, m, v, k, xt, wt)
+    Exact(x, w, y).check(*ops.linear_cross_entropy_step(x, w, y))
+
+
 def test_pieces_of_the_vocabulary(ops):
     """More rows times columns than a piece's gradient holds (2^28): two pieces."""
     m, v, k = 65536, 8200, 64

@@ -305,10 +305,10 @@ void check_captured_backward() {
   if (!node) return;
   const auto here = node->stream();
   if (!here) return;
+  const hipStream_t stream = c10::hip::getCurrentHIPStream(here->device_index()).stream();
+  if (!stream) return;   // the default stream is never captured, and must not be asked while another one is
   hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(c10::hip::getCurrentHIPStream(here->device_index()).stream(), &status) != hipSuccess ||
-      status == hipStreamCaptureStatusNone)
-    return;
+  if (hipStreamIsCapturing(stream, &status) != hipSuccess || status == hipStreamCaptureStatusNone) return;
   for (size_t i = 0; i < node->num_outputs(); ++i) {
     const auto& edge = node->next_edge(i);
     if (!edge.is_valid() || !node->task_should_compute_output(i)) continue;

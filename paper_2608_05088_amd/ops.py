@@ -15,7 +15,9 @@ allocates outputs and workspaces with torch, and calls the library; there is
 no CPU fallback.  Wrong arguments raise ValueError (TypeError for what is no
 tensor) before anything is enqueued, what only the library tells (buffers that
 overlap, sizes past its limits) libmalt's MaltError.  "Differentiable" means reverse mode, once; a
-tangent of forward mode is refused there.
+tangent of forward mode is refused there.  A captured backward pass of the head's loss or the norm is
+refused where it would go on in a graph of the default stream (an eager graph of the same leaves
+that still lives): no capture survives that.
 
 Work runs on the current stream of the tensors' device, or on `stream`; the
 caller orders that stream after whatever produces the inputs.  Outputs and
@@ -795,8 +797,8 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
     """One AdamW step over many tensors, in place, a launch for each 108 of them:
     m = b1 m + (1 - b1) g, v = b2 v + (1 - b2) g^2 with g = grad_scale * grad, then
     p = p (1 - lr weight_decay) - lr (m / (1 - b1^step)) / (sqrt(v / (1 - b2^step)) + eps).
-    params (contiguous) and grads are float32 or bfloat16, states adamw_state's.  step counts
-    from 1; grad_scale: a number or a float32 scalar tensor, read on the device.
+    params (contiguous) and grads are float32 or bfloat16, states adamw_state's.  eps is at least
+    2^-126; step counts from 1; grad_scale: a number or a float32 scalar tensor, read on the device.
 
     8-bit moments are rounded up or down at random by their distance, so that small changes
     add up; the random numbers follow from `seed`, the tensor's place in the list and the

@@ -49,12 +49,13 @@ using namespace ns;
 namespace {
 
 using G = NsGeom<HEAD_BK, 2, 32>;
-constexpr int BK = G::BK, STAGES = G::STAGES, H = G::H, RB = G::RB, CPR = G::CPR;
+constexpr int BK = G::BK, H = G::H, RB = G::RB, CPR = G::CPR;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr float LOG2E = 1.44269504088896340736f;
-// A tile of E x E and the waves' 2 x 4 parts of it.
-template <int E>
+// A tile of EDGE x EDGE, the waves' 2 x 4 parts of it, and a ring of DEPTH stages.
+template <int EDGE, int DEPTH>
 struct Shape {
+  static constexpr int E = EDGE, STAGES = DEPTH;
   static constexpr int TM = E / 2, TN = E / (NW / 2), NB = TM / 16, NA = TN / 16;
   static constexpr int OPER = E * RB, STAGE = 2 * OPER, RING = STAGES * STAGE;   // bytes
   static constexpr int LOADS = STAGE / 1024 / NW;                                // 1 KB each, a wave's of a stage
@@ -66,11 +67,14 @@ struct Shape {
   static constexpr int GRAD_PITCH = 32 * 4 + 16, GRAD_WAVE = TM * GRAD_PITCH;
   static constexpr int EPI = NW * OUT_WAVE > JOIN ? NW * OUT_WAVE : JOIN;
   static constexpr int LDS = AT_EPI + EPI > NW * GRAD_WAVE ? AT_EPI + EPI : NW * GRAD_WAVE;
-  static constexpr int PER_CU = E == 256 ? 1 : 2, GROUPS = 256 * PER_CU;   // workgroups that run at a time
-  static_assert(PER_CU * LDS <= 160 * 1024 && LOADS * NW * 1024 == STAGE && (STAGE & (STAGE - 1)) == 0, "LDS");
+  static constexpr int PER_CU = 2 * LDS <= 160 * 1024 ? 2 : 1, GROUPS = 256 * PER_CU;   // workgroups that run at a time
+  static_assert(PER_CU * LDS <= 160 * 1024 && LOADS * NW * 1024 == STAGE && (RING & (RING - 1)) == 0, "LDS");
   typedef f32x4 Acc[NA][NB];
 };
-static_assert(STAGES == 2 && BK == 64 && CPR == 8 && NT == 512, "the loads and reads below");
+typedef Shape<256, 2> Large;
+typedef Shape<128, 2> Small;
+typedef Shape<128, 4> Deep;   // for a CU that has one tile at a time: 0.38 us a stage where two slots take 0.55
+static_assert(BK == 64 && CPR == 8 && NT == 512, "the loads and reads below");
 
 __host__ __device__ inline int stages_of(const HeadProduct& g) { return (int)((g.k + BK - 1) / BK); }
 
@@ -93,9 +97,9 @@ __device__ __forceinline__ TileAt tile_at(int b, int tiles_m, int tiles_n, int s
 }
 
 // One operand's loads of 1 KB each: this wave's.
-template <int E>
+template <class S>
 struct Loader {
-  static constexpr int N = Shape<E>::LOADS / 2;
+  static constexpr int E = S::E, N = S::LOADS / 2;
   const uint16_t* base;   // the tile's first row in plane 0
   uint32_t voff[N];
   int64_t plane, step;
@@ -123,19 +127,18 @@ struct Loader {
 // run() does the rest.
 // acc[a][b][e] = C(row0 + wr TM + 16 b + lane % 16, col0 + wc TN + 16 a + 4 (lane / 16) + e).
 // HALVES: the planes are float16.
-template <bool HALVES, int E>
+template <bool HALVES, class S>
 struct Product {
-  typedef Shape<E> S;
-  static constexpr int NA = S::NA, NB = S::NB, LOADS = S::LOADS;
+  static constexpr int NA = S::NA, NB = S::NB, LOADS = S::LOADS, STAGES = S::STAGES;
   const HeadProduct& g;
   char* const lds;
   const int lane, wave;
-  Loader<E> la, lb;
+  Loader<S> la, lb;
   int kt0, KT;   // stages of the contraction, for each pair of planes
   // The next stage to load: its pair of planes, how many stages of that are left, where they lie.
   int pair, left;
   uint64_t at_a, at_b;
-  uint32_t at_lds;
+  uint32_t at_lds, lds0;
 
   __device__ __forceinline__ Product(const HeadProduct& g_, char* lds_)
       : g(g_), lds(lds_), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) {}
@@ -156,7 +159,7 @@ struct Product {
   __device__ __forceinline__ void advance() {
     at_a += 2 * la.step;
     at_b += 2 * lb.step;
-    at_lds ^= S::STAGE;
+    at_lds = lds0 + ((at_lds - lds0 + S::STAGE) & (S::RING - 1));
     if (--left == 0) {
       ++pair;
       start_pair();
@@ -170,7 +173,7 @@ struct Product {
     la.init(g.a, tile_a, wave, lane);
     lb.init(g.b, tile_b, wave, lane);
     pair = 0;
-    at_lds = lds_u32(lds) + wave * 1024;
+    at_lds = lds0 = lds_u32(lds) + wave * 1024;
     start_pair();
     const int total = KT * g.pairs;
 #pragma unroll
@@ -187,9 +190,20 @@ struct Product {
     wait_vm_c<0>();
   }
 
-  // Two stages of loads: at the barrier that closes stage st, stage st + 1 has arrived and every wave is
-  // done with the slot of stage st, which then receives stage st + 2; half of its loads go out at
+  // A ring of loads: at the barrier that closes stage st, stage st + 1 has arrived and every wave is
+  // done with the slot of stage st, which then receives stage st + STAGES; half of its loads go out at
   // once, half from among the products that follow.  Fragments are read one sub-step ahead.
+  // Loads arrive in order: while as many are under way as stages st + 2 and later have, one of st + 1 cannot be.
+  __device__ __forceinline__ static void next_arrived(int later) {
+    if constexpr (STAGES > 2) {
+      static_assert(STAGES == 4, "the cases below");
+      if (later >= 2) wait_vm_c<2 * LOADS>();
+      else if (later == 1) wait_vm_c<LOADS>();
+      else wait_vm_c<0>();
+    } else {
+      wait_vm_c<0>();
+    }
+  }
   __device__ __forceinline__ void run(typename S::Acc& acc) {
     const int wr = wave / (NW / 2), wc = wave % (NW / 2);
     // Block b's fragment lies 16 b rows below block 0's: 16 rows keep the swizzle's phase.
@@ -216,8 +230,8 @@ struct Product {
     asm volatile("" ::: "memory");
     read(0, lds, 0);
     auto stage = [&](const int st, auto steady_tag) {
-      constexpr bool steady = decltype(steady_tag)::value;   // stage st + 2 exists
-      const char* const slot = lds + (st & 1) * S::STAGE;
+      constexpr bool steady = decltype(steady_tag)::value;   // stage st + STAGES exists
+      const char* const slot = lds + (st & (STAGES - 1)) * S::STAGE;
 #pragma unroll
       for (int h = 0; h < H; ++h) {
         const int c = h & 1;
@@ -225,14 +239,14 @@ struct Product {
           read(c ^ 1, slot, h + 1);
         } else if (steady || st + 1 < total) {
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's reads of the stage are done
-          wait_vm_c<0>();
+          next_arrived(steady ? STAGES - 2 : total - st - 2);
           __builtin_amdgcn_s_barrier();
           asm volatile("" ::: "memory");
           if constexpr (steady) {
 #pragma unroll
             for (int q = LOADS / 2; q < LOADS; ++q) issue(q);
           }
-          read(c ^ 1, lds + ((st + 1) & 1) * S::STAGE, 0);
+          read(c ^ 1, lds + ((st + 1) & (STAGES - 1)) * S::STAGE, 0);
         }
 #pragma unroll
         for (int a = 0; a < NA; ++a)
@@ -313,16 +327,15 @@ __device__ __forceinline__ int label_of(const HeadLabels& l, int64_t r, int64_t 
 
 // A workgroup takes every 32nd tile of its XCD's.  While a tile's sums are formed in registers,
 // the next one's first stages arrive.
-template <bool HALVES, int E>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE * Shape<E>::PER_CU, WPE * Shape<E>::PER_CU)))
+template <bool HALVES, class S>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE * S::PER_CU, WPE * S::PER_CU)))
 void head_first_kernel(HeadLogits a) {
-  typedef Shape<E> S;
-  constexpr int TM = S::TM, TN = S::TN, NA = S::NA, NB = S::NB;
+  constexpr int E = S::E, TM = S::TM, TN = S::TN, NA = S::NA, NB = S::NB;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   int block = blockIdx.x;
   TileAt t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
   if (t.i < 0) return;
-  Product<HALVES, E> product(a.g, lds);
+  Product<HALVES, S> product(a.g, lds);
   const int lane = product.lane, wave = product.wave, wr = wave / (NW / 2), wc = wave % (NW / 2), g = lane >> 4;
   const int KT = stages_of(a.g);
   product.prime(t.i, t.j, 0, KT);
@@ -416,16 +429,15 @@ void head_first_kernel(HeadLogits a) {
   }
 }
 
-template <bool HALVES, int E>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE * Shape<E>::PER_CU, WPE * Shape<E>::PER_CU)))
+template <bool HALVES, class S>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE * S::PER_CU, WPE * S::PER_CU)))
 void head_second_kernel(HeadLogits a) {
-  typedef Shape<E> S;
-  constexpr int TM = S::TM, TN = S::TN, NA = S::NA, NB = S::NB;
+  constexpr int E = S::E, TM = S::TM, TN = S::TN, NA = S::NA, NB = S::NB;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   int block = blockIdx.x;
   TileAt t = tile_at(block, a.g.tiles_m, a.g.tiles_n, 1);
   if (t.i < 0) return;
-  Product<HALVES, E> product(a.g, lds);
+  Product<HALVES, S> product(a.g, lds);
   const int lane = product.lane, wave = product.wave, wr = wave / (NW / 2), wc = wave % (NW / 2), g = lane >> 4;
   const int KT = stages_of(a.g);
   product.prime(t.i, t.j, 0, KT);
@@ -580,10 +592,9 @@ __device__ __forceinline__ float scale_of(const HeadGrads& a) { return a.scale_a
 // A wave's sub-tile leaves through its own part of LDS, 32 of its columns at a time, so that a
 // store covers eight rows' 128 bytes, and in a loop: straight from the registers it is 30 KB of code,
 // run once a tile.
-template <class T, int E>
+template <class T, class S>
 __device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, int split, int64_t row0, int64_t col0, char* lds,
-                                          const typename Shape<E>::Acc& acc) {
-  typedef Shape<E> S;
+                                          const typename S::Acc& acc) {
   constexpr int TM = S::TM, TN = S::TN, NB = S::NB;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave / (NW / 2), wc = wave % (NW / 2);
@@ -632,8 +643,8 @@ __device__ __forceinline__ void write_out(const HeadOut& o, const HeadGrads& a, 
 
 }  // namespace
 
-template <int E>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE * Shape<E>::PER_CU, WPE * Shape<E>::PER_CU)))
+template <class S>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE * S::PER_CU, WPE * S::PER_CU)))
 void head_grads_kernel(HeadGrads a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   int b = blockIdx.x, which = 0;
@@ -646,16 +657,16 @@ void head_grads_kernel(HeadGrads a) {
   const TileAt t = tile_at(b, o.g.tiles_m, o.g.tiles_n, o.splits);
   if (t.i < 0) return;
   const int split = t.split;
-  const int64_t row0 = (int64_t)t.i * E, col0 = (int64_t)t.j * E;
+  const int64_t row0 = (int64_t)t.i * S::E, col0 = (int64_t)t.j * S::E;
   const int KT = stages_of(o.g), kt0 = (int)((int64_t)KT * split / o.splits), kt1 = (int)((int64_t)KT * (split + 1) / o.splits);
-  typename Shape<E>::Acc acc;
-  Product<false, E> product(o.g, lds);
+  typename S::Acc acc;
+  Product<false, S> product(o.g, lds);
   product.prime(t.i, t.j, kt0, kt1 - kt0);
   product.arrived();
   product.run(acc);
   lds_free();
-  if (o.f32) write_out<float, E>(o, a, split, row0, col0, lds, acc);
-  else write_out<bf16_t, E>(o, a, split, row0, col0, lds, acc);
+  if (o.f32) write_out<float, S>(o, a, split, row0, col0, lds, acc);
+  else write_out<bf16_t, S>(o, a, split, row0, col0, lds, acc);
 }
 
 // The sums of contractions' parts, four columns a thread: one result's, then the other's.  Of many parts
@@ -698,6 +709,19 @@ __global__ __launch_bounds__(64 * SUM_WAVES) void head_sum_kernel(HeadGrads a, i
   else sum4<bf16_t>(o, a, block, join);
 }
 
+namespace {
+template <class S>
+hipError_t raise_limits() {
+  for (const void* f : {reinterpret_cast<const void*>(&head_first_kernel<false, S>), reinterpret_cast<const void*>(&head_first_kernel<true, S>),
+                        reinterpret_cast<const void*>(&head_second_kernel<false, S>), reinterpret_cast<const void*>(&head_second_kernel<true, S>),
+                        reinterpret_cast<const void*>(&head_grads_kernel<S>)}) {
+    const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+}  // namespace
+
 // The kernels use more dynamic LDS than the default limit: raised once for each device.
 hipError_t head_setup() {
   static std::atomic<uint64_t> raised{0};
@@ -706,44 +730,40 @@ hipError_t head_setup() {
   if (e != hipSuccess) return e;
   const uint64_t bit = uint64_t(1) << (dev & 63);
   if (dev <= 63 && raised.load(std::memory_order_relaxed) & bit) return hipSuccess;
-  struct { const void* kernel; int bytes; } const all[] = {
-      {reinterpret_cast<const void*>(&head_first_kernel<false, 256>), Shape<256>::LDS}, {reinterpret_cast<const void*>(&head_first_kernel<true, 256>), Shape<256>::LDS},
-      {reinterpret_cast<const void*>(&head_second_kernel<false, 256>), Shape<256>::LDS}, {reinterpret_cast<const void*>(&head_second_kernel<true, 256>), Shape<256>::LDS},
-      {reinterpret_cast<const void*>(&head_grads_kernel<256>), Shape<256>::LDS},
-      {reinterpret_cast<const void*>(&head_first_kernel<false, 128>), Shape<128>::LDS}, {reinterpret_cast<const void*>(&head_first_kernel<true, 128>), Shape<128>::LDS},
-      {reinterpret_cast<const void*>(&head_second_kernel<false, 128>), Shape<128>::LDS}, {reinterpret_cast<const void*>(&head_second_kernel<true, 128>), Shape<128>::LDS},
-      {reinterpret_cast<const void*>(&head_grads_kernel<128>), Shape<128>::LDS}};
-  for (const auto& f : all) {
-    e = hipFuncSetAttribute(f.kernel, hipFuncAttributeMaxDynamicSharedMemorySize, f.bytes);
-    if (e != hipSuccess) return e;
-  }
+  e = raise_limits<Large>();
+  if (e == hipSuccess) e = raise_limits<Small>();
+  if (e == hipSuccess) e = raise_limits<Deep>();
+  if (e != hipSuccess) return e;
   if (dev <= 63) raised.fetch_or(bit, std::memory_order_relaxed);
   return hipSuccess;
 }
 
 namespace {
-template <int E>
-void logits_of(const HeadLogits& a, bool second, hipStream_t s) {
-  const int blocks = tile_blocks(a.g.tiles_m, a.g.tiles_n, 1);
-  const dim3 grid((unsigned)(blocks < Shape<E>::GROUPS ? blocks : Shape<E>::GROUPS));
-  if (second && a.x_scales) hipLaunchKernelGGL((head_second_kernel<true, E>), grid, dim3(NT), Shape<E>::LDS, s, a);
-  else if (second) hipLaunchKernelGGL((head_second_kernel<false, E>), grid, dim3(NT), Shape<E>::LDS, s, a);
-  else if (a.x_scales) hipLaunchKernelGGL((head_first_kernel<true, E>), grid, dim3(NT), Shape<E>::LDS, s, a);
-  else hipLaunchKernelGGL((head_first_kernel<false, E>), grid, dim3(NT), Shape<E>::LDS, s, a);
+template <class S>
+void logits_of(const HeadLogits& a, bool second, int blocks, hipStream_t s) {
+  const dim3 grid((unsigned)(blocks < S::GROUPS ? blocks : S::GROUPS));
+  if (second && a.x_scales) hipLaunchKernelGGL((head_second_kernel<true, S>), grid, dim3(NT), S::LDS, s, a);
+  else if (second) hipLaunchKernelGGL((head_second_kernel<false, S>), grid, dim3(NT), S::LDS, s, a);
+  else if (a.x_scales) hipLaunchKernelGGL((head_first_kernel<true, S>), grid, dim3(NT), S::LDS, s, a);
+  else hipLaunchKernelGGL((head_first_kernel<false, S>), grid, dim3(NT), S::LDS, s, a);
 }
 }  // namespace
 
 hipError_t launch_head_logits(const HeadLogits& a, int edge, bool second, hipStream_t s) {
-  if (edge == 256) logits_of<256>(a, second, s);
-  else logits_of<128>(a, second, s);
+  const int blocks = tile_blocks(a.g.tiles_m, a.g.tiles_n, 1);
+  if (edge == 256) logits_of<Large>(a, second, blocks, s);
+  else if (blocks > Deep::GROUPS) logits_of<Small>(a, second, blocks, s);
+  else logits_of<Deep>(a, second, blocks, s);
   return hipGetLastError();
 }
 
 hipError_t launch_head_grads(const HeadGrads& a, int edge, hipStream_t s) {
   int blocks = 0;
   for (int i = 0; i < a.parts; ++i) blocks += tile_blocks(a.part[i].g.tiles_m, a.part[i].g.tiles_n, a.part[i].splits);
-  if (edge == 256) hipLaunchKernelGGL(head_grads_kernel<256>, dim3((unsigned)blocks), dim3(NT), Shape<256>::LDS, s, a);
-  else hipLaunchKernelGGL(head_grads_kernel<128>, dim3((unsigned)blocks), dim3(NT), Shape<128>::LDS, s, a);
+  const dim3 grid((unsigned)blocks);
+  if (edge == 256) hipLaunchKernelGGL(head_grads_kernel<Large>, grid, dim3(NT), Large::LDS, s, a);
+  else if (blocks > Deep::GROUPS) hipLaunchKernelGGL(head_grads_kernel<Small>, grid, dim3(NT), Small::LDS, s, a);
+  else hipLaunchKernelGGL(head_grads_kernel<Deep>, grid, dim3(NT), Deep::LDS, s, a);
   return hipGetLastError();
 }
 

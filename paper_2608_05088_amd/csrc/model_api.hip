@@ -126,6 +126,7 @@ int head_pair_count(int na, int nb, int planes) {
 //   second       300 x 1000 x 64 10 | 26, 2000 x 12000 x 768 54 | 62, 8192 x 50257 x 1280 762 | 660 (half of it)
 int head_edge(int64_t rows, int64_t cols, int64_t stages, double big, double small) {
   auto rounds = [&](int64_t e) { return double((up(rows, e) / e * (up(cols, e) / e) + 255) / 256); };
+  if (rounds(256) > 64) return 256;   // little to win, and a row's statistics take twice the workspace
   return 0.5 * rounds(128) * (0.78 * double(stages) + small) < rounds(256) * (1.43 * double(stages) + big) ? 128 : 256;
 }
 

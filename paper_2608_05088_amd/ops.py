@@ -557,22 +557,22 @@ def _fp8_rows(x: Fp8Rows, dev, k: int, kb: int) -> int:
     return m
 
 
-@functools.lru_cache(maxsize=4096)
-def _matmul_size(m: int, n: int, k: int, out_type: int) -> int:
-    size = c_size_t(0)
-    lm._check(lm.lib().malt_block_matmul_size(m, n, k, out_type, byref(size)))
-    return size.value
-
-
 def fp8_forward(x: Union[torch.Tensor, Fp8Rows], values: torch.Tensor, scales: torch.Tensor,
                 out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """fp8_linear on kept weights (fp8_quantize_weight), without gradients:
     x (..., inner), values (outer, inner padded to whole blocks).  x may be in 8 bits
     already (rms_norm_fp8's rows; out_dtype is bfloat16 then unless given).  Precision by
     out_dtype, as there."""
+    ready = isinstance(x, Fp8Rows)
+    if (ready and all(isinstance(t, torch.Tensor) for t in (x.values, x.scales, values, scales)) and values.is_cuda
+            and (out_dtype is None or out_dtype in _DTYPES)):
+        out_type = _DTYPES[out_dtype or torch.bfloat16]
+        y = _on(values.device, stream, (x.values, x.scales, values, scales),
+                lambda s: _host().fp8_rows(x.values, x.scales, x.shape, values, scales, out_type, s))
+        if y is not None:
+            return y   # otherwise the checks below say what is wrong
     _tensor("values", values, (torch.float8_e4m3fn,))
     dev = values.device
-    ready = isinstance(x, Fp8Rows)
     if not ready:
         _tensor("x", x, _DTYPES, dev)
     _tensor("scales", scales, (torch.uint8,), dev)
@@ -594,18 +594,7 @@ def fp8_forward(x: Union[torch.Tensor, Fp8Rows], values: torch.Tensor, scales: t
         raise ValueError(f"scales must be contiguous, ({-(-n // BLOCK)}, {kb}) "
                          f"(got {tuple(scales.shape)}, strides {scales.stride()})")
     if ready:
-        def work_ready(s):
-            y = torch.empty((*x.shape[:-1], n), dtype=out_dtype, device=dev)
-            if m:
-                out_type = _DTYPES[out_dtype]
-                size = _matmul_size(m, n, k, out_type) if m > 32 else 0
-                ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
-                lm._check(lm.lib().malt_block_linear_operand(
-                    x.values.data_ptr(), x.scales.data_ptr(), m, k, values.data_ptr(), scales.data_ptr(), n, y.data_ptr(),
-                    out_type, n, ws.data_ptr() if size else None, size, s))
-            return y
-
-        return _on(dev, stream, (x.values, x.scales, values, scales), work_ready)
+        raise ValueError(f"x, values and scales do not belong together (x of {tuple(x.shape)}, values {tuple(values.shape)})")
     x = x.detach()
 
     def work(s):

@@ -203,6 +203,31 @@ def test_layer_on_8_bit_rows(ops, m, k, n, out):
 
 
 # --------------------------------------------------------------- layouts and calls
+@pytest.mark.parametrize("stream", [False, True])
+def test_layer_on_8_bit_rows_refuses(ops, stream):
+    x, w = rows(70, 6, 200, BF16).view(2, 3, 200), torch.ones(200, device="cuda")
+    values, scales = ops.fp8_quantize_weight(torch.randn((130, 200), device="cuda", generator=gen(71)))   # scales 2 x 2
+    q = ops.rms_norm_fp8(x, w)
+    kw = dict(stream=torch.cuda.Stream()) if stream else {}
+    torch.cuda.synchronize()
+    assert ops.fp8_forward(q, values, scales, **kw).shape == (2, 3, 130)
+    for bad in (q._replace(values=q.values[:5]), q._replace(values=q.values.view(torch.uint8)), q._replace(scales=q.scales[:1]),
+                q._replace(values=q.values.t().contiguous().t()), q._replace(shape=torch.Size((2, 3, 300))),
+                q._replace(shape=torch.Size((5, 200))), q._replace(shape=torch.Size(())), q._replace(scales=q.scales.cpu()),
+                q._replace(scales=q.scales.float())):
+        with pytest.raises(ValueError):
+            ops.fp8_forward(bad, values, scales, **kw)
+    for args in ((q, values[:, :128], scales), (q, values, scales[:, :1]), (q, values.cpu(), scales), (q, values, scales.t().contiguous().t())):
+        with pytest.raises(ValueError):
+            ops.fp8_forward(*args, **kw)
+    with pytest.raises(ValueError, match="out_dtype"):
+        ops.fp8_forward(q, values, scales, out_dtype=torch.float16, **kw)
+    for bad in (q._replace(values=None), q._replace(scales=3)):
+        with pytest.raises(TypeError):
+            ops.fp8_forward(bad, values, scales, **kw)
+    torch.cuda.synchronize()
+
+
 def test_shapes_and_strides(ops):
     x, w, r = rows(21, 24, 96, BF16), torch.rand(96, device="cuda", generator=gen(22)), rows(23, 24, 96, BF16)
     y, h = ops.rms_norm(x, w, residual=r)

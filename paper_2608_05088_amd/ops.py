@@ -564,7 +564,7 @@ def fp8_forward(x: Union[torch.Tensor, Fp8Rows], values: torch.Tensor, scales: t
     already (rms_norm_fp8's rows; out_dtype is bfloat16 then unless given).  Precision by
     out_dtype, as there."""
     ready = isinstance(x, Fp8Rows)
-    if (ready and all(isinstance(t, torch.Tensor) for t in (x.values, x.scales, values, scales)) and values.is_cuda
+    if (ready and all(isinstance(t, torch.Tensor) and t.is_cuda for t in (x.values, x.scales, values, scales))
             and (out_dtype is None or out_dtype in _DTYPES)):
         out_type = _DTYPES[out_dtype or torch.bfloat16]
         y = _on(values.device, stream, (x.values, x.scales, values, scales),
@@ -755,6 +755,10 @@ def rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
     values), for fp8_forward on kept weights, in one pass and without gradients:
     rows, or (rows, h) with residual.  y is rounded once, from float32."""
     _tensor("x", x, _DTYPES)
+    if stream is not None:   # what is recorded on it
+        _tensor("weight", weight, _DTYPES, x.device)
+        if residual is not None:
+            _tensor("residual", residual, (x.dtype,), x.device)
     values, scales, h = _on(x.device, stream, (x, weight, residual),
                             lambda s: _host().rms_norm_fp8(x, weight, residual, eps, s))
     rows = Fp8Rows(values, scales, x.shape)
@@ -762,6 +766,15 @@ def rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
 
 
 # ------------------------------------------------------------------------- AdamW
+_STATES = (torch.float32, torch.uint8)
+
+
+def _tensors(name: str, tensors, types, dev) -> list:
+    for i, t in enumerate(tensors):
+        _tensor(f"{name}[{i}]", t, types, dev)
+    return tensors
+
+
 @functools.lru_cache(maxsize=4096)
 def _adamw_size(numel: int, bits: int) -> int:
     size = c_size_t(0)
@@ -803,8 +816,15 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
         scale_at, grad_scale = grad_scale, 1.0
     if params:
         _tensor("params[0]", params[0], _DTYPES)
-    dev = params[0].device if params else grads[0].device
-    inputs = (*params, *grads, *states, scale_at) if stream is not None else ()
+        dev = params[0].device
+    else:   # refused below
+        dev = torch.device("cuda", torch.cuda.current_device())
+    inputs = ()
+    if stream is not None:   # what is recorded on it
+        inputs = (*_tensors("params", params, _DTYPES, dev), *_tensors("grads", grads, _DTYPES, dev),
+                  *_tensors("states", states, _STATES, dev), scale_at)
+        if scale_at is not None:
+            _tensor("grad_scale", scale_at, (torch.float32,), dev)
     b1, b2 = betas
     _on(dev, stream, inputs, lambda s: _host().adamw_step(params, grads, states, lr, b1, b2, eps, weight_decay, step,
                                                           grad_scale, scale_at, seed, s))
@@ -818,5 +838,8 @@ def adamw_moments(params: Sequence[torch.Tensor], states: Sequence[torch.Tensor]
         return []
     if params:
         _tensor("params[0]", params[0], _DTYPES)
-    dev = params[0].device if params else states[0].device
-    return _on(dev, stream, states, lambda s: _host().adamw_moments(params, states, s))
+        dev = params[0].device
+    else:   # refused below
+        dev = torch.device("cuda", torch.cuda.current_device())
+    inputs = _tensors("states", states, _STATES, dev) if stream is not None else ()
+    return _on(dev, stream, inputs, lambda s: _host().adamw_moments(params, states, s))

@@ -199,3 +199,36 @@ def test_a_captured_backward_pass_and_an_eager_graph(ops, op):
             torch.cuda.synchronize()
             assert torch.equal(w.grad, want)
         held = None
+
+
+@pytest.mark.parametrize("stream", [False, True])
+def test_host_tensors_and_no_tensors_are_refused(ops, stream):
+    """Before anything is recorded on a stream."""
+    kw = dict(stream=torch.cuda.Stream()) if stream else {}
+    x, w, y = torch.ones((4, 64), device="cuda"), torch.ones((9, 64), device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    gain, st = torch.ones(64, device="cuda"), ops.adamw_state(x)
+    torch.cuda.synchronize()
+    calls = {
+        "loss": (lambda a, b, c: ops.linear_cross_entropy(a, b, c, **kw), (x, w, y)),
+        "step": (lambda a, b, c, g, o: ops.linear_cross_entropy_step(a, b, c, grad=g, out=o, **kw),
+                 (x, w, y, torch.ones(4, device="cuda"), torch.zeros_like(w))),
+        "norm": (lambda a, b, r: ops.rms_norm(a, b, residual=r, **kw), (x, gain, x.clone())),
+        "norm_fp8": (lambda a, b, r: ops.rms_norm_fp8(a, b, residual=r, **kw), (x, gain, x.clone())),
+        "adamw": (lambda p, g, s, c: ops.adamw_step([p], [g], [s], lr=0.0, step=1, grad_scale=c, **kw),
+                  (x.clone(), x, st, torch.ones((), device="cuda"))),
+        "moments": (lambda p, s: ops.adamw_moments([p], [s], **kw), (x, st)),
+    }
+    for name, (call, args) in calls.items():
+        call(*args)
+        for i, t in enumerate(args):
+            with pytest.raises(ValueError):
+                call(*args[:i], t.cpu(), *args[i + 1:])
+            with pytest.raises((TypeError, ValueError)):
+                call(*args[:i], object(), *args[i + 1:])
+    with pytest.raises(ValueError):
+        ops.adamw_step([], [x], [st], lr=0.0, step=1, **kw)
+    with pytest.raises(ValueError):
+        ops.adamw_moments([], [st], **kw)
+    with pytest.raises(ValueError):
+        ops.adamw_step([x], [], [st], lr=0.0, step=1, **kw)
+    torch.cuda.synchronize()

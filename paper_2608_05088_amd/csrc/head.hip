@@ -9,7 +9,7 @@
 // read (twice 4 bytes a logit) as the K products that make one.
 //
 // 8192 x 50257 x 1280 in bf16, 1.05 T operations a product: first pass 950 us (1110 TFLOP/s; the library's
-// product that writes its logits: 939), second 1320 in two pieces, gradients 1740 (1210 TFLOP/s; the library's: 2450).
+// product that writes its logits: 939), second 1310 in two pieces, gradients 1740 (1210 TFLOP/s; the library's: 2450).
 // A stage of 64 takes a tile 1.40 to 1.46 us with random values and 1.23 with zeros: the power limit.  What the
 // second pass takes longer is its writing: a tile's dz, 256 KB both ways, 24 us of 53, while no matrix
 // instruction runs on that CU.
@@ -30,7 +30,7 @@
 //   gradients: three bf16 planes, all 24 bits; six pairs (middle by low and low by low are below
 //     2^-24).  float16 would not do for dz, whose values have no row or column of like size.
 // At the matrix cores' 16-bit rate that is three and 1.5 times the float32 instruction's
-// (1001 x 50257 x 901: 310, 535 and 1040 us; in one float32 product each the matrix cores would need 4 x 590).
+// (1001 x 50257 x 901: 324, 496 and 1070 us; in one float32 product each the matrix cores would need 4 x 590).
 // bf16 gradients take one plane of dz, rounded once more, an error of the size of the result's own
 // rounding (two planes where the problem is small, and of a float32 operand).
 //

@@ -9,16 +9,16 @@
 // read (twice 4 bytes a logit) as the K products that make one.
 //
 // 8192 x 50257 x 1280 in bf16, 1.05 T operations a product: first pass 950 us (1110 TFLOP/s; the library's
-// product that writes its logits: 939), second 1310 in two pieces, gradients 1740 (1210 TFLOP/s; the library's: 2450).
+// product that writes its logits: 939), second 1170 in two pieces, gradients 1700 (1240 TFLOP/s; the library's: 2450).
 // A stage of 64 takes a tile 1.40 to 1.46 us with random values and 1.23 with zeros: the power limit.  What the
-// second pass takes longer is its writing: a tile's dz, 256 KB both ways, 24 us of 53, while no matrix
+// second pass takes longer is its writing: a tile's dz, 256 KB both ways, 18 us of 47, while no matrix
 // instruction runs on that CU.
 //
 // A workgroup of eight waves makes one 256 x 256 tile, the pipeline of the Newton-Schulz
 // update (ns_common.h): stages of 64 contracted values go straight to LDS, two slots deep.  Where
 // there are few tiles or few stages in each, tiles are of 128 x 128, two on a CU, which read twice the LDS for a
-// product but leave no CU out and work on one's stages during the other's epilogue: 300 x 1000 x 64 76 -> 40 us a
-// step, 200 x 8000 x 512 in float32 168 -> 94, 500 x 2000 x 2000 162 -> 87 (the rules are in model_api.hip).  Both
+// product but leave no CU out and work on one's stages during the other's epilogue: 300 x 1000 x 64 76 -> 37 us a
+// step, 200 x 8000 x 512 in float32 168 -> 89, 500 x 2000 x 2000 162 -> 80 (the rules are in model_api.hip).  Both
 // sides of every product lie with the contraction along their rows: x and W are transposed once for
 // the gradients, dz is written both ways.  (Transposed LDS reads instead: 1.84 us a stage, for one side or
 // both; rows of 32 KB apart: 1.70, with a pitch that is no power of two 1.58.)
@@ -30,7 +30,7 @@
 //   gradients: three bf16 planes, all 24 bits; six pairs (middle by low and low by low are below
 //     2^-24).  float16 would not do for dz, whose values have no row or column of like size.
 // At the matrix cores' 16-bit rate that is three and 1.5 times the float32 instruction's
-// (1001 x 50257 x 901: 324, 496 and 1070 us; in one float32 product each the matrix cores would need 4 x 590).
+// (1001 x 50257 x 901: 324, 425 and 1070 us; in one float32 product each the matrix cores would need 4 x 590).
 // bf16 gradients take one plane of dz, rounded once more, an error of the size of the result's own
 // rounding (two planes where the problem is small, and of a float32 operand).
 //
@@ -516,51 +516,64 @@ void head_second_kernel(HeadLogits a) {
     // The next tile's loads are waited for before the stores go out: loads and stores may complete in any
     // order, and waiting for both would put the stores' time between two tiles.
     product.arrived();
+    // 16 rows of dz, or 16 columns of as many rows as the wave has columns, meet in the wave's own region of LDS, so
+    // that stores cover whole lines (8 bytes a lane straight from the registers: dz_t alone 9 us a tile).
+    auto packed = [&](int i, int b) { return uint2{pack_bf16x2(acc[i][b][0], acc[i][b][1]), pack_bf16x2(acc[i][b][2], acc[i][b][3])}; };
+    constexpr int GB = TN / 16, CHUNKS = TN / 8, ROWS = 64 / CHUNKS;   // 16 bytes each; rows a store covers
+    const int col = tile_n * E + wc * TN;
+    auto leave = [&](bf16_t* out) {
+      // The wave's LDS instructions run in order.
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      if (b % 4 == 0 && 16 * b >= rows) break;
-      for (int p = 0; p < a.dz_planes; ++p) {
-        uint2 pk[NA];
+      for (int it = 0; it < 16 / ROWS; ++it) {
+        const int r = lane / CHUNKS + ROWS * it, ch = lane % CHUNKS;
+        const char* src = sto + r * S::OUT_PITCH + ch * 16;
+        const uint2 lo = *reinterpret_cast<const uint2*>(src);
+        const uint2 hi = *reinterpret_cast<const uint2*>(src + 8);
+        const u32x4 v = {lo.x, lo.y, hi.x, hi.y};
+        *reinterpret_cast<MALT_GLOBAL u32x4*>(gptr(out) + r * BK + ch * 8) = v;
+      }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+    };
+    for (int p = 0; p < a.dz_planes; ++p) {
 #pragma unroll
-        for (int i = 0; i < NA; ++i) {
-          pk[i].x = pack_bf16x2(acc[i][b][0], acc[i][b][1]);
-          pk[i].y = pack_bf16x2(acc[i][b][2], acc[i][b][3]);
-          if (p + 1 < a.dz_planes) {
-            acc[i][b][0] -= bf16_lo(pk[i].x);
-            acc[i][b][1] -= bf16_hi(pk[i].x);
-            acc[i][b][2] -= bf16_lo(pk[i].y);
-            acc[i][b][3] -= bf16_hi(pk[i].y);
+      for (int b0 = 0; b0 < NB; b0 += GB) {
+        if (16 * b0 >= rows) break;
+        const int row = tile_m * E + wr * TM + 16 * b0;
+        if (a.dz) {
+          bf16_t* const dz = a.dz + p * a.dz_plane + row / HEAD_TILE * a.dz_tile + col / BK * HEAD_BLOCK + row % HEAD_TILE * BK + col % BK;
+#pragma unroll
+          for (int b = 0; b < GB; ++b) {
+#pragma unroll
+            for (int i = 0; i < NA; ++i) *reinterpret_cast<uint2*>(sto + (lane & 15) * S::OUT_PITCH + (4 * g + i * 16) * 2) = packed(i, b0 + b);
+            leave(dz + 16 * b * BK);
           }
         }
-        const int row = tile_m * E + wr * TM + 16 * b, col = tile_n * E + wc * TN;   // the first ones
         if (a.dz_t) {
-          // Lane p of a quad takes column p of its four rows.
-          bf16_t* const out = a.dz_t + p * a.dz_plane + col / HEAD_TILE * a.dz_t_tile + row / BK * HEAD_BLOCK +
-                              (col % HEAD_TILE + 4 * g + (lane & 3)) * BK + row % BK + (lane & 12);
+          bf16_t* const dz_t = a.dz_t + p * a.dz_plane + col / HEAD_TILE * a.dz_t_tile + row / BK * HEAD_BLOCK + col % HEAD_TILE * BK + row % BK;
 #pragma unroll
           for (int i = 0; i < NA; ++i) {
-            *reinterpret_cast<MALT_GLOBAL op_u32x2*>(gptr(out) + 16 * i * BK) = turn_quad(pk[i], pick, low);
+            // Lane p of a quad takes column p of its four rows.
+#pragma unroll
+            for (int b = 0; b < GB; ++b)
+              *reinterpret_cast<op_u32x2*>(sto + (4 * g + (lane & 3)) * S::OUT_PITCH + (16 * b + (lane & 12)) * 2) =
+                  turn_quad(packed(i, b0 + b), pick, low);
+            leave(dz_t + 16 * i * BK);
           }
         }
-        if (a.dz) {
+        if (p + 1 < a.dz_planes) {
 #pragma unroll
-          for (int i = 0; i < NA; ++i) *reinterpret_cast<uint2*>(sto + (lane & 15) * S::OUT_PITCH + (4 * g + i * 16) * 2) = pk[i];
-          // The wave's own region: its LDS instructions run in order.
-          asm volatile("" ::: "memory");
-          __builtin_amdgcn_wave_barrier();
-          bf16_t* const dz = a.dz + p * a.dz_plane + row / HEAD_TILE * a.dz_tile + col / BK * HEAD_BLOCK + row % HEAD_TILE * BK + col % BK;
-          constexpr int CHUNKS = TN / 8, ROWS = 64 / CHUNKS;   // 16 bytes each; rows a store covers
+          for (int b = b0; b < b0 + GB; ++b)
 #pragma unroll
-          for (int it = 0; it < 16 / ROWS; ++it) {
-            const int r = lane / CHUNKS + ROWS * it, ch = lane % CHUNKS;
-            const char* src = sto + r * S::OUT_PITCH + ch * 16;
-            const uint2 lo = *reinterpret_cast<const uint2*>(src);
-            const uint2 hi = *reinterpret_cast<const uint2*>(src + 8);
-            const u32x4 v = {lo.x, lo.y, hi.x, hi.y};
-            *reinterpret_cast<MALT_GLOBAL u32x4*>(gptr(dz) + r * BK + ch * 8) = v;
-          }
-          asm volatile("" ::: "memory");
-          __builtin_amdgcn_wave_barrier();
+            for (int i = 0; i < NA; ++i) {
+              const uint2 v = packed(i, b);
+              acc[i][b][0] -= bf16_lo(v.x);
+              acc[i][b][1] -= bf16_hi(v.x);
+              acc[i][b][2] -= bf16_lo(v.y);
+              acc[i][b][3] -= bf16_hi(v.y);
+            }
         }
       }
     }

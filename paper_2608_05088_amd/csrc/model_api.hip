@@ -123,7 +123,7 @@ int head_pair_count(int na, int nb, int planes) {
 // The tiles' edge of a pass over rows x cols logits, from what tiles take.  A CU runs one tile of 256 at a time, 1.43 us
 // a stage, or two of 128, 0.78; `big` and `small`: what is done after the stages, in us.  us, tiles of 128 | 256:
 //   first pass   300 x 1000 x 64 6 | 11, 512 x 50257 x 768 45 | 52, 8192 x 50257 x 768 659 | 622
-//   second       300 x 1000 x 64 10 | 26, 2000 x 12000 x 768 54 | 62, 8192 x 50257 x 1280 762 | 660 (half of it)
+//   second       300 x 1000 x 64 9 | 26, 2000 x 12000 x 768 54 | 62, 8192 x 50257 x 1280 762 | 660 (half of it; by now 586)
 int head_edge(int64_t rows, int64_t cols, int64_t stages, double big, double small) {
   auto rounds = [&](int64_t e) { return double((up(rows, e) / e * (up(cols, e) / e) + 255) / 256); };
   if (rounds(256) > 64) return 256;   // little to win, and a row's statistics take twice the workspace
@@ -199,7 +199,7 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     const int64_t dx_stages = L.piece / HEAD_BK * head_pair_count(L.dx_z, L.dx_w, x32 ? HEAD_PLANES : 2);
     const int64_t dw_stages = up(a.rows, HEAD_BK) / HEAD_BK *
                               head_pair_count(L.dw_z, L.dw_x, dw32 ? HEAD_PLANES : 2);
-    L.second_edge = head_edge(a.rows, std::min(L.piece, a.vocab), stages, 4 + 20 * L.dz_planes, 4 + 12 * L.dz_planes);
+    L.second_edge = head_edge(a.rows, std::min(L.piece, a.vocab), stages, 4 + 14 * L.dz_planes, 4 + 9 * L.dz_planes);
     // Of the gradients: by their stages of 256-tiles on each of 256 CUs.  us, tiles of 128 | 256: 500 x 2000 x 2000 (below 36) 24 | 35,
     // 2000 x 12000 x 768 (35) 83 | 101, 512 x 50257 x 768 (37) 119 | 119, 400 x 30000 x 1024 in float32 (165) 401 | 330.
     const int64_t wide = up(a.inner, HEAD_TILE) / HEAD_TILE;

@@ -130,6 +130,27 @@ int head_edge(int64_t rows, int64_t cols, int64_t stages, double big, double sma
   return 0.5 * rounds(128) * (0.78 * double(stages) + small) < rounds(256) * (1.43 * double(stages) + big) ? 128 : 256;
 }
 
+// Parts for dx's contraction where dW's tiles, `small` stages each, fill the CUs that dx's parts leave free and
+// follow them: those that end first by this count, one workgroup a CU.  A tile's epilogue counts as 6 stages, `extra`
+// what a part costs in writing and reading it.  us a step, against even shares: 3000 x 20000 x 1000 in float32 2024 | 2187,
+// 400 x 30000 x 1024 621 | 646, 1001 x 50257 x 901 2034 | 2020 (idle CUs leave the others power), bf16 within 1%.
+int head_parts(int64_t tiles, int64_t stages, int64_t small_tiles, int64_t small, double extra, int64_t most) {
+  double best = 0;
+  int at = 0;
+  for (int64_t n = 1; n <= most && n * tiles <= 256; ++n) {
+    const int64_t l1 = (stages + n - 1) / n + 6, l2 = small + 6, busy = n * tiles;
+    auto done = [&](int64_t t) { return (256 - busy) * (t / l2) + busy * ((t - l1) / l2); };
+    int64_t t = l1;
+    while (done(t) < small_tiles) t = std::min((t / l2 + 1) * l2, t + l2 - (t - l1) % l2);
+    const double cost = double(t) + extra * double(n > 1 ? n : 0);
+    if (at == 0 || cost < best) {
+      best = cost;
+      at = int(n);
+    }
+  }
+  return at;
+}
+
 HeadPlan head_plan(const malt_linear_loss_t& a) {
   HeadPlan L = {};
   const bool x32 = a.x_type == MALT_FLOAT32, w32 = a.weight_type == MALT_FLOAT32;
@@ -216,6 +237,11 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     };
     L.dx_splits = a.dx ? parts(dx_stages, L.piece) : 1;
     L.dw_splits = a.dweight ? parts(dw_stages, a.rows) : 1;
+    if (L.grad_edge == 256 && a.dx && a.dweight && L.dw_splits == 1) {
+      const double extra = double(a.rows) * double(a.inner) * 8 / 5.1e6 / 1.43;   // stages
+      const int n = head_parts(dx_tiles, dx_stages, dw_tiles, dw_stages, extra, std::min<int64_t>(64, L.piece / HEAD_BK));
+      if (n > 0) L.dx_splits = n;
+    }
     if (a.dx && (L.pieces > 1 || L.dx_splits > 1)) L.dx = take(size_t(L.dx_splits) * a.rows * a.inner * 4);
     if (L.dw_splits > 1) L.dw = take(size_t(L.dw_splits) * L.piece * a.inner * 4);
   }

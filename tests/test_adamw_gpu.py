@@ -18,7 +18,7 @@ U = 2.0 ** -24
 
 
 @pytest.fixture(scope="module", autouse=True)
-def _gpu():
+def _gpu(stream_rounds):
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
     lm.lib()

@@ -24,7 +24,7 @@ U = 2.0 ** -24
 
 
 @pytest.fixture(scope="module", autouse=True)
-def _gpu():
+def _gpu(stream_rounds):
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
     lm.lib()
@@ -299,6 +299,23 @@ def test_shapes_strides_and_types(ops):
     odd = torch.empty(300 * 64 + 1, device="cuda", dtype=BF16)[1:].view(300, 64).copy_(w)   # not 16-byte aligned
     for a, b in zip(ops.linear_cross_entropy_step(x, odd, y), want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("m", [20, 50])
+def test_broadcast_inputs(ops, m):
+    """Rows, labels and weights of stride 0; the gradients of what was expanded are sums."""
+    x, w, _ = inputs(28, 1, 70, 64, F32, F32)
+    y = torch.tensor([3], device="cuda")
+    full = [t.contiguous() for t in (x.expand(m, 64), w[:1].expand(70, 64), y.expand(m))]
+    for a, b in zip(ops.linear_cross_entropy_step(x.expand(m, 64), w[:1].expand(70, 64), y.expand(m)), ops.linear_cross_entropy_step(*full)):
+        assert torch.equal(a, b)
+    leaf, lw = x.clone().requires_grad_(), w.clone().requires_grad_()
+    dx, dw = torch.autograd.grad(ops.linear_cross_entropy(leaf.expand(m, 64), lw, y.expand(m)).sum(), (leaf, lw))
+    want = ops.linear_cross_entropy_step(full[0], w, full[2])
+    assert torch.equal(dw, want[2]) and torch.equal(dx, want[1].sum(0, keepdim=True))
+    # One row's gradient, m times: exactly m times it in float32 sums of equal terms of at most 2^-24 each.
+    one = ops.linear_cross_entropy_step(x, w, y)
+    assert float((dw - m * one[2]).abs().max()) <= (m + 40) * 2 * U * m * float(one[2].abs().max())
 
 
 def test_gradient_weights(ops):

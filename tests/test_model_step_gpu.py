@@ -10,7 +10,7 @@ F32, BF16 = torch.float32, torch.bfloat16
 
 
 @pytest.fixture(scope="module", autouse=True)
-def _gpu():
+def _gpu(stream_rounds):
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
     from paper_2608_05088_amd import libmalt as lm

@@ -16,7 +16,7 @@ EPS = 1e-5
 
 
 @pytest.fixture(scope="module", autouse=True)
-def _gpu():
+def _gpu(stream_rounds):
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
     lm.lib()

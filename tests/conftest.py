@@ -16,11 +16,19 @@ def pytest_configure(config):
 @pytest.fixture(scope="module")
 def stream_rounds():
     """For a module that takes streams: torch hands them out of a pool in turn, and the card's four hardware queues
-    are behind them in turn, the default stream's among them.  The pool is left where a round starts, so that tests
-    after the module, some of which keep the default stream busy, meet the queues that they would have met without it."""
+    go to them in turn as each is first used, the default stream's among them.  The module leaves whole rounds of used
+    streams, so that tests after it, some of which keep the default stream busy, meet the queues that they would have
+    met without it."""
     yield
     import torch
-    if torch.cuda.is_available():
-        for _ in range(4):
-            if (torch.cuda.Stream().stream_id >> 5) % 4 == 3:
-                break
+    if not torch.cuda.is_available():
+        return
+    for _ in range(4):
+        s = torch.cuda.Stream()
+        if (s.stream_id >> 5) % 4 == 3:
+            break
+    for i in range((s.stream_id >> 5) + 1):
+        with torch.cuda.stream(torch.cuda.Stream(stream_id=s.stream_id & 31 | i << 5, device_index=s.device_index,
+                                                 device_type=s.device_type)):
+            torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()

@@ -684,7 +684,7 @@ void head_grads_kernel(HeadGrads a) {
 
 // The sums of contractions' parts, four columns a thread: one result's, then the other's.  Of many parts
 // a wave takes a quarter each, or few outputs would wait for one load after another (74 x 431, 64 parts: 30 -> 9 us).
-constexpr int SUM_MANY = 16, SUM_WAVES = 4;
+constexpr int SUM_MANY = 8, SUM_WAVES = 4;
 __host__ __device__ inline int sum_quads(const HeadOut& o) { return o.splits >= SUM_MANY ? 64 : 64 * SUM_WAVES; }   // of a workgroup
 template <class T>
 __device__ __forceinline__ void sum4(const HeadOut& o, const HeadGrads& a, int64_t block, op_f32x4 (&join)[SUM_WAVES][64]) {

@@ -384,8 +384,10 @@ __global__ __launch_bounds__(T) void head_join_kernel(HeadJoin a) {
     gptr(a.losses)[r] = loss;
   }
   if (a.stats || a.records) {
-    // The reference is the larger of both: no power of two above 1 is formed.
-    const float t = fmaxf(ref, y), o = sum * exp2f(ref - t), total = o + exp2f(y - t);
+    // The reference is the larger of both: no power of two above 1 is formed.  Where no other column has mass it is the
+    // label's logit itself, however small: 2^(y - 0) would underflow below -149, and the total with it.
+    const bool alone = all == -__builtin_inff();
+    const float t = alone ? y : fmaxf(all, y), o = alone ? sum : sum * exp2f(all - t), total = o + exp2f(y - t);
     const f32x4 v = {t, 1.f / total, o / total, 0.f};
     if (a.stats) *reinterpret_cast<MALT_GLOBAL f32x4*>(gptr(reinterpret_cast<float*>(a.stats + r))) = v;
     if (a.records) write_record(a.rows, r, true, label, v, a.records);

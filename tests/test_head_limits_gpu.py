@@ -1,0 +1,72 @@
+"""The head's loss where its numbers run out: rows in which the label alone has mass, operands of
+unlike magnitude, weights of zero beside rows that hold no numbers."""
+import math
+
+import pytest
+import torch
+
+from paper_2608_05088_amd import libmalt as lm
+
+pytestmark = pytest.mark.gpu
+F32, BF16, I64 = torch.float32, torch.bfloat16, torch.int64
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    lm.lib()
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2608_05088_amd import ops as module
+    return module
+
+
+# ------------------------------------------------------------ the label alone
+# Natural logarithms: where 2^z is a subnormal number, where it is zero, far from either.
+ALONE = (200.0, 3.0, -3.0, -86.0, -89.0, -100.0, -104.0, -110.0, -200.0, -1e4, -1e20)
+
+
+def _nothing(ops, x, w, y):
+    """Loss and gradients are zeros: with probability 1 for the label d = 0, and a product with zero is zero."""
+    losses, dx, dw = ops.linear_cross_entropy_step(x, w, y)
+    lx, lw = x.clone().requires_grad_(), w.clone().requires_grad_()
+    out = ops.linear_cross_entropy(lx, lw, y)
+    for t in (losses, dx, dw, out.detach(), *torch.autograd.grad(out.sum(), (lx, lw))):
+        assert bool((t == 0).all()), t.flatten()[:8]
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("m", [11, 300])
+def test_a_vocabulary_of_one(ops, m, t):
+    z = torch.tensor(ALONE, device="cuda").repeat(28)[:m]
+    x = torch.zeros((m, 5), device="cuda")
+    x[:, 2] = z
+    w = torch.zeros((1, 5), device="cuda")
+    w[0, 2] = 1.0
+    _nothing(ops, x.to(t), w.to(t), torch.zeros(m, dtype=I64, device="cuda"))
+
+
+@pytest.mark.parametrize("t,far", [(F32, -2.0 ** 110), (BF16, -2.0 ** 110), (F32, -math.inf)])
+@pytest.mark.parametrize("m", [11, 300])
+def test_all_other_logits_are_infinite(ops, m, t, far):
+    """Logits below -2^100 count as -inf.  (A bfloat16 weight of -inf itself is a factor of dx: 0 times it is no number.)"""
+    z = torch.tensor(ALONE, device="cuda").repeat(28)[:m]
+    x = torch.zeros((m, 64), device="cuda")
+    x[:, 0], x[:, 1] = 1.0, z
+    w = torch.zeros((300, 64), device="cuda")
+    w[:, 0] = far
+    w[7, 0], w[7, 1] = 0.0, 1.0
+    y = torch.full((m,), 7, device="cuda")
+    y[::5] = -100
+    _nothing(ops, x.to(t), w.to(t), y)
+
+
+@pytest.mark.parametrize("m", [11, 300])
+def test_a_row_without_a_finite_logit_is_no_number(ops, m):
+    x = torch.ones((m, 8), device="cuda")
+    w = torch.full((40, 8), -2.0 ** 110, device="cuda")
+    losses, dx, _ = ops.linear_cross_entropy_step(x, w, torch.zeros(m, dtype=I64, device="cuda"))
+    assert bool(losses.isnan().all()) and bool(dx.isnan().all())

@@ -52,7 +52,11 @@ def test_a_vocabulary_of_one(ops, m, t):
 @pytest.mark.parametrize("t,far", [(F32, -2.0 ** 110), (BF16, -2.0 ** 110), (F32, -math.inf)])
 @pytest.mark.parametrize("m", [11, 300])
 def test_all_other_logits_are_infinite(ops, m, t, far):
-    """Logits below -2^100 count as -inf.  (A bfloat16 weight of -inf itself is a factor of dx: 0 times it is no number.)"""
+    """Logits below -2^100 count as -inf.  (A bfloat16 weight of -inf itself is a factor of dx: 0 times it is no number.)
+
+    Logits of float32 hold a row's values to 2^-39 of its largest: beside -1e20 a 1 is nothing, so in the rows that hold
+    these two the other logits are 0 and the label's, -1e20, has no mass.  Up to 32 rows there is no such row with a
+    label here.  All else is zero, exactly."""
     z = torch.tensor(ALONE, device="cuda").repeat(28)[:m]
     x = torch.zeros((m, 64), device="cuda")
     x[:, 0], x[:, 1] = 1.0, z
@@ -61,7 +65,18 @@ def test_all_other_logits_are_infinite(ops, m, t, far):
     w[7, 0], w[7, 1] = 0.0, 1.0
     y = torch.full((m,), 7, device="cuda")
     y[::5] = -100
-    _nothing(ops, x.to(t), w.to(t), y)
+    lost = (z < -2.0 ** 39) & (y == 7) & (t == F32)
+    if not bool(lost.any()):
+        return _nothing(ops, x.to(t), w.to(t), y)
+    n = int(lost.sum())
+    big = max(far, -(2.0 - 2.0 ** -7) * 2.0 ** 127)   # an infinity is the largest number there
+    want_dx, want_dw = torch.zeros((m, 64), dtype=torch.float64, device="cuda"), torch.zeros((300, 64), dtype=torch.float64, device="cuda")
+    want_dx[lost, 0], want_dx[lost, 1] = big, -1.0    # the others' mean, less the label's row
+    want_dw[:, 0], want_dw[:, 1] = n / 299, n * -1e20 / 299
+    want_dw[7, 0], want_dw[7, 1] = -n, n * 1e20
+    # Logits of 22 bits, probabilities and sums of float32: (299 + 300) 2^-24 of themselves and 2^-20 more.
+    for got, want in zip(ops.linear_cross_entropy_step(x, w, y), (1e20 * lost.double(), want_dx, want_dw)):
+        assert bool(((got.double() - want).abs() <= 2.0 ** -14 * want.abs()).all())
 
 
 @pytest.mark.parametrize("m", [11, 300])

@@ -297,18 +297,29 @@ __device__ __forceinline__ op_u32x2 turn_quad(uint2 v, uint32_t pick, bool low) 
   return op_u32x2{low ? a : got, low ? got : b};
 }
 
-// The scales of this lane's columns into its logits.
+// A power of two's exponent.
+__device__ __forceinline__ int exponent_of(float scale) { return (int)(__float_as_uint(scale) >> 23) - 127; }
+
+// The scales of rows (in LDS, `scales` of this lane's first) and of this lane's columns into its logits: exponents are added
+// before they are applied.  Two products, one after the other, would pass through infinity or lose bits below the
+// smallest normal number where a large row meets a small one.
 template <int NA, int NB>
-__device__ __forceinline__ void scale_columns(const float* scales, int c, int g, f32x4 (&acc)[NA][NB]) {
-  f32x4 w[NA];
+__device__ __forceinline__ void scale_logits(const float* columns, int c, int g, const float* scales, f32x4 (&acc)[NA][NB]) {
+  i32x4 w[NA];
 #pragma unroll
-  for (int i = 0; i < NA; ++i) w[i] = *reinterpret_cast<const MALT_GLOBAL f32x4*>(gptr(scales) + c + 16 * i + 4 * g);
+  for (int i = 0; i < NA; ++i) {
+    const f32x4 s = *reinterpret_cast<const MALT_GLOBAL f32x4*>(gptr(columns) + c + 16 * i + 4 * g);
 #pragma unroll
-  for (int i = 0; i < NA; ++i)
+    for (int e = 0; e < 4; ++e) w[i][e] = exponent_of(s[e]);
+  }
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+  for (int b = 0; b < NB; ++b) {
+    const int x = exponent_of(scales[16 * b]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][b][e] *= w[i][e];
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][b][e] = __builtin_amdgcn_ldexpf(acc[i][b][e], w[i][e] + x);
+  }
 }
 
 // All waves are done with what they read of LDS.
@@ -370,12 +381,11 @@ void head_first_kernel(HeadLogits a) {
     const int c = (int)col0 + wc * TN, left = a.g.n - c - 4 * g;   // columns there are from this lane's first
     const bool end = a.g.n - c < TN;
     const int rows = a.g.m - (int)row0 - wr * TM;   // this wave's
-    if constexpr (HALVES) scale_columns(a.w_scales, c, g, acc);
+    if constexpr (HALVES) scale_logits(a.w_scales, c, g, scales + turn * E + wr * TM + (lane & 15), acc);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       if (b % 4 == 0 && 16 * b >= rows) break;
       const int ml = wr * TM + b * 16 + (lane & 15), yl = labels[turn * E + ml] - c;   // the label's place in the wave's columns
-      const float unit = HALVES ? scales[turn * E + ml] * LOG2E : LOG2E;
       if (__builtin_amdgcn_ballot_w64((unsigned)yl < TN)) {   // few waves meet a label
         float z = 0.f;
 #pragma unroll
@@ -386,7 +396,7 @@ void head_first_kernel(HeadLogits a) {
             z = label ? acc[i][b][e] : z;
             acc[i][b][e] = label ? -__builtin_inff() : acc[i][b][e];
           }
-        if ((unsigned)yl < TN && ((yl >> 2) & 3) == g) gptr(a.at_label)[row0 + ml] = z * unit;
+        if ((unsigned)yl < TN && ((yl >> 2) & 3) == g) gptr(a.at_label)[row0 + ml] = z * LOG2E;
       }
       if (end) {
 #pragma unroll
@@ -399,13 +409,13 @@ void head_first_kernel(HeadLogits a) {
       for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[i][b][e]);
-      top = across(top, [](float a, float b) { return fmaxf(a, b); }) * unit;
+      top = across(top, [](float a, float b) { return fmaxf(a, b); }) * LOG2E;
       const float ref = top == -__builtin_inff() ? 0.f : top;
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < NA; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], unit, -ref));
+        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], LOG2E, -ref));
       sum = across(sum, [](float a, float b) { return a + b; });
       if (g == 0) join[ml * (NW / 2) + wc] = malt_f32x2{top, sum};
     }
@@ -476,19 +486,18 @@ void head_second_kernel(HeadLogits a) {
     const bool end = a.g.n - c < TN;
     // This wave's rows, to the end of the last stage that the gradients read.
     const int rows = (a.g.m - tile_m * E + BK - 1) / BK * BK - wr * TM;
-    if constexpr (HALVES) scale_columns(a.w_scales, c, g, acc);
+    if constexpr (HALVES) scale_logits(a.w_scales, c, g, scales + turn * E + wr * TM + (lane & 15), acc);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       if (b % 4 == 0 && 16 * b >= rows) break;
       const int ml = wr * TM + b * 16 + (lane & 15);
       const f32x4 s = records[turn * E + ml];
-      const float unit = HALVES ? scales[turn * E + ml] * LOG2E : LOG2E;
       const int y = __float_as_int(s.w), yl = y < 0 ? -1 : y - (int)a.col0 - c;
 #pragma unroll
       for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          acc[i][b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], unit, -s.x)) * s.y;
+          acc[i][b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][e], LOG2E, -s.x)) * s.y;
       if (__builtin_amdgcn_ballot_w64((unsigned)yl < TN)) {
 #pragma unroll
         for (int i = 0; i < NA; ++i)

@@ -85,3 +85,35 @@ def test_a_row_without_a_finite_logit_is_no_number(ops, m):
     w = torch.full((40, 8), -2.0 ** 110, device="cuda")
     losses, dx, _ = ops.linear_cross_entropy_step(x, w, torch.zeros(m, dtype=I64, device="cuda"))
     assert bool(losses.isnan().all()) and bool(dx.isnan().all())
+
+
+# ------------------------------------------------------ operands of unlike magnitude
+@pytest.mark.parametrize("xt", [F32, BF16])
+@pytest.mark.parametrize("p", [112, -112])
+@pytest.mark.parametrize("m", [20, 300])
+def test_large_rows_beside_small_ones(ops, m, p, xt):
+    """x 2^-p and weight 2^p have the logits of x and weight, of a size that float32 holds; their scales, taken
+    one after the other, would pass its range.  Losses have the same bits: powers of two are exact.
+    The gradients are those of x and weight times 2^p and 2^-p.  Of those near 2^-112 the planes, the products and their
+    sums may lie below float32's smallest normal number and be taken as zero, off by less than 2^-126 each: for each of n
+    terms three planes (times |d| <= 1), six products and six additions, and the result: 16 n 2^-126 at most.  Beside
+    that float32's sums are off by n + 8 roundings of the terms' sizes, and three products below 2^-24 are left out."""
+    v, k = 257, 65
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m + p)
+    w = torch.randn((v, k), device="cuda", generator=g)
+    y = torch.randint(0, v, (m,), device="cuda", generator=g)
+    x = (torch.randn((m, k), device="cuda", generator=g) + w[y]).to(xt)
+    want = ops.linear_cross_entropy_step(x, w, y)
+    got = ops.linear_cross_entropy_step(x * 2.0 ** -p, w * 2.0 ** p, y)
+    assert torch.equal(got[0], want[0])
+    z = x.double() @ w.double().t()
+    d = torch.softmax(z, 1)
+    d[torch.arange(m, device="cuda"), y] -= 1.0
+    u = 2.0 ** -24
+    for i, (a, b, power, n) in enumerate(((d, w, p, v), (d.t(), x, -p, m))):
+        one, two = want[1 + i].double(), got[1 + i].double() * 2.0 ** -power
+        size = a.abs() @ b.double().abs()
+        lost = 16 * n * 2.0 ** (-126 - power)
+        tol = 2 * (n + 16) * u * size + lost + (2 * torch.finfo(want[1 + i].dtype).eps / 2 * one.abs() * 1.01) + 1e-38
+        assert bool(((two - one).abs() <= tol).all()), (i, float(((two - one).abs() / tol).max()))

@@ -476,9 +476,19 @@ malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, in
  * weights: float32, one every weight_stride elements (0: one for all rows), or NULL for the
  * scalar weight_value.
  * workspace: device memory of malt_linear_loss_size's bytes for the same arguments, 256-byte
- * aligned, of no meaning before or after the call.  It holds d for a piece of the vocabulary at a
- * time, at most 512 MiB (a tile's 256 columns at the least), x and, where it is float32
- * or not laid out for whole 16-byte loads, the weight in bfloat16.
+ * aligned, of no meaning before or after the call.  It holds
+ *  - 8 bytes for each row and 256 columns of the vocabulary (128 for small problems, 64 or 16 up to 32 rows);
+ *  - but for the losses of up to 32 rows: x in 2 bytes a value (4 if float32), and the weight in as
+ *    many where x or it is float32, or where its rows are no whole 16-byte loads;
+ *  - for dx d, and for dweight d transposed, of a piece of the vocabulary at a time: 2 bytes a value if the
+ *    gradient is bfloat16 (4 below 2^32 products), 6 if it is float32 (the larger for both), each of
+ *    the two at most 512 MiB, or 256 columns;
+ *  - for dx the weight transposed, 2 bytes a value, 6 if both are float32 (4 if it alone is), by pieces too where it
+ *    is more than 512 MiB; for dweight x transposed in as many;
+ *  - dx in float32 where there are several pieces, and parts of the gradients' sums in
+ *    float32, 128 MiB for either at the most.
+ * That is little beside the logits and their gradient for a long batch and much for a short one: 8192 x 50257 x 1280 in
+ * bfloat16 takes 1.1 GB (float32 logits 1.6, and as much again for their gradient), 1001 x 50257 x 901 in float32 1.2 (0.2).
  * Limits: rows <= 65536, 1 <= inner <= 65536, 1 <= vocab <= 2^22, vocab * inner <= 2^33,
  * rows * vocab <= 2^38 (both rounded up to 256). */
 typedef struct {

@@ -81,7 +81,7 @@ malt_status_t adam_launches(AdamArgs& a, int count, const int64_t* numel, Fill&&
 
 // ------------------------------------------------------------------------- head
 constexpr int64_t kHeadRows = 65536, kHeadInner = 65536, kHeadVocab = int64_t(1) << 22, kHeadWeight = int64_t(1) << 33;
-constexpr int64_t kHeadPiece = int64_t(1) << 28;   // elements of a piece's dz, all planes
+constexpr int64_t kHeadPiece = int64_t(1) << 28;   // elements of a piece's dz, of its transpose and of W^T's piece, all planes
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
@@ -92,9 +92,10 @@ struct HeadPlan {
   int x_halves, w_halves;
   bool pack_w;           // otherwise the products read the weights as they lie
   int dz_planes, dx_z, dx_w, dw_z, dw_x;   // bf16 planes of the gradients' products
-  int64_t rows_pad, cols_pad, vocab_pad;
+  int64_t rows_pad, cols_pad;
   int64_t piece;         // vocabulary columns of a piece, a multiple of the tile
   int pieces;
+  bool turn_pieces;      // W^T is packed by pieces, in one place
   int first_edge, second_edge, grad_edge;   // of the tiles
   int parts;             // of a row's statistics
   int dx_splits, dw_splits;   // parts of the gradients' contractions
@@ -195,9 +196,14 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     }
   }
   if (L.grads) {
-    // Pieces of like size, as few as keep dz within its share of memory.
-    const int64_t all = up(a.vocab, HEAD_TILE);
-    int64_t most = L.rows_pad > 0 ? kHeadPiece / (L.rows_pad * L.dz_planes) / HEAD_TILE * HEAD_TILE : all;
+    // Pieces of like size, as few as keep dz and W^T within their shares of memory.  Half the share would be 7% slower (8192 x
+    // 50257 x 1280 in bf16: 3890 -> 4150 us a step in twice the pieces, 1024 x 131072 x 2048 in float32 8650 -> 9620).
+    // W^T is packed at once where all of it is within its share (a launch for each piece: 3890 -> 3930), by pieces otherwise
+    // (1024 x 131072 x 2048 in float32: 3.6 -> 2.0 GB of workspace, 8650 -> 8710 us).
+    const int64_t all = up(a.vocab, HEAD_TILE), across_w = a.dx ? up(a.inner, HEAD_TILE) * L.dx_w : 0;
+    L.turn_pieces = across_w * all > kHeadPiece;
+    const int64_t column = std::max(L.rows_pad * L.dz_planes, L.turn_pieces ? across_w : 0);   // elements
+    int64_t most = L.rows_pad > 0 ? kHeadPiece / column / HEAD_TILE * HEAD_TILE : all;
     if (most < HEAD_TILE) most = HEAD_TILE;
     const int64_t pieces = (all + most - 1) / most;
     L.piece = up((all + pieces - 1) / pieces, HEAD_TILE);
@@ -206,9 +212,8 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     if (pieces > 1 && up(L.piece, whole) <= most) L.piece = up(L.piece, whole);
     L.pieces = int((all + L.piece - 1) / L.piece);
     L.records = take(size_t(L.rows_pad) * sizeof(HeadRow));
-    L.vocab_pad = L.piece * L.pieces;
     if (a.dx) {
-      L.w_t = take(size_t(L.dx_w) * up(a.inner, HEAD_TILE) * L.vocab_pad * 2);
+      L.w_t = take(size_t(across_w) * (L.turn_pieces ? L.piece : L.piece * L.pieces) * 2);
       L.dz = take(size_t(L.dz_planes) * L.rows_pad * L.piece * 2);
     }
     if (a.dweight) {
@@ -586,8 +591,10 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       wside = packed_side(prepare.part[2].out, up(a.vocab, HEAD_TILE), L.cols_pad);
     }
     if (want_dx) {
-      prepare.part[3] = turned(w, L.w_t, L.vocab_pad, L.dx_w);
-      w_t = packed_side(prepare.part[3].out, up(a.inner, HEAD_TILE), L.vocab_pad);
+      const int64_t cols = L.turn_pieces ? L.piece : L.piece * L.pieces;
+      prepare.part[3] = turned(w, L.w_t, cols, L.dx_w);
+      prepare.part[3].rows = std::min(cols, a.vocab);
+      w_t = packed_side(prepare.part[3].out, up(a.inner, HEAD_TILE), cols);
       w_t.rows = a.inner;
     }
     MALT_TRY(launched(launch_head_prepare(prepare, f32x, f32w, s), "packing the head's operands"));
@@ -650,6 +657,13 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
   uint16_t *const dz = reinterpret_cast<uint16_t*>(ws + L.dz), *const dz_t = reinterpret_cast<uint16_t*>(ws + L.dz_t);
   for (int p = 0; p < L.pieces; ++p) {
     const int64_t v0 = p * L.piece, n = a.vocab - v0 < L.piece ? a.vocab - v0 : L.piece;
+    if (want_dx && L.turn_pieces && p > 0) {
+      HeadPrepare next = {};
+      next.part[3] = prepare.part[3];
+      next.part[3].x = static_cast<const char*>(a.weight) + size_t(v0) * a.ldw * w.elem();
+      next.part[3].rows = n;
+      MALT_TRY(launched(launch_head_prepare(next, f32x, f32w, s), "packing a piece of the head's weight"));
+    }
     if (a.rows > 0) {
       HeadLogits second = z;
       second.g.b.p += v0 / HEAD_TILE * wside.tile;
@@ -673,7 +687,7 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       o = HeadOut{};
       o.g.a = packed_side(dz, L.rows_pad, L.piece);
       o.g.b = w_t;
-      o.g.b.p += v0 / HEAD_BK * HEAD_BLOCK;
+      if (!L.turn_pieces) o.g.b.p += v0 / HEAD_BK * HEAD_BLOCK;
       o.g.m = (int32_t)a.rows;
       o.g.n = (int32_t)a.inner;
       o.g.k = n;

@@ -117,3 +117,19 @@ def test_large_rows_beside_small_ones(ops, m, p, xt):
         lost = 16 * n * 2.0 ** (-126 - power)
         tol = 2 * (n + 16) * u * size + lost + (2 * torch.finfo(want[1 + i].dtype).eps / 2 * one.abs() * 1.01) + 1e-38
         assert bool(((two - one).abs() <= tol).all()), (i, float(((two - one).abs() / tol).max()))
+
+
+# ------------------------------------------------------- the weight turned by pieces
+@pytest.mark.parametrize("m,v,k,xt,wt,pitch", [(40, 90000, 1024, F32, F32, 0), (33, 131001, 2000, F32, F32, 0), (300, 140003, 1029, BF16, F32, 3),
+                                               (20, 300001, 1000, BF16, BF16, 1)])
+def test_large_weights_are_turned_by_pieces(ops, m, v, k, xt, wt, pitch):
+    """Where the transposed weight passes its share of memory it is packed again for each piece of the vocabulary: two
+    pieces, four with a short last one, two of a pitched weight in two planes; two of one plane."""
+    from test_head_gpu import Exact, inputs
+    x, w, y = inputs(m + v, m, v, k, xt, wt)
+    if pitch:
+        big = torch.full((v, k + pitch), float("nan"), device="cuda", dtype=wt)
+        big[:, :k] = w
+        w = big[:, :k]
+    y[0], y[1] = v - 1, 0
+    Exact(x, w, y).check(*ops.linear_cross_entropy_step(x, w, y))

@@ -528,7 +528,8 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
  *    scales of m [blocks] (float32), scales of v.  A moment is its code's value times its
  *    block's scale.  m's codes: sign, 4 exponent bits (bias 7), 3 mantissa bits; v's: 5 exponent bits (bias 15),
  *    3 mantissa bits, no sign.  Scales are the block's largest magnitude times 1/448 and 1/61440
- *    (0 for a block below 2^-100, not a number where the block holds an infinity or a NaN).  A magnitude x =
+ *    (0 for a block below 2^-100, and for m's where v's is 0: m / eps would be a step of any size; not a
+ *    number where the block holds an infinity or a NaN).  A magnitude x =
  *    |m| (1 / largest) 448 between two neighbours a step apart becomes floor(x / step + u) step, a
  *    v above zero at least one step.  u in (0, 1) is a hash of seed, the tensor's place in the
  *    call, the block and the element's place in it: equal calls give equal bits, and another seed for each

@@ -18,9 +18,10 @@
 //   first moment: sign, 4 exponent bits, 3 mantissa bits up to 448, s = max|m| / 448: 2^-18
 //     of the largest is kept;
 //   second: no sign, 5 exponent bits, 3 mantissa bits up to 61440 (a float16's bits shifted by
-//     7), s = max v / 61440: 2^-33 of the largest.  A second moment above zero never becomes
-//     zero: where m outlives v the update would be m / eps.  What m can keep below that
-//     (2^-18 of the largest, over the root of 2^-33) is an update of ordinary size.
+//     7), s = max v / 61440: 2^-33 of the largest.  A second moment above zero becomes zero only
+//     with its whole block, and then the first moments go with it: where m outlives v the update
+//     would be m / eps.  What m can keep otherwise (2^-18 of the largest, over the root of
+//     2^-33) is an update of ordinary size.
 // The step itself takes the moments before they are rounded.  Moments and codes are computed
 // one rounding at a time (no fused multiply-add): the same bits on every machine.
 #include "adamw.h"
@@ -32,7 +33,7 @@ namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr float FIRST_MAX = 448.f, SECOND_MAX = 61440.f;
-constexpr float LEAST = 0x1p-100f;   // a block whose largest is below is zero: its reciprocal times 61440 has to be a number
+constexpr float LEAST = 0x1p-100f;   // moments of a block whose largest is below are zero: its reciprocal times 61440 has to be a number
 
 __device__ __forceinline__ uint32_t mixed(uint32_t x) {
   // Shifts, and products with odd numbers from the digits of the golden ratio and of the root of 3.
@@ -227,7 +228,9 @@ __device__ __forceinline__ void step8(const AdamArgs& a, const AdamTensor& t, in
       uv[j] = __builtin_fmaf((float)(r >> 16), 0x1p-16f, 0x1p-17f);
     }
     float im, iv;
-    const float nm = block_scale(wave_max(tm), FIRST_MAX, &im), nv = block_scale(wave_max(tv), SECOND_MAX, &iv);
+    const float nv = block_scale(wave_max(tv), SECOND_MAX, &iv);
+    float nm = block_scale(wave_max(tm), FIRST_MAX, &im);
+    if (nv == 0.f && nm > 0.f) nm = 0.f;
     *reinterpret_cast<MALT_GLOBAL uint32_t*>(gptr(mc) + c) = nm > 0.f ? first_codes(m, im, um) : 0u;
     *reinterpret_cast<MALT_GLOBAL uint32_t*>(gptr(vc) + c) = nv > 0.f ? second_codes(v, iv, uv) : 0u;
     if (lane == 0) {

@@ -61,6 +61,10 @@ class AdamW(torch.optim.Optimizer):
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay))
         self.bits, self.min_8bit, self.seed = bits, min_8bit, seed
 
+    def __getstate__(self):
+        # torch's keeps the defaults, the state and the groups: copies and pickles would lack the rest.
+        return {**super().__getstate__(), "bits": self.bits, "min_8bit": self.min_8bit, "seed": self.seed}
+
     @torch.no_grad()
     def step(self, closure=None):
         from . import ops

@@ -96,14 +96,39 @@ class AdamW(torch.optim.Optimizer):
                     self.state[p]["step"] = t
         return loss
 
-    def load_state_dict(self, state_dict: Dict) -> None:
-        super().load_state_dict(state_dict)
-        # Moments keep the type they were saved in, whatever the parameter's.
+    def _loaded(self, state_dict: Dict) -> List[Tuple[torch.Tensor, dict]]:
+        """The state's entries by parameter; ValueError where one is no state of this optimizer for it."""
         ids = itertools.chain.from_iterable(g["params"] for g in state_dict["param_groups"])
+        entries = []
         for i, p in zip(ids, itertools.chain.from_iterable(g["params"] for g in self.param_groups)):
-            if i in state_dict["state"]:
-                st = state_dict["state"][i]
-                self.state[p] = {"step": int(st["step"]), "moments": st["moments"].detach().clone().to(p.device)}
+            st = state_dict["state"].get(i)
+            if not st:
+                continue
+            if set(st) != {"step", "moments"}:
+                raise ValueError(f"parameter {i}: {sorted(st)} are not the step and moments of this AdamW")
+            try:
+                step = int(st["step"])
+            except (TypeError, ValueError):
+                step = -1
+            if step < 0:
+                raise ValueError(f"parameter {i}: the step is {st['step']}")
+            m, n = st["moments"], p.numel()
+            # 8 bits: two codes for each place of whole blocks of 256, and two scales for each block.
+            shape = {torch.float32: (2, n), torch.uint8: (-(-n // 256) * 520,)}
+            if not isinstance(m, torch.Tensor) or tuple(m.shape) != shape.get(m.dtype):
+                raise ValueError(f"parameter {i} of {n} elements: moments must be float32 {shape[torch.float32]} or uint8 "
+                                 f"{shape[torch.uint8]} (got {f'{m.dtype} {tuple(m.shape)}' if isinstance(m, torch.Tensor) else type(m).__name__})")
+            entries.append((p, {"step": step, "moments": m}))
+        return entries
+
+    def load_state_dict(self, state_dict: Dict) -> None:
+        """Takes a state of this class over, or raises ValueError and leaves everything as it was."""
+        entries = self._loaded(state_dict)
+        super().load_state_dict(state_dict)   # refuses other groups than these
+        # Moments keep the type they were saved in, whatever the parameter's.
+        for p, st in entries:
+            m = st["moments"].detach().to(p.device).clone(memory_format=torch.contiguous_format)
+            self.state[p] = {"step": st["step"], "moments": m}
 
 
 class MALT(torch.optim.Optimizer):
@@ -222,14 +247,18 @@ class MALT(torch.optim.Optimizer):
         for k, pl in enumerate(sd["plans"]):
             if pl is not None and [tuple(s) for s in pl["shapes"]] != [tuple(p.shape) for p in self._mats[k]]:
                 raise ValueError(f"group {k}: matrix shapes differ from the saved state")
+        # The other parameters first: what does not fit there raises, and nothing has changed.
+        if self._adam is not None and sd.get("adamw") is not None:
+            if not isinstance(self._adam, AdamW) and any("moments" in st for st in sd["adamw"]["state"].values()):
+                raise ValueError("the state was saved with adamw_bits: it is not one of torch's AdamW")
+            self._adam.load_state_dict(sd["adamw"])
+        for k, pl in enumerate(sd["plans"]):
             if self._plans[k] is not None:
                 self._plans[k].close()
                 self._plans[k] = None
             self._resume[k] = pl
         for g, s in zip(self.param_groups, sd["groups"]):
             g.update(s)
-        if self._adam is not None and sd.get("adamw") is not None:
-            self._adam.load_state_dict(sd["adamw"])
 
     @torch.no_grad()
     def precond_condition(self) -> Dict[torch.Tensor, Tuple[float, float]]:

@@ -59,7 +59,7 @@ class AdamW(torch.optim.Optimizer):
         if not 0 <= seed < 1 << 32:
             raise ValueError(f"seed must be in [0, 2^32) (got {seed})")
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay))
-        self.bits, self.min_8bit, self.seed = bits, min_8bit, seed
+        self.bits, self.min_8bit, self.seed = bits, min_8bit, int(seed)
 
     def __getstate__(self):
         # torch's keeps the defaults, the state and the groups: copies and pickles would lack the rest.
@@ -96,6 +96,9 @@ class AdamW(torch.optim.Optimizer):
                     self.state[p]["step"] = t
         return loss
 
+    def state_dict(self) -> Dict:
+        return {**super().state_dict(), "seed": self.seed}
+
     def _loaded(self, state_dict: Dict) -> List[Tuple[torch.Tensor, dict]]:
         """The state's entries by parameter; ValueError where one is no state of this optimizer for it."""
         ids = itertools.chain.from_iterable(g["params"] for g in state_dict["param_groups"])
@@ -122,9 +125,13 @@ class AdamW(torch.optim.Optimizer):
         return entries
 
     def load_state_dict(self, state_dict: Dict) -> None:
-        """Takes a state of this class over, or raises ValueError and leaves everything as it was."""
+        """Takes a state of this class over, its seed too, or raises ValueError and leaves everything as it was."""
         entries = self._loaded(state_dict)
+        seed = state_dict.get("seed", self.seed)
+        if not isinstance(seed, int) or not 0 <= seed < 1 << 32:
+            raise ValueError(f"the state's seed must be in [0, 2^32) (got {seed})")
         super().load_state_dict(state_dict)   # refuses other groups than these
+        self.seed = seed
         # Moments keep the type they were saved in, whatever the parameter's.
         for p, st in entries:
             m = st["moments"].detach().to(p.device).clone(memory_format=torch.contiguous_format)

@@ -163,3 +163,26 @@ def test_a_later_group_that_does_not_fit_leaves_the_earlier_ones():
     with pytest.raises(ValueError, match="group 1"):
         opt.load_state_dict(other.state_dict())
     assert all(a is b for a, b in zip(opt._resume, before))
+
+
+@pytest.mark.parametrize("own", [0, 7])
+def test_a_resumed_run_rounds_as_the_first(steps, own, tmp_path):
+    """The seed is part of what is saved; a state without one leaves the optimizer's own."""
+    opt, ps = adamw(bits=8, seed=7)
+    opt.step()
+    torch.save(opt.state_dict(), tmp_path / "o.pt")
+    saved = torch.load(tmp_path / "o.pt", weights_only=True)
+    other, qs = adamw(bits=8, seed=own)
+    other.load_state_dict(saved)
+    steps.clear()
+    opt.step(), other.step()
+    assert steps[0] == steps[1] and steps[0]["seed"] >> 32 == 7
+    third, rs = adamw(bits=8, seed=3)
+    third.load_state_dict({k: v for k, v in saved.items() if k in ("state", "param_groups")})
+    assert third.seed == 3 and third.state[rs[0]]["step"] == 1
+    for bad in (-1, 1 << 32, None, 0.5):
+        before = _snapshot(third, rs)
+        with pytest.raises(ValueError, match="seed"):
+            third.load_state_dict({**saved, "seed": bad})
+        _unchanged(third, rs, before)
+        assert third.seed == 3

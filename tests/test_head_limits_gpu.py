@@ -133,3 +133,34 @@ def test_large_weights_are_turned_by_pieces(ops, m, v, k, xt, wt, pitch):
         w = big[:, :k]
     y[0], y[1] = v - 1, 0
     Exact(x, w, y).check(*ops.linear_cross_entropy_step(x, w, y))
+
+
+# ------------------------------------------------------------------ weights, sums
+@pytest.mark.parametrize("zero", [0.0, "device"])
+@pytest.mark.parametrize("m", [20, 100])
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_a_weight_of_zero_leaves_nothing(ops, m, t, zero):
+    """One weight for all rows, rows that hold no numbers among them: every gradient is zero."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m)
+    x = torch.randn((m, 64), device="cuda", generator=g).to(t)
+    w = torch.randn((300, 64), device="cuda", generator=g).to(t)
+    y = torch.randint(0, 300, (m,), device="cuda", generator=g)
+    x[6] = float("nan")
+    losses, dx, dw = ops.linear_cross_entropy_step(x, w, y, grad=torch.zeros((), device="cuda") if zero == "device" else zero)
+    assert bool(losses[6].isnan()) and bool(losses[:6].isfinite().all())
+    assert bool((dx == 0).all()) and bool((dw == 0).all())
+
+
+def test_accumulated_gradients_are_one_sum(ops):
+    """A float32 gradient is added once to what was there: its rounded sum, bit by bit."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    x, w = (torch.randn(s, device="cuda", generator=g).to(BF16) for s in ((300, 128), (700, 128)))
+    y = torch.randint(0, 700, (300,), device="cuda", generator=g)
+    out = torch.empty((700, 128), device="cuda")
+    one = ops.linear_cross_entropy_step(x, w, y, out=out)[2].clone()
+    before = torch.randn((700, 128), device="cuda", generator=g) * 1e-3
+    out.copy_(before)
+    ops.linear_cross_entropy_step(x, w, y, out=out, accumulate=True)
+    assert torch.equal(out, before + one)

@@ -187,7 +187,7 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     L.partial = take(size_t(a.rows) * L.parts * 8);
     L.at_label = take(size_t(a.rows) * 4);
   }
-  if (L.grads || !L.few) {
+  if (a.rows > 0 && (L.grads || !L.few)) {
     L.x = take(size_t(L.x_halves) * L.rows_pad * L.cols_pad * 2);
     if (L.pack_w) L.w = take(size_t(L.w_halves) * up(a.vocab, HEAD_TILE) * L.cols_pad * 2);
     if (L.halves) {
@@ -200,7 +200,7 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     // 50257 x 1280 in bf16: 3890 -> 4150 us a step in twice the pieces, 1024 x 131072 x 2048 in float32 8650 -> 9620).
     // W^T is packed at once where all of it is within its share (a launch for each piece: 3890 -> 3930), by pieces otherwise
     // (1024 x 131072 x 2048 in float32: 3.6 -> 2.0 GB of workspace, 8650 -> 8710 us).
-    const int64_t all = up(a.vocab, HEAD_TILE), across_w = a.dx ? up(a.inner, HEAD_TILE) * L.dx_w : 0;
+    const int64_t all = up(a.vocab, HEAD_TILE), across_w = a.dx && a.rows > 0 ? up(a.inner, HEAD_TILE) * L.dx_w : 0;
     L.turn_pieces = across_w * all > kHeadPiece;
     const int64_t column = std::max(L.rows_pad * L.dz_planes, L.turn_pieces ? across_w : 0);   // elements
     int64_t most = L.rows_pad > 0 ? kHeadPiece / column / HEAD_TILE * HEAD_TILE : all;

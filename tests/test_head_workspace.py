@@ -74,3 +74,9 @@ def test_ordinary_steps_take_less_than_the_logits_and_their_gradient(L):
         assert size(L, m, 50257, k, BF16, BF16, BF16) < 0.6 * 2 * logits
         assert size(L, m, 50257, k, F32, F32, F32) < 2 * logits
         assert size(L, m, 50257, k, BF16, BF16, BF16, False, False) < 0.03 * logits
+
+
+def test_no_rows_take_no_copies_of_the_weight(L):
+    for xt, wt in itertools.product((F32, BF16), repeat=2):
+        for dx, dw in ((True, True), (True, False), (False, True), (False, False)):
+            assert size(L, 0, 131072, 4096, xt, wt, wt, dx, dw) <= 4096

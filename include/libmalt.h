@@ -462,14 +462,17 @@ malt_status_t malt_block_layer_backward(const void* dy, malt_dtype_t dy_type, in
  *  - Logits of -inf have probability zero, and so has a probability below 2^-126; a labelled row without a finite logit is NaN, as are
  *    rows with a NaN or +inf.
  *  - Products of bfloat16 are exact and summed in float32.  Logits of float32 values take 22 bits of
- *    them (two float16 numbers under a power of two for each row, to 2^-39 of the row's largest), or
- *    all 24 for up to 32 rows; a product is off by up to 3 2^-22 of itself before it is summed in float32.
+ *    them (two float16 numbers under a power of two for each row, to 2^-39 of the row's largest); a
+ *    product is off by up to 3 2^-22 of itself before it is summed in float32.  The losses and stats of up to 32 rows
+ *    take all 24 (their gradients' logits 22).
  *    Gradients take float32 values whole, as three bfloat16 numbers; of their nine products the
  *    three smallest, below 2^-24 of the whole each, are left out.  Where x or weight is float32 an
- *    infinite value enters as a number past all others.  Softmax and losses are float32.  1 - q_y is formed from the other
+ *    infinite value enters as a number past all others; into the losses and stats of up to 32 rows as it is
+ *    (0 times it is no number).  Softmax and losses are float32.  1 - q_y is formed from the other
  *    columns' sum.  Gradients of type float32 take d, x and weight whole; bfloat16 ones take
  *    d, x and weight rounded to bfloat16, which puts them off by about as much as their own
- *    rounding.
+ *    rounding.  (Below 2^32 products, and of a float32 partner, two bfloat16 numbers each, so a part of a batch may
+ *    be nearer to the definition than the whole.)
  * losses, dx, dweight may be NULL (not wanted).  stats: rows x 4 float32, 16-byte aligned, what
  * the gradients need of the first pass: written, or, with stats_given, read from an earlier call
  * on the same x, weight and labels (losses is NULL then); NULL: kept in the workspace.

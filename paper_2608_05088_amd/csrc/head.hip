@@ -6,7 +6,8 @@
 //
 // Bound by the matrix cores: 2 M V K operations a product, four products with both gradients.
 // The logits are formed twice because M x V of them in 32 bits would cost as much to write and
-// read (twice 4 bytes a logit) as the K products that make one.
+// read (twice 4 bytes a logit) as the K products that make one.  (Not tried: some rows' logits at a time, kept
+// where the last-level cache holds them.)
 //
 // 8192 x 50257 x 1280 in bf16, 1.05 T operations a product: first pass 950 us (1110 TFLOP/s; the library's
 // product that writes its logits: 939), second 1170 in two pieces, gradients 1700 (1240 TFLOP/s; the library's: 2450).
@@ -28,7 +29,8 @@
 //   logits: two float16 planes under a power of two for each row, 22 bits; three pairs (low by low is
 //     below 2^-22 of the whole, as the planes' own rounding).
 //   gradients: three bf16 planes, all 24 bits; six pairs (middle by low and low by low are below
-//     2^-24).  float16 would not do for dz, whose values have no row or column of like size.
+//     2^-24).  dz has no float16 planes: along a row its values are below the label's, so that dx could take
+//     three pairs under a power of two for each row, but dW's sums run across rows of unlike size.
 // At the matrix cores' 16-bit rate that is three and 1.5 times the float32 instruction's
 // (1001 x 50257 x 901: 324, 425 and 1070 us; in one float32 product each the matrix cores would need 4 x 590).
 // bf16 gradients take one plane of dz, rounded once more, an error of the size of the result's own

@@ -685,8 +685,8 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Te
     x (..., inner) and weight (vocab, inner), float32 of labels' shape.  The logits
     are never held: neither here nor in the backward pass.  A label outside the vocabulary
     (-1, -100) is none: the row's loss is 0, whatever x holds there, and it adds no gradient.
-    Types may differ (float32, bfloat16); of float32 values the logits take 22 bits (24 for up to 32
-    rows), the gradients all.  Differentiable in x and weight; gradients are of their types."""
+    Types may differ (float32, bfloat16); of float32 values the logits take 22 bits (24 for the losses of
+    up to 32 rows), the gradients all.  Differentiable in x and weight; gradients are of their types."""
     for name, t in (("x", x), ("weight", weight)):
         if isinstance(t, torch.Tensor):
             _no_tangent(name, t)

@@ -6,8 +6,7 @@
 //
 // Bound by the matrix cores: 2 M V K operations a product, four products with both gradients.
 // The logits are formed twice because M x V of them in 32 bits would cost as much to write and
-// read (twice 4 bytes a logit) as the K products that make one.  (Not tried: some rows' logits at a time, kept
-// where the last-level cache holds them.)
+// read (twice 4 bytes a logit) as the K products that make one.
 //
 // 8192 x 50257 x 1280 in bf16, 1.05 T operations a product: first pass 950 us (1110 TFLOP/s; the library's
 // product that writes its logits: 939), second 1170 in two pieces, gradients 1700 (1240 TFLOP/s; the library's: 2450).

@@ -213,7 +213,7 @@ HeadPlan head_plan(const malt_linear_loss_t& a) {
     L.pieces = int((all + L.piece - 1) / L.piece);
     L.records = take(size_t(L.rows_pad) * sizeof(HeadRow));
     if (a.dx) {
-      L.w_t = take(size_t(across_w) * (L.turn_pieces ? L.piece : L.piece * L.pieces) * 2);
+      L.w_t = take(size_t(across_w) * (L.turn_pieces ? L.piece : all) * 2);
       L.dz = take(size_t(L.dz_planes) * L.rows_pad * L.piece * 2);
     }
     if (a.dweight) {
@@ -591,7 +591,7 @@ malt_status_t malt_linear_loss(const malt_linear_loss_t* args, void* workspace, 
       wside = packed_side(prepare.part[2].out, up(a.vocab, HEAD_TILE), L.cols_pad);
     }
     if (want_dx) {
-      const int64_t cols = L.turn_pieces ? L.piece : L.piece * L.pieces;
+      const int64_t cols = L.turn_pieces ? L.piece : up(a.vocab, HEAD_TILE);   // the last piece's may end before it does
       prepare.part[3] = turned(w, L.w_t, cols, L.dx_w);
       prepare.part[3].rows = std::min(cols, a.vocab);
       w_t = packed_side(prepare.part[3].out, up(a.inner, HEAD_TILE), cols);

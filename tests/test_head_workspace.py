@@ -48,7 +48,7 @@ def bound(m, v, k, xt, wt, dwt, dx, dw):
     n += (dx + dw) * min(rows * words * d + 256 * rows * d, max(SHARE, 256 * rows * d))
     if dx:
         b = {(F32, F32): 6, (BF16, F32): 4}.get((xt, wt), 2)
-        n += min(wide * words * b * 2, max(SHARE, wide * 256 * b))   # twice: pieces of whole rounds may pass the vocabulary
+        n += min(wide * words * b, max(SHARE, wide * 256 * b))
         n += max(128 << 20, m * k * 4)
     if dw:
         n += wide * rows * {(F32, F32): 6, (F32, BF16): 4}.get((xt, dwt), 2) + (128 << 20)
@@ -57,7 +57,7 @@ def bound(m, v, k, xt, wt, dwt, dx, dw):
 
 SIZES = [(1, 50257, 1280), (20, 50257, 768), (33, 1000, 64), (300, 1000, 129), (1001, 50257, 901), (4096, 50257, 768),
          (8192, 50257, 1280), (1024, 131072, 2048), (4096, 131072, 4096), (65536, 8200, 64), (65536, 100000, 512), (5, 1 << 22, 576),
-         (50, 4000, 16384), (3999, 8190, 1500)]
+         (50, 4000, 16384), (3999, 8190, 1500), (12000, 50257, 5000), (20000, 16600, 14000)]
 
 
 @pytest.mark.parametrize("m,v,k", SIZES)
